@@ -69,6 +69,7 @@ extern "C" {
 #define SQUANT_ERR_TIMEOUT (-10)    /* a kernel gave up a bounded wait on an asynchronous copy; the
                                        outputs of that launch are incomplete */
 #define SQUANT_ERR_CAPTURE (-11)    /* squant_quantize_layer_noalloc on a stream that is being captured */
+#define SQUANT_ERR_WORKSPACE (-12)  /* the workspace is too small or not 16-byte aligned */
 #define SQUANT_ERR_LIMIT (-9)       /* the layer needs more launch-table entries than the fixed
                                        table of squant_quantize_layer_noalloc holds */
 
@@ -233,6 +234,107 @@ int squant_plan_kernels(const squant_layer *layers, int32_t n_layers, const squa
 #define SQUANT_NOALLOC_TABLE_BYTES (256 + 8 * SQUANT_NOALLOC_MAX_CTAS)
 int squant_quantize_layer_noalloc(const squant_layer *layer, const squant_options *opt,
                                   void *cuda_stream);
+
+/*
+ * Linear layers on quantized weights: a layer's codes and scales as squant_quantize_layer writes them (kh = kw = 1)
+ * are multiplied with 16-bit activations.  With C the codes, s the scales, b the bias, r the residual:
+ *
+ *   u = x C^T,  z = s * u + b,  y = act(z) + r
+ *
+ * A code is exact in the activations' type, so the products are exact, their sums are fp32 and the only roundings of a value
+ * are those of fp32 sums and the one of y.  Tokens are rows; strides count elements from one row to the next, so that x,
+ * residual, y and the gradients may be slices of wider buffers.  No alignment is asked of 16-bit tensors beyond their
+ * elements' own; rows that start on 16 bytes (and codes whose rows do) are read faster.
+ *
+ * All pointers are DEVICE pointers.  Calls are asynchronous on `cuda_stream`, allocate nothing (a workspace is the caller's) and
+ * may be captured into a graph; calls on different streams do not share anything but what the caller passes to both.
+ * Arguments are validated on the host first; a failed call launches nothing and writes nothing.
+ */
+#define SQUANT_BF16 0 /* activation types */
+#define SQUANT_FP16 1
+
+#define SQUANT_ACT_NONE 0
+#define SQUANT_ACT_RELU 1
+#define SQUANT_ACT_GELU 2 /* z * (1 + erf(z / sqrt 2)) / 2 */
+#define SQUANT_ACT_SILU 3 /* z / (1 + exp(-z)) */
+
+/*
+ * An activation in 8 bits.  32 consecutive features of a row share a power of two: with a = max|v| over them,
+ * E = max(1, exponent field of a in fp32 - 6) and code = clamp(rint(v * 2^(127-E)), -127, 127), ties to even; the value is
+ * code * 2^(E-127), exact in bf16 and at most half a step 2^(E-127) from v (a step for |v| above 127.5 steps, which
+ * bf16 values never are).  A group with an infinity or a NaN has E = 255 and its values are NaN.  33 bits of 64 of a bf16 tensor.
+ *   codes  [rows][code_pitch] int8, code_pitch = features rounded up to 32; the codes behind the last feature are 0
+ *   exps   [rows][exps_pitch] uint8, exps_pitch = code_pitch / 32
+ * Both start on 16 bytes.
+ */
+typedef struct squant_checkpoint_data {
+    int8_t *codes;
+    uint8_t *exps;
+} squant_checkpoint_data;
+
+/* x [rows][features] bf16 (rows `stride` elements apart) to 8 bits, and back (`out` likewise bf16). */
+int squant_checkpoint(const void *x, int64_t rows, int32_t features, int64_t stride, const squant_checkpoint_data *to, void *cuda_stream);
+int squant_checkpoint_restore(const squant_checkpoint_data *from, int64_t rows, int32_t features, void *out, int64_t stride,
+                              void *cuda_stream);
+
+typedef struct squant_linear_args {
+    int64_t tokens;          /* >= 0 */
+    int32_t cin, cout;
+    uint32_t dtype;          /* of x, residual and y: SQUANT_BF16 or SQUANT_FP16 */
+    uint32_t act;            /* SQUANT_ACT_* */
+    uint32_t flags;          /* SQUANT_FLAG_PACK_INT4: packed codes */
+    const void *x;           /* in : [tokens][cin] */
+    int64_t x_stride;
+    const int8_t *codes;     /* in : [cout][cin], packed: [cout][ceil(cin / 2)] */
+    const float *scales;     /* in : [cout] */
+    const float *bias;       /* in, may be NULL: [cout] */
+    const void *residual;    /* in, may be NULL: [tokens][cout]; may be y itself */
+    int64_t residual_stride;
+    void *y;                 /* out: [tokens][cout]; no other overlap with an input */
+    int64_t y_stride;
+    squant_checkpoint_data z; /* out, codes may be NULL: the pre-activation z in 8 bits, for squant_linear_backward */
+    void *workspace;         /* squant_linear_workspace() bytes, 16-byte aligned; NULL where that is 0 */
+    int64_t workspace_bytes;
+} squant_linear_args;
+
+/* Bytes of workspace the call with these arguments needs (0 unless x has rows that start anywhere), or a negative error. */
+int64_t squant_linear_workspace(const squant_linear_args *args);
+int squant_linear(const squant_linear_args *args, void *cuda_stream);
+
+/*
+ * Gradients of the layer, in bf16 (fp16's range does not hold gradients times scales).  With zhat and xhat the values of the
+ * 8-bit checkpoints of z (written by squant_linear) and of x (by squant_checkpoint):
+ *
+ *   dz = dy * act'(zhat)      (relu: 0 at 0)
+ *   dbias = sum over tokens of dz,  dscales = sum over tokens of dz * (zhat - b) / s
+ *   dx = (dz * s) C,  dweight = dz^T xhat   - the gradient of the weights the codes stand for, which a training loop hands
+ *                                             on to the weights it quantizes
+ *
+ * dz and dz * s are rounded to bf16 for the tensor cores; their sums, dbias and dscales are fp32 and taken before that rounding.
+ * The residual's gradient is dy.  Results repeat to the bit.
+ */
+typedef struct squant_linear_grad_args {
+    int64_t tokens;
+    int32_t cin, cout;
+    uint32_t act, flags;
+    const void *dy;          /* in : [tokens][cout] bf16 */
+    int64_t dy_stride;
+    const int8_t *codes;     /* in : as above; needed for dx */
+    const float *scales;     /* in : needed for dx and dscales */
+    const float *bias;       /* in, may be NULL: of the forward pass; used for dscales */
+    squant_checkpoint_data z; /* in : [tokens][cout]; needed with an activation and for dscales */
+    squant_checkpoint_data x; /* in : [tokens][cin]; needed for dweight */
+    void *dx;                /* out, may be NULL: [tokens][cin] bf16 */
+    int64_t dx_stride;
+    void *dweight;           /* out, may be NULL: [cout][cin] bf16 */
+    int64_t dweight_stride;
+    float *dbias, *dscales;  /* out, may be NULL: [cout] */
+    void *workspace;         /* squant_linear_backward_workspace() bytes, 16-byte aligned */
+    int64_t workspace_bytes;
+} squant_linear_grad_args;
+
+int64_t squant_linear_backward_workspace(const squant_linear_grad_args *args);
+int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_stream);
 
 /*
  * Self-check of the arithmetic shortcut in SQuant-E (Algorithm 1 "Scale and SQuant-E").  The 3x3

@@ -1,0 +1,466 @@
+// Host side of the linear operators: validation, choice of kernels, launches (C ABI of include/squant.h).
+#include "squant.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "linear_device.cuh"
+#include "linear_gemm.cuh"
+#include "linear_rows.cuh"
+#include "linear_small.cuh"
+#include "squant_host.h"
+
+namespace {
+
+constexpr int kMaxDevices = 64;
+constexpr int64_t kMaxRows = 1ll << 30;
+constexpr int kSmallTokens = 32;   // up to as many tokens the forward product goes to small_kernel
+
+#define SQ_CUDA(call)                                                      \
+    do {                                                                   \
+        cudaError_t e__ = (call);                                          \
+        if (e__ != cudaSuccess) return sq_host::cuda_failed(e__, #call);   \
+    } while (0)
+
+inline bool misaligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) & (to - 1); }
+inline int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+// Rows that start on 16 bytes (one row: only its own start counts).
+inline bool rows_on_vectors(const void *p, int64_t stride, int64_t rows) { return !misaligned(p, 16) && (rows <= 1 || stride % 8 == 0); }
+
+int launched()
+{
+    SQ_CUDA(cudaGetLastError());
+    sq_host::count_launch();
+    return SQUANT_OK;
+}
+
+int device_sms(int &device, int &sms)
+{
+    SQ_CUDA(cudaGetDevice(&device));
+    SQ_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    return SQUANT_OK;
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encoder(EncodeTiled &fn)
+{
+    static std::atomic<void *> cached{nullptr};
+    void *p = cached.load(std::memory_order_acquire);
+    if (!p) {
+        cudaDriverEntryPointQueryResult found;
+        SQ_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found));
+        if (found != cudaDriverEntryPointSuccess || !p) return sq_host::cuda_failed(cudaErrorNotSupported, "cuTensorMapEncodeTiled");
+        cached.store(p, std::memory_order_release);
+    }
+    fn = reinterpret_cast<EncodeTiled>(p);
+    return SQUANT_OK;
+}
+
+// A 16-bit matrix [rows][cols] whose boxes are 64 elements wide and `box_rows` high; elements outside read as zero.
+int matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t cols, int64_t stride, bool half, int box_rows)
+{
+    EncodeTiled encode;
+    if (int rc = encoder(encode)) return rc;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(2 * (rows <= 1 ? up(cols, 8) : stride))};
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)}, step[2] = {1, 1};
+    const CUresult r = encode(&map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(p),
+                              dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SQUANT_OK : sq_host::cuda_failed(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+}
+
+template <int kMode, int kKind, bool kHalf, int kCols>
+int launch_gemm(const CUtensorMap &map, sq::GemmArgs a, int device, int sms, cudaStream_t stream)
+{
+    auto kernel = sq::gemm_kernel<kMode, kKind, kHalf, kCols>;
+    constexpr int smem = sq::GemmShape<kCols>::kSmem;
+    static std::atomic<bool> ready[kMaxDevices];
+    if (device >= kMaxDevices || !ready[device].load(std::memory_order_relaxed)) {
+        SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        if (device < kMaxDevices) ready[device].store(true, std::memory_order_relaxed);
+    }
+    a.row_tiles = (a.rows + sq::kTileRows - 1) / sq::kTileRows;
+    a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + kCols - 1) / kCols);
+    kernel<<<static_cast<unsigned>(std::min<int64_t>(a.tiles, sms)), sq::kGemmThreads, smem, stream>>>(map, a);
+    return launched();
+}
+
+// The widest tile that still gives every multiprocessor one: a wide tile reads less of the 16-bit operand per product
+// and converts each code for more rows.
+template <int kMode, int kKind, bool kHalf>
+int launch_gemm_cols(const CUtensorMap &map, const sq::GemmArgs &a, int device, int sms, cudaStream_t stream)
+{
+    const int64_t row_tiles = (static_cast<int64_t>(a.rows) + sq::kTileRows - 1) / sq::kTileRows;
+    if (row_tiles * ((static_cast<int64_t>(a.cols) + 255) / 256) >= sms) return launch_gemm<kMode, kKind, kHalf, 256>(map, a, device, sms, stream);
+    if (row_tiles * ((static_cast<int64_t>(a.cols) + 127) / 128) >= sms) return launch_gemm<kMode, kKind, kHalf, 128>(map, a, device, sms, stream);
+    return launch_gemm<kMode, kKind, kHalf, 64>(map, a, device, sms, stream);
+}
+
+template <int kKind, bool kHalf, int kTiles>
+int launch_small(const sq::SmallArgs &a, bool vector, cudaStream_t stream)
+{
+    const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kSmallRows - 1) / sq::kSmallRows);
+    if (vector) sq::small_kernel<kKind, kHalf, kTiles, true><<<grid, 32 * sq::kSmallWarps, 0, stream>>>(a);
+    else sq::small_kernel<kKind, kHalf, kTiles, false><<<grid, 32 * sq::kSmallWarps, 0, stream>>>(a);
+    return launched();
+}
+
+template <int kKind, bool kHalf>
+int launch_small_tokens(const sq::SmallArgs &a, bool vector, cudaStream_t stream)
+{
+    if (a.tokens <= 8) return launch_small<kKind, kHalf, 1>(a, vector, stream);
+    if (a.tokens <= 16) return launch_small<kKind, kHalf, 2>(a, vector, stream);
+    return launch_small<kKind, kHalf, 4>(a, vector, stream);
+}
+
+enum class RowKernel { kCheckpoint, kRestore, kAlign };
+
+// Launches over ranges of rows, so that indices within a launch fit 32 bits.
+int launch_rows(RowKernel which, sq::RowArgs a, int64_t rows, cudaStream_t stream)
+{
+    const int64_t most = std::max<int64_t>(1, ((1ll << 31) - 4096) / a.pieces);
+    for (int64_t r = 0; r < rows; r += most) {
+        sq::RowArgs b = a;
+        b.rows = static_cast<uint32_t>(std::min(most, rows - r));
+        if (b.in) b.in += r * a.in_stride;
+        if (b.out) b.out += r * a.out_stride;
+        if (b.codes) { b.codes += r * a.code_pitch; b.exps += r * a.exps_pitch; }
+        const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(b.rows) * b.pieces + sq::kRowThreads * sq::kRowPieces - 1) / (sq::kRowThreads * sq::kRowPieces));
+        switch (which) {
+            case RowKernel::kCheckpoint: sq::checkpoint_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
+            case RowKernel::kRestore: sq::restore_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
+            case RowKernel::kAlign: sq::align_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
+        }
+        if (int rc = launched()) return rc;
+    }
+    return SQUANT_OK;
+}
+
+bool good_dims(int64_t tokens, int64_t cin, int64_t cout)
+{
+    return tokens >= 0 && tokens <= kMaxRows && cin >= 1 && cin <= kMaxRows && cout >= 1 && cout <= kMaxRows && cin * cout <= (1ll << 40);
+}
+bool good_stride(int64_t stride, int64_t cols, int64_t rows) { return rows <= 1 || (stride >= cols && stride <= (1ll << 36)); }
+bool bad_checkpoint(const squant_checkpoint_data &c) { return misaligned(c.codes, 16) || misaligned(c.exps, 16); }
+
+// ---- forward
+
+bool x_needs_copy(const squant_linear_args &a)
+{
+    return a.tokens > kSmallTokens && !rows_on_vectors(a.x, a.x_stride, a.tokens);
+}
+
+int check(const squant_linear_args *args)
+{
+    if (!args) return SQUANT_ERR_NULL;
+    const squant_linear_args &a = *args;
+    if (!good_dims(a.tokens, a.cin, a.cout)) return SQUANT_ERR_SHAPE;
+    if (!good_stride(a.x_stride, a.cin, a.tokens) || !good_stride(a.y_stride, a.cout, a.tokens) ||
+        (a.residual && !good_stride(a.residual_stride, a.cout, a.tokens))) return SQUANT_ERR_SHAPE;
+    if (a.dtype > SQUANT_FP16 || a.act > SQUANT_ACT_SILU || (a.flags & ~SQUANT_FLAG_PACK_INT4)) return SQUANT_ERR_MODE;
+    if (!a.codes || !a.scales) return SQUANT_ERR_NULL;
+    if (a.tokens > 0 && (!a.x || !a.y)) return SQUANT_ERR_NULL;
+    if (a.z.codes && !a.z.exps) return SQUANT_ERR_NULL;
+    if (misaligned(a.x, 2) || misaligned(a.y, 2) || misaligned(a.residual, 2) || misaligned(a.scales, 4) || misaligned(a.bias, 4) ||
+        (a.z.codes && bad_checkpoint(a.z))) return SQUANT_ERR_ALIGN;
+    return SQUANT_OK;
+}
+
+template <int kKind, bool kHalf>
+int forward(const squant_linear_args &a, cudaStream_t stream)
+{
+    const int64_t pitch = kKind == sq::kInt4 ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
+    const bool code_vector = !misaligned(a.codes, 16) && pitch % 16 == 0;
+    const int64_t z_pitch = up(a.cout, 32);
+    if (a.tokens <= kSmallTokens) {
+        sq::SmallArgs s{};
+        s.x = static_cast<const uint16_t *>(a.x);
+        s.x_stride = a.x_stride;
+        s.codes = reinterpret_cast<const uint8_t *>(a.codes);
+        s.code_pitch = pitch;
+        s.code_bytes = pitch * a.cout;
+        s.tokens = static_cast<int32_t>(a.tokens);
+        s.cin = a.cin;
+        s.cout = a.cout;
+        s.scales = a.scales;
+        s.bias = a.bias;
+        s.residual = static_cast<const uint16_t *>(a.residual);
+        s.residual_stride = a.residual_stride;
+        s.y = static_cast<uint16_t *>(a.y);
+        s.y_stride = a.y_stride;
+        s.act = static_cast<int32_t>(a.act);
+        s.z_codes = reinterpret_cast<uint8_t *>(a.z.codes);
+        s.z_exps = a.z.exps;
+        s.z_pitch = z_pitch;
+        s.z_exps_pitch = z_pitch / 32;
+        return launch_small_tokens<kKind, kHalf>(s, code_vector && rows_on_vectors(a.x, a.x_stride, a.tokens) && a.cin % 8 == 0, stream);
+    }
+    int device, sms;
+    if (int rc = device_sms(device, sms)) return rc;
+    const void *x = a.x;
+    int64_t x_stride = a.x_stride;
+    if (x_needs_copy(a)) {
+        sq::RowArgs r{};
+        r.in = static_cast<const uint16_t *>(a.x);
+        r.in_stride = a.x_stride;
+        r.out = static_cast<uint16_t *>(a.workspace);
+        r.out_stride = up(a.cin, 8);
+        r.pieces = static_cast<uint32_t>(r.out_stride / 8);
+        r.features = a.cin;
+        if (int rc = launch_rows(RowKernel::kAlign, r, a.tokens, stream)) return rc;
+        x = a.workspace;
+        x_stride = r.out_stride;
+    }
+    CUtensorMap map;
+    if (int rc = matrix_map(map, x, a.tokens, a.cin, x_stride, kHalf, sq::kTileRows)) return rc;
+    sq::GemmArgs g{};
+    g.codes = reinterpret_cast<const uint8_t *>(a.codes);
+    g.code_pitch = pitch;
+    g.code_bytes = pitch * a.cout;
+    g.code_rows = a.cout;
+    g.code_row_bytes = static_cast<int32_t>(pitch);
+    g.vector = code_vector;
+    g.rows = static_cast<int32_t>(a.tokens);
+    g.cols = a.cout;
+    g.depth = a.cin;
+    g.out = static_cast<uint16_t *>(a.y);
+    g.out_stride = a.y_stride;
+    g.out_vector = rows_on_vectors(a.y, a.y_stride, a.tokens);
+    g.scales = a.scales;
+    g.bias = a.bias;
+    g.residual = static_cast<const uint16_t *>(a.residual);
+    g.residual_stride = a.residual_stride;
+    g.residual_vector = rows_on_vectors(a.residual, a.residual_stride, a.tokens);
+    g.act = static_cast<int32_t>(a.act);
+    g.z_codes = reinterpret_cast<uint8_t *>(a.z.codes);
+    g.z_exps = a.z.exps;
+    g.z_pitch = z_pitch;
+    g.z_exps_pitch = z_pitch / 32;
+    return launch_gemm_cols<sq::kForward, kKind, kHalf>(map, g, device, sms, stream);
+}
+
+// ---- backward
+
+// What the gradients need of dy * act'(zhat): parts of the workspace, each [tokens][pitch] bf16.
+struct SlopePlan {
+    bool dzs = false, dz = false, any = false;
+    int64_t pitch = 0, bytes = 0;
+};
+
+SlopePlan slope_plan(const squant_linear_grad_args &a)
+{
+    SlopePlan s;
+    s.pitch = up(a.cout, 8);
+    s.dzs = a.dx && a.tokens > 0;
+    s.dz = a.dweight && a.tokens > 0 && (a.act != SQUANT_ACT_NONE || !rows_on_vectors(a.dy, a.dy_stride, a.tokens));
+    s.any = s.dzs || s.dz || a.dbias || a.dscales;
+    s.bytes = (s.dzs + s.dz) * a.tokens * s.pitch * 2;
+    return s;
+}
+
+int check(const squant_linear_grad_args *args)
+{
+    if (!args) return SQUANT_ERR_NULL;
+    const squant_linear_grad_args &a = *args;
+    if (!good_dims(a.tokens, a.cin, a.cout)) return SQUANT_ERR_SHAPE;
+    if (!good_stride(a.dy_stride, a.cout, a.tokens) || (a.dx && !good_stride(a.dx_stride, a.cin, a.tokens)) ||
+        (a.dweight && !good_stride(a.dweight_stride, a.cin, a.cout))) return SQUANT_ERR_SHAPE;
+    if (a.act > SQUANT_ACT_SILU || (a.flags & ~SQUANT_FLAG_PACK_INT4)) return SQUANT_ERR_MODE;
+    if (a.dx && (!a.codes || !a.scales)) return SQUANT_ERR_NULL;
+    if (a.dscales && !a.scales) return SQUANT_ERR_NULL;
+    if (a.tokens > 0) {
+        if (!a.dy) return SQUANT_ERR_NULL;
+        if ((a.act != SQUANT_ACT_NONE || a.dscales) && (!a.z.codes || !a.z.exps)) return SQUANT_ERR_NULL;
+        if (a.dweight && (!a.x.codes || !a.x.exps)) return SQUANT_ERR_NULL;
+    }
+    if (misaligned(a.dy, 2) || misaligned(a.dx, 2) || misaligned(a.dweight, 2) || misaligned(a.scales, 4) || misaligned(a.bias, 4) ||
+        misaligned(a.dbias, 4) || misaligned(a.dscales, 4) || bad_checkpoint(a.z) || bad_checkpoint(a.x)) return SQUANT_ERR_ALIGN;
+    return SQUANT_OK;
+}
+
+int slope(const squant_linear_grad_args &a, const SlopePlan &plan, uint16_t *dzs, uint16_t *dz, cudaStream_t stream)
+{
+    sq::SlopeArgs s{};
+    s.dy = static_cast<const uint16_t *>(a.dy);
+    s.dy_stride = a.dy_stride;
+    s.dy_vector = rows_on_vectors(a.dy, a.dy_stride, a.tokens);
+    const bool need_z = a.act != SQUANT_ACT_NONE || a.dscales;
+    s.z_codes = need_z ? reinterpret_cast<const uint8_t *>(a.z.codes) : nullptr;
+    s.z_exps = need_z ? a.z.exps : nullptr;
+    s.z_pitch = up(a.cout, 32);
+    s.z_exps_pitch = s.z_pitch / 32;
+    s.scales = a.scales;
+    s.bias = a.bias;
+    s.tokens = a.tokens;
+    s.cout = a.cout;
+    s.act = static_cast<int32_t>(a.act);
+    s.dz = dz;
+    s.dzs = dzs;
+    s.pitch = plan.pitch;
+    s.dbias = a.dbias;
+    s.dscales = a.dscales;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    const unsigned ranks = static_cast<unsigned>(std::min<int64_t>(sq::kSlopeCluster, std::max<int64_t>(1, (a.tokens + 31) / 32)));
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {1, ranks, 1};
+    cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kSlopeCols - 1) / sq::kSlopeCols), ranks);
+    cfg.blockDim = dim3(sq::kRowThreads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SQ_CUDA(cudaLaunchKernelEx(&cfg, sq::slope_kernel, s));
+    sq_host::count_launch();
+    return SQUANT_OK;
+}
+
+}  // namespace
+
+namespace sq_host {
+
+cudaError_t take_linear_status(int *status)
+{
+    cudaError_t e = cudaMemcpyFromSymbol(status, sq::g_linear_status, sizeof(int));
+    const int zero = 0;
+    if (e == cudaSuccess && *status) e = cudaMemcpyToSymbol(sq::g_linear_status, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace sq_host
+
+extern "C" {
+
+int squant_checkpoint(const void *x, int64_t rows, int32_t features, int64_t stride, const squant_checkpoint_data *to, void *cuda_stream)
+{
+    if (!to) return SQUANT_ERR_NULL;
+    if (!good_dims(rows, features, 1) || !good_stride(stride, features, rows)) return SQUANT_ERR_SHAPE;
+    if (rows == 0) return SQUANT_OK;
+    if (!x || !to->codes || !to->exps) return SQUANT_ERR_NULL;
+    if (misaligned(x, 2) || bad_checkpoint(*to)) return SQUANT_ERR_ALIGN;
+    sq::RowArgs r{};
+    r.in = static_cast<const uint16_t *>(x);
+    r.in_stride = stride;
+    r.codes = reinterpret_cast<uint8_t *>(to->codes);
+    r.exps = to->exps;
+    r.code_pitch = up(features, 32);
+    r.exps_pitch = r.code_pitch / 32;
+    r.pieces = static_cast<uint32_t>(r.code_pitch / 8);
+    r.features = features;
+    r.vector = rows_on_vectors(x, stride, rows);
+    return launch_rows(RowKernel::kCheckpoint, r, rows, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int squant_checkpoint_restore(const squant_checkpoint_data *from, int64_t rows, int32_t features, void *out, int64_t stride,
+                              void *cuda_stream)
+{
+    if (!from) return SQUANT_ERR_NULL;
+    if (!good_dims(rows, features, 1) || !good_stride(stride, features, rows)) return SQUANT_ERR_SHAPE;
+    if (rows == 0) return SQUANT_OK;
+    if (!out || !from->codes || !from->exps) return SQUANT_ERR_NULL;
+    if (misaligned(out, 2) || bad_checkpoint(*from)) return SQUANT_ERR_ALIGN;
+    sq::RowArgs r{};
+    r.out = static_cast<uint16_t *>(out);
+    r.out_stride = stride;
+    r.codes = reinterpret_cast<uint8_t *>(from->codes);
+    r.exps = from->exps;
+    r.code_pitch = up(features, 32);
+    r.exps_pitch = r.code_pitch / 32;
+    r.pieces = static_cast<uint32_t>(r.code_pitch / 8);
+    r.features = features;
+    r.vector = rows_on_vectors(out, stride, rows);
+    return launch_rows(RowKernel::kRestore, r, rows, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int64_t squant_linear_workspace(const squant_linear_args *args)
+{
+    if (int rc = check(args)) return rc;
+    return x_needs_copy(*args) ? args->tokens * up(args->cin, 8) * 2 : 0;
+}
+
+int squant_linear(const squant_linear_args *args, void *cuda_stream)
+{
+    if (int rc = check(args)) return rc;
+    const squant_linear_args &a = *args;
+    if (a.tokens == 0) return SQUANT_OK;
+    if (x_needs_copy(a) && (!a.workspace || misaligned(a.workspace, 16) || a.workspace_bytes < a.tokens * up(a.cin, 8) * 2))
+        return SQUANT_ERR_WORKSPACE;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const bool half = a.dtype == SQUANT_FP16;
+    if (a.flags & SQUANT_FLAG_PACK_INT4) return half ? forward<sq::kInt4, true>(a, stream) : forward<sq::kInt4, false>(a, stream);
+    return half ? forward<sq::kInt8, true>(a, stream) : forward<sq::kInt8, false>(a, stream);
+}
+
+int64_t squant_linear_backward_workspace(const squant_linear_grad_args *args)
+{
+    if (int rc = check(args)) return rc;
+    return slope_plan(*args).bytes;
+}
+
+int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_stream)
+{
+    if (int rc = check(args)) return rc;
+    const squant_linear_grad_args &a = *args;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const SlopePlan plan = slope_plan(a);
+    if (plan.bytes && (!a.workspace || misaligned(a.workspace, 16) || a.workspace_bytes < plan.bytes)) return SQUANT_ERR_WORKSPACE;
+    int device, sms;
+    if (int rc = device_sms(device, sms)) return rc;
+    uint16_t *dzs = plan.dzs ? static_cast<uint16_t *>(a.workspace) : nullptr;
+    uint16_t *dz = plan.dz ? static_cast<uint16_t *>(a.workspace) + (plan.dzs ? a.tokens * plan.pitch : 0) : nullptr;
+    if (plan.any)
+        if (int rc = slope(a, plan, dzs, dz, stream)) return rc;
+    if (plan.dzs) {
+        const bool packed = a.flags & SQUANT_FLAG_PACK_INT4;
+        CUtensorMap map;
+        if (int rc = matrix_map(map, dzs, a.tokens, a.cout, plan.pitch, false, sq::kTileRows)) return rc;
+        sq::GemmArgs g{};
+        g.codes = reinterpret_cast<const uint8_t *>(a.codes);
+        g.code_pitch = packed ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
+        g.code_bytes = g.code_pitch * a.cout;
+        g.code_rows = a.cout;
+        g.code_row_bytes = static_cast<int32_t>(g.code_pitch);
+        g.vector = !misaligned(a.codes, 16) && g.code_pitch % 16 == 0;
+        g.rows = static_cast<int32_t>(a.tokens);
+        g.cols = a.cin;
+        g.depth = a.cout;
+        g.out = static_cast<uint16_t *>(a.dx);
+        g.out_stride = a.dx_stride;
+        g.out_vector = rows_on_vectors(a.dx, a.dx_stride, a.tokens);
+        if (int rc = packed ? launch_gemm_cols<sq::kInputGrad, sq::kInt4, false>(map, g, device, sms, stream)
+                            : launch_gemm_cols<sq::kInputGrad, sq::kInt8, false>(map, g, device, sms, stream)) return rc;
+    }
+    if (a.dweight) {
+        if (a.tokens == 0) {
+            SQ_CUDA(cudaMemset2DAsync(a.dweight, 2 * (a.cout == 1 ? a.cin : a.dweight_stride), 0, 2 * static_cast<size_t>(a.cin), a.cout, stream));
+            return SQUANT_OK;
+        }
+        CUtensorMap map;
+        if (int rc = matrix_map(map, dz ? dz : a.dy, a.tokens, a.cout, dz ? plan.pitch : a.dy_stride, false, sq::kTileDepth)) return rc;
+        sq::GemmArgs g{};
+        g.codes = reinterpret_cast<const uint8_t *>(a.x.codes);
+        g.exps = a.x.exps;
+        g.code_pitch = up(a.cin, 32);
+        g.exps_pitch = g.code_pitch / 32;
+        g.code_bytes = g.code_pitch * a.tokens;
+        g.code_rows = static_cast<int32_t>(a.tokens);
+        g.code_row_bytes = static_cast<int32_t>(g.code_pitch);
+        g.vector = 1;
+        g.rows = a.cout;
+        g.cols = a.cin;
+        g.depth = static_cast<int32_t>(a.tokens);
+        g.out = static_cast<uint16_t *>(a.dweight);
+        g.out_stride = a.dweight_stride;
+        g.out_vector = rows_on_vectors(a.dweight, a.dweight_stride, a.cout);
+        if (int rc = launch_gemm_cols<sq::kWeightGrad, sq::kCkpt8, false>(map, g, device, sms, stream)) return rc;
+    }
+    return SQUANT_OK;
+}
+
+}  // extern "C"

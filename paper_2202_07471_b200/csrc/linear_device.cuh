@@ -1,0 +1,288 @@
+// Device helpers of the linear operators: codes to 16-bit floats, the 8-bit checkpoint format, activations,
+// mbarriers, TMA and tcgen05 wrappers.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace sq {
+
+enum { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
+enum CodeKind { kInt4 = 0, kInt8 = 1, kCkpt8 = 2 };
+
+// Set by a kernel of this file's users that gave up a bounded wait (read and cleared by squant_device_status()).
+static __device__ int g_linear_status = 0;
+
+// ---------------------------------------------------------------- 8-bit checkpoints
+//
+// 32 consecutive features of a row share a power of two: with a = max|v|, E = max(1, exponent field of a - 6) and
+// q = clamp(rint(v * 2^(127 - E)), -127, 127); the value is q * 2^(E - 127).  E = 255 marks a group with an infinity
+// or a NaN: its values are NaN.  A power of two costs up to one bit against a scale of absmax / 127, and makes every
+// value exact in bfloat16 (seven significant bits), so that the tensor cores read what was stored.
+__device__ __forceinline__ uint32_t ckpt_exponent(float absmax)   // absmax: NaN if any value is
+{
+    const uint32_t field = __float_as_uint(absmax) >> 23;
+    return field >= 255u ? 255u : field < 7u ? 1u : field - 6u;
+}
+__device__ __forceinline__ float ckpt_inverse(uint32_t e)   // 2^(127 - E); 0 for a group that is not finite
+{
+    return e == 255u ? 0.0f : __uint_as_float((254u - e) << 23);
+}
+__device__ __forceinline__ int ckpt_code(float v, float inverse)
+{
+    // the product is exact unless it is far below one half; 0 * inf is NaN, which __float2int_rn turns into 0
+    const int q = __float2int_rn(v * inverse);
+    return q > 127 ? 127 : q < -127 ? -127 : q;
+}
+__device__ __forceinline__ float ckpt_scale(uint32_t e) { return __uint_as_float(e << 23); }   // 255: inf, 0 * inf = NaN
+// max that keeps a NaN
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// ---------------------------------------------------------------- activations (fp32)
+
+__device__ __forceinline__ float act_value(float z, int act)
+{
+    if (act == kActRelu) return z < 0.0f ? 0.0f : z;             // keeps a NaN
+    if (act == kActGelu) return 0.5f * z * erfcf(z * -0.70710678118654752f);   // no cancellation at negative z
+    if (act == kActSilu) return __fdividef(z, 1.0f + expf(-z));
+    return z;
+}
+__device__ __forceinline__ float act_slope(float z, int act)
+{
+    if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
+    if (act == kActGelu) return 0.5f * erfcf(z * -0.70710678118654752f) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    if (act == kActSilu) {
+        const float p = 1.0f / (1.0f + expf(-z));
+        return p * (1.0f + z * (1.0f - p));
+    }
+    return 1.0f;
+}
+
+// ---------------------------------------------------------------- 16-bit types
+
+template <bool kHalf>
+__device__ __forceinline__ float to_float(uint16_t v)
+{
+    if constexpr (kHalf) return __half2float(__ushort_as_half(v));
+    else return __uint_as_float(static_cast<uint32_t>(v) << 16);
+}
+template <bool kHalf>
+__device__ __forceinline__ uint16_t to_16(float v)
+{
+    if constexpr (kHalf) return __half_as_ushort(__float2half_rn(v));
+    else return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+}
+template <bool kHalf>
+__device__ __forceinline__ uint32_t to_16x2(float lo, float hi)
+{
+    if constexpr (kHalf) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+}
+
+template <bool kHalf>
+__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t r;
+    if constexpr (kHalf) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t sub2_bf16(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul2_bf16(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Eight int4 codes (low nibble first) to four pairs of 16-bit floats, exactly.  A code's nibble n, its sign bit
+// flipped, becomes the low mantissa bits of 128 (bf16) or 1024 (fp16), which gives 128 + n + 8; the odd codes' nibbles
+// sit three bits further up (the word shifted by one), which gives 128 + 8 (n + 8).  One fused multiply-add on the
+// pair takes the offsets off and divides the odd code by 8: three instructions a pair and one shift a word.
+template <bool kHalf>
+__device__ __forceinline__ void int4_to_16(uint32_t w, uint32_t out[4])
+{
+    constexpr uint32_t base = kHalf ? 0x64006400u : 0x43004300u;
+    constexpr uint32_t factor = kHalf ? 0x30003c00u : 0x3e003f80u;    // (1, 1/8), low half first
+    constexpr uint32_t offset = kHalf ? 0xd840e408u : 0xc1c0c308u;    // fp16 (-1032, -136), bf16 (-136, -24)
+    const uint32_t s = w >> 1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t v = __byte_perm(w, s, 0x0400u | (0x0101u * j));   // byte 0: w's byte j, byte 2: s's byte j
+        out[j] = fma2<kHalf>((v & 0x0078000fu) ^ (base | 0x00400008u), factor, offset);
+    }
+}
+
+// Four int8 codes to two pairs of 16-bit floats, exactly.  bf16 has seven mantissa bits: the low seven bits L of a
+// byte give 128 + L, its sign bit S gives 128 + 128 S as exponent bit; the difference is L - 128 S.
+template <bool kHalf>
+__device__ __forceinline__ void int8_to_16(uint32_t w, uint32_t out[2])
+{
+    if constexpr (kHalf) {
+        const uint32_t u = w ^ 0x80808080u;                              // 1024 + (code + 128)
+        out[0] = fma2<true>(__byte_perm(u, 0x64u, 0x4140), 0x3c003c00u, 0xe480e480u);
+        out[1] = fma2<true>(__byte_perm(u, 0x64u, 0x4342), 0x3c003c00u, 0xe480e480u);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t h = __byte_perm(w, 0x43u, j ? 0x4342 : 0x4140);
+            out[j] = sub2_bf16(h & 0xff7fff7fu, h & 0xff80ff80u);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- guarded loads
+
+__device__ __forceinline__ uint4 ldg128(const void *p)
+{
+    uint4 r;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+
+// 16 bytes from any address: five aligned words, shifted.  Words that are not wholly inside [lo, hi) are put
+// together from the bytes that are; other bytes read as zero.
+__device__ __noinline__ uint4 load_bytes16(const uint8_t *p, const uint8_t *lo, const uint8_t *hi)
+{
+    const uint8_t *a = reinterpret_cast<const uint8_t *>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t{3});
+    const unsigned sh = static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) & 3) * 8;
+    uint32_t w[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        const uint8_t *q = a + 4 * i;
+        if (q >= lo && q + 4 <= hi) {
+            w[i] = __ldg(reinterpret_cast<const uint32_t *>(q));
+        } else {
+            uint32_t v = 0;
+            for (int b = 0; b < 4; ++b)
+                if (q + b >= lo && q + b < hi) v |= static_cast<uint32_t>(__ldg(q + b)) << (8 * b);
+            w[i] = v;
+        }
+    }
+    return make_uint4(__funnelshift_r(w[0], w[1], sh), __funnelshift_r(w[1], w[2], sh), __funnelshift_r(w[2], w[3], sh),
+                      __funnelshift_r(w[3], w[4], sh));
+}
+
+// ---------------------------------------------------------------- mbarriers, TMA, tcgen05
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+constexpr int kWaitLimit = 1 << 22;   // tries, each of which the hardware parks for a while: seconds
+
+// False when the wait ran out or another thread of the block gave up (*gave_up is shared by the block).
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
+{
+    if (bar_try(bar, parity)) return true;
+    for (int i = 0; i < kWaitLimit; ++i) {
+        if (bar_try(bar, parity)) return true;
+        if (*gave_up) return false;
+    }
+    *gave_up = 1;
+    atomicExch(&g_linear_status, 1);
+    return false;
+}
+// The same for a whole warp, which goes on or gives up together.
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *gave_up)
+{
+    return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up));
+}
+// The wait for one's own copies after the block has given up: bounded, without a look at the flag.
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity)
+{
+    for (int i = 0; i < (1 << 16); ++i)
+        if (bar_try(bar, parity)) return;
+}
+
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void tmem_alloc(uint32_t where, uint32_t columns)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// Shared-memory matrix descriptor, 128-byte swizzle.  A panel has rows of 64 16-bit elements (128 bytes), its eight
+// 16-byte pieces permuted by the row's low three bits; eight rows are 1024 bytes.
+//   contraction along the rows' 64 elements ("K-major"): 1024 bytes between groups of eight rows; the next 16 elements
+//   of the contraction are 32 bytes on
+//   contraction over the rows ("MN-major"): the panel's 64 elements are 64 columns of the tile, `panel` bytes to the
+//   next 64; 1024 bytes between groups of eight rows, 16 of which a matrix instruction takes: the next start 2048 on
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t leading)
+{
+    return (static_cast<uint64_t>(addr & 0x3ffffu) >> 4) | (static_cast<uint64_t>(leading >> 4) << 16) |
+           (static_cast<uint64_t>(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+}  // namespace sq

@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "squant_device.cuh"
+#include "squant_host.h"
 #include "squant_stream.cuh"
 #include "squant_wide.cuh"
 
@@ -862,6 +863,13 @@ int noalloc_table_address(int device, void *&ptr)
 
 }  // namespace
 
+namespace sq_host {
+
+int cuda_failed(cudaError_t e, const char *what) { return cuda_fail(e, what); }
+void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
+
+}  // namespace sq_host
+
 extern "C" {
 
 int squant_quantize_model(const squant_layer *layers, int32_t n_layers, const squant_options *opt,
@@ -1161,7 +1169,9 @@ int squant_device_status(void)
     SQ_CUDA(cudaDeviceSynchronize());
     int st = 0;
     SQ_CUDA(cudaMemcpyFromSymbol(&st, sq::g_device_status, sizeof(int)));
-    if (st == 0) return SQUANT_OK;
+    int linear = 0;
+    SQ_CUDA(sq_host::take_linear_status(&linear));
+    if (st == 0) return linear == 0 ? SQUANT_OK : SQUANT_ERR_TIMEOUT;
     const int zero = 0;
     SQ_CUDA(cudaMemcpyToSymbol(sq::g_device_status, &zero, sizeof(int)));
     // a launch that gave up may have left its work counters half drawn: all start clean again
@@ -1236,6 +1246,7 @@ const char *squant_strerror(int code)
         case SQUANT_ERR_NOMEM: return "out of host or device memory";
         case SQUANT_ERR_TIMEOUT: return "a kernel gave up a bounded wait on an asynchronous copy; outputs of that launch are incomplete";
         case SQUANT_ERR_CAPTURE: return "squant_quantize_layer_noalloc was called on a stream that is being captured; it uploads its launch table from a host image that the next call rewrites";
+        case SQUANT_ERR_WORKSPACE: return "the workspace is missing, too small or not 16-byte aligned";
         case SQUANT_ERR_LIMIT: return "the layer needs more thread blocks than the fixed launch table of squant_quantize_layer_noalloc holds (SQUANT_NOALLOC_MAX_CTAS); split it by output-channel range";
         default: return "unknown squant error code";
     }
