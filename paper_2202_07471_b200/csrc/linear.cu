@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "linear_dense.cuh"
 #include "linear_device.cuh"
 #include "linear_gemm.cuh"
 #include "linear_rows.cuh"
@@ -18,6 +19,7 @@ namespace {
 constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxRows = 1ll << 30;
 constexpr int kSmallTokens = 32;   // up to as many tokens the forward product goes to small_kernel
+constexpr int kFusedTokens = 128;  // up to as many gemm_kernel turns the codes into floats itself; beyond, they are expanded once
 
 #define SQ_CUDA(call)                                                      \
     do {                                                                   \
@@ -103,6 +105,40 @@ int launch_gemm_cols(const CUtensorMap &map, const sq::GemmArgs &a, int device, 
     return launch_gemm<kMode, kKind, kHalf, 64>(map, a, device, sms, stream);
 }
 
+template <int kMode, bool kHalf, int kCols>
+int launch_dense(const CUtensorMap &map_a, const CUtensorMap &map_b, sq::GemmArgs a, int device, int sms, cudaStream_t stream)
+{
+    auto kernel = sq::dense_kernel<kMode, kHalf, kCols>;
+    constexpr int smem = sq::DenseShape<kCols>::kSmem;
+    static std::atomic<bool> ready[kMaxDevices];
+    if (device >= kMaxDevices || !ready[device].load(std::memory_order_relaxed)) {
+        SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        if (device < kMaxDevices) ready[device].store(true, std::memory_order_relaxed);
+    }
+    a.row_tiles = (a.rows + sq::kPairRows - 1) / sq::kPairRows;
+    a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + kCols - 1) / kCols);
+    kernel<<<2 * static_cast<unsigned>(std::min<int64_t>(a.tiles, sms / 2)), sq::kDenseThreads, smem, stream>>>(map_a, map_b, a);
+    return launched();
+}
+
+// The product of two 16-bit matrices: `a` as gemm's 16-bit operand, `b` [cols][depth] (forward) or [depth][cols].  Tiles of
+// 256 or 128 columns, whichever is done in fewer waves; a wave of narrow tiles takes about 0.6 of one of wide tiles.
+template <int kMode, bool kHalf>
+int dense(const void *a, int64_t a_stride, const void *b, int64_t b_stride, const sq::GemmArgs &g, int device, int sms, cudaStream_t stream)
+{
+    const int64_t row_tiles = (static_cast<int64_t>(g.rows) + sq::kPairRows - 1) / sq::kPairRows, pairs = sms / 2;
+    const int64_t wide = (row_tiles * ((static_cast<int64_t>(g.cols) + 255) / 256) + pairs - 1) / pairs;
+    const int64_t narrow = (row_tiles * ((static_cast<int64_t>(g.cols) + 127) / 128) + pairs - 1) / pairs;
+    const bool use_wide = 10 * wide <= 6 * narrow;
+    CUtensorMap map_a, map_b;
+    if (int rc = kMode == sq::kWeightGrad ? matrix_map(map_a, a, g.depth, g.rows, a_stride, kHalf, sq::kTileDepth)
+                                          : matrix_map(map_a, a, g.rows, g.depth, a_stride, kHalf, 128)) return rc;
+    if (int rc = kMode == sq::kForward ? matrix_map(map_b, b, g.cols, g.depth, b_stride, kHalf, use_wide ? 128 : 64)
+                                       : matrix_map(map_b, b, g.depth, g.cols, b_stride, kHalf, sq::kTileDepth)) return rc;
+    return use_wide ? launch_dense<kMode, kHalf, 256>(map_a, map_b, g, device, sms, stream)
+                    : launch_dense<kMode, kHalf, 128>(map_a, map_b, g, device, sms, stream);
+}
+
 template <int kKind, bool kHalf, int kTiles>
 int launch_small(const sq::SmallArgs &a, bool vector, cudaStream_t stream)
 {
@@ -120,7 +156,7 @@ int launch_small_tokens(const sq::SmallArgs &a, bool vector, cudaStream_t stream
     return launch_small<kKind, kHalf, 4>(a, vector, stream);
 }
 
-enum class RowKernel { kCheckpoint, kRestore, kAlign };
+enum class RowKernel { kCheckpoint, kRestore, kAlign, kExpandInt4Bf16, kExpandInt4Fp16, kExpandInt8Bf16, kExpandInt8Fp16 };
 
 // Launches over ranges of rows, so that indices within a launch fit 32 bits.
 int launch_rows(RowKernel which, sq::RowArgs a, int64_t rows, cudaStream_t stream)
@@ -131,16 +167,52 @@ int launch_rows(RowKernel which, sq::RowArgs a, int64_t rows, cudaStream_t strea
         b.rows = static_cast<uint32_t>(std::min(most, rows - r));
         if (b.in) b.in += r * a.in_stride;
         if (b.out) b.out += r * a.out_stride;
-        if (b.codes) { b.codes += r * a.code_pitch; b.exps += r * a.exps_pitch; }
+        if (b.codes) b.codes += r * a.code_pitch;
+        if (b.exps) b.exps += r * a.exps_pitch;
         const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(b.rows) * b.pieces + sq::kRowThreads * sq::kRowPieces - 1) / (sq::kRowThreads * sq::kRowPieces));
         switch (which) {
             case RowKernel::kCheckpoint: sq::checkpoint_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
             case RowKernel::kRestore: sq::restore_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
             case RowKernel::kAlign: sq::align_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
+            case RowKernel::kExpandInt4Bf16: sq::expand_kernel<sq::kInt4, false><<<grid, sq::kRowThreads, 0, stream>>>(b); break;
+            case RowKernel::kExpandInt4Fp16: sq::expand_kernel<sq::kInt4, true><<<grid, sq::kRowThreads, 0, stream>>>(b); break;
+            case RowKernel::kExpandInt8Bf16: sq::expand_kernel<sq::kInt8, false><<<grid, sq::kRowThreads, 0, stream>>>(b); break;
+            case RowKernel::kExpandInt8Fp16: sq::expand_kernel<sq::kInt8, true><<<grid, sq::kRowThreads, 0, stream>>>(b); break;
         }
         if (int rc = launched()) return rc;
     }
     return SQUANT_OK;
+}
+
+int restore(const squant_checkpoint_data &from, int64_t rows, int32_t features, void *out, int64_t stride, cudaStream_t stream)
+{
+    sq::RowArgs r{};
+    r.out = static_cast<uint16_t *>(out);
+    r.out_stride = stride;
+    r.codes = reinterpret_cast<uint8_t *>(from.codes);
+    r.exps = from.exps;
+    r.code_pitch = up(features, 32);
+    r.exps_pitch = r.code_pitch / 32;
+    r.pieces = static_cast<uint32_t>(r.code_pitch / 8);
+    r.features = features;
+    r.vector = rows_on_vectors(out, stride, rows);
+    return launch_rows(RowKernel::kRestore, r, rows, stream);
+}
+
+// Codes [cout][cin] to 16-bit floats [cout][cin rounded up to 8].
+int expand(const int8_t *codes, int64_t cout, int32_t cin, bool packed, bool half, void *out, cudaStream_t stream)
+{
+    sq::RowArgs r{};
+    r.codes = reinterpret_cast<uint8_t *>(const_cast<int8_t *>(codes));
+    r.code_pitch = packed ? (static_cast<int64_t>(cin) + 1) / 2 : cin;
+    r.out = static_cast<uint16_t *>(out);
+    r.out_stride = up(cin, 8);
+    r.pieces = static_cast<uint32_t>(r.out_stride / 8);
+    r.features = cin;
+    const int64_t piece = packed ? 4 : 8;
+    r.vector = !misaligned(codes, piece) && r.code_pitch % piece == 0;
+    return launch_rows(packed ? (half ? RowKernel::kExpandInt4Fp16 : RowKernel::kExpandInt4Bf16)
+                              : (half ? RowKernel::kExpandInt8Fp16 : RowKernel::kExpandInt8Bf16), r, cout, stream);
 }
 
 bool good_dims(int64_t tokens, int64_t cin, int64_t cout)
@@ -152,9 +224,20 @@ bool bad_checkpoint(const squant_checkpoint_data &c) { return misaligned(c.codes
 
 // ---- forward
 
-bool x_needs_copy(const squant_linear_args &a)
+// Parts of the workspace: a copy of x with rows that TMA can read, the codes as 16-bit floats.
+struct ForwardPlan {
+    bool copy = false, dense = false;
+    int64_t copy_bytes = 0, bytes = 0;
+};
+
+ForwardPlan forward_plan(const squant_linear_args &a)
 {
-    return a.tokens > kSmallTokens && !rows_on_vectors(a.x, a.x_stride, a.tokens);
+    ForwardPlan p;
+    p.copy = a.tokens > kSmallTokens && !rows_on_vectors(a.x, a.x_stride, a.tokens);
+    p.dense = a.tokens > kFusedTokens;
+    if (p.copy) p.copy_bytes = a.tokens * up(a.cin, 8) * 2;
+    p.bytes = p.copy_bytes + (p.dense ? a.cout * up(a.cin, 8) * 2 : 0);
+    return p;
 }
 
 int check(const squant_linear_args *args)
@@ -206,7 +289,8 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
     if (int rc = device_sms(device, sms)) return rc;
     const void *x = a.x;
     int64_t x_stride = a.x_stride;
-    if (x_needs_copy(a)) {
+    const ForwardPlan plan = forward_plan(a);
+    if (plan.copy) {
         sq::RowArgs r{};
         r.in = static_cast<const uint16_t *>(a.x);
         r.in_stride = a.x_stride;
@@ -218,15 +302,7 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
         x = a.workspace;
         x_stride = r.out_stride;
     }
-    CUtensorMap map;
-    if (int rc = matrix_map(map, x, a.tokens, a.cin, x_stride, kHalf, sq::kTileRows)) return rc;
     sq::GemmArgs g{};
-    g.codes = reinterpret_cast<const uint8_t *>(a.codes);
-    g.code_pitch = pitch;
-    g.code_bytes = pitch * a.cout;
-    g.code_rows = a.cout;
-    g.code_row_bytes = static_cast<int32_t>(pitch);
-    g.vector = code_vector;
     g.rows = static_cast<int32_t>(a.tokens);
     g.cols = a.cout;
     g.depth = a.cin;
@@ -235,6 +311,7 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
     g.out_vector = rows_on_vectors(a.y, a.y_stride, a.tokens);
     g.scales = a.scales;
     g.bias = a.bias;
+    g.param_vector = !misaligned(a.scales, 16) && !misaligned(a.bias, 16);
     g.residual = static_cast<const uint16_t *>(a.residual);
     g.residual_stride = a.residual_stride;
     g.residual_vector = rows_on_vectors(a.residual, a.residual_stride, a.tokens);
@@ -243,6 +320,19 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
     g.z_exps = a.z.exps;
     g.z_pitch = z_pitch;
     g.z_exps_pitch = z_pitch / 32;
+    if (plan.dense) {
+        uint8_t *b = static_cast<uint8_t *>(a.workspace) + plan.copy_bytes;
+        if (int rc = expand(a.codes, a.cout, a.cin, kKind == sq::kInt4, kHalf, b, stream)) return rc;
+        return dense<sq::kForward, kHalf>(x, x_stride, b, up(a.cin, 8), g, device, sms, stream);
+    }
+    CUtensorMap map;
+    if (int rc = matrix_map(map, x, a.tokens, a.cin, x_stride, kHalf, sq::kTileRows)) return rc;
+    g.codes = reinterpret_cast<const uint8_t *>(a.codes);
+    g.code_pitch = pitch;
+    g.code_bytes = pitch * a.cout;
+    g.code_rows = a.cout;
+    g.code_row_bytes = static_cast<int32_t>(pitch);
+    g.vector = code_vector;
     return launch_gemm_cols<sq::kForward, kKind, kHalf>(map, g, device, sms, stream);
 }
 
@@ -250,8 +340,10 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
 
 // What the gradients need of dy * act'(zhat): parts of the workspace, each [tokens][pitch] bf16.
 struct SlopePlan {
-    bool dzs = false, dz = false, any = false;
-    int64_t pitch = 0, bytes = 0;
+    bool dzs = false, dz = false, any = false, dense = false;
+    int64_t pitch = 0, slope_bytes = 0;
+    int64_t wide_bytes = 0;   // behind them: the codes, then the input as 16-bit floats
+    int64_t bytes = 0;
 };
 
 SlopePlan slope_plan(const squant_linear_grad_args &a)
@@ -261,7 +353,11 @@ SlopePlan slope_plan(const squant_linear_grad_args &a)
     s.dzs = a.dx && a.tokens > 0;
     s.dz = a.dweight && a.tokens > 0 && (a.act != SQUANT_ACT_NONE || !rows_on_vectors(a.dy, a.dy_stride, a.tokens));
     s.any = s.dzs || s.dz || a.dbias || a.dscales;
-    s.bytes = (s.dzs + s.dz) * a.tokens * s.pitch * 2;
+    s.slope_bytes = (s.dzs + s.dz) * a.tokens * s.pitch * 2;
+    s.dense = s.dzs && a.tokens > kFusedTokens;
+    const int64_t row = up(a.cin, 8) * 2;
+    s.wide_bytes = std::max(s.dense ? a.cout * row : 0, a.dweight ? a.tokens * row : 0);
+    s.bytes = s.slope_bytes + s.wide_bytes;
     return s;
 }
 
@@ -365,23 +461,13 @@ int squant_checkpoint_restore(const squant_checkpoint_data *from, int64_t rows, 
     if (rows == 0) return SQUANT_OK;
     if (!out || !from->codes || !from->exps) return SQUANT_ERR_NULL;
     if (misaligned(out, 2) || bad_checkpoint(*from)) return SQUANT_ERR_ALIGN;
-    sq::RowArgs r{};
-    r.out = static_cast<uint16_t *>(out);
-    r.out_stride = stride;
-    r.codes = reinterpret_cast<uint8_t *>(from->codes);
-    r.exps = from->exps;
-    r.code_pitch = up(features, 32);
-    r.exps_pitch = r.code_pitch / 32;
-    r.pieces = static_cast<uint32_t>(r.code_pitch / 8);
-    r.features = features;
-    r.vector = rows_on_vectors(out, stride, rows);
-    return launch_rows(RowKernel::kRestore, r, rows, static_cast<cudaStream_t>(cuda_stream));
+    return restore(*from, rows, features, out, stride, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int64_t squant_linear_workspace(const squant_linear_args *args)
 {
     if (int rc = check(args)) return rc;
-    return x_needs_copy(*args) ? args->tokens * up(args->cin, 8) * 2 : 0;
+    return forward_plan(*args).bytes;
 }
 
 int squant_linear(const squant_linear_args *args, void *cuda_stream)
@@ -389,8 +475,8 @@ int squant_linear(const squant_linear_args *args, void *cuda_stream)
     if (int rc = check(args)) return rc;
     const squant_linear_args &a = *args;
     if (a.tokens == 0) return SQUANT_OK;
-    if (x_needs_copy(a) && (!a.workspace || misaligned(a.workspace, 16) || a.workspace_bytes < a.tokens * up(a.cin, 8) * 2))
-        return SQUANT_ERR_WORKSPACE;
+    const int64_t need = forward_plan(a).bytes;
+    if (need && (!a.workspace || misaligned(a.workspace, 16) || a.workspace_bytes < need)) return SQUANT_ERR_WORKSPACE;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool half = a.dtype == SQUANT_FP16;
     if (a.flags & SQUANT_FLAG_PACK_INT4) return half ? forward<sq::kInt4, true>(a, stream) : forward<sq::kInt4, false>(a, stream);
@@ -416,49 +502,46 @@ int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_strea
     uint16_t *dz = plan.dz ? static_cast<uint16_t *>(a.workspace) + (plan.dzs ? a.tokens * plan.pitch : 0) : nullptr;
     if (plan.any)
         if (int rc = slope(a, plan, dzs, dz, stream)) return rc;
+    uint8_t *wide = static_cast<uint8_t *>(a.workspace) + plan.slope_bytes;
     if (plan.dzs) {
         const bool packed = a.flags & SQUANT_FLAG_PACK_INT4;
-        CUtensorMap map;
-        if (int rc = matrix_map(map, dzs, a.tokens, a.cout, plan.pitch, false, sq::kTileRows)) return rc;
         sq::GemmArgs g{};
-        g.codes = reinterpret_cast<const uint8_t *>(a.codes);
-        g.code_pitch = packed ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
-        g.code_bytes = g.code_pitch * a.cout;
-        g.code_rows = a.cout;
-        g.code_row_bytes = static_cast<int32_t>(g.code_pitch);
-        g.vector = !misaligned(a.codes, 16) && g.code_pitch % 16 == 0;
         g.rows = static_cast<int32_t>(a.tokens);
         g.cols = a.cin;
         g.depth = a.cout;
         g.out = static_cast<uint16_t *>(a.dx);
         g.out_stride = a.dx_stride;
         g.out_vector = rows_on_vectors(a.dx, a.dx_stride, a.tokens);
-        if (int rc = packed ? launch_gemm_cols<sq::kInputGrad, sq::kInt4, false>(map, g, device, sms, stream)
-                            : launch_gemm_cols<sq::kInputGrad, sq::kInt8, false>(map, g, device, sms, stream)) return rc;
+        if (plan.dense) {
+            if (int rc = expand(a.codes, a.cout, a.cin, packed, false, wide, stream)) return rc;
+            if (int rc = dense<sq::kInputGrad, false>(dzs, plan.pitch, wide, up(a.cin, 8), g, device, sms, stream)) return rc;
+        } else {
+            CUtensorMap map;
+            if (int rc = matrix_map(map, dzs, a.tokens, a.cout, plan.pitch, false, sq::kTileRows)) return rc;
+            g.codes = reinterpret_cast<const uint8_t *>(a.codes);
+            g.code_pitch = packed ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
+            g.code_bytes = g.code_pitch * a.cout;
+            g.code_rows = a.cout;
+            g.code_row_bytes = static_cast<int32_t>(g.code_pitch);
+            g.vector = !misaligned(a.codes, 16) && g.code_pitch % 16 == 0;
+            if (int rc = packed ? launch_gemm_cols<sq::kInputGrad, sq::kInt4, false>(map, g, device, sms, stream)
+                                : launch_gemm_cols<sq::kInputGrad, sq::kInt8, false>(map, g, device, sms, stream)) return rc;
+        }
     }
     if (a.dweight) {
         if (a.tokens == 0) {
             SQ_CUDA(cudaMemset2DAsync(a.dweight, 2 * (a.cout == 1 ? a.cin : a.dweight_stride), 0, 2 * static_cast<size_t>(a.cin), a.cout, stream));
             return SQUANT_OK;
         }
-        CUtensorMap map;
-        if (int rc = matrix_map(map, dz ? dz : a.dy, a.tokens, a.cout, dz ? plan.pitch : a.dy_stride, false, sq::kTileDepth)) return rc;
+        if (int rc = restore(a.x, a.tokens, a.cin, wide, up(a.cin, 8), stream)) return rc;
         sq::GemmArgs g{};
-        g.codes = reinterpret_cast<const uint8_t *>(a.x.codes);
-        g.exps = a.x.exps;
-        g.code_pitch = up(a.cin, 32);
-        g.exps_pitch = g.code_pitch / 32;
-        g.code_bytes = g.code_pitch * a.tokens;
-        g.code_rows = static_cast<int32_t>(a.tokens);
-        g.code_row_bytes = static_cast<int32_t>(g.code_pitch);
-        g.vector = 1;
         g.rows = a.cout;
         g.cols = a.cin;
         g.depth = static_cast<int32_t>(a.tokens);
         g.out = static_cast<uint16_t *>(a.dweight);
         g.out_stride = a.dweight_stride;
         g.out_vector = rows_on_vectors(a.dweight, a.dweight_stride, a.cout);
-        if (int rc = launch_gemm_cols<sq::kWeightGrad, sq::kCkpt8, false>(map, g, device, sms, stream)) return rc;
+        if (int rc = dense<sq::kWeightGrad, false>(dz ? dz : a.dy, dz ? plan.pitch : a.dy_stride, wide, up(a.cin, 8), g, device, sms, stream)) return rc;
     }
     return SQUANT_OK;
 }

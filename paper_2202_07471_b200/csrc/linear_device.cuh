@@ -12,7 +12,7 @@
 namespace sq {
 
 enum { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
-enum CodeKind { kInt4 = 0, kInt8 = 1, kCkpt8 = 2 };
+enum CodeKind { kInt4 = 0, kInt8 = 1 };
 
 // Set by a kernel of this file's users that gave up a bounded wait (read and cleared by squant_device_status()).
 static __device__ int g_linear_status = 0;

@@ -17,8 +17,7 @@ enum GemmMode { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
 
 struct GemmArgs {
     const uint8_t *codes;    // coded operand, rows of code_pitch bytes
-    const uint8_t *exps;     // checkpoint exponents, rows of exps_pitch bytes (weight gradient)
-    int64_t code_pitch, exps_pitch;
+    int64_t code_pitch;
     int64_t code_bytes;      // of the whole operand
     int32_t code_rows;       // rows of the coded operand
     int32_t code_row_bytes;  // bytes of a row that may be read
@@ -32,6 +31,7 @@ struct GemmArgs {
     int32_t out_vector;      // rows of the result start on 16 bytes
     // forward only
     const float *scales, *bias;
+    int32_t param_vector;    // scales and bias start on 16 bytes
     const uint16_t *residual;
     int64_t residual_stride;
     int32_t residual_vector;
@@ -79,7 +79,7 @@ __device__ __forceinline__ void piece_place(int piece, int &row, int &sub)
 template <int kMode, int kKind>
 struct CodeCursor {
     static constexpr int kApart = 32 * kConverterWarps / Pieces<kKind>::kPerRow;   // panel rows between a thread's pieces
-    const uint8_t *ptr, *exp;
+    const uint8_t *ptr;
     int row;   // of the operand
     int off;   // byte within the row
 
@@ -96,18 +96,15 @@ struct CodeCursor {
         }
         off = kKind == kInt4 ? first >> 1 : first;
         ptr = p.codes + static_cast<int64_t>(row) * p.code_pitch + off;
-        if (kKind == kCkpt8) exp = p.exps + static_cast<int64_t>(row) * p.exps_pitch + (first >> 5);
     }
-    __device__ __forceinline__ void load(const GemmArgs &p, int i, uint4 &codes, uint32_t &e) const
+    __device__ __forceinline__ void load(const GemmArgs &p, int i, uint4 &codes) const
     {
         const int r = kMode == kForward ? row + i * kApart : row;
         const int along = kMode == kForward ? 0 : i * (kKind == kInt4 ? kApart / 2 : kApart);
         codes = make_uint4(0, 0, 0, 0);
-        e = 0;
         if (r < p.code_rows && off + along < p.code_row_bytes) {
             const uint8_t *q = ptr + (kMode == kForward ? static_cast<int64_t>(i * kApart) * p.code_pitch : along);
             codes = p.vector ? ldg128(q) : load_bytes16(q, p.codes, p.codes + p.code_bytes);
-            if (kKind == kCkpt8) e = __ldg(exp + (along >> 5));
         }
     }
     __device__ __forceinline__ void next(const GemmArgs &p)
@@ -118,13 +115,12 @@ struct CodeCursor {
         } else {
             row += kTileDepth;
             ptr += kTileDepth * p.code_pitch;
-            if (kKind == kCkpt8) exp += kTileDepth * p.exps_pitch;
         }
     }
 };
 
 template <int kKind, bool kHalf>
-__device__ __forceinline__ void store_piece(uint32_t panel, int piece, const uint4 &c, uint32_t e)
+__device__ __forceinline__ void store_piece(uint32_t panel, int piece, const uint4 &c)
 {
     int row, sub;
     piece_place<kKind>(piece, row, sub);
@@ -138,11 +134,6 @@ __device__ __forceinline__ void store_piece(uint32_t panel, int piece, const uin
         } else {
             int8_to_16<kHalf>(w[2 * j], o);
             int8_to_16<kHalf>(w[2 * j + 1], o + 2);
-            if constexpr (kKind == kCkpt8) {
-                const uint32_t scale = e << 7 | e << 23;   // 2^(E - 127) twice in bf16; E = 255: inf, and 0 * inf = NaN
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = mul2_bf16(o[i], scale);
-            }
         }
         const uint32_t chunk = sub * Pieces<kKind>::kChunks + j;
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + ((chunk ^ (row & 7)) << 4)), "r"(o[0]), "r"(o[1]),
@@ -175,10 +166,22 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(acc[i]);
     if constexpr (kMode == kForward) {
+        if (p.param_vector && n == 32) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const int c = i < n ? col + i : col;
-            v[i] = fmaf(v[i], __ldg(p.scales + c), p.bias ? __ldg(p.bias + c) : 0.0f);
+            for (int j = 0; j < 8; ++j) {
+                const float4 s = __ldg(reinterpret_cast<const float4 *>(p.scales + col) + j);
+                const float4 b = p.bias ? __ldg(reinterpret_cast<const float4 *>(p.bias + col) + j) : make_float4(0, 0, 0, 0);
+                v[4 * j] = fmaf(v[4 * j], s.x, b.x);
+                v[4 * j + 1] = fmaf(v[4 * j + 1], s.y, b.y);
+                v[4 * j + 2] = fmaf(v[4 * j + 2], s.z, b.z);
+                v[4 * j + 3] = fmaf(v[4 * j + 3], s.w, b.w);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int c = i < n ? col + i : col;
+                v[i] = fmaf(v[i], __ldg(p.scales + c), p.bias ? __ldg(p.bias + c) : 0.0f);
+            }
         }
         if (p.z_codes) {
             float a = 0.0f;
@@ -302,21 +305,20 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         constexpr int kAhead = Pieces<kKind>::kAhead;
         const int tid = threadIdx.x - 128;
         uint4 codes[kAhead][kMine];
-        uint32_t exps[kAhead][kMine];
         CodeCursor<kMode, kKind> cursor;
         int64_t load_tile = blockIdx.x;
         int load_step = 0;
-        auto load = [&](uint4 (&c)[kMine], uint32_t (&e)[kMine]) {
+        auto load = [&](uint4 (&c)[kMine]) {
             if (load_tile >= p.tiles) return;
             if (load_step == 0) cursor.start(p, tid, static_cast<int>(load_tile / p.row_tiles) * kCols);
 #pragma unroll
             for (int i = 0; i < kMine; ++i)
-                if (kPieces % kThreads == 0 || tid < kPieces) cursor.load(p, i, c[i], e[i]);
+                if (kPieces % kThreads == 0 || tid < kPieces) cursor.load(p, i, c[i]);
             cursor.next(p);
             if (++load_step == steps) { load_step = 0; load_tile += gridDim.x; }
         };
 #pragma unroll
-        for (int d = 0; d < kAhead; ++d) load(codes[d], exps[d]);
+        for (int d = 0; d < kAhead; ++d) load(codes[d]);
         const int64_t my_tiles = blockIdx.x < p.tiles ? (p.tiles - 1 - blockIdx.x) / gridDim.x + 1 : 0;
         const int64_t total = my_tiles * steps;
         bool ok = true;
@@ -331,11 +333,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
 #pragma unroll
                         for (int i = 0; i < kMine; ++i)
                             if (kPieces % kThreads == 0 || tid < kPieces)
-                                store_piece<kKind, kHalf>(smem_b + s * S::kBytesB, tid + i * kThreads, codes[d][i], exps[d][i]);
+                                store_piece<kKind, kHalf>(smem_b + s * S::kBytesB, tid + i * kThreads, codes[d][i]);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                         if (lane == 0) bar_arrive(full_b(s));
-                        load(codes[d], exps[d]);
+                        load(codes[d]);
                         if (++s == S::kStages) { s = 0; parity ^= 1; }
                     }
                 }
@@ -353,12 +355,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
                     if (!ok) break;
                     bar_expect(full_a(s), S::kBytesA);
                     const uint32_t dst = smem_a + s * S::kBytesA;
-                    if (kMode == kWeightGrad) {   // two panels of 64 columns, 64 rows of the contraction each
-                        tma_2d(dst, &map, row0, k * kTileDepth, full_a(s));
-                        tma_2d(dst + 8192, &map, row0 + 64, k * kTileDepth, full_a(s));
-                    } else {
-                        tma_2d(dst, &map, k * kTileDepth, row0, full_a(s));
-                    }
+                    tma_2d(dst, &map, k * kTileDepth, row0, full_a(s));
                     if (issued < S::kStages) ++issued;
                     if (++s == S::kStages) { s = 0; parity ^= 1; }
                 }
@@ -371,9 +368,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         }
     } else if (lane == 0) {
         constexpr uint32_t kIdesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) |
-                                    (kMode == kWeightGrad ? 1u << 15 : 0u) | (kMode != kForward ? 1u << 16 : 0u) |
+                                    (kMode != kForward ? 1u << 16 : 0u) |
                                     (static_cast<uint32_t>(kCols >> 3) << 17) | (static_cast<uint32_t>(kTileRows >> 4) << 24);
-        constexpr uint32_t kStepA = kMode == kWeightGrad ? 2048 : 32, kStepB = kMode == kForward ? 32 : 2048;
+        constexpr uint32_t kStepA = 32, kStepB = kMode == kForward ? 32 : 2048;
         bool ok = true;
         int s = 0, n = 0;
         uint32_t parity = 0;
@@ -390,7 +387,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
                 const uint32_t at = smem_a + s * S::kBytesA, bt = smem_b + s * S::kBytesB;
 #pragma unroll
                 for (int i = 0; i < kTileDepth / 16; ++i)
-                    mma_f16(tmem + a * kCols, smem_desc(at + i * kStepA, kMode == kWeightGrad ? 8192 : 16),
+                    mma_f16(tmem + a * kCols, smem_desc(at + i * kStepA, 16),
                             smem_desc(bt + i * kStepB, kMode == kForward ? 16 : 8192), kIdesc, k > 0 || i > 0);
                 mma_commit(empty(s));
                 last_s = s;

@@ -118,6 +118,50 @@ static __global__ void __launch_bounds__(kRowThreads) restore_kernel(const RowAr
     }
 }
 
+// Codes to 16-bit floats, eight a thread and piece: rows of `code_pitch` bytes to rows that start on 16 bytes.
+// vector: every row of codes starts on a piece's bytes.
+template <int kKind, bool kHalf>
+static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArgs p)
+{
+    constexpr int kBytes = kKind == kInt4 ? 4 : 8;   // of a piece
+    const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
+    uint2 c[kRowPieces];
+    uint32_t row[kRowPieces], piece[kRowPieces];
+#pragma unroll
+    for (int i = 0; i < kRowPieces; ++i) {
+        const uint32_t at = first + i * kRowThreads;
+        row[i] = at / p.pieces;
+        piece[i] = at - row[i] * p.pieces;
+        c[i] = make_uint2(0, 0);
+        if (at < total) {
+            const uint8_t *q = p.codes + row[i] * p.code_pitch + piece[i] * kBytes;
+            if (p.vector) {
+                if (kKind == kInt4) c[i].x = __ldg(reinterpret_cast<const uint32_t *>(q));
+                else c[i] = __ldg(reinterpret_cast<const uint2 *>(q));
+            } else {
+                const int left = static_cast<int>(p.code_pitch - piece[i] * kBytes);
+                uint32_t w[2] = {0, 0};
+#pragma unroll
+                for (int b = 0; b < kBytes; ++b)
+                    if (b < left) w[b >> 2] |= static_cast<uint32_t>(__ldg(q + b)) << (8 * (b & 3));
+                c[i] = make_uint2(w[0], w[1]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kRowPieces; ++i) {
+        if (first + i * kRowThreads >= total) continue;
+        uint32_t o[4];
+        if constexpr (kKind == kInt4) {
+            int4_to_16<kHalf>(c[i].x, o);
+        } else {
+            int8_to_16<kHalf>(c[i].x, o);
+            int8_to_16<kHalf>(c[i].y, o + 2);
+        }
+        *reinterpret_cast<uint4 *>(p.out + row[i] * p.out_stride + piece[i] * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
 // Rows that start anywhere to rows that start on 16 bytes, which TMA can read (the elements behind a row's end become 0).
 static __global__ void __launch_bounds__(kRowThreads) align_kernel(const RowArgs p)
 {
