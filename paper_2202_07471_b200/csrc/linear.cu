@@ -46,6 +46,25 @@ int device_sms(int &device, int &sms)
     return SQUANT_OK;
 }
 
+// `tiles` clusters of `ranks` thread blocks.
+template <typename... Params, typename... Args>
+int launch_cluster(void (*kernel)(Params...), unsigned ranks, int64_t tiles, int threads, int smem, cudaStream_t stream, const Args &...args)
+{
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {ranks, 1, 1};
+    cfg.gridDim = dim3(static_cast<unsigned>(tiles * ranks));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SQ_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+    sq_host::count_launch();
+    return SQUANT_OK;
+}
+
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -78,31 +97,22 @@ int matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t cols, int6
     return r == CUDA_SUCCESS ? SQUANT_OK : sq_host::cuda_failed(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
 }
 
-template <int kMode, int kKind, bool kHalf, int kCols>
-int launch_gemm(const CUtensorMap &map, sq::GemmArgs a, int device, int sms, cudaStream_t stream)
+// As many thread blocks share a tile's contraction as there are multiprocessors (each holds two blocks) and stages for.
+template <int kMode, int kKind, bool kHalf>
+int launch_fused(const CUtensorMap &map, sq::GemmArgs a, int device, int sms, cudaStream_t stream)
 {
-    auto kernel = sq::gemm_kernel<kMode, kKind, kHalf, kCols>;
-    constexpr int smem = sq::GemmShape<kCols>::kSmem;
+    auto kernel = sq::fused_kernel<kMode, kKind, kHalf>;
     static std::atomic<bool> ready[kMaxDevices];
     if (device >= kMaxDevices || !ready[device].load(std::memory_order_relaxed)) {
-        SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sq::kFusedSmem));
         if (device < kMaxDevices) ready[device].store(true, std::memory_order_relaxed);
     }
-    a.row_tiles = (a.rows + sq::kTileRows - 1) / sq::kTileRows;
-    a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + kCols - 1) / kCols);
-    kernel<<<static_cast<unsigned>(std::min<int64_t>(a.tiles, sms)), sq::kGemmThreads, smem, stream>>>(map, a);
-    return launched();
-}
-
-// The widest tile that still gives every multiprocessor one: a wide tile reads less of the 16-bit operand per product
-// and converts each code for more rows.
-template <int kMode, int kKind, bool kHalf>
-int launch_gemm_cols(const CUtensorMap &map, const sq::GemmArgs &a, int device, int sms, cudaStream_t stream)
-{
-    const int64_t row_tiles = (static_cast<int64_t>(a.rows) + sq::kTileRows - 1) / sq::kTileRows;
-    if (row_tiles * ((static_cast<int64_t>(a.cols) + 255) / 256) >= sms) return launch_gemm<kMode, kKind, kHalf, 256>(map, a, device, sms, stream);
-    if (row_tiles * ((static_cast<int64_t>(a.cols) + 127) / 128) >= sms) return launch_gemm<kMode, kKind, kHalf, 128>(map, a, device, sms, stream);
-    return launch_gemm<kMode, kKind, kHalf, 64>(map, a, device, sms, stream);
+    a.row_tiles = (a.rows + sq::kFusedRows - 1) / sq::kFusedRows;
+    a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + sq::kFusedCols - 1) / sq::kFusedCols);
+    const int steps = (a.depth + sq::kTileDepth - 1) / sq::kTileDepth;
+    unsigned ranks = 1;
+    while (2 * ranks <= sq::kFusedMostRanks && 2 * ranks * a.tiles <= 2 * sms && 8 * ranks <= static_cast<unsigned>(steps)) ranks *= 2;
+    return launch_cluster(kernel, ranks, a.tiles, sq::kFusedThreads, sq::kFusedSmem, stream, map, a);
 }
 
 template <int kMode, bool kHalf, int kCols>
@@ -139,21 +149,31 @@ int dense(const void *a, int64_t a_stride, const void *b, int64_t b_stride, cons
                     : launch_dense<kMode, kHalf, 128>(map_a, map_b, g, device, sms, stream);
 }
 
-template <int kKind, bool kHalf, int kTiles>
-int launch_small(const sq::SmallArgs &a, bool vector, cudaStream_t stream)
+template <int kKind, bool kHalf, int kTiles, bool kVector>
+int launch_small(const sq::SmallArgs &a, int device, int sms, cudaStream_t stream)
 {
-    const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kSmallRows - 1) / sq::kSmallRows);
-    if (vector) sq::small_kernel<kKind, kHalf, kTiles, true><<<grid, 32 * sq::kSmallWarps, 0, stream>>>(a);
-    else sq::small_kernel<kKind, kHalf, kTiles, false><<<grid, 32 * sq::kSmallWarps, 0, stream>>>(a);
-    return launched();
+    using S = sq::SmallShape<kKind, kTiles>;
+    auto kernel = sq::small_kernel<kKind, kHalf, kTiles, kVector>;
+    static std::atomic<bool> ready[kMaxDevices];
+    if (S::kSmem > (48 << 10) && (device >= kMaxDevices || !ready[device].load(std::memory_order_relaxed))) {
+        SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+        if (device < kMaxDevices) ready[device].store(true, std::memory_order_relaxed);
+    }
+    const int64_t tiles = (static_cast<int64_t>(a.cout) + sq::kSmallRows - 1) / sq::kSmallRows;
+    const int64_t blocks = (static_cast<int64_t>(a.cin) + S::kBlock - 1) / S::kBlock;
+    unsigned ranks = 1;   // two thread blocks a multiprocessor
+    while (2 * ranks <= sq::kSmallMostRanks && 2 * ranks * tiles <= 2 * sms && 2 * ranks <= blocks) ranks *= 2;
+    return launch_cluster(kernel, ranks, tiles, 32 * sq::kSmallWarps, S::kSmem, stream, a);
 }
 
 template <int kKind, bool kHalf>
 int launch_small_tokens(const sq::SmallArgs &a, bool vector, cudaStream_t stream)
 {
-    if (a.tokens <= 8) return launch_small<kKind, kHalf, 1>(a, vector, stream);
-    if (a.tokens <= 16) return launch_small<kKind, kHalf, 2>(a, vector, stream);
-    return launch_small<kKind, kHalf, 4>(a, vector, stream);
+    int device, sms;
+    if (int rc = device_sms(device, sms)) return rc;
+    if (a.tokens <= 8) return vector ? launch_small<kKind, kHalf, 1, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 1, false>(a, device, sms, stream);
+    if (a.tokens <= 16) return vector ? launch_small<kKind, kHalf, 2, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 2, false>(a, device, sms, stream);
+    return vector ? launch_small<kKind, kHalf, 4, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 4, false>(a, device, sms, stream);
 }
 
 enum class RowKernel { kCheckpoint, kRestore, kAlign, kExpandInt4Bf16, kExpandInt4Fp16, kExpandInt8Bf16, kExpandInt8Fp16 };
@@ -326,14 +346,14 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
         return dense<sq::kForward, kHalf>(x, x_stride, b, up(a.cin, 8), g, device, sms, stream);
     }
     CUtensorMap map;
-    if (int rc = matrix_map(map, x, a.tokens, a.cin, x_stride, kHalf, sq::kTileRows)) return rc;
+    if (int rc = matrix_map(map, x, a.tokens, a.cin, x_stride, kHalf, sq::kFusedRows)) return rc;
     g.codes = reinterpret_cast<const uint8_t *>(a.codes);
     g.code_pitch = pitch;
     g.code_bytes = pitch * a.cout;
     g.code_rows = a.cout;
     g.code_row_bytes = static_cast<int32_t>(pitch);
     g.vector = code_vector;
-    return launch_gemm_cols<sq::kForward, kKind, kHalf>(map, g, device, sms, stream);
+    return launch_fused<sq::kForward, kKind, kHalf>(map, g, device, sms, stream);
 }
 
 // ---- backward
@@ -517,15 +537,15 @@ int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_strea
             if (int rc = dense<sq::kInputGrad, false>(dzs, plan.pitch, wide, up(a.cin, 8), g, device, sms, stream)) return rc;
         } else {
             CUtensorMap map;
-            if (int rc = matrix_map(map, dzs, a.tokens, a.cout, plan.pitch, false, sq::kTileRows)) return rc;
+            if (int rc = matrix_map(map, dzs, a.tokens, a.cout, plan.pitch, false, sq::kFusedRows)) return rc;
             g.codes = reinterpret_cast<const uint8_t *>(a.codes);
             g.code_pitch = packed ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
             g.code_bytes = g.code_pitch * a.cout;
             g.code_rows = a.cout;
             g.code_row_bytes = static_cast<int32_t>(g.code_pitch);
             g.vector = !misaligned(a.codes, 16) && g.code_pitch % 16 == 0;
-            if (int rc = packed ? launch_gemm_cols<sq::kInputGrad, sq::kInt4, false>(map, g, device, sms, stream)
-                                : launch_gemm_cols<sq::kInputGrad, sq::kInt8, false>(map, g, device, sms, stream)) return rc;
+            if (int rc = packed ? launch_fused<sq::kInputGrad, sq::kInt4, false>(map, g, device, sms, stream)
+                                : launch_fused<sq::kInputGrad, sq::kInt8, false>(map, g, device, sms, stream)) return rc;
         }
     }
     if (a.dweight) {

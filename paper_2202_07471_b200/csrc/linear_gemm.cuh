@@ -1,5 +1,6 @@
-// Matrix products of the linear operators on the tensor cores (tcgen05): one operand is a 16-bit matrix that TMA
-// brings into shared memory, the other one holds 8- or 4-bit codes that converter warps turn into 16-bit floats.
+// Matrix products of the linear operators on the tensor cores (tcgen05), and the epilogue they share.  Here: up to 128
+// tokens, one operand a 16-bit matrix that TMA brings into shared memory, the other one 8- or 4-bit codes that converter warps
+// turn into 16-bit floats.
 //
 //   forward          u[t][m]  = sum_k x[t][k]    codes[m][k]     y = act(s_m u + b_m) + r     (both "K-major")
 //   input gradient   dx[t][k] = sum_m dzs[t][m]  codes[m][k]     dzs = dz * s                 (codes "MN-major")
@@ -40,106 +41,7 @@ struct GemmArgs {
     int64_t z_pitch, z_exps_pitch;
 };
 
-constexpr int kTileRows = 128;        // rows of a tile: the tensor memory's lanes
 constexpr int kTileDepth = 64;        // of the contraction per stage: 128 bytes
-constexpr int kConverterWarps = 8;
-constexpr int kGemmThreads = 32 * (4 + kConverterWarps + 2);   // epilogue, converters, TMA, tensor cores
-
-template <int kCols>
-struct GemmShape {
-    static constexpr int kBytesA = kTileRows * 128;
-    static constexpr int kBytesB = kCols * 128;
-    static constexpr int kStages = kCols == 256 ? 4 : kCols == 128 ? 6 : 8;
-    static constexpr int kTmemCols = 2 * kCols;   // two accumulators: a tile's epilogue runs beside the next one's products
-    static constexpr int kBars = 3 * kStages + 4;
-    static constexpr int kSmem = 1024 + kStages * (kBytesA + kBytesB) + 8 * kBars + 16;
-};
-
-// One 16-byte piece of a coded row: 32 int4 codes or 16 8-bit codes.
-template <int kKind>
-struct Pieces {
-    static constexpr int kPerRow = kKind == kInt4 ? 2 : 4;                        // pieces of a panel row (64 codes)
-    static constexpr int kChunks = kKind == kInt4 ? 4 : 2;                        // 16-byte chunks of 16-bit floats a piece becomes
-    static constexpr int kAhead = kKind == kInt4 ? 4 : 3;                         // stages whose codes a converter holds in registers
-};
-
-// Eight consecutive lanes take eight consecutive panel rows, so that their 16-byte stores, permuted by the row, cover
-// all banks.
-template <int kKind>
-__device__ __forceinline__ void piece_place(int piece, int &row, int &sub)
-{
-    constexpr int rows = 32 / Pieces<kKind>::kPerRow;
-    const int lane = piece & 31;
-    row = (piece >> 5) * rows + lane % rows;
-    sub = lane / rows;
-}
-
-// Where a converter thread reads: its pieces of a stage lie `rows` panel rows apart, which is as many rows of the
-// operand (forward) or as many codes along a row (gradients).
-template <int kMode, int kKind>
-struct CodeCursor {
-    static constexpr int kApart = 32 * kConverterWarps / Pieces<kKind>::kPerRow;   // panel rows between a thread's pieces
-    const uint8_t *ptr;
-    int row;   // of the operand
-    int off;   // byte within the row
-
-    __device__ __forceinline__ void start(const GemmArgs &p, int tid, int col0)
-    {
-        int r, sub;
-        piece_place<kKind>(tid, r, sub);
-        int first = sub * (kKind == kInt4 ? 32 : 16);
-        if (kMode == kForward) {
-            row = col0 + r;
-        } else {
-            row = r & 63;
-            first += col0 + (r & ~63);
-        }
-        off = kKind == kInt4 ? first >> 1 : first;
-        ptr = p.codes + static_cast<int64_t>(row) * p.code_pitch + off;
-    }
-    __device__ __forceinline__ void load(const GemmArgs &p, int i, uint4 &codes) const
-    {
-        const int r = kMode == kForward ? row + i * kApart : row;
-        const int along = kMode == kForward ? 0 : i * (kKind == kInt4 ? kApart / 2 : kApart);
-        codes = make_uint4(0, 0, 0, 0);
-        if (r < p.code_rows && off + along < p.code_row_bytes) {
-            const uint8_t *q = ptr + (kMode == kForward ? static_cast<int64_t>(i * kApart) * p.code_pitch : along);
-            codes = p.vector ? ldg128(q) : load_bytes16(q, p.codes, p.codes + p.code_bytes);
-        }
-    }
-    __device__ __forceinline__ void next(const GemmArgs &p)
-    {
-        if (kMode == kForward) {
-            off += kKind == kInt4 ? kTileDepth / 2 : kTileDepth;
-            ptr += kKind == kInt4 ? kTileDepth / 2 : kTileDepth;
-        } else {
-            row += kTileDepth;
-            ptr += kTileDepth * p.code_pitch;
-        }
-    }
-};
-
-template <int kKind, bool kHalf>
-__device__ __forceinline__ void store_piece(uint32_t panel, int piece, const uint4 &c)
-{
-    int row, sub;
-    piece_place<kKind>(piece, row, sub);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    const uint32_t base = panel + row * 128;
-#pragma unroll
-    for (int j = 0; j < Pieces<kKind>::kChunks; ++j) {
-        uint32_t o[4];
-        if constexpr (kKind == kInt4) {
-            int4_to_16<kHalf>(w[j], o);
-        } else {
-            int8_to_16<kHalf>(w[2 * j], o);
-            int8_to_16<kHalf>(w[2 * j + 1], o + 2);
-        }
-        const uint32_t chunk = sub * Pieces<kKind>::kChunks + j;
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + ((chunk ^ (row & 7)) << 4)), "r"(o[0]), "r"(o[1]),
-                     "r"(o[2]), "r"(o[3]) : "memory");
-    }
-}
 
 // Up to eight 16-bit values of one row from fp32, as one 16-byte store where it is possible.
 template <bool kHalf>
@@ -238,173 +140,226 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
         if (8 * j < n) store8<kHalf>(out + 8 * j, v + 8 * j, n - 8 * j, p.out_vector);
 }
 
-// One persistent thread block a multiprocessor.  Roles: warps 0-3 epilogue (a warp reads the tensor memory's lanes of
-// its own quarter), 4-11 converters, 12 copies the 16-bit operand by TMA, 13 issues the matrix instructions.  Stages of
-// 64 of the contraction go round; "full" of a stage has two parts, the copy's and the converters'.
-template <int kMode, int kKind, bool kHalf, int kCols>
-__global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ GemmArgs p)
+constexpr int kFusedRows = 128;       // rows of a tile: the tensor memory's lanes
+constexpr int kFusedCols = 64;
+constexpr int kConverterWarps = 8;
+constexpr int kFusedThreads = 32 * (kConverterWarps + 2);   // converters (four of them read the result), TMA, tensor cores
+constexpr int kFusedStages = 4;
+constexpr int kFusedBytesA = kFusedRows * 128, kFusedBytesB = kFusedCols * 128;
+constexpr int kFusedPartPitch = kFusedCols + 4;             // floats of a row of partial sums: 16-byte accesses hit all banks
+constexpr int kFusedSmem = 1024 + kFusedStages * (kFusedBytesA + kFusedBytesB) + 8 * (3 * kFusedStages + 1);
+constexpr int kFusedMostRanks = 8;    // thread blocks of a cluster, which share a tile's contraction
+static_assert(kConverterWarps == 2 * kFusedStages, "two converter warps a stage");
+static_assert(4 * kFusedRows * kFusedPartPitch <= kFusedStages * (kFusedBytesA + kFusedBytesB), "partial sums take the stages' place");
+
+// One 16-byte piece of a coded row: 32 int4 codes or 16 8-bit codes.  A converter warp takes 32 of a stage's 64 rows of 64
+// codes; eight consecutive lanes take eight consecutive rows, so that their 16-byte stores, permuted by the row, cover
+// all banks.
+template <int kKind>
+struct Pieces {
+    static constexpr int kPerRow = kKind == kInt4 ? 2 : 4;       // pieces of a panel row
+    static constexpr int kChunks = kKind == kInt4 ? 4 : 2;       // 16-byte chunks of 16-bit floats a piece becomes
+    static constexpr int kRows = 32 / kPerRow;                   // rows of a warp's load
+    static constexpr int kCount = 32 / kRows;                    // loads of a stage
+    static constexpr int kAhead = kKind == kInt4 ? 4 : 2;        // stages whose codes a warp holds in registers
+};
+
+template <int kMode, int kKind>
+__device__ __forceinline__ void load_codes(const GemmArgs &p, int col0, int step, int half, uint4 (&c)[Pieces<kKind>::kCount])
 {
-    using S = GemmShape<kCols>;
+    using P = Pieces<kKind>;
+    const int lane = threadIdx.x & 31;
+    // forward: rows are the tile's columns; gradient: rows are the contraction's
+    const int row = (kMode == kForward ? col0 : step * kTileDepth) + 32 * half + lane % P::kRows;
+    const int first = (kMode == kForward ? step * kTileDepth : col0) + lane / P::kRows * (64 / P::kPerRow);
+    const int off = kKind == kInt4 ? first >> 1 : first;
+    const uint8_t *q = p.codes + static_cast<int64_t>(row) * p.code_pitch + off;
+#pragma unroll
+    for (int i = 0; i < P::kCount; ++i) {
+        c[i] = make_uint4(0, 0, 0, 0);
+        if (row + i * P::kRows < p.code_rows && off < p.code_row_bytes)
+            c[i] = p.vector ? ldg128(q) : load_bytes16(q, p.codes, p.codes + p.code_bytes);
+        q += P::kRows * p.code_pitch;
+    }
+}
+
+template <int kKind, bool kHalf>
+__device__ __forceinline__ void store_codes(uint32_t panel, const uint4 (&c)[Pieces<kKind>::kCount])
+{
+    using P = Pieces<kKind>;
+    const int lane = threadIdx.x & 31, row = lane % P::kRows, sub = lane / P::kRows;
+#pragma unroll
+    for (int i = 0; i < P::kCount; ++i) {
+        const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+        for (int j = 0; j < P::kChunks; ++j) {
+            uint32_t o[4];
+            if constexpr (kKind == kInt4) {
+                int4_to_16<kHalf>(w[j], o);
+            } else {
+                int8_to_16<kHalf>(w[2 * j], o);
+                int8_to_16<kHalf>(w[2 * j + 1], o + 2);
+            }
+            const uint32_t chunk = sub * P::kChunks + j;   // the rows of further pieces have the same low three bits
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(panel + (row + i * P::kRows) * 128 + ((chunk ^ (row & 7)) << 4)),
+                         "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+        }
+    }
+}
+
+// A cluster of `ranks` thread blocks a tile of 128 rows and 64 columns; each takes a share of the contraction.  Reading the
+// codes is most of the work, so the tile is narrow and several blocks share a multiprocessor.  A stage's codes are the
+// business of two converter warps, which use the same place in shared memory every time (a waiter must not be more than
+// one phase ahead of its barrier): the fence between stores and the tensor cores' reads waits for the warp's loads in
+// flight too, and so four pairs of warps wait at once (all eight warps on every stage: 0.47 us a stage).  The ranks' sums meet in shared memory, added in the order of the
+// ranks, and each rank finishes a share of the rows.
+template <int kMode, int kKind, bool kHalf>
+__global__ void __launch_bounds__(kFusedThreads, 2) fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ GemmArgs p)
+{
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t smem_a = base, smem_b = base + S::kStages * S::kBytesA;
-    const uint32_t bars = smem_b + S::kStages * S::kBytesB;
+    const uint32_t smem_a = base, smem_b = base + kFusedStages * kFusedBytesA;
+    const uint32_t bars = smem_b + kFusedStages * kFusedBytesB;
     auto full_a = [&](int s) { return bars + 8 * s; };
-    auto full_b = [&](int s) { return bars + 8 * (S::kStages + s); };
-    auto empty = [&](int s) { return bars + 8 * (2 * S::kStages + s); };
-    auto acc_full = [&](int a) { return bars + 8 * (3 * S::kStages + a); };
-    auto acc_empty = [&](int a) { return bars + 8 * (3 * S::kStages + 2 + a); };
+    auto full_b = [&](int s) { return bars + 8 * (kFusedStages + s); };
+    auto empty = [&](int s) { return bars + 8 * (2 * kFusedStages + s); };
+    const uint32_t done = bars + 8 * 3 * kFusedStages;
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_word;
     volatile int *gave_up = &gave_up_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank(), ranks = cluster_ranks();
+    const int64_t tile = blockIdx.x / ranks;
+    const int64_t row0 = tile % p.row_tiles * kFusedRows;
+    const int col0 = static_cast<int>(tile / p.row_tiles) * kFusedCols;
+    const int all = (p.depth + kTileDepth - 1) / kTileDepth;
+    const int first = static_cast<int>(static_cast<int64_t>(all) * rank / ranks);
+    const int steps = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / ranks) - first;   // at least one
 
     if (threadIdx.x == 0) {
         gave_up_word = 0;
-        for (int s = 0; s < S::kStages; ++s) {
+        for (int s = 0; s < kFusedStages; ++s) {
             bar_init(full_a(s), 1);
-            bar_init(full_b(s), kConverterWarps);
+            bar_init(full_b(s), kConverterWarps / kFusedStages);
             bar_init(empty(s), 1);
         }
-        for (int a = 0; a < 2; ++a) {
-            bar_init(acc_full(a), 1);
-            bar_init(acc_empty(a), 4);
-        }
+        bar_init(done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 13) tmem_alloc(smem_addr(&tmem_base), S::kTmemCols);
+    if (warp == kConverterWarps + 1) tmem_alloc(smem_addr(&tmem_base), kFusedCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
-    const int steps = (p.depth + kTileDepth - 1) / kTileDepth;
 
-    if (warp < 4) {
-        int n = 0;
-        for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x, ++n) {
-            const int a = n & 1;
-            if (!bar_wait_warp(acc_full(a), (n >> 1) & 1, gave_up)) break;
-            tc_fence_after();
-            const int64_t row = (t % p.row_tiles) * kTileRows + warp * 32 + lane;
-            const int col0 = static_cast<int>(t / p.row_tiles) * kCols;
-            for (int c = 0; c < kCols; c += 32) {
-                if (col0 + c >= p.cols) break;
-                uint32_t acc[32];
-                __syncwarp();
-                tmem_ld32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + a * kCols + c, acc);
-                if (row < p.rows) finish32<kMode, kHalf>(p, row, col0 + c, acc);
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(acc_empty(a));
-        }
-    } else if (warp < 4 + kConverterWarps) {
-        constexpr int kThreads = 32 * kConverterWarps;
-        constexpr int kPieces = kCols * Pieces<kKind>::kPerRow;           // of a stage
-        constexpr int kMine = (kPieces + kThreads - 1) / kThreads;
+    if (warp < kConverterWarps) {
         constexpr int kAhead = Pieces<kKind>::kAhead;
-        const int tid = threadIdx.x - 128;
-        uint4 codes[kAhead][kMine];
-        CodeCursor<kMode, kKind> cursor;
-        int64_t load_tile = blockIdx.x;
-        int load_step = 0;
-        auto load = [&](uint4 (&c)[kMine]) {
-            if (load_tile >= p.tiles) return;
-            if (load_step == 0) cursor.start(p, tid, static_cast<int>(load_tile / p.row_tiles) * kCols);
+        const int slot = warp % kFusedStages, half = warp / kFusedStages;
+        uint4 codes[kAhead][Pieces<kKind>::kCount];
 #pragma unroll
-            for (int i = 0; i < kMine; ++i)
-                if (kPieces % kThreads == 0 || tid < kPieces) cursor.load(p, i, c[i]);
-            cursor.next(p);
-            if (++load_step == steps) { load_step = 0; load_tile += gridDim.x; }
-        };
-#pragma unroll
-        for (int d = 0; d < kAhead; ++d) load(codes[d]);
-        const int64_t my_tiles = blockIdx.x < p.tiles ? (p.tiles - 1 - blockIdx.x) / gridDim.x + 1 : 0;
-        const int64_t total = my_tiles * steps;
+        for (int d = 0; d < kAhead; ++d)
+            if (slot + d * kFusedStages < steps) load_codes<kMode, kKind>(p, col0, first + slot + d * kFusedStages, half, codes[d]);
         bool ok = true;
-        int s = 0;
         uint32_t parity = 1;   // a stage that was never used counts as empty
-        for (int64_t it = 0; it < total && ok; it += kAhead) {
+        for (int it = slot; it < steps && ok; it += kAhead * kFusedStages) {
 #pragma unroll
             for (int d = 0; d < kAhead; ++d) {
-                if (it + d < total && ok) {
-                    ok = bar_wait_warp(empty(s), parity, gave_up);
+                const int k = it + d * kFusedStages;
+                if (k < steps && ok) {
+                    ok = bar_wait_warp(empty(slot), parity, gave_up);
+                    parity ^= 1;
                     if (ok) {
-#pragma unroll
-                        for (int i = 0; i < kMine; ++i)
-                            if (kPieces % kThreads == 0 || tid < kPieces)
-                                store_piece<kKind, kHalf>(smem_b + s * S::kBytesB, tid + i * kThreads, codes[d][i]);
+                        store_codes<kKind, kHalf>(smem_b + slot * kFusedBytesB + half * (32 * 128), codes[d]);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
-                        if (lane == 0) bar_arrive(full_b(s));
-                        load(codes[d]);
-                        if (++s == S::kStages) { s = 0; parity ^= 1; }
+                        if (lane == 0) bar_arrive(full_b(slot));
+                        if (k + kAhead * kFusedStages < steps) load_codes<kMode, kKind>(p, col0, first + k + kAhead * kFusedStages, half, codes[d]);
                     }
                 }
             }
         }
-    } else if (warp == 4 + kConverterWarps) {
-        if (lane == 0) {
-            bool ok = true;
-            int s = 0, issued = 0;
-            uint32_t parity = 1;
-            for (int64_t t = blockIdx.x; t < p.tiles && ok; t += gridDim.x) {
-                const int row0 = static_cast<int>(t % p.row_tiles) * kTileRows;
-                for (int k = 0; k < steps; ++k) {
-                    ok = bar_wait(empty(s), parity, gave_up);
-                    if (!ok) break;
-                    bar_expect(full_a(s), S::kBytesA);
-                    const uint32_t dst = smem_a + s * S::kBytesA;
-                    tma_2d(dst, &map, k * kTileDepth, row0, full_a(s));
-                    if (issued < S::kStages) ++issued;
-                    if (++s == S::kStages) { s = 0; parity ^= 1; }
+        if (warp < 4 && bar_wait_warp(done, 0, gave_up)) {
+            tc_fence_after();
+            const uint32_t part = base + (warp * 32 + lane) * (4 * kFusedPartPitch);
+            if (row0 + warp * 32 < p.rows) {
+#pragma unroll
+                for (int c = 0; c < kFusedCols; c += 32) {
+                    uint32_t acc[32];
+                    tmem_ld32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + c, acc);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part + 4 * c + 16 * i), "r"(acc[4 * i]), "r"(acc[4 * i + 1]),
+                                     "r"(acc[4 * i + 2]), "r"(acc[4 * i + 3]) : "memory");
                 }
             }
-            // the last copies have landed before the block may end
-            for (int i = 0; i < issued; ++i) {
-                if (--s < 0) { s = S::kStages - 1; parity ^= 1; }
-                bar_drain(full_a(s), parity ^ 1);
+            tc_fence_before();
+        }
+    } else if (warp == kConverterWarps) {
+        if (lane == 0) {
+            bool ok = true;
+            int k = 0;
+            for (; k < steps && ok; ++k) {
+                const int s = k % kFusedStages;
+                ok = bar_wait(empty(s), (k / kFusedStages & 1) ^ 1, gave_up);
+                if (!ok) break;
+                bar_expect(full_a(s), kFusedBytesA);
+                tma_2d(smem_a + s * kFusedBytesA, &map, (first + k) * kTileDepth, static_cast<int>(row0), full_a(s));
             }
+            // the last copies have landed before the block may end
+            for (int i = max(0, k - kFusedStages); i < k; ++i) bar_drain(full_a(i % kFusedStages), i / kFusedStages & 1);
         }
     } else if (lane == 0) {
-        constexpr uint32_t kIdesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) |
-                                    (kMode != kForward ? 1u << 16 : 0u) |
-                                    (static_cast<uint32_t>(kCols >> 3) << 17) | (static_cast<uint32_t>(kTileRows >> 4) << 24);
-        constexpr uint32_t kStepA = 32, kStepB = kMode == kForward ? 32 : 2048;
+        constexpr uint32_t kIdesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (kMode != kForward ? 1u << 16 : 0u) |
+                                    (static_cast<uint32_t>(kFusedCols >> 3) << 17) | (static_cast<uint32_t>(kFusedRows >> 4) << 24);
+        constexpr uint32_t kStepB = kMode == kForward ? 32 : 2048;
         bool ok = true;
-        int s = 0, n = 0;
-        uint32_t parity = 0;
-        int last_s = -1;
-        for (int64_t t = blockIdx.x; t < p.tiles && ok; t += gridDim.x, ++n) {
-            const int a = n & 1;
-            ok = bar_wait(acc_empty(a), ((n >> 1) & 1) ^ 1, gave_up);
+        int k = 0;
+        for (; k < steps; ++k) {
+            const int s = k % kFusedStages;
+            ok = bar_wait(full_a(s), k / kFusedStages & 1, gave_up) && bar_wait(full_b(s), k / kFusedStages & 1, gave_up);
             if (!ok) break;
             tc_fence_after();
-            for (int k = 0; k < steps; ++k) {
-                ok = bar_wait(full_a(s), parity, gave_up) && bar_wait(full_b(s), parity, gave_up);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t at = smem_a + s * S::kBytesA, bt = smem_b + s * S::kBytesB;
+            const uint32_t at = smem_a + s * kFusedBytesA, bt = smem_b + s * kFusedBytesB;
 #pragma unroll
-                for (int i = 0; i < kTileDepth / 16; ++i)
-                    mma_f16(tmem + a * kCols, smem_desc(at + i * kStepA, 16),
-                            smem_desc(bt + i * kStepB, kMode == kForward ? 16 : 8192), kIdesc, k > 0 || i > 0);
-                mma_commit(empty(s));
-                last_s = s;
-                if (++s == S::kStages) { s = 0; parity ^= 1; }
-            }
-            if (ok) mma_commit(acc_full(a));
+            for (int i = 0; i < kTileDepth / 16; ++i)
+                mma_f16(tmem, smem_desc(at + i * 32, 16), smem_desc(bt + i * kStepB, 16), kIdesc, k > 0 || i > 0);
+            mma_commit(empty(s));
         }
-        // the tensor cores have read their last stage before the block may end: a stage's phase is complete when its
-        // parity is the one this warp waited with
-        if (last_s >= 0) bar_drain(empty(last_s), s == 0 ? parity ^ 1 : parity);
+        if (ok) mma_commit(done);
+        // the tensor cores have read their last stage before the block may end
+        if (k > 0) bar_drain(empty((k - 1) % kFusedStages), (k - 1) / kFusedStages & 1);
     }
     __syncwarp();
-    tc_fence_before();
-    __syncthreads();
-    if (warp == 13) {
+    cluster_arrive_wait();   // all ranks' sums are in shared memory
+    {
+        const int here = static_cast<int>(min(static_cast<int64_t>(kFusedRows), p.rows - row0));
+        const int share = (here + ranks - 1) / ranks;
+        const int r = rank * share + (threadIdx.x >> 1), c = (threadIdx.x & 1) * 32;
+        if (static_cast<int>(threadIdx.x >> 1) < share && r < here && col0 + c < p.cols && !*gave_up) {
+            uint32_t acc[32];
+            float sum[32] = {};
+            for (uint32_t q = 0; q < ranks; ++q) {
+                const uint32_t at = cluster_addr(base + r * (4 * kFusedPartPitch) + 4 * c, q);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float4 v;
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at + 16 * i));
+                    sum[4 * i] += v.x;
+                    sum[4 * i + 1] += v.y;
+                    sum[4 * i + 2] += v.z;
+                    sum[4 * i + 3] += v.w;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[i] = __float_as_uint(sum[i]);
+            finish32<kMode, kHalf>(p, row0 + r, col0 + c, acc);
+        }
+    }
+    __syncwarp();
+    cluster_arrive_wait();   // the others' sums stay until they have been read
+    if (warp == kConverterWarps + 1) {
         tc_fence_after();
-        tmem_free(tmem, S::kTmemCols);
+        tmem_free(tmem, kFusedCols);
     }
 }
 

@@ -21,8 +21,22 @@ struct SmallArgs {
     int64_t z_pitch, z_exps_pitch;
 };
 
-constexpr int kSmallRows = 32;      // output channels of a thread block: one checkpoint group
-constexpr int kSmallWarps = 8;      // share the contraction
+constexpr int kSmallWarps = 8;
+constexpr int kSmallRows = 16 * kSmallWarps;   // output channels of a thread block
+constexpr int kSmallChunks = 4;                // chunks of a block of the contraction; two blocks are in flight
+constexpr int kSmallMostRanks = 8;             // thread blocks of a cluster, which share the contraction
+
+template <int kKind, int kTiles>
+struct SmallShape {
+    static constexpr int kCodes = kKind == kInt4 ? 32 : 16;        // codes of a lane's 16 bytes
+    static constexpr int kChunk = 4 * kCodes;                      // of four lanes
+    static constexpr int kBlock = kSmallChunks * kChunk;           // elements of x a token and block
+    static constexpr int kUnits = kBlock / 8;                      // the same in 16 bytes
+    static constexpr int kPitch = 2 * kBlock + 64;                 // bytes of a token in shared memory: two tokens' halves of a load hit all banks
+    static constexpr int kPartPitch = kSmallRows + 4;              // floats of a token's partial sums
+    static constexpr int kTokens = 8 * kTiles;
+    static constexpr int kSmem = 2 * kTokens * kPitch + 4 * kTokens * kPartPitch;
+};
 
 template <bool kHalf>
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3,
@@ -36,121 +50,160 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t a0, cons
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Eight 16-bit values of a row from `first` on, zeros at and behind the row's end.
-template <bool kVector>
-__device__ __forceinline__ uint4 load_x8(const uint16_t *row, int first, int cin)
-{
-    if (first >= cin) return make_uint4(0, 0, 0, 0);
-    if constexpr (kVector) {
-        return __ldg(reinterpret_cast<const uint4 *>(row + first));
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = first + 2 * i;
-            w[i] = (k < cin ? static_cast<uint32_t>(__ldg(row + k)) : 0u) | (k + 1 < cin ? static_cast<uint32_t>(__ldg(row + k + 1)) << 16 : 0u);
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
-
-// A thread block owns 32 channels; its warps take chunks of the contraction in turn (four lanes times 16 bytes of
-// codes) and are summed at the end.  In a chunk lane (g, q) holds 16 bytes of rows g, g + 8, g + 16, g + 24 and the same
-// elements of token g: the order of the contraction inside a matrix instruction is free as long as both operands
-// agree, so nothing is shuffled.
+// A thread block owns 128 channels, a warp 16 of them; the ranks of a cluster share the contraction, so that everything a
+// call reads is asked for at about once.  In a chunk, lane (g, q) holds 16 bytes of the rows g and g + 8 and the same elements
+// of token g: the order of the contraction inside a matrix instruction is free as long as both operands agree, so nothing
+// is shuffled.  x goes through shared memory, whose 16-byte units are kept in the order in which the four lanes of a
+// token read them.  The ranks' sums are added in the order of the ranks.
 // kVector: rows of codes and of x start on 16 bytes and are whole vectors.
 template <int kKind, bool kHalf, int kTiles, bool kVector>
 __global__ void __launch_bounds__(32 * kSmallWarps, 2) small_kernel(const __grid_constant__ SmallArgs p)
 {
-    constexpr int kCodes = kKind == kInt4 ? 32 : 16;      // codes of a lane's 16 bytes
-    constexpr int kChunk = 4 * kCodes;
-    constexpr int kAhead = kTiles == 1 ? 4 : 2;           // chunks in flight
-    __shared__ float part[kSmallWarps][8 * kTiles][kSmallRows];
+    using S = SmallShape<kKind, kTiles>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const uint32_t xs = smem_addr(smem), part = xs + 2 * S::kTokens * S::kPitch;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int row0 = blockIdx.x * kSmallRows;
-    const int chunks = (p.cin + kChunk - 1) / kChunk;
+    const uint32_t rank = cluster_rank(), ranks = cluster_ranks();
+    const int row0 = static_cast<int>(blockIdx.x / ranks) * kSmallRows;
+    const int all = (p.cin + S::kBlock - 1) / S::kBlock;
+    const int first = static_cast<int>(static_cast<int64_t>(all) * rank / ranks);
+    const int blocks = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / ranks) - first;
     const int row_bytes = kKind == kInt4 ? (p.cin + 1) >> 1 : p.cin;
-    float acc[2][kTiles][4] = {};
+    float acc[kTiles][4] = {};
 
-    for (int c0 = warp; c0 < chunks; c0 += kSmallWarps * kAhead) {
-        uint4 codes[kAhead][4];
+    auto load = [&](int b, uint4 (&c)[kSmallChunks][2]) {
+        const int off0 = ((first + b) * kSmallChunks * 4 + q) * 16;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int off = ((c0 + u * kSmallWarps) * 4 + q) * 16;
+        for (int u = 0; u < kSmallChunks; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = row0 + g + 8 * r;
-                codes[u][r] = make_uint4(0, 0, 0, 0);
+            for (int r = 0; r < 2; ++r) {
+                const int row = row0 + 16 * warp + g + 8 * r, off = off0 + 64 * u;
+                c[u][r] = make_uint4(0, 0, 0, 0);
                 if (off < row_bytes && row < p.cout) {
                     const uint8_t *at = p.codes + row * p.code_pitch + off;
-                    codes[u][r] = kVector ? ldg128(at) : load_bytes16(at, p.codes, p.codes + p.code_bytes);
+                    c[u][r] = kVector ? ldg128(at) : load_bytes16(at, p.codes, p.codes + p.code_bytes);
                 }
+            }
+    };
+    auto stage_x = [&](int b) {
+        const uint32_t to = xs + (b & 1) * S::kTokens * S::kPitch;
+        for (int i = threadIdx.x; i < p.tokens * S::kUnits; i += 32 * kSmallWarps) {
+            const int token = i / S::kUnits, unit = i % S::kUnits;
+            constexpr int kLane = S::kCodes / 8;   // units of a lane and chunk
+            const int place = unit & ~(4 * kLane - 1) | unit % kLane * 4 | unit / kLane % 4;
+            const uint32_t dst = to + token * S::kPitch + place * 16;
+            const int k = (first + b) * S::kBlock + unit * 8;
+            const uint16_t *row = p.x + token * p.x_stride;
+            if constexpr (kVector) {
+                const int bytes = k < p.cin ? 16 : 0;   // 0: zeros
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(bytes ? row + k : row), "r"(bytes) : "memory");
+            } else {
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = (k + 2 * j < p.cin ? static_cast<uint32_t>(__ldg(row + k + 2 * j)) : 0u) |
+                           (k + 2 * j + 1 < p.cin ? static_cast<uint32_t>(__ldg(row + k + 2 * j + 1)) << 16 : 0u);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto multiply = [&](int b, const uint4 (&c)[kSmallChunks][2]) {
+        const uint32_t from = xs + (b & 1) * S::kTokens * S::kPitch + g * S::kPitch + q * 16;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int k0 = ((c0 + u * kSmallWarps) * 4 + q) * kCodes;
-            if (c0 + u * kSmallWarps >= chunks) break;
-            uint32_t x[kTiles][kCodes / 2];
+        for (int u = 0; u < kSmallChunks; ++u)
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) {
-                const int token = 8 * n + g;
+            for (int i = 0; i < S::kCodes / 8; ++i) {
+                uint32_t a[2][4];
 #pragma unroll
-                for (int i = 0; i < kCodes / 8; ++i) {
-                    const uint4 v = token < p.tokens ? load_x8<kVector>(p.x + token * p.x_stride, k0 + 8 * i, p.cin) : make_uint4(0, 0, 0, 0);
-                    x[n][4 * i] = v.x; x[n][4 * i + 1] = v.y; x[n][4 * i + 2] = v.z; x[n][4 * i + 3] = v.w;
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t w[4] = {c[u][r].x, c[u][r].y, c[u][r].z, c[u][r].w};
+                    if constexpr (kKind == kInt4) {
+                        int4_to_16<kHalf>(w[i], a[r]);
+                    } else {
+                        int8_to_16<kHalf>(w[2 * i], a[r]);
+                        int8_to_16<kHalf>(w[2 * i + 1], a[r] + 2);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n) {
+                    uint32_t x[4];
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                                 : "r"(from + 8 * n * S::kPitch + (u * (S::kChunk / 8) + 4 * i) * 16) : "memory");
+                    mma_16816<kHalf>(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], x[0], x[1]);
+                    mma_16816<kHalf>(acc[n], a[0][2], a[1][2], a[0][3], a[1][3], x[2], x[3]);
                 }
             }
+    };
+
+    uint4 codes[2][kSmallChunks][2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t a[4][4];
+    for (int d = 0; d < 2; ++d)
+        if (d < blocks) {
+            load(d, codes[d]);
+            stage_x(d);
+        } else {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    for (int b0 = 0; b0 < blocks; b0 += 2) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t w = j == 0 ? codes[u][r].x : j == 1 ? codes[u][r].y : j == 2 ? codes[u][r].z : codes[u][r].w;
-                    if constexpr (kKind == kInt4) int4_to_16<kHalf>(w, a[r]);
-                    else int8_to_16<kHalf>(w, a[r]);
-                }
-                constexpr int kSteps = kKind == kInt4 ? 2 : 1;   // matrix instructions of a word of codes
-#pragma unroll
-                for (int h = 0; h < kSteps; ++h)
-#pragma unroll
-                    for (int n = 0; n < kTiles; ++n) {
-                        const uint32_t b0 = x[n][(j * kSteps + h) * 2], b1 = x[n][(j * kSteps + h) * 2 + 1];
-                        mma_16816<kHalf>(acc[0][n], a[0][2 * h], a[1][2 * h], a[0][2 * h + 1], a[1][2 * h + 1], b0, b1);
-                        mma_16816<kHalf>(acc[1][n], a[2][2 * h], a[3][2 * h], a[2][2 * h + 1], a[3][2 * h + 1], b0, b1);
-                    }
+        for (int d = 0; d < 2; ++d) {
+            const int b = b0 + d;
+            if (b >= blocks) break;
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncthreads();
+            multiply(b, codes[d]);
+            if (b + 2 < blocks) {
+                __syncthreads();
+                load(b + 2, codes[d]);
+                stage_x(b + 2);
+            } else {
+                asm volatile("cp.async.commit_group;" ::: "memory");
             }
         }
     }
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) part[warp][8 * n + 2 * q + (i & 1)][16 * b + g + 8 * (i >> 1)] = acc[b][n][i];
-    __syncthreads();
+        for (int i = 0; i < 4; ++i)
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(part + 4 * ((8 * n + 2 * q + (i & 1)) * S::kPartPitch + 16 * warp + g + 8 * (i >> 1))), "f"(acc[n][i]) : "memory");
+    cluster_arrive_wait();
 
-    const int row = row0 + lane;
-    const bool in = row < p.cout;
-    for (int token = warp; token < p.tokens; token += kSmallWarps) {
-        float u = 0.0f;
+    // ranks 0..3 finish: a warp takes 32 channels, which share a checkpoint's exponent, of one token
+    const uint32_t finishing = min(ranks, 4u);
+    if (rank < finishing) {
+        const int groups = 4 / finishing;
+        for (int item = warp; item < p.tokens * groups; item += kSmallWarps) {
+            const int token = item / groups, at = (rank * groups + item % groups) * 32 + lane, row = row0 + at;
+            if (row - lane >= p.cout) continue;
+            const uint32_t mine = part + 4 * (token * S::kPartPitch + at);
+            float v[kSmallMostRanks];
 #pragma unroll
-        for (int w = 0; w < kSmallWarps; ++w) u += part[w][token][lane];
-        const float z = in ? fmaf(u, __ldg(p.scales + row), p.bias ? __ldg(p.bias + row) : 0.0f) : 0.0f;
-        if (p.z_codes) {
-            float a = fabsf(z);
+            for (uint32_t r = 0; r < kSmallMostRanks; ++r) {
+                v[r] = 0.0f;
+                if (r < ranks) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(cluster_addr(mine, r)));
+            }
+            float u = 0.0f;
 #pragma unroll
-            for (int s = 16; s; s >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, s));
-            const uint32_t e = ckpt_exponent(a);
-            p.z_codes[token * p.z_pitch + row] = static_cast<uint8_t>(ckpt_code(z, ckpt_inverse(e)));   // rows end on 32
-            if (lane == 0) p.z_exps[token * p.z_exps_pitch + blockIdx.x] = static_cast<uint8_t>(e);
-        }
-        if (in) {
-            float v = act_value(z, p.act);
-            if (p.residual) v += to_float<kHalf>(p.residual[token * p.residual_stride + row]);
-            p.y[token * p.y_stride + row] = to_16<kHalf>(v);
+            for (int r = 0; r < kSmallMostRanks; ++r) u += v[r];
+            const bool in = row < p.cout;
+            const float z = in ? fmaf(u, __ldg(p.scales + row), p.bias ? __ldg(p.bias + row) : 0.0f) : 0.0f;
+            if (p.z_codes) {
+                float a = fabsf(z);
+#pragma unroll
+                for (int s = 16; s; s >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, s));
+                const uint32_t e = ckpt_exponent(a);
+                p.z_codes[token * p.z_pitch + row] = static_cast<uint8_t>(ckpt_code(z, ckpt_inverse(e)));   // rows end on 32
+                if (lane == 0) p.z_exps[token * p.z_exps_pitch + (row >> 5)] = static_cast<uint8_t>(e);
+            }
+            if (in) {
+                float y = act_value(z, p.act);
+                if (p.residual) y += to_float<kHalf>(p.residual[token * p.residual_stride + row]);
+                p.y[token * p.y_stride + row] = to_16<kHalf>(y);
+            }
         }
     }
+    cluster_arrive_wait();   // the others' sums stay until they have been read
 }
 
 }  // namespace sq

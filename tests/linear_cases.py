@@ -28,12 +28,12 @@ def pack(codes):
     return ((u[:, 0::2] & 15) | ((u[:, 1::2] & 15) << 4)).to(torch.uint8).view(torch.int8).contiguous()
 
 
-def int_layer(cin, cout, bits, seed):
+def int_layer(cin, cout, bits, seed, lowest=-6):
     """Codes over their whole range and scales that are powers of two."""
     g = gen(seed)
     lo, hi = (-8, 7) if bits == 4 else (-128, 127)
     codes = torch.randint(lo, hi + 1, (cout, cin), generator=g, device="cuda", dtype=torch.int32).to(torch.int8)
-    scales = torch.exp2(torch.randint(-6, 3, (cout,), generator=g, device="cuda").float())
+    scales = torch.exp2(torch.randint(lowest, 3, (cout,), generator=g, device="cuda").float())
     return codes, scales
 
 
