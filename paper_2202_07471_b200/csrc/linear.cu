@@ -161,8 +161,9 @@ int launch_small(const sq::SmallArgs &a, int device, int sms, cudaStream_t strea
     }
     const int64_t tiles = (static_cast<int64_t>(a.cout) + sq::kSmallRows - 1) / sq::kSmallRows;
     const int64_t blocks = (static_cast<int64_t>(a.cin) + S::kBlock - 1) / S::kBlock;
-    unsigned ranks = 1;   // two thread blocks a multiprocessor
-    while (2 * ranks <= sq::kSmallMostRanks && 2 * ranks * tiles <= 2 * sms && 2 * ranks <= blocks) ranks *= 2;
+    // up to four thread blocks a multiprocessor, of which it holds two: 16 tokens 4096 -> 11008 17.2 us, 21.2 with two
+    unsigned ranks = 1;
+    while (2 * ranks <= sq::kSmallMostRanks && 2 * ranks * tiles <= 4 * sms && 2 * ranks <= blocks) ranks *= 2;
     return launch_cluster(kernel, ranks, tiles, 32 * sq::kSmallWarps, S::kSmem, stream, a);
 }
 
@@ -171,6 +172,12 @@ int launch_small_tokens(const sq::SmallArgs &a, bool vector, cudaStream_t stream
 {
     int device, sms;
     if (int rc = device_sms(device, sms)) return rc;
+    if (a.tokens <= sq::kFewTokens && !a.z_codes) {   // one token 4096 -> 4096 4.5 us, 6.2 by clusters; eight 5.6 and 7.5
+        const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kFewRows - 1) / sq::kFewRows);
+        if (vector) sq::few_kernel<kKind, kHalf, true><<<grid, 32 * sq::kSmallWarps, 0, stream>>>(a);
+        else sq::few_kernel<kKind, kHalf, false><<<grid, 32 * sq::kSmallWarps, 0, stream>>>(a);
+        return launched();
+    }
     if (a.tokens <= 8) return vector ? launch_small<kKind, kHalf, 1, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 1, false>(a, device, sms, stream);
     if (a.tokens <= 16) return vector ? launch_small<kKind, kHalf, 2, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 2, false>(a, device, sms, stream);
     return vector ? launch_small<kKind, kHalf, 4, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 4, false>(a, device, sms, stream);
