@@ -64,6 +64,7 @@ class LinearGrads:
 
 
 _ready = None
+_address = {}   # of the library's functions, for the native extension
 
 
 def _lib() -> ctypes.CDLL:
@@ -81,12 +82,32 @@ def _lib() -> ctypes.CDLL:
             getattr(lib, f).restype = ctypes.c_int
         for f in ("squant_linear_workspace", "squant_linear_backward_workspace"):
             getattr(lib, f).restype = i64
+        for f in ("squant_checkpoint", "squant_checkpoint_restore", "squant_linear", "squant_linear_workspace", "squant_linear_backward",
+                  "squant_linear_backward_workspace"):
+            _address[f] = ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
         _ready = lib
     return lib
 
 
+def _native():
+    """The extension that makes whole calls for plain tensors (None: not built, or built with other argument structs)."""
+    m = binding._marshal
+    if (getattr(m, "linear_bytes", None) != ctypes.sizeof(LinearArgs) or getattr(m, "linear_grad_bytes", None) != ctypes.sizeof(LinearGradArgs)
+            or binding._raw_stream is None or not torch.cuda.is_initialized()):
+        return None
+    _lib()
+    return m
+
+
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+def _result(got):
+    """What the extension returned, if it is not an error code."""
+    if type(got) is int:
+        _check(got)
+    return got
 
 
 class _On:
@@ -181,6 +202,12 @@ def _run(fn, need, args, handle, device: torch.device) -> None:
 def squant_checkpoint(x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> Checkpoint:
     """An activation (bfloat16 [..., features]) in 8 bits: 33/64 of its bytes, at most half a step of the largest of 32
     neighbours off (2^-7 of its power of two)."""
+    native = None if stream is not None else _native()
+    if native is not None:
+        device = torch.cuda.current_device()
+        got = native.checkpoint(_address["squant_checkpoint"], binding._raw_stream(device), device, x)
+        if got is not None:
+            return Checkpoint(*_result(got))
     with _On(x.device, stream) as handle:
         if x.dtype != torch.bfloat16:
             raise ValueError("checkpoints are taken of bfloat16 tensors")
@@ -192,6 +219,12 @@ def squant_checkpoint(x: torch.Tensor, stream: Optional[torch.cuda.Stream] = Non
 
 def squant_checkpoint_restore(c: Checkpoint, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The values of a checkpoint as a bfloat16 tensor [rows, features], exactly."""
+    native = None if stream is not None else _native()
+    if native is not None:
+        device = torch.cuda.current_device()
+        got = native.restore(_address["squant_checkpoint_restore"], binding._raw_stream(device), device, c.codes, c.exps, c.features)
+        if got is not None:
+            return _result(got)
     device = c.codes.device
     with _On(device, stream) as handle:
         rows = c.codes.shape[0]
@@ -209,6 +242,14 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
     bias: fp32 [cout]; residual: like the output.  act: "none", "relu", "gelu" (with erf) or "silu".  With `checkpoint`
     returns (y, Checkpoint of the pre-activation [tokens, cout]) for squant_linear_backward.  out: the tensor to write; it may
     be `residual` itself, and must not overlap the other inputs otherwise."""
+    native = None if stream is not None else _native()
+    if native is not None:
+        device = torch.cuda.current_device()
+        got = native.linear(_address["squant_linear"], _address["squant_linear_workspace"], binding._raw_stream(device), device, x, codes, scales,
+                            bias, residual, out, _act(act), pack_int4, checkpoint)
+        if got is not None:
+            got = _result(got)
+            return (got[0], Checkpoint(got[1], got[2], codes.shape[0])) if checkpoint else got
     device = x.device
     with _On(device, stream) as handle:
         if x.dtype not in _TYPES:
@@ -244,6 +285,16 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
     z: checkpoint of the pre-activation (needed with an activation and for dscales); x: checkpoint of the input (needed
     for dweight); cin is needed with pack_int4, whose rows do not tell it.  dweight is the gradient of the weights
     codes * scales: a training loop applies it to the weights that it quantizes."""
+    native = None if stream is not None else _native()
+    if native is not None and (z is None or z.features == dy.shape[-1]) and not (cin is None and pack_int4):
+        device = torch.cuda.current_device()
+        width = codes.shape[-1] if cin is None else cin
+        if x is None or x.features == width:
+            got = native.linear_backward(_address["squant_linear_backward"], _address["squant_linear_backward_workspace"],
+                                         binding._raw_stream(device), device, dy, codes, scales, bias, z and z.codes, z and z.exps, x and x.codes,
+                                         x and x.exps, width, _act(act), pack_int4, dx, dweight, dbias, dscales)
+            if got is not None:
+                return LinearGrads(*_result(got))
     device = dy.device
     with _On(device, stream) as handle:
         if dy.dtype != torch.bfloat16:
