@@ -32,13 +32,6 @@ inline int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // Rows that start on 16 bytes (one row: only its own start counts).
 inline bool rows_on_vectors(const void *p, int64_t stride, int64_t rows) { return !misaligned(p, 16) && (rows <= 1 || stride % 8 == 0); }
 
-int launched()
-{
-    SQ_CUDA(cudaGetLastError());
-    sq_host::count_launch();
-    return SQUANT_OK;
-}
-
 int device_sms(int &device, int &sms)
 {
     SQ_CUDA(cudaGetDevice(&device));
@@ -46,20 +39,22 @@ int device_sms(int &device, int &sms)
     return SQUANT_OK;
 }
 
-// `tiles` clusters of `ranks` thread blocks.
+// Clusters of `cluster` thread blocks; the kernel may be set up while the launch before it ends (wait_for_previous()).
 template <typename... Params, typename... Args>
-int launch_cluster(void (*kernel)(Params...), unsigned ranks, int64_t tiles, int threads, int smem, cudaStream_t stream, const Args &...args)
+int launch(void (*kernel)(Params...), dim3 grid, dim3 cluster, int threads, int smem, cudaStream_t stream, const Args &...args)
 {
     cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {ranks, 1, 1};
-    cfg.gridDim = dim3(static_cast<unsigned>(tiles * ranks));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {cluster.x, cluster.y, 1};
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster.x * cluster.y > 1 ? 2 : 1;
     SQ_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
     sq_host::count_launch();
     return SQUANT_OK;
@@ -112,7 +107,7 @@ int launch_fused(const CUtensorMap &map, sq::GemmArgs a, int device, int sms, cu
     const int steps = (a.depth + sq::kTileDepth - 1) / sq::kTileDepth;
     unsigned ranks = 1;
     while (2 * ranks <= sq::kFusedMostRanks && 2 * ranks * a.tiles <= 2 * sms && 8 * ranks <= static_cast<unsigned>(steps)) ranks *= 2;
-    return launch_cluster(kernel, ranks, a.tiles, sq::kFusedThreads, sq::kFusedSmem, stream, map, a);
+    return launch(kernel, dim3(static_cast<unsigned>(a.tiles * ranks)), dim3(ranks), sq::kFusedThreads, sq::kFusedSmem, stream, map, a);
 }
 
 template <int kMode, bool kHalf, int kCols>
@@ -127,8 +122,7 @@ int launch_dense(const CUtensorMap &map_a, const CUtensorMap &map_b, sq::GemmArg
     }
     a.row_tiles = (a.rows + sq::kPairRows - 1) / sq::kPairRows;
     a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + kCols - 1) / kCols);
-    kernel<<<2 * static_cast<unsigned>(std::min<int64_t>(a.tiles, sms / 2)), sq::kDenseThreads, smem, stream>>>(map_a, map_b, a);
-    return launched();
+    return launch(kernel, dim3(2 * static_cast<unsigned>(std::min<int64_t>(a.tiles, sms / 2))), dim3(2), sq::kDenseThreads, smem, stream, map_a, map_b, a);
 }
 
 // The product of two 16-bit matrices: `a` as gemm's 16-bit operand, `b` [cols][depth] (forward) or [depth][cols].  Tiles of
@@ -164,7 +158,7 @@ int launch_small(const sq::SmallArgs &a, int device, int sms, cudaStream_t strea
     // up to four thread blocks a multiprocessor, of which it holds two: 16 tokens 4096 -> 11008 17.2 us, 21.2 with two
     unsigned ranks = 1;
     while (2 * ranks <= sq::kSmallMostRanks && 2 * ranks * tiles <= 4 * sms && 2 * ranks <= blocks) ranks *= 2;
-    return launch_cluster(kernel, ranks, tiles, 32 * sq::kSmallWarps, S::kSmem, stream, a);
+    return launch(kernel, dim3(static_cast<unsigned>(tiles * ranks)), dim3(ranks), 32 * sq::kSmallWarps, S::kSmem, stream, a);
 }
 
 template <int kKind, bool kHalf>
@@ -174,9 +168,7 @@ int launch_small_tokens(const sq::SmallArgs &a, bool vector, cudaStream_t stream
     if (int rc = device_sms(device, sms)) return rc;
     if (a.tokens <= sq::kFewTokens && !a.z_codes) {   // one token 4096 -> 4096 4.5 us, 6.2 by clusters; eight 5.6 and 7.5
         const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kFewRows - 1) / sq::kFewRows);
-        if (vector) sq::few_kernel<kKind, kHalf, true><<<grid, 32 * sq::kSmallWarps, 0, stream>>>(a);
-        else sq::few_kernel<kKind, kHalf, false><<<grid, 32 * sq::kSmallWarps, 0, stream>>>(a);
-        return launched();
+        return launch(vector ? sq::few_kernel<kKind, kHalf, true> : sq::few_kernel<kKind, kHalf, false>, dim3(grid), dim3(1), 32 * sq::kSmallWarps, 0, stream, a);
     }
     if (a.tokens <= 8) return vector ? launch_small<kKind, kHalf, 1, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 1, false>(a, device, sms, stream);
     if (a.tokens <= 16) return vector ? launch_small<kKind, kHalf, 2, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 2, false>(a, device, sms, stream);
@@ -197,16 +189,17 @@ int launch_rows(RowKernel which, sq::RowArgs a, int64_t rows, cudaStream_t strea
         if (b.codes) b.codes += r * a.code_pitch;
         if (b.exps) b.exps += r * a.exps_pitch;
         const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(b.rows) * b.pieces + sq::kRowThreads * sq::kRowPieces - 1) / (sq::kRowThreads * sq::kRowPieces));
+        void (*kernel)(sq::RowArgs) = nullptr;
         switch (which) {
-            case RowKernel::kCheckpoint: sq::checkpoint_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
-            case RowKernel::kRestore: sq::restore_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
-            case RowKernel::kAlign: sq::align_kernel<<<grid, sq::kRowThreads, 0, stream>>>(b); break;
-            case RowKernel::kExpandInt4Bf16: sq::expand_kernel<sq::kInt4, false><<<grid, sq::kRowThreads, 0, stream>>>(b); break;
-            case RowKernel::kExpandInt4Fp16: sq::expand_kernel<sq::kInt4, true><<<grid, sq::kRowThreads, 0, stream>>>(b); break;
-            case RowKernel::kExpandInt8Bf16: sq::expand_kernel<sq::kInt8, false><<<grid, sq::kRowThreads, 0, stream>>>(b); break;
-            case RowKernel::kExpandInt8Fp16: sq::expand_kernel<sq::kInt8, true><<<grid, sq::kRowThreads, 0, stream>>>(b); break;
+            case RowKernel::kCheckpoint: kernel = sq::checkpoint_kernel; break;
+            case RowKernel::kRestore: kernel = sq::restore_kernel; break;
+            case RowKernel::kAlign: kernel = sq::align_kernel; break;
+            case RowKernel::kExpandInt4Bf16: kernel = sq::expand_kernel<sq::kInt4, false>; break;
+            case RowKernel::kExpandInt4Fp16: kernel = sq::expand_kernel<sq::kInt4, true>; break;
+            case RowKernel::kExpandInt8Bf16: kernel = sq::expand_kernel<sq::kInt8, false>; break;
+            case RowKernel::kExpandInt8Fp16: kernel = sq::expand_kernel<sq::kInt8, true>; break;
         }
-        if (int rc = launched()) return rc;
+        if (int rc = launch(kernel, dim3(grid), dim3(1), sq::kRowThreads, 0, stream, b)) return rc;
     }
     return SQUANT_OK;
 }
@@ -429,19 +422,9 @@ int slope(const squant_linear_grad_args &a, const SlopePlan &plan, uint16_t *dzs
     s.pitch = plan.pitch;
     s.dbias = a.dbias;
     s.dscales = a.dscales;
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[1];
     const unsigned ranks = static_cast<unsigned>(std::min<int64_t>(sq::kSlopeCluster, std::max<int64_t>(1, (a.tokens + 31) / 32)));
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {1, ranks, 1};
-    cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kSlopeCols - 1) / sq::kSlopeCols), ranks);
-    cfg.blockDim = dim3(sq::kRowThreads);
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    SQ_CUDA(cudaLaunchKernelEx(&cfg, sq::slope_kernel, s));
-    sq_host::count_launch();
-    return SQUANT_OK;
+    const unsigned columns = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kSlopeCols - 1) / sq::kSlopeCols);
+    return launch(sq::slope_kernel, dim3(columns, ranks), dim3(1, ranks), sq::kRowThreads, 0, stream, s);
 }
 
 }  // namespace

@@ -177,12 +177,25 @@ __device__ __forceinline__ void int8_to_16(uint32_t w, uint32_t out[2])
     }
 }
 
-// ---------------------------------------------------------------- guarded loads
+// ---------------------------------------------------------------- order of launches
+//
+// Every kernel says at its start that the next launch may come, and waits before its first access to global memory until
+// the launch before it has ended: launched with programmatic stream serialization, a kernel is set up while the one
+// before it ends.  The waits make a chain, so that what follows the last launch follows all of them.
+__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// ---------------------------------------------------------------- loads
+//
+// No read-only (.nc) loads: they may be moved up, past the wait for the launch before.
+
+template <typename T>
+__device__ __forceinline__ T get(const T *p) { return *p; }
 
 __device__ __forceinline__ uint4 ldg128(const void *p)
 {
     uint4 r;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
     return r;
 }
 
@@ -197,11 +210,11 @@ __device__ __noinline__ uint4 load_bytes16(const uint8_t *p, const uint8_t *lo, 
     for (int i = 0; i < 5; ++i) {
         const uint8_t *q = a + 4 * i;
         if (q >= lo && q + 4 <= hi) {
-            w[i] = __ldg(reinterpret_cast<const uint32_t *>(q));
+            w[i] = get(reinterpret_cast<const uint32_t *>(q));
         } else {
             uint32_t v = 0;
             for (int b = 0; b < 4; ++b)
-                if (q + b >= lo && q + b < hi) v |= static_cast<uint32_t>(__ldg(q + b)) << (8 * b);
+                if (q + b >= lo && q + b < hi) v |= static_cast<uint32_t>(get(q + b)) << (8 * b);
             w[i] = v;
         }
     }

@@ -71,8 +71,8 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
         if (p.param_vector && n == 32) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float4 s = __ldg(reinterpret_cast<const float4 *>(p.scales + col) + j);
-                const float4 b = p.bias ? __ldg(reinterpret_cast<const float4 *>(p.bias + col) + j) : make_float4(0, 0, 0, 0);
+                const float4 s = get(reinterpret_cast<const float4 *>(p.scales + col) + j);
+                const float4 b = p.bias ? get(reinterpret_cast<const float4 *>(p.bias + col) + j) : make_float4(0, 0, 0, 0);
                 v[4 * j] = fmaf(v[4 * j], s.x, b.x);
                 v[4 * j + 1] = fmaf(v[4 * j + 1], s.y, b.y);
                 v[4 * j + 2] = fmaf(v[4 * j + 2], s.z, b.z);
@@ -82,7 +82,7 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 const int c = i < n ? col + i : col;
-                v[i] = fmaf(v[i], __ldg(p.scales + c), p.bias ? __ldg(p.bias + c) : 0.0f);
+                v[i] = fmaf(v[i], get(p.scales + c), p.bias ? get(p.bias + c) : 0.0f);
             }
         }
         if (p.z_codes) {
@@ -120,7 +120,7 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
             if (p.residual_vector && n == 32) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint4 q = __ldg(reinterpret_cast<const uint4 *>(r) + j);
+                    const uint4 q = get(reinterpret_cast<const uint4 *>(r) + j);
                     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -131,13 +131,66 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
             } else {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (i < n) v[i] += to_float<kHalf>(__ldg(r + i));
+                    if (i < n) v[i] += to_float<kHalf>(get(r + i));
             }
         }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (8 * j < n) store8<kHalf>(out + 8 * j, v + 8 * j, n - 8 * j, p.out_vector);
+}
+
+// The same for four columns a thread: eight neighbouring lanes hold the 32 channels of an exponent.  All lanes of a warp call
+// it; `valid`: this lane's row is there.
+template <int kMode, bool kHalf>
+__device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col, float (&v)[4], bool valid)
+{
+    const int n = valid ? p.cols - col : 0;   // columns of this thread, if below four
+    if constexpr (kMode == kForward) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = i < n ? fmaf(v[i], get(p.scales + col + i), p.bias ? get(p.bias + col + i) : 0.0f) : 0.0f;
+        if (p.z_codes) {
+            float a = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a = max_nan(a, fabsf(v[i]));
+#pragma unroll
+            for (int s = 1; s <= 4; s <<= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, s));
+            const uint32_t e = ckpt_exponent(a);
+            const float inverse = ckpt_inverse(e);
+            uint32_t w = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w |= static_cast<uint32_t>(ckpt_code(v[i], inverse) & 255) << (8 * i);
+            if (valid && (col & ~31) < p.cols) {   // rows end on 32
+                *reinterpret_cast<uint32_t *>(p.z_codes + row * p.z_pitch + col) = w;
+                if ((col & 31) == 0) p.z_exps[row * p.z_exps_pitch + (col >> 5)] = static_cast<uint8_t>(e);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act_value(v[i], p.act);
+        if (p.residual) {
+            const uint16_t *r = p.residual + row * p.residual_stride + col;
+            if (p.residual_vector && n >= 4) {
+                const uint2 q = get(reinterpret_cast<const uint2 *>(r));
+                v[0] += to_float<kHalf>(static_cast<uint16_t>(q.x));
+                v[1] += to_float<kHalf>(static_cast<uint16_t>(q.x >> 16));
+                v[2] += to_float<kHalf>(static_cast<uint16_t>(q.y));
+                v[3] += to_float<kHalf>(static_cast<uint16_t>(q.y >> 16));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < n) v[i] += to_float<kHalf>(get(r + i));
+            }
+        }
+    }
+    uint16_t *out = p.out + row * p.out_stride + col;
+    if (p.out_vector && n >= 4) {
+        *reinterpret_cast<uint2 *>(out) = make_uint2(to_16x2<kHalf>(v[0], v[1]), to_16x2<kHalf>(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) out[i] = to_16<kHalf>(v[i]);
+    }
 }
 
 constexpr int kFusedRows = 128;       // rows of a tile: the tensor memory's lanes
@@ -251,6 +304,8 @@ __global__ void __launch_bounds__(kFusedThreads, 2) fused_kernel(const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
+    next_may_start();   // not before: a block of the next launch must not take the tensor memory that this one is yet to allocate
+    wait_for_previous();
 
     if (warp < kConverterWarps) {
         constexpr int kAhead = Pieces<kKind>::kAhead;
@@ -331,28 +386,28 @@ __global__ void __launch_bounds__(kFusedThreads, 2) fused_kernel(const __grid_co
     }
     __syncwarp();
     cluster_arrive_wait();   // all ranks' sums are in shared memory
-    {
+    if (warp < kConverterWarps) {   // sixteen threads a row
         const int here = static_cast<int>(min(static_cast<int64_t>(kFusedRows), p.rows - row0));
-        const int share = (here + ranks - 1) / ranks;
-        const int r = rank * share + (threadIdx.x >> 1), c = (threadIdx.x & 1) * 32;
-        if (static_cast<int>(threadIdx.x >> 1) < share && r < here && col0 + c < p.cols && !*gave_up) {
-            uint32_t acc[32];
-            float sum[32] = {};
-            for (uint32_t q = 0; q < ranks; ++q) {
-                const uint32_t at = cluster_addr(base + r * (4 * kFusedPartPitch) + 4 * c, q);
+        const int share = (here + static_cast<int>(ranks) - 1) / static_cast<int>(ranks);
+        const int end = min(here, (static_cast<int>(rank) + 1) * share), c = (threadIdx.x & 15) * 4;
+        const bool whole = !*gave_up;
+        for (int r = static_cast<int>(rank) * share + (threadIdx.x >> 4); r - (lane >> 4) < end && whole; r += 2 * kConverterWarps) {
+            float v[4] = {};
+            if (r < end) {
+                const uint32_t mine = base + r * (4 * kFusedPartPitch) + 4 * c;
+                float part[kFusedMostRanks][4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float4 v;
-                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at + 16 * i));
-                    sum[4 * i] += v.x;
-                    sum[4 * i + 1] += v.y;
-                    sum[4 * i + 2] += v.z;
-                    sum[4 * i + 3] += v.w;
-                }
+                for (uint32_t q = 0; q < kFusedMostRanks; ++q)
+                    if (q < ranks)
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(part[q][0]), "=f"(part[q][1]), "=f"(part[q][2]), "=f"(part[q][3])
+                                     : "r"(cluster_addr(mine, q)));
+#pragma unroll
+                for (uint32_t q = 0; q < kFusedMostRanks; ++q)
+                    if (q < ranks)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] += part[q][i];
             }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) acc[i] = __float_as_uint(sum[i]);
-            finish32<kMode, kHalf>(p, row0 + r, col0 + c, acc);
+            finish4<kMode, kHalf>(p, row0 + r, col0 + c, v, r < end);
         }
     }
     __syncwarp();

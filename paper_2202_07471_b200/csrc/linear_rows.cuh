@@ -14,11 +14,11 @@ constexpr int kRowPieces = 4;    // pieces of eight elements a thread: four load
 // Eight 16-bit values of a row from `first` on, of which n are inside the row.
 __device__ __forceinline__ uint4 load8(const uint16_t *at, int n, bool vector)
 {
-    if (vector && n >= 8) return __ldg(reinterpret_cast<const uint4 *>(at));
+    if (vector && n >= 8) return get(reinterpret_cast<const uint4 *>(at));
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        w[i] = (2 * i < n ? static_cast<uint32_t>(__ldg(at + 2 * i)) : 0u) | (2 * i + 1 < n ? static_cast<uint32_t>(__ldg(at + 2 * i + 1)) << 16 : 0u);
+        w[i] = (2 * i < n ? static_cast<uint32_t>(get(at + 2 * i)) : 0u) | (2 * i + 1 < n ? static_cast<uint32_t>(get(at + 2 * i + 1)) << 16 : 0u);
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ void put8(uint16_t *at, const uint4 &v, int n, bool vector)
@@ -55,6 +55,8 @@ struct RowArgs {
 // Four lanes share a group of 32 features.
 static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const RowArgs p)
 {
+    next_may_start();
+    wait_for_previous();
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint4 v[kRowPieces];
     uint32_t row[kRowPieces];
@@ -89,6 +91,8 @@ static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const Ro
 
 static __global__ void __launch_bounds__(kRowThreads) restore_kernel(const RowArgs p)
 {
+    next_may_start();
+    wait_for_previous();
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint2 c[kRowPieces];
     uint32_t e[kRowPieces], row[kRowPieces];
@@ -101,8 +105,8 @@ static __global__ void __launch_bounds__(kRowThreads) restore_kernel(const RowAr
         c[i] = make_uint2(0, 0);
         e[i] = 0;
         if (at < total) {
-            c[i] = __ldg(reinterpret_cast<const uint2 *>(p.codes + row[i] * p.code_pitch + col[i]));
-            e[i] = __ldg(p.exps + row[i] * p.exps_pitch + (col[i] >> 5));
+            c[i] = get(reinterpret_cast<const uint2 *>(p.codes + row[i] * p.code_pitch + col[i]));
+            e[i] = get(p.exps + row[i] * p.exps_pitch + (col[i] >> 5));
         }
     }
 #pragma unroll
@@ -124,6 +128,8 @@ template <int kKind, bool kHalf>
 static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArgs p)
 {
     constexpr int kBytes = kKind == kInt4 ? 4 : 8;   // of a piece
+    next_may_start();
+    wait_for_previous();
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint2 c[kRowPieces];
     uint32_t row[kRowPieces], piece[kRowPieces];
@@ -136,14 +142,14 @@ static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArg
         if (at < total) {
             const uint8_t *q = p.codes + row[i] * p.code_pitch + piece[i] * kBytes;
             if (p.vector) {
-                if (kKind == kInt4) c[i].x = __ldg(reinterpret_cast<const uint32_t *>(q));
-                else c[i] = __ldg(reinterpret_cast<const uint2 *>(q));
+                if (kKind == kInt4) c[i].x = get(reinterpret_cast<const uint32_t *>(q));
+                else c[i] = get(reinterpret_cast<const uint2 *>(q));
             } else {
                 const int left = static_cast<int>(p.code_pitch - piece[i] * kBytes);
                 uint32_t w[2] = {0, 0};
 #pragma unroll
                 for (int b = 0; b < kBytes; ++b)
-                    if (b < left) w[b >> 2] |= static_cast<uint32_t>(__ldg(q + b)) << (8 * (b & 3));
+                    if (b < left) w[b >> 2] |= static_cast<uint32_t>(get(q + b)) << (8 * (b & 3));
                 c[i] = make_uint2(w[0], w[1]);
             }
         }
@@ -165,6 +171,8 @@ static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArg
 // Rows that start anywhere to rows that start on 16 bytes, which TMA can read (the elements behind a row's end become 0).
 static __global__ void __launch_bounds__(kRowThreads) align_kernel(const RowArgs p)
 {
+    next_may_start();
+    wait_for_previous();
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint4 v[kRowPieces];
 #pragma unroll
@@ -203,6 +211,8 @@ constexpr int kSlopeCluster = 8;    // thread blocks that share the tokens of th
 static __global__ void __launch_bounds__(kRowThreads) slope_kernel(const __grid_constant__ SlopeArgs p)
 {
     namespace cg = cooperative_groups;
+    next_may_start();
+    wait_for_previous();
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, warp = threadIdx.x >> 5;
@@ -213,8 +223,8 @@ static __global__ void __launch_bounds__(kRowThreads) slope_kernel(const __grid_
     float scale[8], bias[8], db[8] = {}, ds[8] = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        scale[i] = i < n ? __ldg(p.scales + col + i) : 1.0f;
-        bias[i] = i < n && p.bias ? __ldg(p.bias + col + i) : 0.0f;
+        scale[i] = i < n ? get(p.scales + col + i) : 1.0f;
+        bias[i] = i < n && p.bias ? get(p.bias + col + i) : 0.0f;
     }
     const int64_t share = ((p.tokens + ranks - 1) / ranks + 31) / 32 * 32;
     const int64_t end = min(p.tokens, (rank + 1) * share);
@@ -224,8 +234,8 @@ static __global__ void __launch_bounds__(kRowThreads) slope_kernel(const __grid_
             float dz[8];
             unpack8(load8(p.dy + t * p.dy_stride + col, n, p.dy_vector), dz);
             if (p.z_codes) {
-                const uint2 c = __ldg(reinterpret_cast<const uint2 *>(p.z_codes + t * p.z_pitch + col));
-                const float zs = ckpt_scale(__ldg(p.z_exps + t * p.z_exps_pitch + (col >> 5)));
+                const uint2 c = get(reinterpret_cast<const uint2 *>(p.z_codes + t * p.z_pitch + col));
+                const float zs = ckpt_scale(get(p.z_exps + t * p.z_exps_pitch + (col >> 5)));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float z = zs * static_cast<float>(static_cast<int8_t>((i < 4 ? c.x : c.y) >> (8 * (i & 3))));
@@ -275,7 +285,7 @@ static __global__ void __launch_bounds__(kRowThreads) slope_kernel(const __grid_
             if (threadIdx.x < kSlopeCols) {
                 if (p.dbias) p.dbias[c] = s;
             } else if (p.dscales) {
-                p.dscales[c] = s / __ldg(p.scales + c);
+                p.dscales[c] = s / get(p.scales + c);
             }
         }
     }

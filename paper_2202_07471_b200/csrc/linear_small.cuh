@@ -56,13 +56,13 @@ __device__ __forceinline__ uint4 load_x8(const uint16_t *row, int first, int cin
 {
     if (first >= cin) return make_uint4(0, 0, 0, 0);
     if constexpr (kVector) {
-        return __ldg(reinterpret_cast<const uint4 *>(row + first));
+        return get(reinterpret_cast<const uint4 *>(row + first));
     } else {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int k = first + 2 * i;
-            w[i] = (k < cin ? static_cast<uint32_t>(__ldg(row + k)) : 0u) | (k + 1 < cin ? static_cast<uint32_t>(__ldg(row + k + 1)) << 16 : 0u);
+            w[i] = (k < cin ? static_cast<uint32_t>(get(row + k)) : 0u) | (k + 1 < cin ? static_cast<uint32_t>(get(row + k + 1)) << 16 : 0u);
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -88,9 +88,11 @@ __global__ void __launch_bounds__(32 * kSmallWarps, 2) small_kernel(const __grid
     const int blocks = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / ranks) - first;
     const int row_bytes = kKind == kInt4 ? (p.cin + 1) >> 1 : p.cin;
     float acc[kTiles][4] = {};
+    next_may_start();
+    wait_for_previous();
     const int row = row0 + (warp & 3) * 32 + lane;   // that this thread finishes
     const bool in = row < p.cout;
-    const float scale = in ? __ldg(p.scales + row) : 0.0f, bias = in && p.bias ? __ldg(p.bias + row) : 0.0f;
+    const float scale = in ? get(p.scales + row) : 0.0f, bias = in && p.bias ? get(p.bias + row) : 0.0f;
 
     auto load = [&](int b, uint4 (&c)[kSmallChunks][2]) {
         const int off0 = ((first + b) * kSmallChunks * 4 + q) * 16;
@@ -232,13 +234,15 @@ __global__ void __launch_bounds__(32 * kSmallWarps, 2) few_kernel(const __grid_c
     const int row0 = static_cast<int>(blockIdx.x) * kFewRows;
     const int chunks = (p.cin + 4 * kCodes - 1) / (4 * kCodes);
     const int row_bytes = kKind == kInt4 ? (p.cin + 1) >> 1 : p.cin;
+    next_may_start();
+    wait_for_previous();
     // the thread that finishes (token, row)
     const int token = threadIdx.x / kFewRows, row = row0 + static_cast<int>(threadIdx.x) % kFewRows;
     const bool mine = token < p.tokens && row < p.cout;
     float scale = 0.0f, bias = 0.0f, res = 0.0f;
     if (mine) {
-        scale = __ldg(p.scales + row);
-        if (p.bias) bias = __ldg(p.bias + row);
+        scale = get(p.scales + row);
+        if (p.bias) bias = get(p.bias + row);
         if (p.residual) res = to_float<kHalf>(p.residual[token * p.residual_stride + row]);
     }
     float acc[2][4] = {};
