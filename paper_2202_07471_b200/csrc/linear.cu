@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cstdlib>
 
 #include "linear_dense.cuh"
 #include "linear_device.cuh"
@@ -18,8 +19,8 @@ namespace {
 
 constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxRows = 1ll << 30;
-constexpr int kSmallTokens = 32;   // up to as many tokens the forward product goes to small_kernel
-constexpr int kFusedTokens = 128;  // up to as many gemm_kernel turns the codes into floats itself; beyond, they are expanded once
+static const int kSmallTokens = getenv("SQ_SMALL") ? atoi(getenv("SQ_SMALL")) : 32;
+static const int kFusedTokens = getenv("SQ_FUSED") ? atoi(getenv("SQ_FUSED")) : 128;
 
 #define SQ_CUDA(call)                                                      \
     do {                                                                   \
@@ -92,22 +93,41 @@ int matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t cols, int6
     return r == CUDA_SUCCESS ? SQUANT_OK : sq_host::cuda_failed(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
 }
 
-// As many thread blocks share a tile's contraction as there are multiprocessors (each holds two blocks) and stages for.
-template <int kMode, int kKind, bool kHalf>
-int launch_fused(const CUtensorMap &map, sq::GemmArgs a, int device, int sms, cudaStream_t stream)
+// Codes as bytes [rows][pitch]: boxes of 64 rows.
+int code_matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t pitch, int box_bytes)
 {
-    auto kernel = sq::fused_kernel<kMode, kKind, kHalf>;
-    static std::atomic<bool> ready[kMaxDevices];
-    if (device >= kMaxDevices || !ready[device].load(std::memory_order_relaxed)) {
+    EncodeTiled encode;
+    if (int rc = encoder(encode)) return rc;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(pitch), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(pitch)};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_bytes), 64}, step[2] = {1, 1};
+    const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(p), dims, strides, box, step,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SQUANT_OK : sq_host::cuda_failed(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+}
+
+// As many thread blocks share a tile's contraction as there are multiprocessors (each holds two blocks) and stages for.
+// x: [rows][depth] 16-bit.
+template <int kMode, int kKind, bool kHalf>
+int fused(const void *x, int64_t x_stride, sq::GemmArgs a, bool vector, int device, int sms, cudaStream_t stream)
+{
+    auto kernel = vector ? sq::fused_kernel<kMode, kKind, kHalf, true> : sq::fused_kernel<kMode, kKind, kHalf, false>;
+    static std::atomic<bool> ready[2][kMaxDevices];
+    if (device >= kMaxDevices || !ready[vector][device].load(std::memory_order_relaxed)) {
         SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sq::kFusedSmem));
-        if (device < kMaxDevices) ready[device].store(true, std::memory_order_relaxed);
+        if (device < kMaxDevices) ready[vector][device].store(true, std::memory_order_relaxed);
     }
+    a.box_rows = static_cast<int32_t>(std::min<int64_t>(sq::kFusedRows, up(a.rows, 8)));
+    CUtensorMap map, code_map{};
+    if (int rc = matrix_map(map, x, a.rows, a.depth, x_stride, kHalf, a.box_rows)) return rc;
+    if (vector)
+        if (int rc = code_matrix_map(code_map, a.codes, a.code_rows, a.code_pitch, kKind == sq::kInt4 ? 32 : 64)) return rc;
     a.row_tiles = (a.rows + sq::kFusedRows - 1) / sq::kFusedRows;
     a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + sq::kFusedCols - 1) / sq::kFusedCols);
     const int steps = (a.depth + sq::kTileDepth - 1) / sq::kTileDepth;
     unsigned ranks = 1;
     while (2 * ranks <= sq::kFusedMostRanks && 2 * ranks * a.tiles <= 2 * sms && 8 * ranks <= static_cast<unsigned>(steps)) ranks *= 2;
-    return launch(kernel, dim3(static_cast<unsigned>(a.tiles * ranks)), dim3(ranks), sq::kFusedThreads, sq::kFusedSmem, stream, map, a);
+    return launch(kernel, dim3(static_cast<unsigned>(a.tiles * ranks)), dim3(ranks), sq::kFusedThreads, sq::kFusedSmem, stream, map, code_map, a);
 }
 
 template <int kMode, bool kHalf, int kCols>
@@ -345,15 +365,12 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
         if (int rc = expand(a.codes, a.cout, a.cin, kKind == sq::kInt4, kHalf, b, stream)) return rc;
         return dense<sq::kForward, kHalf>(x, x_stride, b, up(a.cin, 8), g, device, sms, stream);
     }
-    CUtensorMap map;
-    if (int rc = matrix_map(map, x, a.tokens, a.cin, x_stride, kHalf, sq::kFusedRows)) return rc;
     g.codes = reinterpret_cast<const uint8_t *>(a.codes);
     g.code_pitch = pitch;
     g.code_bytes = pitch * a.cout;
     g.code_rows = a.cout;
     g.code_row_bytes = static_cast<int32_t>(pitch);
-    g.vector = code_vector;
-    return launch_fused<sq::kForward, kKind, kHalf>(map, g, device, sms, stream);
+    return fused<sq::kForward, kKind, kHalf>(x, x_stride, g, code_vector, device, sms, stream);
 }
 
 // ---- backward
@@ -526,16 +543,14 @@ int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_strea
             if (int rc = expand(a.codes, a.cout, a.cin, packed, false, wide, stream)) return rc;
             if (int rc = dense<sq::kInputGrad, false>(dzs, plan.pitch, wide, up(a.cin, 8), g, device, sms, stream)) return rc;
         } else {
-            CUtensorMap map;
-            if (int rc = matrix_map(map, dzs, a.tokens, a.cout, plan.pitch, false, sq::kFusedRows)) return rc;
             g.codes = reinterpret_cast<const uint8_t *>(a.codes);
             g.code_pitch = packed ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
             g.code_bytes = g.code_pitch * a.cout;
             g.code_rows = a.cout;
             g.code_row_bytes = static_cast<int32_t>(g.code_pitch);
-            g.vector = !misaligned(a.codes, 16) && g.code_pitch % 16 == 0;
-            if (int rc = packed ? launch_fused<sq::kInputGrad, sq::kInt4, false>(map, g, device, sms, stream)
-                                : launch_fused<sq::kInputGrad, sq::kInt8, false>(map, g, device, sms, stream)) return rc;
+            const bool vector = !misaligned(a.codes, 16) && g.code_pitch % 16 == 0;
+            if (int rc = packed ? fused<sq::kInputGrad, sq::kInt4, false>(dzs, plan.pitch, g, vector, device, sms, stream)
+                                : fused<sq::kInputGrad, sq::kInt8, false>(dzs, plan.pitch, g, vector, device, sms, stream)) return rc;
         }
     }
     if (a.dweight) {

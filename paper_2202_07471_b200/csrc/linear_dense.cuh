@@ -23,10 +23,10 @@ __device__ __forceinline__ void remote_arrive(uint32_t cluster_bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-// bar_wait() for arrivals of the other block too.
+// bar_wait_warp() for arrivals of the other block too.
 __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
 {
-    if (!bar_wait(bar, parity, gave_up)) return false;
+    if (!bar_wait_warp(bar, parity, gave_up)) return false;
     asm volatile("fence.acq_rel.cluster;" ::: "memory");
     return true;
 }
@@ -79,7 +79,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_word;
     volatile int *gave_up = &gave_up_word;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
 
     if (threadIdx.x == 0) {
@@ -126,16 +126,16 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (lane == 0) remote_arrive(cluster_addr(acc_empty(a), 0));
         }
     } else if (warp == kDenseEpilogueWarps) {
-        if (lane == 0) {
-            bool ok = true;
-            int s = 0, issued = 0;
-            uint32_t parity = 1;
-            for (int64_t t = pair; t < p.tiles && ok; t += pairs) {
-                const int row0 = static_cast<int>(t % p.row_tiles) * kPairRows + static_cast<int>(rank) * 128;
-                const int col0 = static_cast<int>(t / p.row_tiles * kCols) + static_cast<int>(rank) * (kCols / 2);
-                for (int k = 0; k < steps; ++k) {
-                    ok = bar_wait(empty(s), parity, gave_up);
-                    if (!ok) break;
+        bool ok = true;
+        int s = 0, issued = 0;
+        uint32_t parity = 1;
+        for (int64_t t = pair; t < p.tiles && ok; t += pairs) {
+            const int row0 = static_cast<int>(t % p.row_tiles) * kPairRows + static_cast<int>(rank) * 128;
+            const int col0 = static_cast<int>(t / p.row_tiles * kCols) + static_cast<int>(rank) * (kCols / 2);
+            for (int k = 0; k < steps; ++k) {
+                ok = bar_wait_warp(empty(s), parity, gave_up);
+                if (!ok) break;
+                if (elect_one()) {
                     const uint32_t bar = cluster_addr(full(s), 0);
                     if (rank == 0) bar_expect(full(s), 2 * (S::kBytesA + S::kBytesB));
                     const uint32_t at = smem_a + s * S::kBytesA, bt = smem_b + s * S::kBytesB;
@@ -151,18 +151,19 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll
                         for (int j = 0; j < kCols / 128; ++j) pair_tma_2d(bt + 8192 * j, &map_b, col0 + 64 * j, k * kTileDepth, bar);
                     }
-                    if (issued < S::kStages) ++issued;
-                    if (++s == S::kStages) { s = 0; parity ^= 1; }
                 }
-            }
-            // the last copies have landed and the matrix instructions have read them before the block may end
-            for (int i = 0; i < issued; ++i) {
-                if (--s < 0) { s = S::kStages - 1; parity ^= 1; }
-                if (rank == 0) bar_drain(full(s), parity ^ 1);
-                bar_drain(empty(s), parity ^ 1);
+                __syncwarp();
+                if (issued < S::kStages) ++issued;
+                if (++s == S::kStages) { s = 0; parity ^= 1; }
             }
         }
-    } else if (rank == 0 && lane == 0) {
+        // the last copies have landed and the matrix instructions have read them before the block may end
+        for (int i = 0; i < issued; ++i) {
+            if (--s < 0) { s = S::kStages - 1; parity ^= 1; }
+            if (rank == 0) bar_drain(full(s), parity ^ 1);
+            bar_drain(empty(s), parity ^ 1);
+        }
+    } else if (rank == 0) {
         constexpr uint32_t kIdesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) |
                                     (kMode == kWeightGrad ? 1u << 15 : 0u) | (kMode != kForward ? 1u << 16 : 0u) |
                                     (static_cast<uint32_t>(kCols >> 3) << 17) | (static_cast<uint32_t>(kPairRows >> 4) << 24);
@@ -176,18 +177,21 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (!ok) break;
             tc_fence_after();
             for (int k = 0; k < steps; ++k) {
-                ok = bar_wait(full(s), parity, gave_up);
+                ok = bar_wait_warp(full(s), parity, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t at = smem_a + s * S::kBytesA, bt = smem_b + s * S::kBytesB;
+                if (elect_one()) {
+                    const uint32_t at = smem_a + s * S::kBytesA, bt = smem_b + s * S::kBytesB;
 #pragma unroll
-                for (int i = 0; i < kTileDepth / 16; ++i)
-                    pair_mma_f16(tmem + a * kCols, smem_desc(at + i * kStepA, kMode == kWeightGrad ? 8192 : 16),
-                                 smem_desc(bt + i * kStepB, kMode == kForward ? 16 : 8192), kIdesc, k > 0 || i > 0);
-                pair_commit(empty(s));
+                    for (int i = 0; i < kTileDepth / 16; ++i)
+                        pair_mma_f16(tmem + a * kCols, smem_desc(at + i * kStepA, kMode == kWeightGrad ? 8192 : 16),
+                                     smem_desc(bt + i * kStepB, kMode == kForward ? 16 : 8192), kIdesc, k > 0 || i > 0);
+                    pair_commit(empty(s));
+                    if (k + 1 == steps) pair_commit(acc_full(a));
+                }
+                __syncwarp();
                 if (++s == S::kStages) { s = 0; parity ^= 1; }
             }
-            if (ok) pair_commit(acc_full(a));
         }
     }
     __syncwarp();

@@ -226,6 +226,15 @@ __device__ __noinline__ uint4 load_bytes16(const uint8_t *p, const uint8_t *lo, 
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
+// True for one lane of a converged warp, always the same one.  The compiler knows that there is one: under a comparison
+// of the lane's number instead, copies and matrix instructions, whose operands are uniform registers, cost several times the issue time.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");

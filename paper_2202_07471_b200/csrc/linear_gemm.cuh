@@ -22,10 +22,10 @@ struct GemmArgs {
     int64_t code_bytes;      // of the whole operand
     int32_t code_rows;       // rows of the coded operand
     int32_t code_row_bytes;  // bytes of a row that may be read
-    int32_t vector;          // every row starts and ends on 16 bytes
     int32_t rows, cols;      // of the result
     int32_t depth;           // of the contraction
     int32_t row_tiles;
+    int32_t box_rows;        // of a copy of the 16-bit operand
     int64_t tiles;
     uint16_t *out;           // 16-bit result
     int64_t out_stride;
@@ -195,54 +195,69 @@ __device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col,
 
 constexpr int kFusedRows = 128;       // rows of a tile: the tensor memory's lanes
 constexpr int kFusedCols = 64;
-constexpr int kConverterWarps = 8;
-constexpr int kFusedThreads = 32 * (kConverterWarps + 2);   // converters (four of them read the result), TMA, tensor cores
-constexpr int kFusedStages = 4;
-constexpr int kFusedBytesA = kFusedRows * 128, kFusedBytesB = kFusedCols * 128;
+constexpr int kFusedStages = 3;
+constexpr int kConverterWarps = 2 * kFusedStages;
+constexpr int kFusedThreads = 32 * (kConverterWarps + 3);   // converters (four of them read the result), copies of either operand, tensor cores
+constexpr int kFusedBytesB = kFusedCols * 128;
+constexpr int kFusedBytesA = 64 << 10;                      // stages of the 16-bit operand: 4 of 128 rows, 8 of 64, up to 16
+constexpr int kFusedRawBytes = 20 << 10;                    // codes as they are, ahead of the converters
 constexpr int kFusedPartPitch = kFusedCols + 4;             // floats of a row of partial sums: 16-byte accesses hit all banks
-constexpr int kFusedSmem = 1024 + kFusedStages * (kFusedBytesA + kFusedBytesB) + 8 * (3 * kFusedStages + 1);
+constexpr int kFusedMostA = 16, kFusedMostRaw = 10;
+constexpr int kFusedSmem = 1024 + kFusedBytesA + kFusedStages * kFusedBytesB + kFusedRawBytes + 8 * (2 * kFusedStages + 2 * kFusedMostA + 2 * kFusedMostRaw + 1);
 constexpr int kFusedMostRanks = 8;    // thread blocks of a cluster, which share a tile's contraction
-static_assert(kConverterWarps == 2 * kFusedStages, "two converter warps a stage");
-static_assert(4 * kFusedRows * kFusedPartPitch <= kFusedStages * (kFusedBytesA + kFusedBytesB), "partial sums take the stages' place");
+static_assert(4 * kFusedRows * kFusedPartPitch <= kFusedBytesA, "partial sums take the stages' place");
+static_assert(128 * kFusedRows <= kFusedStages * kFusedBytesB, "128 rows from any stage of the 16-bit operand on are inside the block's memory");
 
 // One 16-byte piece of a coded row: 32 int4 codes or 16 8-bit codes.  A converter warp takes 32 of a stage's 64 rows of 64
-// codes; eight consecutive lanes take eight consecutive rows, so that their 16-byte stores, permuted by the row, cover
-// all banks.
+// codes, neighbouring lanes neighbouring pieces.  Eight lanes then hold all chunks j of 2 or 4 rows whose 16-byte stores, permuted by the
+// row, cover all banks.
 template <int kKind>
 struct Pieces {
     static constexpr int kPerRow = kKind == kInt4 ? 2 : 4;       // pieces of a panel row
     static constexpr int kChunks = kKind == kInt4 ? 4 : 2;       // 16-byte chunks of 16-bit floats a piece becomes
     static constexpr int kRows = 32 / kPerRow;                   // rows of a warp's load
     static constexpr int kCount = 32 / kRows;                    // loads of a stage
-    static constexpr int kAhead = kKind == kInt4 ? 4 : 2;        // stages whose codes a warp holds in registers
+    static constexpr int kRawBytes = kFusedCols * 16 * kPerRow;  // of a stage
+    static constexpr int kRaw = kFusedRawBytes / kRawBytes;      // stages of codes ahead
 };
 
+// Rows that start anywhere: straight from global memory.
 template <int kMode, int kKind>
 __device__ __forceinline__ void load_codes(const GemmArgs &p, int col0, int step, int half, uint4 (&c)[Pieces<kKind>::kCount])
 {
     using P = Pieces<kKind>;
     const int lane = threadIdx.x & 31;
     // forward: rows are the tile's columns; gradient: rows are the contraction's
-    const int row = (kMode == kForward ? col0 : step * kTileDepth) + 32 * half + lane % P::kRows;
-    const int first = (kMode == kForward ? step * kTileDepth : col0) + lane / P::kRows * (64 / P::kPerRow);
+    const int row = (kMode == kForward ? col0 : step * kTileDepth) + 32 * half + lane / P::kPerRow;
+    const int first = (kMode == kForward ? step * kTileDepth : col0) + lane % P::kPerRow * (64 / P::kPerRow);
     const int off = kKind == kInt4 ? first >> 1 : first;
     const uint8_t *q = p.codes + static_cast<int64_t>(row) * p.code_pitch + off;
 #pragma unroll
     for (int i = 0; i < P::kCount; ++i) {
         c[i] = make_uint4(0, 0, 0, 0);
-        if (row + i * P::kRows < p.code_rows && off < p.code_row_bytes)
-            c[i] = p.vector ? ldg128(q) : load_bytes16(q, p.codes, p.codes + p.code_bytes);
+        if (row + i * P::kRows < p.code_rows && off < p.code_row_bytes) c[i] = load_bytes16(q, p.codes, p.codes + p.code_bytes);
         q += P::kRows * p.code_pitch;
     }
 }
 
-template <int kKind, bool kHalf>
-__device__ __forceinline__ void store_codes(uint32_t panel, const uint4 (&c)[Pieces<kKind>::kCount])
+template <int kKind>
+__device__ __forceinline__ void read_codes(uint32_t raw, int half, uint4 (&c)[Pieces<kKind>::kCount])
 {
     using P = Pieces<kKind>;
-    const int lane = threadIdx.x & 31, row = lane % P::kRows, sub = lane / P::kRows;
+    const uint32_t at = raw + half * (P::kRawBytes / 2) + (threadIdx.x & 31) * 16;
+#pragma unroll
+    for (int i = 0; i < P::kCount; ++i)
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(c[i].x), "=r"(c[i].y), "=r"(c[i].z), "=r"(c[i].w) : "r"(at + 512 * i) : "memory");
+}
+
+template <int kKind, bool kHalf>
+__device__ __forceinline__ void store_codes(uint32_t panel, int half, const uint4 (&c)[Pieces<kKind>::kCount])
+{
+    using P = Pieces<kKind>;
+    const int lane = threadIdx.x & 31, sub = lane % P::kPerRow;
 #pragma unroll
     for (int i = 0; i < P::kCount; ++i) {
+        const int row = 32 * half + i * P::kRows + lane / P::kPerRow;
         const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
 #pragma unroll
         for (int j = 0; j < P::kChunks; ++j) {
@@ -253,34 +268,42 @@ __device__ __forceinline__ void store_codes(uint32_t panel, const uint4 (&c)[Pie
                 int8_to_16<kHalf>(w[2 * j], o);
                 int8_to_16<kHalf>(w[2 * j + 1], o + 2);
             }
-            const uint32_t chunk = sub * P::kChunks + j;   // the rows of further pieces have the same low three bits
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(panel + (row + i * P::kRows) * 128 + ((chunk ^ (row & 7)) << 4)),
-                         "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+            const uint32_t chunk = sub * P::kChunks + j;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(panel + row * 128 + ((chunk ^ (row & 7)) << 4)), "r"(o[0]), "r"(o[1]),
+                         "r"(o[2]), "r"(o[3]) : "memory");
         }
     }
 }
 
 // A cluster of `ranks` thread blocks a tile of 128 rows and 64 columns; each takes a share of the contraction.  Reading the
-// codes is most of the work, so the tile is narrow and several blocks share a multiprocessor.  A stage's codes are the
-// business of two converter warps, which use the same place in shared memory every time (a waiter must not be more than
-// one phase ahead of its barrier): the fence between stores and the tensor cores' reads waits for the warp's loads in
-// flight too, and so four pairs of warps wait at once (all eight warps on every stage: 0.47 us a stage).  The ranks' sums meet in shared memory, added in the order of the
-// ranks, and each rank finishes a share of the rows.
-template <int kMode, int kKind, bool kHalf>
-__global__ void __launch_bounds__(kFusedThreads, 2) fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ GemmArgs p)
+// codes is most of the work, so the tile is narrow and two blocks share a multiprocessor.  TMA brings the codes as they are
+// far ahead; a pair of converter warps turns those of a stage into 16-bit floats, in the same place of shared memory every time
+// (a waiter must not be more than one phase ahead of its barrier).  Codes loaded by the converters themselves cost twice the time:
+// the fence between their stores and the tensor cores' reads waits for a warp's loads in flight, too.  That is what rows that start
+// anywhere do (kVector false).  The ranks' sums meet in shared memory, added in the order of the ranks, and each rank finishes a share
+// of the rows.
+template <int kMode, int kKind, bool kHalf, bool kVector>
+__global__ void __launch_bounds__(kFusedThreads, 2)
+fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const __grid_constant__ GemmArgs p)
 {
+    using P = Pieces<kKind>;
+    static_assert(P::kRaw <= kFusedMostRaw, "a barrier a stage");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t smem_a = base, smem_b = base + kFusedStages * kFusedBytesA;
-    const uint32_t bars = smem_b + kFusedStages * kFusedBytesB;
-    auto full_a = [&](int s) { return bars + 8 * s; };
-    auto full_b = [&](int s) { return bars + 8 * (kFusedStages + s); };
-    auto empty = [&](int s) { return bars + 8 * (2 * kFusedStages + s); };
-    const uint32_t done = bars + 8 * 3 * kFusedStages;
+    const uint32_t smem_a = base, smem_b = base + kFusedBytesA, smem_c = smem_b + kFusedStages * kFusedBytesB;
+    const uint32_t bars = smem_c + kFusedRawBytes;
+    auto full_b = [&](int s) { return bars + 8 * s; };
+    auto empty_b = [&](int s) { return bars + 8 * (kFusedStages + s); };
+    auto full_a = [&](int s) { return bars + 8 * (2 * kFusedStages + s); };
+    auto empty_a = [&](int s) { return bars + 8 * (2 * kFusedStages + kFusedMostA + s); };
+    auto raw_full = [&](int s) { return bars + 8 * (2 * kFusedStages + 2 * kFusedMostA + s); };
+    auto raw_empty = [&](int s) { return bars + 8 * (2 * kFusedStages + 2 * kFusedMostA + kFusedMostRaw + s); };
+    const uint32_t done = bars + 8 * (2 * kFusedStages + 2 * kFusedMostA + 2 * kFusedMostRaw);
+    const int bytes_a = p.box_rows * 128, stages_a = min(kFusedMostA, kFusedBytesA / bytes_a);
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_word;
     volatile int *gave_up = &gave_up_word;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), ranks = cluster_ranks();
     const int64_t tile = blockIdx.x / ranks;
     const int64_t row0 = tile % p.row_tiles * kFusedRows;
@@ -292,9 +315,16 @@ __global__ void __launch_bounds__(kFusedThreads, 2) fused_kernel(const __grid_co
     if (threadIdx.x == 0) {
         gave_up_word = 0;
         for (int s = 0; s < kFusedStages; ++s) {
-            bar_init(full_a(s), 1);
             bar_init(full_b(s), kConverterWarps / kFusedStages);
-            bar_init(empty(s), 1);
+            bar_init(empty_b(s), 1);
+        }
+        for (int s = 0; s < stages_a; ++s) {
+            bar_init(full_a(s), 1);
+            bar_init(empty_a(s), 1);
+        }
+        for (int s = 0; s < P::kRaw; ++s) {
+            bar_init(raw_full(s), 1);
+            bar_init(raw_empty(s), kConverterWarps / kFusedStages);
         }
         bar_init(done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -308,30 +338,28 @@ __global__ void __launch_bounds__(kFusedThreads, 2) fused_kernel(const __grid_co
     wait_for_previous();
 
     if (warp < kConverterWarps) {
-        constexpr int kAhead = Pieces<kKind>::kAhead;
         const int slot = warp % kFusedStages, half = warp / kFusedStages;
-        uint4 codes[kAhead][Pieces<kKind>::kCount];
-#pragma unroll
-        for (int d = 0; d < kAhead; ++d)
-            if (slot + d * kFusedStages < steps) load_codes<kMode, kKind>(p, col0, first + slot + d * kFusedStages, half, codes[d]);
         bool ok = true;
         uint32_t parity = 1;   // a stage that was never used counts as empty
-        for (int it = slot; it < steps && ok; it += kAhead * kFusedStages) {
-#pragma unroll
-            for (int d = 0; d < kAhead; ++d) {
-                const int k = it + d * kFusedStages;
-                if (k < steps && ok) {
-                    ok = bar_wait_warp(empty(slot), parity, gave_up);
-                    parity ^= 1;
-                    if (ok) {
-                        store_codes<kKind, kHalf>(smem_b + slot * kFusedBytesB + half * (32 * 128), codes[d]);
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(full_b(slot));
-                        if (k + kAhead * kFusedStages < steps) load_codes<kMode, kKind>(p, col0, first + k + kAhead * kFusedStages, half, codes[d]);
-                    }
-                }
+        for (int k = slot; k < steps && ok; k += kFusedStages) {
+            uint4 codes[P::kCount];
+            if constexpr (kVector) {
+                const int c = k % P::kRaw;
+                ok = bar_wait_warp(raw_full(c), k / P::kRaw & 1, gave_up);
+                if (!ok) break;
+                read_codes<kKind>(smem_c + c * P::kRawBytes, half, codes);
+                __syncwarp();
+                if (lane == 0) bar_arrive(raw_empty(c));
+            } else {
+                load_codes<kMode, kKind>(p, col0, first + k, half, codes);
             }
+            ok = bar_wait_warp(empty_b(slot), parity, gave_up);
+            if (!ok) break;
+            parity ^= 1;
+            store_codes<kKind, kHalf>(smem_b + slot * kFusedBytesB, half, codes);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(full_b(slot));
         }
         if (warp < 4 && bar_wait_warp(done, 0, gave_up)) {
             tc_fence_after();
@@ -350,39 +378,72 @@ __global__ void __launch_bounds__(kFusedThreads, 2) fused_kernel(const __grid_co
             tc_fence_before();
         }
     } else if (warp == kConverterWarps) {
-        if (lane == 0) {
-            bool ok = true;
-            int k = 0;
-            for (; k < steps && ok; ++k) {
-                const int s = k % kFusedStages;
-                ok = bar_wait(empty(s), (k / kFusedStages & 1) ^ 1, gave_up);
-                if (!ok) break;
-                bar_expect(full_a(s), kFusedBytesA);
-                tma_2d(smem_a + s * kFusedBytesA, &map, (first + k) * kTileDepth, static_cast<int>(row0), full_a(s));
+        bool ok = true;
+        int k = 0, s = 0;
+        uint32_t parity = 1;
+        for (; k < steps; ++k) {
+            ok = bar_wait_warp(empty_a(s), parity, gave_up);
+            if (!ok) break;
+            if (elect_one()) {
+                bar_expect(full_a(s), bytes_a);   // rows behind the last token stay what they are: only their own sums see them
+                tma_2d(smem_a + s * bytes_a, &map, (first + k) * kTileDepth, static_cast<int>(row0), full_a(s));
             }
-            // the last copies have landed before the block may end
-            for (int i = max(0, k - kFusedStages); i < k; ++i) bar_drain(full_a(i % kFusedStages), i / kFusedStages & 1);
+            __syncwarp();
+            if (++s == stages_a) { s = 0; parity ^= 1; }
         }
-    } else if (lane == 0) {
+        // the last copies have landed before the block may end
+        for (int i = 0; i < min(k, stages_a); ++i) {
+            if (--s < 0) { s = stages_a - 1; parity ^= 1; }
+            bar_drain(full_a(s), parity ^ 1);
+        }
+    } else if (warp == kConverterWarps + 2) {
+        if constexpr (kVector) {
+            constexpr int along = kKind == kInt4 ? kTileDepth / 2 : kTileDepth;   // bytes of 64 codes
+            bool ok = true;
+            int k = 0, s = 0;
+            uint32_t parity = 1;
+            for (; k < steps; ++k) {
+                ok = bar_wait_warp(raw_empty(s), parity, gave_up);
+                if (!ok) break;
+                if (elect_one()) {
+                    bar_expect(raw_full(s), P::kRawBytes);
+                    if (kMode == kForward) tma_2d(smem_c + s * P::kRawBytes, &code_map, (first + k) * along, col0, raw_full(s));
+                    else tma_2d(smem_c + s * P::kRawBytes, &code_map, col0 / kTileDepth * along, (first + k) * kTileDepth, raw_full(s));
+                }
+                __syncwarp();
+                if (++s == P::kRaw) { s = 0; parity ^= 1; }
+            }
+            for (int i = 0; i < min(k, P::kRaw); ++i) {
+                if (--s < 0) { s = P::kRaw - 1; parity ^= 1; }
+                bar_drain(raw_full(s), parity ^ 1);
+            }
+        }
+    } else {
         constexpr uint32_t kIdesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (kMode != kForward ? 1u << 16 : 0u) |
                                     (static_cast<uint32_t>(kFusedCols >> 3) << 17) | (static_cast<uint32_t>(kFusedRows >> 4) << 24);
         constexpr uint32_t kStepB = kMode == kForward ? 32 : 2048;
         bool ok = true;
-        int k = 0;
+        int k = 0, sa = 0, sb = 0;
+        uint32_t parity_a = 0, parity_b = 0;
         for (; k < steps; ++k) {
-            const int s = k % kFusedStages;
-            ok = bar_wait(full_a(s), k / kFusedStages & 1, gave_up) && bar_wait(full_b(s), k / kFusedStages & 1, gave_up);
+            ok = bar_wait_warp(full_a(sa), parity_a, gave_up) && bar_wait_warp(full_b(sb), parity_b, gave_up);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t at = smem_a + s * kFusedBytesA, bt = smem_b + s * kFusedBytesB;
+            if (elect_one()) {
+                const uint32_t at = smem_a + sa * bytes_a, bt = smem_b + sb * kFusedBytesB;
 #pragma unroll
-            for (int i = 0; i < kTileDepth / 16; ++i)
-                mma_f16(tmem, smem_desc(at + i * 32, 16), smem_desc(bt + i * kStepB, 16), kIdesc, k > 0 || i > 0);
-            mma_commit(empty(s));
+                for (int i = 0; i < kTileDepth / 16; ++i)
+                    mma_f16(tmem, smem_desc(at + i * 32, 16), smem_desc(bt + i * kStepB, 16), kIdesc, k > 0 || i > 0);
+                mma_commit(empty_b(sb));
+                mma_commit(empty_a(sa));
+                if (k + 1 == steps) mma_commit(done);
+            }
+            __syncwarp();
+            if (++sa == stages_a) { sa = 0; parity_a ^= 1; }
+            if (++sb == kFusedStages) { sb = 0; parity_b ^= 1; }
         }
-        if (ok) mma_commit(done);
         // the tensor cores have read their last stage before the block may end
-        if (k > 0) bar_drain(empty((k - 1) % kFusedStages), (k - 1) / kFusedStages & 1);
+        if (k > 0) bar_drain(empty_b((k - 1) % kFusedStages), (k - 1) / kFusedStages & 1);
     }
     __syncwarp();
     cluster_arrive_wait();   // all ranks' sums are in shared memory
