@@ -195,20 +195,24 @@ __device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col,
 
 constexpr int kFusedRows = 128;       // rows of a tile: the tensor memory's lanes
 constexpr int kFusedCols = 64;
-constexpr int kFusedStages = 3;
-constexpr int kConverterWarps = 2 * kFusedStages;
+constexpr int kConverterGroups = 2, kGroupWarps = 4, kConverterWarps = kConverterGroups * kGroupWarps;
 constexpr int kFusedThreads = 32 * (kConverterWarps + 3);   // converters (four of them read the result), copies of either operand, tensor cores
 constexpr int kFusedBytesB = kFusedCols * 128;
-constexpr int kFusedBytesA = 64 << 10;                      // stages of the 16-bit operand: 4 of 128 rows, 8 of 64, up to 16
-constexpr int kFusedRawBytes = 20 << 10;                    // codes as they are, ahead of the converters
+constexpr int kFusedStageBytes = 96 << 10;                  // 4 stages of 128 rows, 6 of up to 64, 8 of up to 32
+constexpr int kFusedMostStages = 8;
+constexpr int kFusedRawBytes = 12 << 10;                    // codes as they are, ahead of the converters
+constexpr int kFusedRawBars = 6;                           // even and a multiple of the stages of codes: one group waits for each
 constexpr int kFusedPartPitch = kFusedCols + 4;             // floats of a row of partial sums: 16-byte accesses hit all banks
-constexpr int kFusedMostA = 16, kFusedMostRaw = 10;
-constexpr int kFusedSmem = 1024 + kFusedBytesA + kFusedStages * kFusedBytesB + kFusedRawBytes + 8 * (2 * kFusedStages + 2 * kFusedMostA + 2 * kFusedMostRaw + 1);
+constexpr int kFusedSmem = 1024 + kFusedStageBytes + kFusedRawBytes + 8 * (2 * kFusedMostStages + 2 * kFusedRawBars + 1);
 constexpr int kFusedMostRanks = 8;    // thread blocks of a cluster, which share a tile's contraction
-static_assert(4 * kFusedRows * kFusedPartPitch <= kFusedBytesA, "partial sums take the stages' place");
-static_assert(128 * kFusedRows <= kFusedStages * kFusedBytesB, "128 rows from any stage of the 16-bit operand on are inside the block's memory");
+static_assert(4 * kFusedRows * kFusedPartPitch <= kFusedStageBytes, "partial sums take the stages' place");
+// Even: a stage belongs to one group of converters (a waiter must not be more than one phase ahead of its barrier).
+__host__ __device__ constexpr int fused_stages(int box_rows) { return box_rows > 64 ? 4 : box_rows > 32 ? 6 : 8; }
+static_assert(4 * (128 * 128 + kFusedBytesB) <= kFusedStageBytes && 6 * (64 * 128 + kFusedBytesB) <= kFusedStageBytes &&
+              8 * (32 * 128 + kFusedBytesB) <= kFusedStageBytes && 4 * kFusedBytesB >= 128 * 128,
+              "the stages fit, and 128 rows from any stage of the 16-bit operand on are inside them");
 
-// One 16-byte piece of a coded row: 32 int4 codes or 16 8-bit codes.  A converter warp takes 32 of a stage's 64 rows of 64
+// One 16-byte piece of a coded row: 32 int4 codes or 16 8-bit codes.  A converter warp takes 16 of a stage's 64 rows of 64
 // codes, neighbouring lanes neighbouring pieces.  Eight lanes then hold all chunks j of 2 or 4 rows whose 16-byte stores, permuted by the
 // row, cover all banks.
 template <int kKind>
@@ -216,19 +220,19 @@ struct Pieces {
     static constexpr int kPerRow = kKind == kInt4 ? 2 : 4;       // pieces of a panel row
     static constexpr int kChunks = kKind == kInt4 ? 4 : 2;       // 16-byte chunks of 16-bit floats a piece becomes
     static constexpr int kRows = 32 / kPerRow;                   // rows of a warp's load
-    static constexpr int kCount = 32 / kRows;                    // loads of a stage
+    static constexpr int kCount = 64 / kGroupWarps / kRows;      // loads of a stage
     static constexpr int kRawBytes = kFusedCols * 16 * kPerRow;  // of a stage
     static constexpr int kRaw = kFusedRawBytes / kRawBytes;      // stages of codes ahead
 };
 
 // Rows that start anywhere: straight from global memory.
 template <int kMode, int kKind>
-__device__ __forceinline__ void load_codes(const GemmArgs &p, int col0, int step, int half, uint4 (&c)[Pieces<kKind>::kCount])
+__device__ __forceinline__ void load_codes(const GemmArgs &p, int col0, int step, int part, uint4 (&c)[Pieces<kKind>::kCount])
 {
     using P = Pieces<kKind>;
     const int lane = threadIdx.x & 31;
     // forward: rows are the tile's columns; gradient: rows are the contraction's
-    const int row = (kMode == kForward ? col0 : step * kTileDepth) + 32 * half + lane / P::kPerRow;
+    const int row = (kMode == kForward ? col0 : step * kTileDepth) + 64 / kGroupWarps * part + lane / P::kPerRow;
     const int first = (kMode == kForward ? step * kTileDepth : col0) + lane % P::kPerRow * (64 / P::kPerRow);
     const int off = kKind == kInt4 ? first >> 1 : first;
     const uint8_t *q = p.codes + static_cast<int64_t>(row) * p.code_pitch + off;
@@ -241,23 +245,23 @@ __device__ __forceinline__ void load_codes(const GemmArgs &p, int col0, int step
 }
 
 template <int kKind>
-__device__ __forceinline__ void read_codes(uint32_t raw, int half, uint4 (&c)[Pieces<kKind>::kCount])
+__device__ __forceinline__ void read_codes(uint32_t raw, int part, uint4 (&c)[Pieces<kKind>::kCount])
 {
     using P = Pieces<kKind>;
-    const uint32_t at = raw + half * (P::kRawBytes / 2) + (threadIdx.x & 31) * 16;
+    const uint32_t at = raw + part * (P::kRawBytes / kGroupWarps) + (threadIdx.x & 31) * 16;
 #pragma unroll
     for (int i = 0; i < P::kCount; ++i)
         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(c[i].x), "=r"(c[i].y), "=r"(c[i].z), "=r"(c[i].w) : "r"(at + 512 * i) : "memory");
 }
 
 template <int kKind, bool kHalf>
-__device__ __forceinline__ void store_codes(uint32_t panel, int half, const uint4 (&c)[Pieces<kKind>::kCount])
+__device__ __forceinline__ void store_codes(uint32_t panel, int part, const uint4 (&c)[Pieces<kKind>::kCount])
 {
     using P = Pieces<kKind>;
     const int lane = threadIdx.x & 31, sub = lane % P::kPerRow;
 #pragma unroll
     for (int i = 0; i < P::kCount; ++i) {
-        const int row = 32 * half + i * P::kRows + lane / P::kPerRow;
+        const int row = 64 / kGroupWarps * part + i * P::kRows + lane / P::kPerRow;
         const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
 #pragma unroll
         for (int j = 0; j < P::kChunks; ++j) {
@@ -277,29 +281,27 @@ __device__ __forceinline__ void store_codes(uint32_t panel, int half, const uint
 
 // A cluster of `ranks` thread blocks a tile of 128 rows and 64 columns; each takes a share of the contraction.  Reading the
 // codes is most of the work, so the tile is narrow and two blocks share a multiprocessor.  TMA brings the codes as they are
-// far ahead; a pair of converter warps turns those of a stage into 16-bit floats, in the same place of shared memory every time
-// (a waiter must not be more than one phase ahead of its barrier).  Codes loaded by the converters themselves cost twice the time:
-// the fence between their stores and the tensor cores' reads waits for a warp's loads in flight, too.  That is what rows that start
-// anywhere do (kVector false).  The ranks' sums meet in shared memory, added in the order of the ranks, and each rank finishes a share
-// of the rows.
+// ahead; two groups of converter warps turn those of a stage into 16-bit floats in turn.  The issuing warp's loop of one wait, four
+// matrix instructions and one commit is the longest chain: with a barrier for either operand and six converter warps a step of 64
+// took 0.45 us.  Codes loaded by the converters themselves, as rows that start anywhere are (kVector false), cost more: the fence
+// between their stores and the tensor cores' reads waits for a warp's loads in flight, too.  The ranks' sums meet in shared
+// memory, added in the order of the ranks, and each rank finishes a share of the rows.
 template <int kMode, int kKind, bool kHalf, bool kVector>
 __global__ void __launch_bounds__(kFusedThreads, 2)
 fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const __grid_constant__ GemmArgs p)
 {
     using P = Pieces<kKind>;
-    static_assert(P::kRaw <= kFusedMostRaw, "a barrier a stage");
+    static_assert(kFusedRawBars % P::kRaw == 0 && kFusedRawBars % kConverterGroups == 0, "a barrier belongs to one place and one group");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t smem_a = base, smem_b = base + kFusedBytesA, smem_c = smem_b + kFusedStages * kFusedBytesB;
+    const int bytes_a = p.box_rows * 128, stages = fused_stages(p.box_rows);
+    const uint32_t smem_a = base, smem_b = base + stages * bytes_a, smem_c = base + kFusedStageBytes;
     const uint32_t bars = smem_c + kFusedRawBytes;
-    auto full_b = [&](int s) { return bars + 8 * s; };
-    auto empty_b = [&](int s) { return bars + 8 * (kFusedStages + s); };
-    auto full_a = [&](int s) { return bars + 8 * (2 * kFusedStages + s); };
-    auto empty_a = [&](int s) { return bars + 8 * (2 * kFusedStages + kFusedMostA + s); };
-    auto raw_full = [&](int s) { return bars + 8 * (2 * kFusedStages + 2 * kFusedMostA + s); };
-    auto raw_empty = [&](int s) { return bars + 8 * (2 * kFusedStages + 2 * kFusedMostA + kFusedMostRaw + s); };
-    const uint32_t done = bars + 8 * (2 * kFusedStages + 2 * kFusedMostA + 2 * kFusedMostRaw);
-    const int bytes_a = p.box_rows * 128, stages_a = min(kFusedMostA, kFusedBytesA / bytes_a);
+    auto full = [&](int s) { return bars + 8 * s; };
+    auto empty = [&](int s) { return bars + 8 * (kFusedMostStages + s); };
+    auto raw_full = [&](int s) { return bars + 8 * (2 * kFusedMostStages + s); };
+    auto raw_empty = [&](int s) { return bars + 8 * (2 * kFusedMostStages + kFusedRawBars + s); };
+    const uint32_t done = bars + 8 * (2 * kFusedMostStages + 2 * kFusedRawBars);
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_word;
     volatile int *gave_up = &gave_up_word;
@@ -314,17 +316,13 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
 
     if (threadIdx.x == 0) {
         gave_up_word = 0;
-        for (int s = 0; s < kFusedStages; ++s) {
-            bar_init(full_b(s), kConverterWarps / kFusedStages);
-            bar_init(empty_b(s), 1);
+        for (int s = 0; s < stages; ++s) {
+            bar_init(full(s), 1 + kGroupWarps);
+            bar_init(empty(s), 1);
         }
-        for (int s = 0; s < stages_a; ++s) {
-            bar_init(full_a(s), 1);
-            bar_init(empty_a(s), 1);
-        }
-        for (int s = 0; s < P::kRaw; ++s) {
+        for (int s = 0; s < kFusedRawBars; ++s) {
             bar_init(raw_full(s), 1);
-            bar_init(raw_empty(s), kConverterWarps / kFusedStages);
+            bar_init(raw_empty(s), kGroupWarps);
         }
         bar_init(done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -338,28 +336,27 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     wait_for_previous();
 
     if (warp < kConverterWarps) {
-        const int slot = warp % kFusedStages, half = warp / kFusedStages;
-        bool ok = true;
+        const int part = warp % kGroupWarps;
+        int s = warp / kGroupWarps;
         uint32_t parity = 1;   // a stage that was never used counts as empty
-        for (int k = slot; k < steps && ok; k += kFusedStages) {
+        for (int k = s; k < steps; k += kConverterGroups) {
             uint4 codes[P::kCount];
             if constexpr (kVector) {
-                const int c = k % P::kRaw;
-                ok = bar_wait_warp(raw_full(c), k / P::kRaw & 1, gave_up);
-                if (!ok) break;
-                read_codes<kKind>(smem_c + c * P::kRawBytes, half, codes);
+                const int b = k % kFusedRawBars;
+                if (!bar_wait_warp(raw_full(b), k / kFusedRawBars & 1, gave_up)) break;
+                read_codes<kKind>(smem_c + k % P::kRaw * P::kRawBytes, part, codes);
                 __syncwarp();
-                if (lane == 0) bar_arrive(raw_empty(c));
+                if (lane == 0) bar_arrive(raw_empty(b));
             } else {
-                load_codes<kMode, kKind>(p, col0, first + k, half, codes);
+                load_codes<kMode, kKind>(p, col0, first + k, part, codes);
             }
-            ok = bar_wait_warp(empty_b(slot), parity, gave_up);
-            if (!ok) break;
-            parity ^= 1;
-            store_codes<kKind, kHalf>(smem_b + slot * kFusedBytesB, half, codes);
+            if (!bar_wait_warp(empty(s), parity, gave_up)) break;
+            store_codes<kKind, kHalf>(smem_b + s * kFusedBytesB, part, codes);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) bar_arrive(full_b(slot));
+            if (lane == 0) bar_arrive(full(s));
+            s += kConverterGroups;
+            if (s >= stages) { s -= stages; parity ^= 1; }
         }
         if (warp < 4 && bar_wait_warp(done, 0, gave_up)) {
             tc_fence_after();
@@ -382,68 +379,60 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
         int k = 0, s = 0;
         uint32_t parity = 1;
         for (; k < steps; ++k) {
-            ok = bar_wait_warp(empty_a(s), parity, gave_up);
+            ok = bar_wait_warp(empty(s), parity, gave_up);
             if (!ok) break;
             if (elect_one()) {
-                bar_expect(full_a(s), bytes_a);   // rows behind the last token stay what they are: only their own sums see them
-                tma_2d(smem_a + s * bytes_a, &map, (first + k) * kTileDepth, static_cast<int>(row0), full_a(s));
+                bar_expect(full(s), bytes_a);   // rows behind the last token stay what they are: only their own sums see them
+                tma_2d(smem_a + s * bytes_a, &map, (first + k) * kTileDepth, static_cast<int>(row0), full(s));
             }
             __syncwarp();
-            if (++s == stages_a) { s = 0; parity ^= 1; }
+            if (++s == stages) { s = 0; parity ^= 1; }
         }
         // the last copies have landed before the block may end
-        for (int i = 0; i < min(k, stages_a); ++i) {
-            if (--s < 0) { s = stages_a - 1; parity ^= 1; }
-            bar_drain(full_a(s), parity ^ 1);
+        for (int i = 0; i < min(k, stages); ++i) {
+            if (--s < 0) { s = stages - 1; parity ^= 1; }
+            bar_drain(full(s), parity ^ 1);
         }
     } else if (warp == kConverterWarps + 2) {
         if constexpr (kVector) {
             constexpr int along = kKind == kInt4 ? kTileDepth / 2 : kTileDepth;   // bytes of 64 codes
-            bool ok = true;
-            int k = 0, s = 0;
-            uint32_t parity = 1;
+            int k = 0;
             for (; k < steps; ++k) {
-                ok = bar_wait_warp(raw_empty(s), parity, gave_up);
-                if (!ok) break;
+                const int b = k % kFusedRawBars, before = k - P::kRaw;
+                if (before >= 0 && !bar_wait_warp(raw_empty(before % kFusedRawBars), before / kFusedRawBars & 1, gave_up)) break;
                 if (elect_one()) {
-                    bar_expect(raw_full(s), P::kRawBytes);
-                    if (kMode == kForward) tma_2d(smem_c + s * P::kRawBytes, &code_map, (first + k) * along, col0, raw_full(s));
-                    else tma_2d(smem_c + s * P::kRawBytes, &code_map, col0 / kTileDepth * along, (first + k) * kTileDepth, raw_full(s));
+                    const uint32_t to = smem_c + k % P::kRaw * P::kRawBytes;
+                    bar_expect(raw_full(b), P::kRawBytes);
+                    if (kMode == kForward) tma_2d(to, &code_map, (first + k) * along, col0, raw_full(b));
+                    else tma_2d(to, &code_map, col0 / kTileDepth * along, (first + k) * kTileDepth, raw_full(b));
                 }
                 __syncwarp();
-                if (++s == P::kRaw) { s = 0; parity ^= 1; }
             }
-            for (int i = 0; i < min(k, P::kRaw); ++i) {
-                if (--s < 0) { s = P::kRaw - 1; parity ^= 1; }
-                bar_drain(raw_full(s), parity ^ 1);
-            }
+            for (int i = max(0, k - P::kRaw); i < k; ++i) bar_drain(raw_full(i % kFusedRawBars), i / kFusedRawBars & 1);
         }
     } else {
         constexpr uint32_t kIdesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (kMode != kForward ? 1u << 16 : 0u) |
                                     (static_cast<uint32_t>(kFusedCols >> 3) << 17) | (static_cast<uint32_t>(kFusedRows >> 4) << 24);
         constexpr uint32_t kStepB = kMode == kForward ? 32 : 2048;
-        bool ok = true;
-        int k = 0, sa = 0, sb = 0;
-        uint32_t parity_a = 0, parity_b = 0;
+        int k = 0, s = 0, last = 0;
+        uint32_t parity = 0;
         for (; k < steps; ++k) {
-            ok = bar_wait_warp(full_a(sa), parity_a, gave_up) && bar_wait_warp(full_b(sb), parity_b, gave_up);
-            if (!ok) break;
+            if (!bar_wait_warp(full(s), parity, gave_up)) break;
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t at = smem_a + sa * bytes_a, bt = smem_b + sb * kFusedBytesB;
+                const uint32_t at = smem_a + s * bytes_a, bt = smem_b + s * kFusedBytesB;
 #pragma unroll
                 for (int i = 0; i < kTileDepth / 16; ++i)
                     mma_f16(tmem, smem_desc(at + i * 32, 16), smem_desc(bt + i * kStepB, 16), kIdesc, k > 0 || i > 0);
-                mma_commit(empty_b(sb));
-                mma_commit(empty_a(sa));
-                if (k + 1 == steps) mma_commit(done);
+                mma_commit(k + 1 == steps ? done : empty(s));
             }
             __syncwarp();
-            if (++sa == stages_a) { sa = 0; parity_a ^= 1; }
-            if (++sb == kFusedStages) { sb = 0; parity_b ^= 1; }
+            last = s;
+            if (++s == stages) { s = 0; parity ^= 1; }
         }
         // the tensor cores have read their last stage before the block may end
-        if (k > 0) bar_drain(empty_b((k - 1) % kFusedStages), (k - 1) / kFusedStages & 1);
+        if (k == steps) bar_drain(done, 0);
+        else if (k > 0) bar_drain(empty(last), s == 0 ? parity ^ 1 : parity);
     }
     __syncwarp();
     cluster_arrive_wait();   // all ranks' sums are in shared memory
