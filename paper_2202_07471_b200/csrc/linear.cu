@@ -6,7 +6,6 @@
 
 #include <algorithm>
 #include <atomic>
-#include <cstdlib>
 
 #include "linear_dense.cuh"
 #include "linear_device.cuh"
@@ -19,8 +18,9 @@ namespace {
 
 constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxRows = 1ll << 30;
-static const int kSmallTokens = getenv("SQ_SMALL") ? atoi(getenv("SQ_SMALL")) : 32;
-static const int kFusedTokens = getenv("SQ_FUSED") ? atoi(getenv("SQ_FUSED")) : 128;
+// Up to as many tokens fused_kernel turns the codes into floats on the way to the tensor cores; beyond, they are expanded once.
+// 4096 -> 4096 int4, fused and expanded: 256 tokens 16.9 and 21.3 us, 384 tokens 33 and 21.5; 4096 -> 11008 256 tokens 43 and 49.
+constexpr int kFusedTokens = 256;
 
 #define SQ_CUDA(call)                                                      \
     do {                                                                   \
@@ -93,13 +93,13 @@ int matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t cols, int6
     return r == CUDA_SUCCESS ? SQUANT_OK : sq_host::cuda_failed(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
 }
 
-// Codes as bytes [rows][pitch]: boxes of 64 rows.
-int code_matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t pitch, int box_bytes)
+// Codes as bytes [rows][pitch].
+int code_matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t pitch, int box_bytes, int box_rows)
 {
     EncodeTiled encode;
     if (int rc = encoder(encode)) return rc;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(pitch), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(pitch)};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_bytes), 64}, step[2] = {1, 1};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_bytes), static_cast<cuuint32_t>(box_rows)}, step[2] = {1, 1};
     const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(p), dims, strides, box, step,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -117,16 +117,17 @@ int fused(const void *x, int64_t x_stride, sq::GemmArgs a, bool vector, int devi
         SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sq::kFusedSmem));
         if (device < kMaxDevices) ready[vector][device].store(true, std::memory_order_relaxed);
     }
-    a.box_rows = static_cast<int32_t>(std::min<int64_t>(sq::kFusedRows, up(a.rows, 8)));
+    a.box_rows = static_cast<int32_t>(std::min<int64_t>(sq::kFusedTokens, up(a.rows, 16)));
     CUtensorMap map, code_map{};
     if (int rc = matrix_map(map, x, a.rows, a.depth, x_stride, kHalf, a.box_rows)) return rc;
+    const int bytes = kKind == sq::kInt4 ? 32 : 64;   // of 64 codes
     if (vector)
-        if (int rc = code_matrix_map(code_map, a.codes, a.code_rows, a.code_pitch, kKind == sq::kInt4 ? 32 : 64)) return rc;
-    a.row_tiles = (a.rows + sq::kFusedRows - 1) / sq::kFusedRows;
+        if (int rc = kMode == sq::kForward ? code_matrix_map(code_map, a.codes, a.code_rows, a.code_pitch, bytes, sq::kFusedCols)
+                                           : code_matrix_map(code_map, a.codes, a.code_rows, a.code_pitch, 2 * bytes, sq::kTileDepth)) return rc;
+    a.row_tiles = (a.rows + sq::kFusedTokens - 1) / sq::kFusedTokens;
     a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + sq::kFusedCols - 1) / sq::kFusedCols);
-    const int steps = (a.depth + sq::kTileDepth - 1) / sq::kTileDepth;
-    unsigned ranks = 1;
-    while (2 * ranks <= sq::kFusedMostRanks && 2 * ranks * a.tiles <= 2 * sms && 8 * ranks <= static_cast<unsigned>(steps)) ranks *= 2;
+    const int64_t steps = (static_cast<int64_t>(a.depth) + sq::kTileDepth - 1) / sq::kTileDepth;
+    const unsigned ranks = static_cast<unsigned>(std::max<int64_t>(1, std::min({static_cast<int64_t>(sq::kFusedMostRanks), 2 * sms / a.tiles, steps / 2})));
     return launch(kernel, dim3(static_cast<unsigned>(a.tiles * ranks)), dim3(ranks), sq::kFusedThreads, sq::kFusedSmem, stream, map, code_map, a);
 }
 
@@ -161,38 +162,6 @@ int dense(const void *a, int64_t a_stride, const void *b, int64_t b_stride, cons
                                        : matrix_map(map_b, b, g.depth, g.cols, b_stride, kHalf, sq::kTileDepth)) return rc;
     return use_wide ? launch_dense<kMode, kHalf, 256>(map_a, map_b, g, device, sms, stream)
                     : launch_dense<kMode, kHalf, 128>(map_a, map_b, g, device, sms, stream);
-}
-
-template <int kKind, bool kHalf, int kTiles, bool kVector>
-int launch_small(const sq::SmallArgs &a, int device, int sms, cudaStream_t stream)
-{
-    using S = sq::SmallShape<kKind, kTiles>;
-    auto kernel = sq::small_kernel<kKind, kHalf, kTiles, kVector>;
-    static std::atomic<bool> ready[kMaxDevices];
-    if (S::kSmem > (48 << 10) && (device >= kMaxDevices || !ready[device].load(std::memory_order_relaxed))) {
-        SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
-        if (device < kMaxDevices) ready[device].store(true, std::memory_order_relaxed);
-    }
-    const int64_t tiles = (static_cast<int64_t>(a.cout) + sq::kSmallRows - 1) / sq::kSmallRows;
-    const int64_t blocks = (static_cast<int64_t>(a.cin) + S::kBlock - 1) / S::kBlock;
-    // up to four thread blocks a multiprocessor, of which it holds two: 16 tokens 4096 -> 11008 17.2 us, 21.2 with two
-    unsigned ranks = 1;
-    while (2 * ranks <= sq::kSmallMostRanks && 2 * ranks * tiles <= 4 * sms && 2 * ranks <= blocks) ranks *= 2;
-    return launch(kernel, dim3(static_cast<unsigned>(tiles * ranks)), dim3(ranks), 32 * sq::kSmallWarps, S::kSmem, stream, a);
-}
-
-template <int kKind, bool kHalf>
-int launch_small_tokens(const sq::SmallArgs &a, bool vector, cudaStream_t stream)
-{
-    int device, sms;
-    if (int rc = device_sms(device, sms)) return rc;
-    if (a.tokens <= sq::kFewTokens && !a.z_codes) {   // one token 4096 -> 4096 4.5 us, 6.2 by clusters; eight 5.6 and 7.5
-        const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kFewRows - 1) / sq::kFewRows);
-        return launch(vector ? sq::few_kernel<kKind, kHalf, true> : sq::few_kernel<kKind, kHalf, false>, dim3(grid), dim3(1), 32 * sq::kSmallWarps, 0, stream, a);
-    }
-    if (a.tokens <= 8) return vector ? launch_small<kKind, kHalf, 1, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 1, false>(a, device, sms, stream);
-    if (a.tokens <= 16) return vector ? launch_small<kKind, kHalf, 2, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 2, false>(a, device, sms, stream);
-    return vector ? launch_small<kKind, kHalf, 4, true>(a, device, sms, stream) : launch_small<kKind, kHalf, 4, false>(a, device, sms, stream);
 }
 
 enum class RowKernel { kCheckpoint, kRestore, kAlign, kExpandInt4Bf16, kExpandInt4Fp16, kExpandInt8Bf16, kExpandInt8Fp16 };
@@ -270,10 +239,12 @@ struct ForwardPlan {
     int64_t copy_bytes = 0, bytes = 0;
 };
 
+bool few(const squant_linear_args &a) { return a.tokens <= sq::kFewTokens && !a.z.codes; }
+
 ForwardPlan forward_plan(const squant_linear_args &a)
 {
     ForwardPlan p;
-    p.copy = a.tokens > kSmallTokens && !rows_on_vectors(a.x, a.x_stride, a.tokens);
+    p.copy = !few(a) && !rows_on_vectors(a.x, a.x_stride, a.tokens);
     p.dense = a.tokens > kFusedTokens;
     if (p.copy) p.copy_bytes = a.tokens * up(a.cin, 8) * 2;
     p.bytes = p.copy_bytes + (p.dense ? a.cout * up(a.cin, 8) * 2 : 0);
@@ -302,8 +273,8 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
     const int64_t pitch = kKind == sq::kInt4 ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
     const bool code_vector = !misaligned(a.codes, 16) && pitch % 16 == 0;
     const int64_t z_pitch = up(a.cout, 32);
-    if (a.tokens <= kSmallTokens) {
-        sq::SmallArgs s{};
+    if (few(a)) {
+        sq::FewArgs s{};
         s.x = static_cast<const uint16_t *>(a.x);
         s.x_stride = a.x_stride;
         s.codes = reinterpret_cast<const uint8_t *>(a.codes);
@@ -319,11 +290,9 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
         s.y = static_cast<uint16_t *>(a.y);
         s.y_stride = a.y_stride;
         s.act = static_cast<int32_t>(a.act);
-        s.z_codes = reinterpret_cast<uint8_t *>(a.z.codes);
-        s.z_exps = a.z.exps;
-        s.z_pitch = z_pitch;
-        s.z_exps_pitch = z_pitch / 32;
-        return launch_small_tokens<kKind, kHalf>(s, code_vector && rows_on_vectors(a.x, a.x_stride, a.tokens) && a.cin % 8 == 0, stream);
+        const bool vector = code_vector && rows_on_vectors(a.x, a.x_stride, a.tokens) && a.cin % 8 == 0;
+        const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kFewRows - 1) / sq::kFewRows);
+        return launch(vector ? sq::few_kernel<kKind, kHalf, true> : sq::few_kernel<kKind, kHalf, false>, dim3(grid), dim3(1), 32 * sq::kFewWarps, 0, stream, s);
     }
     int device, sms;
     if (int rc = device_sms(device, sms)) return rc;

@@ -51,11 +51,11 @@ __device__ __forceinline__ void pair_commit(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
 }
-__device__ __forceinline__ void pair_mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+__device__ __forceinline__ void pair_mma_f16(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)), "n"(kDescHigh) : "memory");
 }
 
 // Clusters of two thread blocks, persistent, one block a multiprocessor.  A tile of 256 rows belongs to a pair: each
@@ -168,7 +168,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                                     (kMode == kWeightGrad ? 1u << 15 : 0u) | (kMode != kForward ? 1u << 16 : 0u) |
                                     (static_cast<uint32_t>(kCols >> 3) << 17) | (static_cast<uint32_t>(kPairRows >> 4) << 24);
         constexpr uint32_t kStepA = kMode == kWeightGrad ? 2048 : 32, kStepB = kMode == kForward ? 32 : 2048;
-        bool ok = true;
+        bool ok = true, there = false;
         int s = 0, n = 0;
         uint32_t parity = 0;
         for (int64_t t = pair; t < p.tiles && ok; t += pairs, ++n) {
@@ -177,20 +177,22 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (!ok) break;
             tc_fence_after();
             for (int k = 0; k < steps; ++k) {
-                ok = bar_wait_warp(full(s), parity, gave_up);
+                ok = there || bar_wait_warp(full(s), parity, gave_up);
                 if (!ok) break;
                 tc_fence_after();
+                const int now = s;
+                const uint32_t at = desc_low(smem_a + s * S::kBytesA, kMode == kWeightGrad ? 8192 : 16);
+                const uint32_t bt = desc_low(smem_b + s * S::kBytesB, kMode == kForward ? 16 : 8192);
+                if (++s == S::kStages) { s = 0; parity ^= 1; }
+                there = __all_sync(0xffffffffu, bar_try(full(s), parity));   // the next step's copies, while this one's products are issued
                 if (elect_one()) {
-                    const uint32_t at = smem_a + s * S::kBytesA, bt = smem_b + s * S::kBytesB;
 #pragma unroll
                     for (int i = 0; i < kTileDepth / 16; ++i)
-                        pair_mma_f16(tmem + a * kCols, smem_desc(at + i * kStepA, kMode == kWeightGrad ? 8192 : 16),
-                                     smem_desc(bt + i * kStepB, kMode == kForward ? 16 : 8192), kIdesc, k > 0 || i > 0);
-                    pair_commit(empty(s));
+                        pair_mma_f16(tmem + a * kCols, at + i * (kStepA >> 4), bt + i * (kStepB >> 4), kIdesc, k > 0 || i > 0);
+                    pair_commit(empty(now));
                     if (k + 1 == steps) pair_commit(acc_full(a));
                 }
                 __syncwarp();
-                if (++s == S::kStages) { s = 0; parity ^= 1; }
             }
         }
     }

@@ -80,6 +80,21 @@ __device__ __forceinline__ float act_value(float z, int act)
     if (act == kActSilu) return z * sigmoid(z);
     return z;
 }
+// One branch for all values.
+template <int kCount>
+__device__ __forceinline__ void act_values(float (&v)[kCount], int act)
+{
+    if (act == kActRelu) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) v[i] = act_value(v[i], kActRelu);
+    } else if (act == kActGelu) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) v[i] = act_value(v[i], kActGelu);
+    } else if (act == kActSilu) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) v[i] = act_value(v[i], kActSilu);
+    }
+}
 __device__ __forceinline__ float act_slope(float z, int act)
 {
     if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
@@ -303,6 +318,17 @@ __device__ __forceinline__ void cluster_arrive_wait()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// Shared-memory matrix descriptor, 128-byte swizzle.  A panel has rows of 64 16-bit elements (128 bytes), its eight
+// 16-byte pieces permuted by the row's low three bits; eight rows are 1024 bytes.
+//   contraction along the rows' 64 elements ("K-major"): 1024 bytes between groups of eight rows; the next 16 elements
+//   of the contraction are 32 bytes on
+//   contraction over the rows ("MN-major"): the panel's 64 elements are 64 columns of the tile, `panel` bytes to the
+//   next 64; 1024 bytes between groups of eight rows, 16 of which a matrix instruction takes: the next start 2048 on
+// The low word holds the address and the leading distance in 16 bytes (so 16 bytes further is one more); the high word is the
+// same for all: 1024 bytes between groups, version 1, swizzle mode 2.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t leading) { return ((addr & 0x3ffffu) >> 4) | ((leading >> 4) << 16); }
+
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -322,11 +348,12 @@ __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+// a, b: low words of the operands' descriptors
+__device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)), "n"(kDescHigh) : "memory");
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -343,18 +370,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
-// Shared-memory matrix descriptor, 128-byte swizzle.  A panel has rows of 64 16-bit elements (128 bytes), its eight
-// 16-byte pieces permuted by the row's low three bits; eight rows are 1024 bytes.
-//   contraction along the rows' 64 elements ("K-major"): 1024 bytes between groups of eight rows; the next 16 elements
-//   of the contraction are 32 bytes on
-//   contraction over the rows ("MN-major"): the panel's 64 elements are 64 columns of the tile, `panel` bytes to the
-//   next 64; 1024 bytes between groups of eight rows, 16 of which a matrix instruction takes: the next start 2048 on
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t leading)
-{
-    return (static_cast<uint64_t>(addr & 0x3ffffu) >> 4) | (static_cast<uint64_t>(leading >> 4) << 16) |
-           (static_cast<uint64_t>(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
 }  // namespace sq

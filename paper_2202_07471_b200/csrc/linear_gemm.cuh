@@ -105,16 +105,7 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
             zc[1] = make_uint4(w[4], w[5], w[6], w[7]);
             p.z_exps[row * p.z_exps_pitch + (col >> 5)] = static_cast<uint8_t>(e);
         }
-        if (p.act == kActRelu) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], kActRelu);
-        } else if (p.act == kActGelu) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], kActGelu);
-        } else if (p.act == kActSilu) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = act_value(v[i], kActSilu);
-        }
+        act_values(v, p.act);
         if (p.residual) {
             const uint16_t *r = p.residual + row * p.residual_stride + col;
             if (p.residual_vector && n == 32) {
@@ -140,16 +131,14 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
         if (8 * j < n) store8<kHalf>(out + 8 * j, v + 8 * j, n - 8 * j, p.out_vector);
 }
 
-// The same for four columns a thread: eight neighbouring lanes hold the 32 channels of an exponent.  All lanes of a warp call
-// it; `valid`: this lane's row is there.
+// The same for four columns a thread: eight neighbouring lanes hold the 32 channels of an exponent, all lanes of a warp call it.
 template <int kMode, bool kHalf>
-__device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col, float (&v)[4], bool valid)
+__device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col, const float (&scale)[4], const float (&bias)[4], float (&v)[4])
 {
-    const int n = valid ? p.cols - col : 0;   // columns of this thread, if below four
+    const int n = p.cols - col;   // columns of this thread, if below four
     if constexpr (kMode == kForward) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = i < n ? fmaf(v[i], get(p.scales + col + i), p.bias ? get(p.bias + col + i) : 0.0f) : 0.0f;
+        for (int i = 0; i < 4; ++i) v[i] = fmaf(v[i], scale[i], bias[i]);   // 0 behind the last channel
         if (p.z_codes) {
             float a = 0.0f;
 #pragma unroll
@@ -161,13 +150,12 @@ __device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col,
             uint32_t w = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) w |= static_cast<uint32_t>(ckpt_code(v[i], inverse) & 255) << (8 * i);
-            if (valid && (col & ~31) < p.cols) {   // rows end on 32
+            if ((col & ~31) < p.cols) {   // rows end on 32
                 *reinterpret_cast<uint32_t *>(p.z_codes + row * p.z_pitch + col) = w;
                 if ((col & 31) == 0) p.z_exps[row * p.z_exps_pitch + (col >> 5)] = static_cast<uint8_t>(e);
             }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = act_value(v[i], p.act);
+        act_values(v, p.act);
         if (p.residual) {
             const uint16_t *r = p.residual + row * p.residual_stride + col;
             if (p.residual_vector && n >= 4) {
@@ -193,141 +181,149 @@ __device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col,
     }
 }
 
-constexpr int kFusedRows = 128;       // rows of a tile: the tensor memory's lanes
-constexpr int kFusedCols = 64;
+constexpr int kFusedCols = 128;       // columns of the result a tile: the tensor memory's lanes
+constexpr int kFusedTokens = 128;     // rows of the result a tile, at most
 constexpr int kConverterGroups = 2, kGroupWarps = 4, kConverterWarps = kConverterGroups * kGroupWarps;
 constexpr int kFusedThreads = 32 * (kConverterWarps + 3);   // converters (four of them read the result), copies of either operand, tensor cores
-constexpr int kFusedBytesB = kFusedCols * 128;
-constexpr int kFusedStageBytes = 96 << 10;                  // 4 stages of 128 rows, 6 of up to 64, 8 of up to 32
-constexpr int kFusedMostStages = 8;
-constexpr int kFusedRawBytes = 12 << 10;                    // codes as they are, ahead of the converters
-constexpr int kFusedRawBars = 6;                           // even and a multiple of the stages of codes: one group waits for each
-constexpr int kFusedPartPitch = kFusedCols + 4;             // floats of a row of partial sums: 16-byte accesses hit all banks
-constexpr int kFusedSmem = 1024 + kFusedStageBytes + kFusedRawBytes + 8 * (2 * kFusedMostStages + 2 * kFusedRawBars + 1);
+constexpr int kFusedBytesA = kFusedCols * 128;              // of a stage: 64 codes of 128 columns as 16-bit floats
+constexpr int kFusedMemory = 110 << 10;                     // stages, then codes as they are, ahead of the converters
+constexpr int kFusedMostStages = 3, kFusedMostRaw = 13;
+constexpr int kFusedPartPitch = kFusedCols + 4;             // floats of a token's partial sums
+constexpr int kFusedSmem = 1024 + kFusedMemory + 8 * (4 * kFusedMostStages + 4 * kFusedMostRaw + 1);
 constexpr int kFusedMostRanks = 8;    // thread blocks of a cluster, which share a tile's contraction
-static_assert(4 * kFusedRows * kFusedPartPitch <= kFusedStageBytes, "partial sums take the stages' place");
-// Even: a stage belongs to one group of converters (a waiter must not be more than one phase ahead of its barrier).
-__host__ __device__ constexpr int fused_stages(int box_rows) { return box_rows > 64 ? 4 : box_rows > 32 ? 6 : 8; }
-static_assert(4 * (128 * 128 + kFusedBytesB) <= kFusedStageBytes && 6 * (64 * 128 + kFusedBytesB) <= kFusedStageBytes &&
-              8 * (32 * 128 + kFusedBytesB) <= kFusedStageBytes && 4 * kFusedBytesB >= 128 * 128,
-              "the stages fit, and 128 rows from any stage of the 16-bit operand on are inside them");
+static_assert(4 * (kFusedTokens + kFusedMostRanks - 1) * kFusedPartPitch <= kFusedMemory, "all ranks' sums of a share of the tokens take the stages' place");
+static_assert(2 * (kFusedSmem + 128 + 1024) <= 228 << 10, "two blocks a multiprocessor");
+static_assert(2 * (kFusedBytesA + 128 * kFusedTokens) + 2 * (8 << 10) <= kFusedMemory, "two stages and two of codes fit always");
 
-// One 16-byte piece of a coded row: 32 int4 codes or 16 8-bit codes.  A converter warp takes 16 of a stage's 64 rows of 64
-// codes, neighbouring lanes neighbouring pieces.  Eight lanes then hold all chunks j of 2 or 4 rows whose 16-byte stores, permuted by the
-// row, cover all banks.
-template <int kKind>
+// One 16-byte piece of a coded row: 32 int4 codes or 16 8-bit codes.  Neighbouring converter lanes take the pieces of a row's 64
+// codes, then the next rows': eight lanes hold all chunks j of 2 or 4 rows, whose 16-byte stores, permuted by the row, cover
+// all banks.
+template <int kMode, int kKind>
 struct Pieces {
-    static constexpr int kPerRow = kKind == kInt4 ? 2 : 4;       // pieces of a panel row
-    static constexpr int kChunks = kKind == kInt4 ? 4 : 2;       // 16-byte chunks of 16-bit floats a piece becomes
-    static constexpr int kRows = 32 / kPerRow;                   // rows of a warp's load
-    static constexpr int kCount = 64 / kGroupWarps / kRows;      // loads of a stage
-    static constexpr int kRawBytes = kFusedCols * 16 * kPerRow;  // of a stage
-    static constexpr int kRaw = kFusedRawBytes / kRawBytes;      // stages of codes ahead
+    static constexpr int kPerRow = kKind == kInt4 ? 2 : 4;                       // pieces of a panel row
+    static constexpr int kChunks = kKind == kInt4 ? 4 : 2;                       // 16-byte chunks of 16-bit floats a piece becomes
+    static constexpr int kCount = kFusedCols * kPerRow / (32 * kGroupWarps); // of a converter thread and stage
+    static constexpr int kRawBytes = kFusedCols * kPerRow * 16;                  // of a stage
+
+    int row, panel, sub;
+    // forward: one panel of 128 rows (columns of the result) by 64 codes of the contraction; gradient: two panels of 64 rows (of the
+    // contraction) by 64 columns
+    __device__ __forceinline__ explicit Pieces(int i)
+    {
+        const int piece = static_cast<int>(threadIdx.x) % (32 * kGroupWarps) + i * 32 * kGroupWarps, r = piece / kPerRow;
+        sub = piece % kPerRow;
+        row = kMode == kForward ? r : r & 63;
+        panel = kMode == kForward ? 0 : r >> 6;
+    }
 };
 
 // Rows that start anywhere: straight from global memory.
 template <int kMode, int kKind>
-__device__ __forceinline__ void load_codes(const GemmArgs &p, int col0, int step, int part, uint4 (&c)[Pieces<kKind>::kCount])
+__device__ __forceinline__ uint4 load_codes(const GemmArgs &p, int col0, int step, const Pieces<kMode, kKind> &at)
 {
-    using P = Pieces<kKind>;
-    const int lane = threadIdx.x & 31;
-    // forward: rows are the tile's columns; gradient: rows are the contraction's
-    const int row = (kMode == kForward ? col0 : step * kTileDepth) + 64 / kGroupWarps * part + lane / P::kPerRow;
-    const int first = (kMode == kForward ? step * kTileDepth : col0) + lane % P::kPerRow * (64 / P::kPerRow);
+    const int row = (kMode == kForward ? col0 : step * kTileDepth) + at.row;
+    const int first = (kMode == kForward ? step * kTileDepth : col0 + 64 * at.panel) + at.sub * (64 / at.kPerRow);
     const int off = kKind == kInt4 ? first >> 1 : first;
-    const uint8_t *q = p.codes + static_cast<int64_t>(row) * p.code_pitch + off;
-#pragma unroll
-    for (int i = 0; i < P::kCount; ++i) {
-        c[i] = make_uint4(0, 0, 0, 0);
-        if (row + i * P::kRows < p.code_rows && off < p.code_row_bytes) c[i] = load_bytes16(q, p.codes, p.codes + p.code_bytes);
-        q += P::kRows * p.code_pitch;
-    }
+    if (row >= p.code_rows || off >= p.code_row_bytes) return make_uint4(0, 0, 0, 0);
+    return load_bytes16(p.codes + static_cast<int64_t>(row) * p.code_pitch + off, p.codes, p.codes + p.code_bytes);
 }
 
-template <int kKind>
-__device__ __forceinline__ void read_codes(uint32_t raw, int part, uint4 (&c)[Pieces<kKind>::kCount])
+template <int kMode, int kKind>
+__device__ __forceinline__ uint4 read_codes(uint32_t raw, const Pieces<kMode, kKind> &at)
 {
-    using P = Pieces<kKind>;
-    const uint32_t at = raw + part * (P::kRawBytes / kGroupWarps) + (threadIdx.x & 31) * 16;
-#pragma unroll
-    for (int i = 0; i < P::kCount; ++i)
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(c[i].x), "=r"(c[i].y), "=r"(c[i].z), "=r"(c[i].w) : "r"(at + 512 * i) : "memory");
+    const uint32_t from = raw + ((kMode == kForward ? at.row : 2 * at.row + at.panel) * at.kPerRow + at.sub) * 16;
+    uint4 c;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(c.x), "=r"(c.y), "=r"(c.z), "=r"(c.w) : "r"(from) : "memory");
+    return c;
 }
 
-template <int kKind, bool kHalf>
-__device__ __forceinline__ void store_codes(uint32_t panel, int part, const uint4 (&c)[Pieces<kKind>::kCount])
+template <int kMode, int kKind, bool kHalf>
+__device__ __forceinline__ void store_codes(uint32_t stage, const Pieces<kMode, kKind> &at, const uint4 &c)
 {
-    using P = Pieces<kKind>;
-    const int lane = threadIdx.x & 31, sub = lane % P::kPerRow;
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w}, to = stage + at.panel * 8192 + at.row * 128;
 #pragma unroll
-    for (int i = 0; i < P::kCount; ++i) {
-        const int row = 64 / kGroupWarps * part + i * P::kRows + lane / P::kPerRow;
-        const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
-#pragma unroll
-        for (int j = 0; j < P::kChunks; ++j) {
-            uint32_t o[4];
-            if constexpr (kKind == kInt4) {
-                int4_to_16<kHalf>(w[j], o);
-            } else {
-                int8_to_16<kHalf>(w[2 * j], o);
-                int8_to_16<kHalf>(w[2 * j + 1], o + 2);
-            }
-            const uint32_t chunk = sub * P::kChunks + j;
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(panel + row * 128 + ((chunk ^ (row & 7)) << 4)), "r"(o[0]), "r"(o[1]),
-                         "r"(o[2]), "r"(o[3]) : "memory");
+    for (int j = 0; j < at.kChunks; ++j) {
+        uint32_t o[4];
+        if constexpr (kKind == kInt4) {
+            int4_to_16<kHalf>(w[j], o);
+        } else {
+            int8_to_16<kHalf>(w[2 * j], o);
+            int8_to_16<kHalf>(w[2 * j + 1], o + 2);
         }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((at.sub * at.kChunks + j) ^ (at.row & 7)) << 4)), "r"(o[0]), "r"(o[1]),
+                     "r"(o[2]), "r"(o[3]) : "memory");
     }
 }
 
-// A cluster of `ranks` thread blocks a tile of 128 rows and 64 columns; each takes a share of the contraction.  Reading the
-// codes is most of the work, so the tile is narrow and two blocks share a multiprocessor.  TMA brings the codes as they are
-// ahead; two groups of converter warps turn those of a stage into 16-bit floats in turn.  The issuing warp's loop of one wait, four
-// matrix instructions and one commit is the longest chain: with a barrier for either operand and six converter warps a step of 64
-// took 0.45 us.  Codes loaded by the converters themselves, as rows that start anywhere are (kVector false), cost more: the fence
-// between their stores and the tensor cores' reads waits for a warp's loads in flight, too.  The ranks' sums meet in shared
-// memory, added in the order of the ranks, and each rank finishes a share of the rows.
+// Step k of a ring of n places: place k mod n, barriers k mod 2n.  Two barriers a place, since the steps of a place fall to both
+// groups of converters when n is odd, and a waiter must not be more than one phase ahead of its barrier: with two, the next
+// phase of the barrier that step k waits for (of step k - n) is that of step k + n, which cannot be before step k.
+struct Turn {
+    int n, bar;
+    uint32_t parity = 0;   // of the barriers' phase for this step
+    __device__ __forceinline__ Turn(int places, int k) : n(places), bar(k) {}   // k < 2n
+    __device__ __forceinline__ int place() const { return bar >= n ? bar - n : bar; }
+    __device__ __forceinline__ int before() const { return bar >= n ? bar - n : bar + n; }
+    __device__ __forceinline__ uint32_t before_parity() const { return bar >= n ? parity : parity ^ 1; }
+    __device__ __forceinline__ void next(int by)
+    {
+        bar += by;
+        if (bar >= 2 * n) { bar -= 2 * n; parity ^= 1; }
+    }
+};
+
+// A cluster of `ranks` thread blocks a tile of 128 columns and up to 128 tokens; each takes a share of the contraction, and
+// two blocks share a multiprocessor.  The codes are the matrix instructions' first operand, whose 128 rows they always fill, so
+// that a step of the contraction (64) does as much as it can: the issuing warp's chain of one wait, four matrix instructions and one
+// commit is among the longest (with the tokens as first operand and 64 columns a tile it took 0.33 us for half the codes).  TMA
+// brings the codes as they are ahead, two groups of converter warps turn the stages into 16-bit floats in turn.  Codes loaded by the converters
+// themselves, as rows that start anywhere are (kVector false), cost more: the fence between their stores and the tensor cores' reads
+// waits for a warp's loads in flight, too.  The ranks' sums meet in shared memory, added in the order of the ranks, and each rank
+// finishes a share of the tokens.
 template <int kMode, int kKind, bool kHalf, bool kVector>
 __global__ void __launch_bounds__(kFusedThreads, 2)
 fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const __grid_constant__ GemmArgs p)
 {
-    using P = Pieces<kKind>;
-    static_assert(kFusedRawBars % P::kRaw == 0 && kFusedRawBars % kConverterGroups == 0, "a barrier belongs to one place and one group");
+    using P = Pieces<kMode, kKind>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const int bytes_a = p.box_rows * 128, stages = fused_stages(p.box_rows);
-    const uint32_t smem_a = base, smem_b = base + stages * bytes_a, smem_c = base + kFusedStageBytes;
-    const uint32_t bars = smem_c + kFusedRawBytes;
+    // three stages where that leaves room for two of codes, else two (8-bit codes, more than 64 tokens)
+    const int bytes_b = p.box_rows * 128, stages = kFusedMemory - 3 * (kFusedBytesA + bytes_b) >= 2 * P::kRawBytes ? 3 : 2;
+    const uint32_t smem_a = base, smem_b = base + stages * kFusedBytesA, smem_c = smem_b + stages * bytes_b;
+    const int raws = min(kFusedMostRaw, (kFusedMemory - stages * (kFusedBytesA + bytes_b)) / P::kRawBytes);   // at least two
+    const uint32_t bars = base + kFusedMemory;
     auto full = [&](int s) { return bars + 8 * s; };
-    auto empty = [&](int s) { return bars + 8 * (kFusedMostStages + s); };
-    auto raw_full = [&](int s) { return bars + 8 * (2 * kFusedMostStages + s); };
-    auto raw_empty = [&](int s) { return bars + 8 * (2 * kFusedMostStages + kFusedRawBars + s); };
-    const uint32_t done = bars + 8 * (2 * kFusedMostStages + 2 * kFusedRawBars);
+    auto empty = [&](int s) { return bars + 8 * (2 * kFusedMostStages + s); };
+    auto raw_full = [&](int s) { return bars + 8 * (4 * kFusedMostStages + s); };
+    auto raw_empty = [&](int s) { return bars + 8 * (4 * kFusedMostStages + 2 * kFusedMostRaw + s); };
+    const uint32_t done = bars + 8 * (4 * kFusedMostStages + 4 * kFusedMostRaw);
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_word;
     volatile int *gave_up = &gave_up_word;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), ranks = cluster_ranks();
     const int64_t tile = blockIdx.x / ranks;
-    const int64_t row0 = tile % p.row_tiles * kFusedRows;
+    const int64_t row0 = tile % p.row_tiles * kFusedTokens;
     const int col0 = static_cast<int>(tile / p.row_tiles) * kFusedCols;
     const int all = (p.depth + kTileDepth - 1) / kTileDepth;
     const int first = static_cast<int>(static_cast<int64_t>(all) * rank / ranks);
     const int steps = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / ranks) - first;   // at least one
+    const int here = static_cast<int>(min(static_cast<int64_t>(kFusedTokens), p.rows - row0));
 
     if (threadIdx.x == 0) {
         gave_up_word = 0;
-        for (int s = 0; s < stages; ++s) {
+        for (int s = 0; s < 2 * stages; ++s) {
             bar_init(full(s), 1 + kGroupWarps);
             bar_init(empty(s), 1);
         }
-        for (int s = 0; s < kFusedRawBars; ++s) {
+        for (int s = 0; s < 2 * raws; ++s) {
             bar_init(raw_full(s), 1);
             bar_init(raw_empty(s), kGroupWarps);
         }
         bar_init(done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kConverterWarps + 1) tmem_alloc(smem_addr(&tmem_base), kFusedCols);
+    if (warp == kConverterWarps + 1) tmem_alloc(smem_addr(&tmem_base), kFusedTokens);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -336,135 +332,136 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     wait_for_previous();
 
     if (warp < kConverterWarps) {
-        const int part = warp % kGroupWarps;
-        int s = warp / kGroupWarps;
-        uint32_t parity = 1;   // a stage that was never used counts as empty
-        for (int k = s; k < steps; k += kConverterGroups) {
+        Turn stage(stages, warp / kGroupWarps), raw(raws, warp / kGroupWarps);
+        for (int k = warp / kGroupWarps; k < steps; k += kConverterGroups) {
             uint4 codes[P::kCount];
             if constexpr (kVector) {
-                const int b = k % kFusedRawBars;
-                if (!bar_wait_warp(raw_full(b), k / kFusedRawBars & 1, gave_up)) break;
-                read_codes<kKind>(smem_c + k % P::kRaw * P::kRawBytes, part, codes);
-                __syncwarp();
-                if (lane == 0) bar_arrive(raw_empty(b));
+                if (!bar_wait_warp(raw_full(raw.bar), raw.parity, gave_up)) break;
+#pragma unroll
+                for (int i = 0; i < P::kCount; ++i) codes[i] = read_codes<kMode, kKind>(smem_c + raw.place() * P::kRawBytes, P(i));
             } else {
-                load_codes<kMode, kKind>(p, col0, first + k, part, codes);
+#pragma unroll
+                for (int i = 0; i < P::kCount; ++i) codes[i] = load_codes<kMode, kKind>(p, col0, first + k, P(i));
             }
-            if (!bar_wait_warp(empty(s), parity, gave_up)) break;
-            store_codes<kKind, kHalf>(smem_b + s * kFusedBytesB, part, codes);
+            if (k >= stages && !bar_wait_warp(empty(stage.before()), stage.before_parity(), gave_up)) break;
+#pragma unroll
+            for (int i = 0; i < P::kCount; ++i) store_codes<kMode, kKind, kHalf>(smem_a + stage.place() * kFusedBytesA, P(i), codes[i]);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) bar_arrive(full(s));
-            s += kConverterGroups;
-            if (s >= stages) { s -= stages; parity ^= 1; }
+            if (lane == 0) bar_arrive(full(stage.bar));
+            stage.next(kConverterGroups);
+            if constexpr (kVector) {   // not before: the codes have been read for certain once their floats are stored
+                if (lane == 0) bar_arrive(raw_empty(raw.bar));
+                raw.next(kConverterGroups);
+            }
         }
-        if (warp < 4 && bar_wait_warp(done, 0, gave_up)) {
+        if (bar_wait_warp(done, 0, gave_up)) {
             tc_fence_after();
-            const uint32_t part = base + (warp * 32 + lane) * (4 * kFusedPartPitch);
-            if (row0 + warp * 32 < p.rows) {
+            const int quarter = warp & 3;
+            const uint32_t part = base + 4 * (quarter * 32 + lane);
+            for (int t = warp / 4 * 32; t < here; t += 64) {
+                uint32_t acc[32];
+                tmem_ld32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + t, acc);
 #pragma unroll
-                for (int c = 0; c < kFusedCols; c += 32) {
-                    uint32_t acc[32];
-                    tmem_ld32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + c, acc);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part + 4 * c + 16 * i), "r"(acc[4 * i]), "r"(acc[4 * i + 1]),
-                                     "r"(acc[4 * i + 2]), "r"(acc[4 * i + 3]) : "memory");
-                }
+                for (int i = 0; i < 32; ++i)
+                    if (t + i < here) asm volatile("st.shared.b32 [%0], %1;" ::"r"(part + (t + i) * (4 * kFusedPartPitch)), "r"(acc[i]) : "memory");
             }
             tc_fence_before();
         }
     } else if (warp == kConverterWarps) {
-        bool ok = true;
-        int k = 0, s = 0;
-        uint32_t parity = 1;
+        Turn stage(stages, 0);
+        int k = 0;
         for (; k < steps; ++k) {
-            ok = bar_wait_warp(empty(s), parity, gave_up);
-            if (!ok) break;
+            if (k >= stages && !bar_wait_warp(empty(stage.before()), stage.before_parity(), gave_up)) break;
             if (elect_one()) {
-                bar_expect(full(s), bytes_a);   // rows behind the last token stay what they are: only their own sums see them
-                tma_2d(smem_a + s * bytes_a, &map, (first + k) * kTileDepth, static_cast<int>(row0), full(s));
+                bar_expect(full(stage.bar), bytes_b);
+                tma_2d(smem_b + stage.place() * bytes_b, &map, (first + k) * kTileDepth, static_cast<int>(row0), full(stage.bar));
             }
             __syncwarp();
-            if (++s == stages) { s = 0; parity ^= 1; }
+            stage.next(1);
         }
         // the last copies have landed before the block may end
-        for (int i = 0; i < min(k, stages); ++i) {
-            if (--s < 0) { s = stages - 1; parity ^= 1; }
-            bar_drain(full(s), parity ^ 1);
-        }
+        for (int i = max(0, k - stages); i < k; ++i) bar_drain(full(i % (2 * stages)), i / (2 * stages) & 1);
     } else if (warp == kConverterWarps + 2) {
         if constexpr (kVector) {
             constexpr int along = kKind == kInt4 ? kTileDepth / 2 : kTileDepth;   // bytes of 64 codes
+            Turn raw(raws, 0);
             int k = 0;
             for (; k < steps; ++k) {
-                const int b = k % kFusedRawBars, before = k - P::kRaw;
-                if (before >= 0 && !bar_wait_warp(raw_empty(before % kFusedRawBars), before / kFusedRawBars & 1, gave_up)) break;
+                if (k >= raws && !bar_wait_warp(raw_empty(raw.before()), raw.before_parity(), gave_up)) break;
                 if (elect_one()) {
-                    const uint32_t to = smem_c + k % P::kRaw * P::kRawBytes;
-                    bar_expect(raw_full(b), P::kRawBytes);
-                    if (kMode == kForward) tma_2d(to, &code_map, (first + k) * along, col0, raw_full(b));
-                    else tma_2d(to, &code_map, col0 / kTileDepth * along, (first + k) * kTileDepth, raw_full(b));
+                    const uint32_t to = smem_c + raw.place() * P::kRawBytes;
+                    bar_expect(raw_full(raw.bar), P::kRawBytes);
+                    if (kMode == kForward) tma_2d(to, &code_map, (first + k) * along, col0, raw_full(raw.bar));
+                    else tma_2d(to, &code_map, col0 / 64 * along, (first + k) * kTileDepth, raw_full(raw.bar));
                 }
                 __syncwarp();
+                raw.next(1);
             }
-            for (int i = max(0, k - P::kRaw); i < k; ++i) bar_drain(raw_full(i % kFusedRawBars), i / kFusedRawBars & 1);
+            for (int i = max(0, k - raws); i < k; ++i) bar_drain(raw_full(i % (2 * raws)), i / (2 * raws) & 1);
         }
     } else {
-        constexpr uint32_t kIdesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (kMode != kForward ? 1u << 16 : 0u) |
-                                    (static_cast<uint32_t>(kFusedCols >> 3) << 17) | (static_cast<uint32_t>(kFusedRows >> 4) << 24);
-        constexpr uint32_t kStepB = kMode == kForward ? 32 : 2048;
-        int k = 0, s = 0, last = 0;
-        uint32_t parity = 0;
+        const uint32_t idesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (kMode != kForward ? 1u << 15 : 0u) |
+                               (static_cast<uint32_t>(p.box_rows >> 3) << 17) | (static_cast<uint32_t>(kFusedCols >> 4) << 24);
+        constexpr uint32_t kStepA = kMode == kForward ? 32 : 2048;
+        Turn stage(stages, 0);
+        int k = 0;
+        bool there = false;
         for (; k < steps; ++k) {
-            if (!bar_wait_warp(full(s), parity, gave_up)) break;
+            if (!there && !bar_wait_warp(full(stage.bar), stage.parity, gave_up)) break;
             tc_fence_after();
+            const int now = stage.bar;
+            const uint32_t at = desc_low(smem_a + stage.place() * kFusedBytesA, kMode == kForward ? 16 : 8192);
+            const uint32_t bt = desc_low(smem_b + stage.place() * bytes_b, 16);
+            stage.next(1);
+            there = __all_sync(0xffffffffu, k + 1 < steps && bar_try(full(stage.bar), stage.parity));   // the next step's, while this one's are issued
             if (elect_one()) {
-                const uint32_t at = smem_a + s * bytes_a, bt = smem_b + s * kFusedBytesB;
 #pragma unroll
-                for (int i = 0; i < kTileDepth / 16; ++i)
-                    mma_f16(tmem, smem_desc(at + i * 32, 16), smem_desc(bt + i * kStepB, 16), kIdesc, k > 0 || i > 0);
-                mma_commit(k + 1 == steps ? done : empty(s));
+                for (int i = 0; i < kTileDepth / 16; ++i) mma_f16(tmem, at + i * (kStepA >> 4), bt + i * 2, idesc, k > 0 || i > 0);
+                mma_commit(k + 1 == steps ? done : empty(now));
             }
             __syncwarp();
-            last = s;
-            if (++s == stages) { s = 0; parity ^= 1; }
         }
         // the tensor cores have read their last stage before the block may end
         if (k == steps) bar_drain(done, 0);
-        else if (k > 0) bar_drain(empty(last), s == 0 ? parity ^ 1 : parity);
+        else if (k > 0) bar_drain(empty((k - 1) % (2 * stages)), (k - 1) / (2 * stages) & 1);
     }
     __syncwarp();
-    cluster_arrive_wait();   // all ranks' sums are in shared memory
-    if (warp < kConverterWarps) {   // sixteen threads a row
-        const int here = static_cast<int>(min(static_cast<int64_t>(kFusedRows), p.rows - row0));
-        const int share = (here + static_cast<int>(ranks) - 1) / static_cast<int>(ranks);
-        const int end = min(here, (static_cast<int>(rank) + 1) * share), c = (threadIdx.x & 15) * 4;
-        const bool whole = !*gave_up;
-        for (int r = static_cast<int>(rank) * share + (threadIdx.x >> 4); r - (lane >> 4) < end && whole; r += 2 * kConverterWarps) {
-            float v[4] = {};
-            if (r < end) {
-                const uint32_t mine = base + r * (4 * kFusedPartPitch) + 4 * c;
-                float part[kFusedMostRanks][4];
+    const int col = col0 + 4 * lane;   // a warp finishes tokens, a lane four channels of each
+    float scale[4] = {}, bias[4] = {};
+    if (kMode == kForward && warp < kConverterWarps) {
 #pragma unroll
-                for (uint32_t q = 0; q < kFusedMostRanks; ++q)
-                    if (q < ranks)
-                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(part[q][0]), "=f"(part[q][1]), "=f"(part[q][2]), "=f"(part[q][3])
-                                     : "r"(cluster_addr(mine, q)));
-#pragma unroll
-                for (uint32_t q = 0; q < kFusedMostRanks; ++q)
-                    if (q < ranks)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] += part[q][i];
+        for (int i = 0; i < 4; ++i)
+            if (col + i < p.cols) {
+                scale[i] = get(p.scales + col + i);
+                if (p.bias) bias[i] = get(p.bias + col + i);
             }
-            finish4<kMode, kHalf>(p, row0 + r, col0 + c, v, r < end);
+    }
+    const int share = (here + static_cast<int>(ranks) - 1) / static_cast<int>(ranks);   // of the tokens a rank finishes
+    cluster_arrive_wait();   // all ranks' sums are in shared memory
+    if (warp < kConverterWarps && !*gave_up) {   // a warp a token
+        const int end = min(here, (static_cast<int>(rank) + 1) * share);
+        for (int r = static_cast<int>(rank) * share + warp; r < end; r += kConverterWarps) {
+            const uint32_t mine = base + 4 * (r * kFusedPartPitch + 4 * lane);
+            float v[4] = {}, part[kFusedMostRanks][4];
+#pragma unroll
+            for (uint32_t q = 0; q < kFusedMostRanks; ++q)
+                if (q < ranks)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(part[q][0]), "=f"(part[q][1]), "=f"(part[q][2]), "=f"(part[q][3])
+                                 : "r"(cluster_addr(mine, q)));
+#pragma unroll
+            for (uint32_t q = 0; q < kFusedMostRanks; ++q)
+                if (q < ranks)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] += part[q][i];
+            finish4<kMode, kHalf>(p, row0 + r, col, scale, bias, v);
         }
     }
     __syncwarp();
     cluster_arrive_wait();   // the others' sums stay until they have been read
     if (warp == kConverterWarps + 1) {
         tc_fence_after();
-        tmem_free(tmem, kFusedCols);
+        tmem_free(tmem, kFusedTokens);
     }
 }
 
