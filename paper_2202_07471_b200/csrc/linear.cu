@@ -348,6 +348,8 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
 struct SlopePlan {
     bool dzs = false, dz = false, any = false, dense = false;
     int64_t pitch = 0, slope_bytes = 0;
+    int64_t share = 0, shares = 1;   // tokens of a thread block of slope_kernel
+    int64_t partial_bytes = 0;       // behind dzs and dz: sums of the shares
     int64_t wide_bytes = 0;   // behind them: the codes, then the input as 16-bit floats
     int64_t bytes = 0;
 };
@@ -359,7 +361,11 @@ SlopePlan slope_plan(const squant_linear_grad_args &a)
     s.dzs = a.dx && a.tokens > 0;
     s.dz = a.dweight && a.tokens > 0 && (a.act != SQUANT_ACT_NONE || !rows_on_vectors(a.dy, a.dy_stride, a.tokens));
     s.any = s.dzs || s.dz || a.dbias || a.dscales;
-    s.slope_bytes = (s.dzs + s.dz) * a.tokens * s.pitch * 2;
+    const int64_t columns = (static_cast<int64_t>(a.cout) + sq::kSlopeCols - 1) / sq::kSlopeCols;
+    s.shares = std::max<int64_t>(1, std::min(sq::kSlopeBlocks / columns, (a.tokens + sq::kSlopeLeast - 1) / sq::kSlopeLeast));
+    s.share = std::max<int64_t>(1, (a.tokens + s.shares - 1) / s.shares);
+    if (s.shares > 1 && (a.dbias || a.dscales)) s.partial_bytes = up(s.shares * 2 * a.cout * 4, 16);
+    s.slope_bytes = (s.dzs + s.dz) * a.tokens * s.pitch * 2 + s.partial_bytes;
     s.dense = s.dzs && a.tokens > kFusedTokens;
     const int64_t row = up(a.cin, 8) * 2;
     s.wide_bytes = std::max(s.dense ? a.cout * row : 0, a.dweight ? a.tokens * row : 0);
@@ -387,12 +393,11 @@ int check(const squant_linear_grad_args *args)
     return SQUANT_OK;
 }
 
-int slope(const squant_linear_grad_args &a, const SlopePlan &plan, uint16_t *dzs, uint16_t *dz, cudaStream_t stream)
+int slope(const squant_linear_grad_args &a, const SlopePlan &plan, uint16_t *dzs, uint16_t *dz, float *partial, cudaStream_t stream)
 {
     sq::SlopeArgs s{};
     s.dy = static_cast<const uint16_t *>(a.dy);
     s.dy_stride = a.dy_stride;
-    s.dy_vector = rows_on_vectors(a.dy, a.dy_stride, a.tokens);
     const bool need_z = a.act != SQUANT_ACT_NONE || a.dscales;
     s.z_codes = need_z ? reinterpret_cast<const uint8_t *>(a.z.codes) : nullptr;
     s.z_exps = need_z ? a.z.exps : nullptr;
@@ -408,9 +413,21 @@ int slope(const squant_linear_grad_args &a, const SlopePlan &plan, uint16_t *dzs
     s.pitch = plan.pitch;
     s.dbias = a.dbias;
     s.dscales = a.dscales;
-    const unsigned ranks = static_cast<unsigned>(std::min<int64_t>(sq::kSlopeCluster, std::max<int64_t>(1, (a.tokens + 31) / 32)));
+    s.share = plan.share;
+    s.shares = static_cast<int32_t>(plan.shares);
+    s.partial = plan.partial_bytes ? partial : nullptr;
     const unsigned columns = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kSlopeCols - 1) / sq::kSlopeCols);
-    return launch(sq::slope_kernel, dim3(columns, ranks), dim3(1, ranks), sq::kRowThreads, 0, stream, s);
+    const bool vector = a.cout % 4 == 0 && !misaligned(a.dy, 8) && (a.tokens <= 1 || a.dy_stride % 4 == 0);
+    void (*kernel)(sq::SlopeArgs) = nullptr;
+    if (!need_z) kernel = vector ? sq::slope_kernel<sq::kNoZ, true> : sq::slope_kernel<sq::kNoZ, false>;
+    else if (a.act == SQUANT_ACT_NONE) kernel = vector ? sq::slope_kernel<sq::kActNone, true> : sq::slope_kernel<sq::kActNone, false>;
+    else if (a.act == SQUANT_ACT_RELU) kernel = vector ? sq::slope_kernel<sq::kActRelu, true> : sq::slope_kernel<sq::kActRelu, false>;
+    else if (a.act == SQUANT_ACT_GELU) kernel = vector ? sq::slope_kernel<sq::kActGelu, true> : sq::slope_kernel<sq::kActGelu, false>;
+    else kernel = vector ? sq::slope_kernel<sq::kActSilu, true> : sq::slope_kernel<sq::kActSilu, false>;
+    if (int rc = launch(kernel, dim3(columns, static_cast<unsigned>(plan.shares)), dim3(1), sq::kRowThreads, 0, stream, s)) return rc;
+    if (!s.partial) return SQUANT_OK;
+    const unsigned grid = static_cast<unsigned>((2 * static_cast<int64_t>(a.cout) + sq::kRowThreads - 1) / sq::kRowThreads);
+    return launch(sq::sums_kernel, dim3(grid), dim3(1), sq::kRowThreads, 0, stream, s);
 }
 
 }  // namespace
@@ -496,8 +513,9 @@ int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_strea
     if (int rc = device_sms(device, sms)) return rc;
     uint16_t *dzs = plan.dzs ? static_cast<uint16_t *>(a.workspace) : nullptr;
     uint16_t *dz = plan.dz ? static_cast<uint16_t *>(a.workspace) + (plan.dzs ? a.tokens * plan.pitch : 0) : nullptr;
+    float *partial = reinterpret_cast<float *>(static_cast<uint8_t *>(a.workspace) + plan.slope_bytes - plan.partial_bytes);
     if (plan.any)
-        if (int rc = slope(a, plan, dzs, dz, stream)) return rc;
+        if (int rc = slope(a, plan, dzs, dz, partial, stream)) return rc;
     uint8_t *wide = static_cast<uint8_t *>(a.workspace) + plan.slope_bytes;
     if (plan.dzs) {
         const bool packed = a.flags & SQUANT_FLAG_PACK_INT4;

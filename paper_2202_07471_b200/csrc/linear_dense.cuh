@@ -168,7 +168,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                                     (kMode == kWeightGrad ? 1u << 15 : 0u) | (kMode != kForward ? 1u << 16 : 0u) |
                                     (static_cast<uint32_t>(kCols >> 3) << 17) | (static_cast<uint32_t>(kPairRows >> 4) << 24);
         constexpr uint32_t kStepA = kMode == kWeightGrad ? 2048 : 32, kStepB = kMode == kForward ? 32 : 2048;
-        bool ok = true, there = false;
+        bool ok = true;
         int s = 0, n = 0;
         uint32_t parity = 0;
         for (int64_t t = pair; t < p.tiles && ok; t += pairs, ++n) {
@@ -177,22 +177,20 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (!ok) break;
             tc_fence_after();
             for (int k = 0; k < steps; ++k) {
-                ok = there || bar_wait_warp(full(s), parity, gave_up);
+                ok = bar_wait_warp(full(s), parity, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                const int now = s;
                 const uint32_t at = desc_low(smem_a + s * S::kBytesA, kMode == kWeightGrad ? 8192 : 16);
                 const uint32_t bt = desc_low(smem_b + s * S::kBytesB, kMode == kForward ? 16 : 8192);
-                if (++s == S::kStages) { s = 0; parity ^= 1; }
-                there = __all_sync(0xffffffffu, bar_try(full(s), parity));   // the next step's copies, while this one's products are issued
                 if (elect_one()) {
 #pragma unroll
                     for (int i = 0; i < kTileDepth / 16; ++i)
                         pair_mma_f16(tmem + a * kCols, at + i * (kStepA >> 4), bt + i * (kStepB >> 4), kIdesc, k > 0 || i > 0);
-                    pair_commit(empty(now));
+                    pair_commit(empty(s));
                     if (k + 1 == steps) pair_commit(acc_full(a));
                 }
                 __syncwarp();
+                if (++s == S::kStages) { s = 0; parity ^= 1; }
             }
         }
     }

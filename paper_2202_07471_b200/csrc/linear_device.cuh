@@ -32,11 +32,15 @@ __device__ __forceinline__ float ckpt_inverse(uint32_t e)   // 2^(127 - E); 0 fo
 {
     return e == 255u ? 0.0f : __uint_as_float((254u - e) << 23);
 }
-__device__ __forceinline__ int ckpt_code(float v, float inverse)
+// Codes of four values, the first in the low byte.  The product with a power of two is exact unless it is far below one half;
+// adding 1.5 * 2^23 rounds it to an integer, ties to even, whose low byte is the code.  In a group that is not finite the codes are 0.
+__device__ __forceinline__ uint32_t ckpt_codes(const float *v, float inverse)
 {
-    // the product is exact unless it is far below one half; 0 * inf is NaN, which __float2int_rn turns into 0
-    const int q = __float2int_rn(v * inverse);
-    return q > 127 ? 127 : q < -127 ? -127 : q;
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(__fadd_rn(fminf(fmaxf(__fmul_rn(v[i], inverse), -127.0f), 127.0f), 12582912.0f));
+    const uint32_t w = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
+    return inverse == 0.0f ? 0u : w;
 }
 __device__ __forceinline__ float ckpt_scale(uint32_t e) { return __uint_as_float(e << 23); }   // 255: inf, 0 * inf = NaN
 // max that keeps a NaN
@@ -49,64 +53,99 @@ __device__ __forceinline__ float max_nan(float a, float b)
 
 // ---------------------------------------------------------------- activations (fp32)
 
-// P(N(0, 1) > a) for a >= 0 and e = exp(-a^2 / 2): e times a polynomial in u = 1 / (1 + 0.3 a) without a constant term, since
-// exp(a^2 / 2) P falls like 1 / a.  The coefficients are a weighted least-squares fit of erfcx(a / sqrt 2) / 2 over [0, 14], at
-// most 1.5e-7 of the value off; beyond, the value is no normal fp32 number.  gelu and its slope share e, and the tail keeps its
-// relative accuracy, which 1 + erf(z / sqrt 2) would lose.  A fifth of the instructions of erfcf() and expf().
-__device__ __forceinline__ float normal_tail(float a, float e)
+// Two fp32 operations in one instruction.
+struct Two {
+    uint64_t v;
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ explicit Two(uint64_t u) : v(u) {}
+    __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Two fma(Two a, Two b, Two c)
 {
-    const float u = __fdividef(1.0f, fmaf(a, 0.3f, 1.0f));
-    float q = 0.03567597f;
-    q = fmaf(q, u, -0.15720823f);
-    q = fmaf(q, u, 0.20636259f);
-    q = fmaf(q, u, -0.05369217f);
-    q = fmaf(q, u, 0.1285662f);
-    q = fmaf(q, u, 0.0999121f);
-    q = fmaf(q, u, 0.12075418f);
-    q = fmaf(q, u, 0.11962928f);
-    return e * (q * u);
+    Two r(0ull);
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
 }
-__device__ __forceinline__ float normal_below(float z, float e)   // P(N(0, 1) < z)
+__device__ __forceinline__ Two mul(Two a, Two b)
 {
-    const float h = normal_tail(fabsf(z), e);
-    return z < 0.0f ? h : 1.0f - h;
+    Two r(0ull);
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+
+// P(N(0, 1) < z) of two values and e = exp(-z^2 / 2).  With a = |z| the upper tail is e times a polynomial in u = 1 / (1 + 0.3 a)
+// without a constant term, since exp(a^2 / 2) P falls like 1 / a.  The coefficients are a weighted least-squares fit of
+// erfcx(a / sqrt 2) / 2 over [0, 14], at most 1.5e-7 of the value off (4.8e-7 in fp32); beyond, the value is no normal fp32 number.
+// gelu and its slope share e, and the tail keeps its relative accuracy, which 1 + erf(z / sqrt 2) would lose.  Two values at a
+// time take 23 instructions, erfcf() and expf() of both about 180.
+__device__ __forceinline__ void normal_below(float z0, float z1, float &p0, float &p1, float &e0, float &e1)
+{
+    float x0, x1, d0, d1, h0, h1;
+    const Two z(z0, z1), half(-0.5f, -0.5f);
+    mul(mul(z, half), z).get(x0, x1);
+    e0 = __expf(x0);
+    e1 = __expf(x1);
+    fma(Two(fabsf(z0), fabsf(z1)), Two(0.3f, 0.3f), Two(1.0f, 1.0f)).get(d0, d1);
+    const Two u(__fdividef(1.0f, d0), __fdividef(1.0f, d1));
+    Two q(0.03567597f, 0.03567597f);
+    q = fma(q, u, Two(-0.15720823f, -0.15720823f));
+    q = fma(q, u, Two(0.20636259f, 0.20636259f));
+    q = fma(q, u, Two(-0.05369217f, -0.05369217f));
+    q = fma(q, u, Two(0.1285662f, 0.1285662f));
+    q = fma(q, u, Two(0.0999121f, 0.0999121f));
+    q = fma(q, u, Two(0.12075418f, 0.12075418f));
+    q = fma(q, u, Two(0.11962928f, 0.11962928f));
+    mul(mul(q, u), Two(e0, e1)).get(h0, h1);
+    p0 = z0 < 0.0f ? h0 : 1.0f - h0;
+    p1 = z1 < 0.0f ? h1 : 1.0f - h1;
 }
 __device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
-__device__ __forceinline__ float act_value(float z, int act)
-{
-    if (act == kActRelu) return z < 0.0f ? 0.0f : z;   // keeps a NaN
-    if (act == kActGelu) return z * normal_below(z, __expf(-0.5f * z * z));
-    if (act == kActSilu) return z * sigmoid(z);
-    return z;
-}
-// One branch for all values.
+// act(v) of all values: one branch for all.
 template <int kCount>
 __device__ __forceinline__ void act_values(float (&v)[kCount], int act)
 {
     if (act == kActRelu) {
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) v[i] = act_value(v[i], kActRelu);
+        for (int i = 0; i < kCount; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];   // keeps a NaN
     } else if (act == kActGelu) {
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) v[i] = act_value(v[i], kActGelu);
+        for (int i = 0; i < kCount; i += 2) {
+            float p0, p1, e0, e1;
+            normal_below(v[i], v[i + 1], p0, p1, e0, e1);
+            v[i] *= p0;
+            v[i + 1] *= p1;
+        }
     } else if (act == kActSilu) {
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) v[i] = act_value(v[i], kActSilu);
+        for (int i = 0; i < kCount; ++i) v[i] *= sigmoid(v[i]);
     }
 }
-__device__ __forceinline__ float act_slope(float z, int act)
+__device__ __forceinline__ float act_value(float z, int act)
 {
-    if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == kActGelu) {
-        const float e = __expf(-0.5f * z * z);
-        return fmaf(z * 0.39894228040143268f, e, normal_below(z, e));
+    float v[2] = {z, z};
+    act_values(v, act);
+    return v[0];
+}
+// act'(z)
+template <int kAct, int kCount>
+__device__ __forceinline__ void act_slopes(const float (&z)[kCount], float (&slope)[kCount])
+{
+#pragma unroll
+    for (int i = 0; i < kCount; i += 2) {
+        if constexpr (kAct == kActGelu) {
+            float p0, p1, e0, e1;
+            normal_below(z[i], z[i + 1], p0, p1, e0, e1);
+            slope[i] = fmaf(z[i] * 0.39894228040143268f, e0, p0);
+            slope[i + 1] = fmaf(z[i + 1] * 0.39894228040143268f, e1, p1);
+        } else {
+#pragma unroll
+            for (int j = i; j < i + 2; ++j) {
+                const float p = kAct == kActSilu ? sigmoid(z[j]) : 0.0f;
+                slope[j] = kAct == kActSilu ? p * fmaf(z[j], 1.0f - p, 1.0f) : kAct == kActRelu ? (z[j] > 0.0f ? 1.0f : 0.0f) : 1.0f;
+            }
+        }
     }
-    if (act == kActSilu) {
-        const float p = sigmoid(z);
-        return p * fmaf(z, 1.0f - p, 1.0f);
-    }
-    return 1.0f;
 }
 
 // ---------------------------------------------------------------- 16-bit types

@@ -93,13 +93,12 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
             const uint32_t e = ckpt_exponent(a);
             const float inverse = ckpt_inverse(e);
             uint32_t w[8];
+            if (n < 32)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] = 0;
+                for (int i = 0; i < 32; ++i)
+                    if (i >= n) v[i] = 0.0f;
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    if (4 * i + b < n) w[i] |= static_cast<uint32_t>(ckpt_code(v[4 * i + b], inverse) & 255) << (8 * b);
-            }
+            for (int i = 0; i < 8; ++i) w[i] = ckpt_codes(v + 4 * i, inverse);
             uint4 *zc = reinterpret_cast<uint4 *>(p.z_codes + row * p.z_pitch + col);
             zc[0] = make_uint4(w[0], w[1], w[2], w[3]);
             zc[1] = make_uint4(w[4], w[5], w[6], w[7]);
@@ -147,9 +146,7 @@ __device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col,
             for (int s = 1; s <= 4; s <<= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, s));
             const uint32_t e = ckpt_exponent(a);
             const float inverse = ckpt_inverse(e);
-            uint32_t w = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w |= static_cast<uint32_t>(ckpt_code(v[i], inverse) & 255) << (8 * i);
+            const uint32_t w = ckpt_codes(v, inverse);
             if ((col & ~31) < p.cols) {   // rows end on 32
                 *reinterpret_cast<uint32_t *>(p.z_codes + row * p.z_pitch + col) = w;
                 if ((col & 31) == 0) p.z_exps[row * p.z_exps_pitch + (col >> 5)] = static_cast<uint8_t>(e);
@@ -406,21 +403,18 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
         constexpr uint32_t kStepA = kMode == kForward ? 32 : 2048;
         Turn stage(stages, 0);
         int k = 0;
-        bool there = false;
         for (; k < steps; ++k) {
-            if (!there && !bar_wait_warp(full(stage.bar), stage.parity, gave_up)) break;
+            if (!bar_wait_warp(full(stage.bar), stage.parity, gave_up)) break;
             tc_fence_after();
-            const int now = stage.bar;
             const uint32_t at = desc_low(smem_a + stage.place() * kFusedBytesA, kMode == kForward ? 16 : 8192);
             const uint32_t bt = desc_low(smem_b + stage.place() * bytes_b, 16);
-            stage.next(1);
-            there = __all_sync(0xffffffffu, k + 1 < steps && bar_try(full(stage.bar), stage.parity));   // the next step's, while this one's are issued
             if (elect_one()) {
 #pragma unroll
                 for (int i = 0; i < kTileDepth / 16; ++i) mma_f16(tmem, at + i * (kStepA >> 4), bt + i * 2, idesc, k > 0 || i > 0);
-                mma_commit(k + 1 == steps ? done : empty(now));
+                mma_commit(k + 1 == steps ? done : empty(stage.bar));
             }
             __syncwarp();
+            stage.next(1);
         }
         // the tensor cores have read their last stage before the block may end
         if (k == steps) bar_drain(done, 0);

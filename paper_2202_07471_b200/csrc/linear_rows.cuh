@@ -2,8 +2,6 @@
 // pre-activation with the sums over the tokens, and copies of rows that TMA cannot read.
 #pragma once
 
-#include <cooperative_groups.h>
-
 #include "linear_device.cuh"
 
 namespace sq {
@@ -79,9 +77,7 @@ static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const Ro
         a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, 2));
         const uint32_t e = ckpt_exponent(a);
         const float inverse = ckpt_inverse(e);
-        uint32_t w[2] = {0, 0};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j >> 2] |= static_cast<uint32_t>(ckpt_code(f[j], inverse) & 255) << (8 * (j & 3));
+        const uint32_t w[2] = {ckpt_codes(f, inverse), ckpt_codes(f + 4, inverse)};
         if (first + i * kRowThreads < total) {
             *reinterpret_cast<uint2 *>(p.codes + row[i] * p.code_pitch + col[i]) = make_uint2(w[0], w[1]);
             if ((threadIdx.x & 3) == 0) p.exps[row[i] * p.exps_pitch + (col[i] >> 5)] = static_cast<uint8_t>(e);
@@ -191,7 +187,6 @@ static __global__ void __launch_bounds__(kRowThreads) align_kernel(const RowArgs
 struct SlopeArgs {
     const uint16_t *dy;
     int64_t dy_stride;
-    int32_t dy_vector;
     const uint8_t *z_codes, *z_exps;   // null: no activation and no gradient of the scales
     int64_t z_pitch, z_exps_pitch;
     const float *scales, *bias;
@@ -200,96 +195,147 @@ struct SlopeArgs {
     uint16_t *dz, *dzs;                // null where not wanted
     int64_t pitch;                     // elements, a multiple of 8
     float *dbias, *dscales;            // null where not wanted
+    int64_t share;                     // tokens of a thread block
+    float *partial;                    // [shares][2][cout] sums of the shares; null: there is one
+    int32_t shares;
 };
 
-constexpr int kSlopeCols = 64;      // a thread block's columns: eight threads of eight, 32 rows at a time
-constexpr int kSlopeCluster = 8;    // thread blocks that share the tokens of the same columns
+constexpr int kSlopeCols = 64;      // a thread block's columns: sixteen threads of four, 16 rows at a time
+constexpr int kSlopeRows = kRowThreads / 16;
+constexpr int kSlopeBatch = 4;      // rows a thread has in flight
+constexpr int kSlopeBlocks = 592;   // wanted of a launch: three a multiprocessor of a B200
+constexpr int kSlopeLeast = 64;     // tokens of a share
+
+template <int kValue>
+struct Count {
+    static constexpr int value = kValue;
+};
+
+// Four 16-bit values of a row, of which n are inside the row.
+__device__ __forceinline__ uint2 load4(const uint16_t *at, int n, bool vector)
+{
+    if (vector && n >= 4) return get(reinterpret_cast<const uint2 *>(at));
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = (2 * i < n ? static_cast<uint32_t>(get(at + 2 * i)) : 0u) | (2 * i + 1 < n ? static_cast<uint32_t>(get(at + 2 * i + 1)) << 16 : 0u);
+    return make_uint2(w[0], w[1]);
+}
 
 // dz = dy * act'(zhat) in bf16, and times the scales; sums over the tokens of dz and of dz * (zhat - bias) / scale in
-// fp32 from the unrounded products.  The thread blocks of a cluster each take a range of tokens; their sums meet
-// through distributed shared memory in a fixed order, so that a call repeats to the bit.
-static __global__ void __launch_bounds__(kRowThreads) slope_kernel(const __grid_constant__ SlopeArgs p)
+// fp32 from the unrounded products.  Thread blocks share the tokens; the sums of their shares go through global memory and are
+// added in their order by sums_kernel, so that a call repeats to the bit.  What the kernel needs is loads in flight: four columns a
+// thread keep sums and factors in few registers.  (Eight columns a thread and shares joined by clusters of eight, which allow 264
+// blocks at once, took 34 to 50 us for 4096 x 4096.)
+// kAct: kActNone and so on, or kNoZ where zhat is not needed.  kVector: whole vectors of four, rows of dy start on 8 bytes.
+constexpr int kNoZ = -1;
+template <int kAct, bool kVector>
+__global__ void __launch_bounds__(kRowThreads, 4) slope_kernel(const __grid_constant__ SlopeArgs p)
 {
-    namespace cg = cooperative_groups;
     next_may_start();
     wait_for_previous();
-    cg::cluster_group cluster = cg::this_cluster();
-    const int ranks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
-    const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, warp = threadIdx.x >> 5;
-    const int col = blockIdx.x * kSlopeCols + tx * 8;
-    const int n = p.cout - col;   // columns of this thread inside the row, possibly none
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, warp = threadIdx.x >> 5;
+    const int col = blockIdx.x * kSlopeCols + tx * 4;
+    const int n = kVector ? (col < p.cout ? 4 : 0) : p.cout - col;   // columns of this thread inside the row, possibly none
     __shared__ float part[kRowThreads / 32][2 * kSlopeCols];
-    __shared__ float sums[2 * kSlopeCols];
-    float scale[8], bias[8], db[8] = {}, ds[8] = {};
+    float scale[4], bias[4], db[4] = {}, ds[4] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        scale[i] = i < n ? get(p.scales + col + i) : 1.0f;
+    for (int i = 0; i < 4; ++i) {
+        scale[i] = i < n && p.dzs ? get(p.scales + col + i) : 1.0f;
         bias[i] = i < n && p.bias ? get(p.bias + col + i) : 0.0f;
     }
-    const int64_t share = ((p.tokens + ranks - 1) / ranks + 31) / 32 * 32;
-    const int64_t end = min(p.tokens, (rank + 1) * share);
-    if (n > 0)
-#pragma unroll 2
-        for (int64_t t = rank * share + ty; t < end; t += 32) {
-            float dz[8];
-            unpack8(load8(p.dy + t * p.dy_stride + col, n, p.dy_vector), dz);
-            if (p.z_codes) {
-                const uint2 c = get(reinterpret_cast<const uint2 *>(p.z_codes + t * p.z_pitch + col));
-                const float zs = ckpt_scale(get(p.z_exps + t * p.z_exps_pitch + (col >> 5)));
+    const int64_t end = min(p.tokens, (blockIdx.y + 1) * p.share);
+    if (n > 0) {
+        int64_t t0 = blockIdx.y * p.share + ty;
+        const uint16_t *dy_at = p.dy + t0 * p.dy_stride + col;
+        const uint8_t *zc_at = p.z_codes + t0 * p.z_pitch + col, *ze_at = p.z_exps + t0 * p.z_exps_pitch + (col >> 5);
+        const int64_t out0 = t0 * p.pitch + col;
+        uint16_t *dz_at = p.dz + out0, *dzs_at = p.dzs + out0;
+        // whole batches without a look at the end, then what is left row by row
+        auto rows = [&](auto count) {
+            constexpr int kCount = decltype(count)::value;
+            uint2 dy[kCount];
+            [[maybe_unused]] uint32_t zc[kCount], ze[kCount];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float z = zs * static_cast<float>(static_cast<int8_t>((i < 4 ? c.x : c.y) >> (8 * (i & 3))));
-                    if (i < n) {
-                        dz[i] *= act_slope(z, p.act);
-                        ds[i] = fmaf(dz[i], z - bias[i], ds[i]);
-                    }
+            for (int b = 0; b < kCount; ++b) {
+                if constexpr (kVector) dy[b] = get(reinterpret_cast<const uint2 *>(dy_at));
+                else dy[b] = load4(dy_at, n, false);
+                dy_at += kSlopeRows * p.dy_stride;
+                if constexpr (kAct != kNoZ) {
+                    zc[b] = get(reinterpret_cast<const uint32_t *>(zc_at));
+                    ze[b] = get(ze_at);
+                    zc_at += kSlopeRows * p.z_pitch;
+                    ze_at += kSlopeRows * p.z_exps_pitch;
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) db[i] += dz[i];
-            if (p.dz)
-                *reinterpret_cast<uint4 *>(p.dz + t * p.pitch + col) = make_uint4(to_16x2<false>(dz[0], dz[1]), to_16x2<false>(dz[2], dz[3]),
-                                                                                  to_16x2<false>(dz[4], dz[5]), to_16x2<false>(dz[6], dz[7]));
-            if (p.dzs)
-                *reinterpret_cast<uint4 *>(p.dzs + t * p.pitch + col) =
-                    make_uint4(to_16x2<false>(dz[0] * scale[0], dz[1] * scale[1]), to_16x2<false>(dz[2] * scale[2], dz[3] * scale[3]),
-                               to_16x2<false>(dz[4] * scale[4], dz[5] * scale[5]), to_16x2<false>(dz[6] * scale[6], dz[7] * scale[7]));
-        }
+            for (int b = 0; b < kCount; ++b) {
+                float dz[4] = {__uint_as_float(dy[b].x << 16), __uint_as_float(dy[b].x & 0xffff0000u), __uint_as_float(dy[b].y << 16),
+                               __uint_as_float(dy[b].y & 0xffff0000u)};
+                if constexpr (kAct != kNoZ) {
+                    const float zs = ckpt_scale(ze[b]);
+                    float z[4], slope[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] = zs * static_cast<float>(static_cast<int8_t>(zc[b] >> (8 * i)));
+                    act_slopes<kAct>(z, slope);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (kVector || i < n) {   // behind the row's end an exponent may stand for NaN
+                            dz[i] *= slope[i];
+                            ds[i] = fmaf(dz[i], z[i] - bias[i], ds[i]);
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) db[i] += dz[i];
+                if (p.dz) *reinterpret_cast<uint2 *>(dz_at) = make_uint2(to_16x2<false>(dz[0], dz[1]), to_16x2<false>(dz[2], dz[3]));
+                if (p.dzs)
+                    *reinterpret_cast<uint2 *>(dzs_at) = make_uint2(to_16x2<false>(dz[0] * scale[0], dz[1] * scale[1]),
+                                                                    to_16x2<false>(dz[2] * scale[2], dz[3] * scale[3]));
+                dz_at += kSlopeRows * p.pitch;
+                dzs_at += kSlopeRows * p.pitch;
+            }
+        };
+        for (; t0 + (kSlopeBatch - 1) * kSlopeRows < end; t0 += kSlopeBatch * kSlopeRows) rows(Count<kSlopeBatch>{});
+        for (; t0 < end; t0 += kSlopeRows) rows(Count<1>{});
+    }
     if (!p.dbias && !p.dscales) return;   // the same for all threads of the launch
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i) {
+        db[i] += __shfl_xor_sync(0xffffffffu, db[i], 16);
+        ds[i] += __shfl_xor_sync(0xffffffffu, ds[i], 16);
+    }
+    if ((threadIdx.x & 31) < 16)
 #pragma unroll
-        for (int s = 8; s <= 16; s <<= 1) {
-            db[i] += __shfl_xor_sync(0xffffffffu, db[i], s);
-            ds[i] += __shfl_xor_sync(0xffffffffu, ds[i], s);
-        }
-    if ((threadIdx.x & 31) < 8)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            part[warp][tx * 8 + i] = db[i];
-            part[warp][kSlopeCols + tx * 8 + i] = ds[i];
+        for (int i = 0; i < 4; ++i) {
+            part[warp][tx * 4 + i] = db[i];
+            part[warp][kSlopeCols + tx * 4 + i] = ds[i];
         }
     __syncthreads();
-    if (threadIdx.x < 2 * kSlopeCols) {
+    const int which = threadIdx.x / kSlopeCols, c = blockIdx.x * kSlopeCols + static_cast<int>(threadIdx.x) % kSlopeCols;
+    if (which < 2 && c < p.cout) {
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < kRowThreads / 32; ++w) s += part[w][threadIdx.x];
-        sums[threadIdx.x] = s;
+        if (p.partial) p.partial[(static_cast<int64_t>(blockIdx.y) * 2 + which) * p.cout + c] = s;
+        else if (which == 0 && p.dbias) p.dbias[c] = s;
+        else if (which == 1 && p.dscales) p.dscales[c] = s / get(p.scales + c);
     }
-    cluster.sync();
-    if (rank == 0 && threadIdx.x < 2 * kSlopeCols) {
-        float s = 0.0f;
-        for (int r = 0; r < ranks; ++r) s += cluster.map_shared_rank(sums, r)[threadIdx.x];
-        const int c = blockIdx.x * kSlopeCols + (threadIdx.x & (kSlopeCols - 1));
-        if (c < p.cout) {
-            if (threadIdx.x < kSlopeCols) {
-                if (p.dbias) p.dbias[c] = s;
-            } else if (p.dscales) {
-                p.dscales[c] = s / get(p.scales + c);
-            }
-        }
-    }
-    cluster.sync();   // the others' sums stay until rank 0 has read them
+}
+
+static __global__ void __launch_bounds__(kRowThreads) sums_kernel(const __grid_constant__ SlopeArgs p)
+{
+    next_may_start();
+    wait_for_previous();
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
+    if (i >= 2 * static_cast<int64_t>(p.cout)) return;
+    const bool scales = i >= p.cout;
+    const int64_t c = scales ? i - p.cout : i;
+    if (scales ? !p.dscales : !p.dbias) return;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int r = 0; r < p.shares; ++r) s += get(p.partial + static_cast<int64_t>(r) * 2 * p.cout + i);
+    if (scales) p.dscales[c] = s / get(p.scales + c);
+    else p.dbias[c] = s;
 }
 
 }  // namespace sq
