@@ -170,6 +170,12 @@ enum class RowKernel { kCheckpoint, kRestore, kAlign, kExpandInt4Bf16, kExpandIn
 int launch_rows(RowKernel which, sq::RowArgs a, int64_t rows, cudaStream_t stream)
 {
     const int64_t most = std::max<int64_t>(1, ((1ll << 31) - 4096) / a.pieces);
+    // with 2^(L-1) < pieces <= 2^L and magic = floor(2^(31+L) / pieces) + 1, at * magic / 2^(31+L) exceeds at / pieces by less than
+    // at / 2^(31+L) < 1 / pieces
+    uint32_t bits = 0;
+    while ((1ull << bits) < a.pieces) ++bits;
+    a.magic = bits ? static_cast<uint32_t>((1ull << (31 + bits)) / a.pieces + 1) : 0;
+    a.shift = bits ? bits - 1 : 0;
     for (int64_t r = 0; r < rows; r += most) {
         sq::RowArgs b = a;
         b.rows = static_cast<uint32_t>(std::min(most, rows - r));

@@ -47,8 +47,11 @@ struct RowArgs {
     uint8_t *codes, *exps;
     int64_t in_stride, out_stride, code_pitch, exps_pitch;
     uint32_t rows, pieces;   // pieces of eight elements a row
+    uint32_t magic, shift;   // at / pieces = at * magic >> 32 >> shift for at < 2^31; magic 0: one piece a row
     int32_t features, vector;
 };
+
+__device__ __forceinline__ uint32_t row_of(const RowArgs &p, uint32_t at) { return p.magic ? __umulhi(at, p.magic) >> p.shift : at; }
 
 // Four lanes share a group of 32 features.
 static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const RowArgs p)
@@ -62,7 +65,7 @@ static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const Ro
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
         const uint32_t at = first + i * kRowThreads;
-        row[i] = at / p.pieces;
+        row[i] = row_of(p, at);
         col[i] = static_cast<int>(at - row[i] * p.pieces) * 8;
         v[i] = make_uint4(0, 0, 0, 0);
         if (at < total && col[i] < p.features) v[i] = load8(p.in + row[i] * p.in_stride + col[i], p.features - col[i], p.vector);
@@ -96,7 +99,7 @@ static __global__ void __launch_bounds__(kRowThreads) restore_kernel(const RowAr
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
         const uint32_t at = first + i * kRowThreads;
-        row[i] = at / p.pieces;
+        row[i] = row_of(p, at);
         col[i] = static_cast<int>(at - row[i] * p.pieces) * 8;
         c[i] = make_uint2(0, 0);
         e[i] = 0;
@@ -132,7 +135,7 @@ static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArg
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
         const uint32_t at = first + i * kRowThreads;
-        row[i] = at / p.pieces;
+        row[i] = row_of(p, at);
         piece[i] = at - row[i] * p.pieces;
         c[i] = make_uint2(0, 0);
         if (at < total) {
@@ -173,13 +176,13 @@ static __global__ void __launch_bounds__(kRowThreads) align_kernel(const RowArgs
     uint4 v[kRowPieces];
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
-        const uint32_t at = first + i * kRowThreads, row = at / p.pieces;
+        const uint32_t at = first + i * kRowThreads, row = row_of(p, at);
         const int col = static_cast<int>(at - row * p.pieces) * 8;
         if (at < total) v[i] = load8(p.in + row * p.in_stride + col, p.features - col, false);
     }
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
-        const uint32_t at = first + i * kRowThreads, row = at / p.pieces;
+        const uint32_t at = first + i * kRowThreads, row = row_of(p, at);
         if (at < total) *reinterpret_cast<uint4 *>(p.out + row * p.out_stride + (at - row * p.pieces) * 8) = v[i];
     }
 }
