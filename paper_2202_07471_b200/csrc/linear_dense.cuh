@@ -16,7 +16,8 @@ struct DenseShape {
     static constexpr int kBytesB = kCols / 2 * 128;      // and half of the columns
     static constexpr int kStages = kCols == 256 ? 6 : 8;
     static constexpr int kTmemCols = 2 * kCols;
-    static constexpr int kSmem = 1024 + kStages * (kBytesA + kBytesB) + 8 * (2 * kStages + 4);
+    static constexpr int kSmem = 1024 + kStages * (kBytesA + kBytesB) + kDenseEpilogueWarps * kTurnBytes + 8 * (2 * kStages + 4);
+    static_assert(kSmem + 1024 + 128 <= 228 << 10, "fits a multiprocessor");
 };
 
 __device__ __forceinline__ void remote_arrive(uint32_t cluster_bar)
@@ -71,7 +72,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t smem_a = base, smem_b = base + S::kStages * S::kBytesA;
-    const uint32_t bars = smem_b + S::kStages * S::kBytesB;
+    const uint32_t turns = smem_b + S::kStages * S::kBytesB, bars = turns + kDenseEpilogueWarps * kTurnBytes;
     auto full = [&](int s) { return bars + 8 * s; };
     auto empty = [&](int s) { return bars + 8 * (S::kStages + s); };
     auto acc_full = [&](int a) { return bars + 8 * (2 * S::kStages + a); };
@@ -112,14 +113,14 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const int a = n & 1;
             if (!bar_wait_warp(acc_full(a), (n >> 1) & 1, gave_up)) break;
             tc_fence_after();
-            const int64_t row = (t % p.row_tiles) * kPairRows + rank * 128 + quarter * 32 + lane;
+            const int64_t row = (t % p.row_tiles) * kPairRows + rank * 128 + quarter * 32;
             const int64_t col0 = t / p.row_tiles * kCols;
             for (int c = part * (kCols / 2); c < (part + 1) * (kCols / 2); c += 32) {
                 if (col0 + c >= p.cols) break;
                 uint32_t acc[32];
                 __syncwarp();
                 tmem_ld32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + a * kCols + c, acc);
-                if (row < p.rows) finish32<kMode, kHalf>(p, row, static_cast<int>(col0) + c, acc);
+                finish32<kMode, kHalf>(p, row, static_cast<int>(col0) + c, acc, turns + warp * kTurnBytes);
             }
             tc_fence_before();
             __syncwarp();

@@ -43,27 +43,48 @@ struct GemmArgs {
 
 constexpr int kTileDepth = 64;        // of the contraction per stage: 128 bytes
 
-// Up to eight 16-bit values of one row from fp32, as one 16-byte store where it is possible.
-template <bool kHalf>
-__device__ __forceinline__ void store8(uint16_t *out, const float *v, int n, bool vector)
+// Places where a warp turns 32 rows by 32 columns of 16-bit values round, for rows that a thread cannot read or write in vectors: a
+// thread's row lies in 17 words, so that rows and columns hit all banks.
+constexpr int kTurnWords = 17, kTurnBytes = 4 * 32 * kTurnWords;
+
+// `out`: the warp's first row and column of the matrix; rows, n: of them inside it.
+__device__ __forceinline__ void turn_store(uint32_t turn, const uint32_t (&packed)[16], uint16_t *out, int64_t stride, int rows, int n)
 {
-    if (vector && n >= 8) {
-        *reinterpret_cast<uint4 *>(out) = make_uint4(to_16x2<kHalf>(v[0], v[1]), to_16x2<kHalf>(v[2], v[3]),
-                                                     to_16x2<kHalf>(v[4], v[5]), to_16x2<kHalf>(v[6], v[7]));
-    } else {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) out[i] = to_16<kHalf>(v[i]);
+    for (int i = 0; i < 16; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(turn + 4 * (lane * kTurnWords + i)), "r"(packed[i]) : "memory");
+    __syncwarp();
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r) {
+        uint16_t v;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(turn + 4 * r * kTurnWords + 2 * lane) : "memory");
+        if (lane < n) out[r * stride + lane] = v;
     }
 }
-
-// 32 columns of one row of the result.  A thread of the epilogue owns a row, so the 32 channels that share a
-// checkpoint's exponent are all its own.
-template <int kMode, bool kHalf>
-__device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col, const uint32_t (&acc)[32])
+__device__ __forceinline__ void turn_load(uint32_t turn, uint32_t (&packed)[16], const uint16_t *in, int64_t stride, int rows, int n)
 {
-    const int n = min(32, p.cols - col);
-    uint16_t *out = p.out + row * p.out_stride + col;
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r) {
+        const uint16_t v = lane < n ? in[r * stride + lane] : static_cast<uint16_t>(0);
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(turn + 4 * r * kTurnWords + 2 * lane), "h"(v) : "memory");
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(packed[i]) : "r"(turn + 4 * (lane * kTurnWords + i)) : "memory");
+}
+
+// 32 columns of 32 rows of the result from `row0` on; a lane owns a row, so the 32 channels that share a checkpoint's exponent are
+// all its own.  All lanes of a warp call it; `turn` is the warp's place in shared memory.
+template <int kMode, bool kHalf>
+__device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row0, int col, const uint32_t (&acc)[32], uint32_t turn)
+{
+    const int n = min(32, p.cols - col), rows = static_cast<int>(min(static_cast<int64_t>(32), p.rows - row0));   // rows may be negative
+    if (rows <= 0) return;
+    const int64_t row = row0 + (threadIdx.x & 31);
+    const bool valid = static_cast<int>(threadIdx.x & 31) < rows;
     float v[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(acc[i]);
@@ -80,54 +101,57 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row, int col
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const int c = i < n ? col + i : col;
-                v[i] = fmaf(v[i], get(p.scales + c), p.bias ? get(p.bias + c) : 0.0f);
-            }
+            for (int i = 0; i < 32; ++i)
+                v[i] = i < n ? fmaf(v[i], get(p.scales + col + i), p.bias ? get(p.bias + col + i) : 0.0f) : 0.0f;
         }
         if (p.z_codes) {
             float a = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < n) a = max_nan(a, fabsf(v[i]));
+            for (int i = 0; i < 32; ++i) a = max_nan(a, fabsf(v[i]));
             const uint32_t e = ckpt_exponent(a);
             const float inverse = ckpt_inverse(e);
             uint32_t w[8];
-            if (n < 32)
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i >= n) v[i] = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = ckpt_codes(v + 4 * i, inverse);
-            uint4 *zc = reinterpret_cast<uint4 *>(p.z_codes + row * p.z_pitch + col);
-            zc[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            zc[1] = make_uint4(w[4], w[5], w[6], w[7]);
-            p.z_exps[row * p.z_exps_pitch + (col >> 5)] = static_cast<uint8_t>(e);
+            if (valid) {
+                uint4 *zc = reinterpret_cast<uint4 *>(p.z_codes + row * p.z_pitch + col);
+                zc[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                zc[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                p.z_exps[row * p.z_exps_pitch + (col >> 5)] = static_cast<uint8_t>(e);
+            }
         }
         act_values(v, p.act);
         if (p.residual) {
-            const uint16_t *r = p.residual + row * p.residual_stride + col;
+            uint32_t w[16];
             if (p.residual_vector && n == 32) {
+                const uint16_t *r = p.residual + (valid ? row : row0) * p.residual_stride + col;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint4 q = get(reinterpret_cast<const uint4 *>(r) + j);
-                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[8 * j + 2 * i] += to_float<kHalf>(static_cast<uint16_t>(w[i]));
-                        v[8 * j + 2 * i + 1] += to_float<kHalf>(static_cast<uint16_t>(w[i] >> 16));
-                    }
+                    w[4 * j] = q.x; w[4 * j + 1] = q.y; w[4 * j + 2] = q.z; w[4 * j + 3] = q.w;
                 }
             } else {
+                turn_load(turn, w, p.residual + row0 * p.residual_stride + col, p.residual_stride, rows, n);
+            }
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i < n) v[i] += to_float<kHalf>(get(r + i));
+            for (int i = 0; i < 16; ++i) {
+                v[2 * i] += to_float<kHalf>(static_cast<uint16_t>(w[i]));
+                v[2 * i + 1] += to_float<kHalf>(static_cast<uint16_t>(w[i] >> 16));
             }
         }
     }
+    uint32_t packed[16];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (8 * j < n) store8<kHalf>(out + 8 * j, v + 8 * j, n - 8 * j, p.out_vector);
+    for (int i = 0; i < 16; ++i) packed[i] = to_16x2<kHalf>(v[2 * i], v[2 * i + 1]);
+    if (p.out_vector && n == 32) {
+        if (valid) {
+            uint4 *out = reinterpret_cast<uint4 *>(p.out + row * p.out_stride + col);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) out[j] = make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
+        }
+    } else {
+        turn_store(turn, packed, p.out + row0 * p.out_stride + col, p.out_stride, rows, n);
+    }
 }
 
 // The same for four columns a thread: eight neighbouring lanes hold the 32 channels of an exponent, all lanes of a warp call it.

@@ -7,7 +7,7 @@
 namespace sq {
 
 constexpr int kRowThreads = 256;
-constexpr int kRowPieces = 4;    // pieces of eight elements a thread: four loads in flight
+constexpr int kRowPieces = 2;    // pieces of eight elements a thread (four and eight are no faster for large tensors and slower for small ones)
 
 // Eight 16-bit values of a row from `first` on, of which n are inside the row.
 __device__ __forceinline__ uint4 load8(const uint16_t *at, int n, bool vector)
