@@ -40,22 +40,22 @@ int device_sms(int &device, int &sms)
     return SQUANT_OK;
 }
 
-// Clusters of `cluster` thread blocks; the kernel may be set up while the launch before it ends (wait_for_previous()).
+// Clusters of `cluster` thread blocks.  Not with programmatic stream serialization: with it (every kernel letting the next one start
+// at once and waiting for the one before) a call was 0.2 to 1 us a launch shorter, but some hundred backward calls in a row without a
+// synchronization stopped for good.
 template <typename... Params, typename... Args>
 int launch(void (*kernel)(Params...), dim3 grid, dim3 cluster, int threads, int smem, cudaStream_t stream, const Args &...args)
 {
     cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim = {cluster.x, cluster.y, 1};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {cluster.x, cluster.y, 1};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster.x * cluster.y > 1 ? 2 : 1;
+    cfg.numAttrs = 1;
     SQ_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
     sq_host::count_launch();
     return SQUANT_OK;

@@ -101,8 +101,6 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     cluster_arrive_wait();   // the other block's barriers are there
     tc_fence_after();
     const uint32_t tmem = tmem_base;
-    next_may_start();   // not before: a block of the next launch must not take the tensor memory that this one is yet to allocate
-    wait_for_previous();
     const int steps = (p.depth + kTileDepth - 1) / kTileDepth;
     const int64_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 

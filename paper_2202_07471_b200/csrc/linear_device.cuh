@@ -231,18 +231,9 @@ __device__ __forceinline__ void int8_to_16(uint32_t w, uint32_t out[2])
     }
 }
 
-// ---------------------------------------------------------------- order of launches
-//
-// Every kernel says at its start that the next launch may come, and waits before its first access to global memory until
-// the launch before it has ended: launched with programmatic stream serialization, a kernel is set up while the one
-// before it ends.  The waits make a chain, so that what follows the last launch follows all of them.
-__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;"); }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // ---------------------------------------------------------------- loads
-//
-// No read-only (.nc) loads: they may be moved up, past the wait for the launch before.
 
+// Not read-only (.nc): the residual may be the output.
 template <typename T>
 __device__ __forceinline__ T get(const T *p) { return *p; }
 

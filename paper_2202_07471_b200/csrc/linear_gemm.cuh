@@ -349,8 +349,6 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
-    next_may_start();   // not before: a block of the next launch must not take the tensor memory that this one is yet to allocate
-    wait_for_previous();
 
     if (warp < kConverterWarps) {
         Turn stage(stages, warp / kGroupWarps), raw(raws, warp / kGroupWarps);

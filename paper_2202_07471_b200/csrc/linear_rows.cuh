@@ -56,8 +56,6 @@ __device__ __forceinline__ uint32_t row_of(const RowArgs &p, uint32_t at) { retu
 // Four lanes share a group of 32 features.
 static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const RowArgs p)
 {
-    next_may_start();
-    wait_for_previous();
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint4 v[kRowPieces];
     uint32_t row[kRowPieces];
@@ -90,8 +88,6 @@ static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const Ro
 
 static __global__ void __launch_bounds__(kRowThreads) restore_kernel(const RowArgs p)
 {
-    next_may_start();
-    wait_for_previous();
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint2 c[kRowPieces];
     uint32_t e[kRowPieces], row[kRowPieces];
@@ -127,8 +123,6 @@ template <int kKind, bool kHalf>
 static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArgs p)
 {
     constexpr int kBytes = kKind == kInt4 ? 4 : 8;   // of a piece
-    next_may_start();
-    wait_for_previous();
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint2 c[kRowPieces];
     uint32_t row[kRowPieces], piece[kRowPieces];
@@ -170,8 +164,6 @@ static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArg
 // Rows that start anywhere to rows that start on 16 bytes, which TMA can read (the elements behind a row's end become 0).
 static __global__ void __launch_bounds__(kRowThreads) align_kernel(const RowArgs p)
 {
-    next_may_start();
-    wait_for_previous();
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint4 v[kRowPieces];
 #pragma unroll
@@ -235,8 +227,6 @@ constexpr int kNoZ = -1;
 template <int kAct, bool kVector>
 __global__ void __launch_bounds__(kRowThreads, 4) slope_kernel(const __grid_constant__ SlopeArgs p)
 {
-    next_may_start();
-    wait_for_previous();
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, warp = threadIdx.x >> 5;
     const int col = blockIdx.x * kSlopeCols + tx * 4;
     const int n = kVector ? (col < p.cout ? 4 : 0) : p.cout - col;   // columns of this thread inside the row, possibly none
@@ -327,8 +317,6 @@ __global__ void __launch_bounds__(kRowThreads, 4) slope_kernel(const __grid_cons
 
 static __global__ void __launch_bounds__(kRowThreads) sums_kernel(const __grid_constant__ SlopeArgs p)
 {
-    next_may_start();
-    wait_for_previous();
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
     if (i >= 2 * static_cast<int64_t>(p.cout)) return;
     const bool scales = i >= p.cout;

@@ -72,8 +72,6 @@ __global__ void __launch_bounds__(32 * kFewWarps, 2) few_kernel(const __grid_con
     const int row0 = static_cast<int>(blockIdx.x) * kFewRows;
     const int chunks = (p.cin + 4 * kCodes - 1) / (4 * kCodes);
     const int row_bytes = kKind == kInt4 ? (p.cin + 1) >> 1 : p.cin;
-    next_may_start();
-    wait_for_previous();
     // the thread that finishes (token, row)
     const int token = threadIdx.x / kFewRows, row = row0 + static_cast<int>(threadIdx.x) % kFewRows;
     const bool mine = token < p.tokens && row < p.cout;
