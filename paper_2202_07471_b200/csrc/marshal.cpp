@@ -117,8 +117,26 @@ using RestoreFn = int (*)(const squant_checkpoint_data *, int64_t, int32_t, void
 
 constexpr int64_t kMostRows = std::numeric_limits<int32_t>::max();
 
-template <typename Fn>
-Fn function(unsigned long long address) { return reinterpret_cast<Fn>(static_cast<uintptr_t>(address)); }
+// The library's functions, as use() was told them.
+struct Library {
+    LinearFn linear;
+    LinearNeedFn linear_need;
+    GradFn grad;
+    GradNeedFn grad_need;
+    CheckpointFn checkpoint;
+    RestoreFn restore;
+} s_lib;
+
+PyObject *use(PyObject *, PyObject *args)
+{
+    unsigned long long a[6];
+    if (!PyArg_ParseTuple(args, "KKKKKK", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5])) return nullptr;
+    const auto at = [&](int i) { return static_cast<uintptr_t>(a[i]); };
+    s_lib = {reinterpret_cast<LinearFn>(at(0)), reinterpret_cast<LinearNeedFn>(at(1)), reinterpret_cast<GradFn>(at(2)),
+             reinterpret_cast<GradNeedFn>(at(3)), reinterpret_cast<CheckpointFn>(at(4)), reinterpret_cast<RestoreFn>(at(5))};
+    Py_RETURN_NONE;
+}
+
 void *stream_of(unsigned long long handle) { return reinterpret_cast<void *>(static_cast<uintptr_t>(handle)); }
 
 // The tensor itself; null for None; false where it is anything but a plain tensor.
@@ -193,16 +211,16 @@ at::Tensor new_tensor(at::IntArrayRef shape, at::ScalarType type, const at::Devi
 
 PyObject *linear(PyObject *, PyObject *args)
 {
-    unsigned long long fn, need, stream;
+    unsigned long long stream;
     PyObject *po[6];   // x, codes, scales, bias, residual, out
     int device, act, packed, save;
-    if (!PyArg_ParseTuple(args, "KKKiOOOOOOipp", &fn, &need, &stream, &device, &po[0], &po[1], &po[2], &po[3], &po[4], &po[5], &act, &packed, &save))
+    if (!PyArg_ParseTuple(args, "KiOOOOOOipp", &stream, &device, &po[0], &po[1], &po[2], &po[3], &po[4], &po[5], &act, &packed, &save))
         return nullptr;
     return guarded([&]() -> PyObject * {
         const at::Tensor *t[6];
         for (int i = 0; i < 6; ++i)
             if (!plain(po[i], t[i])) return none();
-        if (!t[0] || !t[1] || !t[2]) return none();
+        if (!t[0] || !t[1] || !t[2] || act < 0) return none();
         const at::Tensor &x = *t[0];
         const at::Device d = x.device();
         const auto type = x.scalar_type();
@@ -238,14 +256,14 @@ PyObject *linear(PyObject *, PyObject *args)
             exps = new_tensor({a.tokens, groups}, at::kByte, d);
             a.z = {static_cast<int8_t *>(codes.data_ptr()), static_cast<uint8_t *>(exps.data_ptr())};
         }
-        const int64_t bytes = function<LinearNeedFn>(need)(&a);
+        const int64_t bytes = s_lib.linear_need(&a);
         if (bytes < 0) return none();
         if (bytes > 0) {
             workspace = new_tensor({bytes}, at::kByte, d);
             a.workspace = workspace.data_ptr();
             a.workspace_bytes = bytes;
         }
-        const int rc = function<LinearFn>(fn)(&a, stream_of(stream));
+        const int rc = s_lib.linear(&a, stream_of(stream));
         if (rc != SQUANT_OK) return PyLong_FromLong(rc);
         if (!save) {
             if (!t[5]) return THPVariable_Wrap(y);
@@ -261,18 +279,18 @@ PyObject *linear(PyObject *, PyObject *args)
 
 PyObject *linear_backward(PyObject *, PyObject *args)
 {
-    unsigned long long fn, need, stream;
+    unsigned long long stream;
     PyObject *po[8];   // dy, codes, scales, bias, z codes, z exps, x codes, x exps
     int device, act, packed, want_dx, want_dw, want_db, want_ds;
     long long cin;
-    if (!PyArg_ParseTuple(args, "KKKiOOOOOOOOLippppp", &fn, &need, &stream, &device, &po[0], &po[1], &po[2], &po[3], &po[4], &po[5], &po[6], &po[7],
+    if (!PyArg_ParseTuple(args, "KiOOOOOOOOLippppp", &stream, &device, &po[0], &po[1], &po[2], &po[3], &po[4], &po[5], &po[6], &po[7],
                           &cin, &act, &packed, &want_dx, &want_dw, &want_db, &want_ds))
         return nullptr;
     return guarded([&]() -> PyObject * {
         const at::Tensor *t[8];
         for (int i = 0; i < 8; ++i)
             if (!plain(po[i], t[i])) return none();
-        if (!t[0] || !t[1] || !t[2]) return none();
+        if (!t[0] || !t[1] || !t[2] || act < 0) return none();
         const at::Tensor &dy = *t[0];
         const at::Device d = dy.device();
         if (!d.is_cuda() || d.index() != device || dy.scalar_type() != at::kBFloat16 || cin < 1 || cin > kMostRows) return none();
@@ -305,14 +323,14 @@ PyObject *linear_backward(PyObject *, PyObject *args)
         a.dx_stride = a.dweight_stride = cin;
         a.dbias = want_db ? static_cast<float *>(db.data_ptr()) : nullptr;
         a.dscales = want_ds ? static_cast<float *>(ds.data_ptr()) : nullptr;
-        const int64_t bytes = function<GradNeedFn>(need)(&a);
+        const int64_t bytes = s_lib.grad_need(&a);
         if (bytes < 0) return none();
         if (bytes > 0) {
             workspace = new_tensor({bytes}, at::kByte, d);
             a.workspace = workspace.data_ptr();
             a.workspace_bytes = bytes;
         }
-        const int rc = function<GradFn>(fn)(&a, stream_of(stream));
+        const int rc = s_lib.grad(&a, stream_of(stream));
         if (rc != SQUANT_OK) return PyLong_FromLong(rc);
         return Py_BuildValue("(NNNN)", tensor_or_none(dx), tensor_or_none(dw), tensor_or_none(db), tensor_or_none(ds));
     });
@@ -320,10 +338,10 @@ PyObject *linear_backward(PyObject *, PyObject *args)
 
 PyObject *checkpoint(PyObject *, PyObject *args)
 {
-    unsigned long long fn, stream;
+    unsigned long long stream;
     PyObject *px;
     int device;
-    if (!PyArg_ParseTuple(args, "KKiO", &fn, &stream, &device, &px)) return nullptr;
+    if (!PyArg_ParseTuple(args, "KiO", &stream, &device, &px)) return nullptr;
     return guarded([&]() -> PyObject * {
         const at::Tensor *x;
         int64_t rows, features, stride;
@@ -332,7 +350,7 @@ PyObject *checkpoint(PyObject *, PyObject *args)
         const int64_t groups = (features + 31) / 32;
         at::Tensor codes = new_tensor({rows, 32 * groups}, at::kChar, x->device()), exps = new_tensor({rows, groups}, at::kByte, x->device());
         const squant_checkpoint_data to{static_cast<int8_t *>(codes.data_ptr()), static_cast<uint8_t *>(exps.data_ptr())};
-        const int rc = function<CheckpointFn>(fn)(x->data_ptr(), rows, static_cast<int32_t>(features), stride, &to, stream_of(stream));
+        const int rc = s_lib.checkpoint(x->data_ptr(), rows, static_cast<int32_t>(features), stride, &to, stream_of(stream));
         if (rc != SQUANT_OK) return PyLong_FromLong(rc);
         return Py_BuildValue("(NNL)", THPVariable_Wrap(codes), THPVariable_Wrap(exps), static_cast<long long>(features));
     });
@@ -340,11 +358,11 @@ PyObject *checkpoint(PyObject *, PyObject *args)
 
 PyObject *restore(PyObject *, PyObject *args)
 {
-    unsigned long long fn, stream;
+    unsigned long long stream;
     PyObject *pc, *pe;
     int device;
     long long features;
-    if (!PyArg_ParseTuple(args, "KKiOOL", &fn, &stream, &device, &pc, &pe, &features)) return nullptr;
+    if (!PyArg_ParseTuple(args, "KiOOL", &stream, &device, &pc, &pe, &features)) return nullptr;
     return guarded([&]() -> PyObject * {
         const at::Tensor *codes, *exps;
         if (!plain(pc, codes) || !plain(pe, exps) || !codes || !exps || !codes->is_cuda() || codes->device().index() != device || codes->dim() != 2 ||
@@ -352,12 +370,13 @@ PyObject *restore(PyObject *, PyObject *args)
         const int64_t rows = codes->size(0);
         at::Tensor out = new_tensor({rows, features}, at::kBFloat16, codes->device());
         const squant_checkpoint_data from{static_cast<int8_t *>(codes->data_ptr()), static_cast<uint8_t *>(exps->data_ptr())};
-        const int rc = function<RestoreFn>(fn)(&from, rows, static_cast<int32_t>(features), out.data_ptr(), features, stream_of(stream));
+        const int rc = s_lib.restore(&from, rows, static_cast<int32_t>(features), out.data_ptr(), features, stream_of(stream));
         return rc != SQUANT_OK ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
     });
 }
 
-PyMethodDef methods[] = {{"linear", linear, METH_VARARGS, "one call of squant_linear: the output (with its checkpoint's codes and exponents), an error code, or None"},
+PyMethodDef methods[] = {{"use", use, METH_VARARGS, "addresses of the library's functions"},
+                         {"linear", linear, METH_VARARGS, "one call of squant_linear: the output (with its checkpoint's codes and exponents), an error code, or None"},
                          {"linear_backward", linear_backward, METH_VARARGS, "one call of squant_linear_backward: four gradients, an error code, or None"},
                          {"checkpoint", checkpoint, METH_VARARGS, "one call of squant_checkpoint: codes, exponents and features, an error code, or None"},
                          {"restore", restore, METH_VARARGS, "one call of squant_checkpoint_restore: the values, an error code, or None"},

@@ -63,6 +63,7 @@ class LinearGrads:
     dscales: Optional[torch.Tensor] = None   # fp32 [cout]
 
 
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device   # the latter also initializes CUDA
 _ready = None
 _address = {}   # of the library's functions, for the native extension
 
@@ -89,14 +90,24 @@ def _lib() -> ctypes.CDLL:
     return lib
 
 
+_checked = (None, None, None)   # extension, library, and the extension if it was built with the library's argument structs
+
+
 def _native():
     """The extension that makes whole calls for plain tensors (None: not built, or built with other argument structs)."""
-    m = binding._marshal
-    if (getattr(m, "linear_bytes", None) != ctypes.sizeof(LinearArgs) or getattr(m, "linear_grad_bytes", None) != ctypes.sizeof(LinearGradArgs)
-            or binding._raw_stream is None or not torch.cuda.is_initialized()):
+    global _checked
+    if _checked[0] is binding._marshal and _checked[1] is binding._lib and _checked[1] is not None:
+        return _checked[2]
+    if not torch.cuda.is_initialized():
         return None
-    _lib()
-    return m
+    m, lib = binding._marshal, _lib()
+    fits = (getattr(m, "linear_bytes", None) == ctypes.sizeof(LinearArgs) and getattr(m, "linear_grad_bytes", None) == ctypes.sizeof(LinearGradArgs)
+            and binding._raw_stream is not None)
+    if fits:
+        m.use(_address["squant_linear"], _address["squant_linear_workspace"], _address["squant_linear_backward"],
+              _address["squant_linear_backward_workspace"], _address["squant_checkpoint"], _address["squant_checkpoint_restore"])
+    _checked = (m, lib, m if fits else None)
+    return _checked[2]
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -204,8 +215,8 @@ def squant_checkpoint(x: torch.Tensor, stream: Optional[torch.cuda.Stream] = Non
     neighbours off (2^-7 of its power of two)."""
     native = None if stream is not None else _native()
     if native is not None:
-        device = torch.cuda.current_device()
-        got = native.checkpoint(_address["squant_checkpoint"], binding._raw_stream(device), device, x)
+        device = _device()
+        got = native.checkpoint(binding._raw_stream(device), device, x)
         if got is not None:
             return Checkpoint(*_result(got))
     with _On(x.device, stream) as handle:
@@ -221,8 +232,8 @@ def squant_checkpoint_restore(c: Checkpoint, stream: Optional[torch.cuda.Stream]
     """The values of a checkpoint as a bfloat16 tensor [rows, features], exactly."""
     native = None if stream is not None else _native()
     if native is not None:
-        device = torch.cuda.current_device()
-        got = native.restore(_address["squant_checkpoint_restore"], binding._raw_stream(device), device, c.codes, c.exps, c.features)
+        device = _device()
+        got = native.restore(binding._raw_stream(device), device, c.codes, c.exps, c.features)
         if got is not None:
             return _result(got)
     device = c.codes.device
@@ -244,9 +255,8 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
     be `residual` itself, and must not overlap the other inputs otherwise."""
     native = None if stream is not None else _native()
     if native is not None:
-        device = torch.cuda.current_device()
-        got = native.linear(_address["squant_linear"], _address["squant_linear_workspace"], binding._raw_stream(device), device, x, codes, scales,
-                            bias, residual, out, _act(act), pack_int4, checkpoint)
+        device = _device()
+        got = native.linear(binding._raw_stream(device), device, x, codes, scales, bias, residual, out, ACTIVATIONS.get(act, -1), pack_int4, checkpoint)
         if got is not None:
             got = _result(got)
             return (got[0], Checkpoint(got[1], got[2], codes.shape[0])) if checkpoint else got
@@ -287,12 +297,11 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
     codes * scales: a training loop applies it to the weights that it quantizes."""
     native = None if stream is not None else _native()
     if native is not None and (z is None or z.features == dy.shape[-1]) and not (cin is None and pack_int4):
-        device = torch.cuda.current_device()
+        device = _device()
         width = codes.shape[-1] if cin is None else cin
         if x is None or x.features == width:
-            got = native.linear_backward(_address["squant_linear_backward"], _address["squant_linear_backward_workspace"],
-                                         binding._raw_stream(device), device, dy, codes, scales, bias, z and z.codes, z and z.exps, x and x.codes,
-                                         x and x.exps, width, _act(act), pack_int4, dx, dweight, dbias, dscales)
+            got = native.linear_backward(binding._raw_stream(device), device, dy, codes, scales, bias, z and z.codes, z and z.exps, x and x.codes,
+                                         x and x.exps, width, ACTIVATIONS.get(act, -1), pack_int4, dx, dweight, dbias, dscales)
             if got is not None:
                 return LinearGrads(*_result(got))
     device = dy.device
