@@ -297,7 +297,8 @@ typedef struct squant_linear_args {
     int64_t workspace_bytes;
 } squant_linear_args;
 
-/* Bytes of workspace the call with these arguments needs (0 unless x has rows that start anywhere), or a negative error. */
+/* Bytes of workspace the call with these arguments needs, or a negative error: up to 256 tokens 0 unless rows of x or of the codes start
+ * off 16 bytes, beyond that the codes as 16-bit floats. */
 int64_t squant_linear_workspace(const squant_linear_args *args);
 int squant_linear(const squant_linear_args *args, void *cuda_stream);
 

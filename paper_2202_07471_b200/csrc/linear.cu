@@ -109,21 +109,20 @@ int code_matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t pitch
 // As many thread blocks share a tile's contraction as there are multiprocessors (each holds two blocks) and stages for.
 // x: [rows][depth] 16-bit.
 template <int kMode, int kKind, bool kHalf>
-int fused(const void *x, int64_t x_stride, sq::GemmArgs a, bool vector, int device, int sms, cudaStream_t stream)
+int fused(const void *x, int64_t x_stride, sq::GemmArgs a, int device, int sms, cudaStream_t stream)
 {
-    auto kernel = vector ? sq::fused_kernel<kMode, kKind, kHalf, true> : sq::fused_kernel<kMode, kKind, kHalf, false>;
-    static std::atomic<bool> ready[2][kMaxDevices];
-    if (device >= kMaxDevices || !ready[vector][device].load(std::memory_order_relaxed)) {
+    auto kernel = sq::fused_kernel<kMode, kKind, kHalf>;
+    static std::atomic<bool> ready[kMaxDevices];
+    if (device >= kMaxDevices || !ready[device].load(std::memory_order_relaxed)) {
         SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sq::kFusedSmem));
-        if (device < kMaxDevices) ready[vector][device].store(true, std::memory_order_relaxed);
+        if (device < kMaxDevices) ready[device].store(true, std::memory_order_relaxed);
     }
     a.box_rows = static_cast<int32_t>(std::min<int64_t>(sq::kFusedTokens, up(a.rows, 16)));
-    CUtensorMap map, code_map{};
+    CUtensorMap map, code_map;
     if (int rc = matrix_map(map, x, a.rows, a.depth, x_stride, kHalf, a.box_rows)) return rc;
     const int bytes = kKind == sq::kInt4 ? 32 : 64;   // of 64 codes
-    if (vector)
-        if (int rc = kMode == sq::kForward ? code_matrix_map(code_map, a.codes, a.code_rows, a.code_pitch, bytes, sq::kFusedCols)
-                                           : code_matrix_map(code_map, a.codes, a.code_rows, a.code_pitch, 2 * bytes, sq::kTileDepth)) return rc;
+    if (int rc = kMode == sq::kForward ? code_matrix_map(code_map, a.codes, a.code_rows, a.code_pitch, bytes, sq::kFusedCols)
+                                       : code_matrix_map(code_map, a.codes, a.code_rows, a.code_pitch, 2 * bytes, sq::kTileDepth)) return rc;
     a.row_tiles = (a.rows + sq::kFusedTokens - 1) / sq::kFusedTokens;
     a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + sq::kFusedCols - 1) / sq::kFusedCols);
     const int64_t steps = (static_cast<int64_t>(a.depth) + sq::kTileDepth - 1) / sq::kTileDepth;
@@ -164,18 +163,68 @@ int dense(const void *a, int64_t a_stride, const void *b, int64_t b_stride, cons
                     : launch_dense<kMode, kHalf, 128>(map_a, map_b, g, device, sms, stream);
 }
 
-enum class RowKernel { kCheckpoint, kRestore, kAlign, kExpandInt4Bf16, kExpandInt4Fp16, kExpandInt8Bf16, kExpandInt8Fp16 };
+enum class RowKernel { kCheckpoint, kRestore, kExpandInt4Bf16, kExpandInt4Fp16, kExpandInt8Bf16, kExpandInt8Fp16 };
+
+// With 2^(L-1) < by <= 2^L and magic = floor(2^(31+L) / by) + 1, at * magic / 2^(31+L) exceeds at / by by less than at / 2^(31+L) < 1 / by.
+void division(uint32_t by, uint32_t &magic, uint32_t &shift)
+{
+    uint32_t bits = 0;
+    while ((1ull << bits) < by) ++bits;
+    magic = bits ? static_cast<uint32_t>((1ull << (31 + bits)) / by + 1) : 0;
+    shift = bits ? bits - 1 : 0;
+}
+
+// Rows of `bytes` bytes to rows that start on 16 bytes.
+struct Copy {
+    const void *in = nullptr;   // null: nothing to copy
+    int64_t rows = 0, bytes = 0, pitch = 0;
+    void *out = nullptr;
+    int64_t out_pitch() const { return up(bytes, 16); }
+    int64_t out_bytes() const { return in ? rows * out_pitch() : 0; }
+};
+
+// Both in one launch where they are not very large, else in ranges of rows.
+int launch_copies(const Copy &a, const Copy &b, cudaStream_t stream)
+{
+    const auto job = [](const Copy &c, int64_t row, int64_t rows) {
+        sq::CopyJob j{};
+        if (!c.in || rows <= 0) return j;
+        j.in = static_cast<const uint8_t *>(c.in) + row * c.pitch;
+        j.end = static_cast<const uint8_t *>(c.in) + (c.rows - 1) * c.pitch + c.bytes;
+        j.out = static_cast<uint8_t *>(c.out) + row * c.out_pitch();
+        j.in_pitch = c.pitch;
+        j.out_pitch = c.out_pitch();
+        j.rows = static_cast<uint32_t>(rows);
+        j.pieces = static_cast<uint32_t>(c.out_pitch() / 16);
+        division(j.pieces, j.magic, j.shift);
+        return j;
+    };
+    const auto blocks = [](const sq::CopyJob &j) {
+        return static_cast<uint32_t>((static_cast<int64_t>(j.rows) * j.pieces + sq::kRowThreads * sq::kRowPieces - 1) / (sq::kRowThreads * sq::kRowPieces));
+    };
+    const int64_t limit = (1ll << 31) - 4096;
+    const auto pieces = [](const Copy &c) { return c.in ? c.rows * (c.out_pitch() / 16) : 0; };
+    if (pieces(a) <= limit && pieces(b) <= limit) {
+        const sq::CopyJob ja = job(a, 0, a.rows), jb = job(b, 0, b.rows);
+        const uint32_t ba = blocks(ja), bb = blocks(jb);
+        return ba + bb ? launch(sq::copy_kernel, dim3(ba + bb), dim3(1), sq::kRowThreads, 0, stream, ja, jb, ba) : SQUANT_OK;
+    }
+    for (const Copy *c : {&a, &b}) {
+        if (!c->in) continue;
+        const int64_t most = std::max<int64_t>(1, limit / (c->out_pitch() / 16));
+        for (int64_t r = 0; r < c->rows; r += most) {
+            const sq::CopyJob j = job(*c, r, std::min(most, c->rows - r));
+            if (int rc = launch(sq::copy_kernel, dim3(blocks(j)), dim3(1), sq::kRowThreads, 0, stream, j, sq::CopyJob{}, blocks(j))) return rc;
+        }
+    }
+    return SQUANT_OK;
+}
 
 // Launches over ranges of rows, so that indices within a launch fit 32 bits.
 int launch_rows(RowKernel which, sq::RowArgs a, int64_t rows, cudaStream_t stream)
 {
     const int64_t most = std::max<int64_t>(1, ((1ll << 31) - 4096) / a.pieces);
-    // with 2^(L-1) < pieces <= 2^L and magic = floor(2^(31+L) / pieces) + 1, at * magic / 2^(31+L) exceeds at / pieces by less than
-    // at / 2^(31+L) < 1 / pieces
-    uint32_t bits = 0;
-    while ((1ull << bits) < a.pieces) ++bits;
-    a.magic = bits ? static_cast<uint32_t>((1ull << (31 + bits)) / a.pieces + 1) : 0;
-    a.shift = bits ? bits - 1 : 0;
+    division(a.pieces, a.magic, a.shift);
     for (int64_t r = 0; r < rows; r += most) {
         sq::RowArgs b = a;
         b.rows = static_cast<uint32_t>(std::min(most, rows - r));
@@ -188,7 +237,6 @@ int launch_rows(RowKernel which, sq::RowArgs a, int64_t rows, cudaStream_t strea
         switch (which) {
             case RowKernel::kCheckpoint: kernel = sq::checkpoint_kernel; break;
             case RowKernel::kRestore: kernel = sq::restore_kernel; break;
-            case RowKernel::kAlign: kernel = sq::align_kernel; break;
             case RowKernel::kExpandInt4Bf16: kernel = sq::expand_kernel<sq::kInt4, false>; break;
             case RowKernel::kExpandInt4Fp16: kernel = sq::expand_kernel<sq::kInt4, true>; break;
             case RowKernel::kExpandInt8Bf16: kernel = sq::expand_kernel<sq::kInt8, false>; break;
@@ -239,21 +287,29 @@ bool bad_checkpoint(const squant_checkpoint_data &c) { return misaligned(c.codes
 
 // ---- forward
 
-// Parts of the workspace: a copy of x with rows that TMA can read, the codes as 16-bit floats.
-struct ForwardPlan {
-    bool copy = false, dense = false;
-    int64_t copy_bytes = 0, bytes = 0;
-};
-
 bool few(const squant_linear_args &a) { return a.tokens <= sq::kFewTokens && !a.z.codes; }
+
+// Bytes of a row of codes, and whether every row starts on 16 bytes.
+int64_t code_pitch(int32_t cin, uint32_t flags) { return flags & SQUANT_FLAG_PACK_INT4 ? (static_cast<int64_t>(cin) + 1) / 2 : cin; }
+bool codes_on_vectors(const int8_t *codes, int64_t pitch) { return !misaligned(codes, 16) && pitch % 16 == 0; }
+
+// Parts of the workspace: copies of x and of the codes with rows that TMA can read, or the codes as 16-bit floats.
+struct ForwardPlan {
+    bool dense = false;
+    Copy x, codes;
+    int64_t bytes = 0;
+};
 
 ForwardPlan forward_plan(const squant_linear_args &a)
 {
     ForwardPlan p;
-    p.copy = !few(a) && !rows_on_vectors(a.x, a.x_stride, a.tokens);
     p.dense = a.tokens > kFusedTokens;
-    if (p.copy) p.copy_bytes = a.tokens * up(a.cin, 8) * 2;
-    p.bytes = p.copy_bytes + (p.dense ? a.cout * up(a.cin, 8) * 2 : 0);
+    if (few(a)) return p;
+    uint8_t *at = static_cast<uint8_t *>(a.workspace);
+    if (!rows_on_vectors(a.x, a.x_stride, a.tokens)) p.x = {a.x, a.tokens, 2 * static_cast<int64_t>(a.cin), 2 * (a.tokens > 1 ? a.x_stride : a.cin), at};
+    const int64_t pitch = code_pitch(a.cin, a.flags);
+    if (!p.dense && !codes_on_vectors(a.codes, pitch)) p.codes = {a.codes, a.cout, pitch, pitch, at ? at + p.x.out_bytes() : nullptr};
+    p.bytes = p.x.out_bytes() + p.codes.out_bytes() + (p.dense ? a.cout * up(a.cin, 8) * 2 : 0);
     return p;
 }
 
@@ -276,8 +332,7 @@ int check(const squant_linear_args *args)
 template <int kKind, bool kHalf>
 int forward(const squant_linear_args &a, cudaStream_t stream)
 {
-    const int64_t pitch = kKind == sq::kInt4 ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
-    const bool code_vector = !misaligned(a.codes, 16) && pitch % 16 == 0;
+    const int64_t pitch = code_pitch(a.cin, a.flags);
     const int64_t z_pitch = up(a.cout, 32);
     if (few(a)) {
         sq::FewArgs s{};
@@ -296,27 +351,16 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
         s.y = static_cast<uint16_t *>(a.y);
         s.y_stride = a.y_stride;
         s.act = static_cast<int32_t>(a.act);
-        const bool vector = code_vector && rows_on_vectors(a.x, a.x_stride, a.tokens) && a.cin % 8 == 0;
+        const bool vector = codes_on_vectors(a.codes, pitch) && rows_on_vectors(a.x, a.x_stride, a.tokens) && a.cin % 8 == 0;
         const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kFewRows - 1) / sq::kFewRows);
         return launch(vector ? sq::few_kernel<kKind, kHalf, true> : sq::few_kernel<kKind, kHalf, false>, dim3(grid), dim3(1), 32 * sq::kFewWarps, 0, stream, s);
     }
     int device, sms;
     if (int rc = device_sms(device, sms)) return rc;
-    const void *x = a.x;
-    int64_t x_stride = a.x_stride;
     const ForwardPlan plan = forward_plan(a);
-    if (plan.copy) {
-        sq::RowArgs r{};
-        r.in = static_cast<const uint16_t *>(a.x);
-        r.in_stride = a.x_stride;
-        r.out = static_cast<uint16_t *>(a.workspace);
-        r.out_stride = up(a.cin, 8);
-        r.pieces = static_cast<uint32_t>(r.out_stride / 8);
-        r.features = a.cin;
-        if (int rc = launch_rows(RowKernel::kAlign, r, a.tokens, stream)) return rc;
-        x = a.workspace;
-        x_stride = r.out_stride;
-    }
+    if (int rc = launch_copies(plan.x, plan.codes, stream)) return rc;
+    const void *x = plan.x.in ? plan.x.out : a.x;
+    const int64_t x_stride = plan.x.in ? plan.x.out_pitch() / 2 : a.x_stride;
     sq::GemmArgs g{};
     g.rows = static_cast<int32_t>(a.tokens);
     g.cols = a.cout;
@@ -336,16 +380,14 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
     g.z_pitch = z_pitch;
     g.z_exps_pitch = z_pitch / 32;
     if (plan.dense) {
-        uint8_t *b = static_cast<uint8_t *>(a.workspace) + plan.copy_bytes;
+        uint8_t *b = static_cast<uint8_t *>(a.workspace) + plan.x.out_bytes();
         if (int rc = expand(a.codes, a.cout, a.cin, kKind == sq::kInt4, kHalf, b, stream)) return rc;
         return dense<sq::kForward, kHalf>(x, x_stride, b, up(a.cin, 8), g, device, sms, stream);
     }
-    g.codes = reinterpret_cast<const uint8_t *>(a.codes);
-    g.code_pitch = pitch;
-    g.code_bytes = pitch * a.cout;
+    g.codes = static_cast<const uint8_t *>(plan.codes.in ? plan.codes.out : a.codes);
+    g.code_pitch = plan.codes.in ? plan.codes.out_pitch() : pitch;
     g.code_rows = a.cout;
-    g.code_row_bytes = static_cast<int32_t>(pitch);
-    return fused<sq::kForward, kKind, kHalf>(x, x_stride, g, code_vector, device, sms, stream);
+    return fused<sq::kForward, kKind, kHalf>(x, x_stride, g, device, sms, stream);
 }
 
 // ---- backward
@@ -356,7 +398,8 @@ struct SlopePlan {
     int64_t pitch = 0, slope_bytes = 0;
     int64_t share = 0, shares = 1;   // tokens of a thread block of slope_kernel
     int64_t partial_bytes = 0;       // behind dzs and dz: sums of the shares
-    int64_t wide_bytes = 0;   // behind them: the codes, then the input as 16-bit floats
+    Copy codes;               // a copy of the codes with rows that TMA can read
+    int64_t wide_bytes = 0;   // behind them: that copy or the codes as 16-bit floats, then the input as 16-bit floats
     int64_t bytes = 0;
 };
 
@@ -374,7 +417,10 @@ SlopePlan slope_plan(const squant_linear_grad_args &a)
     s.slope_bytes = (s.dzs + s.dz) * a.tokens * s.pitch * 2 + s.partial_bytes;
     s.dense = s.dzs && a.tokens > kFusedTokens;
     const int64_t row = up(a.cin, 8) * 2;
-    s.wide_bytes = std::max(s.dense ? a.cout * row : 0, a.dweight ? a.tokens * row : 0);
+    const int64_t pitch = code_pitch(a.cin, a.flags);
+    if (s.dzs && !s.dense && !codes_on_vectors(a.codes, pitch))
+        s.codes = {a.codes, a.cout, pitch, pitch, a.workspace ? static_cast<uint8_t *>(a.workspace) + s.slope_bytes : nullptr};
+    s.wide_bytes = std::max({s.dense ? a.cout * row : 0, s.codes.out_bytes(), a.dweight ? a.tokens * row : 0});
     s.bytes = s.slope_bytes + s.wide_bytes;
     return s;
 }
@@ -536,14 +582,12 @@ int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_strea
             if (int rc = expand(a.codes, a.cout, a.cin, packed, false, wide, stream)) return rc;
             if (int rc = dense<sq::kInputGrad, false>(dzs, plan.pitch, wide, up(a.cin, 8), g, device, sms, stream)) return rc;
         } else {
-            g.codes = reinterpret_cast<const uint8_t *>(a.codes);
-            g.code_pitch = packed ? (static_cast<int64_t>(a.cin) + 1) / 2 : a.cin;
-            g.code_bytes = g.code_pitch * a.cout;
+            if (int rc = launch_copies(plan.codes, Copy{}, stream)) return rc;
+            g.codes = static_cast<const uint8_t *>(plan.codes.in ? plan.codes.out : a.codes);
+            g.code_pitch = plan.codes.in ? plan.codes.out_pitch() : code_pitch(a.cin, a.flags);
             g.code_rows = a.cout;
-            g.code_row_bytes = static_cast<int32_t>(g.code_pitch);
-            const bool vector = !misaligned(a.codes, 16) && g.code_pitch % 16 == 0;
-            if (int rc = packed ? fused<sq::kInputGrad, sq::kInt4, false>(dzs, plan.pitch, g, vector, device, sms, stream)
-                                : fused<sq::kInputGrad, sq::kInt8, false>(dzs, plan.pitch, g, vector, device, sms, stream)) return rc;
+            if (int rc = packed ? fused<sq::kInputGrad, sq::kInt4, false>(dzs, plan.pitch, g, device, sms, stream)
+                                : fused<sq::kInputGrad, sq::kInt8, false>(dzs, plan.pitch, g, device, sms, stream)) return rc;
         }
     }
     if (a.dweight) {

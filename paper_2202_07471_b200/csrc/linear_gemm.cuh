@@ -19,9 +19,7 @@ enum GemmMode { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
 struct GemmArgs {
     const uint8_t *codes;    // coded operand, rows of code_pitch bytes
     int64_t code_pitch;
-    int64_t code_bytes;      // of the whole operand
-    int32_t code_rows;       // rows of the coded operand
-    int32_t code_row_bytes;  // bytes of a row that may be read
+    int32_t code_rows;
     int32_t rows, cols;      // of the result
     int32_t depth;           // of the contraction
     int32_t row_tiles;
@@ -238,17 +236,6 @@ struct Pieces {
     }
 };
 
-// Rows that start anywhere: straight from global memory.
-template <int kMode, int kKind>
-__device__ __forceinline__ uint4 load_codes(const GemmArgs &p, int col0, int step, const Pieces<kMode, kKind> &at)
-{
-    const int row = (kMode == kForward ? col0 : step * kTileDepth) + at.row;
-    const int first = (kMode == kForward ? step * kTileDepth : col0 + 64 * at.panel) + at.sub * (64 / at.kPerRow);
-    const int off = kKind == kInt4 ? first >> 1 : first;
-    if (row >= p.code_rows || off >= p.code_row_bytes) return make_uint4(0, 0, 0, 0);
-    return load_bytes16(p.codes + static_cast<int64_t>(row) * p.code_pitch + off, p.codes, p.codes + p.code_bytes);
-}
-
 template <int kMode, int kKind>
 __device__ __forceinline__ uint4 read_codes(uint32_t raw, const Pieces<kMode, kKind> &at)
 {
@@ -298,10 +285,10 @@ struct Turn {
 // that a step of the contraction (64) does as much as it can: the issuing warp's chain of one wait, four matrix instructions and one
 // commit is among the longest (with the tokens as first operand and 64 columns a tile it took 0.33 us for half the codes).  TMA
 // brings the codes as they are ahead, two groups of converter warps turn the stages into 16-bit floats in turn.  Codes loaded by the converters
-// themselves, as rows that start anywhere are (kVector false), cost more: the fence between their stores and the tensor cores' reads
-// waits for a warp's loads in flight, too.  The ranks' sums meet in shared memory, added in the order of the ranks, and each rank
+// themselves cost more: the fence between their stores and the tensor cores' reads waits for a warp's loads in flight, too (so rows
+// that start anywhere are copied first).  The ranks' sums meet in shared memory, added in the order of the ranks, and each rank
 // finishes a share of the tokens.
-template <int kMode, int kKind, bool kHalf, bool kVector>
+template <int kMode, int kKind, bool kHalf>
 __global__ void __launch_bounds__(kFusedThreads, 2)
 fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const __grid_constant__ GemmArgs p)
 {
@@ -354,14 +341,9 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
         Turn stage(stages, warp / kGroupWarps), raw(raws, warp / kGroupWarps);
         for (int k = warp / kGroupWarps; k < steps; k += kConverterGroups) {
             uint4 codes[P::kCount];
-            if constexpr (kVector) {
-                if (!bar_wait_warp(raw_full(raw.bar), raw.parity, gave_up)) break;
+            if (!bar_wait_warp(raw_full(raw.bar), raw.parity, gave_up)) break;
 #pragma unroll
-                for (int i = 0; i < P::kCount; ++i) codes[i] = read_codes<kMode, kKind>(smem_c + raw.place() * P::kRawBytes, P(i));
-            } else {
-#pragma unroll
-                for (int i = 0; i < P::kCount; ++i) codes[i] = load_codes<kMode, kKind>(p, col0, first + k, P(i));
-            }
+            for (int i = 0; i < P::kCount; ++i) codes[i] = read_codes<kMode, kKind>(smem_c + raw.place() * P::kRawBytes, P(i));
             if (k >= stages && !bar_wait_warp(empty(stage.before()), stage.before_parity(), gave_up)) break;
 #pragma unroll
             for (int i = 0; i < P::kCount; ++i) store_codes<kMode, kKind, kHalf>(smem_a + stage.place() * kFusedBytesA, P(i), codes[i]);
@@ -369,10 +351,8 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
             __syncwarp();
             if (lane == 0) bar_arrive(full(stage.bar));
             stage.next(kConverterGroups);
-            if constexpr (kVector) {   // not before: the codes have been read for certain once their floats are stored
-                if (lane == 0) bar_arrive(raw_empty(raw.bar));
-                raw.next(kConverterGroups);
-            }
+            if (lane == 0) bar_arrive(raw_empty(raw.bar));   // not before: the codes have been read for certain once their floats are stored
+            raw.next(kConverterGroups);
         }
         if (bar_wait_warp(done, 0, gave_up)) {
             tc_fence_after();
@@ -402,23 +382,21 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
         // the last copies have landed before the block may end
         for (int i = max(0, k - stages); i < k; ++i) bar_drain(full(i % (2 * stages)), i / (2 * stages) & 1);
     } else if (warp == kConverterWarps + 2) {
-        if constexpr (kVector) {
-            constexpr int along = kKind == kInt4 ? kTileDepth / 2 : kTileDepth;   // bytes of 64 codes
-            Turn raw(raws, 0);
-            int k = 0;
-            for (; k < steps; ++k) {
-                if (k >= raws && !bar_wait_warp(raw_empty(raw.before()), raw.before_parity(), gave_up)) break;
-                if (elect_one()) {
-                    const uint32_t to = smem_c + raw.place() * P::kRawBytes;
-                    bar_expect(raw_full(raw.bar), P::kRawBytes);
-                    if (kMode == kForward) tma_2d(to, &code_map, (first + k) * along, col0, raw_full(raw.bar));
-                    else tma_2d(to, &code_map, col0 / 64 * along, (first + k) * kTileDepth, raw_full(raw.bar));
-                }
-                __syncwarp();
-                raw.next(1);
+        constexpr int along = kKind == kInt4 ? kTileDepth / 2 : kTileDepth;   // bytes of 64 codes
+        Turn raw(raws, 0);
+        int k = 0;
+        for (; k < steps; ++k) {
+            if (k >= raws && !bar_wait_warp(raw_empty(raw.before()), raw.before_parity(), gave_up)) break;
+            if (elect_one()) {
+                const uint32_t to = smem_c + raw.place() * P::kRawBytes;
+                bar_expect(raw_full(raw.bar), P::kRawBytes);
+                if (kMode == kForward) tma_2d(to, &code_map, (first + k) * along, col0, raw_full(raw.bar));
+                else tma_2d(to, &code_map, col0 / 64 * along, (first + k) * kTileDepth, raw_full(raw.bar));
             }
-            for (int i = max(0, k - raws); i < k; ++i) bar_drain(raw_full(i % (2 * raws)), i / (2 * raws) & 1);
+            __syncwarp();
+            raw.next(1);
         }
+        for (int i = max(0, k - raws); i < k; ++i) bar_drain(raw_full(i % (2 * raws)), i / (2 * raws) & 1);
     } else {
         const uint32_t idesc = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (kMode != kForward ? 1u << 15 : 0u) |
                                (static_cast<uint32_t>(p.box_rows >> 3) << 17) | (static_cast<uint32_t>(kFusedCols >> 4) << 24);

@@ -161,21 +161,26 @@ static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArg
     }
 }
 
-// Rows that start anywhere to rows that start on 16 bytes, which TMA can read (the elements behind a row's end become 0).
-static __global__ void __launch_bounds__(kRowThreads) align_kernel(const RowArgs p)
+// Rows of bytes that start anywhere to rows that start on 16 bytes, which TMA can read (what lies behind a row's last byte is not used).
+struct CopyJob {
+    const uint8_t *in, *end;   // end: of what may be read
+    uint8_t *out;
+    int64_t in_pitch, out_pitch;
+    uint32_t rows, pieces;     // of 16 bytes a row
+    uint32_t magic, shift;     // as in RowArgs
+};
+
+// Two jobs in one launch: the first `blocks` thread blocks take the first.
+static __global__ void __launch_bounds__(kRowThreads) copy_kernel(const __grid_constant__ CopyJob a, const __grid_constant__ CopyJob b, uint32_t blocks)
 {
-    const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
-    uint4 v[kRowPieces];
+    const bool second = blockIdx.x >= blocks;
+    const CopyJob &p = second ? b : a;
+    const uint32_t first = (blockIdx.x - (second ? blocks : 0)) * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
-        const uint32_t at = first + i * kRowThreads, row = row_of(p, at);
-        const int col = static_cast<int>(at - row * p.pieces) * 8;
-        if (at < total) v[i] = load8(p.in + row * p.in_stride + col, p.features - col, false);
-    }
-#pragma unroll
-    for (int i = 0; i < kRowPieces; ++i) {
-        const uint32_t at = first + i * kRowThreads, row = row_of(p, at);
-        if (at < total) *reinterpret_cast<uint4 *>(p.out + row * p.out_stride + (at - row * p.pieces) * 8) = v[i];
+        const uint32_t at = first + i * kRowThreads, row = p.magic ? __umulhi(at, p.magic) >> p.shift : at, piece = at - row * p.pieces;
+        if (at < total)
+            *reinterpret_cast<uint4 *>(p.out + row * p.out_pitch + piece * 16) = load_bytes16(p.in + row * p.in_pitch + piece * 16, p.in, p.end);
     }
 }
 

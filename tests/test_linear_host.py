@@ -92,13 +92,13 @@ def test_calls_without_tokens_need_nothing():
 
 
 def test_workspace_sizes():
-    """What the header documents: nothing for rows on 16 bytes up to 256 tokens; a copy of x, the codes as 16-bit floats, dz and dz * s,
-    the sums of shares of the tokens."""
+    """What the header documents: nothing for rows on 16 bytes up to 256 tokens; copies of x and of the codes, the codes as 16-bit floats,
+    dz and dz * s."""
     lib = linear._lib()
     need = lambda **kw: lib.squant_linear_workspace(ctypes.byref(forward(**kw)))
     assert need() == 0 and need(tokens=256) == 0 and need(tokens=8, x=OK_PTR + 2) == 0
     assert need(tokens=9, x=OK_PTR + 2) == 9 * 64 * 2                      # rows that start anywhere
-    assert need(tokens=9, cin=61, x_stride=61) == 9 * 64 * 2
+    assert need(tokens=9, cin=61, x_stride=61) == 9 * 64 * 2 + 32 * 64     # and the codes'
     assert need(tokens=257) == 32 * 64 * 2
     assert need(tokens=257, cin=61, x_stride=61) == 257 * 64 * 2 + 32 * 64 * 2
     need = lambda **kw: lib.squant_linear_backward_workspace(ctypes.byref(backward(**kw)))
@@ -107,6 +107,7 @@ def test_workspace_sizes():
     assert need(act=1, z=CK, dx=None, dweight=OK_PTR, dweight_stride=64, x=CK) == 4 * 32 * 2 + 4 * 64 * 2
     assert need(dx=None, dweight=OK_PTR, dweight_stride=64, x=CK) == 4 * 64 * 2   # dz is dy itself
     assert need(tokens=1000) == 1000 * 32 * 2 + 32 * 64 * 2
+    assert need(cin=61, dx_stride=61) == 4 * 32 * 2 + 32 * 64
 
 
 def test_tensors_have_to_be_on_a_gpu():
