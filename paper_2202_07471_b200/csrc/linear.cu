@@ -512,7 +512,7 @@ int squant_checkpoint(const void *x, int64_t rows, int32_t features, int64_t str
     r.exps = to->exps;
     r.code_pitch = up(features, 32);
     r.exps_pitch = r.code_pitch / 32;
-    r.pieces = static_cast<uint32_t>(r.code_pitch / 8);
+    r.pieces = static_cast<uint32_t>(r.code_pitch / 16);
     r.features = features;
     r.vector = rows_on_vectors(x, stride, rows);
     return launch_rows(RowKernel::kCheckpoint, r, rows, static_cast<cudaStream_t>(cuda_stream));

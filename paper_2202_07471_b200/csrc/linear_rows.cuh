@@ -46,42 +46,46 @@ struct RowArgs {
     uint16_t *out;
     uint8_t *codes, *exps;
     int64_t in_stride, out_stride, code_pitch, exps_pitch;
-    uint32_t rows, pieces;   // pieces of eight elements a row
+    uint32_t rows, pieces;   // pieces of eight elements (checkpoint_kernel: sixteen) a row
     uint32_t magic, shift;   // at / pieces = at * magic >> 32 >> shift for at < 2^31; magic 0: one piece a row
     int32_t features, vector;
 };
 
 __device__ __forceinline__ uint32_t row_of(const RowArgs &p, uint32_t at) { return p.magic ? __umulhi(at, p.magic) >> p.shift : at; }
 
-// Four lanes share a group of 32 features.
+// Pieces of sixteen elements; two lanes share a group of 32 features.
 static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const RowArgs p)
 {
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
-    uint4 v[kRowPieces];
+    uint4 v[kRowPieces][2];
     uint32_t row[kRowPieces];
     int col[kRowPieces];
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
         const uint32_t at = first + i * kRowThreads;
         row[i] = row_of(p, at);
-        col[i] = static_cast<int>(at - row[i] * p.pieces) * 8;
-        v[i] = make_uint4(0, 0, 0, 0);
-        if (at < total && col[i] < p.features) v[i] = load8(p.in + row[i] * p.in_stride + col[i], p.features - col[i], p.vector);
+        col[i] = static_cast<int>(at - row[i] * p.pieces) * 16;
+        const int n = at < total ? p.features - col[i] : 0;
+        const uint16_t *from = p.in + row[i] * p.in_stride + col[i];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[i][h] = n > 8 * h ? load8(from + 8 * h, n - 8 * h, p.vector) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
-        float f[8], a = 0.0f;
-        unpack8(v[i], f);
+        float f[2][8], a = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) a = max_nan(a, fabsf(f[j]));
+        for (int h = 0; h < 2; ++h) {
+            unpack8(v[i][h], f[h]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) a = max_nan(a, fabsf(f[h][j]));
+        }
         a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, 1));
-        a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, 2));
         const uint32_t e = ckpt_exponent(a);
         const float inverse = ckpt_inverse(e);
-        const uint32_t w[2] = {ckpt_codes(f, inverse), ckpt_codes(f + 4, inverse)};
+        const uint4 w = make_uint4(ckpt_codes(f[0], inverse), ckpt_codes(f[0] + 4, inverse), ckpt_codes(f[1], inverse), ckpt_codes(f[1] + 4, inverse));
         if (first + i * kRowThreads < total) {
-            *reinterpret_cast<uint2 *>(p.codes + row[i] * p.code_pitch + col[i]) = make_uint2(w[0], w[1]);
-            if ((threadIdx.x & 3) == 0) p.exps[row[i] * p.exps_pitch + (col[i] >> 5)] = static_cast<uint8_t>(e);
+            *reinterpret_cast<uint4 *>(p.codes + row[i] * p.code_pitch + col[i]) = w;
+            if ((threadIdx.x & 1) == 0) p.exps[row[i] * p.exps_pitch + (col[i] >> 5)] = static_cast<uint8_t>(e);
         }
     }
 }
