@@ -198,20 +198,31 @@ __device__ __forceinline__ uint32_t mul2_bf16(uint32_t a, uint32_t b)
 // Eight int4 codes (low nibble first) to four pairs of 16-bit floats, exactly.  A code's nibble n, its sign bit
 // flipped, becomes the low mantissa bits of 128 (bf16) or 1024 (fp16), which gives 128 + n + 8; the odd codes' nibbles
 // sit three bits further up (the word shifted by one), which gives 128 + 8 (n + 8).  One fused multiply-add on the
-// pair takes the offsets off and divides the odd code by 8: three instructions a pair and one shift a word.
+// pair takes the offsets off and divides the odd code by 8: three instructions a pair and one shift a word.  The constants come from
+// registers that the compiler cannot see through: known ones it writes into the instructions, which hold one each, and
+// takes five instructions a pair.
 template <bool kHalf>
-__device__ __forceinline__ void int4_to_16(uint32_t w, uint32_t out[4])
-{
-    constexpr uint32_t base = kHalf ? 0x64006400u : 0x43004300u;
-    constexpr uint32_t factor = kHalf ? 0x30003c00u : 0x3e003f80u;    // (1, 1/8), low half first
-    constexpr uint32_t offset = kHalf ? 0xd840e408u : 0xc1c0c308u;    // fp16 (-1032, -136), bf16 (-136, -24)
-    const uint32_t s = w >> 1;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t v = __byte_perm(w, s, 0x0400u | (0x0101u * j));   // byte 0: w's byte j, byte 2: s's byte j
-        out[j] = fma2<kHalf>((v & 0x0078000fu) ^ (base | 0x00400008u), factor, offset);
+struct Int4To16 {
+    uint32_t mask, flip, factor, offset;
+    __device__ __forceinline__ Int4To16()
+    {
+        asm volatile("mov.b32 %0, 0x0078000f;" : "=r"(mask));
+        asm volatile("mov.b32 %0, %1;" : "=r"(flip) : "n"(kHalf ? 0x64406408u : 0x43404308u));
+        asm volatile("mov.b32 %0, %1;" : "=r"(factor) : "n"(kHalf ? 0x30003c00u : 0x3e003f80u));   // (1, 1/8), low half first
+        asm volatile("mov.b32 %0, %1;" : "=r"(offset) : "n"(kHalf ? 0xd840e408u : 0xc1c0c308u));   // fp16 (-1032, -136), bf16 (-136, -24)
     }
-}
+    __device__ __forceinline__ void operator()(uint32_t w, uint32_t out[4]) const
+    {
+        const uint32_t s = w >> 1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t v = __byte_perm(w, s, 0x0400u | (0x0101u * j));   // byte 0: w's byte j, byte 2: s's byte j
+            uint32_t u;
+            asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(v), "r"(mask), "r"(flip));   // (v & mask) ^ flip
+            out[j] = fma2<kHalf>(u, factor, offset);
+        }
+    }
+};
 
 // Four int8 codes to two pairs of 16-bit floats, exactly.  bf16 has seven mantissa bits: the low seven bits L of a
 // byte give 128 + L, its sign bit S gives 128 + 128 S as exponent bit; the difference is L - 128 S.

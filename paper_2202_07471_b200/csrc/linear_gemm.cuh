@@ -246,14 +246,14 @@ __device__ __forceinline__ uint4 read_codes(uint32_t raw, const Pieces<kMode, kK
 }
 
 template <int kMode, int kKind, bool kHalf>
-__device__ __forceinline__ void store_codes(uint32_t stage, const Pieces<kMode, kKind> &at, const uint4 &c)
+__device__ __forceinline__ void store_codes(uint32_t stage, const Pieces<kMode, kKind> &at, const uint4 &c, const Int4To16<kHalf> &int4)
 {
     const uint32_t w[4] = {c.x, c.y, c.z, c.w}, to = stage + at.panel * 8192 + at.row * 128;
 #pragma unroll
     for (int j = 0; j < at.kChunks; ++j) {
         uint32_t o[4];
         if constexpr (kKind == kInt4) {
-            int4_to_16<kHalf>(w[j], o);
+            int4(w[j], o);
         } else {
             int8_to_16<kHalf>(w[2 * j], o);
             int8_to_16<kHalf>(w[2 * j + 1], o + 2);
@@ -338,6 +338,7 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     const uint32_t tmem = tmem_base;
 
     if (warp < kConverterWarps) {
+        const Int4To16<kHalf> int4;
         Turn stage(stages, warp / kGroupWarps), raw(raws, warp / kGroupWarps);
         for (int k = warp / kGroupWarps; k < steps; k += kConverterGroups) {
             uint4 codes[P::kCount];
@@ -346,7 +347,7 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
             for (int i = 0; i < P::kCount; ++i) codes[i] = read_codes<kMode, kKind>(smem_c + raw.place() * P::kRawBytes, P(i));
             if (k >= stages && !bar_wait_warp(empty(stage.before()), stage.before_parity(), gave_up)) break;
 #pragma unroll
-            for (int i = 0; i < P::kCount; ++i) store_codes<kMode, kKind, kHalf>(smem_a + stage.place() * kFusedBytesA, P(i), codes[i]);
+            for (int i = 0; i < P::kCount; ++i) store_codes<kMode, kKind, kHalf>(smem_a + stage.place() * kFusedBytesA, P(i), codes[i], int4);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) bar_arrive(full(stage.bar));

@@ -127,6 +127,7 @@ template <int kKind, bool kHalf>
 static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArgs p)
 {
     constexpr int kBytes = kKind == kInt4 ? 4 : 8;   // of a piece
+    [[maybe_unused]] const Int4To16<kHalf> int4;
     const uint32_t first = blockIdx.x * (kRowThreads * kRowPieces) + threadIdx.x, total = p.rows * p.pieces;
     uint2 c[kRowPieces];
     uint32_t row[kRowPieces], piece[kRowPieces];
@@ -156,7 +157,7 @@ static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArg
         if (first + i * kRowThreads >= total) continue;
         uint32_t o[4];
         if constexpr (kKind == kInt4) {
-            int4_to_16<kHalf>(c[i].x, o);
+            int4(c[i].x, o);
         } else {
             int8_to_16<kHalf>(c[i].x, o);
             int8_to_16<kHalf>(c[i].y, o + 2);

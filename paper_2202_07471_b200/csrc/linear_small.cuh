@@ -52,18 +52,20 @@ __device__ __forceinline__ uint4 load_x8(const uint16_t *row, int first, int cin
 constexpr int kFewWarps = 8;       // share the contraction
 constexpr int kFewRows = 16;       // output channels of a thread block
 constexpr int kFewTokens = 8;
-constexpr int kFewChunks = 4;      // in flight a warp
+constexpr int kFewChunks = 2;      // in flight a warp
 
 // Without a checkpoint (its 32 channels would be two thread blocks'): a thread block owns 16 channels, its warps take chunks of the
 // contraction in turn and are summed at the end.  In a chunk (four lanes times 16 bytes of codes) lane (g, q) holds 16 bytes of the
 // rows g and g + 8 and the same elements of token g: the order of the contraction inside a matrix instruction is free as long as
-// both operands agree, so nothing is shuffled.  A lane asks for the codes and the elements of x of four chunks at once, and
+// both operands agree, so nothing is shuffled.  A lane asks for the codes and the elements of x of two chunks at once, and
 // nothing waits for another thread before the sum: for so few tokens x is small beside the codes although every block reads all
-// of it.  (128 channels a block, x through shared memory and the contraction shared by a cluster took 6.2 us for one token
-// 4096 -> 4096 int4, this 4.2; mma.sync, since tcgen05 has no use for eight tokens: its step of 64 takes longer.)
+// of it.  Bound by the issue of instructions (about two a code) and the latency of a batch: one token int4 4096 -> 4096 4.3 us,
+// 11008 -> 32768 51 us (3.5 TB/s); four chunks and two blocks a multiprocessor 4.35 and 64.  (128 channels a block, x through shared
+// memory and the contraction shared by a cluster: 6.2 us.  mma.sync, since tcgen05 has no use for eight tokens: a step of 64
+// takes longer there.)
 // kVector: rows of codes and of x start on 16 bytes and are whole vectors.
 template <int kKind, bool kHalf, bool kVector>
-__global__ void __launch_bounds__(32 * kFewWarps, 2) few_kernel(const __grid_constant__ FewArgs p)
+__global__ void __launch_bounds__(32 * kFewWarps, 3) few_kernel(const __grid_constant__ FewArgs p)
 {
     constexpr int kCodes = kKind == kInt4 ? 32 : 16;
     constexpr int kUnits = kCodes / 8;   // 16 bytes of x a lane and chunk
@@ -82,6 +84,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 2) few_kernel(const __grid_con
         if (p.residual) res = to_float<kHalf>(p.residual[token * p.residual_stride + row]);
     }
     float acc[2][4] = {};
+    [[maybe_unused]] const Int4To16<kHalf> int4;
 
     for (int c0 = warp; c0 < chunks; c0 += kFewWarps * kFewChunks) {
         uint4 codes[kFewChunks][2], x[kFewChunks][kUnits];
@@ -114,7 +117,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 2) few_kernel(const __grid_con
                 for (int r = 0; r < 2; ++r) {
                     const uint32_t w[4] = {codes[u][r].x, codes[u][r].y, codes[u][r].z, codes[u][r].w};
                     if constexpr (kKind == kInt4) {
-                        int4_to_16<kHalf>(w[i], a[r]);
+                        int4(w[i], a[r]);
                     } else {
                         int8_to_16<kHalf>(w[2 * i], a[r]);
                         int8_to_16<kHalf>(w[2 * i + 1], a[r] + 2);

@@ -3,12 +3,14 @@
   python -m paper_2202_07471_b200.profile_case [--channels M] [--launches L] [--mode 7]
   python -m paper_2202_07471_b200.profile_case --workload resnet50 [--launches L]
   python -m paper_2202_07471_b200.profile_case --layer 128x65541x1x1 [--pack] [--no-sums] [--bits B]
+  python -m paper_2202_07471_b200.profile_case --linear 2048x4096x11008 [--pack] [--backward]
 
 Quantizes one [M, 2048, 3, 3] layer (default M = 4096: 302 MB of weights, larger than L2, a few
 hundred MB on the device) L times through the C ABI.  Values follow the large-layer recipe
 (seeded normal weights with a per-channel log-uniform scale).  With --workload NAME the whole
 model of that name (resnet18, resnet50, mobilenetv2, mixed_kernels) is quantized in one call instead,
-with --layer one layer of that shape (normal weights; --pack: packed int4 codes).
+with --layer one layer of that shape (normal weights; --pack: packed int4 codes).  With --linear
+TOKENSxCINxCOUT a linear layer is quantized and called (--backward: its gradients with gelu, from 8-bit checkpoints).
 """
 from __future__ import annotations
 
@@ -18,6 +20,7 @@ import numpy as np
 import torch
 
 from . import binding as sq
+from . import linear
 from . import workloads as W
 
 
@@ -31,7 +34,26 @@ def main() -> None:
     ap.add_argument("--layer", default="", help="cout x cin x kh x kw")
     ap.add_argument("--pack", action="store_true")
     ap.add_argument("--no-sums", action="store_true", help="no kernel and channel error sums")
+    ap.add_argument("--linear", default="", help="tokens x cin x cout")
+    ap.add_argument("--backward", action="store_true")
     args = ap.parse_args()
+    if args.linear:
+        tokens, cin, cout = (int(v) for v in args.linear.split("x"))
+        g = torch.Generator("cuda").manual_seed(0)
+        buf = sq.alloc_outputs(torch.randn((cout, cin), device="cuda", generator=g) / cin ** 0.5, False, False, pack_int4=args.pack)
+        sq.squant_quantize_model([buf], bits=4 if args.pack else 8, flags=sq.FLAG_NARROW_RANGE | (sq.FLAG_PACK_INT4 if args.pack else 0))
+        x = torch.randn((tokens, cin), device="cuda", generator=g).bfloat16()
+        dy = torch.randn((tokens, cout), device="cuda", generator=g).bfloat16()
+        if args.backward:
+            x8, z8 = linear.squant_checkpoint(x), linear.squant_checkpoint(dy)
+        for _ in range(args.launches):
+            if args.backward:
+                linear.squant_linear_backward(dy, buf.codes, buf.scales, cin=cin, act="gelu", pack_int4=args.pack, z=z8, x=x8, dweight=True, dbias=True)
+            else:
+                linear.squant_linear(x, buf.codes, buf.scales, pack_int4=args.pack)
+        sq.squant_device_status()
+        print(f"ok: {args.launches} calls of a linear layer, {tokens} tokens, {cin} to {cout}")
+        return
     if args.layer:
         shape = [int(v) for v in args.layer.split("x")]
         w = torch.randn(shape, device="cuda", generator=torch.Generator("cuda").manual_seed(0)) * (2.0 / (shape[1] * shape[2] * shape[3])) ** 0.5
