@@ -59,10 +59,10 @@ extern "C" {
 /* error codes (0 = success) */
 #define SQUANT_OK 0
 #define SQUANT_ERR_NULL (-1)        /* a required pointer is NULL */
-#define SQUANT_ERR_SHAPE (-2)       /* a dimension is <= 0 or the element count overflows */
+#define SQUANT_ERR_SHAPE (-2)       /* a dimension is <= 0, a stride smaller than a row, or the element count overflows */
 #define SQUANT_ERR_BITS (-3)        /* bits outside 2..8 */
-#define SQUANT_ERR_MODE (-4)        /* mode mask without SQUANT_MODE_E, or unknown mode / flag bits */
-#define SQUANT_ERR_ALIGN (-5)       /* weights / scales / error pointers not 4-byte aligned */
+#define SQUANT_ERR_MODE (-4)        /* mode mask without SQUANT_MODE_E, or unknown mode / flag bits, type or activation */
+#define SQUANT_ERR_ALIGN (-5)       /* weights / scales / error pointers not 4-byte aligned, 16-bit tensors not 2-byte, checkpoints not 16-byte */
 #define SQUANT_ERR_TOO_WIDE (-6)    /* one output channel does not fit the on-chip path */
 #define SQUANT_ERR_CUDA (-7)        /* a CUDA runtime call failed; see squant_last_cuda_error() */
 #define SQUANT_ERR_NOMEM (-8)       /* host or device allocation failed */
@@ -262,7 +262,7 @@ int squant_quantize_layer_noalloc(const squant_layer *layer, const squant_option
  * An activation in 8 bits.  32 consecutive features of a row share a power of two: with a = max|v| over them,
  * E = max(1, exponent field of a in fp32 - 6) and code = clamp(rint(v * 2^(127-E)), -127, 127), ties to even; the value is
  * code * 2^(E-127), exact in bf16 and at most half a step 2^(E-127) from v (a step for |v| above 127.5 steps, which
- * bf16 values never are).  A group with an infinity or a NaN has E = 255 and its values are NaN.  33 bits of 64 of a bf16 tensor.
+ * bf16 values never are).  A group with an infinity or a NaN has E = 255 and its values are NaN.  33/64 of a bf16 tensor's bytes.
  *   codes  [rows][code_pitch] int8, code_pitch = features rounded up to 32; the codes behind the last feature are 0
  *   exps   [rows][exps_pitch] uint8, exps_pitch = code_pitch / 32
  * Both start on 16 bytes.

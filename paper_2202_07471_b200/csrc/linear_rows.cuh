@@ -208,7 +208,7 @@ struct SlopeArgs {
 constexpr int kSlopeCols = 64;      // a thread block's columns: sixteen threads of four, 16 rows at a time
 constexpr int kSlopeRows = kRowThreads / 16;
 constexpr int kSlopeBatch = 4;      // rows a thread has in flight
-constexpr int kSlopeBlocks = 592;   // wanted of a launch: three a multiprocessor of a B200
+constexpr int kSlopeBlocks = 592;   // wanted of a launch: four a multiprocessor of a B200
 constexpr int kSlopeLeast = 64;     // tokens of a share
 
 template <int kValue>

@@ -176,7 +176,7 @@ bool vector_ok(const at::Tensor *t, int64_t n, const at::Device &d)
 
 bool codes_ok(const at::Tensor &codes, int64_t cout, int64_t cin, bool packed, const at::Device &d)
 {
-    return codes.scalar_type() == at::kChar && codes.dim() == 2 && codes.size(0) == cout && codes.size(1) == (packed ? (cin + 1) / 2 : cin) &&
+    return codes.scalar_type() == at::kChar && codes.dim() >= 2 && codes.size(0) == cout && codes.numel() == cout * (packed ? (cin + 1) / 2 : cin) &&
            codes.is_contiguous() && codes.device() == d;
 }
 
@@ -224,7 +224,7 @@ PyObject *linear(PyObject *, PyObject *args)
         const at::Tensor &x = *t[0];
         const at::Device d = x.device();
         const auto type = x.scalar_type();
-        if (!d.is_cuda() || d.index() != device || (type != at::kBFloat16 && type != at::kHalf) || t[1]->dim() != 2) return none();
+        if (!d.is_cuda() || d.index() != device || (type != at::kBFloat16 && type != at::kHalf) || t[1]->dim() < 2) return none();
         squant_linear_args a{};
         int64_t cin = 0;
         const int64_t cout = t[1]->size(0);

@@ -1237,10 +1237,10 @@ const char *squant_strerror(int code)
     switch (code) {
         case SQUANT_OK: return "success";
         case SQUANT_ERR_NULL: return "a required pointer is NULL";
-        case SQUANT_ERR_SHAPE: return "a layer dimension is not positive or the element count overflows";
+        case SQUANT_ERR_SHAPE: return "a dimension is not positive, a stride is smaller than a row, or the element count overflows";
         case SQUANT_ERR_BITS: return "bits must be in 2..8 (2..4 with SQUANT_FLAG_PACK_INT4)";
-        case SQUANT_ERR_MODE: return "mode mask must contain E (E, E|K, E|C or E|K|C); unknown mode or flag bits are rejected";
-        case SQUANT_ERR_ALIGN: return "float pointers must be 4-byte aligned";
+        case SQUANT_ERR_MODE: return "mode mask must contain E (E, E|K, E|C or E|K|C); unknown mode or flag bits, types and activations are rejected";
+        case SQUANT_ERR_ALIGN: return "float pointers must be 4-byte aligned, 16-bit ones 2-byte, checkpoints 16-byte";
         case SQUANT_ERR_TOO_WIDE: return "an output channel (cin*kh*kw) does not fit the on-chip path, not even spread over a cluster of 8 thread blocks";
         case SQUANT_ERR_CUDA: return "a CUDA runtime call failed (see squant_last_cuda_error)";
         case SQUANT_ERR_NOMEM: return "out of host or device memory";

@@ -48,7 +48,7 @@ class LinearGradArgs(ctypes.Structure):
 @dataclass
 class Checkpoint:
     """An activation [rows, features] in 8 bits: int8 codes [rows, features rounded up to 32] and uint8 exponents
-    [rows, groups of 32]; the values are codes * 2^(exponent - 127)."""
+    [rows, groups of 32], both contiguous and on 16 bytes; the values are codes * 2^(exponent - 127)."""
     codes: torch.Tensor
     exps: torch.Tensor
     features: int
@@ -57,7 +57,7 @@ class Checkpoint:
 @dataclass
 class LinearGrads:
     """Gradients of a linear layer, None where not asked for."""
-    dx: Optional[torch.Tensor] = None        # bfloat16 [tokens, cin]
+    dx: Optional[torch.Tensor] = None        # bfloat16 [..., cin], leading dimensions as dy's
     dweight: Optional[torch.Tensor] = None   # bfloat16 [cout, cin], of the weights codes * scales
     dbias: Optional[torch.Tensor] = None     # fp32 [cout]
     dscales: Optional[torch.Tensor] = None   # fp32 [cout]
@@ -171,7 +171,7 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str, device: torch.device) 
 def _codes(codes: torch.Tensor, cin: int, pack_int4: bool, device: torch.device) -> int:
     """Number of output channels."""
     width = (cin + 1) // 2 if pack_int4 else cin
-    if codes.dtype != torch.int8 or not codes.is_contiguous() or codes.device != device or codes.dim() < 2 or codes[0].numel() != width:
+    if codes.dtype != torch.int8 or not codes.is_contiguous() or codes.device != device or codes.dim() < 2 or math.prod(codes.shape[1:]) != width:
         raise ValueError(f"codes must be a contiguous int8 tensor [cout, {width}] next to the activations")
     return int(codes.shape[0])
 
@@ -296,9 +296,9 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
     for dweight); cin is needed with pack_int4, whose rows do not tell it.  dweight is the gradient of the weights
     codes * scales: a training loop applies it to the weights that it quantizes."""
     native = None if stream is not None else _native()
-    if native is not None and (z is None or z.features == dy.shape[-1]) and not (cin is None and pack_int4):
+    if native is not None and dy.dim() and (z is None or z.features == dy.shape[-1]) and not (cin is None and pack_int4):
         device = _device()
-        width = codes.shape[-1] if cin is None else cin
+        width = math.prod(codes.shape[1:]) if cin is None else cin
         if x is None or x.features == width:
             got = native.linear_backward(binding._raw_stream(device), device, dy, codes, scales, bias, z and z.codes, z and z.exps, x and x.codes,
                                          x and x.exps, width, ACTIVATIONS.get(act, -1), pack_int4, dx, dweight, dbias, dscales)
@@ -314,7 +314,7 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
         if cin is None:
             if pack_int4:
                 raise ValueError("cin must be given with pack_int4")
-            cin = codes[0].numel()
+            cin = math.prod(codes.shape[1:])
         if _codes(codes, cin, pack_int4, device) != cout:
             raise ValueError(f"codes have {codes.shape[0]} output channels, dy {cout}")
         _vector(scales, cout, "scales", device)

@@ -1,5 +1,8 @@
 """The linear operators as a program uses them: with the quantizer, in a training step, on other streams, in graphs, at the edges."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -80,6 +83,10 @@ def test_leading_dimensions():
     assert one.shape == (40,) and same_bits(one, want[0, 0, 0].to(torch.bfloat16))
     g = sq.squant_linear_backward(res, codes, scales, x=sq.squant_checkpoint(x), dweight=True)
     assert g.dx.shape == x.shape and g.dweight.shape == (40, 96)
+    # codes of a 1x1 convolution's weights
+    c4 = codes.view(40, 96, 1, 1)
+    assert same_bits(sq.squant_linear(x, c4, scales), want.to(torch.bfloat16))
+    assert same_bits(sq.squant_linear_backward(res, c4, scales).dx, g.dx)
     # a slice of heads: rows that lie apart
     wide = torch.zeros((30, 3, 96), device="cuda", dtype=torch.bfloat16)
     wide[:, 1] = x.view(30, 96)
@@ -192,11 +199,16 @@ def test_refusals():
                  lambda: sq.squant_linear_backward(dy, codes, scales, dweight=True, x=z8),
                  lambda: sq.squant_linear_backward(dy, pack(codes), scales, pack_int4=True),
                  lambda: sq.squant_linear_backward(dy, pack(codes), scales, cin=62, pack_int4=True),
-                 lambda: sq.squant_linear(x, codes, scales, stream=torch.cuda.Stream(), act="x")):
+                 lambda: sq.squant_linear(x, codes, scales, stream=torch.cuda.Stream(), act="x"),
+                 lambda: sq.squant_linear(x, codes.view(-1), scales), lambda: sq.squant_linear_backward(dy, codes.view(-1), scales),
+                 lambda: sq.squant_linear_backward(dy[0, 0], codes, scales, act="relu", z=z8)):
         with pytest.raises(ValueError):
             call()
-    with pytest.raises(sq.SquantError):   # one row for all tokens
-        sq.squant_linear(x[:1].expand(4, 64), codes, scales)
+    for call in (lambda: sq.squant_linear(x[:1].expand(4, 64), codes, scales),   # one row for all tokens
+                 lambda: sq.squant_linear(x, codes[:0], scales[:0]), lambda: sq.squant_linear_backward(dy[:, :0].contiguous(), codes[:0], scales[:0]),
+                 lambda: sq.squant_checkpoint_restore(sq.Checkpoint(x8.codes[1:], x8.exps[1:], 64))):   # exponents start on 2 bytes
+        with pytest.raises((ValueError, sq.SquantError)):
+            call()
     assert sq.squant_launch_count() == n
 
 
@@ -361,3 +373,51 @@ def test_codes_beyond_32_bits(tokens):
     mass = (x.double().abs() @ codes[-64:].double().abs().T).max()
     assert mass < 2 ** 24   # sums are exact in any order
     assert same_bits(y[:, -64:], want.to(torch.bfloat16)) and same_bits(y[:, :63], want[:, :63].to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("tokens", [6, 90, 400])
+def test_first_calls_of_a_process_in_a_capture(tokens):
+    """Kernels are loaded and set up while a graph is being recorded."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    program = f"""
+import sys
+sys.path[:0] = [{here!r}, {os.path.dirname(here)!r}]
+import torch
+import paper_2202_07471_b200 as sq
+from linear_cases import gen, pack, real_layer, same_bits
+codes, scales = real_layer(200, 136, 4, 1)
+stored, bias = pack(codes), torch.randn(136, generator=gen(2), device="cuda")
+x, dy = torch.randn(({tokens}, 200), generator=gen(3), device="cuda").bfloat16(), torch.randn(({tokens}, 136), generator=gen(4), device="cuda").bfloat16()
+def work():
+    y, z = sq.squant_linear(x, stored, scales, bias, act="gelu", pack_int4=True, checkpoint=True)
+    x8 = sq.squant_checkpoint(x)
+    g = sq.squant_linear_backward(dy, stored, scales, bias, cin=200, act="gelu", pack_int4=True, z=z, x=x8, dweight=True, dbias=True, dscales=True)
+    return y, sq.squant_linear(x[:3], stored, scales, pack_int4=True), sq.squant_checkpoint_restore(x8), g.dx, g.dweight, g.dbias, g.dscales
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = work()
+graph.replay()
+assert all(same_bits(a, b) for a, b in zip(out, work()))
+sq.squant_device_status()
+"""
+    done = subprocess.run([sys.executable, "-c", program], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
+
+
+def test_more_rows_than_a_launch_takes():
+    """2^30 rows: a launch indexes fewer than 2^31 pieces of rows."""
+    rows = 1 << 30
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB")
+    base = torch.randint(-127, 128, (1000003, 1), generator=gen(1), device="cuda").to(torch.bfloat16)
+    x = base.repeat(rows // 1000003 + 1, 1)[:rows]
+    c = sq.squant_checkpoint(x)
+    assert torch.equal(sq.squant_checkpoint_restore(c), x)
+    assert (c.codes[::99991, 1:] == 0).all()
+    del c, x
+    base = torch.randint(-3, 4, (1000003, 9), generator=gen(2), device="cuda").to(torch.bfloat16)
+    x = base.repeat(rows // 1000003 + 1, 1)[:rows]   # rows of 18 bytes, which are copied first
+    codes, scales = int_layer(9, 1, 8, 3)
+    want = _want(base, codes, scales).to(torch.bfloat16).repeat(rows // 1000003 + 1, 1)[:rows]
+    assert torch.equal(sq.squant_linear(x, codes, scales), want)
+    sq.squant_device_status()
