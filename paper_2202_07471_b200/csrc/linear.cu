@@ -79,31 +79,40 @@ int encoder(EncodeTiled &fn)
     return SQUANT_OK;
 }
 
+// A two-dimensional map.  The driver's function wants a current context, which a thread has once the runtime has set it up there: in a
+// thread that has done nothing on the GPU yet, the current device is set and the call made again.
+int encode(CUtensorMap &map, CUtensorMapDataType type, const void *p, const cuuint64_t (&dims)[2], const cuuint64_t (&strides)[1],
+           const cuuint32_t (&box)[2], const cuuint32_t (&step)[2], CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion)
+{
+    EncodeTiled fn;
+    if (int rc = encoder(fn)) return rc;
+    for (int attempt = 0;; ++attempt) {
+        const CUresult r = fn(&map, type, 2, const_cast<void *>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r == CUDA_SUCCESS) return SQUANT_OK;
+        if (r != CUDA_ERROR_INVALID_CONTEXT || attempt) return sq_host::cuda_failed(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+        int device;
+        SQ_CUDA(cudaGetDevice(&device));
+        SQ_CUDA(cudaSetDevice(device));
+    }
+}
+
 // A 16-bit matrix [rows][cols] whose boxes are 64 elements wide and `box_rows` high; elements outside read as zero.
 int matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t cols, int64_t stride, bool half, int box_rows)
 {
-    EncodeTiled encode;
-    if (int rc = encoder(encode)) return rc;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(2 * (rows <= 1 ? up(cols, 8) : stride))};
     const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)}, step[2] = {1, 1};
-    const CUresult r = encode(&map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(p),
-                              dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? SQUANT_OK : sq_host::cuda_failed(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    return encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p, dims, strides, box, step,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 // Codes as bytes [rows][pitch].
 int code_matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t pitch, int box_bytes, int box_rows)
 {
-    EncodeTiled encode;
-    if (int rc = encoder(encode)) return rc;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(pitch), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(pitch)};
     const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_bytes), static_cast<cuuint32_t>(box_rows)}, step[2] = {1, 1};
-    const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(p), dims, strides, box, step,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? SQUANT_OK : sq_host::cuda_failed(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, p, dims, strides, box, step, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 // As many thread blocks share a tile's contraction as there are multiprocessors (each holds two blocks) and stages for.

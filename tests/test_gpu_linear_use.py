@@ -3,6 +3,7 @@ import math
 import os
 import subprocess
 import sys
+import threading
 
 import pytest
 import torch
@@ -373,6 +374,55 @@ def test_codes_beyond_32_bits(tokens):
     mass = (x.double().abs() @ codes[-64:].double().abs().T).max()
     assert mass < 2 ** 24   # sums are exact in any order
     assert same_bits(y[:, -64:], want.to(torch.bfloat16)) and same_bits(y[:, :63], want[:, :63].to(torch.bfloat16))
+
+
+def test_calls_from_other_threads():
+    """A thread's first work on the GPU is a call (each kind of it), and four threads call at once on streams of their own."""
+    codes, scales = real_layer(256, 136, 4, 1)
+    stored, bias = pack(codes), torch.randn(136, generator=gen(2), device="cuda")
+    cases = []
+    for tokens in (6, 64, 400):
+        x, dy = torch.randn((tokens, 256), generator=gen(tokens), device="cuda").bfloat16(), torch.randn((tokens, 136), generator=gen(9), device="cuda").bfloat16()
+        cases.append((x, dy, [t.clone() for t in _layer_pass(x, dy, stored, scales, bias, True)]))
+    torch.cuda.synchronize()
+    failed = []
+
+    def guarded(work):
+        def run():
+            try:
+                work()
+            except Exception as e:
+                failed.append(e)
+        return run
+
+    def first_call(x, dy, want):
+        out = torch.empty_like(want[0])
+
+        def work():
+            assert same_bits(sq.squant_linear(x, stored, scales, bias, act="gelu", pack_int4=True, out=out), want[0])
+        return work
+
+    def many(k):
+        def work():
+            side = torch.cuda.Stream()
+            with torch.cuda.stream(side):
+                for i in range(60):
+                    x, dy, want = cases[(i + k) % 3]
+                    got = _layer_pass(x, dy, stored, scales, bias, True)
+                    assert all(same_bits(a, b) for a, b in zip(got, want))
+        return work
+
+    for case in cases:
+        t = threading.Thread(target=guarded(first_call(*case)))
+        t.start()
+        t.join()
+    threads = [threading.Thread(target=guarded(many(k))) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    sq.squant_device_status()
 
 
 @pytest.mark.parametrize("tokens", [6, 90, 400])
