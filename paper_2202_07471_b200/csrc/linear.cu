@@ -21,6 +21,12 @@ constexpr int64_t kMaxRows = 1ll << 30;
 // Up to as many tokens fused_kernel turns the codes into floats on the way to the tensor cores; beyond, they are expanded once.
 // 4096 -> 4096 int4, fused and expanded: 256 tokens 16.9 and 21.3 us, 384 tokens 33 and 21.5; 4096 -> 11008 256 tokens 43 and 49.
 constexpr int kFusedTokens = 256;
+// Up to eight tokens few_kernel is faster for every size.  Up to 32 it reads all of x once for 16 channels, so that its time grows with tokens
+// times codes while fused_kernel starts at 6 to 10 us: the line is drawn at this many codes times tiles of eight tokens (two or four).  int4, few
+// and fused: 512 -> 1000 2.3 and 5.7 us (16 tokens); 4096 -> 4096 6.2 and 10.6 (16), 10.1 and 11.3 (32); 4096 -> 6144 17.9 and 18.0 (32);
+// 4096 -> 11008 13.3 and 15.1 (16), 26.5 and 15.9 (32); 8192 -> 8192 19.4 and 18.8 (16).
+constexpr int kFewMost = 32;
+constexpr int64_t kFewWork = 3ll << 25;
 
 #define SQ_CUDA(call)                                                      \
     do {                                                                   \
@@ -296,11 +302,22 @@ bool bad_checkpoint(const squant_checkpoint_data &c) { return misaligned(c.codes
 
 // ---- forward
 
-bool few(const squant_linear_args &a) { return a.tokens <= sq::kFewTokens && !a.z.codes; }
-
 // Bytes of a row of codes, and whether every row starts on 16 bytes.
 int64_t code_pitch(int32_t cin, uint32_t flags) { return flags & SQUANT_FLAG_PACK_INT4 ? (static_cast<int64_t>(cin) + 1) / 2 : cin; }
 bool codes_on_vectors(const int8_t *codes, int64_t pitch) { return !misaligned(codes, 16) && pitch % 16 == 0; }
+
+// Bytes that rows of x start on for few_kernel (0: any, or rows of codes that start off 16), and the calls it takes.
+int few_align(const squant_linear_args &a)
+{
+    if (!codes_on_vectors(a.codes, code_pitch(a.cin, a.flags)) || !rows_on_vectors(a.x, a.x_stride, a.tokens) || a.cin % 8) return 0;
+    return a.cin % 16 || misaligned(a.x, 32) || (a.tokens > 1 && a.x_stride % 16) ? 16 : 32;
+}
+bool few(const squant_linear_args &a)
+{
+    if (a.z.codes || a.tokens > kFewMost) return false;
+    if (a.tokens <= sq::kFewTokens) return true;
+    return static_cast<int64_t>(a.cin) * a.cout * (a.tokens > 2 * sq::kFewTokens ? 4 : 2) <= kFewWork && few_align(a) == 32;
+}
 
 // Parts of the workspace: copies of x and of the codes with rows that TMA can read, or the codes as 16-bit floats.
 struct ForwardPlan {
@@ -360,9 +377,14 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
         s.y = static_cast<uint16_t *>(a.y);
         s.y_stride = a.y_stride;
         s.act = static_cast<int32_t>(a.act);
-        const bool vector = codes_on_vectors(a.codes, pitch) && rows_on_vectors(a.x, a.x_stride, a.tokens) && a.cin % 8 == 0;
+        const int align = few_align(a);
+        const auto kernel = a.tokens > 2 * sq::kFewTokens ? sq::few_kernel<kKind, kHalf, 32, 4>
+                            : a.tokens > sq::kFewTokens   ? sq::few_kernel<kKind, kHalf, 32, 2>
+                            : align == 32                 ? sq::few_kernel<kKind, kHalf, 32, 1>
+                            : align == 16                 ? sq::few_kernel<kKind, kHalf, 16, 1>
+                                                          : sq::few_kernel<kKind, kHalf, 0, 1>;
         const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kFewRows - 1) / sq::kFewRows);
-        return launch(vector ? sq::few_kernel<kKind, kHalf, true> : sq::few_kernel<kKind, kHalf, false>, dim3(grid), dim3(1), 32 * sq::kFewWarps, 0, stream, s);
+        return launch(kernel, dim3(grid), dim3(1), 32 * sq::kFewWarps, 0, stream, s);
     }
     int device, sms;
     if (int rc = device_sms(device, sms)) return rc;

@@ -53,6 +53,38 @@ def test_forward_of_integers_is_exact(tokens, cin, cout, bits, dtype):
     sq.squant_device_status()
 
 
+# up to 32 tokens: rows of x on 32, 16 or fewer bytes, tiles of tokens that end inside, channels that end inside a group of 16; either side
+# of the line between the kernels (50 million codes for 16 tokens, 25 for 32)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("tokens", [1, 3, 8, 9, 15, 16, 17, 24, 25, 32])
+@pytest.mark.parametrize("cin,cout", [(32, 16), (96, 17), (1056, 40), (2080, 9), (16, 8), (24, 33)])
+def test_few_tokens(tokens, cin, cout, bits, dtype):
+    codes, scales = int_layer(cin, cout, bits, 1)
+    if dtype == torch.float16:
+        scales = scales * 2.0 ** -9
+    bias, res = _ints((cout,), -9, 9, 3, torch.float32), _ints((tokens, cout), -20, 20, 4, dtype)
+    x = _ints((tokens, cin), -3, 3, 2, dtype)
+    want = ((x.double() @ codes.double().T) * scales.double() + bias.double() + res.double()).to(dtype)
+    for pad, offset in ((0, 0), (16, 0), (8, 0), (16, 8), (32, 16), (1, 0)):
+        buf = torch.full((tokens * (cin + pad) + offset + 16,), float("nan"), device="cuda", dtype=dtype)
+        xs = buf.as_strided((tokens, cin), (cin + pad, 1), offset)
+        xs.copy_(x)
+        out = torch.full((tokens + 1, cout + 1), 7.0, device="cuda", dtype=dtype)
+        sq.squant_linear(xs, pack(codes) if bits == 4 else codes, scales, bias, residual=res, pack_int4=bits == 4, out=out[:tokens, :cout])
+        assert same_bits(out[:tokens, :cout], want), (pad, offset)
+        assert (out[tokens:] == 7).all() and (out[:, cout:] == 7).all()
+
+
+@pytest.mark.parametrize("tokens,cin,cout", [(16, 4096, 12288), (16, 4096, 12304), (32, 4096, 6144), (32, 4096, 6160)])
+def test_either_side_of_the_line_for_few_tokens(tokens, cin, cout):
+    codes, scales = int_layer(cin, cout, 4, 1)
+    x = _ints((tokens, cin), -3, 3, 2, torch.bfloat16)
+    got = sq.squant_linear(x, pack(codes), scales, pack_int4=True)
+    assert same_bits(got, ((x.double() @ codes.double().T) * scales.double()).to(torch.bfloat16))
+    sq.squant_device_status()
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("bits,dtype,tokens", [(4, torch.bfloat16, 5), (8, torch.float16, 20), (4, torch.float16, 70), (8, torch.bfloat16, 140)])
 def test_forward_of_activations(act, bits, dtype, tokens):
