@@ -228,3 +228,36 @@ def test_gradients_of_real_values(tokens, cin, cout, bits, act):
     d = zv - bias.double()
     exact = (dz * d).sum(0) / s
     assert ((g.dscales.double() - exact).abs() <= ((dz.abs() * place * 2 + dz_off) * (d.abs() + bias.double().abs() * 2.0 ** -23)).sum(0) / s).all()
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_slopes_of_long_columns(act):
+    """Codes are the unit matrix and scales 1, so that dx is dz rounded to bf16.  Groups have exponents of all kinds, and the call on all tokens
+    gives what calls on a hundred at a time give."""
+    tokens, width = 1300, 4096
+    codes, scales = torch.eye(width, device="cuda").to(torch.int8), torch.ones(width, device="cuda")
+    g = gen(1)
+    unit = torch.exp2(torch.randint(-12, 12, (tokens, width // 32), generator=g, device="cuda").float()).repeat_interleave(32, 1)
+    z = (torch.randn((tokens, width), generator=g, device="cuda") * unit).to(torch.bfloat16)
+    z[7, 100] = float("nan")
+    dy = torch.randn((tokens, width), generator=g, device="cuda").to(torch.bfloat16)
+    z8 = sq.squant_checkpoint(z)
+    got = sq.squant_linear_backward(dy, codes, scales, act=act, z=z8, dbias=True, dscales=True)
+    for t in range(0, tokens, 100):
+        part = sq.Checkpoint(z8.codes[t:t + 100].clone(), z8.exps[t:t + 100].clone(), width)
+        assert same_bits(sq.squant_linear_backward(dy[t:t + 100], codes, scales, act=act, z=part).dx, got.dx[t:t + 100])
+    zv = decode64(z8.codes, z8.exps, width)
+    slope = slope64(zv, act)
+    exact = dy.double() * slope
+    # dz is off by the slope's few last places of its largest term (1 + |z|), the result by half a step
+    off = dy.double().abs() * 16 * 2.0 ** -23 * (1 + zv.abs())
+    good = ~torch.isnan(zv)
+    rows = good.all(1)   # a NaN times the unit matrix's zeros is a NaN in all of its row
+    assert torch.equal(torch.isnan(got.dx), ~rows[:, None].expand_as(got.dx))
+    assert ((got.dx.double() - exact).abs() <= off + 2.0 ** -8 * (exact.abs() + off))[rows].all()
+    columns = good.all(0)
+    # sums of `tokens` terms in fp32: at most tokens + 2 last places of the terms' magnitudes
+    for have, terms in ((got.dbias, exact), (got.dscales, exact * zv)):
+        mass = terms.abs().sum(0) + (off * (1 + zv.abs())).sum(0)
+        assert ((have.double() - terms.sum(0)).abs() <= (off * (1 + zv.abs())).sum(0) + (tokens + 2) * 2.0 ** -23 * mass)[columns].all()
+        assert torch.isnan(have[~columns]).all()
