@@ -21,12 +21,14 @@ constexpr int64_t kMaxRows = 1ll << 30;
 // Up to as many tokens fused_kernel turns the codes into floats on the way to the tensor cores; beyond, they are expanded once.
 // 4096 -> 4096 int4, fused and expanded: 256 tokens 16.9 and 21.3 us, 384 tokens 33 and 21.5; 4096 -> 11008 256 tokens 43 and 49.
 constexpr int kFusedTokens = 256;
-// Up to eight tokens few_kernel is faster for every size.  Up to 32 it reads all of x once for 16 channels, so that its time grows with tokens
-// times codes while fused_kernel starts at 6 to 10 us: the line is drawn at this many codes times tiles of eight tokens (two or four).  int4, few
-// and fused: 512 -> 1000 2.3 and 5.7 us (16 tokens); 4096 -> 4096 6.2 and 10.6 (16), 10.1 and 11.3 (32); 4096 -> 6144 17.9 and 18.0 (32);
-// 4096 -> 11008 13.3 and 15.1 (16), 26.5 and 15.9 (32); 8192 -> 8192 19.4 and 18.8 (16).
-constexpr int kFewMost = 32;
-constexpr int64_t kFewWork = 3ll << 25;
+// Up to eight tokens few_kernel is faster for every size.  Beyond, it reads all of x once for 16 channels, and from 33 tokens on the codes for
+// 32 tokens anew, so that its time grows with tokens times codes while fused_kernel starts at 6 to 10 us: the lines are drawn at this many
+// codes times tiles of eight tokens, a contraction of less than 2048 counted as that (a block's warps do not all have work) and fewer than
+// 4096 channels, all blocks of tokens together, as that (the GPU is not full).  int4, few and fused: 16 tokens 512 -> 1000 2.3 and 5.7 us, 4096 -> 4096 6.2 and 10.6, 4096 -> 11008
+// 13.3 and 15.1, 8192 -> 8192 19.4 and 18.8; 32 tokens 4096 -> 4096 10.1 and 11.3, 4096 -> 6144 17.9 and 18.0, 4096 -> 11008 26.5 and 15.9;
+// 64 tokens 512 -> 1000 2.5 and 6.7, 2048 -> 4096 11.2 and 11.3; 96 tokens 2048 -> 4096 15.1 and 12.7; 128 tokens 1024 -> 4096 12.5 and 12.9, 512 -> 4096 8.6
+// and 8.1; 64 tokens 16384 -> 256 19.7 and 14.9; 256 tokens 1024 -> 1024 6.9 and 10.5, 512 -> 4096 15.4 and 9.9.
+constexpr int64_t kFewWork = 3ll << 25, kFewWorkBeyond32 = 1ll << 26;
 
 #define SQ_CUDA(call)                                                      \
     do {                                                                   \
@@ -312,11 +314,15 @@ int few_align(const squant_linear_args &a)
     if (!codes_on_vectors(a.codes, code_pitch(a.cin, a.flags)) || !rows_on_vectors(a.x, a.x_stride, a.tokens) || a.cin % 8) return 0;
     return a.cin % 16 || misaligned(a.x, 32) || (a.tokens > 1 && a.x_stride % 16) ? 16 : 32;
 }
+// Thread blocks that share the tokens: four tiles each.
+int64_t few_blocks(int64_t tokens) { return (tokens + 4 * sq::kFewTokens - 1) / (4 * sq::kFewTokens); }
 bool few(const squant_linear_args &a)
 {
-    if (a.z.codes || a.tokens > kFewMost) return false;
+    if (a.z.codes || a.tokens > kFusedTokens) return false;
     if (a.tokens <= sq::kFewTokens) return true;
-    return static_cast<int64_t>(a.cin) * a.cout * (a.tokens > 2 * sq::kFewTokens ? 4 : 2) <= kFewWork && few_align(a) == 32;
+    const int64_t blocks = few_blocks(a.tokens), tiles = a.tokens > 2 * sq::kFewTokens ? 4 : 2;
+    const int64_t codes = std::max<int64_t>(a.cin, 2048) * std::max<int64_t>(a.cout * blocks, 4096);
+    return codes * tiles <= (blocks > 1 ? kFewWorkBeyond32 : kFewWork) && few_align(a) == 32;
 }
 
 // Parts of the workspace: copies of x and of the codes with rows that TMA can read, or the codes as 16-bit floats.
@@ -384,7 +390,7 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
                             : align == 16                 ? sq::few_kernel<kKind, kHalf, 16, 1>
                                                           : sq::few_kernel<kKind, kHalf, 0, 1>;
         const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.cout) + sq::kFewRows - 1) / sq::kFewRows);
-        return launch(kernel, dim3(grid), dim3(1), 32 * sq::kFewWarps, 0, stream, s);
+        return launch(kernel, dim3(grid, static_cast<unsigned>(few_blocks(a.tokens))), dim3(1), 32 * sq::kFewWarps, 0, stream, s);
     }
     int device, sms;
     if (int rc = device_sms(device, sms)) return rc;

@@ -74,7 +74,8 @@ constexpr int kFewTokens = 8;      // of a tile
 // from DRAM.  (128 channels a block, x through shared memory and the contraction shared by a cluster: 6.2 us for one token; 32 channels
 // a block: 6.1, 8 tokens 6.6; sixteen tokens with one chunk in flight and three blocks a multiprocessor: 6.7.  mma.sync, since a step
 // of 64 takes tcgen05 longer here.)
-// kAlign: rows of x as load_x16 says; rows of codes start on 16 bytes unless it is 0.  kTiles: tiles of eight tokens.
+// kAlign: rows of x as load_x16 says; rows of codes start on 16 bytes unless it is 0.  kTiles: tiles of eight tokens of a thread block (y:
+// the next tokens).
 template <int kKind, bool kHalf, int kAlign, int kTiles>
 __global__ void __launch_bounds__(32 * kFewWarps, kTiles == 1 ? 3 : 2) few_kernel(const __grid_constant__ FewArgs p)
 {
@@ -85,19 +86,21 @@ __global__ void __launch_bounds__(32 * kFewWarps, kTiles == 1 ? 3 : 2) few_kerne
     constexpr int kMine = kTiles <= 2 ? 1 : kTiles / 2;     // results a thread finishes
     __shared__ float part[kFewWarps][kTiles * kFewTokens][kFewRows];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int token0 = static_cast<int>(blockIdx.y) * (kTiles * kFewTokens), tokens = p.tokens - token0;   // from token0 on
+    const uint16_t *const x_from = p.x + token0 * p.x_stride;
     const int row0 = static_cast<int>(blockIdx.x) * kFewRows;
     const int chunks = (p.cin + 4 * kCodes - 1) / (4 * kCodes);
     const int row_bytes = kKind == kInt4 ? (p.cin + 1) >> 1 : p.cin;
     // what the thread finishes: a channel of the tokens first, first + 16, ..
     const int first = threadIdx.x / kFewRows, row = row0 + static_cast<int>(threadIdx.x) % kFewRows;
     float scale = 0.0f, bias = 0.0f, res[kMine] = {};
-    if (first < p.tokens && row < p.cout) {
+    if (first < tokens && row < p.cout) {
         scale = get(p.scales + row);
         if (p.bias) bias = get(p.bias + row);
         if (p.residual)
 #pragma unroll
             for (int j = 0; j < kMine; ++j)
-                if (first + 16 * j < p.tokens) res[j] = to_float<kHalf>(p.residual[(first + 16 * j) * p.residual_stride + row]);
+                if (first + 16 * j < tokens) res[j] = to_float<kHalf>(p.residual[(token0 + first + 16 * j) * p.residual_stride + row]);
     }
     float acc[kTiles][kSums][4] = {};
     [[maybe_unused]] const Int4To16<kHalf> int4;
@@ -125,7 +128,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kTiles == 1 ? 3 : 2) few_kerne
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
                     const int row = g + 8 * t;
-                    load_x16<kAlign>(p.x + row * p.x_stride, k + 16 * i, row < p.tokens ? p.cin : 0, x[u][i][t]);
+                    load_x16<kAlign>(x_from + row * p.x_stride, k + 16 * i, row < tokens ? p.cin : 0, x[u][i][t]);
                 }
         }
 #pragma unroll
@@ -160,11 +163,11 @@ __global__ void __launch_bounds__(32 * kFewWarps, kTiles == 1 ? 3 : 2) few_kerne
 #pragma unroll
     for (int j = 0; j < kMine; ++j) {
         const int token = first + 16 * j;
-        if (token >= p.tokens) return;
+        if (token >= tokens) return;
         float u = 0.0f;
 #pragma unroll
         for (int w = 0; w < kFewWarps; ++w) u += part[w][token][row - row0];
-        p.y[token * p.y_stride + row] = to_16<kHalf>(act_value(fmaf(u, scale, bias), p.act) + res[j]);
+        p.y[(token0 + token) * p.y_stride + row] = to_16<kHalf>(act_value(fmaf(u, scale, bias), p.act) + res[j]);
     }
 }
 

@@ -53,11 +53,11 @@ def test_forward_of_integers_is_exact(tokens, cin, cout, bits, dtype):
     sq.squant_device_status()
 
 
-# up to 32 tokens: rows of x on 32, 16 or fewer bytes, tiles of tokens that end inside, channels that end inside a group of 16; either side
-# of the line between the kernels (50 million codes for 16 tokens, 25 for 32)
+# few tokens: rows of x on 32, 16 or fewer bytes, tiles of tokens that end inside, channels that end inside a group of 16; either side
+# of the lines between the kernels (50 million codes for 16 tokens, 25 for 32, 8 for 64, 2 for 256)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("tokens", [1, 3, 8, 9, 15, 16, 17, 24, 25, 32])
+@pytest.mark.parametrize("tokens", [1, 3, 8, 9, 15, 16, 17, 24, 25, 32, 33, 64, 71, 256])
 @pytest.mark.parametrize("cin,cout", [(32, 16), (96, 17), (1056, 40), (2080, 9), (16, 8), (24, 33)])
 def test_few_tokens(tokens, cin, cout, bits, dtype):
     codes, scales = int_layer(cin, cout, bits, 1)
@@ -76,7 +76,8 @@ def test_few_tokens(tokens, cin, cout, bits, dtype):
         assert (out[tokens:] == 7).all() and (out[:, cout:] == 7).all()
 
 
-@pytest.mark.parametrize("tokens,cin,cout", [(16, 4096, 12288), (16, 4096, 12304), (32, 4096, 6144), (32, 4096, 6160)])
+@pytest.mark.parametrize("tokens,cin,cout", [(16, 4096, 12288), (16, 4096, 12304), (32, 4096, 6144), (32, 4096, 6160),
+                                             (64, 4096, 2048), (64, 4096, 2064), (65, 1024, 5472), (256, 512, 1024), (256, 512, 1040), (64, 4112, 64)])
 def test_either_side_of_the_line_for_few_tokens(tokens, cin, cout):
     codes, scales = int_layer(cin, cout, 4, 1)
     x = _ints((tokens, cin), -3, 3, 2, torch.bfloat16)

@@ -35,7 +35,8 @@ def test_kernels_of_a_forward_call(tokens, save, launches):
 
 # more steps of the contraction than a tile's stages, shared by several thread blocks; several tiles a thread block
 @pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("tokens,cin,cout", [(5, 4096, 300), (16, 4096, 512), (40, 4096, 1100), (64, 11008, 256), (100, 4096, 512), (128, 2048, 1000), (200, 1500, 700), (700, 256, 9000)])
+@pytest.mark.parametrize("tokens,cin,cout", [(5, 4096, 300), (16, 4096, 512), (40, 4096, 1100), (64, 11008, 256), (100, 4096, 512), (128, 2048, 1000), (200, 1500, 700), (700, 256, 9000),
+                                             (40, 4096, 2200), (64, 11008, 1100), (100, 4096, 1500), (128, 4096, 1400), (24, 8192, 4096)])
 def test_calls_repeat_to_the_bit(tokens, cin, cout, bits):
     codes, scales = int_layer(cin, cout, bits, 1)
     x = _x(tokens, cin)
