@@ -242,7 +242,8 @@ int squant_quantize_layer_noalloc(const squant_layer *layer, const squant_option
  *   u = x C^T,  z = s * u + b,  y = act(z) + r
  *
  * A code is exact in the activations' type, so the products are exact, their sums are fp32 and the only roundings of a value
- * are those of fp32 sums and the one of y.  Tokens are rows; strides count elements from one row to the next, so that x,
+ * are those of fp32 sums and the one of y.  The tensor cores cut off what does not fit when they add up, which costs values of one sign 5.6e-9 of
+ * their sum a term; sums of more than 65,536 terms are put together from shorter ones.  Tokens are rows; strides count elements from one row to the next, so that x,
  * residual, y and the gradients may be slices of wider buffers.  No alignment is asked of 16-bit tensors beyond their
  * elements' own; rows that start on 16 bytes (and codes whose rows do) are read faster.
  *
@@ -298,7 +299,7 @@ typedef struct squant_linear_args {
 } squant_linear_args;
 
 /* Bytes of workspace the call with these arguments needs, or a negative error: up to 256 tokens 0 unless rows of x or of the codes start
- * off 16 bytes, beyond that the codes as 16-bit floats. */
+ * off 16 bytes, beyond that (and for cin above 524,288) the codes as 16-bit floats, and fp32 sums of y's shape for cin above 65,536. */
 int64_t squant_linear_workspace(const squant_linear_args *args);
 int squant_linear(const squant_linear_args *args, void *cuda_stream);
 

@@ -30,6 +30,9 @@ constexpr int kFusedTokens = 256;
 // and 8.1; 64 tokens 16384 -> 256 19.7 and 14.9; 256 tokens 1024 -> 1024 6.9 and 10.5, 512 -> 4096 15.4 and 9.9.
 constexpr int64_t kFewWork = 3ll << 25, kFewWorkBeyond32 = 1ll << 26;
 
+// Contractions that fused_kernel's thread blocks and few_kernel's warps can share so that no sum has more than kLongestSum terms.
+constexpr int64_t kLongestFused = sq::kLongestSum * std::min(sq::kFusedMostRanks, sq::kFewWarps);
+
 #define SQ_CUDA(call)                                                      \
     do {                                                                   \
         cudaError_t e__ = (call);                                          \
@@ -123,7 +126,7 @@ int code_matrix_map(CUtensorMap &map, const void *p, int64_t rows, int64_t pitch
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, p, dims, strides, box, step, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
-// As many thread blocks share a tile's contraction as there are multiprocessors (each holds two blocks) and stages for.
+// As many thread blocks share a tile's contraction as there are multiprocessors (each holds two blocks) and stages for, and as its length asks for.
 // x: [rows][depth] 16-bit.
 template <int kMode, int kKind, bool kHalf>
 int fused(const void *x, int64_t x_stride, sq::GemmArgs a, int device, int sms, cudaStream_t stream)
@@ -143,7 +146,8 @@ int fused(const void *x, int64_t x_stride, sq::GemmArgs a, int device, int sms, 
     a.row_tiles = (a.rows + sq::kFusedTokens - 1) / sq::kFusedTokens;
     a.tiles = static_cast<int64_t>(a.row_tiles) * ((static_cast<int64_t>(a.cols) + sq::kFusedCols - 1) / sq::kFusedCols);
     const int64_t steps = (static_cast<int64_t>(a.depth) + sq::kTileDepth - 1) / sq::kTileDepth;
-    const unsigned ranks = static_cast<unsigned>(std::max<int64_t>(1, std::min({static_cast<int64_t>(sq::kFusedMostRanks), 2 * sms / a.tiles, steps / 2})));
+    const int64_t needed = (a.depth + sq::kLongestSum - 1) / sq::kLongestSum;   // at most kFusedMostRanks: kLongestFused
+    const unsigned ranks = static_cast<unsigned>(std::max(needed, std::min({static_cast<int64_t>(sq::kFusedMostRanks), 2 * sms / a.tiles, steps / 2})));
     return launch(kernel, dim3(static_cast<unsigned>(a.tiles * ranks)), dim3(ranks), sq::kFusedThreads, sq::kFusedSmem, stream, map, code_map, a);
 }
 
@@ -162,10 +166,14 @@ int launch_dense(const CUtensorMap &map_a, const CUtensorMap &map_b, sq::GemmArg
     return launch(kernel, dim3(2 * static_cast<unsigned>(std::min<int64_t>(a.tiles, sms / 2))), dim3(2), sq::kDenseThreads, smem, stream, map_a, map_b, a);
 }
 
+// Bytes of the sums that the parts of a long contraction hand on.
+int64_t sums_bytes(int64_t rows, int64_t cols, int64_t depth) { return depth > sq::kLongestSum ? rows * up(cols, 32) * 4 : 0; }
+
 // The product of two 16-bit matrices: `a` as gemm's 16-bit operand, `b` [cols][depth] (forward) or [depth][cols].  Tiles of
 // 256 or 128 columns, whichever is done in fewer waves; a wave of narrow tiles takes about 0.6 of one of wide tiles.
+// sums: sums_bytes() of workspace.
 template <int kMode, bool kHalf>
-int dense(const void *a, int64_t a_stride, const void *b, int64_t b_stride, const sq::GemmArgs &g, int device, int sms, cudaStream_t stream)
+int dense(const void *a, int64_t a_stride, const void *b, int64_t b_stride, sq::GemmArgs g, void *sums, int device, int sms, cudaStream_t stream)
 {
     const int64_t row_tiles = (static_cast<int64_t>(g.rows) + sq::kPairRows - 1) / sq::kPairRows, pairs = sms / 2;
     const int64_t wide = (row_tiles * ((static_cast<int64_t>(g.cols) + 255) / 256) + pairs - 1) / pairs;
@@ -176,8 +184,19 @@ int dense(const void *a, int64_t a_stride, const void *b, int64_t b_stride, cons
                                           : matrix_map(map_a, a, g.rows, g.depth, a_stride, kHalf, 128)) return rc;
     if (int rc = kMode == sq::kForward ? matrix_map(map_b, b, g.cols, g.depth, b_stride, kHalf, use_wide ? 128 : 64)
                                        : matrix_map(map_b, b, g.depth, g.cols, b_stride, kHalf, sq::kTileDepth)) return rc;
-    return use_wide ? launch_dense<kMode, kHalf, 256>(map_a, map_b, g, device, sms, stream)
-                    : launch_dense<kMode, kHalf, 128>(map_a, map_b, g, device, sms, stream);
+    const int64_t steps = (static_cast<int64_t>(g.depth) + sq::kTileDepth - 1) / sq::kTileDepth;
+    const int64_t parts = (g.depth + sq::kLongestSum - 1) / sq::kLongestSum;
+    if (parts > 1) g.sums = static_cast<float *>(sums);
+    g.sums_pitch = up(g.cols, 32);
+    for (int64_t part = 0; part < parts; ++part) {
+        g.first_step = static_cast<int32_t>(steps * part / parts);
+        g.steps = static_cast<int32_t>(steps * (part + 1) / parts) - g.first_step;
+        g.sums_in = part > 0;
+        g.sums_out = part + 1 < parts;
+        if (int rc = use_wide ? launch_dense<kMode, kHalf, 256>(map_a, map_b, g, device, sms, stream)
+                              : launch_dense<kMode, kHalf, 128>(map_a, map_b, g, device, sms, stream)) return rc;
+    }
+    return SQUANT_OK;
 }
 
 enum class RowKernel { kCheckpoint, kRestore, kExpandInt4Bf16, kExpandInt4Fp16, kExpandInt8Bf16, kExpandInt8Fp16 };
@@ -318,30 +337,32 @@ int few_align(const squant_linear_args &a)
 int64_t few_blocks(int64_t tokens) { return (tokens + 4 * sq::kFewTokens - 1) / (4 * sq::kFewTokens); }
 bool few(const squant_linear_args &a)
 {
-    if (a.z.codes || a.tokens > kFusedTokens) return false;
+    if (a.z.codes || a.tokens > kFusedTokens || a.cin > kLongestFused) return false;
     if (a.tokens <= sq::kFewTokens) return true;
     const int64_t blocks = few_blocks(a.tokens), tiles = a.tokens > 2 * sq::kFewTokens ? 4 : 2;
     const int64_t codes = std::max<int64_t>(a.cin, 2048) * std::max<int64_t>(a.cout * blocks, 4096);
     return codes * tiles <= (blocks > 1 ? kFewWorkBeyond32 : kFewWork) && few_align(a) == 32;
 }
 
-// Parts of the workspace: copies of x and of the codes with rows that TMA can read, or the codes as 16-bit floats.
+// Parts of the workspace: copies of x and of the codes with rows that TMA can read, or the codes as 16-bit floats and the sums of a long contraction.
 struct ForwardPlan {
     bool dense = false;
     Copy x, codes;
+    int64_t wide_bytes = 0;   // the codes as 16-bit floats
     int64_t bytes = 0;
 };
 
 ForwardPlan forward_plan(const squant_linear_args &a)
 {
     ForwardPlan p;
-    p.dense = a.tokens > kFusedTokens;
+    p.dense = a.tokens > kFusedTokens || a.cin > kLongestFused;
     if (few(a)) return p;
     uint8_t *at = static_cast<uint8_t *>(a.workspace);
     if (!rows_on_vectors(a.x, a.x_stride, a.tokens)) p.x = {a.x, a.tokens, 2 * static_cast<int64_t>(a.cin), 2 * (a.tokens > 1 ? a.x_stride : a.cin), at};
     const int64_t pitch = code_pitch(a.cin, a.flags);
     if (!p.dense && !codes_on_vectors(a.codes, pitch)) p.codes = {a.codes, a.cout, pitch, pitch, at ? at + p.x.out_bytes() : nullptr};
-    p.bytes = p.x.out_bytes() + p.codes.out_bytes() + (p.dense ? a.cout * up(a.cin, 8) * 2 : 0);
+    p.wide_bytes = p.dense ? a.cout * up(a.cin, 8) * 2 : 0;
+    p.bytes = p.x.out_bytes() + p.codes.out_bytes() + p.wide_bytes + (p.dense ? sums_bytes(a.tokens, a.cout, a.cin) : 0);
     return p;
 }
 
@@ -419,7 +440,7 @@ int forward(const squant_linear_args &a, cudaStream_t stream)
     if (plan.dense) {
         uint8_t *b = static_cast<uint8_t *>(a.workspace) + plan.x.out_bytes();
         if (int rc = expand(a.codes, a.cout, a.cin, kKind == sq::kInt4, kHalf, b, stream)) return rc;
-        return dense<sq::kForward, kHalf>(x, x_stride, b, up(a.cin, 8), g, device, sms, stream);
+        return dense<sq::kForward, kHalf>(x, x_stride, b, up(a.cin, 8), g, b + plan.wide_bytes, device, sms, stream);
     }
     g.codes = static_cast<const uint8_t *>(plan.codes.in ? plan.codes.out : a.codes);
     g.code_pitch = plan.codes.in ? plan.codes.out_pitch() : pitch;
@@ -437,7 +458,7 @@ struct SlopePlan {
     int64_t partial_bytes = 0;       // behind dzs and dz: sums of the shares
     Copy codes;               // a copy of the codes with rows that TMA can read
     int64_t wide_bytes = 0;   // behind them: that copy or the codes as 16-bit floats, then the input as 16-bit floats
-    int64_t bytes = 0;
+    int64_t bytes = 0;        // behind these the sums of a long contraction, of dx and then of dweight
 };
 
 SlopePlan slope_plan(const squant_linear_grad_args &a)
@@ -452,13 +473,13 @@ SlopePlan slope_plan(const squant_linear_grad_args &a)
     s.share = std::max<int64_t>(1, (a.tokens + s.shares - 1) / s.shares);
     if (s.shares > 1 && (a.dbias || a.dscales)) s.partial_bytes = up(s.shares * 2 * a.cout * 4, 16);
     s.slope_bytes = (s.dzs + s.dz) * a.tokens * s.pitch * 2 + s.partial_bytes;
-    s.dense = s.dzs && a.tokens > kFusedTokens;
+    s.dense = s.dzs && (a.tokens > kFusedTokens || a.cout > kLongestFused);
     const int64_t row = up(a.cin, 8) * 2;
     const int64_t pitch = code_pitch(a.cin, a.flags);
     if (s.dzs && !s.dense && !codes_on_vectors(a.codes, pitch))
         s.codes = {a.codes, a.cout, pitch, pitch, a.workspace ? static_cast<uint8_t *>(a.workspace) + s.slope_bytes : nullptr};
     s.wide_bytes = std::max({s.dense ? a.cout * row : 0, s.codes.out_bytes(), a.dweight ? a.tokens * row : 0});
-    s.bytes = s.slope_bytes + s.wide_bytes;
+    s.bytes = s.slope_bytes + s.wide_bytes + std::max(s.dense ? sums_bytes(a.tokens, a.cin, a.cout) : 0, a.dweight ? sums_bytes(a.cout, a.cin, a.tokens) : 0);
     return s;
 }
 
@@ -605,7 +626,7 @@ int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_strea
     float *partial = reinterpret_cast<float *>(static_cast<uint8_t *>(a.workspace) + plan.slope_bytes - plan.partial_bytes);
     if (plan.any)
         if (int rc = slope(a, plan, dzs, dz, partial, stream)) return rc;
-    uint8_t *wide = static_cast<uint8_t *>(a.workspace) + plan.slope_bytes;
+    uint8_t *wide = static_cast<uint8_t *>(a.workspace) + plan.slope_bytes, *sums = wide + plan.wide_bytes;
     if (plan.dzs) {
         const bool packed = a.flags & SQUANT_FLAG_PACK_INT4;
         sq::GemmArgs g{};
@@ -617,7 +638,7 @@ int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_strea
         g.out_vector = rows_on_vectors(a.dx, a.dx_stride, a.tokens);
         if (plan.dense) {
             if (int rc = expand(a.codes, a.cout, a.cin, packed, false, wide, stream)) return rc;
-            if (int rc = dense<sq::kInputGrad, false>(dzs, plan.pitch, wide, up(a.cin, 8), g, device, sms, stream)) return rc;
+            if (int rc = dense<sq::kInputGrad, false>(dzs, plan.pitch, wide, up(a.cin, 8), g, sums, device, sms, stream)) return rc;
         } else {
             if (int rc = launch_copies(plan.codes, Copy{}, stream)) return rc;
             g.codes = static_cast<const uint8_t *>(plan.codes.in ? plan.codes.out : a.codes);
@@ -640,7 +661,7 @@ int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_strea
         g.out = static_cast<uint16_t *>(a.dweight);
         g.out_stride = a.dweight_stride;
         g.out_vector = rows_on_vectors(a.dweight, a.dweight_stride, a.cout);
-        if (int rc = dense<sq::kWeightGrad, false>(dz ? dz : a.dy, dz ? plan.pitch : a.dy_stride, wide, up(a.cin, 8), g, device, sms, stream)) return rc;
+        if (int rc = dense<sq::kWeightGrad, false>(dz ? dz : a.dy, dz ? plan.pitch : a.dy_stride, wide, up(a.cin, 8), g, sums, device, sms, stream)) return rc;
     }
     return SQUANT_OK;
 }

@@ -102,7 +102,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     cluster_arrive_wait();   // the other block's barriers are there
     tc_fence_after();
     const uint32_t tmem = tmem_base;
-    const int steps = (p.depth + kTileDepth - 1) / kTileDepth;
+    const int steps = p.steps;
     const int64_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (warp < kDenseEpilogueWarps) {
@@ -139,17 +139,18 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     const uint32_t bar = cluster_addr(full(s), 0);
                     if (rank == 0) bar_expect(full(s), 2 * (S::kBytesA + S::kBytesB));
                     const uint32_t at = smem_a + s * S::kBytesA, bt = smem_b + s * S::kBytesB;
+                    const int from = (p.first_step + k) * kTileDepth;
                     if (kMode == kWeightGrad) {
-                        pair_tma_2d(at, &map_a, row0, k * kTileDepth, bar);
-                        pair_tma_2d(at + 8192, &map_a, row0 + 64, k * kTileDepth, bar);
+                        pair_tma_2d(at, &map_a, row0, from, bar);
+                        pair_tma_2d(at + 8192, &map_a, row0 + 64, from, bar);
                     } else {
-                        pair_tma_2d(at, &map_a, k * kTileDepth, row0, bar);
+                        pair_tma_2d(at, &map_a, from, row0, bar);
                     }
                     if (kMode == kForward) {
-                        pair_tma_2d(bt, &map_b, k * kTileDepth, col0, bar);
+                        pair_tma_2d(bt, &map_b, from, col0, bar);
                     } else {
 #pragma unroll
-                        for (int j = 0; j < kCols / 128; ++j) pair_tma_2d(bt + 8192 * j, &map_b, col0 + 64 * j, k * kTileDepth, bar);
+                        for (int j = 0; j < kCols / 128; ++j) pair_tma_2d(bt + 8192 * j, &map_b, col0 + 64 * j, from, bar);
                     }
                 }
                 __syncwarp();

@@ -310,7 +310,8 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-constexpr int kWaitLimit = 1 << 22;   // tries, each of which the hardware parks for a while: seconds
+// Tries of a wait: 0.2 s.  The longest wait that goes well is for a tile's sums, at most kLongestSum terms of a contraction: below a millisecond.
+constexpr int kWaitLimit = 1 << 22;
 
 // False when the wait ran out or another thread of the block gave up (*gave_up is shared by the block).
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)

@@ -22,6 +22,11 @@ struct GemmArgs {
     int32_t code_rows;
     int32_t rows, cols;      // of the result
     int32_t depth;           // of the contraction
+    // dense_kernel only: the launch's part of a long contraction, in steps of kTileDepth, and the fp32 sums that its parts hand on
+    int32_t first_step, steps;
+    float *sums;             // [rows][sums_pitch], or null: one part
+    int64_t sums_pitch;      // a multiple of 32
+    int32_t sums_in, sums_out;   // add what the parts before left; leave the sums and no result
     int32_t row_tiles;
     int32_t box_rows;        // of a copy of the 16-bit operand
     int64_t tiles;
@@ -40,6 +45,12 @@ struct GemmArgs {
 };
 
 constexpr int kTileDepth = 64;        // of the contraction per stage: 128 bytes
+
+// Terms of a contraction that one accumulator of a matrix instruction takes, at most.  The tensor cores cut off what does not fit when they add
+// up: sums of values of one sign lose 5.6e-9 of themselves a term (dweight of 2^21 tokens 1.2 %, 2^16 tokens 4e-4, an eighth of bf16's half step).
+// Longer contractions are shared by warps and thread blocks where they are shared anyhow, or go through dense_kernel in parts whose sums are added
+// in fp32, to the nearest.  A part also bounds what a wait for a tile's sums has to cover: 1,024 steps, below a millisecond.
+constexpr int64_t kLongestSum = 1 << 16;
 
 // Places where a warp turns 32 rows by 32 columns of 16-bit values round, for rows that a thread cannot read or write in vectors: a
 // thread's row lies in 17 words, so that rows and columns hit all banks.
@@ -86,6 +97,24 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row0, int co
     float v[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(acc[i]);
+    if (p.sums) {
+        float4 *sums = reinterpret_cast<float4 *>(p.sums + row * p.sums_pitch + col);   // 32 columns: the pitch is a multiple of that
+        if (valid && p.sums_in)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float4 s = get(sums + j);
+                v[4 * j] += s.x;
+                v[4 * j + 1] += s.y;
+                v[4 * j + 2] += s.z;
+                v[4 * j + 3] += s.w;
+            }
+        if (p.sums_out) {
+            if (valid)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sums[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            return;
+        }
+    }
     if constexpr (kMode == kForward) {
         if (p.param_vector && n == 32) {
 #pragma unroll

@@ -110,6 +110,28 @@ def test_workspace_sizes():
     assert need(cin=61, dx_stride=61) == 4 * 32 * 2 + 32 * 64
 
 
+def test_workspace_of_long_contractions():
+    """More than 65,536 terms go in parts, whose fp32 sums [rows][columns rounded up to 32] lie behind the rest; up to 256 tokens eight thread
+    blocks or warps share 524,288."""
+    lib = linear._lib()
+    need = lambda **kw: lib.squant_linear_workspace(ctypes.byref(forward(**kw)))
+    k = 1 << 16
+    assert need(tokens=300, cin=k, x_stride=k) == 32 * k * 2
+    assert need(tokens=300, cin=k + 16, x_stride=k + 16) == 32 * (k + 16) * 2 + 300 * 32 * 4
+    assert need(tokens=300, cin=k + 16, x_stride=k + 16, cout=33, y_stride=33) == 33 * (k + 16) * 2 + 300 * 64 * 4
+    assert need(tokens=4, cin=8 * k, x_stride=8 * k) == 0 and need(tokens=40, cin=8 * k, x_stride=8 * k) == 0
+    for tokens in (1, 4, 40):
+        assert need(tokens=tokens, cin=8 * k + 16, x_stride=8 * k + 16) == 32 * (8 * k + 16) * 2 + tokens * 32 * 4
+    need = lambda **kw: lib.squant_linear_backward_workspace(ctypes.byref(backward(**kw)))
+    assert need(tokens=k, dx=None, dweight=OK_PTR, dweight_stride=64, x=CK) == k * 64 * 2
+    assert need(tokens=k + 1, dx=None, dweight=OK_PTR, dweight_stride=64, x=CK) == (k + 1) * 64 * 2 + 32 * 64 * 4
+    assert need(tokens=300, cout=k + 8, dy_stride=k + 8) == 300 * (k + 8) * 2 + (k + 8) * 64 * 2 + 300 * 64 * 4
+    assert need(tokens=4, cout=8 * k, dy_stride=8 * k) == 4 * 8 * k * 2
+    assert need(tokens=4, cout=8 * k + 8, dy_stride=8 * k + 8) == 4 * (8 * k + 8) * 2 + (8 * k + 8) * 64 * 2 + 4 * 64 * 4
+    # both sums take the same place
+    assert need(tokens=k + 1, cout=k + 8, dy_stride=k + 8, dweight=OK_PTR, dweight_stride=64, x=CK) == (k + 1) * (k + 8) * 2 + (k + 8) * 64 * 2 + (k + 8) * 64 * 4
+
+
 def test_tensors_have_to_be_on_a_gpu():
     x, codes, scales = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(32, 64, dtype=torch.int8), torch.ones(32)
     with pytest.raises(ValueError, match="CUDA"):
