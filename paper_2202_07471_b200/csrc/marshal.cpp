@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -139,6 +140,15 @@ PyObject *use(PyObject *, PyObject *args)
 
 void *stream_of(unsigned long long handle) { return reinterpret_cast<void *>(static_cast<uintptr_t>(handle)); }
 
+// Whether a result would have to be part of an autograd graph, which these calls make none of: the Python code refuses it.
+bool wants_graph(std::initializer_list<const at::Tensor *> inputs)
+{
+    if (!at::GradMode::is_enabled()) return false;
+    for (const at::Tensor *t : inputs)
+        if (t && t->requires_grad()) return true;
+    return false;
+}
+
 // The tensor itself; null for None; false where it is anything but a plain tensor.
 bool plain(PyObject *o, const at::Tensor *&t)
 {
@@ -220,7 +230,7 @@ PyObject *linear(PyObject *, PyObject *args)
         const at::Tensor *t[6];
         for (int i = 0; i < 6; ++i)
             if (!plain(po[i], t[i])) return none();
-        if (!t[0] || !t[1] || !t[2] || act < 0) return none();
+        if (!t[0] || !t[1] || !t[2] || act < 0 || wants_graph({t[0], t[2], t[3], t[4], t[5]})) return none();
         const at::Tensor &x = *t[0];
         const at::Device d = x.device();
         const auto type = x.scalar_type();
@@ -290,7 +300,7 @@ PyObject *linear_backward(PyObject *, PyObject *args)
         const at::Tensor *t[8];
         for (int i = 0; i < 8; ++i)
             if (!plain(po[i], t[i])) return none();
-        if (!t[0] || !t[1] || !t[2] || act < 0) return none();
+        if (!t[0] || !t[1] || !t[2] || act < 0 || wants_graph({t[0]})) return none();
         const at::Tensor &dy = *t[0];
         const at::Device d = dy.device();
         if (!d.is_cuda() || d.index() != device || dy.scalar_type() != at::kBFloat16 || cin < 1 || cin > kMostRows) return none();

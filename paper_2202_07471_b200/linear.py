@@ -5,6 +5,10 @@ Activations are bfloat16 or float16 tensors [..., features]; leading dimensions 
 what squant_quantize_layer / squant_quantize_model wrote for a layer of weights [cout, cin]: int8 codes [cout, cin], or
 [cout, ceil(cin / 2)] with pack_int4.  Outputs are allocated from PyTorch's caching allocator on the current stream, or on
 `stream` where one is given.
+
+None of the calls is recorded by autograd.  squant_linear refuses inputs that require a gradient where one would be recorded (grad mode on), and
+squant_linear_backward a dy that does; a torch.autograd.Function around the calls, in whose forward and backward grad mode is off, makes
+them part of a graph.
 """
 from __future__ import annotations
 
@@ -146,6 +150,12 @@ class _On:
             g.__exit__(*exc)
 
 
+def _no_graph(what: str, *inputs: Optional[torch.Tensor]) -> None:
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
+        raise ValueError(f"{what} is not recorded by autograd: call it under torch.no_grad(), or from the forward and backward of a torch.autograd.Function, "
+                         "with squant_linear_backward for the gradients")
+
+
 def _rows(t: torch.Tensor, what: str) -> torch.Tensor:
     """[..., features] as [tokens, features] without a copy."""
     if t.dim() == 0 or t.shape[-1] == 0:
@@ -212,7 +222,7 @@ def _run(fn, need, args, handle, device: torch.device) -> None:
 
 def squant_checkpoint(x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> Checkpoint:
     """An activation (bfloat16 [..., features]) in 8 bits: 33/64 of its bytes, at most half a step of the largest of 32
-    neighbours off (2^-7 of its power of two)."""
+    neighbours off (2^-7 of its power of two).  The checkpoint and what is restored from it carry no gradient."""
     native = None if stream is not None else _native()
     if native is not None:
         device = _device()
@@ -260,6 +270,7 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
         if got is not None:
             got = _result(got)
             return (got[0], Checkpoint(got[1], got[2], codes.shape[0])) if checkpoint else got
+    _no_graph("squant_linear", x, scales, bias, residual, out)
     device = x.device
     with _On(device, stream) as handle:
         if x.dtype not in _TYPES:
@@ -304,6 +315,7 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
                                          x and x.exps, width, ACTIVATIONS.get(act, -1), pack_int4, dx, dweight, dbias, dscales)
             if got is not None:
                 return LinearGrads(*_result(got))
+    _no_graph("squant_linear_backward", dy)
     device = dy.device
     with _On(device, stream) as handle:
         if dy.dtype != torch.bfloat16:

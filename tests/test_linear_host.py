@@ -149,3 +149,20 @@ def test_the_extension_has_the_library_s_structs():
     if m is None:
         pytest.skip("the descriptor extension is not built")
     assert m.linear_bytes == ctypes.sizeof(linear.LinearArgs) and m.linear_grad_bytes == ctypes.sizeof(linear.LinearGradArgs)
+
+
+def test_inputs_that_require_a_gradient_are_refused():
+    """The calls are not recorded by autograd: a loss on their results would train nothing that lies before them."""
+    x, codes, scales = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(32, 64, dtype=torch.int8), torch.ones(32)
+    bias, res, dy = torch.zeros(32), torch.zeros(2, 32, dtype=torch.bfloat16), torch.zeros(2, 32, dtype=torch.bfloat16)
+    for t in (x, scales, bias, res):
+        t.requires_grad_()
+        with pytest.raises(ValueError, match="autograd"):
+            sq.squant_linear(x, codes, scales, bias, residual=res)
+        with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):   # goes on to the next check
+            sq.squant_linear(x, codes, scales, bias, residual=res)
+        t.requires_grad_(False)
+    with pytest.raises(ValueError, match="autograd"):
+        sq.squant_linear(x, codes, scales, out=res.requires_grad_())
+    with pytest.raises(ValueError, match="autograd"):
+        sq.squant_linear_backward(dy.requires_grad_(), codes, scales)
