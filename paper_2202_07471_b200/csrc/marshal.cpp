@@ -275,6 +275,7 @@ PyObject *linear(PyObject *, PyObject *args)
         }
         const int rc = s_lib.linear(&a, stream_of(stream));
         if (rc != SQUANT_OK) return PyLong_FromLong(rc);
+        if (t[5] && !y.is_inference()) y.unsafeGetTensorImpl()->bump_version();   // written in place, as autograd has to know
         if (!save) {
             if (!t[5]) return THPVariable_Wrap(y);
             Py_INCREF(po[5]);

@@ -271,6 +271,7 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
             got = _result(got)
             return (got[0], Checkpoint(got[1], got[2], codes.shape[0])) if checkpoint else got
     _no_graph("squant_linear", x, scales, bias, residual, out)
+    written = out
     device = x.device
     with _On(device, stream) as handle:
         if x.dtype not in _TYPES:
@@ -294,6 +295,8 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
                        CheckpointData(_ptr(z.codes), _ptr(z.exps)) if z else CheckpointData(None, None), None, 0)
         lib = _lib()
         _run(lib.squant_linear, lib.squant_linear_workspace, a, handle, device)
+    if written is not None and not written.is_inference():
+        torch.autograd.graph.increment_version(written)
     return (out, z) if checkpoint else out
 
 

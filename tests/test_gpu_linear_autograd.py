@@ -50,6 +50,26 @@ def test_inputs_that_require_a_gradient_are_refused(path):
     assert g.dx.shape == x.shape and not g.dx.requires_grad
 
 
+def test_a_written_tensor_s_version(path):
+    """Autograd must see that `out` has changed: a product that has kept it refuses its backward pass."""
+    x, codes, scales, bias, res = _inputs()
+    out = torch.ones_like(res)
+    view = out[:, :16]
+    weight = torch.ones_like(res, requires_grad=True)
+    loss = (weight * out).sum()
+    before = out._version
+    assert sq.squant_linear(x, codes, scales, bias, out=out) is out
+    assert out._version > before and view._version == out._version
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    before = out._version
+    sq.squant_linear(x, codes, scales, bias)
+    assert out._version == before
+    with torch.inference_mode():   # such tensors have no version
+        got = sq.squant_linear(x, codes, scales, bias, out=torch.empty_like(res))
+        assert got.is_inference() and same_bits(got, out)
+
+
 class Layer(torch.autograd.Function):
     """A layer whose codes stand for `weight` (a gradient for the weights) and whose activations are kept in 8 bits."""
 
