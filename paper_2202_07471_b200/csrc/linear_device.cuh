@@ -310,8 +310,9 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Tries of a wait: 0.2 s.  The longest wait that goes well is for a tile's sums, at most kLongestSum terms of a contraction: below a millisecond.
-constexpr int kWaitLimit = 1 << 22;
+// Tries of a wait.  The hardware parks a try for 4 us before it fails (4,096 tries: 16.5 ms), so that a wait gives up after a second.  The longest
+// one that goes well is for a tile's sums, at most kLongestSum terms of a contraction: below a millisecond.
+constexpr int kWaitLimit = 1 << 18;
 
 // False when the wait ran out or another thread of the block gave up (*gave_up is shared by the block).
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
@@ -330,10 +331,10 @@ __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, vol
 {
     return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up));
 }
-// The wait for one's own copies after the block has given up: bounded, without a look at the flag.
+// The wait for one's own copies after the block has given up: bounded (16 ms), without a look at the flag.
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity)
 {
-    for (int i = 0; i < (1 << 16); ++i)
+    for (int i = 0; i < (1 << 12); ++i)
         if (bar_try(bar, parity)) return;
 }
 

@@ -90,8 +90,8 @@ def test_sums_of_one_sign_keep_their_value():
         assert ((y.double() - want[:len(rows)]).abs() <= (HALF + CUT + 16 * 2.0 ** -24) * want[:len(rows)]).all()
 
 
-def test_a_contraction_that_outlasts_a_wait():
-    """2^27 tokens of a layer of one tile: a third of a second, more than a kernel waits for one copy or one sum."""
+def test_a_contraction_of_many_parts():
+    """2^27 tokens of a layer of one tile: a third of a second."""
     if torch.cuda.mem_get_info()[0] < 60 << 30:
         pytest.skip("needs 60 GB")
     base, times = 1 << 17, 1 << 10
