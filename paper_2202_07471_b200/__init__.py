@@ -8,7 +8,8 @@ from .binding import (FLAG_NARROW_RANGE, FLAG_PACK_INT4, NOALLOC_MAX_CTAS, MODE_
                       squant_plan_info, squant_plan_kernels, squant_quantize_layer, squant_quantize_layer_noalloc,
                       squant_quantize_model,
                       squant_quantize_model_host, squant_selfcheck_division, squant_shutdown,
-                      squant_debug_set_status, squant_debug_wait_expires, squant_debug_violations, squant_debug_sums_checked, use_library)
+                      squant_debug_set_status, squant_debug_wait_expires, squant_debug_violations, squant_debug_sums_checked, squant_debug_linear_wait_expires, squant_debug_linear_wait_limit,
+                      use_library)
 from .linear import (Checkpoint, LinearGrads, squant_checkpoint, squant_checkpoint_restore, squant_linear, squant_linear_backward)
 
 __all__ = ["FLAG_NARROW_RANGE", "FLAG_PACK_INT4", "NOALLOC_MAX_CTAS", "MODE_C", "MODE_E", "MODE_EKC", "MODE_K", "LayerBuffers",
@@ -16,5 +17,6 @@ __all__ = ["FLAG_NARROW_RANGE", "FLAG_PACK_INT4", "NOALLOC_MAX_CTAS", "MODE_C", 
            "squant_plan_info", "squant_plan_kernels", "squant_quantize_layer", "squant_quantize_layer_noalloc",
            "squant_quantize_model",
            "squant_quantize_model_host", "squant_selfcheck_division", "squant_shutdown",
-           "squant_debug_set_status", "squant_debug_wait_expires", "squant_debug_violations", "squant_debug_sums_checked", "use_library",
+           "squant_debug_set_status", "squant_debug_wait_expires", "squant_debug_violations", "squant_debug_sums_checked", "squant_debug_linear_wait_expires",
+           "squant_debug_linear_wait_limit", "use_library",
            "Checkpoint", "LinearGrads", "squant_checkpoint", "squant_checkpoint_restore", "squant_linear", "squant_linear_backward"]

@@ -31,7 +31,7 @@ EXPORTS = ("squant_quantize_layer", "squant_quantize_layer_noalloc", "squant_qua
            "squant_plan_info", "squant_plan_kernels", "squant_selfcheck_division", "squant_device_status", "squant_launch_count", "squant_strerror", "squant_last_cuda_error",
            "squant_shutdown", "squant_debug_set_status", "squant_debug_wait_expires", "squant_debug_violations",
            "squant_debug_sums_checked", "squant_checkpoint", "squant_checkpoint_restore", "squant_linear_workspace", "squant_linear",
-           "squant_linear_backward_workspace", "squant_linear_backward")
+           "squant_linear_backward_workspace", "squant_linear_backward", "squant_debug_linear_wait_expires", "squant_debug_linear_wait_limit")
 
 
 class SquantError(RuntimeError):
@@ -92,6 +92,10 @@ def load_library() -> ctypes.CDLL:
     lib.squant_debug_set_status.restype = ctypes.c_int
     lib.squant_debug_wait_expires.argtypes = [ctypes.c_int32, vp]
     lib.squant_debug_wait_expires.restype = ctypes.c_int
+    lib.squant_debug_linear_wait_expires.argtypes = [ctypes.c_int32, vp]
+    lib.squant_debug_linear_wait_limit.argtypes = [ctypes.c_int32]
+    for f in ("squant_debug_linear_wait_expires", "squant_debug_linear_wait_limit"):
+        getattr(lib, f).restype = ctypes.c_int
     lib.squant_launch_count.restype = ctypes.c_int64
     lib.squant_strerror.restype = ctypes.c_char_p
     lib.squant_strerror.argtypes = [ctypes.c_int]
@@ -338,6 +342,19 @@ def squant_debug_set_status(value: int) -> None:
 def squant_debug_wait_expires(max_polls: int = 64, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Test hook: one warp waits (at most max_polls polls) on a barrier nobody arrives at."""
     _check(load_library().squant_debug_wait_expires(int(max_polls), _stream_handle(stream)))
+
+
+def squant_debug_linear_wait_expires(max_tries: int = 64, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Test hook: one thread waits as the linear operators' kernels do (at most max_tries tries) on a barrier nobody arrives at."""
+    _check(load_library().squant_debug_linear_wait_expires(int(max_tries), _stream_handle(stream)))
+
+
+def squant_debug_linear_wait_limit(tries: int = -1) -> bool:
+    """Test hook: the limit of the linear operators' waits in the checked build (-1: the regular one, 0: they give up at once); False in the regular build."""
+    rc = int(load_library().squant_debug_linear_wait_limit(int(tries)))
+    if rc < 0:
+        _check(rc)
+    return rc == 1
 
 
 def squant_launch_count() -> int:

@@ -587,6 +587,25 @@ int squant_checkpoint_restore(const squant_checkpoint_data *from, int64_t rows, 
     return restore(*from, rows, features, out, stride, static_cast<cudaStream_t>(cuda_stream));
 }
 
+int squant_debug_linear_wait_expires(int32_t max_tries, void *cuda_stream)
+{
+    if (max_tries < 1 || max_tries > 4096) return SQUANT_ERR_SHAPE;
+    return launch(sq::wait_kernel, dim3(1), dim3(1), 32, 0, static_cast<cudaStream_t>(cuda_stream), max_tries);
+}
+
+int squant_debug_linear_wait_limit(int32_t tries)
+{
+    if (tries < -1 || tries > sq::kWaitLimit) return SQUANT_ERR_SHAPE;
+#ifdef SQUANT_DEBUG_BOUNDS
+    const int limit = tries < 0 ? sq::kWaitLimit : tries;
+    SQ_CUDA(cudaDeviceSynchronize());
+    SQ_CUDA(cudaMemcpyToSymbol(sq::g_wait_limit, &limit, sizeof(int)));
+    return 1;   // this library was built with the checks
+#else
+    return SQUANT_OK;
+#endif
+}
+
 int64_t squant_linear_workspace(const squant_linear_args *args)
 {
     if (int rc = check(args)) return rc;

@@ -196,6 +196,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         }
     }
     __syncwarp();
+    if (*gave_up) __nanosleep(100000);   // nobody has waited for the last signal of a tile's sums: it is here by then
     tc_fence_before();
     __syncthreads();
     cluster_arrive_wait();   // the other block reads this one's shared memory and signals its barriers until here

@@ -313,12 +313,17 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 // Tries of a wait.  The hardware parks a try for 4 us before it fails (4,096 tries: 16.5 ms), so that a wait gives up after a second.  The longest
 // one that goes well is for a tile's sums, at most kLongestSum terms of a contraction: below a millisecond.
 constexpr int kWaitLimit = 1 << 18;
+#ifdef SQUANT_DEBUG_BOUNDS
+static __device__ int g_wait_limit = kWaitLimit;   // tests of the checked build shorten it
+__device__ __forceinline__ int wait_limit() { return *const_cast<volatile int *>(&g_wait_limit); }
+#else
+__device__ __forceinline__ int wait_limit() { return kWaitLimit; }
+#endif
 
 // False when the wait ran out or another thread of the block gave up (*gave_up is shared by the block).
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, int limit = wait_limit())
 {
-    if (bar_try(bar, parity)) return true;
-    for (int i = 0; i < kWaitLimit; ++i) {
+    for (int i = 0; i < limit; ++i) {
         if (bar_try(bar, parity)) return true;
         if (*gave_up) return false;
     }
@@ -330,6 +335,18 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
 __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *gave_up)
 {
     return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up));
+}
+// A wait on its own, at a barrier that nobody arrives at.
+static __global__ void wait_kernel(int limit)
+{
+    __shared__ uint64_t bar;
+    __shared__ int gave_up;
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        bar_init(smem_addr(&bar), 1);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) bar_wait(smem_addr(&bar), 0, &gave_up, limit);
 }
 // The wait for one's own copies after the block has given up: bounded (16 ms), without a look at the flag.
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity)
