@@ -301,6 +301,15 @@ typedef struct squant_linear_args {
 /* Bytes of workspace the call with these arguments needs, or a negative error: up to 256 tokens 0 unless rows of x or of the codes start
  * off 16 bytes, beyond that (and for cin above 524,288) the codes as 16-bit floats, and fp32 sums of y's shape for cin above 65,536. */
 int64_t squant_linear_workspace(const squant_linear_args *args);
+/*
+ * Which kernel makes the product of a call with these arguments on a B200: 0 (no tokens), one of the values below, or the call's negative error.  No
+ * GPU is needed and nothing is read through the pointers, but their alignment and which of them are NULL count.  For tests and tools.
+ */
+#define SQUANT_LINEAR_FEW 1        /* few tokens: warps share the contraction */
+#define SQUANT_LINEAR_FUSED 2      /* up to 256 tokens: codes are converted on the way to the tensor cores */
+#define SQUANT_LINEAR_DENSE 3      /* codes are expanded first; tiles of 256 x 128 */
+#define SQUANT_LINEAR_DENSE_WIDE 4 /* the same, tiles of 256 x 256 */
+int squant_linear_plan(const squant_linear_args *args);
 int squant_linear(const squant_linear_args *args, void *cuda_stream);
 
 /*

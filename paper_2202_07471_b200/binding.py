@@ -30,7 +30,7 @@ NOALLOC_MAX_CTAS = 32768
 EXPORTS = ("squant_quantize_layer", "squant_quantize_layer_noalloc", "squant_quantize_model", "squant_quantize_model_host",
            "squant_plan_info", "squant_plan_kernels", "squant_selfcheck_division", "squant_device_status", "squant_launch_count", "squant_strerror", "squant_last_cuda_error",
            "squant_shutdown", "squant_debug_set_status", "squant_debug_wait_expires", "squant_debug_violations",
-           "squant_debug_sums_checked", "squant_checkpoint", "squant_checkpoint_restore", "squant_linear_workspace", "squant_linear",
+           "squant_debug_sums_checked", "squant_checkpoint", "squant_checkpoint_restore", "squant_linear_workspace", "squant_linear_plan", "squant_linear",
            "squant_linear_backward_workspace", "squant_linear_backward", "squant_debug_linear_wait_expires", "squant_debug_linear_wait_limit")
 
 

@@ -17,6 +17,7 @@
 namespace {
 
 constexpr int kMaxDevices = 64;
+constexpr int kB200Sms = 148;   // for squant_linear_plan
 constexpr int64_t kMaxRows = 1ll << 30;
 // Up to as many tokens fused_kernel turns the codes into floats on the way to the tensor cores; beyond, they are expanded once.
 // 4096 -> 4096 int4, fused and expanded: 256 tokens 16.9 and 21.3 us, 384 tokens 33 and 21.5; 4096 -> 11008 256 tokens 43 and 49.
@@ -169,16 +170,20 @@ int launch_dense(const CUtensorMap &map_a, const CUtensorMap &map_b, sq::GemmArg
 // Bytes of the sums that the parts of a long contraction hand on.
 int64_t sums_bytes(int64_t rows, int64_t cols, int64_t depth) { return depth > sq::kLongestSum ? rows * up(cols, 32) * 4 : 0; }
 
-// The product of two 16-bit matrices: `a` as gemm's 16-bit operand, `b` [cols][depth] (forward) or [depth][cols].  Tiles of
-// 256 or 128 columns, whichever is done in fewer waves; a wave of narrow tiles takes about 0.6 of one of wide tiles.
+// Tiles of 256 or 128 columns, whichever is done in fewer waves; a wave of narrow tiles takes about 0.6 of one of wide tiles.
+bool wide_tiles(int64_t rows, int64_t cols, int64_t sms)
+{
+    const int64_t row_tiles = (rows + sq::kPairRows - 1) / sq::kPairRows, pairs = sms / 2;
+    const int64_t wide = (row_tiles * ((cols + 255) / 256) + pairs - 1) / pairs, narrow = (row_tiles * ((cols + 127) / 128) + pairs - 1) / pairs;
+    return 10 * wide <= 6 * narrow;
+}
+
+// The product of two 16-bit matrices: `a` as gemm's 16-bit operand, `b` [cols][depth] (forward) or [depth][cols].
 // sums: sums_bytes() of workspace.
 template <int kMode, bool kHalf>
 int dense(const void *a, int64_t a_stride, const void *b, int64_t b_stride, sq::GemmArgs g, void *sums, int device, int sms, cudaStream_t stream)
 {
-    const int64_t row_tiles = (static_cast<int64_t>(g.rows) + sq::kPairRows - 1) / sq::kPairRows, pairs = sms / 2;
-    const int64_t wide = (row_tiles * ((static_cast<int64_t>(g.cols) + 255) / 256) + pairs - 1) / pairs;
-    const int64_t narrow = (row_tiles * ((static_cast<int64_t>(g.cols) + 127) / 128) + pairs - 1) / pairs;
-    const bool use_wide = 10 * wide <= 6 * narrow;
+    const bool use_wide = wide_tiles(g.rows, g.cols, sms);
     CUtensorMap map_a, map_b;
     if (int rc = kMode == sq::kWeightGrad ? matrix_map(map_a, a, g.depth, g.rows, a_stride, kHalf, sq::kTileDepth)
                                           : matrix_map(map_a, a, g.rows, g.depth, a_stride, kHalf, 128)) return rc;
@@ -610,6 +615,16 @@ int64_t squant_linear_workspace(const squant_linear_args *args)
 {
     if (int rc = check(args)) return rc;
     return forward_plan(*args).bytes;
+}
+
+int squant_linear_plan(const squant_linear_args *args)
+{
+    if (int rc = check(args)) return rc;
+    const squant_linear_args &a = *args;
+    if (a.tokens == 0) return 0;
+    if (few(a)) return SQUANT_LINEAR_FEW;
+    if (!forward_plan(a).dense) return SQUANT_LINEAR_FUSED;
+    return wide_tiles(a.tokens, a.cout, kB200Sms) ? SQUANT_LINEAR_DENSE_WIDE : SQUANT_LINEAR_DENSE;
 }
 
 int squant_linear(const squant_linear_args *args, void *cuda_stream)

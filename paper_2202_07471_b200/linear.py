@@ -81,9 +81,10 @@ def _lib() -> ctypes.CDLL:
         lib.squant_checkpoint_restore.argtypes = [ck, i64, ctypes.c_int32, vp, i64, vp]
         lib.squant_linear.argtypes = [ctypes.POINTER(LinearArgs), vp]
         lib.squant_linear_workspace.argtypes = [ctypes.POINTER(LinearArgs)]
+        lib.squant_linear_plan.argtypes = [ctypes.POINTER(LinearArgs)]
         lib.squant_linear_backward.argtypes = [ctypes.POINTER(LinearGradArgs), vp]
         lib.squant_linear_backward_workspace.argtypes = [ctypes.POINTER(LinearGradArgs)]
-        for f in ("squant_checkpoint", "squant_checkpoint_restore", "squant_linear", "squant_linear_backward"):
+        for f in ("squant_checkpoint", "squant_checkpoint_restore", "squant_linear", "squant_linear_plan", "squant_linear_backward"):
             getattr(lib, f).restype = ctypes.c_int
         for f in ("squant_linear_workspace", "squant_linear_backward_workspace"):
             getattr(lib, f).restype = i64

@@ -132,6 +132,21 @@ def test_workspace_of_long_contractions():
     assert need(tokens=k + 1, cout=k + 8, dy_stride=k + 8, dweight=OK_PTR, dweight_stride=64, x=CK) == (k + 1) * (k + 8) * 2 + (k + 8) * 64 * 2 + (k + 8) * 64 * 4
 
 
+FEW, FUSED, DENSE, WIDE = 1, 2, 3, 4
+
+
+@pytest.mark.parametrize("kw,kernel", [
+    ({"tokens": 0}, 0), ({"tokens": 1}, FEW), ({"tokens": 8}, FEW), ({"tokens": 9}, FEW), ({"tokens": 256}, FEW), ({"tokens": 257}, DENSE),
+    ({"tokens": 8, "z": CK}, FUSED), ({"tokens": 256, "z": CK}, FUSED), ({"tokens": 257, "z": CK}, DENSE), ({"tokens": 9, "x": OK_PTR + 2}, FUSED),
+    ({"tokens": 9, "x": OK_PTR + 16}, FUSED), ({"tokens": 9, "x_stride": 72}, FUSED), ({"tokens": 9, "cin": 61, "x_stride": 61}, FUSED),
+    ({"tokens": 16, "cin": 4096, "x_stride": 4096, "cout": 12288, "y_stride": 12288}, FEW), ({"tokens": 16, "cin": 4096, "x_stride": 4096, "cout": 12289, "y_stride": 12289}, FUSED),
+    ({"tokens": 2100, "cout": 1700, "y_stride": 1700}, WIDE), ({"tokens": 2100, "cout": 2100, "y_stride": 2100}, DENSE),
+    ({"tokens": 5, "cin": 1 << 19, "x_stride": 1 << 19}, FEW), ({"tokens": 5, "cin": (1 << 19) + 16, "x_stride": (1 << 19) + 16}, DENSE),
+    ({"tokens": -1}, -2), ({"x": None}, -1), ({"act": 9}, -4), ({"x": ODD_PTR}, -5)])
+def test_which_kernel_a_call_takes(kw, kernel):
+    assert linear._lib().squant_linear_plan(ctypes.byref(forward(**kw))) == kernel
+
+
 def test_tensors_have_to_be_on_a_gpu():
     x, codes, scales = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(32, 64, dtype=torch.int8), torch.ones(32)
     with pytest.raises(ValueError, match="CUDA"):
