@@ -321,6 +321,13 @@ int squant_linear(const squant_linear_args *args, void *cuda_stream);
  *   dx = (dz * s) C,  dweight = dz^T xhat   - the gradient of the weights the codes stand for, which a training loop hands
  *                                             on to the weights it quantizes
  *
+ * How near that is to the layer's own gradients: what reads zhat sees z to half a step 2^(E-127) of the largest of 32 neighbouring channels.  act'(zhat) of
+ * channels far smaller than that is act' near 0 (relu: the sign of zhat and z differ for 0.5 % of the values of channels of one size, for 3.5 % where
+ * sizes spread as exp(N(0, 1))), and dscales divides the step by the channel's own scale (which must not be 0): against sum dz (x C^T) it is
+ * 0.9 % off (2-norm, 512 tokens, 256 channels) for channels of one size, 8 to 20 % where sizes spread as exp(N(0, 1)), 60 % as exp(2 N(0, 1)), and more
+ * where biases are large next to a channel's own values.  The sum over k of dweight[m][k] * codes[m][k] is the same gradient from the input, without that
+ * division: 0.9 % off at any spread with act NONE.  Take it wherever the channels of a group of 32 may differ by more than a few times.
+ *
  * dz and dz * s are rounded to bf16 for the tensor cores; their sums, dbias and dscales are fp32 and taken before that rounding.
  * The residual's gradient is dy.  Results repeat to the bit.
  */
@@ -331,7 +338,7 @@ typedef struct squant_linear_grad_args {
     const void *dy;          /* in : [tokens][cout] bf16 */
     int64_t dy_stride;
     const int8_t *codes;     /* in : as above; needed for dx */
-    const float *scales;     /* in : needed for dx and dscales */
+    const float *scales;     /* in : needed for dx and dscales, not 0 there */
     const float *bias;       /* in, may be NULL: of the forward pass; used for dscales */
     squant_checkpoint_data z; /* in : [tokens][cout]; needed with an activation and for dscales */
     squant_checkpoint_data x; /* in : [tokens][cin]; needed for dweight */

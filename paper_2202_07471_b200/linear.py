@@ -309,7 +309,12 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
 
     z: checkpoint of the pre-activation (needed with an activation and for dscales); x: checkpoint of the input (needed
     for dweight); cin is needed with pack_int4, whose rows do not tell it.  dweight is the gradient of the weights
-    codes * scales: a training loop applies it to the weights that it quantizes."""
+    codes * scales: a training loop applies it to the weights that it quantizes.
+
+    dscales divides (z's checkpoint - bias) by the scales, which must not be 0, and with it the checkpoint's step, which the largest of 32 neighbouring channels
+    sets: 0.9 % off the layer's own gradient for channels of one size, 8 to 20 % where their sizes spread as exp(N(0, 1)), of no use where some are
+    tens of times smaller than their neighbours.  There, ask for dweight and take (dweight.float() * codes).sum(1): the same gradient from the input,
+    0.9 % off at any spread without an activation (its slope is read from z's checkpoint too)."""
     native = None if stream is not None else _native()
     if native is not None and dy.dim() and (z is None or z.features == dy.shape[-1]) and not (cin is None and pack_int4):
         device = _device()
