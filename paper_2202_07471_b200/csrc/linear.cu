@@ -22,7 +22,13 @@ constexpr int64_t kMaxRows = 1ll << 30;
 // Up to as many tokens fused_kernel turns the codes into floats on the way to the tensor cores; beyond, they are expanded once.
 // 4096 -> 4096 int4, fused and expanded: 256 tokens 16.9 and 21.3 us, 384 tokens 33 and 21.5; 4096 -> 11008 256 tokens 43 and 49.
 constexpr int kFusedTokens = 256;
-// Up to eight tokens few_kernel is faster for every size.  Beyond, it reads all of x once for 16 channels, and from 33 tokens on the codes for
+// Up to eight tokens few_kernel is faster for every size whose rows of x and codes start on 16 bytes.  Others it reads in small pieces, which costs more than to
+// copy them for fused_kernel beyond this many codes, fewer than 4096 channels counted as that (few_kernel and copy with fused_kernel, 1 and 8 tokens, us:
+// x off 16 bytes 512 -> 1000 int4 3.0 3.7 and 6.3 7.3; 2048 -> 4096 int4 6.1 9.6 and 10.2 10.9, int8 9.9 12.7 and 10.9 11.6; 4096 -> 4096 int4 11.7 17.7 and
+// 12.5 12.7, int8 17.3 22.5 and 13.0 13.3; 8192 -> 16384 int8 96 151 and 37 38; 16384 -> 256 int4 24 34 and 14.5 14.5; codes too 2049 -> 4096 int8 10.8 11.7
+// and 14.2 14.2, 4097 -> 4096 int8 18.3 20.0 and 18.0 18.0, 4097 -> 11008 int8 35 39 and 30 31).
+constexpr int64_t kFewOddCodes = 1ll << 23;
+// Beyond eight tokens, it reads all of x once for 16 channels, and from 33 tokens on the codes for
 // 32 tokens anew, so that its time grows with tokens times codes while fused_kernel starts at 6 to 10 us: the lines are drawn at this many
 // codes times tiles of eight tokens, a contraction of less than 2048 counted as that (a block's warps do not all have work) and fewer than
 // 4096 channels, all blocks of tokens together, as that (the GPU is not full).  int4, few and fused: 16 tokens 512 -> 1000 2.3 and 5.7 us, 4096 -> 4096 6.2 and 10.6, 4096 -> 11008
@@ -343,7 +349,7 @@ int64_t few_blocks(int64_t tokens) { return (tokens + 4 * sq::kFewTokens - 1) / 
 bool few(const squant_linear_args &a)
 {
     if (a.z.codes || a.tokens > kFusedTokens || a.cin > kLongestFused) return false;
-    if (a.tokens <= sq::kFewTokens) return true;
+    if (a.tokens <= sq::kFewTokens) return few_align(a) || a.cin * std::max<int64_t>(a.cout, 4096) <= kFewOddCodes;
     const int64_t blocks = few_blocks(a.tokens), tiles = a.tokens > 2 * sq::kFewTokens ? 4 : 2;
     const int64_t codes = std::max<int64_t>(a.cin, 2048) * std::max<int64_t>(a.cout * blocks, 4096);
     return codes * tiles <= (blocks > 1 ? kFewWorkBeyond32 : kFewWork) && few_align(a) == 32;

@@ -66,6 +66,22 @@ def test_activations(kernel, tokens, cin, cout, pad, save, dtype, bits, act):
             assert cout % 32 == 0 or (z8.codes[:, cout:] == 0).all()
 
 
+# up to eight tokens whose rows start anywhere, either side of the line for them
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("kernel,tokens,cin,cout,pad", [(FEW, 8, 2048, 4096, 1), (FUSED, 2, 2056, 4096, 1), (FUSED, 8, 2049, 4100, 0), (FUSED, 3, 16384, 40, 3), (FEW, 5, 2047, 70, 0)])
+def test_few_tokens_of_rows_that_start_anywhere(kernel, tokens, cin, cout, pad, bits):
+    codes, scales = int_layer(cin, cout, bits, 1)
+    stored = pack(codes) if bits == 4 else codes
+    x, _ = padded(torch.randint(-3, 4, (tokens, cin), generator=gen(2), device="cuda").bfloat16(), pad)
+    assert _kernel(x, stored, cout, False) == kernel
+    want = ((x.double() @ codes.double().T) * scales.double()).to(torch.bfloat16)
+    n = sq.squant_launch_count()
+    assert same_bits(sq.squant_linear(x, stored, scales, pack_int4=bits == 4) + 0.0, want + 0.0)
+    assert sq.squant_launch_count() == n + (1 if kernel == FEW else 2)
+    one = x[1:2]   # a row that starts off 16 bytes, alone
+    assert same_bits(sq.squant_linear(one, stored, scales, pack_int4=bits == 4) + 0.0, want[1:2] + 0.0)
+
+
 @pytest.mark.parametrize("kernel,tokens,cin,cout", [(FUSED, 9, 64, 33), (FUSED, 256, 128, 257), (DENSE, 257, 100, 33), (DENSE, 300, 128, 200), (DENSE, 513, 64, 1001),
                                                     (WIDE, 2100, 72, 1700), (WIDE, 2100, 72, 1663)])
 def test_checkpoints_of_integers_are_exact(kernel, tokens, cin, cout):

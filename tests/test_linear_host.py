@@ -142,6 +142,11 @@ FEW, FUSED, DENSE, WIDE = 1, 2, 3, 4
     ({"tokens": 16, "cin": 4096, "x_stride": 4096, "cout": 12288, "y_stride": 12288}, FEW), ({"tokens": 16, "cin": 4096, "x_stride": 4096, "cout": 12289, "y_stride": 12289}, FUSED),
     ({"tokens": 2100, "cout": 1700, "y_stride": 1700}, WIDE), ({"tokens": 2100, "cout": 2100, "y_stride": 2100}, DENSE),
     ({"tokens": 5, "cin": 1 << 19, "x_stride": 1 << 19}, FEW), ({"tokens": 5, "cin": (1 << 19) + 16, "x_stride": (1 << 19) + 16}, DENSE),
+    # up to eight tokens: rows of x, of the codes or both off 16 bytes, either side of the line for them
+    ({"tokens": 8, "cin": 4096, "x_stride": 4096, "cout": 4096, "y_stride": 4096}, FEW), ({"tokens": 8, "cin": 4096, "x_stride": 4104, "cout": 4096, "y_stride": 4096}, FEW),
+    ({"tokens": 8, "cin": 2048, "x_stride": 2049, "cout": 4096, "y_stride": 4096}, FEW), ({"tokens": 8, "cin": 2049, "x_stride": 2049, "cout": 4096, "y_stride": 4096}, FUSED),
+    ({"tokens": 1, "cin": 4096, "x_stride": 4097, "cout": 4096, "y_stride": 4096}, FEW), ({"tokens": 2, "cin": 4096, "x_stride": 4097, "cout": 4096, "y_stride": 4096}, FUSED),
+    ({"tokens": 1, "x": OK_PTR + 2, "cin": 4096, "x_stride": 4096, "cout": 256, "y_stride": 256}, FUSED), ({"tokens": 1, "x": OK_PTR + 2, "cin": 2000, "x_stride": 2000, "cout": 256, "y_stride": 256}, FEW),
     ({"tokens": -1}, -2), ({"x": None}, -1), ({"act": 9}, -4), ({"x": ODD_PTR}, -5)])
 def test_which_kernel_a_call_takes(kw, kernel):
     assert linear._lib().squant_linear_plan(ctypes.byref(forward(**kw))) == kernel
