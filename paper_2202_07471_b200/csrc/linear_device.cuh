@@ -75,8 +75,9 @@ __device__ __forceinline__ Two mul(Two a, Two b)
 
 // P(N(0, 1) < z) of two values and e = exp(-z^2 / 2).  With a = |z| the upper tail is e times a polynomial in u = 1 / (1 + 0.3 a)
 // without a constant term, since exp(a^2 / 2) P falls like 1 / a.  The coefficients are a weighted least-squares fit of
-// erfcx(a / sqrt 2) / 2 over [0, 14], at most 1.5e-7 of the value off (4.8e-7 in fp32); beyond, the value is no normal fp32 number.
-// gelu and its slope share e, and the tail keeps its relative accuracy, which 1 + erf(z / sqrt 2) would lose.  Two values at a
+// erfcx(a / sqrt 2) / 2 over [0, 14], at most 1.7e-7 of the value off with these coefficients; beyond, the value is no normal fp32 number.
+// The tail is off by that and by what the rounding of -z^2 / 2 and expf's argument makes of e, which grows with it: 9e-7 of itself up to |z| = 4, 2e-6
+// up to 6, 8e-6 up to 13, and expf's own last places; 1 + erf(z / sqrt 2) would keep no digit of it there.  gelu and its slope share e.  Two values at a
 // time take 23 instructions, erfcf() and expf() of both about 180.
 __device__ __forceinline__ void normal_below(float z0, float z1, float &p0, float &p1, float &e0, float &e1)
 {
@@ -99,6 +100,7 @@ __device__ __forceinline__ void normal_below(float z0, float z1, float &p0, floa
     p0 = z0 < 0.0f ? h0 : 1.0f - h0;
     p1 = z1 < 0.0f ? h1 : 1.0f - h1;
 }
+// 0 from z = -87.3 on, where 1 + exp(-z) is more than the division takes and the value less than 1.2e-38.
 __device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
 // act(v) of all values: one branch for all.

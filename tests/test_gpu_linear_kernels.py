@@ -66,6 +66,24 @@ def test_activations(kernel, tokens, cin, cout, pad, save, dtype, bits, act):
             assert cout % 32 == 0 or (z8.codes[:, cout:] == 0).all()
 
 
+@pytest.mark.parametrize("act,lowest", [("gelu", -12.9), ("silu", -87.0)])
+@pytest.mark.parametrize("kernel,tokens,save", [(FEW, 3, False), (FUSED, 40, True), (DENSE, 300, False)])
+def test_tails_of_activations(kernel, tokens, save, act, lowest):
+    """A channel's only product is one times one code of 1 or -1, so that z is the scale or its negative to the bit.  Far down the activation keeps its relative
+    accuracy: half a step of bf16, and 3e-5 for expf of arguments down to -87 (2 + 1.16 * 87 last places, taken twice)."""
+    cout = 1024
+    want_z = torch.linspace(lowest, -lowest, cout, device="cuda")
+    codes = torch.zeros((cout, 32), dtype=torch.int8, device="cuda")
+    codes[:, 5] = torch.sign(want_z).to(torch.int8)
+    x = torch.zeros((tokens, 32), dtype=torch.bfloat16, device="cuda")
+    x[:, 5] = 1
+    assert _kernel(x, codes, cout, save) == kernel
+    y = sq.squant_linear(x, codes, want_z.abs(), act=act, checkpoint=save)
+    exact = act64(want_z.double(), act).expand(tokens, cout)
+    worst = (((y[0] if save else y).double() - exact).abs() / exact.abs()).max().item()
+    assert worst <= 2.0 ** -8 + 3e-5
+
+
 # up to eight tokens whose rows start anywhere, either side of the line for them
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("kernel,tokens,cin,cout,pad", [(FEW, 8, 2048, 4096, 1), (FUSED, 2, 2056, 4096, 1), (FUSED, 8, 2049, 4100, 0), (FUSED, 3, 16384, 40, 3), (FEW, 5, 2047, 70, 0)])
