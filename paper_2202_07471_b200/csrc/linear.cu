@@ -19,22 +19,16 @@ namespace {
 constexpr int kMaxDevices = 64;
 constexpr int kB200Sms = 148;   // for squant_linear_plan
 constexpr int64_t kMaxRows = 1ll << 30;
-// Up to as many tokens fused_kernel turns the codes into floats on the way to the tensor cores; beyond, they are expanded once.
-// 4096 -> 4096 int4, fused and expanded: 256 tokens 16.9 and 21.3 us, 384 tokens 33 and 21.5; 4096 -> 11008 256 tokens 43 and 49.
-constexpr int kFusedTokens = 256;
-// Up to eight tokens few_kernel is faster for every size whose rows of x and codes start on 16 bytes.  Others it reads in small pieces, which costs more than to
-// copy them for fused_kernel beyond this many codes, fewer than 4096 channels counted as that (few_kernel and copy with fused_kernel, 1 and 8 tokens, us:
-// x off 16 bytes 512 -> 1000 int4 3.0 3.7 and 6.3 7.3; 2048 -> 4096 int4 6.1 9.6 and 10.2 10.9, int8 9.9 12.7 and 10.9 11.6; 4096 -> 4096 int4 11.7 17.7 and
-// 12.5 12.7, int8 17.3 22.5 and 13.0 13.3; 8192 -> 16384 int8 96 151 and 37 38; 16384 -> 256 int4 24 34 and 14.5 14.5; codes too 2049 -> 4096 int8 10.8 11.7
-// and 14.2 14.2, 4097 -> 4096 int8 18.3 20.0 and 18.0 18.0, 4097 -> 11008 int8 35 39 and 30 31).
+// Up to as many tokens fused_kernel turns the codes into floats on the way to the tensor cores; beyond, they are expanded once (4096 -> 4096 int4, fused and
+// expanded: 256 tokens 16.9 and 21.3 us, 384 tokens 33 and 21.5).  For narrow results the line would lie higher, since dense_kernel gives a tile's whole
+// contraction to one pair of thread blocks (300 tokens 11008 -> 64 int4 14 and 31 us, 4096 -> 1024 int8 14.5 and 18.4).
+constexpr int kExpandBeyond = 256;
+// few_kernel is faster up to eight tokens.  Its rows of x and codes start on 16 bytes; others it reads in small pieces, which beyond this many codes costs more
+// than to copy them for fused_kernel.  Fewer than 4096 channels count as that: the GPU is not full.
 constexpr int64_t kFewOddCodes = 1ll << 23;
-// Beyond eight tokens, it reads all of x once for 16 channels, and from 33 tokens on the codes for
-// 32 tokens anew, so that its time grows with tokens times codes while fused_kernel starts at 6 to 10 us: the lines are drawn at this many
-// codes times tiles of eight tokens, a contraction of less than 2048 counted as that (a block's warps do not all have work) and fewer than
-// 4096 channels, all blocks of tokens together, as that (the GPU is not full).  int4, few and fused: 16 tokens 512 -> 1000 2.3 and 5.7 us, 4096 -> 4096 6.2 and 10.6, 4096 -> 11008
-// 13.3 and 15.1, 8192 -> 8192 19.4 and 18.8; 32 tokens 4096 -> 4096 10.1 and 11.3, 4096 -> 6144 17.9 and 18.0, 4096 -> 11008 26.5 and 15.9;
-// 64 tokens 512 -> 1000 2.5 and 6.7, 2048 -> 4096 11.2 and 11.3; 96 tokens 2048 -> 4096 15.1 and 12.7; 128 tokens 1024 -> 4096 12.5 and 12.9, 512 -> 4096 8.6
-// and 8.1; 64 tokens 16384 -> 256 19.7 and 14.9; 256 tokens 1024 -> 1024 6.9 and 10.5, 512 -> 4096 15.4 and 9.9.
+// Beyond eight tokens, it reads all of x once for 16 channels, and from 33 tokens on the codes for 32 tokens anew, so that its time grows with tokens
+// times codes while fused_kernel starts at 6 to 10 us: the lines are drawn at this many codes times tiles of eight tokens, a contraction of less than 2048
+// counted as that (a block's warps do not all have work) and fewer than 4096 channels, all blocks of tokens together, as that.
 constexpr int64_t kFewWork = 3ll << 25, kFewWorkBeyond32 = 1ll << 26;
 
 // Contractions that fused_kernel's thread blocks and few_kernel's warps can share so that no sum has more than kLongestSum terms.
@@ -348,7 +342,7 @@ int few_align(const squant_linear_args &a)
 int64_t few_blocks(int64_t tokens) { return (tokens + 4 * sq::kFewTokens - 1) / (4 * sq::kFewTokens); }
 bool few(const squant_linear_args &a)
 {
-    if (a.z.codes || a.tokens > kFusedTokens || a.cin > kLongestFused) return false;
+    if (a.z.codes || a.tokens > kExpandBeyond || a.cin > kLongestFused) return false;
     if (a.tokens <= sq::kFewTokens) return few_align(a) || a.cin * std::max<int64_t>(a.cout, 4096) <= kFewOddCodes;
     const int64_t blocks = few_blocks(a.tokens), tiles = a.tokens > 2 * sq::kFewTokens ? 4 : 2;
     const int64_t codes = std::max<int64_t>(a.cin, 2048) * std::max<int64_t>(a.cout * blocks, 4096);
@@ -366,7 +360,7 @@ struct ForwardPlan {
 ForwardPlan forward_plan(const squant_linear_args &a)
 {
     ForwardPlan p;
-    p.dense = a.tokens > kFusedTokens || a.cin > kLongestFused;
+    p.dense = a.tokens > kExpandBeyond || a.cin > kLongestFused;
     if (few(a)) return p;
     uint8_t *at = static_cast<uint8_t *>(a.workspace);
     if (!rows_on_vectors(a.x, a.x_stride, a.tokens)) p.x = {a.x, a.tokens, 2 * static_cast<int64_t>(a.cin), 2 * (a.tokens > 1 ? a.x_stride : a.cin), at};
@@ -484,7 +478,7 @@ SlopePlan slope_plan(const squant_linear_grad_args &a)
     s.share = std::max<int64_t>(1, (a.tokens + s.shares - 1) / s.shares);
     if (s.shares > 1 && (a.dbias || a.dscales)) s.partial_bytes = up(s.shares * 2 * a.cout * 4, 16);
     s.slope_bytes = (s.dzs + s.dz) * a.tokens * s.pitch * 2 + s.partial_bytes;
-    s.dense = s.dzs && (a.tokens > kFusedTokens || a.cout > kLongestFused);
+    s.dense = s.dzs && (a.tokens > kExpandBeyond || a.cout > kLongestFused);
     const int64_t row = up(a.cin, 8) * 2;
     const int64_t pitch = code_pitch(a.cin, a.flags);
     if (s.dzs && !s.dense && !codes_on_vectors(a.codes, pitch))

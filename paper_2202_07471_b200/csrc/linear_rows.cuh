@@ -212,7 +212,8 @@ constexpr int kSlopeBlocks = 592;   // wanted of a launch: four a multiprocessor
 constexpr int kSlopeLeast = 64;     // tokens of a share
 // A group's exponent leaves its values 255 codes: for the exponents of groups whose largest value is between 2^-2 and 2^6 a block makes
 // tables of gelu' or silu' first (8 KB), if its share is long enough to pay for 2048 of them; they hold what act_slopes gives.
-// 4096 x 4096, sums only, gelu 29 -> 18.5 us; 16384 x 11008 294 -> 161 (42 instructions an element without, which bound it).
+// 4096 x 4096, sums only, gelu 30 -> 18.5 us, silu 26 -> 18.9; 16384 x 11008 290 -> 161 (42 instructions an element without, which bound it).  With every other
+// group off the tables 31.4 and 309: warps take both ways.
 constexpr uint32_t kSlopeTables = 8, kSlopeFirst = 119;
 constexpr int kSlopeTableLeast = 128;   // tokens of a share
 
@@ -233,7 +234,8 @@ __device__ __forceinline__ uint2 load4(const uint16_t *at, int n, bool vector)
 }
 
 // dz = dy * act'(zhat) in bf16, and times the scales; sums over the tokens of dz and of dz * (zhat - bias) / scale in
-// fp32 from the unrounded products.  Thread blocks share the tokens; the sums of their shares go through global memory and are
+// fp32 from the unrounded products.  bf16, since dz and dz * s are the tensor cores' operands: half a step of each term, which makes the gradients' distance
+// from their formulas 0.0024 of their norm instead of the 0.0017 that the rounding of the result alone leaves.  Thread blocks share the tokens; the sums of their shares go through global memory and are
 // added in their order by sums_kernel, so that a call repeats to the bit.  What the kernel needs is loads in flight: four columns a
 // thread keep sums and factors in few registers.  (Eight columns a thread and shares joined by clusters of eight, which allow 264
 // blocks at once, took 34 to 50 us for 4096 x 4096.)
