@@ -396,7 +396,7 @@ int squant_debug_linear_wait_limit(int32_t tries);
 /*
  * The checked build of the library (libsquant_debug.so, compiled with -DSQUANT_DEBUG_BOUNDS; the
  * stand-in for a memory checker on small test cases): its kernels verify the indices they form
- * into shared memory and into the launch table, and the grouped and row kernels take the error sum of
+ * into shared memory and into the launch table (the linear operators': into shared memory, tensor memory and the tensors; sites from 1000 on), and the grouped and row kernels take the error sum of
  * every channel with an absmax scale a second time, from its final codes by plain division (but for
  * depthwise channels, E|C on larger kernels and 1x1 rows of more than 32,768 weights).
  * squant_debug_violations waits for the device, returns the number

@@ -557,6 +557,16 @@ cudaError_t take_linear_status(int *status)
     return e;
 }
 
+cudaError_t take_linear_violations(unsigned *count, int *site)
+{
+    cudaError_t e = cudaMemcpyFromSymbol(count, sq::g_linear_violations, sizeof(unsigned));
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(site, sq::g_linear_site, sizeof(int));
+    const unsigned zero = 0;
+    if (e == cudaSuccess) e = cudaMemcpyToSymbol(sq::g_linear_violations, &zero, sizeof(zero));
+    if (e == cudaSuccess) e = cudaMemcpyToSymbol(sq::g_linear_site, &zero, sizeof(zero));
+    return e;
+}
+
 }  // namespace sq_host
 
 extern "C" {

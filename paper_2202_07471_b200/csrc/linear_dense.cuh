@@ -104,6 +104,9 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const uint32_t tmem = tmem_base;
     const int steps = p.steps;
     const int64_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    SQ_LINEAR_CHECK(bars + 8 * (2 * S::kStages + 4) <= smem_end(smem_raw) && (turns & 3) == 0, 1040);
+    SQ_LINEAR_CHECK(steps >= 1 && static_cast<int64_t>(steps) * kTileDepth <= kLongestSum && p.first_step >= 0 &&
+                    static_cast<int64_t>(p.first_step + steps - 1) * kTileDepth < p.depth, 1041);
 
     if (warp < kDenseEpilogueWarps) {
         const int quarter = warp & 3, part = warp >> 2;
@@ -116,6 +119,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const int64_t col0 = t / p.row_tiles * kCols;
             for (int c = part * (kCols / 2); c < (part + 1) * (kCols / 2); c += 32) {
                 if (col0 + c >= p.cols) break;
+                SQ_LINEAR_CHECK(a * kCols + c + 32 <= S::kTmemCols, 1042);
                 uint32_t acc[32];
                 __syncwarp();
                 tmem_ld32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + a * kCols + c, acc);
@@ -140,6 +144,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     if (rank == 0) bar_expect(full(s), 2 * (S::kBytesA + S::kBytesB));
                     const uint32_t at = smem_a + s * S::kBytesA, bt = smem_b + s * S::kBytesB;
                     const int from = (p.first_step + k) * kTileDepth;
+                    SQ_LINEAR_CHECK(s >= 0 && s < S::kStages && row0 >= 0 && col0 >= 0 && from >= 0 && from < p.depth, 1043);
                     if (kMode == kWeightGrad) {
                         pair_tma_2d(at, &map_a, row0, from, bar);
                         pair_tma_2d(at + 8192, &map_a, row0 + 64, from, bar);

@@ -17,6 +17,22 @@ enum CodeKind { kInt4 = 0, kInt8 = 1 };
 // Set by a kernel of this file's users that gave up a bounded wait (read and cleared by squant_device_status()).
 static __device__ int g_linear_status = 0;
 
+// ---------------------------------------------------------------- checked build
+// Built with -DSQUANT_DEBUG_BOUNDS the kernels check the indices that they form into shared memory, tensor memory and the tensors; a failed check is
+// counted and its site recorded (read and cleared by squant_debug_violations()).  The regular build compiles the checks away.
+static __device__ unsigned g_linear_violations = 0;
+static __device__ int g_linear_site = 0;
+#ifdef SQUANT_DEBUG_BOUNDS
+static __device__ __noinline__ void linear_debug_fail(int site)
+{
+    atomicAdd(&g_linear_violations, 1u);
+    atomicCAS(&g_linear_site, 0, site);
+}
+#define SQ_LINEAR_CHECK(cond, site) do { if (!(cond)) linear_debug_fail(site); } while (0)
+#else
+#define SQ_LINEAR_CHECK(cond, site) do {} while (0)
+#endif
+
 // ---------------------------------------------------------------- 8-bit checkpoints
 //
 // 32 consecutive features of a row share a power of two: with a = max|v|, E = max(1, exponent field of a - 6) and
@@ -268,6 +284,7 @@ __device__ __noinline__ uint4 load_bytes16(const uint8_t *p, const uint8_t *lo, 
     for (int i = 0; i < 5; ++i) {
         const uint8_t *q = a + 4 * i;
         if (q >= lo && q + 4 <= hi) {
+            SQ_LINEAR_CHECK((reinterpret_cast<uintptr_t>(q) & 3) == 0, 1000);
             w[i] = get(reinterpret_cast<const uint32_t *>(q));
         } else {
             uint32_t v = 0;
@@ -283,6 +300,14 @@ __device__ __noinline__ uint4 load_bytes16(const uint8_t *p, const uint8_t *lo, 
 // ---------------------------------------------------------------- mbarriers, TMA, tcgen05
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+// End of the block's dynamic shared memory, which starts at `from`.
+__device__ __forceinline__ uint32_t smem_end(const void *from)
+{
+    uint32_t bytes;
+    asm("mov.u32 %0, %%dynamic_smem_size;" : "=r"(bytes));
+    return smem_addr(from) + bytes;
+}
 
 // True for one lane of a converged warp, always the same one.  The compiler knows that there is one: under a comparison
 // of the lane's number instead, copies and matrix instructions, whose operands are uniform registers, cost several times the issue time.

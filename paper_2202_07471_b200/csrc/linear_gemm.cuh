@@ -92,12 +92,14 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row0, int co
 {
     const int n = min(32, p.cols - col), rows = static_cast<int>(min(static_cast<int64_t>(32), p.rows - row0));   // rows may be negative
     if (rows <= 0) return;
+    SQ_LINEAR_CHECK(n > 0 && row0 >= 0 && col >= 0, 1020);
     const int64_t row = row0 + (threadIdx.x & 31);
     const bool valid = static_cast<int>(threadIdx.x & 31) < rows;
     float v[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(acc[i]);
     if (p.sums) {
+        SQ_LINEAR_CHECK(col + 32 <= p.sums_pitch && (!valid || row < p.rows), 1021);
         float4 *sums = reinterpret_cast<float4 *>(p.sums + row * p.sums_pitch + col);   // 32 columns: the pitch is a multiple of that
         if (valid && p.sums_in)
 #pragma unroll
@@ -141,6 +143,7 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row0, int co
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = ckpt_codes(v + 4 * i, inverse);
             if (valid) {
+                SQ_LINEAR_CHECK(row < p.rows && col + 32 <= p.z_pitch && (col >> 5) < p.z_exps_pitch, 1022);
                 uint4 *zc = reinterpret_cast<uint4 *>(p.z_codes + row * p.z_pitch + col);
                 zc[0] = make_uint4(w[0], w[1], w[2], w[3]);
                 zc[1] = make_uint4(w[4], w[5], w[6], w[7]);
@@ -172,6 +175,7 @@ __device__ __forceinline__ void finish32(const GemmArgs &p, int64_t row0, int co
     for (int i = 0; i < 16; ++i) packed[i] = to_16x2<kHalf>(v[2 * i], v[2 * i + 1]);
     if (p.out_vector && n == 32) {
         if (valid) {
+            SQ_LINEAR_CHECK(row < p.rows && col + 32 <= p.cols && (reinterpret_cast<uintptr_t>(p.out + row * p.out_stride + col) & 15) == 0, 1023);
             uint4 *out = reinterpret_cast<uint4 *>(p.out + row * p.out_stride + col);
 #pragma unroll
             for (int j = 0; j < 4; ++j) out[j] = make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
@@ -186,6 +190,7 @@ template <int kMode, bool kHalf>
 __device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col, const float (&scale)[4], const float (&bias)[4], float (&v)[4])
 {
     const int n = p.cols - col;   // columns of this thread, if below four
+    SQ_LINEAR_CHECK(row >= 0 && row < p.rows, 1024);
     if constexpr (kMode == kForward) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = fmaf(v[i], scale[i], bias[i]);   // 0 behind the last channel
@@ -199,6 +204,7 @@ __device__ __forceinline__ void finish4(const GemmArgs &p, int64_t row, int col,
             const float inverse = ckpt_inverse(e);
             const uint32_t w = ckpt_codes(v, inverse);
             if ((col & ~31) < p.cols) {   // rows end on 32
+                SQ_LINEAR_CHECK(col + 4 <= p.z_pitch && (col >> 5) < p.z_exps_pitch, 1025);
                 *reinterpret_cast<uint32_t *>(p.z_codes + row * p.z_pitch + col) = w;
                 if ((col & 31) == 0) p.z_exps[row * p.z_exps_pitch + (col >> 5)] = static_cast<uint8_t>(e);
             }
@@ -330,6 +336,8 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     const uint32_t smem_a = base, smem_b = base + stages * kFusedBytesA, smem_c = smem_b + stages * bytes_b;
     const int raws = min(kFusedMostRaw, (kFusedMemory - stages * (kFusedBytesA + bytes_b)) / P::kRawBytes);   // at least two
     const uint32_t bars = base + kFusedMemory;
+    SQ_LINEAR_CHECK(stages >= 2 && raws >= 2 && smem_c + raws * P::kRawBytes <= bars && p.box_rows <= kFusedTokens && p.box_rows % 16 == 0, 1030);
+    SQ_LINEAR_CHECK(bars + 8 * (4 * kFusedMostStages + 4 * kFusedMostRaw + 1) <= smem_end(smem_raw), 1031);
     auto full = [&](int s) { return bars + 8 * s; };
     auto empty = [&](int s) { return bars + 8 * (2 * kFusedMostStages + s); };
     auto raw_full = [&](int s) { return bars + 8 * (4 * kFusedMostStages + s); };
@@ -347,6 +355,8 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
     const int first = static_cast<int>(static_cast<int64_t>(all) * rank / ranks);
     const int steps = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / ranks) - first;   // at least one
     const int here = static_cast<int>(min(static_cast<int64_t>(kFusedTokens), p.rows - row0));
+    SQ_LINEAR_CHECK(ranks >= 1 && ranks <= kFusedMostRanks && tile < p.tiles && here > 0 && here <= p.box_rows && col0 < p.cols, 1032);
+    SQ_LINEAR_CHECK(steps >= 1 && static_cast<int64_t>(steps) * kTileDepth <= kLongestSum && first + steps <= all, 1033);
 
     if (threadIdx.x == 0) {
         gave_up_word = 0;
@@ -376,6 +386,9 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
 #pragma unroll
             for (int i = 0; i < P::kCount; ++i) codes[i] = read_codes<kMode, kKind>(smem_c + raw.place() * P::kRawBytes, P(i));
             if (k >= stages && !bar_wait_warp(empty(stage.before()), stage.before_parity(), gave_up)) break;
+            SQ_LINEAR_CHECK(raw.place() == k % raws && raw.bar == k % (2 * raws) && stage.place() == k % stages && stage.bar == k % (2 * stages), 1034);
+#pragma unroll
+            for (int i = 0; i < P::kCount; ++i) SQ_LINEAR_CHECK(P(i).row * 128 + P(i).panel * 8192 + 128 <= kFusedBytesA, 1035);
 #pragma unroll
             for (int i = 0; i < P::kCount; ++i) store_codes<kMode, kKind, kHalf>(smem_a + stage.place() * kFusedBytesA, P(i), codes[i], int4);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -390,6 +403,7 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
             const int quarter = warp & 3;
             const uint32_t part = base + 4 * (quarter * 32 + lane);
             for (int t = warp / 4 * 32; t < here; t += 64) {
+                SQ_LINEAR_CHECK(t + 32 <= kFusedTokens && part + (min(t + 31, here - 1) * kFusedPartPitch + 1) * 4 <= base + kFusedMemory, 1036);
                 uint32_t acc[32];
                 tmem_ld32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + t, acc);
 #pragma unroll
@@ -468,6 +482,7 @@ fused_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CU
         const int end = min(here, (static_cast<int>(rank) + 1) * share);
         for (int r = static_cast<int>(rank) * share + warp; r < end; r += kConverterWarps) {
             const uint32_t mine = base + 4 * (r * kFusedPartPitch + 4 * lane);
+            SQ_LINEAR_CHECK(mine + 16 <= base + kFusedMemory, 1037);
             float v[4] = {}, part[kFusedMostRanks][4];
 #pragma unroll
             for (uint32_t q = 0; q < kFusedMostRanks; ++q)

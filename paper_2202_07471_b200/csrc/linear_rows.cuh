@@ -84,6 +84,7 @@ static __global__ void __launch_bounds__(kRowThreads) checkpoint_kernel(const Ro
         const float inverse = ckpt_inverse(e);
         const uint4 w = make_uint4(ckpt_codes(f[0], inverse), ckpt_codes(f[0] + 4, inverse), ckpt_codes(f[1], inverse), ckpt_codes(f[1] + 4, inverse));
         if (first + i * kRowThreads < total) {
+            SQ_LINEAR_CHECK(row[i] < p.rows && col[i] >= 0 && col[i] + 16 <= p.code_pitch && (col[i] >> 5) < p.exps_pitch, 1050);
             *reinterpret_cast<uint4 *>(p.codes + row[i] * p.code_pitch + col[i]) = w;
             if ((threadIdx.x & 1) == 0) p.exps[row[i] * p.exps_pitch + (col[i] >> 5)] = static_cast<uint8_t>(e);
         }
@@ -104,6 +105,7 @@ static __global__ void __launch_bounds__(kRowThreads) restore_kernel(const RowAr
         c[i] = make_uint2(0, 0);
         e[i] = 0;
         if (at < total) {
+            SQ_LINEAR_CHECK(row[i] < p.rows && col[i] >= 0 && col[i] + 8 <= p.code_pitch && (col[i] >> 5) < p.exps_pitch, 1051);
             c[i] = get(reinterpret_cast<const uint2 *>(p.codes + row[i] * p.code_pitch + col[i]));
             e[i] = get(p.exps + row[i] * p.exps_pitch + (col[i] >> 5));
         }
@@ -139,6 +141,8 @@ static __global__ void __launch_bounds__(kRowThreads) expand_kernel(const RowArg
         c[i] = make_uint2(0, 0);
         if (at < total) {
             const uint8_t *q = p.codes + row[i] * p.code_pitch + piece[i] * kBytes;
+            SQ_LINEAR_CHECK(row[i] < p.rows && piece[i] < p.pieces && piece[i] * 8 + 8 <= p.out_stride, 1052);
+            SQ_LINEAR_CHECK(p.vector ? piece[i] * kBytes + kBytes <= p.code_pitch : piece[i] * kBytes < p.code_pitch, 1053);
             if (p.vector) {
                 if (kKind == kInt4) c[i].x = get(reinterpret_cast<const uint32_t *>(q));
                 else c[i] = get(reinterpret_cast<const uint2 *>(q));
@@ -184,6 +188,7 @@ static __global__ void __launch_bounds__(kRowThreads) copy_kernel(const __grid_c
 #pragma unroll
     for (int i = 0; i < kRowPieces; ++i) {
         const uint32_t at = first + i * kRowThreads, row = p.magic ? __umulhi(at, p.magic) >> p.shift : at, piece = at - row * p.pieces;
+        SQ_LINEAR_CHECK(at >= total || (row < p.rows && piece < p.pieces && piece * 16 + 16 <= p.out_pitch), 1054);
         if (at < total)
             *reinterpret_cast<uint4 *>(p.out + row * p.out_pitch + piece * 16) = load_bytes16(p.in + row * p.in_pitch + piece * 16, p.in, p.end);
     }
@@ -283,10 +288,13 @@ __global__ void __launch_bounds__(kRowThreads, 4) slope_kernel(const __grid_cons
             [[maybe_unused]] uint32_t zc[kCount], ze[kCount];
 #pragma unroll
             for (int b = 0; b < kCount; ++b) {
+                SQ_LINEAR_CHECK(t0 + b * kSlopeRows < p.tokens && dy_at == p.dy + (t0 + b * kSlopeRows) * p.dy_stride + col && col + (kVector ? 4 : 1) <= p.cout, 1055);
                 if constexpr (kVector) dy[b] = get(reinterpret_cast<const uint2 *>(dy_at));
                 else dy[b] = load4(dy_at, n, false);
                 dy_at += kSlopeRows * p.dy_stride;
                 if constexpr (kAct != kNoZ) {
+                    SQ_LINEAR_CHECK(col + 4 <= p.z_pitch && zc_at == p.z_codes + (t0 + b * kSlopeRows) * p.z_pitch + col &&
+                                    ze_at == p.z_exps + (t0 + b * kSlopeRows) * p.z_exps_pitch + (col >> 5), 1056);
                     zc[b] = get(reinterpret_cast<const uint32_t *>(zc_at));
                     ze[b] = get(ze_at);
                     zc_at += kSlopeRows * p.z_pitch;
@@ -321,6 +329,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) slope_kernel(const __grid_cons
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) db[i] += dz[i];
+                SQ_LINEAR_CHECK(col + 4 <= p.pitch && dz_at == p.dz + (t0 + b * kSlopeRows) * p.pitch + col && dzs_at == p.dzs + (t0 + b * kSlopeRows) * p.pitch + col, 1057);
                 if (p.dz) *reinterpret_cast<uint2 *>(dz_at) = make_uint2(to_16x2<false>(dz[0], dz[1]), to_16x2<false>(dz[2], dz[3]));
                 if (p.dzs)
                     *reinterpret_cast<uint2 *>(dzs_at) = make_uint2(to_16x2<false>(dz[0] * scale[0], dz[1] * scale[1]),
@@ -347,6 +356,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) slope_kernel(const __grid_cons
     __syncthreads();
     const int which = threadIdx.x / kSlopeCols, c = blockIdx.x * kSlopeCols + static_cast<int>(threadIdx.x) % kSlopeCols;
     if (which < 2 && c < p.cout) {
+        SQ_LINEAR_CHECK(!p.partial || blockIdx.y < static_cast<unsigned>(p.shares), 1058);
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < kRowThreads / 32; ++w) s += part[w][threadIdx.x];

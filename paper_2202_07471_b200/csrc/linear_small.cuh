@@ -38,6 +38,7 @@ __device__ __forceinline__ void load_x16(const uint16_t *row, int first, int cin
 {
     v[0] = v[1] = make_uint4(0, 0, 0, 0);
     if constexpr (kAlign == 32) {
+        SQ_LINEAR_CHECK(first >= cin || (first + 16 <= cin && (reinterpret_cast<uintptr_t>(row + first) & 31) == 0), 1010);
         if (first < cin)
             asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                          : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z), "=r"(v[1].w) : "l"(row + first));
@@ -45,6 +46,7 @@ __device__ __forceinline__ void load_x16(const uint16_t *row, int first, int cin
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if constexpr (kAlign == 16) {
+                SQ_LINEAR_CHECK(first + 8 * h >= cin || (first + 8 * h + 8 <= cin && (reinterpret_cast<uintptr_t>(row + first) & 15) == 0), 1011);
                 if (first + 8 * h < cin) v[h] = get(reinterpret_cast<const uint4 *>(row + first + 8 * h));
             } else {
                 uint32_t w[4];
@@ -116,6 +118,8 @@ __global__ void __launch_bounds__(32 * kFewWarps, kTiles == 1 ? 3 : 2) few_kerne
                 codes[u][r] = make_uint4(0, 0, 0, 0);
                 if (piece * 16 < row_bytes && at < p.cout) {
                     const uint8_t *from = p.codes + at * p.code_pitch + piece * 16;
+                    SQ_LINEAR_CHECK(from >= p.codes && (kAlign ? from + 16 <= p.codes + p.code_bytes && (reinterpret_cast<uintptr_t>(from) & 15) == 0
+                                                              : from < p.codes + p.code_bytes), 1012);
                     codes[u][r] = kAlign ? ldg128(from) : load_bytes16(from, p.codes, p.codes + p.code_bytes);
                 }
             }
@@ -164,6 +168,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kTiles == 1 ? 3 : 2) few_kerne
     for (int j = 0; j < kMine; ++j) {
         const int token = first + 16 * j;
         if (token >= tokens) return;
+        SQ_LINEAR_CHECK(token < kTiles * kFewTokens && token0 + token < p.tokens && row >= row0 && row < p.cout, 1013);
         float u = 0.0f;
 #pragma unroll
         for (int w = 0; w < kFewWarps; ++w) u += part[w][token][row - row0];

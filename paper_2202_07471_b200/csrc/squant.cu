@@ -1191,8 +1191,11 @@ int squant_debug_violations(int32_t *count, int32_t *first_site)
     int site = 0;
     SQ_CUDA(cudaMemcpyFromSymbol(&n, sq::g_debug_violations, sizeof(n)));
     SQ_CUDA(cudaMemcpyFromSymbol(&site, sq::g_debug_site, sizeof(site)));
-    if (count) *count = static_cast<int32_t>(n);
-    if (first_site) *first_site = site;
+    unsigned linear = 0;
+    int linear_site = 0;
+    SQ_CUDA(sq_host::take_linear_violations(&linear, &linear_site));
+    if (count) *count = static_cast<int32_t>(n + linear);
+    if (first_site) *first_site = n ? site : linear_site;
     const unsigned zero = 0;
     SQ_CUDA(cudaMemcpyToSymbol(sq::g_debug_violations, &zero, sizeof(zero)));
     SQ_CUDA(cudaMemcpyToSymbol(sq::g_debug_site, &zero, sizeof(int)));

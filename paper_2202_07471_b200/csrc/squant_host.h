@@ -11,5 +11,7 @@ int cuda_failed(cudaError_t e, const char *what);
 void count_launch();
 // Whether a kernel of the linear operators gave up a bounded wait on the current device; clears the record.
 cudaError_t take_linear_status(int *status);
+// Failed checks of their checked build and the first one's site; clears both.
+cudaError_t take_linear_violations(unsigned *count, int *site);
 
 }  // namespace sq_host
