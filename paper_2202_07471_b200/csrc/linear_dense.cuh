@@ -18,6 +18,8 @@ struct DenseShape {
     static constexpr int kTmemCols = 2 * kCols;
     static constexpr int kSmem = 1024 + kStages * (kBytesA + kBytesB) + kDenseEpilogueWarps * kTurnBytes + 8 * (2 * kStages + 4);
     static_assert(kSmem + 1024 + 128 <= 228 << 10, "fits a multiprocessor");
+    static_assert(kSmem + kFusedSmem > 228 << 10 && 2 * kSmem > 228 << 10 && kTmemCols <= 512,
+                  "alone among the kernels that use tensor memory, so that what it asks for is always there");
 };
 
 __device__ __forceinline__ void remote_arrive(uint32_t cluster_bar)

@@ -247,6 +247,7 @@ constexpr int kFusedSmem = 1024 + kFusedMemory + 8 * (4 * kFusedMostStages + 4 *
 constexpr int kFusedMostRanks = 8;    // thread blocks of a cluster, which share a tile's contraction
 static_assert(4 * (kFusedTokens + kFusedMostRanks - 1) * kFusedPartPitch <= kFusedMemory, "all ranks' sums of a share of the tokens take the stages' place");
 static_assert(2 * (kFusedSmem + 128 + 1024) <= 228 << 10, "two blocks a multiprocessor");
+static_assert(3 * kFusedSmem > 228 << 10 && 2 * kFusedTokens <= 512, "and no more, so that the tensor memory they ask for is always there");
 static_assert(2 * (kFusedBytesA + 128 * kFusedTokens) + 2 * (8 << 10) <= kFusedMemory, "two stages and two of codes fit always");
 
 // One 16-byte piece of a coded row: 32 int4 codes or 16 8-bit codes.  Neighbouring converter lanes take the pieces of a row's 64

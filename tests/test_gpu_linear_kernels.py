@@ -118,3 +118,30 @@ def test_checkpoints_of_integers_are_exact(kernel, tokens, cin, cout):
     rest = [i for i in range(tokens) if i not in (1, 5)]
     assert (z.exps[[1, 5]] == 255).all() and (z.codes[[1, 5]] == 0).all()
     assert torch.equal(z.exps[rest], e[rest]) and torch.equal(z.codes[rest], q[rest])
+
+
+def test_many_calls_on_two_streams_without_a_wait():
+    """Kernels that take all of a multiprocessor's tensor memory and kernels that share it, from two streams, queued far ahead."""
+    codes, scales = real_layer(1024, 1024, 8, 1)
+    x = torch.randn((300, 1024), generator=gen(2), device="cuda").bfloat16()
+    x8 = sq.squant_checkpoint(x)
+
+    def calls(tokens):
+        y, z = sq.squant_linear(x[:tokens], codes, scales, act="gelu", checkpoint=True)
+        part = sq.Checkpoint(x8.codes[:tokens], x8.exps[:tokens], 1024)
+        g = sq.squant_linear_backward(y, codes, scales, act="gelu", z=z, x=part, dweight=True, dbias=True)
+        return y, z.codes, g.dx, g.dweight, g.dbias
+
+    wants = [[t.clone() for t in calls(tokens)] for tokens in (64, 300)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    last = [None, None]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for i in range(200):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                last[k] = calls((64, 300)[(i + k) % 2])
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(same_bits(a, b) for a, b in zip(last[k], wants[(199 + k) % 2]))
+    sq.squant_device_status()
