@@ -355,6 +355,78 @@ int64_t squant_linear_backward_workspace(const squant_linear_grad_args *args);
 int squant_linear_backward(const squant_linear_grad_args *args, void *cuda_stream);
 
 /*
+ * A key/value cache held in 4 bits, and attention over it.  The cache is an array of uint8 [pages][kv_heads][page_size / 16][18 * head_dim]; head_dim is 64, 128 or
+ * 256, page_size a multiple of 16.  A granule of 18 * head_dim bytes (4.5 bits a value) holds 16 positions of one head:
+ *   32 neighbouring channels of a key or value share a scale s = max|x| / 7, rounded to four significant bits (ties to even); the code of x is
+ *   rint(x / s), ties to even, in -7..7, and stands for code * s, which is exact in bf16 and at most s / 2 from x.  A group below 2^-100 has s = 0 and zeros; one with an
+ *   infinity, a NaN or a magnitude from 2^120 on has s = infinity and stands for NaN.
+ *   words of 8 codes (neighbouring channels, code e in bits 4 * (e / 2) + 16 * (e % 2)); with slabs of up to 128 channels:
+ *     keys [slab][position][word % 4][word / 4], from 8 * head_dim on values [slab][position / 2][word % 8][position % 2][word / 8],
+ *     from 16 * head_dim on the keys' scales [position][group], from 17 * head_dim on the values' [slab][position / 2][group % 2][group / 2][position % 2], bf16.
+ *
+ * Which rows of k, v, q and the outputs belong where is said by arrays on the device, so that a captured graph may be replayed with other ones: rows
+ * starts[b] .. starts[b + 1] are the LAST positions of sequence b, which has lens[b] in all, these included; position p lies in page pages[b][p / page_size].  starts does not
+ * decrease and ends at `rows` at most; rows behind the last sequence are left as they are.  A sequence with more rows than positions has the excess before its first
+ * position: such rows see nothing and are written nowhere.  Nothing in the arrays leads outside the tensors: lengths are cut to 0 .. width * page_size, starts to
+ * 0 .. rows, and a page outside 0 .. page_count - 1 counts as not there (nothing is written to it, it reads as zeros, its positions are not attended to).
+ */
+typedef struct squant_cache_rows {
+    void *data;              /* the cache, 16-byte aligned */
+    int64_t page_count;
+    int32_t kv_heads, head_dim, page_size;
+    int32_t batch;           /* sequences, >= 0 */
+    int32_t width;           /* columns of pages */
+    const int32_t *lens;     /* [batch] */
+    const int32_t *pages;    /* [batch][width], rows pages_stride elements apart */
+    int64_t pages_stride;
+    const int32_t *starts;   /* [batch + 1], or NULL: row b is the last position of sequence b, and rows = batch */
+    int64_t rows;
+} squant_cache_rows;
+
+/* Keys and values [rows][kv_heads][head_dim] (SQUANT_BF16 or SQUANT_FP16); strides in elements from row to row and from head to head, so that they may be slices
+ * of wider buffers.  Rows and heads that start on 16 bytes are moved faster. */
+typedef struct squant_cache_move_args {
+    squant_cache_rows rows;
+    uint32_t dtype;
+    void *k, *v;
+    int64_t k_stride, k_head_stride, v_stride, v_head_stride;
+} squant_cache_move_args;
+
+/* Quantizes k and v into the cache.  Two rows of one call must not have the same place (sequences that share a page may read it, not write it). */
+int squant_cache_write(const squant_cache_move_args *args, void *cuda_stream);
+/* What the cache holds for these rows, into k and v: exact in bf16, rounded to nearest in fp16.  Zeros for rows before a sequence's first position or in a page that is not there. */
+int squant_cache_read(const squant_cache_move_args *args, void *cuda_stream);
+
+/*
+ * Softmax attention of rows over the cache: the row of position i attends to the positions 0 .. i of its sequence, which have been written before.  With q of query
+ * head h, and k, v of kv head h / group, as squant_cache_read returns them in q's type:
+ *   s_j = scale * q k_j,  out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = log sum_j exp(s_j)
+ * A row that sees nothing gets zeros and lse -infinity.  Products are exact, sums and softmax fp32; in calls of more than 8 rows times heads of a sequence the
+ * probabilities are rounded to q's type for the product with the values.  fp16 wants keys and values below 61,600 in magnitude.  Results repeat to the bit.
+ */
+typedef struct squant_cache_attention_args {
+    squant_cache_rows rows;
+    uint32_t dtype;          /* of q and out */
+    int32_t group;           /* query heads of a kv head */
+    int32_t most;            /* rows that no sequence has more of, for the choice of the kernel only; 0: not known */
+    float scale;             /* finite */
+    const void *q;           /* [rows][kv_heads * group][head_dim] */
+    int64_t q_stride, q_head_stride;
+    void *out;               /* likewise; no overlap with q */
+    int64_t out_stride, out_head_stride;
+    float *lse;              /* [rows][kv_heads * group], may be NULL */
+    void *workspace;         /* squant_cache_attention_workspace() bytes, 16-byte aligned, not shared with a call that may run at the same time */
+    int64_t workspace_bytes;
+} squant_cache_attention_args;
+
+int64_t squant_cache_attention_workspace(const squant_cache_attention_args *args);
+/* Which kernel a call with these arguments takes: 0 (no rows), one of the values below, or the call's negative error.  No GPU is needed. */
+#define SQUANT_CACHE_STEP 1     /* tiles of 8 rows (tokens times heads of a group) */
+#define SQUANT_CACHE_STEP_16 2  /* tiles of 16 rows */
+int squant_cache_attention_plan(const squant_cache_attention_args *args);
+int squant_cache_attention(const squant_cache_attention_args *args, void *cuda_stream);
+
+/*
  * Self-check of the arithmetic shortcut in SQuant-E (Algorithm 1 "Scale and SQuant-E").  The 3x3
  * path does not divide every weight by the channel's scale s; it multiplies by one correctly
  * rounded reciprocal per channel and corrects the product with two fused multiply-adds, which

@@ -13,8 +13,9 @@ LIB = os.path.join(HERE, "libsquant.so")
 LIB_DEBUG = os.path.join(HERE, "libsquant_debug.so")   # the checked build (-DSQUANT_DEBUG_BOUNDS), for tests on small cases
 OBJECTS = os.path.join(HERE, "_build")
 SHARED = [os.path.join(ROOT, "include", "squant.h"), os.path.join(CSRC, "squant_host.h")]
-# each translation unit with the headers it alone includes: the quantizer, the linear operators
-UNITS = [(os.path.join(CSRC, unit + ".cu"), sorted(glob.glob(os.path.join(CSRC, unit + "_*.cuh")))) for unit in ("squant", "linear")]
+# each translation unit with its headers: the quantizer, the linear operators, the key/value cache
+UNITS = [(os.path.join(CSRC, unit + ".cu"), sorted(glob.glob(os.path.join(CSRC, unit + "_*.cuh")))) for unit in ("squant", "linear", "cache")]
+UNITS[2][1].append(os.path.join(CSRC, "linear_device.cuh"))
 DEPS = [d for source, headers in UNITS for d in (source, *headers)] + SHARED
 
 # -fmad=false: the solver's fp32 steps (division, rounding, difference) are written with

@@ -615,6 +615,7 @@ int squant_debug_linear_wait_limit(int32_t tries)
     const int limit = tries < 0 ? sq::kWaitLimit : tries;
     SQ_CUDA(cudaDeviceSynchronize());
     SQ_CUDA(cudaMemcpyToSymbol(sq::g_wait_limit, &limit, sizeof(int)));
+    SQ_CUDA(sq_host::set_cache_wait_limit(limit));
     return 1;   // this library was built with the checks
 #else
     return SQUANT_OK;

@@ -275,7 +275,7 @@ __device__ __forceinline__ uint4 ldg128(const void *p)
 
 // 16 bytes from any address: five aligned words, shifted.  Words that are not wholly inside [lo, hi) are put
 // together from the bytes that are; other bytes read as zero.
-__device__ __noinline__ uint4 load_bytes16(const uint8_t *p, const uint8_t *lo, const uint8_t *hi)
+static __device__ __noinline__ uint4 load_bytes16(const uint8_t *p, const uint8_t *lo, const uint8_t *hi)
 {
     const uint8_t *a = reinterpret_cast<const uint8_t *>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t{3});
     const unsigned sh = static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) & 3) * 8;

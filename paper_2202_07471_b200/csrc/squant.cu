@@ -1171,7 +1171,9 @@ int squant_device_status(void)
     SQ_CUDA(cudaMemcpyFromSymbol(&st, sq::g_device_status, sizeof(int)));
     int linear = 0;
     SQ_CUDA(sq_host::take_linear_status(&linear));
-    if (st == 0) return linear == 0 ? SQUANT_OK : SQUANT_ERR_TIMEOUT;
+    int cache = 0;
+    SQ_CUDA(sq_host::take_cache_status(&cache));
+    if (st == 0) return linear == 0 && cache == 0 ? SQUANT_OK : SQUANT_ERR_TIMEOUT;
     const int zero = 0;
     SQ_CUDA(cudaMemcpyToSymbol(sq::g_device_status, &zero, sizeof(int)));
     // a launch that gave up may have left its work counters half drawn: all start clean again
@@ -1194,8 +1196,11 @@ int squant_debug_violations(int32_t *count, int32_t *first_site)
     unsigned linear = 0;
     int linear_site = 0;
     SQ_CUDA(sq_host::take_linear_violations(&linear, &linear_site));
-    if (count) *count = static_cast<int32_t>(n + linear);
-    if (first_site) *first_site = n ? site : linear_site;
+    unsigned cache = 0;
+    int cache_site = 0;
+    SQ_CUDA(sq_host::take_cache_violations(&cache, &cache_site));
+    if (count) *count = static_cast<int32_t>(n + linear + cache);
+    if (first_site) *first_site = n ? site : linear ? linear_site : cache_site;
     const unsigned zero = 0;
     SQ_CUDA(cudaMemcpyToSymbol(sq::g_debug_violations, &zero, sizeof(zero)));
     SQ_CUDA(cudaMemcpyToSymbol(sq::g_debug_site, &zero, sizeof(int)));

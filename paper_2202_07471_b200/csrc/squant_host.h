@@ -13,5 +13,10 @@ void count_launch();
 cudaError_t take_linear_status(int *status);
 // Failed checks of their checked build and the first one's site; clears both.
 cudaError_t take_linear_violations(unsigned *count, int *site);
+// The same for the kernels of the key/value cache.
+cudaError_t take_cache_status(int *status);
+cudaError_t take_cache_violations(unsigned *count, int *site);
+// The limit of their waits on the current device (checked build only).
+cudaError_t set_cache_wait_limit(int tries);
 
 }  // namespace sq_host
