@@ -57,6 +57,7 @@ int check(const squant_cache_rows &r, uint32_t dtype)
     if (r.head_dim != 64 && r.head_dim != 128 && r.head_dim != 256) return SQUANT_ERR_SHAPE;
     if (r.page_size < sq::kGranule || r.page_size % sq::kGranule || r.page_size > (1 << 24) || r.kv_heads < 1 || r.kv_heads > (1 << 16)) return SQUANT_ERR_SHAPE;
     if (r.page_count < 0 || r.page_count > (1ll << 31) || r.batch < 0 || r.width < 0 || r.rows < 0 || r.rows > kMaxRows) return SQUANT_ERR_SHAPE;
+    if (r.page_count * r.kv_heads * (r.page_size / sq::kGranule) >= (1ll << 31)) return SQUANT_ERR_SHAPE;   // granules are counted in 32 bits: 2 TB of them
     if (r.batch > 1 && (r.pages_stride < r.width || r.pages_stride > kMaxStride)) return SQUANT_ERR_SHAPE;
     if (!r.starts && r.rows != r.batch) return SQUANT_ERR_SHAPE;
     if (dtype > SQUANT_FP16) return SQUANT_ERR_MODE;
@@ -150,7 +151,7 @@ int check(const squant_cache_attention_args *args)
     const squant_cache_rows &r = a.rows;
     if (a.group < 1 || a.group > (1 << 16) || a.most < 0) return SQUANT_ERR_SHAPE;
     const int64_t heads = static_cast<int64_t>(r.kv_heads) * a.group;
-    if (heads > (1 << 20) || r.rows * heads > (1ll << 40)) return SQUANT_ERR_SHAPE;
+    if (heads > (1 << 20) || r.rows * a.group >= (1ll << 31)) return SQUANT_ERR_SHAPE;
     if (bad_strides(a.q_stride, a.q_head_stride, heads, r.rows, r.head_dim, false) ||
         bad_strides(a.out_stride, a.out_head_stride, heads, r.rows, r.head_dim, true)) return SQUANT_ERR_SHAPE;
     if (!std::isfinite(a.scale)) return SQUANT_ERR_MODE;
@@ -176,26 +177,30 @@ int plan(const squant_cache_attention_args &a)
 struct StepPlan {
     int64_t blocks = 0, tickets = 0, bytes = 0;
 };
-template <int D>
-StepPlan step_plan(const squant_cache_attention_args &a, int rows)
+template <int D, int kTiles>
+StepPlan step_plan(const squant_cache_attention_args &a)
 {
+    using S = sq::StepShape<D, kTiles>;
     const squant_cache_rows &r = a.rows;
     // units, at most: no more blocks than one a unit and warp of a block
-    const int64_t tiles = (r.rows * a.group + static_cast<int64_t>(std::min<int64_t>(r.batch, r.rows)) * (rows - 1)) / rows;
+    const int64_t tiles = (r.rows * a.group + static_cast<int64_t>(std::min<int64_t>(r.batch, r.rows)) * (S::kRows - 1)) / S::kRows;
     const int64_t positions = std::min<int64_t>(static_cast<int64_t>(r.width) * r.page_size, 1ll << 30);
-    const double units = static_cast<double>(tiles) * r.kv_heads * std::max<int64_t>(1, (positions + sq::kStepPositions - 1) / sq::kStepPositions);
+    const double units = static_cast<double>(tiles) * r.kv_heads * std::max<int64_t>(1, (positions + S::kPositions - 1) / S::kPositions);
     StepPlan s;
-    s.blocks = static_cast<int64_t>(std::min<double>(kB200Sms * sq::StepShape<D>::kBlocks, std::ceil(units / sq::kStepWarps)));
+    s.blocks = static_cast<int64_t>(std::min<double>(kB200Sms * S::kBlocks, std::ceil(units / sq::kStepWarps)));
     s.tickets = up(8 * s.blocks, 128);
-    s.bytes = s.tickets + 2 * s.blocks * sq::part_floats<D>(rows) * 4;
+    s.bytes = s.tickets + s.blocks * S::kParts * S::kPart * 4;
     return s;
 }
+template <int D>
 int64_t attention_bytes(const squant_cache_attention_args &a)
 {
     const int which = plan(a);
-    if (!which) return 0;
-    const int rows = which == SQUANT_CACHE_STEP ? 8 : 16;
-    return (a.rows.head_dim == 64 ? step_plan<64>(a, rows) : a.rows.head_dim == 128 ? step_plan<128>(a, rows) : step_plan<256>(a, rows)).bytes;
+    return !which ? 0 : which == SQUANT_CACHE_STEP ? step_plan<D, 1>(a).bytes : step_plan<D, 2>(a).bytes;
+}
+int64_t attention_bytes(const squant_cache_attention_args &a)
+{
+    return a.rows.head_dim == 64 ? attention_bytes<64>(a) : a.rows.head_dim == 128 ? attention_bytes<128>(a) : attention_bytes<256>(a);
 }
 
 // A number that no other call of any process has put into this call's workspace, 48 bits and not 0.
@@ -209,10 +214,10 @@ unsigned long long nonce()
     return n ? n : nonce();
 }
 
-template <int D, bool kHalf, int kHalves>
+template <int D, bool kHalf, int kTiles>
 int step(const squant_cache_attention_args &a, cudaStream_t stream)
 {
-    const StepPlan s = step_plan<D>(a, 8 * kHalves);
+    const StepPlan s = step_plan<D, kTiles>(a);
     sq::AttendArgs p{};
     p.cache = static_cast<const uint8_t *>(a.rows.data);
     p.r = rows_of(a.rows);
@@ -231,7 +236,7 @@ int step(const squant_cache_attention_args &a, cudaStream_t stream)
     p.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(a.workspace) + s.tickets);
     p.nonce = nonce();
     static std::atomic<bool> ready[kMaxDevices];
-    return launch_large(sq::cache_step_kernel<D, kHalf, kHalves>, ready, s.blocks, sq::kStepThreads, sq::StepShape<D>::kSmem, stream, p);
+    return launch_large(sq::cache_step_kernel<D, kHalf, kTiles>, ready, s.blocks, sq::kStepThreads, sq::StepShape<D, kTiles>::kSmem, stream, p);
 }
 template <int D>
 int attention(const squant_cache_attention_args &a, cudaStream_t stream)

@@ -3,8 +3,7 @@
 // The cache is made of granules: 16 positions of one page and one kv head, 18 * d bytes (d channels: 64, 128 or 256).  32 neighbouring channels of a
 // position's key or value share a scale s, the largest magnitude over 7 rounded to four significant bits (ties to even); the code of x is rint(x / s), which is
 // never outside -7..7 since s is at most 1/17 too small (7.44 steps at 8.5 rounded down to 8).  A value, code * s, has three bits times four and is exact in bf16, so that
-// everything that reads the cache sees the same numbers, and so are the offsets that turn codes into floats (136 s = 17 s * 8: five bits times four):
-// a pair of codes becomes a pair of scaled bf16 values in two instructions.
+// everything that reads the cache sees the same numbers.
 //   0       codes of the keys    [slab][position][word % 4][word / 4]      a word: 8 codes of neighbouring channels, 32 bits; a slab: 128 channels (64)
 //   8 d     codes of the values  [slab][position / 2][word % 8][position % 2][word / 8]
 //   16 d    scales of the keys   [position][group], bf16
@@ -90,7 +89,28 @@ __device__ __forceinline__ int sequence_of(const CacheRows &r, int64_t row)
 
 __device__ __forceinline__ float bf16_float(uint32_t low) { return __uint_as_float(low << 16); }
 
-// A word's (or two half words') codes, one pair of them at a time, times the pair's scales; both halves of `scales` in the values' type.
+// The halves of a register, both or one of them twice.
+__device__ __forceinline__ uint32_t half_twice(uint32_t two, bool high)
+{
+    uint32_t r;
+    if (high) asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tmov.b32 %0, {h, h};\n\t}" : "=r"(r) : "r"(two));
+    else asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tmov.b32 %0, {l, l};\n\t}" : "=r"(r) : "r"(two));
+    return r;
+}
+
+// What the conversion of a word wants of its scales (both halves in the values' type).
+template <bool kHalf>
+struct PairScales {
+    uint32_t scale, other, eight;   // s; bf16: -136 s, 8 s
+};
+
+// A word's (or two half words') codes, pair p of them in bits 4 p of both halves, times the pair's scales.  The integer pipe, which shifts and masks, has half the
+// rate of the one that multiplies, and is what the conversion is bound by: so pairs are taken out where they lie, with one shift a word.
+//   bf16  pairs 0 and 2 (after the shift): the bits of code + 8 become the low mantissa bits of 128, and one multiply-add by s takes 136 s off, exactly (five bits
+//         times four).  Pairs 1 and 3 lie in bits 4 to 7, the upper three of the mantissa and the lowest of the exponent: with all other bits zero that is a number
+//         near the smallest there is, 16 (code + 8) 2^-133, which a multiply-add makes code / 8, and a product with 8 s the value.
+//   fp16  the mantissa holds bits 4 to 7 too: 1024 + 8 + code, and 1024 + 16 (code + 8) = 1152 + 16 code; taking 1032 off, and 1152 (over 16), leaves the code.  No
+//         offset times a scale here, for which large scales leave no room.
 template <bool kHalf>
 struct CodePairs {
     uint32_t mask, flip, mask_high, flip_high;
@@ -99,37 +119,37 @@ struct CodePairs {
         // from registers that the compiler cannot see through, see Int4To16
         asm volatile("mov.b32 %0, 0x000f000f;" : "=r"(mask));
         asm volatile("mov.b32 %0, %1;" : "=r"(flip) : "n"(kHalf ? 0x64086408u : 0x43084308u));
-        if constexpr (kHalf) {
-            asm volatile("mov.b32 %0, 0x00f000f0;" : "=r"(mask_high));
-            asm volatile("mov.b32 %0, 0x64806480;" : "=r"(flip_high));
-        }
+        asm volatile("mov.b32 %0, 0x00f000f0;" : "=r"(mask_high));
+        asm volatile("mov.b32 %0, %1;" : "=r"(flip_high) : "n"(kHalf ? 0x64806480u : 0x00800080u));
     }
-    // What goes with scales: the offset that one fused multiply-add takes off (bf16, exact).  fp16 has no room for the offset of large scales.
-    static __device__ __forceinline__ uint32_t offset(uint32_t scales) { return kHalf ? 0u : mul2_bf16(scales, 0xc308c308u); }   // -136
-    // Pairs 0 .. 3, which are in bits 4 p of both halves.
-    __device__ __forceinline__ void operator()(uint32_t w, uint32_t scales, uint32_t off, uint32_t (&out)[4]) const
+    static __device__ __forceinline__ PairScales<kHalf> scales(uint32_t s)
     {
+        PairScales<kHalf> r;
+        r.scale = s;
         if constexpr (kHalf) {
-            const uint32_t s = w >> 8;
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const uint32_t from = p < 2 ? w : s;
-                uint32_t u;
-                if (p & 1) {   // 1024 + 16 (code + 8), over 16, less 72
-                    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(from), "r"(mask_high), "r"(flip_high));
-                    u = fma2<true>(u, 0x2c002c00u, 0xd480d480u);
-                } else {       // 1024 + 8 + code, less 1032
-                    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(from), "r"(mask), "r"(flip));
-                    u = fma2<true>(u, 0x3c003c00u, 0xe408e408u);
-                }
-                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(out[p]) : "r"(u), "r"(scales));
-            }
+            r.other = r.eight = 0;   // not used
         } else {
+            r.other = mul2_bf16(s, 0xc308c308u);   // -136
+            r.eight = mul2_bf16(s, 0x41004100u);   // 8
+        }
+        return r;
+    }
+    __device__ __forceinline__ void operator()(uint32_t w, const PairScales<kHalf> &s, uint32_t (&out)[4]) const
+    {
+        const uint32_t upper = w >> 8;
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {   // (128 + 8 + code) s - 136 s
-                uint32_t u;
-                asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(w >> (4 * p)), "r"(mask), "r"(flip));
-                out[p] = fma2<false>(u, scales, off);
+        for (int p = 0; p < 4; ++p) {
+            const uint32_t from = p < 2 ? w : upper;
+            uint32_t u;
+            if (p & 1) asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(from), "r"(mask_high), "r"(flip_high));   // (from & mask) ^ flip
+            else asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(from), "r"(mask), "r"(flip));
+            if constexpr (kHalf) {
+                u = p & 1 ? fma2<true>(u, 0x2c002c00u, 0xd480d480u) : fma2<true>(u, 0x3c003c00u, 0xe408e408u);   // u / 16 - 72, u - 1032
+                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(out[p]) : "r"(u), "r"(s.scale));
+            } else if (p & 1) {
+                out[p] = mul2_bf16(fma2<false>(u, 0x7e807e80u, 0xbf80bf80u), s.eight);   // u 2^126 - 1
+            } else {
+                out[p] = fma2<false>(u, s.scale, s.other);
             }
         }
     }
@@ -142,7 +162,7 @@ __device__ __forceinline__ uint32_t scale_twice(uint32_t two, bool high)
         const float s = __uint_as_float(high ? two & 0xffff0000u : two << 16);
         return to_16x2<true>(s, s);
     } else {
-        return __byte_perm(two, 0, high ? 0x3232 : 0x1010);
+        return half_twice(two, high);
     }
 }
 // Two bf16 scales in the values' type.

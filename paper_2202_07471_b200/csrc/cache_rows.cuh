@@ -158,7 +158,7 @@ cache_read_kernel(const __grid_constant__ MoveArgs p)
         if (head >= p.r.kv_heads) continue;
         const uint32_t s = scale_twice<kHalf>(scale[i], false);
         uint32_t out[4];
-        pairs(word[i], s, pairs.offset(s), out);
+        pairs(word[i], pairs.scales(s), out);
         uint16_t *to = at.value ? p.v + row * p.v_stride + head * p.v_head + 8 * at.word : p.k + row * p.k_stride + head * p.k_head + 8 * at.word;
         if (p.vector) {
             *reinterpret_cast<uint4 *>(to) = make_uint4(out[0], out[1], out[2], out[3]);

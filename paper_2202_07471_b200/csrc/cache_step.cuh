@@ -3,13 +3,14 @@
 //   s_ij = scale q_i k_j,   p_ij = exp(s_ij - max_j s_ij),   out_i = sum_j p_ij v_j / sum_j p_ij,   lse_i = log sum_j exp(s_ij)
 //
 // A tile is 8 (or 16) rows of one sequence and kv head: tokens times the query heads of the group.  What bounds it is the cache's bytes, and next to them the instructions that turn
-// codes into floats: at the copy bandwidth a multiprocessor gets 23 bytes a clock, a position of 128 channels (144 bytes) every 6.2 clocks or 25 issue slots,
-// of which the conversion takes 12 and softmax and matrix instructions 7.
+// codes into floats: at the copy bandwidth a multiprocessor gets 23 bytes a clock, a position of 128 channels (144 bytes) every 6.2 clocks or 25 issue slots.
 //
-// Work is cut by what there is, not by sequence: the units (32 positions of a tile) of all sequences stand in one row, and each thread block takes an equal stretch of
-// it, which may hold the end of one tile, whole ones and the beginning of another.  A tile that several blocks have a part of is put together by the block that ends
-// last, in the order of the blocks, so that results repeat to the bit.
+// Work is cut by what there is, not by sequence: the units (32 positions of a tile) of all sequences stand in one row, and each warp takes an equal stretch of
+// it, which may hold the end of one tile, whole ones and the beginning of another.  Whole tiles a warp finishes by itself.  Parts of tiles are put together at the end of the block, and
+// where several blocks have a part, by the block that ends last, always in the order of the stretches, so that results repeat to the bit.
 #pragma once
+
+#include <type_traits>
 
 #include "cache_device.cuh"
 
@@ -33,22 +34,28 @@ struct AttendArgs {
 
 constexpr int kStepWarps = 8, kStepThreads = 32 * kStepWarps;
 constexpr int kStepStages = 2;                 // of a warp: one being read, one in flight
-constexpr int kStepPositions = 2 * kGranule;   // of a unit
-constexpr int kMergeRows = 8;
-constexpr float kGrowth = 8.0f;                // the running maximum is replaced when a new one is 2^8 as large: sums stay far inside fp32 and bf16
+constexpr float kNoScore = -3.0e38f;           // the maximum of no scores
+constexpr float kGrowth = 8.0f;                // the running maximum is replaced when a score is 2^8 beyond it: sums stay far inside fp32 and bf16
 
-template <int D>
+// A tile has 8 * kTiles rows.
+template <int D, int kTiles>
 struct StepShape {
-    static constexpr int kBlocks = D > 128 ? 1 : 2;   // on a multiprocessor
-    static constexpr int kStage = kStepPositions / kGranule * CacheFormat<D>::kBytes;
-    static constexpr int kRing = kStepWarps * kStepStages * kStage;
-    static constexpr int kPitch = D + 4;              // floats of a row's sums
-    static constexpr int kMerge = kStepWarps * kMergeRows * kPitch * 4, kSums = kStepWarps * kMergeRows * 8;
-    static constexpr int kSmem = kRing + kMerge + kSums + 8 * kStepWarps * kStepStages;
+    static constexpr int kRows = 8 * kTiles;
+    static constexpr int kBlocks = D * kTiles > 256 ? 1 : 2;             // on a multiprocessor
+    static constexpr int kGranules = D * kTiles == 256 && kTiles == 1 ? 1 : 2;   // of a unit
+    static constexpr int kPositions = kGranules * kGranule;              // of a unit
+    static constexpr int kStage = kGranules * CacheFormat<D>::kBytes;
+    static constexpr int kWarpBytes = kStepStages * kStage;
+    static constexpr int kRing = kStepWarps * kWarpBytes;
+    static constexpr bool kHeld = kTiles * D <= 128;                     // queries stay in registers
+    static constexpr int kQueries = kHeld ? 0 : kRows * D * 2;           // of a warp
+    static constexpr int kSmem = kRing + kStepWarps * kQueries + 8 * kStepWarps * kStepStages;
+    static constexpr int kPitch = D + 4;                                 // floats of a row's sums in shared memory
+    static constexpr int kPart = kRows * (D + 2);                        // floats of a tile's part in the workspace: sums, then maximum and sum of exponentials of each row
+    static constexpr int kParts = 2 + kStepWarps;                        // of a block: its own two, and each warp's end of a tile that began before
+    static_assert(kBlocks * (kSmem + 1024 + 512) <= 228 << 10, "blocks on a multiprocessor");
+    static_assert(kRows * kPitch * 4 + kRows * 8 <= kWarpBytes, "a warp's part of a tile takes the place of its copies");
 };
-// Floats of a tile's part in the workspace: its rows' sums, then maximum and sum of each row.
-template <int D>
-__host__ __device__ constexpr int part_floats(int rows) { return rows * (D + 2); }
 
 // True in the last of `n` blocks of this call to say so.  The word may hold anything before the call but for its nonce, which no other call has: the first block to come puts
 // nonce and count in, the last one takes them away, so that a replayed graph starts as the call did.
@@ -73,330 +80,474 @@ __device__ __forceinline__ bool arrive(unsigned long long *word, unsigned long l
     return true;
 }
 
-__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, bool half_type)
+// c += a b: a 16 x 16, b 16 x 8
+template <bool kHalf>
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    if (half_type)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    if constexpr (kHalf)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// An 8 x 8 matrix of 16-bit values turned round; a lane has two neighbours of row lane / 4.
+__device__ __forceinline__ uint32_t turned(uint32_t v)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
 
-// A walk over the row of units, the same in all threads of a block.
+// A walk over the row of units, the same in all threads of a warp; sequences are looked up 32 at a time.
 struct Walk {
-    int64_t x, end;       // next unit, and where the block's stretch ends
-    int64_t base;         // first unit of sequence b
-    int64_t tiles, row0;  // tiles of sequence b and kv head; its first row
-    int64_t item0, item1; // units of the piece's tile
-    int b, n, len, units; // sequence, its rows and positions, units of a tile
-    int head, first, last;   // of the piece: kv head, units [first, last)
-    int64_t tile;
+    int64_t x, end;            // next unit, and where the stretch ends
+    int64_t base, item0;       // first unit of sequence b, and of the piece's tile
+    int chunk, row0s, ns, lens;   // sequences chunk + lane: first row, rows, positions
+    int b, row0, n, len;
+    int units, tiles;          // of a tile; of a sequence and kv head
+    int head, tile, first, last;   // of the piece: kv head, tile, units [first, last)
 
-    __device__ __forceinline__ int64_t work(const CacheRows &r) const { return tiles * r.kv_heads * units; }
-    __device__ __forceinline__ void load(const CacheRows &r, int group, int rows)
+    __device__ __forceinline__ void look_up(const CacheRows &r, int from)
     {
-        row0 = row_start(r, b);
-        n = static_cast<int>(max(static_cast<int64_t>(0), (r.starts ? row_start(r, b + 1) : row0 + 1) - row0));
-        len = length_of(r, b);
-        units = max(1, (len + kStepPositions - 1) / kStepPositions);
-        tiles = (static_cast<int64_t>(n) * group + rows - 1) / rows;
+        chunk = from;
+        const int at = from + static_cast<int>(threadIdx.x & 31);
+        row0s = ns = lens = 0;
+        if (at < r.batch) {
+            const int64_t start = row_start(r, at);
+            row0s = static_cast<int>(start);
+            ns = static_cast<int>(max(static_cast<int64_t>(0), (r.starts ? row_start(r, at + 1) : start + 1) - start));
+            lens = length_of(r, at);
+        }
+    }
+    template <typename S>
+    static __device__ __forceinline__ int units_of(int len) { return max(1, (len + S::kPositions - 1) / S::kPositions); }
+    template <typename S>
+    static __device__ __forceinline__ int tiles_of(int n, int group) { return static_cast<int>((static_cast<int64_t>(n) * group + S::kRows - 1) / S::kRows); }
+    template <typename S>
+    __device__ __forceinline__ int64_t lane_work(const CacheRows &r, int group) const
+    {
+        return static_cast<int64_t>(tiles_of<S>(ns, group)) * r.kv_heads * units_of<S>(lens);
+    }
+    template <typename S>
+    __device__ __forceinline__ void enter(const CacheRows &r, int group)
+    {
+        if (b - chunk >= 32) look_up(r, b);
+        row0 = __shfl_sync(0xffffffffu, row0s, b - chunk);
+        n = __shfl_sync(0xffffffffu, ns, b - chunk);
+        len = __shfl_sync(0xffffffffu, lens, b - chunk);
+        units = units_of<S>(len);
+        tiles = tiles_of<S>(n, group);
     }
     // The next piece; false at the end.
-    __device__ __forceinline__ bool next(const CacheRows &r, int group, int rows)
+    template <typename S>
+    __device__ __forceinline__ bool next(const CacheRows &r, int group)
     {
         if (x >= end) return false;
-        for (int64_t w; x >= base + (w = work(r));) {
+        for (int64_t w; x >= base + (w = static_cast<int64_t>(tiles) * r.kv_heads * units);) {
             base += w;
             ++b;
-            load(r, group, rows);
+            enter<S>(r, group);
         }
-        const int64_t item = (x - base) / units;
+        const int64_t in = x - base;
+        const int64_t item = in >> 31 ? in / units : static_cast<int64_t>(static_cast<uint32_t>(in) / static_cast<uint32_t>(units));
         item0 = base + item * units;
-        item1 = item0 + units;
-        head = static_cast<int>(item / tiles);
-        tile = item % tiles;
+        head = static_cast<int>(tiles == 1 ? item : item / tiles);
+        tile = static_cast<int>(item - static_cast<int64_t>(head) * tiles);
         first = static_cast<int>(x - item0);
-        x = min(end, item1);
+        x = min(end, item0 + units);
         last = static_cast<int>(x - item0);
         return true;
     }
+    __device__ __forceinline__ int rows_all(int group) const { return n * group; }   // below 2^31
     // The last position that row `at` of the sequence's rows times heads sees; below 0: none.
-    __device__ __forceinline__ int limit(int64_t at, int group) const { return len - n + static_cast<int>(at / group); }
+    __device__ __forceinline__ int limit(int at, int group) const { return len - n + static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(group)); }
 };
 
-// rows of a tile: 8 * kHalves.  With 8 rows, the other eight of the matrix instructions' 16 hold what the rounding of the first eight's probabilities left over,
-// so that the products with the values are as good as fp32's; with 16 rows probabilities are rounded to the values' type (2^-9 or 2^-12 of each).
-template <int D, bool kHalf, int kHalves>
-__global__ void __launch_bounds__(kStepThreads, StepShape<D>::kBlocks)
-cache_step_kernel(const __grid_constant__ AttendArgs p)
+// The warp's stretch and its block's [x0, x1); false: the block has none.
+template <typename S>
+__device__ __forceinline__ bool begin(Walk &walk, const CacheRows &r, int group, int64_t &share, int64_t &x0, int64_t &x1)
 {
-    using F = CacheFormat<D>;
-    using S = StepShape<D>;
-    constexpr int kRows = 8 * kHalves, kGroupsAll = D / kGroup;
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int64_t warp_sums[kStepWarps];
-    __shared__ int64_t start_base;
-    __shared__ int start_b, gave_up_word, is_last;
-    volatile int *gave_up = &gave_up_word;
-    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    float *const merge = reinterpret_cast<float *>(smem + S::kRing);
-    float2 *const sums = reinterpret_cast<float2 *>(smem + S::kRing + S::kMerge);
-    const uint32_t ring = smem_addr(smem) + warp * kStepStages * S::kStage;
-    const uint32_t bars = smem_addr(smem) + S::kRing + S::kMerge + S::kSums + 8 * warp * kStepStages;
-    SQ_LINEAR_CHECK(smem_addr(smem) + S::kSmem <= smem_end(smem) && (smem_addr(smem) & 15) == 0, 2010);
-    if (threadIdx.x == 0) gave_up_word = 0;
-    if (lane == 0) {
-        for (int s = 0; s < kStepStages; ++s) bar_init(bars + 8 * s, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-
-    // the block's stretch of the units of all sequences
-    Walk walk;
-    const auto work_of = [&](int b) {
-        if (b >= p.r.batch) return static_cast<int64_t>(0);
-        Walk w;
-        w.b = b;
-        w.load(p.r, p.group, kRows);
-        return w.work(p.r);
-    };
-    int64_t sum = 0;
-    for (int b = threadIdx.x; b < p.r.batch; b += kStepThreads) sum += work_of(b);
-#pragma unroll
-    for (int s = 16; s; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-    if (lane == 0) warp_sums[warp] = sum;
-    __syncthreads();
-    int64_t total = 0;
-#pragma unroll
-    for (int w = 0; w < kStepWarps; ++w) total += warp_sums[w];
-    const int64_t share = max(static_cast<int64_t>(kStepWarps), (total + gridDim.x - 1) / gridDim.x);
-    walk.x = share * blockIdx.x;
-    walk.end = min(total, walk.x + share);
-    if (walk.x >= total) return;
-    int64_t before = 0;
-    for (int b0 = 0; b0 < p.r.batch; b0 += kStepThreads) {
-        const int64_t mine = work_of(b0 + threadIdx.x);
-        int64_t upto = mine;
+    const int lane = threadIdx.x & 31;
+    int64_t total = 0, upto = 0, mine = 0;
+    const auto scan = [&](int from) {   // 32 sequences
+        walk.look_up(r, from);
+        upto = mine = walk.lane_work<S>(r, group);
 #pragma unroll
         for (int s = 1; s < 32; s <<= 1) {
             const int64_t v = __shfl_up_sync(0xffffffffu, upto, s);
             if (lane >= s) upto += v;
         }
-        __syncthreads();
-        if (lane == 31) warp_sums[warp] = upto;
-        __syncthreads();
-        int64_t all = 0;
-#pragma unroll
-        for (int w = 0; w < kStepWarps; ++w) {
-            if (w == warp) upto += before + all;
-            all += warp_sums[w];
+        return __shfl_sync(0xffffffffu, upto, 31);
+    };
+    for (int from = 0; from < r.batch; from += 32) total += scan(from);
+    share = kStepWarps * max(static_cast<int64_t>(1), (total + kStepWarps * gridDim.x - 1) / (kStepWarps * gridDim.x));
+    x0 = share * blockIdx.x;
+    x1 = min(total, x0 + share);
+    if (x0 >= total) return false;
+    const int64_t sub = share / kStepWarps, x = min(x1, x0 + (threadIdx.x >> 5) * sub);
+    walk.x = x;
+    walk.end = min(x1, x + sub);
+    if (x >= total) return true;   // the last block's last warps
+    int64_t before = 0;
+    if (r.batch > 32) {
+        for (int from = 0;; from += 32) {   // ends, since x is below the sum of all
+            const int64_t all = scan(from);
+            if (before + all > x) break;
+            before += all;
         }
-        if (walk.x >= upto - mine && walk.x < upto) {   // one thread of all chunks
-            start_b = b0 + static_cast<int>(threadIdx.x);
-            start_base = upto - mine;
-        }
-        before += all;
-        if (before > walk.x) break;
     }
-    __syncthreads();
-    walk.b = start_b;
-    walk.base = start_base;
-    walk.load(p.r, p.group, kRows);
+    const int at = __ffs(__ballot_sync(0xffffffffu, before + upto > x)) - 1;
+    walk.base = before + __shfl_sync(0xffffffffu, upto - mine, at);
+    walk.b = walk.chunk + at;
+    walk.enter<S>(r, group);
+    return true;
+}
 
-    // copies of the warp's units, ahead of what it computes
-    Walk ahead = walk;
-    int ahead_unit = 0, fetched = 0, consumed = 0;
-    uint32_t there = 0;   // two bits a stage: which of its granules have been copied
-    bool more = ahead.next(p.r, p.group, kRows), dead = false;
-    ahead_unit = ahead.first + warp;
-    const auto fetch = [&]() {
-        while (more && ahead_unit >= ahead.last) {
-            more = ahead.next(p.r, p.group, kRows);
-            ahead_unit = ahead.first + warp;
+// Where row `at` of a tile's sequence goes.
+struct Target {
+    int64_t row, head;
+    __device__ __forceinline__ Target(const AttendArgs &p, int row0, int kv_head, int at)
+    {
+        row = row0 + static_cast<uint32_t>(at) / static_cast<uint32_t>(p.group);
+        head = static_cast<int64_t>(kv_head) * p.group + static_cast<uint32_t>(at) % static_cast<uint32_t>(p.group);
+        SQ_LINEAR_CHECK(row < p.r.rows && head < static_cast<int64_t>(p.r.kv_heads) * p.group, 2013);
+    }
+};
+__device__ __forceinline__ void store_lse(const AttendArgs &p, const Target &to, float top, float l)
+{
+    p.lse[to.row * p.r.kv_heads * p.group + to.head] = l == 0.0f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+}
+template <bool kHalf>
+__device__ __forceinline__ void finish4(const AttendArgs &p, const Target &to, int column, float4 v, float top, float l)
+{
+    const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t *out = p.out + to.row * p.out_stride + to.head * p.out_head + column;
+    const uint32_t w0 = to_16x2<kHalf>(v.x * inverse, v.y * inverse), w1 = to_16x2<kHalf>(v.z * inverse, v.w * inverse);
+    if (p.out_vector) {
+        *reinterpret_cast<uint2 *>(out) = make_uint2(w0, w1);
+    } else {
+        out[0] = static_cast<uint16_t>(w0); out[1] = static_cast<uint16_t>(w0 >> 16);
+        out[2] = static_cast<uint16_t>(w1); out[3] = static_cast<uint16_t>(w1 >> 16);
+    }
+    if (p.lse && column == 0) store_lse(p, to, top, l);
+}
+// Sums of parts of a tile, one part after the other; the maximum is taken ahead of the sums it scales.
+struct Joined {
+    float top = kNoScore, l = 0.0f;
+    float4 v = make_float4(0, 0, 0, 0);
+    template <int kCount>
+    __device__ __forceinline__ void add(const float4 (&x)[kCount], const float2 (&ml)[kCount])   // ml: maximum and sum; a row that has seen nothing has sum 0
+    {
+        float next = top;
+#pragma unroll
+        for (int j = 0; j < kCount; ++j)
+            if (ml[j].y != 0.0f) next = fmaxf(next, ml[j].x);
+        const float old = l == 0.0f ? 0.0f : exp2_fast(top - next);
+        l *= old;
+        v.x *= old; v.y *= old; v.z *= old; v.w *= old;
+        top = next;
+#pragma unroll
+        for (int j = 0; j < kCount; ++j) {
+            if (ml[j].y == 0.0f) continue;
+            const float factor = exp2_fast(ml[j].x - top);
+            l = fmaf(ml[j].y, factor, l);
+            v.x = fmaf(x[j].x, factor, v.x); v.y = fmaf(x[j].y, factor, v.y); v.z = fmaf(x[j].z, factor, v.z); v.w = fmaf(x[j].w, factor, v.w);
         }
-        if (!more) return;
-        const int stage = fetched % kStepStages, position = ahead_unit * kStepPositions;
-        const int seen = ahead.limit(min(static_cast<int64_t>(ahead.n) * p.group, (ahead.tile + 1) * kRows) - 1, p.group);   // by the tile's last row
-        const int granules = p.r.page_size / kGranule;
-        const uint8_t *from[2];
+    }
+    // What warps [w, until) of the block have left in shared memory.
+    template <typename S>
+    __device__ __forceinline__ void add_warps(const uint8_t *smem, int w, int until, int row, int column)
+    {
+        float4 x[kStepWarps];
+        float2 ml[kStepWarps];
+#pragma unroll
+        for (int j = 0; j < kStepWarps; ++j) {
+            const float *at = reinterpret_cast<const float *>(smem + min(w + j, until - 1) * S::kWarpBytes);
+            x[j] = *reinterpret_cast<const float4 *>(at + row * S::kPitch + column);
+            ml[j] = reinterpret_cast<const float2 *>(at + S::kRows * S::kPitch)[row];
+            if (w + j >= until) ml[j].y = 0.0f;
+        }
+        add(x, ml);
+    }
+};
+
+// What a warp leaves for the end of the block: the tile that its stretch ends in.
+struct Left {
+    int64_t item0;      // first unit, -1: none
+    int64_t item1;
+    int row0, rows_all, head, tile;
+};
+
+// Keys and values are the first operands of the matrix instructions, 16 positions (16 channels) high, and rows of queries (of probabilities) are the second ones'
+// columns, so that none of the instructions' work goes to rows that do not exist, and sums take few registers.  What the rounding of a probability to 16
+// bits leaves over goes through a second instruction: products with the values are as good as fp32's.
+template <int D, bool kHalf, int kTiles>
+__global__ void __launch_bounds__(kStepThreads, (StepShape<D, kTiles>::kBlocks))
+cache_step_kernel(const __grid_constant__ AttendArgs p)
+{
+    using F = CacheFormat<D>;
+    using S = StepShape<D, kTiles>;
+    constexpr int kRows = S::kRows, kGroupsAll = D / kGroup;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ Left left_over[kStepWarps], first_end;   // first_end: of a tile that begins before the block and ends in the first warp's stretch
+    __shared__ int gave_up_word, is_last[2];
+    volatile int *gave_up = &gave_up_word;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    uint8_t *const ring = smem + warp * S::kWarpBytes;
+    uint4 *const held_q = reinterpret_cast<uint4 *>(smem + S::kRing + warp * S::kQueries);
+    const uint32_t bars = smem_addr(smem) + S::kRing + kStepWarps * S::kQueries + 8 * warp * kStepStages;
+    SQ_LINEAR_CHECK(smem_addr(smem) + S::kSmem <= smem_end(smem) && (smem_addr(smem) & 15) == 0, 2010);
+    if (threadIdx.x == 0) {
+        gave_up_word = 0;
+        first_end.item0 = -1;
+    }
+    if (lane == 0) {
+        left_over[warp].item0 = -1;
+        for (int s = 0; s < kStepStages; ++s) bar_init(bars + 8 * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    Walk walk;
+    int64_t share, x0, x1;
+    if (!begin<S>(walk, p.r, p.group, share, x0, x1)) return;   // all threads of the block
+    __syncthreads();
+
+    // Copies of the warp's units, ahead of what it computes: the numbers of the next granules lie in the warp's lanes, looked up together.
+    Walk ahead = walk;
+    constexpr int kBatch = 32 / S::kGranules;   // units
+    int ahead_unit = 0, listed = 0, taken = 0, granule = -1;
+    unsigned fetched = 0, consumed = 0;
+    uint32_t there = 0;   // which granules of a stage have been copied: two bits a stage
+    bool more = ahead.next<S>(p.r, p.group), dead = false;
+    ahead_unit = ahead.first;
+    const auto fetch = [&]() {
+        if (taken == listed) {
+            if (more && ahead_unit == ahead.last) {
+                more = ahead.next<S>(p.r, p.group);
+                ahead_unit = ahead.first;
+            }
+            if (!more) return;
+            listed = min(kBatch, ahead.last - ahead_unit);
+            taken = 0;
+            const int at = (ahead_unit + lane / S::kGranules) * S::kPositions + lane % S::kGranules * kGranule;
+            const int seen = ahead.limit(min(ahead.rows_all(p.group) - ahead.tile * kRows, kRows) - 1 + ahead.tile * kRows, p.group);   // by the tile's last row
+            granule = -1;
+            if (lane / S::kGranules < listed && at <= seen) {
+                const int column = at / p.r.page_size;
+                const int64_t page = page_of(p.r, ahead.b, column);
+                const int granules = p.r.page_size / kGranule;
+                SQ_LINEAR_CHECK(column < p.r.width, 2011);
+                if (page >= 0) granule = static_cast<int>((page * p.r.kv_heads + ahead.head) * granules + (at - column * p.r.page_size) / kGranule);
+            }
+            ahead_unit += listed;
+        }
+        const unsigned stage = fetched % kStepStages;
+        int from[S::kGranules];
         uint32_t have = 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = position + i * kGranule;
-            if (at > seen) continue;
-            const int column = at / p.r.page_size;
-            const int64_t page = page_of(p.r, ahead.b, column);
-            if (page < 0) continue;
-            have |= 1u << i;
-            from[i] = p.cache + ((page * p.r.kv_heads + ahead.head) * granules + (at - column * p.r.page_size) / kGranule) * F::kBytes;
-            SQ_LINEAR_CHECK(column < p.r.width && from[i] >= p.cache && from[i] + F::kBytes <= p.cache + p.r.page_count * p.r.kv_heads * granules * F::kBytes, 2011);
+        for (int i = 0; i < S::kGranules; ++i) {
+            from[i] = __shfl_sync(0xffffffffu, granule, taken * S::kGranules + i);
+            have |= from[i] >= 0 ? 1u << i : 0u;
         }
         if (elect_one()) {
-            const uint32_t to = ring + stage * S::kStage;
-            bar_expect(bars + 8 * stage, __popc(have) * F::kBytes);
+            const uint32_t to = smem_addr(ring) + stage * S::kStage, bar = bars + 8 * stage;
+            bar_expect(bar, __popc(have) * F::kBytes);
+            if (S::kGranules == 2 && have == 3 && from[S::kGranules - 1] == from[0] + 1) {
+                bulk_load(to, p.cache + static_cast<int64_t>(from[0]) * F::kBytes, S::kStage, bar);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (have >> i & 1) bulk_load(to + i * F::kBytes, from[i], F::kBytes, bars + 8 * stage);
+                for (int i = 0; i < S::kGranules; ++i)
+                    if (have >> i & 1) bulk_load(to + i * F::kBytes, p.cache + static_cast<int64_t>(from[i]) * F::kBytes, F::kBytes, bar);
+            }
         }
         __syncwarp();
         there = (there & ~(3u << (2 * stage))) | have << (2 * stage);
         ++fetched;
-        ahead_unit += kStepWarps;
+        ++taken;
     };
 #pragma unroll
     for (int s = 0; s < kStepStages; ++s) fetch();
 
     const CodePairs<kHalf> pairs;
-    const int heads = p.r.kv_heads * p.group;
-    while (walk.next(p.r, p.group, kRows)) {
-        const int64_t at0 = walk.tile * kRows, rows_all = static_cast<int64_t>(walk.n) * p.group;   // of the sequence's rows times heads
-        uint32_t q[kGroupsAll][kHalves][4];
-        int limit[kHalves];
+    while (walk.next<S>(p.r, p.group)) {
+        const int at0 = walk.tile * kRows, rows_all = walk.rows_all(p.group);   // of the sequence's rows times heads
+        // queries: lane (g, c) has 8 channels of each group of row g
+        uint4 q[S::kHeld ? kTiles * kGroupsAll : 1];
+        const auto query = [&](int i) {   // tile i / kGroupsAll, group i % kGroupsAll
+            const int at = at0 + 8 * (i / kGroupsAll) + g;
+            if (at >= rows_all) return make_uint4(0, 0, 0, 0);
+            const Target to(p, walk.row0, walk.head, at);
+            return load8(p.q + to.row * p.q_stride + to.head * p.q_head + kGroup * (i % kGroupsAll) + 8 * c, p.q_vector);
+        };
+        if constexpr (S::kHeld) {
 #pragma unroll
-        for (int r = 0; r < kHalves; ++r) {
-            const int64_t at = at0 + 8 * r + g;
-            limit[r] = walk.limit(min(at, rows_all - 1), p.group);
-            const uint16_t *from = p.q + (walk.row0 + at / p.group) * p.q_stride + (static_cast<int64_t>(walk.head) * p.group + at % p.group) * p.q_head;
+            for (int i = 0; i < kTiles * kGroupsAll; ++i) q[i] = query(i);
+        } else {
 #pragma unroll
-            for (int n = 0; n < kGroupsAll; ++n) {
-                const uint4 v = at < rows_all ? load8(from + kGroup * n + 8 * c, p.q_vector) : make_uint4(0, 0, 0, 0);
-                q[n][r][0] = v.x; q[n][r][1] = v.y; q[n][r][2] = v.z; q[n][r][3] = v.w;
-            }
+            for (int i = 0; i < kTiles * kGroupsAll; ++i) held_q[i * 32 + lane] = query(i);   // read back by the lane itself
         }
-        const int seen_least = walk.limit(at0, p.group), seen_most = walk.limit(min(rows_all, at0 + kRows) - 1, p.group);
-        float o[D / 8][4], most[kHalves], total_p[kHalves];
+        // the lane's rows: 8 r + 2 c and the next
+        int limit[kTiles][2];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+        for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-        for (int r = 0; r < kHalves; ++r) {
-            most[r] = -INFINITY;
-            total_p[r] = 0.0f;
+            for (int e = 0; e < 2; ++e) limit[r][e] = walk.limit(min(at0 + 8 * r + 2 * c + e, rows_all - 1), p.group);
+        const int seen_least = walk.limit(at0, p.group), seen_most = walk.limit(min(rows_all - at0, kRows) - 1 + at0, p.group);
+        float o[kTiles][D / 16][4], most[kTiles][2], total_p[kTiles][2];
+#pragma unroll
+        for (int r = 0; r < kTiles; ++r) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.0f;
+            most[r][0] = most[r][1] = kNoScore;
+            total_p[r][0] = total_p[r][1] = 0.0f;
         }
 
-        for (int unit = walk.first + warp; unit < walk.last; unit += kStepWarps) {
-            if (dead) break;
-            const int stage = consumed % kStepStages;
-            if (!bar_wait_warp(bars + 8 * stage, consumed / kStepStages & 1, gave_up)) {
+        for (int unit = dead ? walk.last : walk.first; unit < walk.last; ++unit) {
+            const unsigned stage = consumed % kStepStages;
+            // most copies have landed by now
+            if (!__all_sync(0xffffffffu, bar_try(bars + 8 * stage, consumed / kStepStages & 1)) && !bar_wait_warp(bars + 8 * stage, consumed / kStepStages & 1, gave_up)) {
                 dead = true;
                 break;
             }
             SQ_LINEAR_CHECK(consumed < fetched, 2012);
-            const uint32_t have = there >> (2 * stage) & 3u, data = ring + stage * S::kStage;
-            const int position = unit * kStepPositions;
-            if (have) {
-                // scores of 32 positions, 8 at a time; the lane has positions 8 i + 2 c and the next of row g (and g + 8)
-                float s[4][4];
+            const uint32_t have = there >> (2 * stage) & 3u;
+            const uint8_t *const data = ring + stage * S::kStage;
+            const int position = unit * S::kPositions;
+            const auto attend = [&](auto some_hidden) {
+                constexpr bool kMasked = decltype(some_hidden)::value;
+                // scores: the lane has positions g and g + 8 of a granule for its two rows
+                float s[kTiles][S::kGranules][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.0f;
-                    if (!(have >> (i >> 1) & 1)) continue;
-                    const uint32_t granule = data + (i >> 1) * F::kBytes;
-                    const int t = 8 * (i & 1) + g;
-                    uint32_t scales[kGroupsAll / 2];
-                    if constexpr (kGroupsAll == 2) {
-                        scales[0] = lds32(granule + F::key_scale(0, 0) + t * 4);
-                    } else {
+                for (int i = 0; i < S::kGranules; ++i) {
 #pragma unroll
-                        for (int n = 0; n < kGroupsAll / 4; ++n) {
-                            const uint2 v = lds64(granule + F::key_scale(0, 0) + t * (2 * kGroupsAll) + 8 * n);
-                            scales[2 * n] = v.x;
-                            scales[2 * n + 1] = v.y;
+                    for (int r = 0; r < kTiles; ++r) s[r][i][0] = s[r][i][1] = s[r][i][2] = s[r][i][3] = 0.0f;
+                    if (kMasked && !(have >> i & 1)) continue;
+                    const uint8_t *const at = data + i * F::kBytes;
+                    uint32_t scales[2][kGroupsAll / 2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint8_t *const from = at + F::kKeyScales + (g + 8 * h) * (2 * kGroupsAll);
+                        if constexpr (kGroupsAll == 2) {
+                            scales[h][0] = *reinterpret_cast<const uint32_t *>(from);
+                        } else {
+#pragma unroll
+                            for (int n = 0; n < kGroupsAll / 4; ++n) {
+                                const uint2 v = *reinterpret_cast<const uint2 *>(from + 8 * n);
+                                scales[h][2 * n] = v.x;
+                                scales[h][2 * n + 1] = v.y;
+                            }
                         }
                     }
 #pragma unroll
                     for (int a = 0; a < F::kSlabs; ++a) {
-                        uint32_t w[4];
-                        if constexpr (F::kGroups == 2) {
-                            const uint2 v = lds64(granule + t * (4 * F::kWords) + 8 * c);
-                            w[0] = v.x; w[1] = v.y;
-                        } else {
-                            const uint4 v = lds128(granule + a * (64 * F::kWords) + t * (4 * F::kWords) + 16 * c);
-                            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                        uint32_t w[2][4];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint8_t *const from = at + a * (64 * F::kWords) + (g + 8 * h) * (4 * F::kWords) + c * F::kWords;
+                            if constexpr (F::kGroups == 2) {
+                                const uint2 v = *reinterpret_cast<const uint2 *>(from);
+                                w[h][0] = v.x; w[h][1] = v.y;
+                            } else {
+                                const uint4 v = *reinterpret_cast<const uint4 *>(from);
+                                w[h][0] = v.x; w[h][1] = v.y; w[h][2] = v.z; w[h][3] = v.w;
+                            }
                         }
 #pragma unroll
                         for (int j = 0; j < F::kGroups; ++j) {
                             const int n = a * F::kGroups + j;
-                            const uint32_t scale = scale_twice<kHalf>(scales[n / 2], n & 1);
-                            uint32_t k[4];
-                            pairs(w[j], scale, pairs.offset(scale), k);
-                            const uint32_t (&x)[4] = q[n][0], (&y)[4] = q[n][kHalves - 1];
-                            mma_16816(s[i], x[0], kHalves > 1 ? y[0] : 0u, x[1], kHalves > 1 ? y[1] : 0u, k[0], k[1], kHalf);
-                            mma_16816(s[i], x[2], kHalves > 1 ? y[2] : 0u, x[3], kHalves > 1 ? y[3] : 0u, k[2], k[3], kHalf);
+                            uint32_t k[2][4];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                pairs(w[h][j], pairs.scales(scale_twice<kHalf>(scales[h][n / 2], n & 1)), k[h]);
+                            }
+#pragma unroll
+                            for (int r = 0; r < kTiles; ++r) {
+                                const uint4 x = S::kHeld ? q[r * kGroupsAll + n] : held_q[(r * kGroupsAll + n) * 32 + lane];
+                                mma_16816<kHalf>(s[r][i], k[0][0], k[1][0], k[0][1], k[1][1], x.x, x.y);
+                                mma_16816<kHalf>(s[r][i], k[0][2], k[1][2], k[0][3], k[1][3], x.z, x.w);
+                            }
                         }
                     }
                 }
-                const bool masked = position + kStepPositions - 1 > seen_least || have != 3;   // some row does not see all
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2 * kHalves; ++e) {
-                        s[i][e] *= p.scale_log2;
-                        if (masked && (position + 8 * i + 2 * c + (e & 1) > limit[e >> 1] || !(have >> (i >> 1) & 1))) s[i][e] = -INFINITY;
-                    }
-                float reached[kHalves];
+                const auto hidden = [&](int r, int i, int e) {
+                    return kMasked && (position + i * kGranule + g + 8 * (e >> 1) > limit[r][e & 1] || !(have >> i & 1));
+                };
+                // exponents against the maximum so far
+                float x[kTiles][S::kGranules][4];
                 bool grows = false;
 #pragma unroll
-                for (int r = 0; r < kHalves; ++r) {
-                    float v = -INFINITY;
+                for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v = fmaxf(v, fmaxf(s[i][2 * r], s[i][2 * r + 1]));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
-                    reached[r] = v;
-                    grows |= v > most[r] + kGrowth;
-                }
+                    for (int i = 0; i < S::kGranules; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[r][i][e] = hidden(r, i, e) ? -INFINITY : fmaf(s[r][i][e], p.scale_log2, -most[r][e & 1]);
+                            grows |= x[r][i][e] > kGrowth;
+                        }
                 if (__any_sync(0xffffffffu, grows)) {
-                    float factor[kHalves];
 #pragma unroll
-                    for (int r = 0; r < kHalves; ++r) {
-                        const float next = fmaxf(most[r], reached[r]);
-                        factor[r] = next == most[r] ? 1.0f : exp2_fast(most[r] - next);
-                        most[r] = next;
-                        total_p[r] *= factor[r];
-                    }
+                    for (int r = 0; r < kTiles; ++r) {
+                        float factor[2];
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        o[i][0] *= factor[0];
-                        o[i][1] *= factor[0];
-                        o[i][2] *= factor[kHalves - 1];
-                        o[i][3] *= factor[kHalves - 1];
-                    }
-                }
-                // probabilities as the first operand of the product with the values
-                uint32_t hi[4][kHalves], lo[4];
+                        for (int e = 0; e < 2; ++e) {
+                            float next = most[r][e];
 #pragma unroll
-                for (int r = 0; r < kHalves; ++r) {
-                    const float from = most[r] == -INFINITY ? 0.0f : most[r];
+                            for (int i = 0; i < S::kGranules; ++i)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = exp2_fast(s[i][2 * r] - from), b = exp2_fast(s[i][2 * r + 1] - from);
-                        total_p[r] += a + b;
-                        hi[i][r] = to_16x2<kHalf>(a, b);
-                        if (kHalves == 1) lo[i] = to_16x2<kHalf>(a - to_float<kHalf>(static_cast<uint16_t>(hi[i][r])), b - to_float<kHalf>(static_cast<uint16_t>(hi[i][r] >> 16)));
+                                for (int h = 0; h < 2; ++h) next = fmaxf(next, hidden(r, i, 2 * h + e) ? kNoScore : s[r][i][2 * h + e] * p.scale_log2);
+#pragma unroll
+                            for (int j = 4; j < 32; j <<= 1) next = fmaxf(next, __shfl_xor_sync(0xffffffffu, next, j));
+                            factor[e] = exp2_fast(most[r][e] - next);
+                            most[r][e] = next;
+                            total_p[r][e] *= factor[e];
+#pragma unroll
+                            for (int i = 0; i < S::kGranules; ++i)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) x[r][i][2 * h + e] = hidden(r, i, 2 * h + e) ? -INFINITY : fmaf(s[r][i][2 * h + e], p.scale_log2, -next);
+                        }
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[r][i][e] *= factor[e & 1];
                     }
                 }
+                // probabilities, turned round: the lane has positions 2 c and the next (and 8 on) for row g
+                uint32_t hi[kTiles][S::kGranules][2], lo[kTiles][S::kGranules][2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (!(have >> i & 1)) continue;
-                    const uint32_t granule = data + i * F::kBytes;
-                    const int left = seen_most + 1 - (position + i * kGranule);   // positions of the granule that any row sees
+                for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+                    for (int i = 0; i < S::kGranules; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float a = exp2_fast(x[r][i][2 * h]), b = exp2_fast(x[r][i][2 * h + 1]);
+                            total_p[r][0] += a;
+                            total_p[r][1] += b;
+                            const uint32_t v = to_16x2<kHalf>(a, b);
+                            hi[r][i][h] = turned(v);
+                            lo[r][i][h] = turned(to_16x2<kHalf>(a - to_float<kHalf>(static_cast<uint16_t>(v)), b - to_float<kHalf>(static_cast<uint16_t>(v >> 16))));
+                        }
+#pragma unroll
+                for (int i = 0; i < S::kGranules; ++i) {
+                    if (kMasked && !(have >> i & 1)) continue;
+                    const uint8_t *const at = data + i * F::kBytes;
+                    [[maybe_unused]] const int left = seen_most + 1 - (position + i * kGranule);   // positions of the granule that any row sees
                     // scales of positions 2 c, 2 c + 1 and 2 c + 8, 2 c + 9 for the groups of the lane's words
                     uint32_t scales[2][D / 64];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
 #pragma unroll
                         for (int a = 0; a < F::kSlabs; ++a) {
-                            const uint32_t at = granule + F::kValueScales + a * (32 * F::kGroups) + (c + 4 * h) * (4 * F::kGroups) + (g >> 2) * (2 * F::kGroups);
+                            const uint8_t *const from = at + F::kValueScales + a * (32 * F::kGroups) + (c + 4 * h) * (4 * F::kGroups) + (g >> 2) * (2 * F::kGroups);
                             if constexpr (F::kGroups == 2) {
-                                scales[h][0] = lds32(at);
+                                scales[h][0] = *reinterpret_cast<const uint32_t *>(from);
                             } else {
-                                const uint2 v = lds64(at);
+                                const uint2 v = *reinterpret_cast<const uint2 *>(from);
                                 scales[h][2 * a] = v.x;
                                 scales[h][2 * a + 1] = v.y;
                             }
                         }
                     }
-                    if (masked) {
+                    if constexpr (kMasked) {
                         // positions behind the last one may hold anything
                         bool odd = false;
 #pragma unroll
@@ -419,157 +570,234 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
                             for (int t = 0; t < min(left, kGranule); ++t)
 #pragma unroll
                                 for (int n = 0; n < kGroupsAll; ++n) {
-                                    uint16_t v;
-                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(granule + F::value_scale(0, n) + (t >> 1) * (4 * F::kGroups) + 2 * (t & 1)) : "memory");
-                                    if ((v & 0x7f80u) != 0x7f80u || (c >> 1) != (n & 1)) continue;
+                                    const uint16_t v = *reinterpret_cast<const uint16_t *>(at + F::value_scale(0, n) + (t >> 1) * (4 * F::kGroups) + 2 * (t & 1));
+                                    if ((v & 0x7f80u) != 0x7f80u || (g >> 2) != (n & 1)) continue;   // channels 64 (n / 2) + 8 g and on
 #pragma unroll
-                                    for (int r = 0; r < kHalves; ++r)
-                                        if (position + i * kGranule + t <= limit[r])
+                                    for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-                                            for (int e = 0; e < 8; ++e) o[n / 2 * 8 + e][2 * r] = o[n / 2 * 8 + e][2 * r + 1] = __uint_as_float(0x7fffffffu);
+                                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                            for (int e = 0; e < 4; ++e)
+                                                if (position + i * kGranule + t <= limit[r][e & 1]) o[r][n / 2 * 4 + j][e] = __uint_as_float(0x7fffffffu);
                                 }
                         }
                     }
 #pragma unroll
                     for (int a = 0; a < F::kSlabs; ++a) {
+                        constexpr int kLaneWords = F::kWords / 8;
                         uint32_t w[2][4];   // [pair of positions][position % 2, word / 8]
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             if constexpr (F::kGroups == 2) {
-                                const uint2 v = lds64(granule + F::kValues + ((c + 4 * h) * 8 + g) * 8);
+                                const uint2 v = *reinterpret_cast<const uint2 *>(at + F::kValues + ((c + 4 * h) * 8 + g) * 8);
                                 w[h][0] = v.x; w[h][1] = v.y;
                             } else {
-                                const uint4 v = lds128(granule + F::kValues + a * (64 * F::kWords) + ((c + 4 * h) * 8 + g) * 16);
+                                const uint4 v = *reinterpret_cast<const uint4 *>(at + F::kValues + a * (64 * F::kWords) + ((c + 4 * h) * 8 + g) * 16);
                                 w[h][0] = v.x; w[h][1] = v.y; w[h][2] = v.z; w[h][3] = v.w;
                             }
                         }
-                        constexpr int kLaneWords = F::kWords / 8;
 #pragma unroll
                         for (int m = 0; m < kLaneWords; ++m) {
                             const int n = a * kLaneWords + m;
                             uint32_t v[2][2][4];   // [pair of positions][channel % 2][channel / 2]
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                const uint32_t scale = scale_pair<kHalf>(scales[h][n]), off = pairs.offset(scale);
-                                pairs(__byte_perm(w[h][m], w[h][kLaneWords + m], 0x5410), scale, off, v[h][0]);
-                                pairs(__byte_perm(w[h][m], w[h][kLaneWords + m], 0x7632), scale, off, v[h][1]);
+                                const PairScales<kHalf> scale = pairs.scales(scale_pair<kHalf>(scales[h][n]));
+                                pairs(__byte_perm(w[h][m], w[h][kLaneWords + m], 0x5410), scale, v[h][0]);
+                                pairs(__byte_perm(w[h][m], w[h][kLaneWords + m], 0x7632), scale, v[h][1]);
                             }
+                            // rows of the first operand: channels 64 n + 8 g + 2 j, and from 8 on 64 n + 8 g + 2 j + 1
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                mma_16816(o[n * 8 + e], hi[2 * i][0], kHalves > 1 ? hi[2 * i][kHalves - 1] : lo[2 * i], hi[2 * i + 1][0],
-                                          kHalves > 1 ? hi[2 * i + 1][kHalves - 1] : lo[2 * i + 1], v[0][e & 1][e >> 1], v[1][e & 1][e >> 1], kHalf);
+                            for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) mma_16816<kHalf>(o[r][n * 4 + j], v[0][0][j], v[0][1][j], v[1][0][j], v[1][1][j], hi[r][i][0], hi[r][i][1]);
+#pragma unroll
+                            for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) mma_16816<kHalf>(o[r][n * 4 + j], v[0][0][j], v[0][1][j], v[1][0][j], v[1][1][j], lo[r][i][0], lo[r][i][1]);
                         }
                     }
                 }
-            }
+            };
+            // few units have positions that some row does not see, or pages that are not there
+            if (have == (1u << S::kGranules) - 1 && position + S::kPositions - 1 <= seen_least) attend(std::false_type{});
+            else if (have) attend(std::true_type{});
             ++consumed;
             __syncwarp();   // all lanes have read the stage
-            if (!*gave_up) fetch();
+            fetch();
         }
 
-        // the warps' sums, then those of the other blocks that have a part of the tile
-        const int64_t block0 = walk.item0 / share, block1 = (walk.item1 - 1) / share;
-        const unsigned blocks = static_cast<unsigned>(block1 - block0 + 1);
-        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (blockIdx.x == block0 && walk.item0 % share != 0);
-        float *const part = p.parts + slot * part_floats<D>(kRows);
+        float l[kTiles][2];
 #pragma unroll
-        for (int r = 0; r < kHalves; ++r) {
-            float l = total_p[r];
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
-            __syncthreads();   // the sums before have been read
-            if (c == 0) sums[warp * kMergeRows + g] = make_float2(most[r], l);
-            float *to = merge + (warp * kMergeRows + g) * S::kPitch;
+        for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-            for (int n = 0; n < D / 64; ++n)
+            for (int e = 0; e < 2; ++e) {
+                l[r][e] = total_p[r][e];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {   // channels 64 n + 16 c + 8 h + e
+                for (int x = 4; x < 32; x <<= 1) l[r][e] += __shfl_xor_sync(0xffffffffu, l[r][e], x);
+            }
+        // 8 neighbouring channels, 64 n + 8 g and on, of the lane's row e of 8 r
+        const auto sums8 = [&](int r, int e, int n, float (&v)[8]) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] = o[r][4 * n + j][e];
+                v[2 * j + 1] = o[r][4 * n + j][2 + e];
+            }
+        };
+        if (walk.first == 0 && walk.last == walk.units) {   // the whole tile
+            if (dead) continue;
+#pragma unroll
+            for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int at = at0 + 8 * r + 2 * c + e;
+                    if (at >= rows_all) continue;
+                    const Target to(p, walk.row0, walk.head, at);
+                    const float inverse = l[r][e] == 0.0f ? 0.0f : 1.0f / l[r][e];
+                    uint16_t *out = p.out + to.row * p.out_stride + to.head * p.out_head + 8 * g;
+#pragma unroll
+                    for (int n = 0; n < D / 64; ++n) {
+                        float v[8];
+                        uint32_t w[4];
+                        sums8(r, e, n, v);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = to_16x2<kHalf>(v[2 * j] * inverse, v[2 * j + 1] * inverse);
+                        if (p.out_vector) {
+                            *reinterpret_cast<uint4 *>(out + 64 * n) = make_uint4(w[0], w[1], w[2], w[3]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) out[64 * n + j] = static_cast<uint16_t>(w[j / 2] >> (16 * (j & 1)));
+                        }
+                    }
+                    if (p.lse && g == 0) store_lse(p, to, most[r][e], l[r][e]);
+                }
+            continue;
+        }
+        const bool ends_here = walk.x == walk.end;   // the last piece of the warp's stretch: nothing is being copied any more
+        // otherwise the end of a tile that began before: what the block has of it if the block's stretch begins in it too
+        float *const global = p.parts + (static_cast<int64_t>(blockIdx.x) * S::kParts + (warp == 0 ? 0 : 2 + warp)) * S::kPart;
+        float *const local = reinterpret_cast<float *>(ring);
+        SQ_LINEAR_CHECK(ends_here || (walk.first > 0 && walk.last == walk.units), 2015);
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = 8 * r + 2 * c + e;
+#pragma unroll
+                for (int n = 0; n < D / 64; ++n) {
                     float v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = kHalves == 1 ? o[n * 8 + e][h] + o[n * 8 + e][2 + h] : o[n * 8 + e][2 * r + h];
-                    *reinterpret_cast<float4 *>(to + 64 * n + 16 * c + 8 * h) = make_float4(v[0], v[1], v[2], v[3]);
-                    *reinterpret_cast<float4 *>(to + 64 * n + 16 * c + 8 * h + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                    sums8(r, e, n, v);
+                    const float4 a = make_float4(v[0], v[1], v[2], v[3]), b = make_float4(v[4], v[5], v[6], v[7]);
+                    if (ends_here) {
+                        float4 *to = reinterpret_cast<float4 *>(local + row * S::kPitch + 64 * n + 8 * g);
+                        to[0] = a;
+                        to[1] = b;
+                    } else {
+                        float4 *to = reinterpret_cast<float4 *>(global + row * D + 64 * n + 8 * g);
+                        __stcg(to, a);
+                        __stcg(to + 1, b);
+                    }
                 }
-            __syncthreads();
-            for (int i = threadIdx.x; i < kMergeRows * (D / 4); i += kStepThreads) {
-                const int row = i / (D / 4), column = i % (D / 4) * 4;
-                float top = -INFINITY, l_all = 0.0f;
-                float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll
-                for (int w = 0; w < kStepWarps; ++w) top = fmaxf(top, sums[w * kMergeRows + row].x);
-#pragma unroll
-                for (int w = 0; w < kStepWarps; ++w) {
-                    const float2 ml = sums[w * kMergeRows + row];
-                    const float factor = exp2_fast(ml.x - top);
-                    const float4 x = *reinterpret_cast<const float4 *>(merge + (w * kMergeRows + row) * S::kPitch + column);
-                    if (ml.y == 0.0f) continue;   // such a row has seen nothing
-                    l_all = fmaf(ml.y, factor, l_all);
-                    v.x = fmaf(x.x, factor, v.x); v.y = fmaf(x.y, factor, v.y); v.z = fmaf(x.z, factor, v.z); v.w = fmaf(x.w, factor, v.w);
+                if (g == 0) {
+                    if (ends_here) reinterpret_cast<float2 *>(local + kRows * S::kPitch)[row] = make_float2(most[r][e], l[r][e]);
+                    else __stcg(reinterpret_cast<float2 *>(global + kRows * D) + row, make_float2(most[r][e], l[r][e]));
                 }
-                if (blocks > 1) {
-                    __stcg(reinterpret_cast<float4 *>(part + (8 * r + row) * D + column), v);
-                    if (column == 0) __stcg(reinterpret_cast<float2 *>(part + kRows * D) + 8 * r + row, make_float2(top, l_all));
-                    continue;
-                }
-                const int64_t at = at0 + 8 * r + row;
-                if (at >= rows_all || *gave_up) continue;
-                const int64_t q_row = walk.row0 + at / p.group, q_head = static_cast<int64_t>(walk.head) * p.group + at % p.group;
-                const float inverse = l_all == 0.0f ? 0.0f : 1.0f / l_all;
-                SQ_LINEAR_CHECK(q_row < p.r.rows && q_head < heads, 2013);
-                uint16_t *out = p.out + q_row * p.out_stride + q_head * p.out_head + column;
-                const uint32_t w0 = to_16x2<kHalf>(v.x * inverse, v.y * inverse), w1 = to_16x2<kHalf>(v.z * inverse, v.w * inverse);
-                if (p.out_vector) {
-                    *reinterpret_cast<uint2 *>(out) = make_uint2(w0, w1);
-                } else {
-                    out[0] = static_cast<uint16_t>(w0); out[1] = static_cast<uint16_t>(w0 >> 16);
-                    out[2] = static_cast<uint16_t>(w1); out[3] = static_cast<uint16_t>(w1 >> 16);
-                }
-                if (p.lse && column == 0) p.lse[q_row * heads + q_head] = l_all == 0.0f ? -INFINITY : (top + log2f(l_all)) * 0.69314718055994531f;
+            }
+        if (lane == 0 && (ends_here || warp == 0)) (ends_here ? left_over[warp] : first_end) = Left{walk.item0, walk.item0 + walk.units, walk.row0, rows_all, walk.head, walk.tile};
+    }
+    // no copy of a block that has given up may land after its end, or in a part of a tile
+    for (; consumed < fetched; ++consumed) bar_drain(bars + 8 * (consumed % kStepStages), consumed / kStepStages & 1);
+    __syncthreads();
+
+    // parts of tiles that the block has, each begun by a warp's end, with those of the warps that follow it
+    Left mine[2];               // the block's own parts of tiles that others have parts of, too: the one that begins before it, the one that ends after it
+    mine[0].item0 = mine[1].item0 = -1;
+    const int64_t sub = share / kStepWarps;
+    for (int w = 0; w < kStepWarps; ++w) {
+        const Left t = left_over[w];
+        if (t.item0 < 0 || (w > 0 && left_over[w - 1].item0 == t.item0)) continue;
+        int until = w + 1;      // warps [w, until) end in the tile, and the end of it may be the beginning of the next one's stretch
+        while (until < kStepWarps && left_over[until].item0 == t.item0) ++until;
+        const bool further = t.item1 > x0 + until * sub && x0 + until * sub < x1;
+        const bool alone = t.item0 >= x0 && t.item1 <= x1;
+        float *const part = p.parts + (static_cast<int64_t>(blockIdx.x) * S::kParts + (t.item0 >= x0)) * S::kPart;
+        for (int i = threadIdx.x; i < kRows * (D / 4); i += kStepThreads) {
+            const int row = i / (D / 4), column = i % (D / 4) * 4;
+            Joined sum;
+            sum.add_warps<S>(smem, w, until, row, column);
+            if (further) {
+                const float *at = p.parts + (static_cast<int64_t>(blockIdx.x) * S::kParts + 2 + until) * S::kPart;
+                const float4 x1[1] = {__ldcg(reinterpret_cast<const float4 *>(at + row * D + column))};
+                const float2 ml1[1] = {__ldcg(reinterpret_cast<const float2 *>(at + kRows * D) + row)};
+                sum.add(x1, ml1);
+            }
+            if (!alone) {
+                __stcg(reinterpret_cast<float4 *>(part + row * D + column), sum.v);
+                if (column == 0) __stcg(reinterpret_cast<float2 *>(part + kRows * D) + row, make_float2(sum.top, sum.l));
+            } else if (t.tile * kRows + row < t.rows_all && !*gave_up) {
+                finish4<kHalf>(p, Target(p, t.row0, t.head, t.tile * kRows + row), column, sum.v, sum.top, sum.l);
             }
         }
-        if (blocks > 1) {
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) is_last = arrive(p.tickets + block0, p.nonce, blocks);
-            __syncthreads();
-            if (is_last) {
-                __threadfence();
-                for (int i = threadIdx.x; i < kRows * (D / 4); i += kStepThreads) {
-                    const int row = i / (D / 4), column = i % (D / 4) * 4;
-                    const int64_t at = at0 + row;
-                    if (at >= rows_all || *gave_up) continue;
-                    const float *from = p.parts + (2 * block0 + (walk.item0 % share != 0)) * part_floats<D>(kRows);
-                    float top = -INFINITY, l_all = 0.0f;
-                    float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-                    for (int64_t b = block0; b <= block1; ++b) {
-                        const float *mine = b == block0 ? from : p.parts + 2 * b * part_floats<D>(kRows);
-                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(mine + row * D + column));
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(mine + kRows * D) + row);
-                        if (ml.y == 0.0f) continue;
-                        const float next = fmaxf(top, ml.x), old = l_all == 0.0f ? 0.0f : exp2_fast(top - next), factor = exp2_fast(ml.x - next);
-                        l_all = fmaf(ml.y, factor, l_all * old);
-                        v.x = fmaf(x.x, factor, v.x * old); v.y = fmaf(x.y, factor, v.y * old); v.z = fmaf(x.z, factor, v.z * old); v.w = fmaf(x.w, factor, v.w * old);
-                        top = next;
-                    }
-                    const int64_t q_row = walk.row0 + at / p.group, q_head = static_cast<int64_t>(walk.head) * p.group + at % p.group;
-                    const float inverse = l_all == 0.0f ? 0.0f : 1.0f / l_all;
-                    SQ_LINEAR_CHECK(q_row < p.r.rows && q_head < heads, 2014);
-                    uint16_t *out = p.out + q_row * p.out_stride + q_head * p.out_head + column;
-                    const uint32_t w0 = to_16x2<kHalf>(v.x * inverse, v.y * inverse), w1 = to_16x2<kHalf>(v.z * inverse, v.w * inverse);
-                    if (p.out_vector) {
-                        *reinterpret_cast<uint2 *>(out) = make_uint2(w0, w1);
-                    } else {
-                        out[0] = static_cast<uint16_t>(w0); out[1] = static_cast<uint16_t>(w0 >> 16);
-                        out[2] = static_cast<uint16_t>(w1); out[3] = static_cast<uint16_t>(w1 >> 16);
-                    }
-                    if (p.lse && column == 0) p.lse[q_row * heads + q_head] = l_all == 0.0f ? -INFINITY : (top + log2f(l_all)) * 0.69314718055994531f;
-                }
-            }
+        if (!alone) mine[t.item0 >= x0] = t;
+    }
+    if (first_end.item0 >= 0) mine[0] = first_end;
+    // tiles that other blocks have parts of: who comes last puts them together
+    if (mine[0].item0 < 0 && mine[1].item0 < 0) return;
+    __threadfence();
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const Left &t = mine[k];
+        if (threadIdx.x == 32 * k && t.item0 >= 0) {
+            const int64_t block0 = t.item0 / share, block1 = (t.item1 - 1) / share;
+            is_last[k] = arrive(p.tickets + block0, p.nonce, static_cast<unsigned>(block1 - block0 + 1));
         }
     }
-    // no copy of a block that has given up may land after its end
-    for (; consumed < fetched; ++consumed) bar_drain(bars + 8 * (consumed % kStepStages), consumed / kStepStages & 1);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const Left &t = mine[k];
+        if (t.item0 < 0 || !is_last[k]) continue;
+        __threadfence();
+        const int64_t block0 = t.item0 / share;
+        const int blocks = static_cast<int>((t.item1 - 1) / share - block0 + 1);
+        const float *const from = p.parts + block0 * S::kParts * S::kPart;
+        // each warp joins every eighth part, row by row, then the block the warps'
+        constexpr int kPieces = kRows * (D / 4) / 32, kAtOnce = kPieces < 8 ? kPieces : 8;
+        float *const local = reinterpret_cast<float *>(ring);
+        __syncthreads();   // what was there has been read
+        for (int i0 = 0; i0 < kPieces; i0 += kAtOnce) {
+            Joined sum[kAtOnce];
+            for (int b = warp; b < blocks; b += kStepWarps) {
+                const float *at = from + (static_cast<int64_t>(b) * S::kParts + (b == 0)) * S::kPart;
+                float4 x[kAtOnce][1];
+                float2 ml[kAtOnce][1];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    const int i = (i0 + j) * 32 + lane;
+                    x[j][0] = __ldcg(reinterpret_cast<const float4 *>(at) + i);
+                    ml[j][0] = __ldcg(reinterpret_cast<const float2 *>(at + kRows * D) + i / (D / 4));
+                }
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) sum[j].add(x[j], ml[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int i = (i0 + j) * 32 + lane, row = i / (D / 4), column = i % (D / 4) * 4;
+                *reinterpret_cast<float4 *>(local + row * S::kPitch + column) = sum[j].v;
+                if (column == 0) reinterpret_cast<float2 *>(local + kRows * S::kPitch)[row] = make_float2(sum[j].top, sum[j].l);
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < kRows * (D / 4); i += kStepThreads) {
+            const int row = i / (D / 4), column = i % (D / 4) * 4;
+            if (t.tile * kRows + row >= t.rows_all || *gave_up) continue;
+            Joined sum;
+            sum.add_warps<S>(smem, 0, kStepWarps, row, column);
+            finish4<kHalf>(p, Target(p, t.row0, t.head, t.tile * kRows + row), column, sum.v, sum.top, sum.l);
+        }
+    }
 }
 
 }  // namespace sq
