@@ -423,6 +423,7 @@ int64_t squant_cache_attention_workspace(const squant_cache_attention_args *args
 /* Which kernel a call with these arguments takes: 0 (no rows), one of the values below, or the call's negative error.  No GPU is needed. */
 #define SQUANT_CACHE_STEP 1     /* tiles of 8 rows (tokens times heads of a group) */
 #define SQUANT_CACHE_STEP_16 2  /* tiles of 16 rows */
+#define SQUANT_CACHE_PROMPT 3   /* tiles of 128 rows, on the tensor cores' own memory */
 int squant_cache_attention_plan(const squant_cache_attention_args *args);
 int squant_cache_attention(const squant_cache_attention_args *args, void *cuda_stream);
 

@@ -9,6 +9,7 @@
 #include <random>
 
 #include "cache_device.cuh"
+#include "cache_prompt.cuh"
 #include "cache_rows.cuh"
 #include "cache_step.cuh"
 #include "squant_host.h"
@@ -170,7 +171,8 @@ int64_t most_rows(const squant_cache_attention_args &a)
 int plan(const squant_cache_attention_args &a)
 {
     if (nothing(a.rows)) return 0;
-    return most_rows(a) * a.group <= 8 ? SQUANT_CACHE_STEP : SQUANT_CACHE_STEP_16;
+    const int64_t rows = most_rows(a) * a.group;
+    return rows <= 8 ? SQUANT_CACHE_STEP : rows <= 16 ? SQUANT_CACHE_STEP_16 : SQUANT_CACHE_PROMPT;
 }
 
 // Thread blocks and the workspace's parts.
@@ -193,10 +195,28 @@ StepPlan step_plan(const squant_cache_attention_args &a)
     return s;
 }
 template <int D>
+StepPlan prompt_plan(const squant_cache_attention_args &a)
+{
+    using S = sq::PromptShape<D>;
+    const squant_cache_rows &r = a.rows;
+    const int64_t tiles = (r.rows * a.group + static_cast<int64_t>(std::min<int64_t>(r.batch, r.rows)) * (sq::kPromptRows - 1)) / sq::kPromptRows;
+    const int64_t positions = std::min<int64_t>(static_cast<int64_t>(r.width) * r.page_size, 1ll << 30);
+    const double units = static_cast<double>(tiles) * r.kv_heads * (positions / sq::kPromptUnit + 2);
+    StepPlan s;
+    s.blocks = static_cast<int64_t>(std::min<double>(kB200Sms * S::kBlocks, units));
+    s.tickets = up(8 * s.blocks, 128);
+    s.bytes = s.tickets + 2 * s.blocks * S::kPart * 4;
+    return s;
+}
+template <int D>
 int64_t attention_bytes(const squant_cache_attention_args &a)
 {
-    const int which = plan(a);
-    return !which ? 0 : which == SQUANT_CACHE_STEP ? step_plan<D, 1>(a).bytes : step_plan<D, 2>(a).bytes;
+    switch (plan(a)) {
+        case SQUANT_CACHE_STEP: return step_plan<D, 1>(a).bytes;
+        case SQUANT_CACHE_STEP_16: return step_plan<D, 2>(a).bytes;
+        case SQUANT_CACHE_PROMPT: return prompt_plan<D>(a).bytes;
+        default: return 0;
+    }
 }
 int64_t attention_bytes(const squant_cache_attention_args &a)
 {
@@ -214,10 +234,8 @@ unsigned long long nonce()
     return n ? n : nonce();
 }
 
-template <int D, bool kHalf, int kTiles>
-int step(const squant_cache_attention_args &a, cudaStream_t stream)
+sq::AttendArgs attend_args(const squant_cache_attention_args &a, const StepPlan &s)
 {
-    const StepPlan s = step_plan<D, kTiles>(a);
     sq::AttendArgs p{};
     p.cache = static_cast<const uint8_t *>(a.rows.data);
     p.r = rows_of(a.rows);
@@ -235,15 +253,31 @@ int step(const squant_cache_attention_args &a, cudaStream_t stream)
     p.tickets = static_cast<unsigned long long *>(a.workspace);
     p.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(a.workspace) + s.tickets);
     p.nonce = nonce();
+    return p;
+}
+template <int D, bool kHalf, int kTiles>
+int step(const squant_cache_attention_args &a, cudaStream_t stream)
+{
+    const StepPlan s = step_plan<D, kTiles>(a);
     static std::atomic<bool> ready[kMaxDevices];
-    return launch_large(sq::cache_step_kernel<D, kHalf, kTiles>, ready, s.blocks, sq::kStepThreads, sq::StepShape<D, kTiles>::kSmem, stream, p);
+    return launch_large(sq::cache_step_kernel<D, kHalf, kTiles>, ready, s.blocks, sq::kStepThreads, sq::StepShape<D, kTiles>::kSmem, stream, attend_args(a, s));
+}
+template <int D, bool kHalf>
+int prompt(const squant_cache_attention_args &a, cudaStream_t stream)
+{
+    const StepPlan s = prompt_plan<D>(a);
+    static std::atomic<bool> ready[kMaxDevices];
+    return launch_large(sq::cache_prompt_kernel<D, kHalf>, ready, s.blocks, sq::kPromptThreads, sq::PromptShape<D>::kSmem, stream, attend_args(a, s));
 }
 template <int D>
 int attention(const squant_cache_attention_args &a, cudaStream_t stream)
 {
     const bool half = a.dtype == SQUANT_FP16;
-    if (plan(a) == SQUANT_CACHE_STEP) return half ? step<D, true, 1>(a, stream) : step<D, false, 1>(a, stream);
-    return half ? step<D, true, 2>(a, stream) : step<D, false, 2>(a, stream);
+    switch (plan(a)) {
+        case SQUANT_CACHE_STEP: return half ? step<D, true, 1>(a, stream) : step<D, false, 1>(a, stream);
+        case SQUANT_CACHE_STEP_16: return half ? step<D, true, 2>(a, stream) : step<D, false, 2>(a, stream);
+        default: return half ? prompt<D, true>(a, stream) : prompt<D, false>(a, stream);
+    }
 }
 
 }  // namespace

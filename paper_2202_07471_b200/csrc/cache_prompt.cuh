@@ -1,0 +1,621 @@
+// Attention over the cache for many rows: prompts, parts of prompts, many drafted tokens (formulas in cache_step.cuh).
+//
+// A tile is 128 rows of one sequence and kv head, tokens times the query heads of the group.  Its queries stay in shared memory; for 128 positions at a time (64 with 256
+// channels) converter warps turn keys and values into 16-bit floats for the tensor cores:
+//
+//   S = Q K^T   [128 x 128] in tensor memory, a row a lane: softmax warps own a row a thread
+//   P = exp2(scale S - m) over S's place, 16 bits;  O += P V, P from tensor memory
+//
+// The maximum m is replaced only when a score is 2^8 beyond it; then O is scaled, which the softmax warps do between two products.  Per 128 positions the tensor cores work 1,024
+// clocks, the 128 x 128 exponentials take as long, and so do softmax's and the conversion's instructions, so two blocks share a multiprocessor: one's products
+// run while the other one's exponentials do.
+//
+// Work is cut as in cache_step.cuh: the units (128 positions that a tile sees, so that a causal prompt's later tiles have more) of all tiles stand in one row, each block
+// takes an equal stretch, and a tile that several blocks have parts of is put together, in order, by the one that ends last.
+#pragma once
+
+#include "cache_step.cuh"
+
+namespace sq {
+
+constexpr int kPromptRows = 128, kPromptUnit = 128;   // rows of a tile, positions of a unit
+constexpr int kPromptSoftmax = 4, kPromptConverters = 4;   // warps
+constexpr int kPromptThreads = 32 * (kPromptSoftmax + kPromptConverters + 2);   // and one for the copies, one for the tensor cores
+constexpr int kRawGranules = 4, kRawStages = 3;       // keys or values of 64 positions as they are, ahead of the converters
+
+template <int D>
+struct PromptShape {
+    static constexpr int kBlocks = D > 128 ? 1 : 2;                  // on a multiprocessor
+    static constexpr int kPositions = D > 128 ? 64 : 128;            // of a score tile
+    static constexpr int kGranules = kPositions / kGranule;
+    static constexpr int kQueries = kPromptRows * D * 2, kOperand = kPositions * D * 2, kPanel = kPositions * 128, kQueryPanel = kPromptRows * 128;
+    static constexpr int kRawGranule = 9 * D, kRaw = kRawGranules * kRawGranule;   // codes, then scales
+    static constexpr int kParts = kGranules / kRawGranules;          // stages of a score tile's keys
+    static constexpr int kBars = 2 * kRawStages + 9;
+    static constexpr int kNeeded = 1024 + kQueries + 2 * kOperand + kRawStages * kRaw + 8 * kBars;
+    // no more blocks on a multiprocessor than its tensor memory has room for
+    static constexpr int kSmem = kBlocks == 2 && kNeeded < (80 << 10) ? 80 << 10 : kNeeded;
+    static constexpr int kScores = 0, kSums = 128, kColumns = D > 128 ? 512 : 256;   // tensor memory
+    static constexpr int kPart = kPromptRows * (D + 2);              // floats of a tile's part in the workspace
+    static_assert(kBlocks * (kSmem + 1024 + 256) <= 228 << 10, "blocks on a multiprocessor");
+    static_assert((kBlocks + 1) * kSmem > 228 << 10 && kBlocks * kColumns <= 512 && kSums + D <= kColumns, "the tensor memory that blocks ask for is always there");
+};
+
+// The walk over units of 128 positions.  The tile t of a sequence sees its first tokens, and those of its rows up to the tile's last:
+//   units(t) = ceil((len - n + floor((128 t + 127) / group) + 1) / 128) = floor((t + q) / group),   q = floor((group (len - n + 128) + 127) / 128),
+// which is one too many at most, for the last tile.  Sums of floor(i / group) have a closed form, and so does the row of all sequences' units.
+struct PromptWalk {
+    int64_t x, end, base, item0;
+    int chunk, row0s, ns, lens;   // sequences chunk + lane
+    int b, row0, n, len, tiles;
+    int head, tile, first, last, units;   // of the piece
+    int64_t q, span;              // span: units of a kv head of sequence b
+
+    static __device__ __forceinline__ int64_t floors(int64_t n, int group)   // sum of floor(i / group) below n
+    {
+        const int64_t k = n >> 31 ? n / group : static_cast<int64_t>(static_cast<uint32_t>(n) / static_cast<uint32_t>(group));
+        return k * (k - 1) / 2 * group + k * (n - k * group);
+    }
+    static __device__ __forceinline__ int64_t offset_of(int n, int len, int group)
+    {
+        return (static_cast<int64_t>(group) * (max(0, len - n) + kPromptUnit) + kPromptRows - 1) / kPromptRows;
+    }
+    static __device__ __forceinline__ int tiles_of(int n, int group) { return static_cast<int>((static_cast<int64_t>(n) * group + kPromptRows - 1) / kPromptRows); }
+    __device__ __forceinline__ void look_up(const CacheRows &r, int from)
+    {
+        chunk = from;
+        const int at = from + static_cast<int>(threadIdx.x & 31);
+        row0s = ns = lens = 0;
+        if (at < r.batch) {
+            const int64_t start = row_start(r, at);
+            row0s = static_cast<int>(start);
+            ns = static_cast<int>(max(static_cast<int64_t>(0), (r.starts ? row_start(r, at + 1) : start + 1) - start));
+            lens = length_of(r, at);
+        }
+    }
+    __device__ __forceinline__ int64_t lane_work(const CacheRows &r, int group) const
+    {
+        const int64_t o = offset_of(ns, lens, group);
+        return (floors(o + tiles_of(ns, group), group) - floors(o, group)) * r.kv_heads;
+    }
+    __device__ __forceinline__ void enter(const CacheRows &r, int group)
+    {
+        if (b - chunk >= 32) look_up(r, b);
+        row0 = __shfl_sync(0xffffffffu, row0s, b - chunk);
+        n = __shfl_sync(0xffffffffu, ns, b - chunk);
+        len = __shfl_sync(0xffffffffu, lens, b - chunk);
+        tiles = tiles_of(n, group);
+        q = offset_of(n, len, group);
+        span = floors(q + tiles, group) - floors(q, group);
+    }
+    __device__ __forceinline__ bool next(const CacheRows &r, int group)
+    {
+        if (x >= end) return false;
+        while (x >= base + span * r.kv_heads) {
+            base += span * r.kv_heads;
+            ++b;
+            enter(r, group);
+        }
+        const int64_t in = x - base;
+        head = static_cast<int>(in / span);
+        const int64_t at = in - head * span, before = floors(q, group);
+        int lo = 0, hi = tiles;   // the tile that unit `at` of the head's is in
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (floors(q + mid, group) - before <= at) lo = mid;
+            else hi = mid;
+        }
+        tile = lo;
+        item0 = base + head * span + (floors(q + lo, group) - before);
+        units = static_cast<int>((lo + q) / group);
+        first = static_cast<int>(x - item0);
+        x = min(end, item0 + units);
+        last = static_cast<int>(x - item0);
+        return true;
+    }
+    __device__ __forceinline__ int rows_all(int group) const { return n * group; }
+    __device__ __forceinline__ int limit(int at, int group) const { return len - n + static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(group)); }
+    __device__ __forceinline__ int seen_least(int group) const { return limit(tile * kPromptRows, group); }
+    __device__ __forceinline__ int seen_most(int group) const { return limit(min(rows_all(group) - tile * kPromptRows, kPromptRows) - 1 + tile * kPromptRows, group); }
+    // Score tiles of the piece that any row sees.
+    template <int kPositions>
+    __device__ __forceinline__ int steps(int group) const
+    {
+        const int seen = seen_most(group) + 1 - first * kPromptUnit;
+        return seen <= 0 ? 0 : min((last - first) * (kPromptUnit / kPositions), (seen + kPositions - 1) / kPositions);
+    }
+};
+// The block's stretch; false: it has none.  Each warp for itself.
+__device__ __forceinline__ bool begin(PromptWalk &walk, const CacheRows &r, int group, int64_t &share)
+{
+    const int lane = threadIdx.x & 31;
+    int64_t total = 0, upto = 0, mine = 0;
+    const auto scan = [&](int from) {
+        walk.look_up(r, from);
+        upto = mine = walk.lane_work(r, group);
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            const int64_t v = __shfl_up_sync(0xffffffffu, upto, s);
+            if (lane >= s) upto += v;
+        }
+        return __shfl_sync(0xffffffffu, upto, 31);
+    };
+    for (int from = 0; from < r.batch; from += 32) total += scan(from);
+    share = max(static_cast<int64_t>(1), (total + gridDim.x - 1) / gridDim.x);
+    walk.x = share * blockIdx.x;
+    walk.end = min(total, walk.x + share);
+    if (walk.x >= total) return false;
+    int64_t before = 0;
+    if (r.batch > 32) {
+        for (int from = 0;; from += 32) {   // ends, since x is below the sum of all
+            const int64_t all = scan(from);
+            if (before + all > walk.x) break;
+            before += all;
+        }
+    }
+    const int at = __ffs(__ballot_sync(0xffffffffu, before + upto > walk.x)) - 1;
+    walk.base = before + __shfl_sync(0xffffffffu, upto - mine, at);
+    walk.b = walk.chunk + at;
+    walk.enter(r, group);
+    return true;
+}
+
+// The first operand in tensor memory.
+__device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)), "n"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
+          "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+          "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <int D, bool kHalf>
+__global__ void __launch_bounds__(kPromptThreads, PromptShape<D>::kBlocks)
+cache_prompt_kernel(const __grid_constant__ AttendArgs p)
+{
+    using F = CacheFormat<D>;
+    using S = PromptShape<D>;
+    constexpr int kGroupsAll = D / kGroup;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *const smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_addr(smem);
+    const uint32_t smem_q = base, smem_k = base + S::kQueries, smem_v = smem_k + S::kOperand, smem_c = smem_v + S::kOperand;
+    const uint32_t bars = smem_c + kRawStages * S::kRaw;
+    SQ_LINEAR_CHECK(bars + 8 * S::kBars <= smem_end(smem_raw) && (bars & 7) == 0, 2020);
+    const auto raw_full = [&](int s) { return bars + 8 * s; };
+    const auto raw_empty = [&](int s) { return bars + 8 * (kRawStages + s); };
+    const uint32_t queries_full = bars + 16 * kRawStages, keys_full = queries_full + 8, keys_empty = queries_full + 16, values_full = queries_full + 24,
+                   values_empty = queries_full + 32, scores_full = queries_full + 40, weights_full = queries_full + 48, sums_full = queries_full + 56,
+                   together = queries_full + 64;
+    __shared__ uint32_t tmem_base;
+    __shared__ int gave_up_word, is_last;
+    __shared__ uint32_t granules_there[4];       // of the last score tiles, by their number
+    __shared__ int no_number[2][kGroupsAll];     // of the last pieces: the first position whose value group has no number
+    volatile int *gave_up = &gave_up_word;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    PromptWalk walk;
+    int64_t share;
+    if (!begin(walk, p.r, p.group, share)) return;   // all threads of the block
+
+    if (threadIdx.x == 0) {
+        gave_up_word = 0;
+        for (int s = 0; s < kRawStages; ++s) {
+            bar_init(raw_full(s), 1);
+            bar_init(raw_empty(s), kPromptConverters);
+        }
+        bar_init(queries_full, kPromptSoftmax);
+        bar_init(keys_full, kPromptConverters);
+        bar_init(keys_empty, 1);
+        bar_init(values_full, kPromptConverters);
+        bar_init(values_empty, 1);
+        bar_init(scores_full, 1);
+        bar_init(weights_full, kPromptSoftmax);
+        bar_init(sums_full, 1);
+        bar_init(together, kPromptSoftmax);
+        for (int i = 0; i < 2 * kGroupsAll; ++i) no_number[i / kGroupsAll][i % kGroupsAll] = 0x7fffffff;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kPromptSoftmax + kPromptConverters + 1) tmem_alloc(smem_addr(&tmem_base), S::kColumns);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base;
+
+    if (warp < kPromptSoftmax) {
+        const uint32_t mine = tmem + (static_cast<uint32_t>(32 * warp) << 16);   // the warp's lanes of tensor memory
+        uint32_t tiles_done = 0, pieces = 0, joins = 0;
+        bool ok = true;
+        while (ok && walk.next(p.r, p.group)) {
+            const int row = 32 * warp + lane, rows_all = walk.rows_all(p.group), at = walk.tile * kPromptRows + row;
+            const bool valid = at < rows_all;
+            const Target to(p, walk.row0, walk.head, min(at, rows_all - 1));
+            const int limit = walk.limit(min(at, rows_all - 1), p.group);
+            const int steps = walk.steps<S::kPositions>(p.group), seen_least = walk.seen_least(p.group);
+            const bool idle = walk.tile * kPromptRows + 32 * warp >= rows_all;   // all rows of the warp
+            float most = kNoScore, total = 0.0f;
+            if (steps > 0) {
+                const uint16_t *from = p.q + to.row * p.q_stride + to.head * p.q_head;
+#pragma unroll 8
+                for (int j = 0; j < D / 8; ++j) {
+                    const uint4 v = valid ? load8(from + 8 * j, p.q_vector) : make_uint4(0, 0, 0, 0);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem_q + j / 8 * S::kQueryPanel + row * 128 + ((j ^ row) & 7) * 16),
+                                 "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(queries_full);
+            }
+            for (int i = 0; i < steps; ++i, ++tiles_done) {
+                ok = bar_wait_warp(scores_full, tiles_done & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                const int position = walk.first * kPromptUnit + i * S::kPositions;
+                const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[tiles_done & 3]);
+                const bool masked = position + S::kPositions - 1 > seen_least || have != (1u << S::kGranules) - 1;
+                if (!idle) {
+                    float top = kNoScore;
+#pragma unroll
+                    for (int j = 0; j < S::kPositions; j += 32) {
+                        uint32_t s[32];
+                        tmem_ld32(mine + S::kScores + j, s);
+                        if (masked) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                top = fmaxf(top, position + j + e > limit || !(have >> ((j + e) / kGranule) & 1) ? kNoScore : __uint_as_float(s[e]) * p.scale_log2);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(s[e]) * p.scale_log2);
+                        }
+                    }
+                    if (__any_sync(0xffffffffu, top > most + kGrowth)) {
+                        const float next = fmaxf(top, most), factor = exp2_fast(most - next);
+                        most = next;
+                        total *= factor;
+                        if (i > 0) {   // the products with the values of the tiles before have been made
+#pragma unroll
+                            for (int j = 0; j < D; j += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(mine + S::kSums + j, o);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                                tmem_st32(mine + S::kSums + j, o);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < S::kPositions; j += 32) {
+                        uint32_t s[32], w[16];
+                        tmem_ld32(mine + S::kScores + j, s);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float x[2];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                x[h] = fmaf(__uint_as_float(s[e + h]), p.scale_log2, -most);
+                                if (masked && (position + j + e + h > limit || !(have >> ((j + e + h) / kGranule) & 1))) x[h] = -INFINITY;
+                                x[h] = exp2_fast(x[h]);
+                                total += x[h];
+                            }
+                            w[e / 2] = to_16x2<kHalf>(x[0], x[1]);
+                        }
+                        tmem_st16(mine + S::kScores + j / 2, w);   // the scores there have been read
+                    }
+                    tmem_st_wait();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(weights_full);
+            }
+            if (!ok) break;
+            const bool whole = walk.first == 0 && walk.last == walk.units;
+            if (steps > 0) {
+                ok = bar_wait_warp(sums_full, pieces & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+            }
+            const int64_t block0 = walk.item0 / share;
+            float *const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (walk.item0 >= share * blockIdx.x)) * S::kPart;
+            const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+            for (int j = 0; j < D; j += 32) {
+                uint32_t o[32];
+                if (steps > 0) {
+                    tmem_ld32(mine + S::kSums + j, o);
+                    const bool none = *const_cast<volatile int *>(&no_number[pieces & 1][j / kGroup]) <= limit;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = none ? 0x7fffffffu : o[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0;
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        __stcg(reinterpret_cast<float4 *>(part + row * D + j + e), make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
+                                                                                                 __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])));
+                } else if (valid) {
+                    uint16_t *out = p.out + to.row * p.out_stride + to.head * p.out_head + j;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) w[h] = to_16x2<kHalf>(__uint_as_float(o[e + 2 * h]) * inverse, __uint_as_float(o[e + 2 * h + 1]) * inverse);
+                        if (p.out_vector) {
+                            *reinterpret_cast<uint4 *>(out + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < 8; ++h) out[e + h] = static_cast<uint16_t>(w[h / 2] >> (16 * (h & 1)));
+                        }
+                    }
+                }
+            }
+            if (whole && valid && p.lse) store_lse(p, to, most, total);
+            if (!whole) __stcg(reinterpret_cast<float2 *>(part + kPromptRows * D) + row, make_float2(most, total));
+            tc_fence_before();
+            // all have read the sums and what goes with them, and written their part
+            if (!whole) __threadfence();
+            __syncwarp();
+            if (lane == 0) bar_arrive(together);
+            ok = bar_wait_warp(together, joins++ & 1, gave_up);
+            if (!ok) break;
+            if (steps > 0) {
+                if (threadIdx.x < kGroupsAll) no_number[pieces & 1][threadIdx.x] = 0x7fffffff;
+                ++pieces;
+            }
+            if (whole) continue;
+            const int blocks = static_cast<int>((walk.item0 + walk.units - 1) / share - block0 + 1);
+            if (threadIdx.x == 0) is_last = arrive(p.tickets + block0, p.nonce, blocks);
+            __syncwarp();
+            if (lane == 0) bar_arrive(together);
+            ok = bar_wait_warp(together, joins++ & 1, gave_up);
+            if (!ok) break;
+            if (!*const_cast<volatile int *>(&is_last)) continue;
+            __threadfence();
+            const float *const parts = p.parts + 2 * block0 * S::kPart;
+            for (int i = threadIdx.x; i < kPromptRows * (D / 4); i += 32 * kPromptSoftmax) {
+                const int r = i / (D / 4), column = i % (D / 4) * 4;
+                if (walk.tile * kPromptRows + r >= rows_all) break;
+                Joined sum;
+                constexpr int kAtOnce = 4;
+                for (int b0 = 0; b0 < blocks; b0 += kAtOnce) {
+                    float4 x[kAtOnce];
+                    float2 ml[kAtOnce];
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k) {
+                        const int b = min(b0 + k, blocks - 1);
+                        const float *from = parts + (2 * static_cast<int64_t>(b) + (b == 0)) * S::kPart;
+                        x[k] = __ldcg(reinterpret_cast<const float4 *>(from + r * D + column));
+                        ml[k] = __ldcg(reinterpret_cast<const float2 *>(from + kPromptRows * D) + r);
+                        if (b0 + k >= blocks) ml[k].y = 0.0f;
+                    }
+                    sum.add(x, ml);
+                }
+                finish4<kHalf>(p, Target(p, walk.row0, walk.head, walk.tile * kPromptRows + r), column, sum.v, sum.top, sum.l);
+            }
+        }
+    } else if (warp < kPromptSoftmax + kPromptConverters) {
+        const int thread = threadIdx.x - 32 * kPromptSoftmax;
+        const CodePairs<kHalf> pairs;
+        uint32_t stages = 0, tiles_done = 0, pieces = 0;
+        bool ok = true;
+        while (ok && walk.next(p.r, p.group)) {
+            const int steps = walk.steps<S::kPositions>(p.group), seen_most = walk.seen_most(p.group);
+            for (int i = 0; ok && i < steps; ++i, ++tiles_done) {
+                const int position = walk.first * kPromptUnit + i * S::kPositions;
+#pragma unroll 1
+                for (int part = 0; part < 2 * S::kParts; ++part, ++stages) {
+                    const bool value = part >= S::kParts;
+                    const int half = value ? part - S::kParts : part, s = stages % kRawStages;
+                    if (half == 0 && tiles_done > 0) {   // the product with what is there has been made
+                        ok = bar_wait_warp(value ? values_empty : keys_empty, (tiles_done - 1) & 1, gave_up);
+                        if (!ok) break;
+                    }
+                    ok = bar_wait_warp(raw_full(s), stages / kRawStages & 1, gave_up);
+                    if (!ok) break;
+                    const uint8_t *const raw = smem + (smem_c - base) + s * S::kRaw;
+                    const uint32_t to = (value ? smem_v : smem_k);
+                    const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[tiles_done & 3]) >> (half * kRawGranules);
+                    if (!value) {
+                        // (position, word % 4): neighbouring lanes have the words % 4 of positions t and t + 4, whose 16-byte pieces are in different banks
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            const int unit = thread + 128 * n, c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8;   // 0 .. 63
+                            const uint8_t *const granule = raw + t / kGranule * S::kRawGranule;
+                            uint32_t scales[kGroupsAll / 2];
+#pragma unroll
+                            for (int j = 0; j < kGroupsAll / 2; ++j) scales[j] = *reinterpret_cast<const uint32_t *>(granule + 8 * D + t % kGranule * (2 * kGroupsAll) + 4 * j);
+#pragma unroll
+                            for (int a = 0; a < F::kSlabs; ++a) {
+                                uint32_t w[4];
+                                const uint8_t *const from = granule + a * (64 * F::kWords) + t % kGranule * (4 * F::kWords) + c * F::kWords;
+                                if constexpr (F::kGroups == 2) {
+                                    const uint2 v = *reinterpret_cast<const uint2 *>(from);
+                                    w[0] = v.x; w[1] = v.y;
+                                } else {
+                                    const uint4 v = *reinterpret_cast<const uint4 *>(from);
+                                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                                }
+                                const int row = half * 64 + t;
+#pragma unroll
+                                for (int j = 0; j < F::kGroups; ++j) {
+                                    const int g = a * F::kGroups + j, word = 4 * g + c;
+                                    uint32_t o[4];
+                                    pairs(w[j], pairs.scales(scale_twice<kHalf>(scales[g / 2], g & 1)), o);
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + word / 8 * S::kPanel + row * 128 + ((word ^ row) & 7) * 16),
+                                                 "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                                }
+                            }
+                        }
+                    } else {
+                        // (pair of positions, word % 8)
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            const int unit = thread + 128 * n, g = unit & 7, pair = unit >> 3;   // 0 .. 31
+                            const uint8_t *const granule = raw + pair / 8 * S::kRawGranule;
+#pragma unroll
+                            for (int a = 0; a < F::kSlabs; ++a) {
+                                constexpr int kLaneWords = F::kWords / 8;
+                                uint32_t w[4], scales[kLaneWords];
+                                const uint8_t *const from = granule + a * (64 * F::kWords) + (pair % 8 * 8 + g) * (8 * kLaneWords);
+                                if constexpr (kLaneWords == 1) {
+                                    const uint2 v = *reinterpret_cast<const uint2 *>(from);
+                                    w[0] = v.x; w[1] = v.y;
+                                } else {
+                                    const uint4 v = *reinterpret_cast<const uint4 *>(from);
+                                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                                }
+#pragma unroll
+                                for (int m = 0; m < kLaneWords; ++m)
+                                    scales[m] = *reinterpret_cast<const uint32_t *>(granule + 8 * D + a * (32 * F::kGroups) + pair % 8 * (4 * F::kGroups) + (g >> 2) * (2 * F::kGroups) + 4 * m);
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    const int row = half * 64 + 2 * pair + h;
+                                    const bool seen = position + row <= seen_most && (have >> (pair / 8) & 1);
+#pragma unroll
+                                    for (int m = 0; m < kLaneWords; ++m) {
+                                        uint32_t scale = h ? scales[m] >> 16 : scales[m] & 0xffffu;
+                                        if (!seen) scale = 0;   // may hold anything
+                                        if ((scale & 0x7f80u) == 0x7f80u) {   // no number: for rows that see the position only, see the end of the tile
+                                            scale = 0;
+                                            atomicMin(&no_number[pieces & 1][a * F::kGroups + 2 * m + (g >> 2)], position + row);
+                                        }
+                                        uint32_t o[4];
+                                        pairs(w[h * kLaneWords + m], pairs.scales(scale_twice<kHalf>(scale, false)), o);
+                                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (a * kLaneWords + m) * S::kPanel + row * 128 + ((g ^ row) & 7) * 16),
+                                                     "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                                    }
+                                }
+                            }
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        bar_arrive(raw_empty(s));
+                        if (half == S::kParts - 1) bar_arrive(value ? values_full : keys_full);
+                    }
+                }
+            }
+            if (steps > 0) ++pieces;
+        }
+    } else if (warp == kPromptSoftmax + kPromptConverters) {
+        uint32_t stages = 0, tiles_done = 0;
+        bool ok = true;
+        const int granules = p.r.page_size / kGranule;
+        while (ok && walk.next(p.r, p.group)) {
+            const int steps = walk.steps<S::kPositions>(p.group), seen_most = walk.seen_most(p.group);
+            for (int i = 0; ok && i < steps; ++i, ++tiles_done) {
+                const int at = walk.first * kPromptUnit + i * S::kPositions + lane * kGranule;
+                int granule = -1;
+                if (lane < S::kGranules && at <= seen_most) {
+                    const int column = at / p.r.page_size;
+                    const int64_t page = page_of(p.r, walk.b, column);
+                    SQ_LINEAR_CHECK(column < p.r.width, 2022);
+                    if (page >= 0) granule = static_cast<int>((page * p.r.kv_heads + walk.head) * granules + (at - column * p.r.page_size) / kGranule);
+                }
+                const uint32_t have = __ballot_sync(0xffffffffu, granule >= 0);
+#pragma unroll 1
+                for (int part = 0; part < 2 * S::kParts; ++part, ++stages) {
+                    const bool value = part >= S::kParts;
+                    const int half = value ? part - S::kParts : part, s = stages % kRawStages;
+                    if (stages >= kRawStages) {
+                        ok = bar_wait_warp(raw_empty(s), (stages / kRawStages - 1) & 1, gave_up);
+                        if (!ok) break;
+                    }
+                    int from[kRawGranules];
+#pragma unroll
+                    for (int j = 0; j < kRawGranules; ++j) from[j] = __shfl_sync(0xffffffffu, granule, half * kRawGranules + j);
+                    if (elect_one()) {
+                        if (part == 0) *const_cast<volatile uint32_t *>(&granules_there[tiles_done & 3]) = have;
+                        bar_expect(raw_full(s), __popc(have >> (half * kRawGranules) & ((1u << kRawGranules) - 1)) * S::kRawGranule);
+#pragma unroll
+                        for (int j = 0; j < kRawGranules; ++j)
+                            if (from[j] >= 0) {
+                                const uint8_t *const src = p.cache + static_cast<int64_t>(from[j]) * F::kBytes;
+                                const uint32_t dst = smem_c + s * S::kRaw + j * S::kRawGranule;
+                                bulk_load(dst, src + (value ? F::kValues : 0), 8 * D, raw_full(s));
+                                bulk_load(dst + 8 * D, src + (value ? F::kValueScales : F::kKeyScales), D, raw_full(s));
+                            }
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        // the last copies have landed before the block may end
+        for (uint32_t k = stages > kRawStages ? stages - kRawStages : 0; k < stages; ++k) bar_drain(raw_full(k % kRawStages), k / kRawStages & 1);
+    } else {
+        constexpr uint32_t kType = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (static_cast<uint32_t>(kPromptRows >> 4) << 24);
+        constexpr uint32_t kScoresDesc = kType | (static_cast<uint32_t>(S::kPositions >> 3) << 17);
+        constexpr uint32_t kSumsDesc = kType | 1u << 16 | (static_cast<uint32_t>(D >> 3) << 17);   // values with their channels next to each other
+        uint32_t tiles_done = 0, pieces = 0;
+        bool ok = true, products = false;
+        while (ok && walk.next(p.r, p.group)) {
+            const int steps = walk.steps<S::kPositions>(p.group);
+            if (steps == 0) continue;
+            ok = bar_wait_warp(queries_full, pieces & 1, gave_up);
+            for (int i = 0; ok && i < steps; ++i, ++tiles_done) {
+                // the scores' place is the weights' of the product before, which has to be done
+                ok = bar_wait_warp(keys_full, tiles_done & 1, gave_up) && (tiles_done == 0 || bar_wait_warp(values_empty, (tiles_done - 1) & 1, gave_up));
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_f16(tmem + S::kScores, desc_low(smem_q + k / 4 * S::kQueryPanel + k % 4 * 32, 16), desc_low(smem_k + k / 4 * S::kPanel + k % 4 * 32, 16), kScoresDesc, k > 0);
+                    mma_commit(scores_full);
+                    mma_commit(keys_empty);
+                }
+                __syncwarp();
+                products = false;
+                ok = bar_wait_warp(weights_full, tiles_done & 1, gave_up) && bar_wait_warp(values_full, tiles_done & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < S::kPositions / 16; ++k)
+                        mma_f16_tmem(tmem + S::kSums, tmem + S::kScores + 8 * k, desc_low(smem_v + k * 2048, S::kPanel), kSumsDesc, i > 0 || k > 0);
+                    mma_commit(values_empty);
+                    if (i + 1 == steps) mma_commit(sums_full);
+                }
+                __syncwarp();
+                products = true;
+            }
+            ++pieces;
+        }
+        // the tensor cores have done their last product before the block may end
+        if (ok) {
+            if (tiles_done > 0) bar_drain(values_empty, (tiles_done - 1) & 1);
+        } else if (products) {
+            bar_drain(values_empty, (tiles_done - 1) & 1);
+        } else {
+            bar_drain(keys_empty, tiles_done & 1);
+        }
+    }
+    __syncwarp();
+    if (*gave_up) __nanosleep(100000);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kPromptSoftmax + kPromptConverters + 1) {
+        tc_fence_after();
+        tmem_free(tmem, S::kColumns);
+    }
+}
+
+}  // namespace sq
