@@ -6,7 +6,8 @@
 //   S = Q K^T   [128 x 128] in tensor memory, a row a lane: softmax warps own a row a thread
 //   P = exp2(scale S - m) over S's place, 16 bits;  O += P V, P from tensor memory
 //
-// The maximum m is replaced only when a score is 2^8 beyond it; then O is scaled, which the softmax warps do between two products.  Per 128 positions the tensor cores work 1,024
+// m is the maximum of the row's first tile.  It is replaced when a later tile has reached 2^8 beyond it, before the next one: then O is scaled, between two products.  Within a
+// tile weights may be as large as their type holds with room to spare, so that a row's scores are read once.  Per 128 positions the tensor cores work 1,024
 // clocks, the 128 x 128 exponentials take as long, and so do softmax's and the conversion's instructions, so two blocks share a multiprocessor: one's products
 // run while the other one's exponentials do.
 //
@@ -48,7 +49,8 @@ struct PromptWalk {
     int64_t x, end, base, item0;
     int chunk, row0s, ns, lens;   // sequences chunk + lane
     int b, row0, n, len, tiles;
-    int head, tile, first, last, units;   // of the piece
+    int head, tile, first, last;  // of the piece: kv head, tile, units [first, last) of the tile's
+    int units, over;              // floor and remainder of (tile + q) / group
     int64_t q, span;              // span: units of a kv head of sequence b
 
     static __device__ __forceinline__ int64_t floors(int64_t n, int group)   // sum of floor(i / group) below n
@@ -88,18 +90,13 @@ struct PromptWalk {
         q = offset_of(n, len, group);
         span = floors(q + tiles, group) - floors(q, group);
     }
-    __device__ __forceinline__ bool next(const CacheRows &r, int group)
+    // The tile that unit x is in; the walk is in its sequence.
+    __device__ __forceinline__ void find(const CacheRows &r, int group)
     {
-        if (x >= end) return false;
-        while (x >= base + span * r.kv_heads) {
-            base += span * r.kv_heads;
-            ++b;
-            enter(r, group);
-        }
         const int64_t in = x - base;
         head = static_cast<int>(in / span);
         const int64_t at = in - head * span, before = floors(q, group);
-        int lo = 0, hi = tiles;   // the tile that unit `at` of the head's is in
+        int lo = 0, hi = tiles;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (floors(q + mid, group) - before <= at) lo = mid;
@@ -108,6 +105,32 @@ struct PromptWalk {
         tile = lo;
         item0 = base + head * span + (floors(q + lo, group) - before);
         units = static_cast<int>((lo + q) / group);
+        over = static_cast<int>(lo + q - static_cast<int64_t>(units) * group);
+    }
+    // The next piece; false at the end.  Of the tile that was found, then of the ones that follow it.
+    __device__ __forceinline__ bool next(const CacheRows &r, int group)
+    {
+        if (x >= end) return false;
+        if (x >= item0 + units) {
+            item0 += units;
+            ++tile;
+            if (++over == group) {
+                over = 0;
+                ++units;
+            }
+            if (tile == tiles) {
+                tile = 0;
+                if (++head == r.kv_heads) {
+                    head = 0;
+                    do {
+                        ++b;
+                        enter(r, group);
+                    } while (tiles == 0);   // ends, since there are units left
+                }
+                units = static_cast<int>(static_cast<uint32_t>(q) / static_cast<uint32_t>(group));   // q is below 2^31: (positions + 128) * group / 128, rounded up
+                over = static_cast<int>(static_cast<uint32_t>(q) % static_cast<uint32_t>(group));
+            }
+        }
         first = static_cast<int>(x - item0);
         x = min(end, item0 + units);
         last = static_cast<int>(x - item0);
@@ -157,6 +180,7 @@ __device__ __forceinline__ bool begin(PromptWalk &walk, const CacheRows &r, int 
     walk.base = before + __shfl_sync(0xffffffffu, upto - mine, at);
     walk.b = walk.chunk + at;
     walk.enter(r, group);
+    walk.find(r, group);
     return true;
 }
 
@@ -184,7 +208,34 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]
           "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
           "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ Two add(Two a, Two b)
+{
+    Two r(0ull);
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+// Scores of 32 positions from `position` on that the row does not see, or whose granules are not there.
+__device__ __forceinline__ void hide(uint32_t (&s)[32], int position, int limit, uint32_t have)
+{
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        if (position + e > limit || !(have >> (e / kGranule) & 1)) s[e] = 0xff800000u;
+}
 
 template <int D, bool kHalf>
 __global__ void __launch_bounds__(kPromptThreads, PromptShape<D>::kBlocks)
@@ -240,6 +291,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
 
     if (warp < kPromptSoftmax) {
         const uint32_t mine = tmem + (static_cast<uint32_t>(32 * warp) << 16);   // the warp's lanes of tensor memory
+        const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);   // 0: no score is hidden by a product with infinity
         uint32_t tiles_done = 0, pieces = 0, joins = 0;
         bool ok = true;
         while (ok && walk.next(p.r, p.group)) {
@@ -249,15 +301,27 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
             const int limit = walk.limit(min(at, rows_all - 1), p.group);
             const int steps = walk.steps<S::kPositions>(p.group), seen_least = walk.seen_least(p.group);
             const bool idle = walk.tile * kPromptRows + 32 * warp >= rows_all;   // all rows of the warp
-            float most = kNoScore, total = 0.0f;
+            float most = kNoScore, total = 0.0f, beyond = 0.0f;   // beyond: how far the tile before reached beyond the maximum
+            constexpr float kRoom = kHalf ? 14.0f : 64.0f;        // of a weight's exponent
             if (steps > 0) {
-                const uint16_t *from = p.q + to.row * p.q_stride + to.head * p.q_head;
-#pragma unroll 8
-                for (int j = 0; j < D / 8; ++j) {
-                    const uint4 v = valid ? load8(from + 8 * j, p.q_vector) : make_uint4(0, 0, 0, 0);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem_q + j / 8 * S::kQueryPanel + row * 128 + ((j ^ row) & 7) * 16),
-                                 "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-                }
+                // a row's pieces by neighbouring lanes; with a negative scale the queries change their signs, so that larger scores are larger exponents
+                const int64_t offset = to.row * p.q_stride + to.head * p.q_head;
+                const uint32_t flip = p.scale_log2 < 0.0f ? 0x80008000u : 0u;
+                constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;   // rows at once
+                const auto queries = [&](auto on_vectors) {
+                    constexpr bool kVector = decltype(on_vectors)::value;
+#pragma unroll (kVector ? 16 : 1)
+                    for (int j = 0; j < 32; j += kAtOnce) {
+                        const int r = j + lane / kPieces, piece = lane % kPieces, local = 32 * warp + r;
+                        const int64_t from = __shfl_sync(0xffffffffu, offset, r);
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (walk.tile * kPromptRows + local < rows_all) v = load8(p.q + from + 8 * piece, kVector);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem_q + piece / 8 * S::kQueryPanel + local * 128 + ((piece ^ local) & 7) * 16),
+                                     "r"(v.x ^ flip), "r"(v.y ^ flip), "r"(v.z ^ flip), "r"(v.w ^ flip));
+                    }
+                };
+                if (p.q_vector) queries(std::true_type{});
+                else queries(std::false_type{});
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) bar_arrive(queries_full);
@@ -269,55 +333,90 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 const int position = walk.first * kPromptUnit + i * S::kPositions;
                 const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[tiles_done & 3]);
                 const bool masked = position + S::kPositions - 1 > seen_least || have != (1u << S::kGranules) - 1;
-                if (!idle) {
-                    float top = kNoScore;
+                const auto scale_sums = [&](float factor) {   // the products with the values of the tiles before have been made
+                    total *= factor;
+                    if (i == 0) return;
+#pragma unroll 1
+                    for (int j = 0; j < D; j += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(mine + S::kSums + j, o);
 #pragma unroll
-                    for (int j = 0; j < S::kPositions; j += 32) {
-                        uint32_t s[32];
-                        tmem_ld32(mine + S::kScores + j, s);
-                        if (masked) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                top = fmaxf(top, position + j + e > limit || !(have >> ((j + e) / kGranule) & 1) ? kNoScore : __uint_as_float(s[e]) * p.scale_log2);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(s[e]) * p.scale_log2);
-                        }
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                        tmem_st32(mine + S::kSums + j, o);
                     }
-                    if (__any_sync(0xffffffffu, top > most + kGrowth)) {
-                        const float next = fmaxf(top, most), factor = exp2_fast(most - next);
+                };
+                const auto weigh = [&](auto some_hidden) {
+                    constexpr bool kMasked = decltype(some_hidden)::value;
+                    if (__any_sync(0xffffffffu, most == kNoScore)) {   // the first scores that a row sees: their maximum
+                        float top = -INFINITY;
+#pragma unroll 1
+                        for (int j = 0; j < S::kPositions; j += 32) {
+                            uint32_t s[32];
+                            tmem_ld32(mine + S::kScores + j, s);
+                            if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) top = max3(top, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+                        }
+                        const float next = fmaxf(fmaxf(top * scale, most), kNoScore);
+                        scale_sums(exp2_fast(most - next));
                         most = next;
-                        total *= factor;
-                        if (i > 0) {   // the products with the values of the tiles before have been made
-#pragma unroll
-                            for (int j = 0; j < D; j += 32) {
-                                uint32_t o[32];
-                                tmem_ld32(mine + S::kSums + j, o);
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                                tmem_st32(mine + S::kSums + j, o);
-                            }
-                        }
+                    } else if (__any_sync(0xffffffffu, beyond > kGrowth)) {
+                        scale_sums(exp2_fast(-beyond));
+                        most += beyond;
                     }
-#pragma unroll
+                    beyond = 0.0f;
+                    const Two by(scale, scale);
+                    Two sum(total, 0.0f);
+#pragma unroll 1
                     for (int j = 0; j < S::kPositions; j += 32) {
                         uint32_t s[32], w[16];
                         tmem_ld32(mine + S::kScores + j, s);
+                        if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
+                        const Two less(-most, -most);
+                        float x[32], top = beyond;
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
-                            float x[2];
+                            fma(Two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), by, less).get(x[e], x[e + 1]);
+                            top = max3(top, x[e], x[e + 1]);
+                        }
+                        if (__any_sync(0xffffffffu, top > kRoom)) {
+                            // too far beyond the maximum for 16 bits: what there is of the row is scaled at once, this tile's weights so far among it
+                            const float factor = exp2_fast(-top);
+                            float a, b;
+                            sum.get(a, b);
+                            total = a + b;
+                            scale_sums(factor);
+                            sum = Two(total, 0.0f);
+                            most += top;
+#pragma unroll 1
+                            for (int k = 0; k < j / 2; k += 16) {
+                                tmem_ld16(mine + S::kScores + k, w);
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                x[h] = fmaf(__uint_as_float(s[e + h]), p.scale_log2, -most);
-                                if (masked && (position + j + e + h > limit || !(have >> ((j + e + h) / kGranule) & 1))) x[h] = -INFINITY;
-                                x[h] = exp2_fast(x[h]);
-                                total += x[h];
+                                for (int e = 0; e < 16; ++e)
+                                    w[e] = to_16x2<kHalf>(to_float<kHalf>(static_cast<uint16_t>(w[e])) * factor, to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) * factor);
+                                tmem_st16(mine + S::kScores + k, w);
                             }
-                            w[e / 2] = to_16x2<kHalf>(x[0], x[1]);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] -= top;
+                            top = 0.0f;
+                        }
+                        beyond = top;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const float a = exp2_fast(x[e]), b = exp2_fast(x[e + 1]);
+                            sum = add(sum, Two(a, b));
+                            w[e / 2] = to_16x2<kHalf>(a, b);
                         }
                         tmem_st16(mine + S::kScores + j / 2, w);   // the scores there have been read
                     }
+                    float a, b;
+                    sum.get(a, b);
+                    total = a + b;
                     tmem_st_wait();
+                };
+                if (!idle) {
+                    if (masked) weigh(std::true_type{});
+                    else weigh(std::false_type{});
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -389,25 +488,30 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
             if (!*const_cast<volatile int *>(&is_last)) continue;
             __threadfence();
             const float *const parts = p.parts + 2 * block0 * S::kPart;
-            for (int i = threadIdx.x; i < kPromptRows * (D / 4); i += 32 * kPromptSoftmax) {
-                const int r = i / (D / 4), column = i % (D / 4) * 4;
-                if (walk.tile * kPromptRows + r >= rows_all) break;
-                Joined sum;
-                constexpr int kAtOnce = 4;
-                for (int b0 = 0; b0 < blocks; b0 += kAtOnce) {
-                    float4 x[kAtOnce];
-                    float2 ml[kAtOnce];
+            constexpr int kAtOnce = 4;   // rows in flight, with two parts of each
+            for (int i0 = threadIdx.x; i0 < kPromptRows * (D / 4); i0 += kAtOnce * 32 * kPromptSoftmax) {
+                if (walk.tile * kPromptRows + i0 / (D / 4) >= rows_all) break;
+                Joined sum[kAtOnce];
+                for (int b0 = 0; b0 < blocks; b0 += 2) {
+                    float4 x[kAtOnce][2];
+                    float2 ml[kAtOnce][2];
 #pragma unroll
-                    for (int k = 0; k < kAtOnce; ++k) {
-                        const int b = min(b0 + k, blocks - 1);
+                    for (int k = 0; k < 2 * kAtOnce; ++k) {
+                        const int b = min(b0 + k % 2, blocks - 1), i = i0 + k / 2 * 32 * kPromptSoftmax;
                         const float *from = parts + (2 * static_cast<int64_t>(b) + (b == 0)) * S::kPart;
-                        x[k] = __ldcg(reinterpret_cast<const float4 *>(from + r * D + column));
-                        ml[k] = __ldcg(reinterpret_cast<const float2 *>(from + kPromptRows * D) + r);
-                        if (b0 + k >= blocks) ml[k].y = 0.0f;
+                        x[k / 2][k % 2] = __ldcg(reinterpret_cast<const float4 *>(from) + i);
+                        ml[k / 2][k % 2] = __ldcg(reinterpret_cast<const float2 *>(from + kPromptRows * D) + i / (D / 4));
+                        if (b0 + k % 2 >= blocks) ml[k / 2][k % 2].y = 0.0f;
                     }
-                    sum.add(x, ml);
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k) sum[k].add(x[k], ml[k]);
                 }
-                finish4<kHalf>(p, Target(p, walk.row0, walk.head, walk.tile * kPromptRows + r), column, sum.v, sum.top, sum.l);
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    const int i = i0 + k * 32 * kPromptSoftmax, r = i / (D / 4), column = i % (D / 4) * 4;
+                    if (walk.tile * kPromptRows + r < rows_all)
+                        finish4<kHalf>(p, Target(p, walk.row0, walk.head, walk.tile * kPromptRows + r), column, sum[k].v, sum[k].top, sum[k].l);
+                }
             }
         }
     } else if (warp < kPromptSoftmax + kPromptConverters) {

@@ -145,16 +145,22 @@ def test_many_sequences_find_their_rows():
 
 # ---- attention
 
-# The kernels round the output (half a step of the largest value it is made of: 2^-8 or 2^-11 of |out|) and, for more than eight rows, the probabilities
-# (half a step of each: the output moves by at most 2^-8 or 2^-11 of sum p |v|, of which it is an average).  fp32 sums, exponentials and scales are far below: 2^-16 is
-# allowed for them, relative to sum p |v| too.  fp16 values are those that squant_cache_read returns in fp16: 2^-11 of sum p |v|, and of the scores' summands.
+# What the kernels round:
+#   the output, by half a step of its type: 2^-8 (2^-11) of |out|, in fp16 at least 2^-25, half its smallest number
+#   with more than eight rows the weights of the product with the values, by half a step: the output, an average of the values, moves by at most 2^-8 (2^-11) of sum p |v|.  In
+#   fp16 a weight (the largest is at least 1) is off by at least 2^-25 too, also where what is left over goes through a second product: 2^-25 sum |v| in all
+#   scores: their exponents s log2(e) - m in fp32, and the sums of products, of which the tensor cores cut off 2^-23 of the largest at most 16 + 3 times: 2^-18 |s| of each
+#   weight, with |lse| for the largest |s|.  All other fp32 operations: 2^-16 of sum p |v|
+# fp16 values are those that squant_cache_read returns in fp16: exact for the sizes here.
 def check_attention(out, lse, q, batch, cache, scale=None, rounded_p=True):
     want, want_lse = attention(q, batch, cache, scale)
     size = attention_sizes(q, batch, cache, scale)
     step = torch.finfo(out.dtype).eps / 2
     inside = torch.zeros(q.shape[0], dtype=torch.bool, device="cuda")
     inside[:sum(batch.news)] = True
-    slack = step * want.abs() + (step * rounded_p + 2.0 ** -16) * size + 1e-30
+    slack = step * want.abs() + (step * rounded_p + 2.0 ** -16 + 2.0 ** -18 * want_lse.abs().clamp(max=1e6)[..., None]) * size + 1e-30
+    if out.dtype == FP16:
+        slack = slack + 2.0 ** -25 * (1 + max(batch.lens_list) * float(values(cache)[1].nan_to_num(0).abs().max()))
     off = (out.double() - want).abs()
     bad = (off > slack) & inside[:, None, None]
     assert not bad.any(), (int(bad.sum()), float((off / slack)[inside].max()))
@@ -214,3 +220,27 @@ def test_several_tokens(dim, dtype, heads, group, page, lens, news, hint):
     assert got is out and (out[sum(news):] == 3).all()
     check_attention(out, lse, q, batch, cache, 0.11)
     assert sq.squant_device_status() is None
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("news,most", [(1, 1), (2, 2), (40, 0)])
+@pytest.mark.parametrize("rise", [5.0, 30.0, 200.0])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_that_grow(dtype, dim, news, most, rise, sign):
+    """Scores reach far beyond all before, several times, in the middle of what is taken at once; with a negative scale too."""
+    heads, group, page, n = 2, 4, 32, 700
+    batch = Batch([n, 300], [news, news], page, seed=4)
+    shape = (batch.page_count, heads, page // 16, 16, dim)
+    k = torch.randn(shape, generator=gen(1), device="cuda") * 0.3
+    v = torch.randn(shape, generator=gen(2), device="cuda")
+    direction = torch.randn(dim, generator=gen(3), device="cuda").sign()
+    for b in range(2):
+        for step, p in enumerate((3, 70, 130, 165, 217, 290, 450, 455, 640)):
+            if p < batch.lens_list[b]:
+                k[batch.pages_list[b, p // page], :, p % page // 16, p % 16] += direction * (step + 1) * rise / 9 / dim ** 0.5
+    from cache_cases import pack
+    cache = pack(k.to(dtype), v.to(dtype))
+    q = (inputs(batch.rows, heads * group, dim, dtype, 7).float() * 0.3 + direction).to(dtype)
+    out, lse = sq.squant_cache_attention(q, cache, *batch.args, most=most, lse=True, scale=sign * 1.0)
+    check_attention(out, lse, q, batch, cache, sign * 1.0)
