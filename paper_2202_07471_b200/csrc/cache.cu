@@ -199,11 +199,11 @@ StepPlan prompt_plan(const squant_cache_attention_args &a)
 {
     using S = sq::PromptShape<D>;
     const squant_cache_rows &r = a.rows;
-    const int64_t tiles = (r.rows * a.group + static_cast<int64_t>(std::min<int64_t>(r.batch, r.rows)) * (sq::kPromptRows - 1)) / sq::kPromptRows;
+    const int64_t tiles = (r.rows * a.group + static_cast<int64_t>(std::min<int64_t>(r.batch, r.rows)) * (S::kRows - 1)) / S::kRows;
     const int64_t positions = std::min<int64_t>(static_cast<int64_t>(r.width) * r.page_size, 1ll << 30);
-    const double units = static_cast<double>(tiles) * r.kv_heads * (positions / sq::kPromptUnit + 2);
+    const double units = static_cast<double>(tiles) * r.kv_heads * (positions / S::kRows + 2);
     StepPlan s;
-    s.blocks = static_cast<int64_t>(std::min<double>(kB200Sms * S::kBlocks, units));
+    s.blocks = static_cast<int64_t>(std::min<double>(kB200Sms, units));
     s.tickets = up(8 * s.blocks, 128);
     s.bytes = s.tickets + 2 * s.blocks * S::kPart * 4;
     return s;
@@ -267,7 +267,7 @@ int prompt(const squant_cache_attention_args &a, cudaStream_t stream)
 {
     const StepPlan s = prompt_plan<D>(a);
     static std::atomic<bool> ready[kMaxDevices];
-    return launch_large(sq::cache_prompt_kernel<D, kHalf>, ready, s.blocks, sq::kPromptThreads, sq::PromptShape<D>::kSmem, stream, attend_args(a, s));
+    return launch_large(sq::cache_prompt_kernel<D, kHalf>, ready, s.blocks, sq::PromptShape<D>::kThreads, sq::PromptShape<D>::kSmem, stream, attend_args(a, s));
 }
 template <int D>
 int attention(const squant_cache_attention_args &a, cudaStream_t stream)

@@ -1,17 +1,17 @@
 // Attention over the cache for many rows: prompts, parts of prompts, many drafted tokens (formulas in cache_step.cuh).
 //
-// A tile is 128 rows of one sequence and kv head, tokens times the query heads of the group.  Its queries stay in shared memory; for 128 positions at a time (64 with 256
-// channels) converter warps turn keys and values into 16-bit floats for the tensor cores:
+// A tile is 256 rows (128 with 256 channels) of one sequence and kv head, tokens times the query heads of the group, in two slots of 128.  Its queries stay in shared memory; for 128
+// positions at a time (64) converter warps turn keys and values into 16-bit floats for the tensor cores, which both slots use:
 //
 //   S = Q K^T   [128 x 128] in tensor memory, a row a lane: softmax warps own a row a thread
 //   P = exp2(scale S - m) over S's place, 16 bits;  O += P V, P from tensor memory
 //
 // m is the maximum of the row's first tile.  It is replaced when a later tile has reached 2^8 beyond it, before the next one: then O is scaled, between two products.  Within a
-// tile weights may be as large as their type holds with room to spare, so that a row's scores are read once.  Per 128 positions the tensor cores work 1,024
-// clocks, the 128 x 128 exponentials take as long, and so do softmax's and the conversion's instructions, so two blocks share a multiprocessor: one's products
-// run while the other one's exponentials do.
+// tile weights may be as large as their type holds with room to spare, so that a row's scores are read once.  Per 128 positions the tensor cores work 2,048 clocks for both slots, and
+// the exponentials take as long: one slot's products run while the other one's exponentials do.  A tile of up to 128 rows has its positions shared by the slots, every other tile
+// of scores each, and their sums are joined at the end.
 //
-// Work is cut as in cache_step.cuh: the units (128 positions that a tile sees, so that a causal prompt's later tiles have more) of all tiles stand in one row, each block
+// Work is cut as in cache_step.cuh: the units (256 positions that a tile sees, so that a causal prompt's later tiles have more) of all tiles stand in one row, each block
 // takes an equal stretch, and a tile that several blocks have parts of is put together, in order, by the one that ends last.
 #pragma once
 
@@ -19,33 +19,35 @@
 
 namespace sq {
 
-constexpr int kPromptRows = 128, kPromptUnit = 128;   // rows of a tile, positions of a unit
-constexpr int kPromptSoftmax = 4, kPromptConverters = 4;   // warps
-constexpr int kPromptThreads = 32 * (kPromptSoftmax + kPromptConverters + 2);   // and one for the copies, one for the tensor cores
-constexpr int kRawGranules = 4, kRawStages = 3;       // keys or values of 64 positions as they are, ahead of the converters
+constexpr int kSlotRows = 128;           // the tensor memory's lanes
+constexpr int kPromptConverters = 4;     // warps
+constexpr int kRawGranules = 4;          // of a stage: keys or values of 64 positions as they are, ahead of the converters
+constexpr int kTilesAhead = 8;           // score tiles that are being copied, converted or weighed at the same time, at most
 
 template <int D>
 struct PromptShape {
-    static constexpr int kBlocks = D > 128 ? 1 : 2;                  // on a multiprocessor
+    static constexpr int kSlots = D > 128 ? 1 : 2, kRows = kSlots * kSlotRows;
+    static constexpr int kSoftmax = 4 * kSlots, kThreads = 32 * (kSoftmax + kPromptConverters + 2);   // warps; one for the copies, one for the tensor cores
     static constexpr int kPositions = D > 128 ? 64 : 128;            // of a score tile
     static constexpr int kGranules = kPositions / kGranule;
-    static constexpr int kQueries = kPromptRows * D * 2, kOperand = kPositions * D * 2, kPanel = kPositions * 128, kQueryPanel = kPromptRows * 128;
+    static constexpr int kQueries = kSlotRows * D * 2, kOperand = kPositions * D * 2, kPanel = kPositions * 128, kQueryPanel = kSlotRows * 128;
     static constexpr int kRawGranule = 9 * D, kRaw = kRawGranules * kRawGranule;   // codes, then scales
+    static constexpr int kRawStages = D > 128 ? 3 : D > 64 ? 6 : 12;
     static constexpr int kParts = kGranules / kRawGranules;          // stages of a score tile's keys
-    static constexpr int kBars = 2 * kRawStages + 9;
-    static constexpr int kNeeded = 1024 + kQueries + 2 * kOperand + kRawStages * kRaw + 8 * kBars;
-    // no more blocks on a multiprocessor than its tensor memory has room for
-    static constexpr int kSmem = kBlocks == 2 && kNeeded < (80 << 10) ? 80 << 10 : kNeeded;
-    static constexpr int kScores = 0, kSums = 128, kColumns = D > 128 ? 512 : 256;   // tensor memory
-    static constexpr int kPart = kPromptRows * (D + 2);              // floats of a tile's part in the workspace
-    static_assert(kBlocks * (kSmem + 1024 + 256) <= 228 << 10, "blocks on a multiprocessor");
-    static_assert((kBlocks + 1) * kSmem > 228 << 10 && kBlocks * kColumns <= 512 && kSums + D <= kColumns, "the tensor memory that blocks ask for is always there");
+    static constexpr int kBars = 2 * kRawStages + 18;
+    static constexpr int kSmem = 1024 + kSlots * kQueries + 4 * kOperand + kRawStages * kRaw + 8 * kBars;
+    static constexpr int kScores = 128, kSums = D, kFirstSums = 256, kColumns = 512;   // tensor memory: columns of a slot's scores, of its sums
+    static constexpr int kPart = kRows * (D + 2);                    // floats of a tile's part in the workspace
+    static_assert(kSmem + 2048 <= 227 << 10 && 2 * kSmem > 228 << 10, "one block a multiprocessor, so that all of its tensor memory is there");
+    static_assert(kSlots * kScores <= kFirstSums && kFirstSums + kSlots * kSums <= kColumns, "tensor memory");
 };
 
-// The walk over units of 128 positions.  The tile t of a sequence sees its first tokens, and those of its rows up to the tile's last:
-//   units(t) = ceil((len - n + floor((128 t + 127) / group) + 1) / 128) = floor((t + q) / group),   q = floor((group (len - n + 128) + 127) / 128),
+// The walk over units of as many positions as a tile has rows, R.  The tile t of a sequence sees its first tokens, and those of its rows up to the tile's last:
+//   units(t) = ceil((len - n + floor((R t + R - 1) / group) + 1) / R) = floor((t + q) / group),   q = floor((group (len - n + R) + R - 1) / R),
 // which is one too many at most, for the last tile.  Sums of floor(i / group) have a closed form, and so does the row of all sequences' units.
+template <int kRows>
 struct PromptWalk {
+    static constexpr int kUnit = kRows;
     int64_t x, end, base, item0;
     int chunk, row0s, ns, lens;   // sequences chunk + lane
     int b, row0, n, len, tiles;
@@ -60,9 +62,9 @@ struct PromptWalk {
     }
     static __device__ __forceinline__ int64_t offset_of(int n, int len, int group)
     {
-        return (static_cast<int64_t>(group) * (max(0, len - n) + kPromptUnit) + kPromptRows - 1) / kPromptRows;
+        return (static_cast<int64_t>(group) * (max(0, len - n) + kUnit) + kRows - 1) / kRows;
     }
-    static __device__ __forceinline__ int tiles_of(int n, int group) { return static_cast<int>((static_cast<int64_t>(n) * group + kPromptRows - 1) / kPromptRows); }
+    static __device__ __forceinline__ int tiles_of(int n, int group) { return static_cast<int>((static_cast<int64_t>(n) * group + kRows - 1) / kRows); }
     __device__ __forceinline__ void look_up(const CacheRows &r, int from)
     {
         chunk = from;
@@ -127,7 +129,7 @@ struct PromptWalk {
                         enter(r, group);
                     } while (tiles == 0);   // ends, since there are units left
                 }
-                units = static_cast<int>(static_cast<uint32_t>(q) / static_cast<uint32_t>(group));   // q is below 2^31: (positions + 128) * group / 128, rounded up
+                units = static_cast<int>(static_cast<uint32_t>(q) / static_cast<uint32_t>(group));   // q is below 2^31: (positions + R) * group / R, rounded up
                 over = static_cast<int>(static_cast<uint32_t>(q) % static_cast<uint32_t>(group));
             }
         }
@@ -138,18 +140,19 @@ struct PromptWalk {
     }
     __device__ __forceinline__ int rows_all(int group) const { return n * group; }
     __device__ __forceinline__ int limit(int at, int group) const { return len - n + static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(group)); }
-    __device__ __forceinline__ int seen_least(int group) const { return limit(tile * kPromptRows, group); }
-    __device__ __forceinline__ int seen_most(int group) const { return limit(min(rows_all(group) - tile * kPromptRows, kPromptRows) - 1 + tile * kPromptRows, group); }
+    __device__ __forceinline__ int seen_least(int group) const { return limit(tile * kRows, group); }
+    __device__ __forceinline__ int seen_most(int group) const { return limit(min(rows_all(group) - tile * kRows, kRows) - 1 + tile * kRows, group); }
     // Score tiles of the piece that any row sees.
     template <int kPositions>
     __device__ __forceinline__ int steps(int group) const
     {
-        const int seen = seen_most(group) + 1 - first * kPromptUnit;
-        return seen <= 0 ? 0 : min((last - first) * (kPromptUnit / kPositions), (seen + kPositions - 1) / kPositions);
+        const int seen = seen_most(group) + 1 - first * kUnit;
+        return seen <= 0 ? 0 : min((last - first) * (kUnit / kPositions), (seen + kPositions - 1) / kPositions);
     }
 };
 // The block's stretch; false: it has none.  Each warp for itself.
-__device__ __forceinline__ bool begin(PromptWalk &walk, const CacheRows &r, int group, int64_t &share)
+template <int kRows>
+__device__ __forceinline__ bool begin(PromptWalk<kRows> &walk, const CacheRows &r, int group, int64_t &share)
 {
     const int lane = threadIdx.x & 31;
     int64_t total = 0, upto = 0, mine = 0;
@@ -237,8 +240,22 @@ __device__ __forceinline__ void hide(uint32_t (&s)[32], int position, int limit,
         if (position + e > limit || !(have >> (e / kGranule) & 1)) s[e] = 0xff800000u;
 }
 
+// Two slots work on a tile's score tiles in turn.  Events are products of queries and keys (and of weights and values): with more than 128 rows both slots' for each score tile, else the
+// slots take every other one.
+template <int kSlots>
+struct Events {
+    bool shared;   // by both slots
+    int count;
+    __device__ __forceinline__ Events(int steps, bool both) : shared(kSlots == 2 && both), count(shared ? 2 * steps : steps) {}
+    __device__ __forceinline__ int slot(int e) const { return kSlots == 2 ? e & 1 : 0; }
+    __device__ __forceinline__ int tile(int e) const { return shared ? e >> 1 : e; }
+    __device__ __forceinline__ bool first_use(int e) const { return !shared || !(e & 1); }
+    __device__ __forceinline__ bool last_use(int e) const { return !shared || (e & 1); }
+    __device__ __forceinline__ int of_slot(int slot) const { return kSlots == 1 ? count : (count + 1 - slot) >> 1; }
+};
+
 template <int D, bool kHalf>
-__global__ void __launch_bounds__(kPromptThreads, PromptShape<D>::kBlocks)
+__global__ void __launch_bounds__(PromptShape<D>::kThreads, 1)
 cache_prompt_kernel(const __grid_constant__ AttendArgs p)
 {
     using F = CacheFormat<D>;
@@ -247,60 +264,80 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_addr(smem);
-    const uint32_t smem_q = base, smem_k = base + S::kQueries, smem_v = smem_k + S::kOperand, smem_c = smem_v + S::kOperand;
-    const uint32_t bars = smem_c + kRawStages * S::kRaw;
+    const uint32_t smem_q = base, smem_k = base + S::kSlots * S::kQueries, smem_v = smem_k + 2 * S::kOperand, smem_c = smem_v + 2 * S::kOperand;
+    const uint32_t bars = smem_c + S::kRawStages * S::kRaw;
     SQ_LINEAR_CHECK(bars + 8 * S::kBars <= smem_end(smem_raw) && (bars & 7) == 0, 2020);
     const auto raw_full = [&](int s) { return bars + 8 * s; };
-    const auto raw_empty = [&](int s) { return bars + 8 * (kRawStages + s); };
-    const uint32_t queries_full = bars + 16 * kRawStages, keys_full = queries_full + 8, keys_empty = queries_full + 16, values_full = queries_full + 24,
-                   values_empty = queries_full + 32, scores_full = queries_full + 40, weights_full = queries_full + 48, sums_full = queries_full + 56,
-                   together = queries_full + 64;
+    const auto raw_empty = [&](int s) { return bars + 8 * (S::kRawStages + s); };
+    const uint32_t queries_full = bars + 16 * S::kRawStages, together = queries_full + 8;
+    // of the two places of keys and values, and of the slots
+    const auto keys_full = [&](int i) { return queries_full + 16 + 8 * i; };
+    const auto keys_empty = [&](int i) { return queries_full + 32 + 8 * i; };
+    const auto values_full = [&](int i) { return queries_full + 48 + 8 * i; };
+    const auto values_empty = [&](int i) { return queries_full + 64 + 8 * i; };
+    const auto scores_full = [&](int slot) { return queries_full + 80 + 8 * slot; };
+    const auto weights_full = [&](int slot) { return queries_full + 96 + 8 * slot; };
+    const auto weights_empty = [&](int slot) { return queries_full + 112 + 8 * slot; };
+    const auto sums_full = [&](int slot) { return queries_full + 128 + 8 * slot; };
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_word, is_last;
-    __shared__ uint32_t granules_there[4];       // of the last score tiles, by their number
-    __shared__ int no_number[2][kGroupsAll];     // of the last pieces: the first position whose value group has no number
+    __shared__ uint32_t granules_there[kTilesAhead];   // of the last score tiles, by their number
+    __shared__ int no_number[4][kGroupsAll];     // of the last pieces: the first position whose value group has no number
+    __shared__ float2 slot_sums[kSlotRows];      // maximum and sum of the second slot's rows
     volatile int *gave_up = &gave_up_word;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    PromptWalk walk;
+    PromptWalk<S::kRows> walk;
     int64_t share;
     if (!begin(walk, p.r, p.group, share)) return;   // all threads of the block
 
     if (threadIdx.x == 0) {
         gave_up_word = 0;
-        for (int s = 0; s < kRawStages; ++s) {
+        for (int s = 0; s < S::kRawStages; ++s) {
             bar_init(raw_full(s), 1);
             bar_init(raw_empty(s), kPromptConverters);
         }
-        bar_init(queries_full, kPromptSoftmax);
-        bar_init(keys_full, kPromptConverters);
-        bar_init(keys_empty, 1);
-        bar_init(values_full, kPromptConverters);
-        bar_init(values_empty, 1);
-        bar_init(scores_full, 1);
-        bar_init(weights_full, kPromptSoftmax);
-        bar_init(sums_full, 1);
-        bar_init(together, kPromptSoftmax);
-        for (int i = 0; i < 2 * kGroupsAll; ++i) no_number[i / kGroupsAll][i % kGroupsAll] = 0x7fffffff;
+        bar_init(queries_full, S::kSoftmax);
+        bar_init(together, S::kSoftmax);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(keys_full(i), kPromptConverters);
+            bar_init(keys_empty(i), 1);
+            bar_init(values_full(i), kPromptConverters);
+            bar_init(values_empty(i), 1);
+            bar_init(scores_full(i), 1);
+            bar_init(weights_full(i), 4);
+            bar_init(weights_empty(i), 1);
+            bar_init(sums_full(i), 1);
+        }
+        for (int i = 0; i < 4 * kGroupsAll; ++i) no_number[i / kGroupsAll][i % kGroupsAll] = 0x7fffffff;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kPromptSoftmax + kPromptConverters + 1) tmem_alloc(smem_addr(&tmem_base), S::kColumns);
+    if (warp == S::kSoftmax + kPromptConverters + 1) tmem_alloc(smem_addr(&tmem_base), S::kColumns);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
 
-    if (warp < kPromptSoftmax) {
-        const uint32_t mine = tmem + (static_cast<uint32_t>(32 * warp) << 16);   // the warp's lanes of tensor memory
+    if (warp < S::kSoftmax) {
+        const int quarter = warp & 3, slot = warp >> 2;
+        const uint32_t mine = tmem + (static_cast<uint32_t>(32 * quarter) << 16);   // the warp's lanes of tensor memory
+        const uint32_t scores = mine + slot * S::kScores, sums = mine + S::kFirstSums + slot * S::kSums;
         const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);   // 0: no score is hidden by a product with infinity
-        uint32_t tiles_done = 0, pieces = 0, joins = 0;
+        uint32_t tiles_before = 0, weighed = 0, summed = 0, pieces = 0, joins = 0;
         bool ok = true;
+        const auto join = [&]() {
+            __syncwarp();
+            if (lane == 0) bar_arrive(together);
+            ok = bar_wait_warp(together, joins++ & 1, gave_up);
+        };
         while (ok && walk.next(p.r, p.group)) {
-            const int row = 32 * warp + lane, rows_all = walk.rows_all(p.group), at = walk.tile * kPromptRows + row;
+            const int rows_all = walk.rows_all(p.group), tile_row = walk.tile * S::kRows, steps = walk.template steps<S::kPositions>(p.group);
+            const Events<S::kSlots> events(steps, rows_all - tile_row > kSlotRows);
+            const bool alone = S::kSlots == 1 || events.shared;   // the slot has rows of its own
+            const int row = (alone ? slot * kSlotRows : 0) + 32 * quarter + lane, at = tile_row + row;
             const bool valid = at < rows_all;
             const Target to(p, walk.row0, walk.head, min(at, rows_all - 1));
-            const int limit = walk.limit(min(at, rows_all - 1), p.group);
-            const int steps = walk.steps<S::kPositions>(p.group), seen_least = walk.seen_least(p.group);
-            const bool idle = walk.tile * kPromptRows + 32 * warp >= rows_all;   // all rows of the warp
+            const int limit = walk.limit(min(at, rows_all - 1), p.group), seen_least = walk.seen_least(p.group);
+            const bool idle = at - lane >= rows_all;   // all rows of the warp
             float most = kNoScore, total = 0.0f, beyond = 0.0f;   // beyond: how far the tile before reached beyond the maximum
             constexpr float kRoom = kHalf ? 14.0f : 64.0f;        // of a weight's exponent
             if (steps > 0) {
@@ -312,26 +349,29 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                     constexpr bool kVector = decltype(on_vectors)::value;
 #pragma unroll (kVector ? 16 : 1)
                     for (int j = 0; j < 32; j += kAtOnce) {
-                        const int r = j + lane / kPieces, piece = lane % kPieces, local = 32 * warp + r;
+                        const int r = j + lane / kPieces, piece = lane % kPieces, local = 32 * quarter + r;
                         const int64_t from = __shfl_sync(0xffffffffu, offset, r);
                         uint4 v = make_uint4(0, 0, 0, 0);
-                        if (walk.tile * kPromptRows + local < rows_all) v = load8(p.q + from + 8 * piece, kVector);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem_q + piece / 8 * S::kQueryPanel + local * 128 + ((piece ^ local) & 7) * 16),
+                        if (row - lane + r + tile_row < rows_all) v = load8(p.q + from + 8 * piece, kVector);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem_q + slot * S::kQueries + piece / 8 * S::kQueryPanel + local * 128 + ((piece ^ local) & 7) * 16),
                                      "r"(v.x ^ flip), "r"(v.y ^ flip), "r"(v.z ^ flip), "r"(v.w ^ flip));
                     }
                 };
-                if (p.q_vector) queries(std::true_type{});
-                else queries(std::false_type{});
+                if (alone || slot == 0) {
+                    if (p.q_vector) queries(std::true_type{});
+                    else queries(std::false_type{});
+                }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) bar_arrive(queries_full);
             }
-            for (int i = 0; i < steps; ++i, ++tiles_done) {
-                ok = bar_wait_warp(scores_full, tiles_done & 1, gave_up);
+            const int mine_of = events.of_slot(slot);
+            for (int i = 0; i < mine_of; ++i, ++weighed) {
+                ok = bar_wait_warp(scores_full(slot), weighed & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                const int position = walk.first * kPromptUnit + i * S::kPositions;
-                const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[tiles_done & 3]);
+                const int step = alone ? i : 2 * i + slot, position = walk.first * S::kRows + step * S::kPositions;
+                const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[(tiles_before + step) % kTilesAhead]);
                 const bool masked = position + S::kPositions - 1 > seen_least || have != (1u << S::kGranules) - 1;
                 const auto scale_sums = [&](float factor) {   // the products with the values of the tiles before have been made
                     total *= factor;
@@ -339,10 +379,10 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
 #pragma unroll 1
                     for (int j = 0; j < D; j += 32) {
                         uint32_t o[32];
-                        tmem_ld32(mine + S::kSums + j, o);
+                        tmem_ld32(sums + j, o);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                        tmem_st32(mine + S::kSums + j, o);
+                        tmem_st32(sums + j, o);
                     }
                 };
                 const auto weigh = [&](auto some_hidden) {
@@ -352,7 +392,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
 #pragma unroll 1
                         for (int j = 0; j < S::kPositions; j += 32) {
                             uint32_t s[32];
-                            tmem_ld32(mine + S::kScores + j, s);
+                            tmem_ld32(scores + j, s);
                             if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
 #pragma unroll
                             for (int e = 0; e < 32; e += 2) top = max3(top, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
@@ -370,7 +410,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
 #pragma unroll 1
                     for (int j = 0; j < S::kPositions; j += 32) {
                         uint32_t s[32], w[16];
-                        tmem_ld32(mine + S::kScores + j, s);
+                        tmem_ld32(scores + j, s);
                         if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
                         const Two less(-most, -most);
                         float x[32], top = beyond;
@@ -390,11 +430,11 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                             most += top;
 #pragma unroll 1
                             for (int k = 0; k < j / 2; k += 16) {
-                                tmem_ld16(mine + S::kScores + k, w);
+                                tmem_ld16(scores + k, w);
 #pragma unroll
                                 for (int e = 0; e < 16; ++e)
                                     w[e] = to_16x2<kHalf>(to_float<kHalf>(static_cast<uint16_t>(w[e])) * factor, to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) * factor);
-                                tmem_st16(mine + S::kScores + k, w);
+                                tmem_st16(scores + k, w);
                             }
 #pragma unroll
                             for (int e = 0; e < 32; ++e) x[e] -= top;
@@ -407,7 +447,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                             sum = add(sum, Two(a, b));
                             w[e / 2] = to_16x2<kHalf>(a, b);
                         }
-                        tmem_st16(mine + S::kScores + j / 2, w);   // the scores there have been read
+                        tmem_st16(scores + j / 2, w);   // the scores there have been read
                     }
                     float a, b;
                     sum.get(a, b);
@@ -420,87 +460,108 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(weights_full);
+                if (lane == 0) bar_arrive(weights_full(slot));
             }
+            tiles_before += steps;
             if (!ok) break;
-            const bool whole = walk.first == 0 && walk.last == walk.units;
-            if (steps > 0) {
-                ok = bar_wait_warp(sums_full, pieces & 1, gave_up);
+            if (mine_of > 0) {
+                ok = bar_wait_warp(sums_full(slot), summed++ & 1, gave_up);
                 if (!ok) break;
-                tc_fence_after();
             }
+            const bool whole = walk.first == 0 && walk.last == walk.units;
+            float factor = 1.0f, other = 0.0f;   // of the slots' sums
+            if (!alone) {
+                if (slot == 1) slot_sums[32 * quarter + lane] = make_float2(most, total);
+                tc_fence_before();
+                join();
+                if (!ok) break;
+                if (slot == 0) {
+                    const float2 ml = slot_sums[row];
+                    const float next = fmaxf(most, ml.x);
+                    factor = exp2_fast(most - next);
+                    other = exp2_fast(ml.x - next);   // no score: 0, unless neither has one
+                    total = total * factor + ml.y * other;
+                    most = next;
+                }
+            }
+            tc_fence_after();
+            const bool both = !alone && events.count > 1;   // the other slot has sums
             const int64_t block0 = walk.item0 / share;
             float *const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (walk.item0 >= share * blockIdx.x)) * S::kPart;
             const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+            if (alone || slot == 0) {
+#pragma unroll 1
+                for (int j = 0; j < D; j += 32) {
+                    uint32_t o[32];
+                    if (steps > 0) {
+                        tmem_ld32(sums + j, o);
+                        if (both) {
+                            uint32_t more[32];
+                            tmem_ld32(sums + S::kSums + j, more);
 #pragma unroll
-            for (int j = 0; j < D; j += 32) {
-                uint32_t o[32];
-                if (steps > 0) {
-                    tmem_ld32(mine + S::kSums + j, o);
-                    const bool none = *const_cast<volatile int *>(&no_number[pieces & 1][j / kGroup]) <= limit;
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(fmaf(__uint_as_float(more[e]), other, __uint_as_float(o[e]) * factor));
+                        }
+                        const bool none = *const_cast<volatile int *>(&no_number[pieces & 3][j / kGroup]) <= limit;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = none ? 0x7fffffffu : o[e];
-                } else {
+                        for (int e = 0; e < 32; ++e) o[e] = none ? 0x7fffffffu : o[e];
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0;
-                }
-                if (!whole) {
+                        for (int e = 0; e < 32; ++e) o[e] = 0;
+                    }
+                    if (!whole) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        __stcg(reinterpret_cast<float4 *>(part + row * D + j + e), make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
-                                                                                                 __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])));
-                } else if (valid) {
-                    uint16_t *out = p.out + to.row * p.out_stride + to.head * p.out_head + j;
+                        for (int e = 0; e < 32; e += 4)
+                            __stcg(reinterpret_cast<float4 *>(part + row * D + j + e), make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
+                                                                                                     __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])));
+                    } else if (valid) {
+                        uint16_t *out = p.out + to.row * p.out_stride + to.head * p.out_head + j;
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint32_t w[4];
+                        for (int e = 0; e < 32; e += 8) {
+                            uint32_t w[4];
 #pragma unroll
-                        for (int h = 0; h < 4; ++h) w[h] = to_16x2<kHalf>(__uint_as_float(o[e + 2 * h]) * inverse, __uint_as_float(o[e + 2 * h + 1]) * inverse);
-                        if (p.out_vector) {
-                            *reinterpret_cast<uint4 *>(out + e) = make_uint4(w[0], w[1], w[2], w[3]);
-                        } else {
+                            for (int h = 0; h < 4; ++h) w[h] = to_16x2<kHalf>(__uint_as_float(o[e + 2 * h]) * inverse, __uint_as_float(o[e + 2 * h + 1]) * inverse);
+                            if (p.out_vector) {
+                                *reinterpret_cast<uint4 *>(out + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                            } else {
 #pragma unroll
-                            for (int h = 0; h < 8; ++h) out[e + h] = static_cast<uint16_t>(w[h / 2] >> (16 * (h & 1)));
+                                for (int h = 0; h < 8; ++h) out[e + h] = static_cast<uint16_t>(w[h / 2] >> (16 * (h & 1)));
+                            }
                         }
                     }
                 }
+                if (whole && valid && p.lse) store_lse(p, to, most, total);
+                if (!whole) __stcg(reinterpret_cast<float2 *>(part + S::kRows * D) + row, make_float2(most, total));
             }
-            if (whole && valid && p.lse) store_lse(p, to, most, total);
-            if (!whole) __stcg(reinterpret_cast<float2 *>(part + kPromptRows * D) + row, make_float2(most, total));
             tc_fence_before();
             // all have read the sums and what goes with them, and written their part
             if (!whole) __threadfence();
-            __syncwarp();
-            if (lane == 0) bar_arrive(together);
-            ok = bar_wait_warp(together, joins++ & 1, gave_up);
+            join();
             if (!ok) break;
             if (steps > 0) {
-                if (threadIdx.x < kGroupsAll) no_number[pieces & 1][threadIdx.x] = 0x7fffffff;
+                if (threadIdx.x < kGroupsAll) no_number[pieces & 3][threadIdx.x] = 0x7fffffff;
                 ++pieces;
             }
             if (whole) continue;
             const int blocks = static_cast<int>((walk.item0 + walk.units - 1) / share - block0 + 1);
             if (threadIdx.x == 0) is_last = arrive(p.tickets + block0, p.nonce, blocks);
-            __syncwarp();
-            if (lane == 0) bar_arrive(together);
-            ok = bar_wait_warp(together, joins++ & 1, gave_up);
+            join();
             if (!ok) break;
             if (!*const_cast<volatile int *>(&is_last)) continue;
             __threadfence();
             const float *const parts = p.parts + 2 * block0 * S::kPart;
             constexpr int kAtOnce = 4;   // rows in flight, with two parts of each
-            for (int i0 = threadIdx.x; i0 < kPromptRows * (D / 4); i0 += kAtOnce * 32 * kPromptSoftmax) {
-                if (walk.tile * kPromptRows + i0 / (D / 4) >= rows_all) break;
+            for (int i0 = threadIdx.x; i0 < S::kRows * (D / 4); i0 += kAtOnce * 32 * S::kSoftmax) {
+                if (walk.tile * S::kRows + i0 / (D / 4) >= rows_all) break;
                 Joined sum[kAtOnce];
                 for (int b0 = 0; b0 < blocks; b0 += 2) {
                     float4 x[kAtOnce][2];
                     float2 ml[kAtOnce][2];
 #pragma unroll
                     for (int k = 0; k < 2 * kAtOnce; ++k) {
-                        const int b = min(b0 + k % 2, blocks - 1), i = i0 + k / 2 * 32 * kPromptSoftmax;
+                        const int b = min(b0 + k % 2, blocks - 1), i = i0 + k / 2 * 32 * S::kSoftmax;
                         const float *from = parts + (2 * static_cast<int64_t>(b) + (b == 0)) * S::kPart;
                         x[k / 2][k % 2] = __ldcg(reinterpret_cast<const float4 *>(from) + i);
-                        ml[k / 2][k % 2] = __ldcg(reinterpret_cast<const float2 *>(from + kPromptRows * D) + i / (D / 4));
+                        ml[k / 2][k % 2] = __ldcg(reinterpret_cast<const float2 *>(from + S::kRows * D) + i / (D / 4));
                         if (b0 + k % 2 >= blocks) ml[k / 2][k % 2].y = 0.0f;
                     }
 #pragma unroll
@@ -508,39 +569,40 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 }
 #pragma unroll
                 for (int k = 0; k < kAtOnce; ++k) {
-                    const int i = i0 + k * 32 * kPromptSoftmax, r = i / (D / 4), column = i % (D / 4) * 4;
-                    if (walk.tile * kPromptRows + r < rows_all)
-                        finish4<kHalf>(p, Target(p, walk.row0, walk.head, walk.tile * kPromptRows + r), column, sum[k].v, sum[k].top, sum[k].l);
+                    const int i = i0 + k * 32 * S::kSoftmax, r = i / (D / 4), column = i % (D / 4) * 4;
+                    if (walk.tile * S::kRows + r < rows_all)
+                        finish4<kHalf>(p, Target(p, walk.row0, walk.head, walk.tile * S::kRows + r), column, sum[k].v, sum[k].top, sum[k].l);
                 }
             }
         }
-    } else if (warp < kPromptSoftmax + kPromptConverters) {
-        const int thread = threadIdx.x - 32 * kPromptSoftmax;
+    } else if (warp < S::kSoftmax + kPromptConverters) {
+        constexpr int kConverterThreads = 32 * kPromptConverters;   // 256 pieces of 16 bytes a stage and slab
+        const int thread = threadIdx.x - 32 * S::kSoftmax;
         const CodePairs<kHalf> pairs;
-        uint32_t stages = 0, tiles_done = 0, pieces = 0;
+        uint32_t stage = 0, turn = 0, tiles_done = 0, pieces = 0;
         bool ok = true;
         while (ok && walk.next(p.r, p.group)) {
-            const int steps = walk.steps<S::kPositions>(p.group), seen_most = walk.seen_most(p.group);
+            const int steps = walk.template steps<S::kPositions>(p.group), seen_most = walk.seen_most(p.group);
             for (int i = 0; ok && i < steps; ++i, ++tiles_done) {
-                const int position = walk.first * kPromptUnit + i * S::kPositions;
+                const int position = walk.first * S::kRows + i * S::kPositions;
 #pragma unroll 1
-                for (int part = 0; part < 2 * S::kParts; ++part, ++stages) {
+                for (int part = 0; part < 2 * S::kParts; ++part) {
                     const bool value = part >= S::kParts;
-                    const int half = value ? part - S::kParts : part, s = stages % kRawStages;
-                    if (half == 0 && tiles_done > 0) {   // the product with what is there has been made
-                        ok = bar_wait_warp(value ? values_empty : keys_empty, (tiles_done - 1) & 1, gave_up);
+                    const int half = value ? part - S::kParts : part, s = stage;
+                    if (half == 0 && tiles_done > 1) {   // the products with what is there have been made
+                        ok = bar_wait_warp(value ? values_empty(tiles_done & 1) : keys_empty(tiles_done & 1), (tiles_done / 2 - 1) & 1, gave_up);
                         if (!ok) break;
                     }
-                    ok = bar_wait_warp(raw_full(s), stages / kRawStages & 1, gave_up);
+                    ok = bar_wait_warp(raw_full(s), turn, gave_up);
                     if (!ok) break;
                     const uint8_t *const raw = smem + (smem_c - base) + s * S::kRaw;
-                    const uint32_t to = (value ? smem_v : smem_k);
-                    const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[tiles_done & 3]) >> (half * kRawGranules);
+                    const uint32_t to = (value ? smem_v : smem_k) + (tiles_done & 1) * S::kOperand;
+                    const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) >> (half * kRawGranules);
                     if (!value) {
                         // (position, word % 4): neighbouring lanes have the words % 4 of positions t and t + 4, whose 16-byte pieces are in different banks
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) {
-                            const int unit = thread + 128 * n, c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8;   // 0 .. 63
+                        for (int n = 0; n < 256 / kConverterThreads; ++n) {
+                            const int unit = thread + kConverterThreads * n, c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8;   // 0 .. 63
                             const uint8_t *const granule = raw + t / kGranule * S::kRawGranule;
                             uint32_t scales[kGroupsAll / 2];
 #pragma unroll
@@ -570,8 +632,8 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                     } else {
                         // (pair of positions, word % 8)
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) {
-                            const int unit = thread + 128 * n, g = unit & 7, pair = unit >> 3;   // 0 .. 31
+                        for (int n = 0; n < 256 / kConverterThreads; ++n) {
+                            const int unit = thread + kConverterThreads * n, g = unit & 7, pair = unit >> 3;   // 0 .. 31
                             const uint8_t *const granule = raw + pair / 8 * S::kRawGranule;
 #pragma unroll
                             for (int a = 0; a < F::kSlabs; ++a) {
@@ -598,7 +660,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                                         if (!seen) scale = 0;   // may hold anything
                                         if ((scale & 0x7f80u) == 0x7f80u) {   // no number: for rows that see the position only, see the end of the tile
                                             scale = 0;
-                                            atomicMin(&no_number[pieces & 1][a * F::kGroups + 2 * m + (g >> 2)], position + row);
+                                            atomicMin(&no_number[pieces & 3][a * F::kGroups + 2 * m + (g >> 2)], position + row);
                                         }
                                         uint32_t o[4];
                                         pairs(w[h * kLaneWords + m], pairs.scales(scale_twice<kHalf>(scale, false)), o);
@@ -613,20 +675,24 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                     __syncwarp();
                     if (lane == 0) {
                         bar_arrive(raw_empty(s));
-                        if (half == S::kParts - 1) bar_arrive(value ? values_full : keys_full);
+                        if (half == S::kParts - 1) bar_arrive(value ? values_full(tiles_done & 1) : keys_full(tiles_done & 1));
+                    }
+                    if (++stage == S::kRawStages) {
+                        stage = 0;
+                        turn ^= 1;
                     }
                 }
             }
             if (steps > 0) ++pieces;
         }
-    } else if (warp == kPromptSoftmax + kPromptConverters) {
-        uint32_t stages = 0, tiles_done = 0;
+    } else if (warp == S::kSoftmax + kPromptConverters) {
+        uint32_t stage = 0, turn = 1, issued = 0, tiles_done = 0;
         bool ok = true;
         const int granules = p.r.page_size / kGranule;
         while (ok && walk.next(p.r, p.group)) {
-            const int steps = walk.steps<S::kPositions>(p.group), seen_most = walk.seen_most(p.group);
+            const int steps = walk.template steps<S::kPositions>(p.group), seen_most = walk.seen_most(p.group);
             for (int i = 0; ok && i < steps; ++i, ++tiles_done) {
-                const int at = walk.first * kPromptUnit + i * S::kPositions + lane * kGranule;
+                const int at = walk.first * S::kRows + i * S::kPositions + lane * kGranule;
                 int granule = -1;
                 if (lane < S::kGranules && at <= seen_most) {
                     const int column = at / p.r.page_size;
@@ -636,18 +702,16 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 }
                 const uint32_t have = __ballot_sync(0xffffffffu, granule >= 0);
 #pragma unroll 1
-                for (int part = 0; part < 2 * S::kParts; ++part, ++stages) {
+                for (int part = 0; part < 2 * S::kParts; ++part) {
                     const bool value = part >= S::kParts;
-                    const int half = value ? part - S::kParts : part, s = stages % kRawStages;
-                    if (stages >= kRawStages) {
-                        ok = bar_wait_warp(raw_empty(s), (stages / kRawStages - 1) & 1, gave_up);
-                        if (!ok) break;
-                    }
+                    const int half = value ? part - S::kParts : part, s = stage;
+                    ok = bar_wait_warp(raw_empty(s), turn, gave_up);
+                    if (!ok) break;
                     int from[kRawGranules];
 #pragma unroll
                     for (int j = 0; j < kRawGranules; ++j) from[j] = __shfl_sync(0xffffffffu, granule, half * kRawGranules + j);
                     if (elect_one()) {
-                        if (part == 0) *const_cast<volatile uint32_t *>(&granules_there[tiles_done & 3]) = have;
+                        if (part == 0) *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) = have;
                         bar_expect(raw_full(s), __popc(have >> (half * kRawGranules) & ((1u << kRawGranules) - 1)) * S::kRawGranule);
 #pragma unroll
                         for (int j = 0; j < kRawGranules; ++j)
@@ -659,64 +723,89 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                             }
                     }
                     __syncwarp();
+                    if (issued < S::kRawStages) ++issued;
+                    if (++stage == S::kRawStages) {
+                        stage = 0;
+                        turn ^= 1;
+                    }
                 }
             }
         }
         // the last copies have landed before the block may end
-        for (uint32_t k = stages > kRawStages ? stages - kRawStages : 0; k < stages; ++k) bar_drain(raw_full(k % kRawStages), k / kRawStages & 1);
+        for (uint32_t i = 0; i < issued; ++i) {
+            if (stage-- == 0) {
+                stage = S::kRawStages - 1;
+                turn ^= 1;
+            }
+            bar_drain(raw_full(stage), turn ^ 1);
+        }
     } else {
-        constexpr uint32_t kType = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (static_cast<uint32_t>(kPromptRows >> 4) << 24);
+        constexpr uint32_t kType = (1u << 4) | (kHalf ? 0u : 1u << 7) | (kHalf ? 0u : 1u << 10) | (static_cast<uint32_t>(kSlotRows >> 4) << 24);
         constexpr uint32_t kScoresDesc = kType | (static_cast<uint32_t>(S::kPositions >> 3) << 17);
         constexpr uint32_t kSumsDesc = kType | 1u << 16 | (static_cast<uint32_t>(D >> 3) << 17);   // values with their channels next to each other
-        uint32_t tiles_done = 0, pieces = 0;
-        bool ok = true, products = false;
+        uint32_t tiles_before = 0, pieces = 0, scored[2] = {}, summed[2] = {};   // products of each slot
+        bool ok = true;
         while (ok && walk.next(p.r, p.group)) {
-            const int steps = walk.steps<S::kPositions>(p.group);
+            const int steps = walk.template steps<S::kPositions>(p.group);
             if (steps == 0) continue;
-            ok = bar_wait_warp(queries_full, pieces & 1, gave_up);
-            for (int i = 0; ok && i < steps; ++i, ++tiles_done) {
-                // the scores' place is the weights' of the product before, which has to be done
-                ok = bar_wait_warp(keys_full, tiles_done & 1, gave_up) && (tiles_done == 0 || bar_wait_warp(values_empty, (tiles_done - 1) & 1, gave_up));
-                if (!ok) break;
+            const Events<S::kSlots> events(steps, walk.rows_all(p.group) - walk.tile * S::kRows > kSlotRows);
+            const auto score = [&](int e) {
+                const int slot = events.slot(e);
+                const uint32_t tile = tiles_before + events.tile(e), place = tile & 1, count = slot ? summed[1] : summed[0];
+                // the scores' place is the weights' of the slot's product before, which has to be done
+                ok = (!events.first_use(e) || bar_wait_warp(keys_full(place), tile >> 1 & 1, gave_up)) &&
+                     (count == 0 || bar_wait_warp(weights_empty(slot), (count - 1) & 1, gave_up));
+                if (!ok) return;
                 tc_fence_after();
+                const uint32_t a = smem_q + (events.shared ? slot * S::kQueries : 0), b = smem_k + place * S::kOperand;
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
-                        mma_f16(tmem + S::kScores, desc_low(smem_q + k / 4 * S::kQueryPanel + k % 4 * 32, 16), desc_low(smem_k + k / 4 * S::kPanel + k % 4 * 32, 16), kScoresDesc, k > 0);
-                    mma_commit(scores_full);
-                    mma_commit(keys_empty);
+                        mma_f16(tmem + slot * S::kScores, desc_low(a + k / 4 * S::kQueryPanel + k % 4 * 32, 16), desc_low(b + k / 4 * S::kPanel + k % 4 * 32, 16), kScoresDesc, k > 0);
+                    mma_commit(scores_full(slot));
+                    if (events.last_use(e)) mma_commit(keys_empty(place));
                 }
                 __syncwarp();
-                products = false;
-                ok = bar_wait_warp(weights_full, tiles_done & 1, gave_up) && bar_wait_warp(values_full, tiles_done & 1, gave_up);
+                ++(slot ? scored[1] : scored[0]);
+            };
+            ok = bar_wait_warp(queries_full, pieces & 1, gave_up);
+            for (int e = 0; ok && e < min(events.count, S::kSlots); ++e) score(e);
+            for (int e = 0; ok && e < events.count; ++e) {
+                const int slot = events.slot(e);
+                const uint32_t tile = tiles_before + events.tile(e), place = tile & 1;
+                ok = bar_wait_warp(weights_full(slot), ((slot ? scored[1] : scored[0]) - 1) & 1, gave_up) &&
+                     (!events.first_use(e) || bar_wait_warp(values_full(place), tile >> 1 & 1, gave_up));
                 if (!ok) break;
                 tc_fence_after();
+                const uint32_t b = smem_v + place * S::kOperand;
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < S::kPositions / 16; ++k)
-                        mma_f16_tmem(tmem + S::kSums, tmem + S::kScores + 8 * k, desc_low(smem_v + k * 2048, S::kPanel), kSumsDesc, i > 0 || k > 0);
-                    mma_commit(values_empty);
-                    if (i + 1 == steps) mma_commit(sums_full);
+                        mma_f16_tmem(tmem + S::kFirstSums + slot * S::kSums, tmem + slot * S::kScores + 8 * k, desc_low(b + k * 2048, S::kPanel), kSumsDesc, e >= S::kSlots || k > 0);
+                    mma_commit(weights_empty(slot));
+                    if (events.last_use(e)) mma_commit(values_empty(place));
+                    if (e + S::kSlots >= events.count) mma_commit(sums_full(slot));
                 }
                 __syncwarp();
-                products = true;
+                ++(slot ? summed[1] : summed[0]);
+                if (e + S::kSlots < events.count) score(e + S::kSlots);
             }
+            tiles_before += steps;
             ++pieces;
         }
-        // the tensor cores have done their last product before the block may end
-        if (ok) {
-            if (tiles_done > 0) bar_drain(values_empty, (tiles_done - 1) & 1);
-        } else if (products) {
-            bar_drain(values_empty, (tiles_done - 1) & 1);
-        } else {
-            bar_drain(keys_empty, tiles_done & 1);
+        // the tensor cores have done their last products, and said so, before the block may end
+#pragma unroll
+        for (int slot = 0; slot < S::kSlots; ++slot) {
+            if (scored[slot] > 0) bar_drain(scores_full(slot), (scored[slot] - 1) & 1);
+            if (summed[slot] > 0) bar_drain(weights_empty(slot), (summed[slot] - 1) & 1);
         }
+        if (ok && tiles_before > 0) bar_drain(values_empty((tiles_before - 1) & 1), (tiles_before - 1) >> 1 & 1);
     }
     __syncwarp();
     if (*gave_up) __nanosleep(100000);
     tc_fence_before();
     __syncthreads();
-    if (warp == kPromptSoftmax + kPromptConverters + 1) {
+    if (warp == S::kSoftmax + kPromptConverters + 1) {
         tc_fence_after();
         tmem_free(tmem, S::kColumns);
     }
