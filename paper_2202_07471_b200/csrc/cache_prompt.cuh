@@ -21,7 +21,7 @@ namespace sq {
 
 constexpr int kSlotRows = 128;           // the tensor memory's lanes
 constexpr int kPromptConverters = 4;     // warps
-constexpr int kRawGranules = 4;          // of a stage: keys or values of 64 positions as they are, ahead of the converters
+constexpr int kRawGranules = 2;          // of a stage: granules as they are, ahead of the converters
 constexpr int kTilesAhead = 8;           // score tiles that are being copied, converted or weighed at the same time, at most
 
 template <int D>
@@ -31,12 +31,15 @@ struct PromptShape {
     static constexpr int kPositions = D > 128 ? 64 : 128;            // of a score tile
     static constexpr int kGranules = kPositions / kGranule;
     static constexpr int kQueries = kSlotRows * D * 2, kOperand = kPositions * D * 2, kPanel = kPositions * 128, kQueryPanel = kSlotRows * 128;
-    static constexpr int kRawGranule = 9 * D, kRaw = kRawGranules * kRawGranule;   // codes, then scales
+    static constexpr int kRaw = kRawGranules * CacheFormat<D>::kBytes;
     static constexpr int kRawStages = D > 128 ? 3 : D > 64 ? 6 : 12;
-    static constexpr int kParts = kGranules / kRawGranules;          // stages of a score tile's keys
+    static constexpr int kParts = kGranules / kRawGranules;          // stages of a score tile
     static constexpr int kBars = 2 * kRawStages + 18;
     static constexpr int kSmem = 1024 + kSlots * kQueries + 4 * kOperand + kRawStages * kRaw + 8 * kBars;
-    static constexpr int kScores = 128, kSums = D, kFirstSums = 256, kColumns = 512;   // tensor memory: columns of a slot's scores, of its sums
+    // tensor memory: columns of a slot's scores, sums and weights, which take the scores' place where there is no other
+    static constexpr int kScores = 128, kSums = D, kFirstSums = 256, kColumns = 512;
+    static constexpr bool kApart = kFirstSums + kSlots * (kSums + kPositions / 2) <= kColumns;
+    static constexpr int kFirstWeights = kApart ? kFirstSums + kSlots * kSums : 0, kWeights = kApart ? kPositions / 2 : kScores;
     static constexpr int kPart = kRows * (D + 2);                    // floats of a tile's part in the workspace
     static_assert(kSmem + 2048 <= 227 << 10 && 2 * kSmem > 228 << 10, "one block a multiprocessor, so that all of its tensor memory is there");
     static_assert(kSlots * kScores <= kFirstSums && kFirstSums + kSlots * kSums <= kColumns, "tensor memory");
@@ -44,15 +47,19 @@ struct PromptShape {
 
 // The walk over units of as many positions as a tile has rows, R.  The tile t of a sequence sees its first tokens, and those of its rows up to the tile's last:
 //   units(t) = ceil((len - n + floor((R t + R - 1) / group) + 1) / R) = floor((t + q) / group),   q = floor((group (len - n + R) + R - 1) / R),
-// which is one too many at most, for the last tile.  Sums of floor(i / group) have a closed form, and so does the row of all sequences' units.
+// and kExtra more, with q + kExtra group.  It is one too many at most, for the last tile.  Sums of floor(i / group) have a closed form, and so does the row of all sequences' units.
 template <int kRows>
 struct PromptWalk {
     static constexpr int kUnit = kRows;
+    // A tile's first units stand for what it costs besides its positions: its queries, its first scores, its results (20,000 clocks; a unit takes 10,000).  Without them a
+    // block whose stretch was made of short prompts worked twice as long as the others.
+    static constexpr int kExtra = 2;
     int64_t x, end, base, item0;
     int chunk, row0s, ns, lens;   // sequences chunk + lane
     int b, row0, n, len, tiles;
-    int head, tile, first, last;  // of the piece: kv head, tile, units [first, last) of the tile's
-    int units, over;              // floor and remainder of (tile + q) / group
+    int head, tile, first, last;  // of the piece: kv head, tile, units [first, last) of the tile's positions
+    bool whole;                   // the piece is all of the tile
+    int units, over;              // floor and remainder of (tile + q) / group: the tile's units, with the extra ones
     int64_t q, span;              // span: units of a kv head of sequence b
 
     static __device__ __forceinline__ int64_t floors(int64_t n, int group)   // sum of floor(i / group) below n
@@ -62,7 +69,7 @@ struct PromptWalk {
     }
     static __device__ __forceinline__ int64_t offset_of(int n, int len, int group)
     {
-        return (static_cast<int64_t>(group) * (max(0, len - n) + kUnit) + kRows - 1) / kRows;
+        return (static_cast<int64_t>(group) * (max(0, len - n) + kUnit) + kRows - 1) / kRows + static_cast<int64_t>(kExtra) * group;
     }
     static __device__ __forceinline__ int tiles_of(int n, int group) { return static_cast<int>((static_cast<int64_t>(n) * group + kRows - 1) / kRows); }
     __device__ __forceinline__ void look_up(const CacheRows &r, int from)
@@ -133,9 +140,10 @@ struct PromptWalk {
                 over = static_cast<int>(static_cast<uint32_t>(q) % static_cast<uint32_t>(group));
             }
         }
-        first = static_cast<int>(x - item0);
+        whole = x == item0 && end >= item0 + units;
+        first = max(0, static_cast<int>(x - item0) - kExtra);
         x = min(end, item0 + units);
-        last = static_cast<int>(x - item0);
+        last = max(0, static_cast<int>(x - item0) - kExtra);
         return true;
     }
     __device__ __forceinline__ int rows_all(int group) const { return n * group; }
@@ -194,12 +202,6 @@ __device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b,
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
                  ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)), "n"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32])
 {
     asm volatile(
@@ -211,12 +213,29 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]
           "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
           "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16])
+// A load that other work may be put behind, and the wait for it, behind which the registers hold it.
+__device__ __forceinline__ void tmem_ld16_begin(uint32_t addr, uint32_t (&r)[16])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
                    "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ld16_end(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -247,12 +266,37 @@ struct Events {
     bool shared;   // by both slots
     int count;
     __device__ __forceinline__ Events(int steps, bool both) : shared(kSlots == 2 && both), count(shared ? 2 * steps : steps) {}
-    __device__ __forceinline__ int slot(int e) const { return kSlots == 2 ? e & 1 : 0; }
     __device__ __forceinline__ int tile(int e) const { return shared ? e >> 1 : e; }
-    __device__ __forceinline__ bool first_use(int e) const { return !shared || !(e & 1); }
-    __device__ __forceinline__ bool last_use(int e) const { return !shared || (e & 1); }
     __device__ __forceinline__ int of_slot(int slot) const { return kSlots == 1 ? count : (count + 1 - slot) >> 1; }
 };
+
+// Calls f with constants.  The operands of matrix instructions are uniform registers: addresses that the compiler cannot see to be the same in all lanes cost it a move each, and
+// an instruction its 64 clocks' worth of issue time.
+template <typename F>
+__device__ __forceinline__ void with_flags(uint32_t a, bool b, const F &f)
+{
+    const auto second = [&](auto x) {
+        if (b) f(x, std::true_type{});
+        else f(x, std::false_type{});
+    };
+    if (a) second(std::true_type{});
+    else second(std::false_type{});
+}
+// Whether the phase is over, without a wait.
+__device__ __forceinline__ bool bar_test_warp(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return __all_sync(0xffffffffu, ok != 0);
+}
+
+__device__ __forceinline__ void hide16(uint32_t (&s)[kGranule], int position, int limit, uint32_t have)   // of one granule
+{
+    if (!(have & 1)) limit = -1;
+#pragma unroll
+    for (int e = 0; e < kGranule; ++e)
+        if (position + e > limit) s[e] = 0xff800000u;
+}
 
 template <int D, bool kHalf>
 __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1)
@@ -315,12 +359,13 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_base;
+    constexpr uint32_t tmem = 0;   // all columns have been asked for
+    SQ_LINEAR_CHECK(tmem_base == tmem, 2023);
 
     if (warp < S::kSoftmax) {
         const int quarter = warp & 3, slot = warp >> 2;
         const uint32_t mine = tmem + (static_cast<uint32_t>(32 * quarter) << 16);   // the warp's lanes of tensor memory
-        const uint32_t scores = mine + slot * S::kScores, sums = mine + S::kFirstSums + slot * S::kSums;
+        const uint32_t scores = mine + slot * S::kScores, weights = mine + S::kFirstWeights + slot * S::kWeights, sums = mine + S::kFirstSums + slot * S::kSums;
         const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);   // 0: no score is hidden by a product with infinity
         uint32_t tiles_before = 0, weighed = 0, summed = 0, pieces = 0, joins = 0;
         bool ok = true;
@@ -347,14 +392,23 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;   // rows at once
                 const auto queries = [&](auto on_vectors) {
                     constexpr bool kVector = decltype(on_vectors)::value;
-#pragma unroll (kVector ? 16 : 1)
-                    for (int j = 0; j < 32; j += kAtOnce) {
-                        const int r = j + lane / kPieces, piece = lane % kPieces, local = 32 * quarter + r;
-                        const int64_t from = __shfl_sync(0xffffffffu, offset, r);
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (row - lane + r + tile_row < rows_all) v = load8(p.q + from + 8 * piece, kVector);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem_q + slot * S::kQueries + piece / 8 * S::kQueryPanel + local * 128 + ((piece ^ local) & 7) * 16),
-                                     "r"(v.x ^ flip), "r"(v.y ^ flip), "r"(v.z ^ flip), "r"(v.w ^ flip));
+                    constexpr int kBatch = kVector ? 8 : 1;   // pieces in flight
+#pragma unroll 1
+                    for (int j0 = 0; j0 < 32; j0 += kAtOnce * kBatch) {
+                        uint4 v[kBatch];
+#pragma unroll
+                        for (int i = 0; i < kBatch; ++i) {
+                            const int r = j0 + i * kAtOnce + lane / kPieces;
+                            const int64_t from = __shfl_sync(0xffffffffu, offset, r);
+                            v[i] = make_uint4(0, 0, 0, 0);
+                            if (row - lane + r + tile_row < rows_all) v[i] = load8(p.q + from + 8 * (lane % kPieces), kVector);
+                        }
+#pragma unroll
+                        for (int i = 0; i < kBatch; ++i) {
+                            const int local = 32 * quarter + j0 + i * kAtOnce + lane / kPieces, piece = lane % kPieces;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem_q + slot * S::kQueries + piece / 8 * S::kQueryPanel + local * 128 + ((piece ^ local) & 7) * 16),
+                                         "r"(v[i].x ^ flip), "r"(v[i].y ^ flip), "r"(v[i].z ^ flip), "r"(v[i].w ^ flip));
+                        }
                     }
                 };
                 if (alone || slot == 0) {
@@ -407,47 +461,54 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                     beyond = 0.0f;
                     const Two by(scale, scale);
                     Two sum(total, 0.0f);
-#pragma unroll 1
-                    for (int j = 0; j < S::kPositions; j += 32) {
-                        uint32_t s[32], w[16];
-                        tmem_ld32(scores + j, s);
-                        if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
-                        const Two less(-most, -most);
-                        float x[32], top = beyond;
+                    uint32_t s[16];
+                    tmem_ld16_begin(scores, s);
+                    tmem_ld16_end(s);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
+                    for (int j = 0; j < S::kPositions; j += 16) {
+                        if constexpr (kMasked) hide16(s, position + j, limit, have >> (j / kGranule));
+                        const Two less(-most, -most);
+                        float x[16], tops[4];
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) {
                             fma(Two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), by, less).get(x[e], x[e + 1]);
-                            top = max3(top, x[e], x[e + 1]);
+                            tops[e / 2 % 4] = e < 8 ? fmaxf(x[e], x[e + 1]) : max3(tops[e / 2 % 4], x[e], x[e + 1]);
                         }
+                        if (j + 16 < S::kPositions) tmem_ld16_begin(scores + j + 16, s);   // while the exponentials are taken
+                        float top = max3(max3(tops[0], tops[1], tops[2]), tops[3], beyond);
                         if (__any_sync(0xffffffffu, top > kRoom)) {
                             // too far beyond the maximum for 16 bits: what there is of the row is scaled at once, this tile's weights so far among it
                             const float factor = exp2_fast(-top);
                             float a, b;
                             sum.get(a, b);
                             total = a + b;
+                            tmem_ld16_end(s);
                             scale_sums(factor);
                             sum = Two(total, 0.0f);
                             most += top;
 #pragma unroll 1
-                            for (int k = 0; k < j / 2; k += 16) {
-                                tmem_ld16(scores + k, w);
+                            for (int k = 0; k < j / 2; k += 8) {
+                                uint32_t w[8];
+                                tmem_ld8(weights + k, w);
 #pragma unroll
-                                for (int e = 0; e < 16; ++e)
+                                for (int e = 0; e < 8; ++e)
                                     w[e] = to_16x2<kHalf>(to_float<kHalf>(static_cast<uint16_t>(w[e])) * factor, to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) * factor);
-                                tmem_st16(scores + k, w);
+                                tmem_st8(weights + k, w);
                             }
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] -= top;
+                            for (int e = 0; e < 16; ++e) x[e] -= top;
                             top = 0.0f;
                         }
                         beyond = top;
+                        uint32_t w[8];
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
+                        for (int e = 0; e < 16; e += 2) {
                             const float a = exp2_fast(x[e]), b = exp2_fast(x[e + 1]);
                             sum = add(sum, Two(a, b));
                             w[e / 2] = to_16x2<kHalf>(a, b);
                         }
-                        tmem_st16(scores + j / 2, w);   // the scores there have been read
+                        tmem_st8(weights + j / 2, w);   // the scores there have been read
+                        if (j + 16 < S::kPositions) tmem_ld16_end(s);
                     }
                     float a, b;
                     sum.get(a, b);
@@ -468,7 +529,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 ok = bar_wait_warp(sums_full(slot), summed++ & 1, gave_up);
                 if (!ok) break;
             }
-            const bool whole = walk.first == 0 && walk.last == walk.units;
+            const bool whole = walk.whole;
             float factor = 1.0f, other = 0.0f;   // of the slots' sums
             if (!alone) {
                 if (slot == 1) slot_sums[32 * quarter + lane] = make_float2(most, total);
@@ -576,8 +637,9 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
             }
         }
     } else if (warp < S::kSoftmax + kPromptConverters) {
-        constexpr int kConverterThreads = 32 * kPromptConverters;   // 256 pieces of 16 bytes a stage and slab
-        const int thread = threadIdx.x - 32 * S::kSoftmax;
+        // a stage's keys and values: 128 pieces of 16 bytes (8) and slab of each
+        static_assert(kPromptConverters == 4 && kRawGranules == 2, "one of each a thread");
+        const int unit = threadIdx.x - 32 * S::kSoftmax;
         const CodePairs<kHalf> pairs;
         uint32_t stage = 0, turn = 0, tiles_done = 0, pieces = 0;
         bool ok = true;
@@ -585,97 +647,101 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
             const int steps = walk.template steps<S::kPositions>(p.group), seen_most = walk.seen_most(p.group);
             for (int i = 0; ok && i < steps; ++i, ++tiles_done) {
                 const int position = walk.first * S::kRows + i * S::kPositions;
+                if (tiles_done > 1)   // the products with what is there have been made
+                    ok = bar_wait_warp(keys_empty(tiles_done & 1), (tiles_done / 2 - 1) & 1, gave_up) &&
+                         bar_wait_warp(values_empty(tiles_done & 1), (tiles_done / 2 - 1) & 1, gave_up);
 #pragma unroll 1
-                for (int part = 0; part < 2 * S::kParts; ++part) {
-                    const bool value = part >= S::kParts;
-                    const int half = value ? part - S::kParts : part, s = stage;
-                    if (half == 0 && tiles_done > 1) {   // the products with what is there have been made
-                        ok = bar_wait_warp(value ? values_empty(tiles_done & 1) : keys_empty(tiles_done & 1), (tiles_done / 2 - 1) & 1, gave_up);
-                        if (!ok) break;
-                    }
-                    ok = bar_wait_warp(raw_full(s), turn, gave_up);
+                for (int part = 0; ok && part < S::kParts; ++part) {
+                    ok = bar_wait_warp(raw_full(stage), turn, gave_up);
                     if (!ok) break;
-                    const uint8_t *const raw = smem + (smem_c - base) + s * S::kRaw;
-                    const uint32_t to = (value ? smem_v : smem_k) + (tiles_done & 1) * S::kOperand;
-                    const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) >> (half * kRawGranules);
-                    if (!value) {
+                    const uint8_t *const raw = smem + (smem_c - base) + stage * S::kRaw;
+                    {
+                        const uint32_t to = smem_k + (tiles_done & 1) * S::kOperand;
                         // (position, word % 4): neighbouring lanes have the words % 4 of positions t and t + 4, whose 16-byte pieces are in different banks
+                        const int c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8, row = part * (kRawGranules * kGranule) + t;   // t: 0 .. 31
+                        const uint8_t *const granule = raw + t / kGranule * F::kBytes;
+                        uint32_t scales[kGroupsAll / 2], w[F::kSlabs][4];
 #pragma unroll
-                        for (int n = 0; n < 256 / kConverterThreads; ++n) {
-                            const int unit = thread + kConverterThreads * n, c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8;   // 0 .. 63
-                            const uint8_t *const granule = raw + t / kGranule * S::kRawGranule;
-                            uint32_t scales[kGroupsAll / 2];
+                        for (int j = 0; j < kGroupsAll / 2; ++j) scales[j] = *reinterpret_cast<const uint32_t *>(granule + F::kKeyScales + t % kGranule * (2 * kGroupsAll) + 4 * j);
 #pragma unroll
-                            for (int j = 0; j < kGroupsAll / 2; ++j) scales[j] = *reinterpret_cast<const uint32_t *>(granule + 8 * D + t % kGranule * (2 * kGroupsAll) + 4 * j);
-#pragma unroll
-                            for (int a = 0; a < F::kSlabs; ++a) {
-                                uint32_t w[4];
-                                const uint8_t *const from = granule + a * (64 * F::kWords) + t % kGranule * (4 * F::kWords) + c * F::kWords;
-                                if constexpr (F::kGroups == 2) {
-                                    const uint2 v = *reinterpret_cast<const uint2 *>(from);
-                                    w[0] = v.x; w[1] = v.y;
-                                } else {
-                                    const uint4 v = *reinterpret_cast<const uint4 *>(from);
-                                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-                                }
-                                const int row = half * 64 + t;
-#pragma unroll
-                                for (int j = 0; j < F::kGroups; ++j) {
-                                    const int g = a * F::kGroups + j, word = 4 * g + c;
-                                    uint32_t o[4];
-                                    pairs(w[j], pairs.scales(scale_twice<kHalf>(scales[g / 2], g & 1)), o);
-                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + word / 8 * S::kPanel + row * 128 + ((word ^ row) & 7) * 16),
-                                                 "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                                }
+                        for (int a = 0; a < F::kSlabs; ++a) {
+                            const uint8_t *const from = granule + a * (64 * F::kWords) + t % kGranule * (4 * F::kWords) + c * F::kWords;
+                            if constexpr (F::kGroups == 2) {
+                                const uint2 v = *reinterpret_cast<const uint2 *>(from);
+                                w[a][0] = v.x; w[a][1] = v.y;
+                            } else {
+                                const uint4 v = *reinterpret_cast<const uint4 *>(from);
+                                w[a][0] = v.x; w[a][1] = v.y; w[a][2] = v.z; w[a][3] = v.w;
                             }
                         }
-                    } else {
+#pragma unroll
+                        for (int g = 0; g < kGroupsAll; ++g) {
+                            const int word = 4 * g + c;
+                            uint32_t o[4];
+                            pairs(w[g / F::kGroups][g % F::kGroups], pairs.scales(scale_twice<kHalf>(scales[g / 2], g & 1)), o);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + word / 8 * S::kPanel + row * 128 + ((word ^ row) & 7) * 16),
+                                         "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                        }
+                    }
+                    {
+                        const uint32_t to = smem_v + (tiles_done & 1) * S::kOperand;
                         // (pair of positions, word % 8)
+                        constexpr int kLaneWords = F::kWords / 8;
+                        const int g = unit & 7, pair = unit >> 3, row = part * (kRawGranules * kGranule) + 2 * pair;   // pair: 0 .. 15
+                        const uint8_t *const granule = raw + pair / 8 * F::kBytes;
+                        const bool there = *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) >> (part * kRawGranules + pair / 8) & 1;
+                        // positions behind the last one that any row sees, and granules that are not there, may hold anything
+                        const uint32_t seen = (there && position + row <= seen_most ? 0xffffu : 0u) | (there && position + row + 1 <= seen_most ? 0xffff0000u : 0u);
+                        uint32_t scales[F::kSlabs][kLaneWords], w[F::kSlabs][4];
+                        bool odd = false;
 #pragma unroll
-                        for (int n = 0; n < 256 / kConverterThreads; ++n) {
-                            const int unit = thread + kConverterThreads * n, g = unit & 7, pair = unit >> 3;   // 0 .. 31
-                            const uint8_t *const granule = raw + pair / 8 * S::kRawGranule;
+                        for (int a = 0; a < F::kSlabs; ++a) {
+                            const uint8_t *const from = granule + F::kValues + a * (64 * F::kWords) + (pair % 8 * 8 + g) * (8 * kLaneWords);
+                            if constexpr (kLaneWords == 1) {
+                                const uint2 v = *reinterpret_cast<const uint2 *>(from);
+                                w[a][0] = v.x; w[a][1] = v.y;
+                            } else {
+                                const uint4 v = *reinterpret_cast<const uint4 *>(from);
+                                w[a][0] = v.x; w[a][1] = v.y; w[a][2] = v.z; w[a][3] = v.w;
+                            }
 #pragma unroll
-                            for (int a = 0; a < F::kSlabs; ++a) {
-                                constexpr int kLaneWords = F::kWords / 8;
-                                uint32_t w[4], scales[kLaneWords];
-                                const uint8_t *const from = granule + a * (64 * F::kWords) + (pair % 8 * 8 + g) * (8 * kLaneWords);
-                                if constexpr (kLaneWords == 1) {
-                                    const uint2 v = *reinterpret_cast<const uint2 *>(from);
-                                    w[0] = v.x; w[1] = v.y;
-                                } else {
-                                    const uint4 v = *reinterpret_cast<const uint4 *>(from);
-                                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-                                }
+                            for (int m = 0; m < kLaneWords; ++m) {
+                                scales[a][m] = seen & *reinterpret_cast<const uint32_t *>(granule + F::kValueScales + a * (32 * F::kGroups) + pair % 8 * (4 * F::kGroups) + (g >> 2) * (2 * F::kGroups) + 4 * m);
+                                odd |= (scales[a][m] & 0x7f80u) == 0x7f80u || (scales[a][m] & 0x7f800000u) == 0x7f800000u;
+                            }
+                        }
+                        if (odd) {   // no number: for rows that see the position only, see the end of the tile
+#pragma unroll
+                            for (int a = 0; a < F::kSlabs; ++a)
 #pragma unroll
                                 for (int m = 0; m < kLaneWords; ++m)
-                                    scales[m] = *reinterpret_cast<const uint32_t *>(granule + 8 * D + a * (32 * F::kGroups) + pair % 8 * (4 * F::kGroups) + (g >> 2) * (2 * F::kGroups) + 4 * m);
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h)
+                                        if ((scales[a][m] >> (16 * h) & 0x7f80u) == 0x7f80u) {
+                                            scales[a][m] &= h ? 0x0000ffffu : 0xffff0000u;
+                                            atomicMin(&no_number[pieces & 3][a * F::kGroups + 2 * m + (g >> 2)], position + row + h);
+                                        }
+                        }
+#pragma unroll
+                        for (int a = 0; a < F::kSlabs; ++a)
+#pragma unroll
+                            for (int m = 0; m < kLaneWords; ++m)
 #pragma unroll
                                 for (int h = 0; h < 2; ++h) {
-                                    const int row = half * 64 + 2 * pair + h;
-                                    const bool seen = position + row <= seen_most && (have >> (pair / 8) & 1);
-#pragma unroll
-                                    for (int m = 0; m < kLaneWords; ++m) {
-                                        uint32_t scale = h ? scales[m] >> 16 : scales[m] & 0xffffu;
-                                        if (!seen) scale = 0;   // may hold anything
-                                        if ((scale & 0x7f80u) == 0x7f80u) {   // no number: for rows that see the position only, see the end of the tile
-                                            scale = 0;
-                                            atomicMin(&no_number[pieces & 3][a * F::kGroups + 2 * m + (g >> 2)], position + row);
-                                        }
-                                        uint32_t o[4];
-                                        pairs(w[h * kLaneWords + m], pairs.scales(scale_twice<kHalf>(scale, false)), o);
-                                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (a * kLaneWords + m) * S::kPanel + row * 128 + ((g ^ row) & 7) * 16),
-                                                     "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                                    }
+                                    uint32_t o[4];
+                                    pairs(w[a][h * kLaneWords + m], pairs.scales(scale_twice<kHalf>(scales[a][m], h)), o);
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (a * kLaneWords + m) * S::kPanel + (row + h) * 128 + ((g ^ (row + h)) & 7) * 16),
+                                                 "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                                 }
-                            }
-                        }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
-                        bar_arrive(raw_empty(s));
-                        if (half == S::kParts - 1) bar_arrive(value ? values_full(tiles_done & 1) : keys_full(tiles_done & 1));
+                        bar_arrive(raw_empty(stage));
+                        if (part == S::kParts - 1) {
+                            bar_arrive(keys_full(tiles_done & 1));
+                            bar_arrive(values_full(tiles_done & 1));
+                        }
                     }
                     if (++stage == S::kRawStages) {
                         stage = 0;
@@ -702,25 +768,16 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 }
                 const uint32_t have = __ballot_sync(0xffffffffu, granule >= 0);
 #pragma unroll 1
-                for (int part = 0; part < 2 * S::kParts; ++part) {
-                    const bool value = part >= S::kParts;
-                    const int half = value ? part - S::kParts : part, s = stage;
-                    ok = bar_wait_warp(raw_empty(s), turn, gave_up);
+                for (int part = 0; part < S::kParts; ++part) {
+                    ok = bar_wait_warp(raw_empty(stage), turn, gave_up);
                     if (!ok) break;
-                    int from[kRawGranules];
-#pragma unroll
-                    for (int j = 0; j < kRawGranules; ++j) from[j] = __shfl_sync(0xffffffffu, granule, half * kRawGranules + j);
+                    const int from = __shfl_sync(0xffffffffu, granule, part * kRawGranules), next = __shfl_sync(0xffffffffu, granule, part * kRawGranules + 1);
                     if (elect_one()) {
+                        const uint32_t dst = smem_c + stage * S::kRaw, bar = raw_full(stage);
                         if (part == 0) *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) = have;
-                        bar_expect(raw_full(s), __popc(have >> (half * kRawGranules) & ((1u << kRawGranules) - 1)) * S::kRawGranule);
-#pragma unroll
-                        for (int j = 0; j < kRawGranules; ++j)
-                            if (from[j] >= 0) {
-                                const uint8_t *const src = p.cache + static_cast<int64_t>(from[j]) * F::kBytes;
-                                const uint32_t dst = smem_c + s * S::kRaw + j * S::kRawGranule;
-                                bulk_load(dst, src + (value ? F::kValues : 0), 8 * D, raw_full(s));
-                                bulk_load(dst + 8 * D, src + (value ? F::kValueScales : F::kKeyScales), D, raw_full(s));
-                            }
+                        bar_expect(bar, ((from >= 0) + (next >= 0)) * F::kBytes);
+                        if (from >= 0) bulk_load(dst, p.cache + static_cast<int64_t>(from) * F::kBytes, next == from + 1 ? S::kRaw : F::kBytes, bar);
+                        if (next >= 0 && (from < 0 || next != from + 1)) bulk_load(dst + F::kBytes, p.cache + static_cast<int64_t>(next) * F::kBytes, F::kBytes, bar);
                     }
                     __syncwarp();
                     if (issued < S::kRawStages) ++issued;
@@ -744,51 +801,78 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
         constexpr uint32_t kScoresDesc = kType | (static_cast<uint32_t>(S::kPositions >> 3) << 17);
         constexpr uint32_t kSumsDesc = kType | 1u << 16 | (static_cast<uint32_t>(D >> 3) << 17);   // values with their channels next to each other
         uint32_t tiles_before = 0, pieces = 0, scored[2] = {}, summed[2] = {};   // products of each slot
+        int keys_used[2] = {}, values_used[2] = {}, tries = 0;   // by how many slots, of the tile in a place
         bool ok = true;
         while (ok && walk.next(p.r, p.group)) {
             const int steps = walk.template steps<S::kPositions>(p.group);
             if (steps == 0) continue;
             const Events<S::kSlots> events(steps, walk.rows_all(p.group) - walk.tile * S::kRows > kSlotRows);
-            const auto score = [&](int e) {
-                const int slot = events.slot(e);
-                const uint32_t tile = tiles_before + events.tile(e), place = tile & 1, count = slot ? summed[1] : summed[0];
-                // the scores' place is the weights' of the slot's product before, which has to be done
-                ok = (!events.first_use(e) || bar_wait_warp(keys_full(place), tile >> 1 & 1, gave_up)) &&
-                     (count == 0 || bar_wait_warp(weights_empty(slot), (count - 1) & 1, gave_up));
-                if (!ok) return;
-                tc_fence_after();
-                const uint32_t a = smem_q + (events.shared ? slot * S::kQueries : 0), b = smem_k + place * S::kOperand;
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        mma_f16(tmem + slot * S::kScores, desc_low(a + k / 4 * S::kQueryPanel + k % 4 * 32, 16), desc_low(b + k / 4 * S::kPanel + k % 4 * 32, 16), kScoresDesc, k > 0);
-                    mma_commit(scores_full(slot));
-                    if (events.last_use(e)) mma_commit(keys_empty(place));
-                }
-                __syncwarp();
-                ++(slot ? scored[1] : scored[0]);
-            };
             ok = bar_wait_warp(queries_full, pieces & 1, gave_up);
-            for (int e = 0; ok && e < min(events.count, S::kSlots); ++e) score(e);
-            for (int e = 0; ok && e < events.count; ++e) {
-                const int slot = events.slot(e);
+            // each slot's next product, as soon as what it takes is there: the scores of event at[], or, if they have been asked for, the sums of it
+            int at[2] = {0, 1};
+            bool asked[2] = {false, false};
+            const int used_by = events.shared ? 2 : 1;
+            const auto turn = [&](auto slot_c) {
+                constexpr int kSlot = decltype(slot_c)::value;
+                const int e = at[kSlot];
+                if (e >= events.count) return;
                 const uint32_t tile = tiles_before + events.tile(e), place = tile & 1;
-                ok = bar_wait_warp(weights_full(slot), ((slot ? scored[1] : scored[0]) - 1) & 1, gave_up) &&
-                     (!events.first_use(e) || bar_wait_warp(values_full(place), tile >> 1 & 1, gave_up));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t b = smem_v + place * S::kOperand;
-                if (elect_one()) {
+                if (!asked[kSlot]) {
+                    // keys; the scores' place, if the weights of the slot's product before have it, when that has been made
+                    if (!bar_test_warp(keys_full(place), tile >> 1 & 1)) return;
+                    if (!S::kApart && summed[kSlot] > 0 && !bar_test_warp(weights_empty(kSlot), (summed[kSlot] - 1) & 1)) return;
+                    tc_fence_after();
+                    const bool last = ++keys_used[place] == used_by;
+                    if (last) keys_used[place] = 0;
+                    with_flags(place, events.shared, [&](auto place_c, auto shared_c) {
+                        constexpr int kPlace = decltype(place_c)::value, kOwn = decltype(shared_c)::value ? kSlot : 0;
+                        if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < S::kPositions / 16; ++k)
-                        mma_f16_tmem(tmem + S::kFirstSums + slot * S::kSums, tmem + slot * S::kScores + 8 * k, desc_low(b + k * 2048, S::kPanel), kSumsDesc, e >= S::kSlots || k > 0);
-                    mma_commit(weights_empty(slot));
-                    if (events.last_use(e)) mma_commit(values_empty(place));
-                    if (e + S::kSlots >= events.count) mma_commit(sums_full(slot));
+                            for (int k = 0; k < D / 16; ++k)
+                                mma_f16(kSlot * S::kScores, desc_low(smem_q + kOwn * S::kQueries + k / 4 * S::kQueryPanel + k % 4 * 32, 16),
+                                        desc_low(smem_k + kPlace * S::kOperand + k / 4 * S::kPanel + k % 4 * 32, 16), kScoresDesc, k > 0);
+                            mma_commit(scores_full(kSlot));
+                            if (last) mma_commit(keys_empty(kPlace));
+                        }
+                    });
+                    __syncwarp();
+                    ++scored[kSlot];
+                    asked[kSlot] = true;
+                } else {
+                    if (!bar_test_warp(weights_full(kSlot), (scored[kSlot] - 1) & 1) || !bar_test_warp(values_full(place), tile >> 1 & 1)) return;
+                    tc_fence_after();
+                    const bool last = ++values_used[place] == used_by, begins = e < S::kSlots, ends = e + S::kSlots >= events.count;
+                    if (last) values_used[place] = 0;
+                    with_flags(place, false, [&](auto place_c, auto) {
+                        constexpr int kPlace = decltype(place_c)::value;
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < S::kPositions / 16; ++k)
+                                mma_f16_tmem(S::kFirstSums + kSlot * S::kSums, S::kFirstWeights + kSlot * S::kWeights + 8 * k, desc_low(smem_v + kPlace * S::kOperand + k * 2048, S::kPanel),
+                                             kSumsDesc, k > 0 || !begins);
+                            mma_commit(weights_empty(kSlot));
+                            if (last) mma_commit(values_empty(kPlace));
+                            if (ends) mma_commit(sums_full(kSlot));
+                        }
+                    });
+                    __syncwarp();
+                    ++summed[kSlot];
+                    asked[kSlot] = false;
+                    at[kSlot] = e + S::kSlots;
+                    tries = 0;
                 }
-                __syncwarp();
-                ++(slot ? summed[1] : summed[0]);
-                if (e + S::kSlots < events.count) score(e + S::kSlots);
+            };
+            while (ok && (at[0] < events.count || (S::kSlots > 1 && at[1] < events.count))) {
+                turn(std::integral_constant<int, 0>{});
+                if constexpr (S::kSlots > 1) turn(std::integral_constant<int, 1>{});
+                // no try waits: a second's worth of them
+                if (__any_sync(0xffffffffu, ++tries > (wait_limit() << 6 | 63) || *gave_up)) {
+                    if (lane == 0) {
+                        *gave_up = 1;
+                        atomicExch(&g_linear_status, 1);
+                    }
+                    ok = false;
+                }
             }
             tiles_before += steps;
             ++pieces;

@@ -1,6 +1,8 @@
 // Keys and values into the cache and back.
 #pragma once
 
+#include <type_traits>
+
 #include "cache_device.cuh"
 
 namespace sq {
@@ -68,14 +70,19 @@ cache_write_kernel(const __grid_constant__ MoveArgs p)
     const int head0 = static_cast<int>(unit % p.blocks) * kMoveHeads<D>;
     if (row >= p.r.rows) return;
     uint4 x[kMoveLoads];
+    const auto load = [&](auto on_vectors) {
 #pragma unroll
-    for (int i = 0; i < kMoveLoads; ++i) {
-        const Piece<D> at(i);
-        const int head = head0 + at.head;
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (head < p.r.kv_heads)
-            x[i] = load8(at.value ? p.v + row * p.v_stride + head * p.v_head + 8 * at.word : p.k + row * p.k_stride + head * p.k_head + 8 * at.word, p.vector);
-    }
+        for (int i = 0; i < kMoveLoads; ++i) {
+            const Piece<D> at(i);
+            const int head = head0 + at.head;
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (head < p.r.kv_heads)
+                x[i] = load8(at.value ? p.v + row * p.v_stride + head * p.v_head + 8 * at.word : p.k + row * p.k_stride + head * p.k_head + 8 * at.word,
+                             decltype(on_vectors)::value);
+        }
+    };
+    if (p.vector) load(std::true_type{});
+    else load(std::false_type{});
     int b;
     int64_t position;
     const Place to = place_of<D>(p, row, b, position);

@@ -373,19 +373,25 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
         const int at0 = walk.tile * kRows, rows_all = walk.rows_all(p.group);   // of the sequence's rows times heads
         // queries: lane (g, c) has 8 channels of each group of row g
         uint4 q[S::kHeld ? kTiles * kGroupsAll : 1];
-        const auto query = [&](int i) {   // tile i / kGroupsAll, group i % kGroupsAll
-            const int at = at0 + 8 * (i / kGroupsAll) + g;
-            if (at >= rows_all) return make_uint4(0, 0, 0, 0);
-            const Target to(p, walk.row0, walk.head, at);
-            return load8(p.q + to.row * p.q_stride + to.head * p.q_head + kGroup * (i % kGroupsAll) + 8 * c, p.q_vector);
+        const auto queries = [&](auto on_vectors) {   // tile i / kGroupsAll, group i % kGroupsAll
+            constexpr int kBatch = kGroupsAll;         // loads in flight
+#pragma unroll
+            for (int r = 0; r < kTiles; ++r) {
+                uint4 v[kBatch];
+                const int at = at0 + 8 * r + g;
+                const Target to(p, walk.row0, walk.head, min(at, rows_all - 1));
+                const uint16_t *const from = p.q + to.row * p.q_stride + to.head * p.q_head + 8 * c;
+#pragma unroll
+                for (int n = 0; n < kBatch; ++n) v[n] = at < rows_all ? load8(from + kGroup * n, decltype(on_vectors)::value) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int n = 0; n < kBatch; ++n) {
+                    if constexpr (S::kHeld) q[r * kGroupsAll + n] = v[n];
+                    else held_q[(r * kGroupsAll + n) * 32 + lane] = v[n];   // read back by the lane itself
+                }
+            }
         };
-        if constexpr (S::kHeld) {
-#pragma unroll
-            for (int i = 0; i < kTiles * kGroupsAll; ++i) q[i] = query(i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kTiles * kGroupsAll; ++i) held_q[i * 32 + lane] = query(i);   // read back by the lane itself
-        }
+        if (p.q_vector) queries(std::true_type{});
+        else queries(std::false_type{});
         // the lane's rows: 8 r + 2 c and the next
         int limit[kTiles][2];
 #pragma unroll
