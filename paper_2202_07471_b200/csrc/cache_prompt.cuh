@@ -21,7 +21,6 @@ namespace sq {
 
 constexpr int kSlotRows = 128;           // the tensor memory's lanes
 constexpr int kPromptConverters = 4;     // warps
-constexpr int kRawGranules = 2;          // of a stage: granules as they are, ahead of the converters
 constexpr int kTilesAhead = 8;           // score tiles that are being copied, converted or weighed at the same time, at most
 
 template <int D>
@@ -31,8 +30,8 @@ struct PromptShape {
     static constexpr int kPositions = D > 128 ? 64 : 128;            // of a score tile
     static constexpr int kGranules = kPositions / kGranule;
     static constexpr int kQueries = kSlotRows * D * 2, kOperand = kPositions * D * 2, kPanel = kPositions * 128, kQueryPanel = kSlotRows * 128;
-    static constexpr int kRaw = kRawGranules * CacheFormat<D>::kBytes;
-    static constexpr int kRawStages = D > 128 ? 3 : D > 64 ? 6 : 12;
+    // stages of granules as they are, ahead of the converters
+    static constexpr int kRawGranules = D > 128 ? 2 : 4, kRaw = kRawGranules * CacheFormat<D>::kBytes, kRawStages = D > 64 ? 3 : 6;
     static constexpr int kParts = kGranules / kRawGranules;          // stages of a score tile
     static constexpr int kBars = 2 * kRawStages + 18;
     static constexpr int kSmem = 1024 + kSlots * kQueries + 4 * kOperand + kRawStages * kRaw + 8 * kBars;
@@ -637,8 +636,8 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
             }
         }
     } else if (warp < S::kSoftmax + kPromptConverters) {
-        // a stage's keys and values: 128 pieces of 16 bytes (8) and slab of each
-        static_assert(kPromptConverters == 4 && kRawGranules == 2, "one of each a thread");
+        // keys and values of two granules: 128 pieces of 16 bytes (8) and slab of each
+        static_assert(kPromptConverters == 4, "one of each a thread and two granules");
         const int unit = threadIdx.x - 32 * S::kSoftmax;
         const CodePairs<kHalf> pairs;
         uint32_t stage = 0, turn = 0, tiles_done = 0, pieces = 0;
@@ -654,11 +653,14 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 for (int part = 0; ok && part < S::kParts; ++part) {
                     ok = bar_wait_warp(raw_full(stage), turn, gave_up);
                     if (!ok) break;
-                    const uint8_t *const raw = smem + (smem_c - base) + stage * S::kRaw;
+#pragma unroll 1
+                    for (int two = 0; two < S::kRawGranules; two += 2) {
+                    const uint8_t *const raw = smem + (smem_c - base) + stage * S::kRaw + two * F::kBytes;
+                    const int first_row = (part * S::kRawGranules + two) * kGranule;
                     {
                         const uint32_t to = smem_k + (tiles_done & 1) * S::kOperand;
                         // (position, word % 4): neighbouring lanes have the words % 4 of positions t and t + 4, whose 16-byte pieces are in different banks
-                        const int c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8, row = part * (kRawGranules * kGranule) + t;   // t: 0 .. 31
+                        const int c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8, row = first_row + t;   // t: 0 .. 31
                         const uint8_t *const granule = raw + t / kGranule * F::kBytes;
                         uint32_t scales[kGroupsAll / 2], w[F::kSlabs][4];
 #pragma unroll
@@ -687,9 +689,9 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                         const uint32_t to = smem_v + (tiles_done & 1) * S::kOperand;
                         // (pair of positions, word % 8)
                         constexpr int kLaneWords = F::kWords / 8;
-                        const int g = unit & 7, pair = unit >> 3, row = part * (kRawGranules * kGranule) + 2 * pair;   // pair: 0 .. 15
+                        const int g = unit & 7, pair = unit >> 3, row = first_row + 2 * pair;   // pair: 0 .. 15
                         const uint8_t *const granule = raw + pair / 8 * F::kBytes;
-                        const bool there = *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) >> (part * kRawGranules + pair / 8) & 1;
+                        const bool there = *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) >> (first_row / kGranule + pair / 8) & 1;
                         // positions behind the last one that any row sees, and granules that are not there, may hold anything
                         const uint32_t seen = (there && position + row <= seen_most ? 0xffffu : 0u) | (there && position + row + 1 <= seen_most ? 0xffff0000u : 0u);
                         uint32_t scales[F::kSlabs][kLaneWords], w[F::kSlabs][4];
@@ -734,6 +736,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                                                  "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                                 }
                     }
+                    }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
@@ -753,31 +756,47 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
         }
     } else if (warp == S::kSoftmax + kPromptConverters) {
         uint32_t stage = 0, turn = 1, issued = 0, tiles_done = 0;
+        int granule = -1;   // the lane's, of the score tiles to come
         bool ok = true;
         const int granules = p.r.page_size / kGranule;
         while (ok && walk.next(p.r, p.group)) {
             const int steps = walk.template steps<S::kPositions>(p.group), seen_most = walk.seen_most(p.group);
             for (int i = 0; ok && i < steps; ++i, ++tiles_done) {
-                const int at = walk.first * S::kRows + i * S::kPositions + lane * kGranule;
-                int granule = -1;
-                if (lane < S::kGranules && at <= seen_most) {
-                    const int column = at / p.r.page_size;
-                    const int64_t page = page_of(p.r, walk.b, column);
-                    SQ_LINEAR_CHECK(column < p.r.width, 2022);
-                    if (page >= 0) granule = static_cast<int>((page * p.r.kv_heads + walk.head) * granules + (at - column * p.r.page_size) / kGranule);
+                constexpr int kBatch = 32 / S::kGranules;   // score tiles whose granules are looked up together
+                if (i % kBatch == 0) {
+                    const int at = walk.first * S::kRows + i * S::kPositions + lane * kGranule;
+                    granule = -1;
+                    if (at <= seen_most) {
+                        const int column = at / p.r.page_size;
+                        const int64_t page = page_of(p.r, walk.b, column);
+                        SQ_LINEAR_CHECK(column < p.r.width, 2022);
+                        if (page >= 0) granule = static_cast<int>((page * p.r.kv_heads + walk.head) * granules + (at - column * p.r.page_size) / kGranule);
+                    }
                 }
-                const uint32_t have = __ballot_sync(0xffffffffu, granule >= 0);
+                const int from_lane = i % kBatch * S::kGranules;
+                const uint32_t have = __ballot_sync(0xffffffffu, granule >= 0) >> from_lane & ((1u << S::kGranules) - 1);
 #pragma unroll 1
                 for (int part = 0; part < S::kParts; ++part) {
                     ok = bar_wait_warp(raw_empty(stage), turn, gave_up);
                     if (!ok) break;
-                    const int from = __shfl_sync(0xffffffffu, granule, part * kRawGranules), next = __shfl_sync(0xffffffffu, granule, part * kRawGranules + 1);
+                    int from[S::kRawGranules];
+                    bool run = true;   // one behind the other
+#pragma unroll
+                    for (int j = 0; j < S::kRawGranules; ++j) {
+                        from[j] = __shfl_sync(0xffffffffu, granule, from_lane + part * S::kRawGranules + j);
+                        run = run && from[j] >= 0 && from[j] == from[0] + j;
+                    }
                     if (elect_one()) {
                         const uint32_t dst = smem_c + stage * S::kRaw, bar = raw_full(stage);
                         if (part == 0) *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) = have;
-                        bar_expect(bar, ((from >= 0) + (next >= 0)) * F::kBytes);
-                        if (from >= 0) bulk_load(dst, p.cache + static_cast<int64_t>(from) * F::kBytes, next == from + 1 ? S::kRaw : F::kBytes, bar);
-                        if (next >= 0 && (from < 0 || next != from + 1)) bulk_load(dst + F::kBytes, p.cache + static_cast<int64_t>(next) * F::kBytes, F::kBytes, bar);
+                        bar_expect(bar, __popc(have >> (part * S::kRawGranules) & ((1u << S::kRawGranules) - 1)) * F::kBytes);
+                        if (run) {
+                            bulk_load(dst, p.cache + static_cast<int64_t>(from[0]) * F::kBytes, S::kRaw, bar);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < S::kRawGranules; ++j)
+                                if (from[j] >= 0) bulk_load(dst + j * F::kBytes, p.cache + static_cast<int64_t>(from[j]) * F::kBytes, F::kBytes, bar);
+                        }
                     }
                     __syncwarp();
                     if (issued < S::kRawStages) ++issued;
