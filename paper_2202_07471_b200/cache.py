@@ -47,7 +47,26 @@ class CacheAttentionArgs(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_int64)]
 
 
+_device = linear._device
 _ready = None
+_checked = (None, None, None)   # extension, library, and the extension if it was built with the library's argument structs
+
+
+def _native():
+    """The extension that makes whole calls for plain tensors (None: not built, or built with other argument structs)."""
+    global _checked
+    if _checked[0] is binding._marshal and _checked[1] is binding._lib and _checked[1] is not None:
+        return _checked[2]
+    if not torch.cuda.is_initialized():
+        return None
+    m, lib = binding._marshal, _lib()
+    fits = (getattr(m, "cache_move_bytes", None) == ctypes.sizeof(CacheMoveArgs) and getattr(m, "cache_attention_bytes", None) == ctypes.sizeof(CacheAttentionArgs)
+            and binding._raw_stream is not None)
+    if fits:
+        m.use_cache(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in ("squant_cache_write", "squant_cache_read", "squant_cache_attention",
+                                                                                   "squant_cache_attention_workspace")))
+    _checked = (m, lib, m if fits else None)
+    return _checked[2]
 
 
 def _lib() -> ctypes.CDLL:
@@ -126,6 +145,11 @@ def squant_cache_write(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, le
 
     32 neighbouring channels share a scale, the largest magnitude over 7 rounded to four significant bits; a value is at most half a scale off.  Groups with an
     infinity, a NaN or a magnitude from 2^120 on stand for NaN.  No two rows of a call may have the same place."""
+    native = None if stream is not None else _native()
+    if native is not None:
+        device = _device()
+        if _result(native.cache_write(binding._raw_stream(device), device, cache, lens, pages, starts, k, v)) is not None:
+            return
     _no_graph("squant_cache_write", k, v)
     device = cache.device
     with _On(device, stream) as handle:
@@ -146,6 +170,12 @@ def squant_cache_read(cache: torch.Tensor, lens: torch.Tensor, pages: torch.Tens
 
     Rows before a sequence's first position or in a page that is not there are zeros.  k, v: tensors to write, both or none; in new ones, rows behind the
     last sequence hold anything."""
+    native = None if stream is not None or k is not None or v is not None or dtype not in _TYPES else _native()
+    if native is not None:
+        device = _device()
+        got = native.cache_read(binding._raw_stream(device), device, cache, lens, pages, starts, rows, _TYPES[dtype])
+        if got is not None:
+            return _result(got)
     device = cache.device
     with _On(device, stream) as handle:
         if rows < 0:
@@ -178,6 +208,12 @@ def squant_cache_attention(q: torch.Tensor, cache: torch.Tensor, lens: torch.Ten
     most: the number of rows that no sequence has more of, where the caller knows it (it helps to choose the kernel and changes nothing else).  With `lse` returns
     (out, logarithms of the sums of exponentials, fp32 [rows, heads]).  out: the tensor to write, like q; in a new one, rows behind the last sequence hold
     anything.  A row that sees nothing is zeros, its lse -infinity."""
+    native = None if stream is not None or q.dim() != 3 else _native()
+    if native is not None:
+        device = _device()
+        got = native.cache_attention(binding._raw_stream(device), device, cache, lens, pages, starts, q, out, 1.0 / math.sqrt(q.shape[2] or 1) if scale is None else scale, most, lse)
+        if got is not None:
+            return _result(got)
     _no_graph("squant_cache_attention", q, out)
     device = cache.device
     with _On(device, stream) as handle:

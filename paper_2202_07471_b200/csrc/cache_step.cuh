@@ -410,8 +410,7 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
 
         for (int unit = dead ? walk.last : walk.first; unit < walk.last; ++unit) {
             const unsigned stage = consumed % kStepStages;
-            // most copies have landed by now
-            if (!__all_sync(0xffffffffu, bar_try(bars + 8 * stage, consumed / kStepStages & 1)) && !bar_wait_warp(bars + 8 * stage, consumed / kStepStages & 1, gave_up)) {
+            if (!bar_wait_warp(bars + 8 * stage, consumed / kStepStages & 1, gave_up)) {
                 dead = true;
                 break;
             }

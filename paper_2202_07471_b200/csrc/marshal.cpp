@@ -5,14 +5,17 @@
 // would reject.  It neither keeps nor caches anything.
 // linear(), linear_backward(), checkpoint() and restore() make whole calls of the linear operators (linear.py) for plain
 // tensors of the current device: about 20 us in Python, longer than the GPU needs for few tokens.  They return None for
-// whatever they leave to the Python code, which checks the arguments anew and has the errors' texts.
+// whatever they leave to the Python code, which checks the arguments anew and has the errors' texts.  cache_write(), cache_read() and
+// cache_attention() do the same for the key/value cache (cache.py).
 #include <Python.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_like.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstddef>
 #include <limits>
 
@@ -115,6 +118,10 @@ using GradFn = int (*)(const squant_linear_grad_args *, void *);
 using GradNeedFn = int64_t (*)(const squant_linear_grad_args *);
 using CheckpointFn = int (*)(const void *, int64_t, int32_t, int64_t, const squant_checkpoint_data *, void *);
 using RestoreFn = int (*)(const squant_checkpoint_data *, int64_t, int32_t, void *, int64_t, void *);
+
+using CacheMoveFn = int (*)(const squant_cache_move_args *, void *);
+using CacheFn = int (*)(const squant_cache_attention_args *, void *);
+using CacheNeedFn = int64_t (*)(const squant_cache_attention_args *);
 
 constexpr int64_t kMostRows = std::numeric_limits<int32_t>::max();
 
@@ -386,7 +393,177 @@ PyObject *restore(PyObject *, PyObject *args)
     });
 }
 
-PyMethodDef methods[] = {{"use", use, METH_VARARGS, "addresses of the library's functions"},
+// ---- key/value cache
+
+struct CacheLibrary {
+    CacheMoveFn write, read;
+    CacheFn attention;
+    CacheNeedFn attention_need;
+} s_cache;
+
+PyObject *use_cache(PyObject *, PyObject *args)
+{
+    unsigned long long a[4];
+    if (!PyArg_ParseTuple(args, "KKKK", &a[0], &a[1], &a[2], &a[3])) return nullptr;
+    const auto at = [&](int i) { return static_cast<uintptr_t>(a[i]); };
+    s_cache = {reinterpret_cast<CacheMoveFn>(at(0)), reinterpret_cast<CacheMoveFn>(at(1)), reinterpret_cast<CacheFn>(at(2)), reinterpret_cast<CacheNeedFn>(at(3))};
+    Py_RETURN_NONE;
+}
+
+bool index_ok(const at::Tensor *t, int64_t dims, const at::Device &d)
+{
+    return t && t->scalar_type() == at::kInt && t->dim() == dims && t->device() == d && (t->size(dims - 1) <= 1 || t->stride(dims - 1) == 1);
+}
+
+// cache, lens, pages, starts (or null) and the number of rows.
+bool cache_rows(const at::Tensor *const (&t)[4], int device, int64_t rows, squant_cache_rows &r)
+{
+    if (!t[0] || !t[0]->is_cuda() || t[0]->device().index() != device || t[0]->scalar_type() != at::kByte || t[0]->dim() != 4 || !t[0]->is_contiguous()) return false;
+    const at::Device d = t[0]->device();
+    if (!index_ok(t[1], 1, d) || !index_ok(t[2], 2, d) || (t[3] && !index_ok(t[3], 1, d))) return false;
+    const int64_t width = t[0]->size(3), granules = t[0]->size(2), heads = t[0]->size(1), batch = t[1]->size(0);
+    if (width != 18 * 64 && width != 18 * 128 && width != 18 * 256) return false;
+    if (granules > (1 << 20) || heads > (1 << 16) || batch >= kMostRows || t[2]->size(0) != batch || t[2]->size(1) > kMostRows || rows > kMostRows) return false;
+    if (t[3] ? t[3]->size(0) != batch + 1 : rows != batch) return false;
+    r.data = t[0]->data_ptr();
+    r.page_count = t[0]->size(0);
+    r.kv_heads = static_cast<int32_t>(heads);
+    r.head_dim = static_cast<int32_t>(width / 18);
+    r.page_size = static_cast<int32_t>(granules * 16);
+    r.batch = static_cast<int32_t>(batch);
+    r.width = static_cast<int32_t>(t[2]->size(1));
+    r.lens = static_cast<const int32_t *>(t[1]->data_ptr());
+    r.pages = static_cast<const int32_t *>(t[2]->data_ptr());
+    r.pages_stride = t[2]->stride(0);
+    r.starts = t[3] ? static_cast<const int32_t *>(t[3]->data_ptr()) : nullptr;
+    r.rows = rows;
+    return true;
+}
+
+// [rows, heads, head dim] with neighbouring channels
+bool heads_ok(const at::Tensor *t, int64_t heads, int64_t dim, at::ScalarType type, const at::Device &d)
+{
+    return t && t->dim() == 3 && t->size(1) == heads && t->size(2) == dim && t->stride(2) == 1 && t->scalar_type() == type && t->device() == d;
+}
+bool sixteen(at::ScalarType type) { return type == at::kBFloat16 || type == at::kHalf; }
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
+PyObject *cache_write(PyObject *, PyObject *args)
+{
+    unsigned long long stream;
+    PyObject *po[6];   // cache, lens, pages, starts, k, v
+    int device;
+    if (!PyArg_ParseTuple(args, "KiOOOOOO", &stream, &device, &po[0], &po[1], &po[2], &po[3], &po[4], &po[5])) return nullptr;
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *t[4], *k, *v;
+        for (int i = 0; i < 4; ++i)
+            if (!plain(po[i], t[i])) return none();
+        if (!plain(po[4], k) || !plain(po[5], v) || !k || !v || k->dim() != 3 || wants_graph({k, v})) return none();
+        squant_cache_move_args a{};
+        if (!cache_rows(t, device, k->size(0), a.rows) || !sixteen(k->scalar_type())) return none();
+        const at::Device d = t[0]->device();
+        if (!heads_ok(k, a.rows.kv_heads, a.rows.head_dim, k->scalar_type(), d) || !heads_ok(v, a.rows.kv_heads, a.rows.head_dim, k->scalar_type(), d) ||
+            v->size(0) != a.rows.rows) return none();
+        a.dtype = k->scalar_type() == at::kHalf ? SQUANT_FP16 : SQUANT_BF16;
+        a.k = k->data_ptr();
+        a.v = v->data_ptr();
+        a.k_stride = k->stride(0);
+        a.k_head_stride = k->stride(1);
+        a.v_stride = v->stride(0);
+        a.v_head_stride = v->stride(1);
+        const int rc = s_cache.write(&a, stream_of(stream));
+        if (rc != SQUANT_OK) return PyLong_FromLong(rc);
+        written(*t[0]);
+        Py_RETURN_TRUE;
+    });
+}
+
+PyObject *cache_read(PyObject *, PyObject *args)
+{
+    unsigned long long stream;
+    PyObject *po[4];   // cache, lens, pages, starts
+    int device, half;
+    long long rows;
+    if (!PyArg_ParseTuple(args, "KiOOOOLi", &stream, &device, &po[0], &po[1], &po[2], &po[3], &rows, &half)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *t[4];
+        for (int i = 0; i < 4; ++i)
+            if (!plain(po[i], t[i])) return none();
+        squant_cache_move_args a{};
+        if (rows < 0 || !cache_rows(t, device, rows, a.rows)) return none();
+        const auto type = half ? at::kHalf : at::kBFloat16;
+        at::Tensor k = new_tensor({rows, a.rows.kv_heads, a.rows.head_dim}, type, t[0]->device()), v = at::empty_like(k);
+        a.dtype = half ? SQUANT_FP16 : SQUANT_BF16;
+        a.k = k.data_ptr();
+        a.v = v.data_ptr();
+        a.k_stride = a.v_stride = k.stride(0);
+        a.k_head_stride = a.v_head_stride = k.stride(1);
+        const int rc = s_cache.read(&a, stream_of(stream));
+        if (rc != SQUANT_OK) return PyLong_FromLong(rc);
+        return Py_BuildValue("(NN)", THPVariable_Wrap(k), THPVariable_Wrap(v));
+    });
+}
+
+PyObject *cache_attention(PyObject *, PyObject *args)
+{
+    unsigned long long stream;
+    PyObject *po[6];   // cache, lens, pages, starts, q, out
+    int device, want_lse;
+    long long most;
+    double scale;
+    if (!PyArg_ParseTuple(args, "KiOOOOOOdLp", &stream, &device, &po[0], &po[1], &po[2], &po[3], &po[4], &po[5], &scale, &most, &want_lse)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *t[4], *q, *given;
+        for (int i = 0; i < 4; ++i)
+            if (!plain(po[i], t[i])) return none();
+        if (!plain(po[4], q) || !plain(po[5], given) || !q || q->dim() != 3 || wants_graph({q, given})) return none();
+        squant_cache_attention_args a{};
+        if (!cache_rows(t, device, q->size(0), a.rows) || !sixteen(q->scalar_type()) || most < 0) return none();
+        const at::Device d = t[0]->device();
+        const int64_t heads = q->size(1);
+        if (heads < 1 || heads > (1 << 20) || heads % a.rows.kv_heads || !heads_ok(q, heads, a.rows.head_dim, q->scalar_type(), d)) return none();
+        if (given && (!heads_ok(given, heads, a.rows.head_dim, q->scalar_type(), d) || given->size(0) != a.rows.rows)) return none();
+        at::Tensor out = given ? *given : new_tensor(q->sizes(), q->scalar_type(), d), lse, workspace;
+        if (want_lse) lse = new_tensor({a.rows.rows, heads}, at::kFloat, d);
+        a.dtype = q->scalar_type() == at::kHalf ? SQUANT_FP16 : SQUANT_BF16;
+        a.group = static_cast<int32_t>(heads / a.rows.kv_heads);
+        a.most = static_cast<int32_t>(std::min<long long>(most, kMostRows));
+        a.scale = static_cast<float>(scale);
+        a.q = q->data_ptr();
+        a.q_stride = q->stride(0);
+        a.q_head_stride = q->stride(1);
+        a.out = out.data_ptr();
+        a.out_stride = out.stride(0);
+        a.out_head_stride = out.stride(1);
+        a.lse = want_lse ? static_cast<float *>(lse.data_ptr()) : nullptr;
+        const int64_t bytes = s_cache.attention_need(&a);
+        if (bytes < 0) return none();
+        if (bytes > 0) {
+            workspace = new_tensor({bytes}, at::kByte, d);
+            a.workspace = workspace.data_ptr();
+            a.workspace_bytes = bytes;
+        }
+        const int rc = s_cache.attention(&a, stream_of(stream));
+        if (rc != SQUANT_OK) return PyLong_FromLong(rc);
+        PyObject *first = po[5];
+        if (given) {
+            written(out);
+            Py_INCREF(first);
+        } else {
+            first = THPVariable_Wrap(out);
+        }
+        return want_lse ? Py_BuildValue("(NN)", first, THPVariable_Wrap(lse)) : first;
+    });
+}
+
+PyMethodDef methods[] = {{"use_cache", use_cache, METH_VARARGS, "addresses of the library's functions for the key/value cache"},
+                         {"cache_write", cache_write, METH_VARARGS, "one call of squant_cache_write: True, an error code, or None"},
+                         {"cache_read", cache_read, METH_VARARGS, "one call of squant_cache_read: keys and values, an error code, or None"},
+                         {"cache_attention", cache_attention, METH_VARARGS, "one call of squant_cache_attention: the output (with the logarithms of the sums), an error code, or None"},
+                         {"use", use, METH_VARARGS, "addresses of the library's functions"},
                          {"linear", linear, METH_VARARGS, "one call of squant_linear: the output (with its checkpoint's codes and exponents), an error code, or None"},
                          {"linear_backward", linear_backward, METH_VARARGS, "one call of squant_linear_backward: four gradients, an error code, or None"},
                          {"checkpoint", checkpoint, METH_VARARGS, "one call of squant_checkpoint: codes, exponents and features, an error code, or None"},
@@ -413,7 +590,9 @@ PyMODINIT_FUNC PyInit__marshal(void)
                                      offsetof(L, codes), offsetof(L, scales), offsetof(L, kernel_err), offsetof(L, channel_err),
                                      offsetof(L, dequant), offsetof(L, dequant_bf16), offsetof(L, scales_in));
     if (PyModule_AddIntConstant(m, "linear_bytes", sizeof(squant_linear_args)) != 0 ||
-        PyModule_AddIntConstant(m, "linear_grad_bytes", sizeof(squant_linear_grad_args)) != 0) {
+        PyModule_AddIntConstant(m, "linear_grad_bytes", sizeof(squant_linear_grad_args)) != 0 ||
+        PyModule_AddIntConstant(m, "cache_move_bytes", sizeof(squant_cache_move_args)) != 0 ||
+        PyModule_AddIntConstant(m, "cache_attention_bytes", sizeof(squant_cache_attention_args)) != 0) {
         Py_XDECREF(layout);
         Py_DECREF(m);
         return nullptr;
