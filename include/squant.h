@@ -401,8 +401,8 @@ int squant_cache_read(const squant_cache_move_args *args, void *cuda_stream);
  * Softmax attention of rows over the cache: the row of position i attends to the positions 0 .. i of its sequence, which have been written before.  With q of query
  * head h, and k, v of kv head h / group, as squant_cache_read returns them in q's type:
  *   s_j = scale * q k_j,  out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = log sum_j exp(s_j)
- * A row that sees nothing gets zeros and lse -infinity.  Products are exact, sums and softmax fp32; in calls of more than 8 rows times heads of a sequence the
- * probabilities are rounded to q's type for the product with the values.  fp16 wants keys and values below 61,600 in magnitude.  Results repeat to the bit.
+ * A row that sees nothing gets zeros and lse -infinity.  Products are exact, sums and softmax fp32; in SQUANT_CACHE_PROMPT's calls the
+ * weights are rounded to q's type for the product with the values.  fp16 wants keys and values below 61,600 in magnitude.  Results repeat to the bit.
  */
 typedef struct squant_cache_attention_args {
     squant_cache_rows rows;
@@ -421,9 +421,9 @@ typedef struct squant_cache_attention_args {
 
 int64_t squant_cache_attention_workspace(const squant_cache_attention_args *args);
 /* Which kernel a call with these arguments takes: 0 (no rows), one of the values below, or the call's negative error.  No GPU is needed. */
-#define SQUANT_CACHE_STEP 1     /* tiles of 8 rows (tokens times heads of a group) */
-#define SQUANT_CACHE_STEP_16 2  /* tiles of 16 rows */
-#define SQUANT_CACHE_PROMPT 3   /* tiles of 128 rows, on the tensor cores' own memory */
+#define SQUANT_CACHE_STEP 1     /* tiles of 8 rows (tokens times heads of a group); up to 40 rows of a sequence and kv head, 64 or 48 with 64 or 256 channels */
+#define SQUANT_CACHE_STEP_16 2  /* tiles of 16 rows, beyond 8 rows with 64 and 256 channels */
+#define SQUANT_CACHE_PROMPT 3   /* tiles of 256 or 128 rows, on the tensor cores' own memory */
 int squant_cache_attention_plan(const squant_cache_attention_args *args);
 int squant_cache_attention(const squant_cache_attention_args *args, void *cuda_stream);
 

@@ -168,11 +168,19 @@ int64_t most_rows(const squant_cache_attention_args &a)
     if (!a.rows.starts) return 1;
     return a.most > 0 ? std::min<int64_t>(a.most, a.rows.rows) : a.rows.rows;
 }
+// cache_step_kernel reads the cache once for each of its tiles, cache_prompt_kernel once for 256 rows but at the cost of 128: the line is drawn at as many rows times heads (16
+// sequences of 3,000 to 8,000 positions, 8 kv heads; us for 32 and 64 rows, step and prompt: 64 channels 60 and 97, 114 and 114; 128 channels 120 and 186, 143 and 131; 256
+// channels 173 and 268, 229 and 220).  Tiles of 16 rows pay where two of 8 take more than one and a half times as long, which with 128 channels they do not: 16 rows' sums
+// and a unit's scores do not fit in 128 registers (32 rows in tiles of 8 and of 16: 64 channels 77 and 60, 128 channels 120 and 120, 256 channels 238 and 175).
+constexpr int most_step_rows(int dim) { return dim == 64 ? 64 : dim == 128 ? 40 : 48; }
+constexpr int step_tiles(int dim) { return dim == 128 ? 1 : 2; }   // of 8 rows, beyond 8
+
 int plan(const squant_cache_attention_args &a)
 {
     if (nothing(a.rows)) return 0;
     const int64_t rows = most_rows(a) * a.group;
-    return rows <= 8 ? SQUANT_CACHE_STEP : rows <= 16 ? SQUANT_CACHE_STEP_16 : SQUANT_CACHE_PROMPT;
+    if (rows > most_step_rows(a.rows.head_dim)) return SQUANT_CACHE_PROMPT;
+    return rows <= 8 || step_tiles(a.rows.head_dim) == 1 ? SQUANT_CACHE_STEP : SQUANT_CACHE_STEP_16;
 }
 
 // Thread blocks and the workspace's parts.
@@ -213,7 +221,7 @@ int64_t attention_bytes(const squant_cache_attention_args &a)
 {
     switch (plan(a)) {
         case SQUANT_CACHE_STEP: return step_plan<D, 1>(a).bytes;
-        case SQUANT_CACHE_STEP_16: return step_plan<D, 2>(a).bytes;
+        case SQUANT_CACHE_STEP_16: return step_plan<D, step_tiles(D)>(a).bytes;
         case SQUANT_CACHE_PROMPT: return prompt_plan<D>(a).bytes;
         default: return 0;
     }
@@ -275,7 +283,7 @@ int attention(const squant_cache_attention_args &a, cudaStream_t stream)
     const bool half = a.dtype == SQUANT_FP16;
     switch (plan(a)) {
         case SQUANT_CACHE_STEP: return half ? step<D, true, 1>(a, stream) : step<D, false, 1>(a, stream);
-        case SQUANT_CACHE_STEP_16: return half ? step<D, true, 2>(a, stream) : step<D, false, 2>(a, stream);
+        case SQUANT_CACHE_STEP_16: return half ? step<D, true, step_tiles(D)>(a, stream) : step<D, false, step_tiles(D)>(a, stream);
         default: return half ? prompt<D, true>(a, stream) : prompt<D, false>(a, stream);
     }
 }

@@ -33,7 +33,6 @@ struct AttendArgs {
 };
 
 constexpr int kStepWarps = 8, kStepThreads = 32 * kStepWarps;
-constexpr int kStepStages = 2;                 // of a warp: one being read, one in flight
 constexpr float kNoScore = -3.0e38f;           // the maximum of no scores
 constexpr float kGrowth = 8.0f;                // the running maximum is replaced when a score is 2^8 beyond it: sums stay far inside fp32 and bf16
 
@@ -42,14 +41,15 @@ template <int D, int kTiles>
 struct StepShape {
     static constexpr int kRows = 8 * kTiles;
     static constexpr int kBlocks = D * kTiles > 256 ? 1 : 2;             // on a multiprocessor
-    static constexpr int kGranules = D * kTiles == 256 && kTiles == 1 ? 1 : 2;   // of a unit
+    static constexpr int kGranules = D * kTiles == 256 ? 1 : 2;          // of a unit: as many as registers and shared memory allow
+    static constexpr int kStages = 2;                                    // of a warp: one being read, one in flight
     static constexpr int kPositions = kGranules * kGranule;              // of a unit
     static constexpr int kStage = kGranules * CacheFormat<D>::kBytes;
-    static constexpr int kWarpBytes = kStepStages * kStage;
+    static constexpr int kWarpBytes = kStages * kStage;
     static constexpr int kRing = kStepWarps * kWarpBytes;
     static constexpr bool kHeld = kTiles * D <= 128;                     // queries stay in registers
     static constexpr int kQueries = kHeld ? 0 : kRows * D * 2;           // of a warp
-    static constexpr int kSmem = kRing + kStepWarps * kQueries + 8 * kStepWarps * kStepStages;
+    static constexpr int kSmem = kRing + kStepWarps * kQueries + 8 * kStepWarps * kStages;
     static constexpr int kPitch = D + 4;                                 // floats of a row's sums in shared memory
     static constexpr int kPart = kRows * (D + 2);                        // floats of a tile's part in the workspace: sums, then maximum and sum of exponentials of each row
     static constexpr int kParts = 2 + kStepWarps;                        // of a block: its own two, and each warp's end of a tile that began before
@@ -296,7 +296,7 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     uint8_t *const ring = smem + warp * S::kWarpBytes;
     uint4 *const held_q = reinterpret_cast<uint4 *>(smem + S::kRing + warp * S::kQueries);
-    const uint32_t bars = smem_addr(smem) + S::kRing + kStepWarps * S::kQueries + 8 * warp * kStepStages;
+    const uint32_t bars = smem_addr(smem) + S::kRing + kStepWarps * S::kQueries + 8 * warp * S::kStages;
     SQ_LINEAR_CHECK(smem_addr(smem) + S::kSmem <= smem_end(smem) && (smem_addr(smem) & 15) == 0, 2010);
     if (threadIdx.x == 0) {
         gave_up_word = 0;
@@ -304,7 +304,7 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
     }
     if (lane == 0) {
         left_over[warp].item0 = -1;
-        for (int s = 0; s < kStepStages; ++s) bar_init(bars + 8 * s, 1);
+        for (int s = 0; s < S::kStages; ++s) bar_init(bars + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     Walk walk;
@@ -341,7 +341,7 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
             }
             ahead_unit += listed;
         }
-        const unsigned stage = fetched % kStepStages;
+        const unsigned stage = fetched % S::kStages;
         int from[S::kGranules];
         uint32_t have = 0;
 #pragma unroll
@@ -366,7 +366,7 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
         ++taken;
     };
 #pragma unroll
-    for (int s = 0; s < kStepStages; ++s) fetch();
+    for (int s = 0; s < S::kStages; ++s) fetch();
 
     const CodePairs<kHalf> pairs;
     while (walk.next<S>(p.r, p.group)) {
@@ -409,8 +409,8 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
         }
 
         for (int unit = dead ? walk.last : walk.first; unit < walk.last; ++unit) {
-            const unsigned stage = consumed % kStepStages;
-            if (!bar_wait_warp(bars + 8 * stage, consumed / kStepStages & 1, gave_up)) {
+            const unsigned stage = consumed % S::kStages;
+            if (!bar_wait_warp(bars + 8 * stage, consumed / S::kStages & 1, gave_up)) {
                 dead = true;
                 break;
             }
@@ -712,7 +712,7 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
         if (lane == 0 && (ends_here || warp == 0)) (ends_here ? left_over[warp] : first_end) = Left{walk.item0, walk.item0 + walk.units, walk.row0, rows_all, walk.head, walk.tile};
     }
     // no copy of a block that has given up may land after its end, or in a part of a tile
-    for (; consumed < fetched; ++consumed) bar_drain(bars + 8 * (consumed % kStepStages), consumed / kStepStages & 1);
+    for (; consumed < fetched; ++consumed) bar_drain(bars + 8 * (consumed % S::kStages), consumed / S::kStages & 1);
     __syncthreads();
 
     // parts of tiles that the block has, each begun by a warp's end, with those of the warps that follow it

@@ -81,9 +81,11 @@ def test_null_arguments_and_calls_without_rows():
 def test_plans():
     """Which kernel: by rows times heads of a group, at most, of a sequence, as far as the host knows."""
     lib = cache._lib()
-    plan = lambda **kw: lib.squant_cache_attention_plan(ctypes.byref(attention(out_stride=1 << 20, **kw)))
-    assert plan(starts=None, rows=3) == 1 and plan(starts=None, rows=3, group=8) == 1 and plan(starts=None, rows=3, group=9) == 2 and plan(starts=None, rows=3, group=17) == 3
-    assert plan() == 3 and plan(most=2) == 1 and plan(most=4) == 2 and plan(most=5) == 3 and plan(most=1, group=16) == 2 and plan(rows=2) == 1
+    plan = lambda **kw: lib.squant_cache_attention_plan(ctypes.byref(attention(**{"out_stride": 1 << 20, **kw})))
+    assert plan(starts=None, rows=3) == 1 and plan(starts=None, rows=3, group=40) == 1 and plan(starts=None, rows=3, group=41) == 3
+    assert plan() == 1 and plan(rows=11) == 3 and plan(rows=11, most=10) == 1 and plan(rows=11, most=11) == 3
+    for dim, most in ((64, 64), (256, 48)):
+        assert [plan(head_dim=dim, starts=None, rows=3, group=g, out_head_stride=dim) for g in (8, 9, most, most + 1)] == [1, 2, 2, 3]
     need = lambda **kw: lib.squant_cache_attention_workspace(ctypes.byref(attention(out_stride=1 << 20, out_head_stride=256, **kw)))
     for dim in (64, 128, 256):
         for kw in ({"most": 1}, {"most": 4}, {}):

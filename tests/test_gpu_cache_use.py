@@ -98,7 +98,7 @@ def test_streams_and_two_calls_at_once():
 
 @pytest.mark.parametrize("most", [1, 0])
 def test_a_captured_step_is_replayed_with_other_lengths(most):
-    heads, group, dim, page, batch = 2, 4, 128, 32, 5
+    heads, group, dim, page, batch = 2, 4 if most else 12, 128, 32, 5   # with 60 rows of a sequence possible, the kernel for prompts
     room = Batch([400] * batch, [1] * batch, page)
     cache = filled(room, heads, dim, 3)
     lens, q = torch.ones(batch, dtype=torch.int32, device="cuda"), inputs(batch, heads * group, dim, BF16, 4)
