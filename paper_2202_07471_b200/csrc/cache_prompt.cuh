@@ -231,6 +231,12 @@ __device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8])
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
 __device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -460,20 +466,18 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                     beyond = 0.0f;
                     const Two by(scale, scale);
                     Two sum(total, 0.0f);
-                    uint32_t s[16];
-                    tmem_ld16_begin(scores, s);
-                    tmem_ld16_end(s);
-#pragma unroll
-                    for (int j = 0; j < S::kPositions; j += 16) {
-                        if constexpr (kMasked) hide16(s, position + j, limit, have >> (j / kGranule));
+#pragma unroll 1
+                    for (int j = 0; j < S::kPositions; j += 32) {
+                        uint32_t s[32];
+                        tmem_ld32(scores + j, s);
+                        if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
                         const Two less(-most, -most);
-                        float x[16], tops[4];
+                        float x[32], tops[4];
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
+                        for (int e = 0; e < 32; e += 2) {
                             fma(Two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), by, less).get(x[e], x[e + 1]);
                             tops[e / 2 % 4] = e < 8 ? fmaxf(x[e], x[e + 1]) : max3(tops[e / 2 % 4], x[e], x[e + 1]);
                         }
-                        if (j + 16 < S::kPositions) tmem_ld16_begin(scores + j + 16, s);   // while the exponentials are taken
                         float top = max3(max3(tops[0], tops[1], tops[2]), tops[3], beyond);
                         if (__any_sync(0xffffffffu, top > kRoom)) {
                             // too far beyond the maximum for 16 bits: what there is of the row is scaled at once, this tile's weights so far among it
@@ -481,7 +485,6 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                             float a, b;
                             sum.get(a, b);
                             total = a + b;
-                            tmem_ld16_end(s);
                             scale_sums(factor);
                             sum = Two(total, 0.0f);
                             most += top;
@@ -495,19 +498,18 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                                 tmem_st8(weights + k, w);
                             }
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) x[e] -= top;
+                            for (int e = 0; e < 32; ++e) x[e] -= top;
                             top = 0.0f;
                         }
                         beyond = top;
-                        uint32_t w[8];
+                        uint32_t w[16];
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
+                        for (int e = 0; e < 32; e += 2) {
                             const float a = exp2_fast(x[e]), b = exp2_fast(x[e + 1]);
                             sum = add(sum, Two(a, b));
                             w[e / 2] = to_16x2<kHalf>(a, b);
                         }
-                        tmem_st8(weights + j / 2, w);   // the scores there have been read
-                        if (j + 16 < S::kPositions) tmem_ld16_end(s);
+                        tmem_st16(weights + j / 2, w);   // the scores there have been read
                     }
                     float a, b;
                     sum.get(a, b);
