@@ -33,9 +33,9 @@ inline int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 inline bool on_vectors(const void *p, int64_t stride, int64_t head) { return !misaligned(p, 16) && stride % 8 == 0 && head % 8 == 0; }
 
 template <typename Args>
-int launch(void (*kernel)(Args), int64_t grid, int threads, int smem, cudaStream_t stream, const Args &args)
+int launch(void (*kernel)(Args), dim3 grid, int threads, int smem, cudaStream_t stream, const Args &args)
 {
-    kernel<<<static_cast<unsigned>(grid), threads, smem, stream>>>(args);
+    kernel<<<grid, threads, smem, stream>>>(args);
     SQ_CUDA(cudaGetLastError());
     sq_host::count_launch();
     return SQUANT_OK;
@@ -50,7 +50,7 @@ int launch_large(void (*kernel)(Args), std::atomic<bool> (&ready)[kMaxDevices], 
         SQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         if (device < kMaxDevices) ready[device].store(true, std::memory_order_relaxed);
     }
-    return launch(kernel, grid, threads, smem, stream, args);
+    return launch(kernel, dim3(static_cast<unsigned>(grid)), threads, smem, stream, args);
 }
 
 int check(const squant_cache_rows &r, uint32_t dtype)
@@ -124,12 +124,11 @@ int move(const squant_cache_move_args &a, bool write, cudaStream_t stream)
     m.v_stride = a.v_stride;
     m.v_head = a.v_head_stride;
     m.vector = on_vectors(a.k, a.k_stride, a.k_head_stride) && on_vectors(a.v, a.v_stride, a.v_head_stride);
-    m.blocks = (a.rows.kv_heads + sq::kMoveHeads<D> - 1) / sq::kMoveHeads<D>;
     const bool half = a.dtype == SQUANT_FP16;
     const auto kernel = write ? (half ? sq::cache_write_kernel<D, true> : sq::cache_write_kernel<D, false>)
                               : (half ? sq::cache_read_kernel<D, true> : sq::cache_read_kernel<D, false>);
-    const int64_t grid = (a.rows.rows * m.blocks + sq::kMoveThreads / 32 - 1) / (sq::kMoveThreads / 32);
-    if (grid > (1ll << 31) - 1) return SQUANT_ERR_SHAPE;
+    const dim3 grid(static_cast<unsigned>((a.rows.rows + sq::kMoveThreads / 32 - 1) / (sq::kMoveThreads / 32)),
+                    static_cast<unsigned>((a.rows.kv_heads + sq::kMoveHeads<D> - 1) / sq::kMoveHeads<D>));   // at most 32,768 high
     return launch(kernel, grid, sq::kMoveThreads, 0, stream, m);
 }
 

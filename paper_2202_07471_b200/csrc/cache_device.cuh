@@ -200,6 +200,12 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a)
     return r;
 }
 
+__device__ __forceinline__ Two add(Two a, Two b)
+{
+    Two r(0ull);
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float r;

@@ -250,12 +250,6 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-__device__ __forceinline__ Two add(Two a, Two b)
-{
-    Two r(0ull);
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
 // Scores of 32 positions from `position` on that the row does not see, or whose granules are not there.
 __device__ __forceinline__ void hide(uint32_t (&s)[32], int position, int limit, uint32_t have)
 {

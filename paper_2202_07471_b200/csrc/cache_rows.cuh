@@ -13,7 +13,6 @@ struct MoveArgs {
     uint16_t *k, *v;               // read: written
     int64_t k_stride, k_head, v_stride, v_head;   // elements from row to row and from head to head
     int32_t vector;                // all rows of k and v start on 16 bytes
-    int32_t blocks;                // of heads, kMoveHeads each
 };
 
 constexpr int kMoveThreads = 256;
@@ -27,12 +26,12 @@ template <int D>
 struct Piece {
     int head, word;
     bool value;
-    __device__ __forceinline__ explicit Piece(int i)
+    __device__ __forceinline__ explicit Piece(unsigned i)
     {
-        const int at = i * 32 + (threadIdx.x & 31);
-        word = at % (D / 8);
+        const unsigned at = i * 32 + (threadIdx.x & 31);
+        word = static_cast<int>(at % (D / 8));
         value = at / (D / 8) % 2;
-        head = at / (D / 4);
+        head = static_cast<int>(at / (D / 4));
     }
 };
 
@@ -57,17 +56,58 @@ __device__ __forceinline__ Place place_of(const MoveArgs &p, int64_t row, int &b
     return {p.cache + (page * p.r.kv_heads * granules + in / kGranule) * CacheFormat<D>::kBytes, in % kGranule};
 }
 
+// The larger of two magnitudes in each half, NaN if either is one.
+template <bool kHalf>
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    if constexpr (kHalf) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// The scale of a group whose largest magnitude is `top` (at most 11 significant bits): top / 7, correctly rounded by the remainder of a product with the
+// reciprocal (an fma yields it exactly; to 24 bits, so that a tie between two scales shows), then to four significant bits, ties to even.
+__device__ __forceinline__ float group_scale(float top)
+{
+    if (top < kScaleLeast) return 0.0f;
+    if (!(top < kScaleMost)) return __uint_as_float(0x7f800000u);
+    const float q = __fmul_rn(top, 1.0f / 7.0f);
+    const uint32_t bits = __float_as_uint(fmaf(fmaf(-q, 7.0f, top), 1.0f / 7.0f, q));
+    return __uint_as_float((bits + 0x7ffffu + (bits >> 20 & 1)) & ~0xfffffu);
+}
+// Codes of 8 values, two values an instruction.  x / s comes from a product with the reciprocal that is corrected by its remainder: whatever the reciprocal's last bits, a
+// quotient of k + 1/2, the only one that matters, comes out as such.  Adding 1.5 * 2^23 and taking it off rounds to an integer, ties to even; the integers, as digits of 16, make the
+// halves of a word, with 8 added to each (0x8888) so that none is negative, which the last step takes off.
+template <bool kHalf>
+__device__ __forceinline__ uint32_t group_codes(const uint32_t (&w)[4], float scale)
+{
+    if (!(scale > 0.0f && scale < __uint_as_float(0x7f800000u))) return 0;
+    float inverse;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(scale));
+    const Two by(inverse, inverse), minus(-scale, -scale), up(12582912.0f, 12582912.0f), down(-12582912.0f, -12582912.0f), digit(16.0f, 16.0f);
+    Two sum(0.0f, 0.0f);
+#pragma unroll
+    for (int p = 3; p >= 0; --p) {
+        const Two x(to_float<kHalf>(static_cast<uint16_t>(w[p])), to_float<kHalf>(static_cast<uint16_t>(w[p] >> 16)));
+        const Two q = mul(x, by);
+        const Two rounded = add(add(fma(fma(q, minus, x), by, q), up), down);
+        sum = p == 3 ? rounded : fma(sum, digit, rounded);
+    }
+    float low, high;
+    add(sum, Two(8388608.0f + 34952.0f, 8388608.0f + 34952.0f)).get(low, high);   // 2^23 and 0x8888: the low 16 bits
+    return __byte_perm(__float_as_uint(low), __float_as_uint(high), 0x5410) ^ 0x88888888u;
+}
+
 // A warp quantizes kMoveHeads heads of a row: the loads of keys and values, which no position is needed for, are in flight while it looks up where
-// the row belongs.  Four lanes hold the channels that share a scale.  x / s is rounded from a product with the reciprocal that is corrected by its remainder
-// (an fma yields it exactly), so that a quotient of exactly one half, the only one that matters, is one.
+// the row belongs.  Four lanes hold the channels that share a scale.  Instructions bound it next to the bytes (29,656 rows of 8 heads 68 us at 31 instructions a value, 83 % of the issue
+// slots; two values at a time and magnitudes compared in 16 bits: see the measured table).
 template <int D, bool kHalf>
 __global__ void __launch_bounds__(kMoveThreads)
 cache_write_kernel(const __grid_constant__ MoveArgs p)
 {
     using F = CacheFormat<D>;
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + (threadIdx.x >> 5);
-    const int64_t row = unit / p.blocks;
-    const int head0 = static_cast<int>(unit % p.blocks) * kMoveHeads<D>;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + (threadIdx.x >> 5);
+    const int head0 = static_cast<int>(blockIdx.y) * kMoveHeads<D>;
     if (row >= p.r.rows) return;
     uint4 x[kMoveLoads];
     const auto load = [&](auto on_vectors) {
@@ -93,31 +133,11 @@ cache_write_kernel(const __grid_constant__ MoveArgs p)
         const Piece<D> at(i);
         const int head = head0 + at.head;
         const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        float f[8], top = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            f[e] = to_float<kHalf>(static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1))));
-            top = max_nan(top, fabsf(f[e]));
-        }
-        top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // to four significant bits, ties to even; whether a quotient is a tie shows in fp32
-        const uint32_t bits = __float_as_uint(__fdiv_rn(top, 7.0f));
-        float scale = __uint_as_float((bits + 0x7ffffu + (bits >> 20 & 1)) & ~0xfffffu);
-        uint32_t word = 0;
-        if (top < kScaleLeast) {
-            scale = 0.0f;
-        } else if (!(top < kScaleMost)) {
-            scale = __uint_as_float(0x7f800000u);
-        } else {
-            const float inverse = __frcp_rn(scale);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float q = __fmul_rn(f[e], inverse);
-                const float quotient = fmaf(fmaf(-q, scale, f[e]), inverse, q);
-                word |= (__float_as_uint(__fadd_rn(quotient, 12582912.0f)) & 15u) << (4 * (e >> 1) + 16 * (e & 1));   // 1.5 * 2^23: rounded to an integer, ties to even
-            }
-        }
+        uint32_t both = larger2<kHalf>(larger2<kHalf>(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), larger2<kHalf>(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+        both = larger2<kHalf>(both, __shfl_xor_sync(0xffffffffu, both, 1));
+        both = larger2<kHalf>(both, __shfl_xor_sync(0xffffffffu, both, 2));
+        const float scale = group_scale(max_nan(to_float<kHalf>(static_cast<uint16_t>(both)), to_float<kHalf>(static_cast<uint16_t>(both >> 16))));
+        const uint32_t word = group_codes<kHalf>(w, scale);
         if (head < p.r.kv_heads) {
             uint8_t *granule = to.granule + head * head_bytes;
             SQ_LINEAR_CHECK(granule >= p.cache && granule + F::kBytes <= p.cache + p.r.page_count * p.r.kv_heads * head_bytes, 2000);
@@ -135,9 +155,8 @@ __global__ void __launch_bounds__(kMoveThreads)
 cache_read_kernel(const __grid_constant__ MoveArgs p)
 {
     using F = CacheFormat<D>;
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + (threadIdx.x >> 5);
-    const int64_t row = unit / p.blocks;
-    const int head0 = static_cast<int>(unit % p.blocks) * kMoveHeads<D>;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + (threadIdx.x >> 5);
+    const int head0 = static_cast<int>(blockIdx.y) * kMoveHeads<D>;
     if (row >= p.r.rows) return;
     int b;
     int64_t position;
