@@ -279,9 +279,12 @@ struct Left {
     int row0, rows_all, head, tile;
 };
 
-// Keys and values are the first operands of the matrix instructions, 16 positions (16 channels) high, and rows of queries (of probabilities) are the second ones'
-// columns, so that none of the instructions' work goes to rows that do not exist, and sums take few registers.  What the rounding of a probability to 16
-// bits leaves over goes through a second instruction: products with the values are as good as fp32's.
+// Keys and values are the first operands of the matrix instructions, 16 positions (16 channels) high, and rows of queries (of weights) are the second ones'
+// columns, so that none of the instructions' work goes to rows that do not exist, and sums take few registers (queries first and codes second: 120 us for 131,072 positions of 8
+// heads, 54 % more instructions and twice the sums' registers).  What the rounding of a weight to 16 bits leaves over goes through a second instruction: products with the values
+// are as good as fp32's.  62 us now, 38 % of the copy bandwidth: 810 instructions a unit and warp, 52 % of the issue slots (the copies alone take 21 us, 7.3 TB/s), 3 us until the
+// first copies are under way and 12 us for the last blocks to join the parts of 37.
+// Units without a hidden position have code of their own, without masks (931 to 810 instructions).
 template <int D, bool kHalf, int kTiles>
 __global__ void __launch_bounds__(kStepThreads, (StepShape<D, kTiles>::kBlocks))
 cache_step_kernel(const __grid_constant__ AttendArgs p)
@@ -516,7 +519,7 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
                             for (int e = 0; e < 4; ++e) o[r][i][e] *= factor[e & 1];
                     }
                 }
-                // probabilities, turned round: the lane has positions 2 c and the next (and 8 on) for row g
+                // weights, turned round: the lane has positions 2 c and the next (and 8 on) for row g
                 uint32_t hi[kTiles][S::kGranules][2], lo[kTiles][S::kGranules][2];
 #pragma unroll
                 for (int r = 0; r < kTiles; ++r)
