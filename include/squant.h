@@ -459,7 +459,7 @@ int squant_device_status(void);
  */
 int squant_debug_set_status(int value);
 /*
- * The same for the linear operators, whose waits have a limit and a status word of their own.  squant_debug_linear_wait_expires waits on one
+ * The same for the linear operators and the key/value cache, whose waits have a limit and a status word of their own.  squant_debug_linear_wait_expires waits on one
  * warp as above, with a limit of max_tries (1..4096).  squant_debug_linear_wait_limit sets the limit of all their waits on the current device in the checked
  * build (0: every wait gives up at once, -1: the regular limit), so that calls give up: they then leave their results unwritten or incomplete, squant_device_status
  * says so and later calls are not affected.  It returns 1 in the checked build and 0, without an effect, in the regular one.

@@ -152,6 +152,8 @@ int check(const squant_cache_attention_args *args)
     if (a.group < 1 || a.group > (1 << 16) || a.most < 0) return SQUANT_ERR_SHAPE;
     const int64_t heads = static_cast<int64_t>(r.kv_heads) * a.group;
     if (heads > (1 << 20) || r.rows * a.group >= (1ll << 31)) return SQUANT_ERR_SHAPE;
+    // units of a tile are counted in 32 bits, with the group's share in them
+    if (std::min<int64_t>(static_cast<int64_t>(r.width) * r.page_size, 1ll << 30) * a.group >= (1ll << 37)) return SQUANT_ERR_SHAPE;
     if (bad_strides(a.q_stride, a.q_head_stride, heads, r.rows, r.head_dim, false) ||
         bad_strides(a.out_stride, a.out_head_stride, heads, r.rows, r.head_dim, true)) return SQUANT_ERR_SHAPE;
     if (!std::isfinite(a.scale)) return SQUANT_ERR_MODE;

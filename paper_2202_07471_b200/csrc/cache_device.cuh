@@ -87,8 +87,6 @@ __device__ __forceinline__ int sequence_of(const CacheRows &r, int64_t row)
 
 // ---------------------------------------------------------------- codes to floats
 
-__device__ __forceinline__ float bf16_float(uint32_t low) { return __uint_as_float(low << 16); }
-
 // The halves of a register, both or one of them twice.
 __device__ __forceinline__ uint32_t half_twice(uint32_t two, bool high)
 {
@@ -173,7 +171,7 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t two)
     else return two;
 }
 
-// ---------------------------------------------------------------- copies and matrix instructions
+// ---------------------------------------------------------------- copies, arithmetic
 
 // A contiguous copy into shared memory; 16-byte addresses and sizes.
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
@@ -181,25 +179,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ uint4 lds128(uint32_t a)
-{
-    uint4 r;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
-    return r;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a)
-{
-    uint2 r;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a) : "memory");
-    return r;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a)
-{
-    uint32_t r;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(a) : "memory");
-    return r;
-}
-
 __device__ __forceinline__ Two add(Two a, Two b)
 {
     Two r(0ull);

@@ -219,19 +219,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]
           "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
           "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
-// A load that other work may be put behind, and the wait for it, behind which the registers hold it.
-__device__ __forceinline__ void tmem_ld16_begin(uint32_t addr, uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
-}
-__device__ __forceinline__ void tmem_ld16_end(uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
-                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
-}
 __device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -296,14 +283,6 @@ __device__ __forceinline__ bool bar_test_warp(uint32_t bar, uint32_t parity)
     return __all_sync(0xffffffffu, ok != 0);
 }
 
-__device__ __forceinline__ void hide16(uint32_t (&s)[kGranule], int position, int limit, uint32_t have)   // of one granule
-{
-    if (!(have & 1)) limit = -1;
-#pragma unroll
-    for (int e = 0; e < kGranule; ++e)
-        if (position + e > limit) s[e] = 0xff800000u;
-}
-
 template <int D, bool kHalf>
 __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1)
 cache_prompt_kernel(const __grid_constant__ AttendArgs p)
@@ -365,7 +344,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    constexpr uint32_t tmem = 0;   // all columns have been asked for
+    constexpr uint32_t tmem = 0;   // where the columns begin, since all have been asked for
     SQ_LINEAR_CHECK(tmem_base == tmem, 2023);
 
     if (warp < S::kSoftmax) {
@@ -658,87 +637,87 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                     if (!ok) break;
 #pragma unroll 1
                     for (int two = 0; two < S::kRawGranules; two += 2) {
-                    const uint8_t *const raw = smem + (smem_c - base) + stage * S::kRaw + two * F::kBytes;
-                    const int first_row = (part * S::kRawGranules + two) * kGranule;
-                    {
-                        const uint32_t to = smem_k + (tiles_done & 1) * S::kOperand;
-                        // (position, word % 4): neighbouring lanes have the words % 4 of positions t and t + 4, whose 16-byte pieces are in different banks
-                        const int c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8, row = first_row + t;   // t: 0 .. 31
-                        const uint8_t *const granule = raw + t / kGranule * F::kBytes;
-                        uint32_t scales[kGroupsAll / 2], w[F::kSlabs][4];
+                        const uint8_t *const raw = smem + (smem_c - base) + stage * S::kRaw + two * F::kBytes;
+                        const int first_row = (part * S::kRawGranules + two) * kGranule;
+                        {
+                            const uint32_t to = smem_k + (tiles_done & 1) * S::kOperand;
+                            // (position, word % 4): neighbouring lanes have the words % 4 of positions t and t + 4, whose 16-byte pieces are in different banks
+                            const int c = unit & 3, t = (unit >> 2 & 1) * 4 | (unit >> 3 & 3) | (unit >> 5) * 8, row = first_row + t;   // t: 0 .. 31
+                            const uint8_t *const granule = raw + t / kGranule * F::kBytes;
+                            uint32_t scales[kGroupsAll / 2], w[F::kSlabs][4];
 #pragma unroll
-                        for (int j = 0; j < kGroupsAll / 2; ++j) scales[j] = *reinterpret_cast<const uint32_t *>(granule + F::kKeyScales + t % kGranule * (2 * kGroupsAll) + 4 * j);
+                            for (int j = 0; j < kGroupsAll / 2; ++j) scales[j] = *reinterpret_cast<const uint32_t *>(granule + F::kKeyScales + t % kGranule * (2 * kGroupsAll) + 4 * j);
 #pragma unroll
-                        for (int a = 0; a < F::kSlabs; ++a) {
-                            const uint8_t *const from = granule + a * (64 * F::kWords) + t % kGranule * (4 * F::kWords) + c * F::kWords;
-                            if constexpr (F::kGroups == 2) {
-                                const uint2 v = *reinterpret_cast<const uint2 *>(from);
-                                w[a][0] = v.x; w[a][1] = v.y;
-                            } else {
-                                const uint4 v = *reinterpret_cast<const uint4 *>(from);
-                                w[a][0] = v.x; w[a][1] = v.y; w[a][2] = v.z; w[a][3] = v.w;
-                            }
-                        }
-#pragma unroll
-                        for (int g = 0; g < kGroupsAll; ++g) {
-                            const int word = 4 * g + c;
-                            uint32_t o[4];
-                            pairs(w[g / F::kGroups][g % F::kGroups], pairs.scales(scale_twice<kHalf>(scales[g / 2], g & 1)), o);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + word / 8 * S::kPanel + row * 128 + ((word ^ row) & 7) * 16),
-                                         "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                        }
-                    }
-                    {
-                        const uint32_t to = smem_v + (tiles_done & 1) * S::kOperand;
-                        // (pair of positions, word % 8)
-                        constexpr int kLaneWords = F::kWords / 8;
-                        const int g = unit & 7, pair = unit >> 3, row = first_row + 2 * pair;   // pair: 0 .. 15
-                        const uint8_t *const granule = raw + pair / 8 * F::kBytes;
-                        const bool there = *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) >> (first_row / kGranule + pair / 8) & 1;
-                        // positions behind the last one that any row sees, and granules that are not there, may hold anything
-                        const uint32_t seen = (there && position + row <= seen_most ? 0xffffu : 0u) | (there && position + row + 1 <= seen_most ? 0xffff0000u : 0u);
-                        uint32_t scales[F::kSlabs][kLaneWords], w[F::kSlabs][4];
-                        bool odd = false;
-#pragma unroll
-                        for (int a = 0; a < F::kSlabs; ++a) {
-                            const uint8_t *const from = granule + F::kValues + a * (64 * F::kWords) + (pair % 8 * 8 + g) * (8 * kLaneWords);
-                            if constexpr (kLaneWords == 1) {
-                                const uint2 v = *reinterpret_cast<const uint2 *>(from);
-                                w[a][0] = v.x; w[a][1] = v.y;
-                            } else {
-                                const uint4 v = *reinterpret_cast<const uint4 *>(from);
-                                w[a][0] = v.x; w[a][1] = v.y; w[a][2] = v.z; w[a][3] = v.w;
+                            for (int a = 0; a < F::kSlabs; ++a) {
+                                const uint8_t *const from = granule + a * (64 * F::kWords) + t % kGranule * (4 * F::kWords) + c * F::kWords;
+                                if constexpr (F::kGroups == 2) {
+                                    const uint2 v = *reinterpret_cast<const uint2 *>(from);
+                                    w[a][0] = v.x; w[a][1] = v.y;
+                                } else {
+                                    const uint4 v = *reinterpret_cast<const uint4 *>(from);
+                                    w[a][0] = v.x; w[a][1] = v.y; w[a][2] = v.z; w[a][3] = v.w;
+                                }
                             }
 #pragma unroll
-                            for (int m = 0; m < kLaneWords; ++m) {
-                                scales[a][m] = seen & *reinterpret_cast<const uint32_t *>(granule + F::kValueScales + a * (32 * F::kGroups) + pair % 8 * (4 * F::kGroups) + (g >> 2) * (2 * F::kGroups) + 4 * m);
-                                odd |= (scales[a][m] & 0x7f80u) == 0x7f80u || (scales[a][m] & 0x7f800000u) == 0x7f800000u;
+                            for (int g = 0; g < kGroupsAll; ++g) {
+                                const int word = 4 * g + c;
+                                uint32_t o[4];
+                                pairs(w[g / F::kGroups][g % F::kGroups], pairs.scales(scale_twice<kHalf>(scales[g / 2], g & 1)), o);
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + word / 8 * S::kPanel + row * 128 + ((word ^ row) & 7) * 16),
+                                             "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                             }
                         }
-                        if (odd) {   // no number: for rows that see the position only, see the end of the tile
+                        {
+                            const uint32_t to = smem_v + (tiles_done & 1) * S::kOperand;
+                            // (pair of positions, word % 8)
+                            constexpr int kLaneWords = F::kWords / 8;
+                            const int g = unit & 7, pair = unit >> 3, row = first_row + 2 * pair;   // pair: 0 .. 15
+                            const uint8_t *const granule = raw + pair / 8 * F::kBytes;
+                            const bool there = *const_cast<volatile uint32_t *>(&granules_there[tiles_done % kTilesAhead]) >> (first_row / kGranule + pair / 8) & 1;
+                            // positions behind the last one that any row sees, and granules that are not there, may hold anything
+                            const uint32_t seen = (there && position + row <= seen_most ? 0xffffu : 0u) | (there && position + row + 1 <= seen_most ? 0xffff0000u : 0u);
+                            uint32_t scales[F::kSlabs][kLaneWords], w[F::kSlabs][4];
+                            bool odd = false;
+#pragma unroll
+                            for (int a = 0; a < F::kSlabs; ++a) {
+                                const uint8_t *const from = granule + F::kValues + a * (64 * F::kWords) + (pair % 8 * 8 + g) * (8 * kLaneWords);
+                                if constexpr (kLaneWords == 1) {
+                                    const uint2 v = *reinterpret_cast<const uint2 *>(from);
+                                    w[a][0] = v.x; w[a][1] = v.y;
+                                } else {
+                                    const uint4 v = *reinterpret_cast<const uint4 *>(from);
+                                    w[a][0] = v.x; w[a][1] = v.y; w[a][2] = v.z; w[a][3] = v.w;
+                                }
+#pragma unroll
+                                for (int m = 0; m < kLaneWords; ++m) {
+                                    scales[a][m] = seen & *reinterpret_cast<const uint32_t *>(granule + F::kValueScales + a * (32 * F::kGroups) + pair % 8 * (4 * F::kGroups) + (g >> 2) * (2 * F::kGroups) + 4 * m);
+                                    odd |= (scales[a][m] & 0x7f80u) == 0x7f80u || (scales[a][m] & 0x7f800000u) == 0x7f800000u;
+                                }
+                            }
+                            if (odd) {   // no number: for rows that see the position only, see the end of the tile
+#pragma unroll
+                                for (int a = 0; a < F::kSlabs; ++a)
+#pragma unroll
+                                    for (int m = 0; m < kLaneWords; ++m)
+#pragma unroll
+                                        for (int h = 0; h < 2; ++h)
+                                            if ((scales[a][m] >> (16 * h) & 0x7f80u) == 0x7f80u) {
+                                                scales[a][m] &= h ? 0x0000ffffu : 0xffff0000u;
+                                                atomicMin(&no_number[pieces & 3][a * F::kGroups + 2 * m + (g >> 2)], position + row + h);
+                                            }
+                            }
 #pragma unroll
                             for (int a = 0; a < F::kSlabs; ++a)
 #pragma unroll
                                 for (int m = 0; m < kLaneWords; ++m)
 #pragma unroll
-                                    for (int h = 0; h < 2; ++h)
-                                        if ((scales[a][m] >> (16 * h) & 0x7f80u) == 0x7f80u) {
-                                            scales[a][m] &= h ? 0x0000ffffu : 0xffff0000u;
-                                            atomicMin(&no_number[pieces & 3][a * F::kGroups + 2 * m + (g >> 2)], position + row + h);
-                                        }
+                                    for (int h = 0; h < 2; ++h) {
+                                        uint32_t o[4];
+                                        pairs(w[a][h * kLaneWords + m], pairs.scales(scale_twice<kHalf>(scales[a][m], h)), o);
+                                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (a * kLaneWords + m) * S::kPanel + (row + h) * 128 + ((g ^ (row + h)) & 7) * 16),
+                                                     "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                                    }
                         }
-#pragma unroll
-                        for (int a = 0; a < F::kSlabs; ++a)
-#pragma unroll
-                            for (int m = 0; m < kLaneWords; ++m)
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    uint32_t o[4];
-                                    pairs(w[a][h * kLaneWords + m], pairs.scales(scale_twice<kHalf>(scales[a][m], h)), o);
-                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (a * kLaneWords + m) * S::kPanel + (row + h) * 128 + ((g ^ (row + h)) & 7) * 16),
-                                                 "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                                }
-                    }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();

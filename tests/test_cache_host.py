@@ -56,7 +56,7 @@ def test_read_refuses_rows_that_lie_in_one_another(kw):
 
 
 @pytest.mark.parametrize("kw,code", COMMON + [
-    ({"group": 0}, -2), ({"group": (1 << 16) + 1}, -2), ({"group": 1 << 16, "kv_heads": 64}, -2), ({"rows": 1 << 30, "group": 2}, -2), ({"most": -1}, -2), ({"q_stride": -1}, -2),
+    ({"group": 0}, -2), ({"group": (1 << 16) + 1}, -2), ({"group": 1 << 16, "kv_heads": 64}, -2), ({"rows": 1 << 30, "group": 2}, -2), ({"group": 1 << 8, "width": 1 << 20, "pages_stride": 1 << 20, "page_size": 1 << 10, "out_stride": 1 << 20}, -2), ({"most": -1}, -2), ({"q_stride": -1}, -2),
     ({"out_stride": 1023}, -2), ({"out_head_stride": 100}, -2), ({"scale": float("nan")}, -4), ({"scale": float("inf")}, -4), ({"q": None}, -1), ({"out": None}, -1), ({"q": ODD_PTR}, -5),
     ({"out": ODD_PTR}, -5), ({"lse": OK_PTR + 2}, -5), ({}, -12), ({"workspace": OK_PTR, "workspace_bytes": 16}, -12), ({"workspace": OK_PTR + 8, "workspace_bytes": 1 << 40}, -12)])
 def test_attention_refuses(kw, code):
