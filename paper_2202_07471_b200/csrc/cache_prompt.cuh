@@ -236,6 +236,7 @@ __device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8])
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
+// Before another thread, a product or a load of the thread's own may see what it has stored: stores are asynchronous, and loads of the same columns do not wait for them.
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -461,6 +462,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                         float top = max3(max3(tops[0], tops[1], tops[2]), tops[3], beyond);
                         if (__any_sync(0xffffffffu, top > kRoom)) {
                             // too far beyond the maximum for 16 bits: what there is of the row is scaled at once, this tile's weights so far among it
+                            tmem_st_wait();   // weights and sums that this tile has stored are about to be loaded
                             const float factor = exp2_fast(-top);
                             float a, b;
                             sum.get(a, b);

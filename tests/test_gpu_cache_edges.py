@@ -1,0 +1,57 @@
+"""The key/value cache at its edges: scores that grow inside what is taken at once."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2202_07471_b200 as sq
+from cache_cases import Batch, gen, pack
+from paper_2202_07471_b200 import cache as cache_module
+from test_gpu_cache import BF16, FP16, check_attention
+
+pytestmark = pytest.mark.gpu
+PROMPT = 3
+
+
+def plan(q, cache, batch, most):
+    """Which kernel a call takes."""
+    a = cache_module.CacheAttentionArgs(cache_module._cache_rows(cache, *batch.args, q.shape[0]), 0, q.shape[1] // cache.shape[1], most, 1.0, q.data_ptr(),
+                                        q.stride(0), q.stride(1), q.data_ptr(), q.shape[1] * q.shape[2], q.shape[2])
+    return cache_module._lib().squant_cache_attention_plan(ctypes.byref(a))
+
+
+def rising(batch, heads, dim, levels):
+    """A cache whose position p has the score levels[p], in powers of two, for a query of ones: keys of one magnitude, which the codes keep to 2^-5."""
+    v = torch.randn((batch.page_count, heads, batch.page_size // 16, 16, dim), generator=gen(2), device="cuda")
+    k = torch.zeros_like(v)
+    for b, n in enumerate(batch.lens_list):
+        for p in range(n):
+            k[batch.pages_list[b, p // batch.page_size], :, p % batch.page_size // 16, p % 16] = levels[p] / dim
+    return pack(k.to(BF16), v.to(BF16))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("news", [[300, 170], [20, 9]])
+@pytest.mark.parametrize("jumps", [(13, 2), (2, 13), (9, 15), (15, 15, 15), (0, 14, 0, 3, 15, 13), (13, 13, 2, 2)])
+def test_scores_that_grow_several_times_in_one_tile(dim, dtype, news, jumps):
+    """A row whose maximum is replaced inside a score tile has what is there scaled while it is being made: its weights, and its sums, which may just have been scaled for the
+    tile before.  Every 32 positions, which are taken together, the scores rise by another jump, less or more than a weight's type has room for (2^14 in fp16,
+    2^64 in bf16); what came before the jump keeps a part in the result, and would be far too large if it were scaled too little."""
+    heads, group = 2, 8
+    room = 1.0 if dtype == FP16 else 64.0 / 14
+    batch = Batch([300, 170], news, 16, seed=5)
+    level, levels = 0.0, []
+    for i in range(-(-300 // 32)):
+        level += jumps[i % len(jumps)] * room if i >= 2 else 0
+        levels += [level] * 32
+    cache = rising(batch, heads, dim, levels)
+    q = (1 + 0.02 * torch.randn((batch.rows, heads * group, dim), generator=gen(7), device="cuda")).to(dtype)
+    assert plan(q, cache, batch, max(news)) == PROMPT
+    scale = 0.6931471805599453
+    out, lse = sq.squant_cache_attention(q, cache, *batch.args, most=max(news), lse=True, scale=scale)
+    # a weight is rounded once, and again whenever it is scaled: at most three times, once for each later 32 of 128 positions
+    check_attention(out, lse, q, batch, cache, scale, rounded_p=4)
+    again, lse_again = sq.squant_cache_attention(q, cache, *batch.args, most=max(news), lse=True, scale=scale)
+    assert torch.equal(out, again) and torch.equal(lse, lse_again)
+    assert sq.squant_device_status() is None
