@@ -631,7 +631,9 @@ cache_step_kernel(const __grid_constant__ AttendArgs p)
             if (have == (1u << S::kGranules) - 1 && position + S::kPositions - 1 <= seen_least) attend(std::false_type{});
             else if (have) attend(std::true_type{});
             ++consumed;
-            __syncwarp();   // all lanes have read the stage
+            // all lanes have read the stage, and a copy into it comes behind what they have read: nothing else keeps one, which is not theirs, from overtaking their loads
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
             fetch();
         }
 

@@ -1,13 +1,13 @@
-"""The key/value cache at its edges: scores that grow inside what is taken at once."""
+"""The key/value cache at its edges: scores that grow inside what is taken at once, calls that repeat."""
 import ctypes
 
 import pytest
 import torch
 
 import paper_2202_07471_b200 as sq
-from cache_cases import Batch, gen, pack
+from cache_cases import Batch, filled, gen, pack
 from paper_2202_07471_b200 import cache as cache_module
-from test_gpu_cache import BF16, FP16, check_attention
+from test_gpu_cache import BF16, FP16, check_attention, inputs
 
 pytestmark = pytest.mark.gpu
 PROMPT = 3
@@ -54,4 +54,18 @@ def test_scores_that_grow_several_times_in_one_tile(dim, dtype, news, jumps):
     check_attention(out, lse, q, batch, cache, scale, rounded_p=4)
     again, lse_again = sq.squant_cache_attention(q, cache, *batch.args, most=max(news), lse=True, scale=scale)
     assert torch.equal(out, again) and torch.equal(lse, lse_again)
+    assert sq.squant_device_status() is None
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group,news", [(4, 1), (12, 1), (5, 3)])
+def test_steps_repeat_to_the_bit(dim, group, news):
+    """A place in shared memory is given back to the copies behind the loads from it: many short pages, so that copies are small and quick, and every call the same."""
+    batch = Batch([4000, 33, 700, 2049] * 8, [news] * 32, 16, seed=6)
+    cache = filled(batch, 2, dim, 3)
+    for dtype in (BF16, FP16):
+        q = inputs(batch.rows, 2 * group, dim, dtype, 4)
+        want = sq.squant_cache_attention(q, cache, *batch.args, most=news)
+        for _ in range(60):
+            assert torch.equal(sq.squant_cache_attention(q, cache, *batch.args, most=news), want)
     assert sq.squant_device_status() is None
