@@ -1,4 +1,4 @@
-"""The key/value cache at its edges: scores that grow inside what is taken at once, calls that repeat."""
+"""The key/value cache at its edges: scores that grow inside what is taken at once, calls that repeat, captured calls that have given up."""
 import ctypes
 
 import pytest
@@ -6,7 +6,7 @@ import torch
 
 import paper_2202_07471_b200 as sq
 from cache_cases import Batch, filled, gen, pack
-from paper_2202_07471_b200 import cache as cache_module
+from paper_2202_07471_b200 import build as lib_build, cache as cache_module
 from test_gpu_cache import BF16, FP16, check_attention, inputs
 
 pytestmark = pytest.mark.gpu
@@ -69,3 +69,47 @@ def test_steps_repeat_to_the_bit(dim, group, news):
         for _ in range(60):
             assert torch.equal(sq.squant_cache_attention(q, cache, *batch.args, most=news), want)
     assert sq.squant_device_status() is None
+
+
+@pytest.fixture
+def checked_build():
+    sq.use_library(lib_build.LIB_DEBUG)
+    try:
+        yield
+    finally:
+        sq.squant_debug_linear_wait_limit(-1)
+        sq.use_library(None)
+
+
+def status():
+    try:
+        sq.squant_device_status()
+        return 0
+    except sq.SquantError as e:
+        return e.code
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("news,most", [(1, 1), (150, 0)])
+def test_a_captured_call_is_right_again_after_it_has_given_up(checked_build, dim, news, most):
+    """Waits of one to six tries run out in some blocks and not in others: those that share a tile have counted, and a replay, whose number is the same, starts from no count."""
+    batch = Batch([900, 300, 520], [news] * 3, 32)
+    cache = filled(batch, 2, dim, 3)
+    q = inputs(batch.rows, 8, dim, BF16, 4)
+    out = torch.empty(q.shape, dtype=BF16, device="cuda")
+    want = sq.squant_cache_attention(q, cache, *batch.args, most=most)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sq.squant_cache_attention(q, cache, *batch.args, most=most, out=out)
+    assert status() == 0
+    gave_up = 0
+    for tries in (1, 2, 3, 4, 6) * 6 + (0,):
+        assert sq.squant_debug_linear_wait_limit(tries)
+        graph.replay()
+        gave_up += status() == -10
+        assert sq.squant_debug_linear_wait_limit(-1)
+        for _ in range(2):
+            out.zero_()
+            graph.replay()
+            assert torch.equal(out, want) and status() == 0, tries
+    assert gave_up > 0
