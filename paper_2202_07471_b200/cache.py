@@ -207,7 +207,10 @@ def squant_cache_attention(q: torch.Tensor, cache: torch.Tensor, lens: torch.Ten
     heads is a multiple of the cache's kv heads; query head h reads kv head h // (heads / kv heads).  scale: of the products, 1 / sqrt(head dim) by default.
     most: the number of rows that no sequence has more of, where the caller knows it (it helps to choose the kernel and changes nothing else).  With `lse` returns
     (out, logarithms of the sums of exponentials, fp32 [rows, heads]).  out: the tensor to write, like q; in a new one, rows behind the last sequence hold
-    anything.  A row that sees nothing is zeros, its lse -infinity."""
+    anything.  A row that sees nothing is zeros, its lse -infinity.
+
+    fp16 wants a cache of what fp16 holds: groups of 32 channels up to 65,504.  From 2^-18 on their values are those that squant_cache_read returns, below they are 2^-22 off at
+    most."""
     native = None if stream is not None or q.dim() != 3 else _native()
     if native is not None:
         device = _device()

@@ -132,15 +132,21 @@ struct CodePairs {
         }
         return r;
     }
+    // The halves of pair p as described, before arithmetic; upper: w >> 8.
+    __device__ __forceinline__ uint32_t bits(uint32_t w, uint32_t upper, int p) const
+    {
+        const uint32_t from = p < 2 ? w : upper;
+        uint32_t u;
+        if (p & 1) asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(from), "r"(mask_high), "r"(flip_high));   // (from & mask) ^ flip
+        else asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(from), "r"(mask), "r"(flip));
+        return u;
+    }
     __device__ __forceinline__ void operator()(uint32_t w, const PairScales<kHalf> &s, uint32_t (&out)[4]) const
     {
         const uint32_t upper = w >> 8;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const uint32_t from = p < 2 ? w : upper;
-            uint32_t u;
-            if (p & 1) asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(from), "r"(mask_high), "r"(flip_high));   // (from & mask) ^ flip
-            else asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(u) : "r"(from), "r"(mask), "r"(flip));
+            uint32_t u = bits(w, upper, p);
             if constexpr (kHalf) {
                 u = p & 1 ? fma2<true>(u, 0x2c002c00u, 0xd480d480u) : fma2<true>(u, 0x3c003c00u, 0xe408e408u);   // u / 16 - 72, u - 1032
                 asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(out[p]) : "r"(u), "r"(s.scale));
@@ -149,6 +155,27 @@ struct CodePairs {
             } else {
                 out[p] = fma2<false>(u, s.scale, s.other);
             }
+        }
+    }
+    // A word's values, rounded to nearest once whatever the scale is.  In fp16 a scale below 2^-21 loses bits and one from 2^16 on is infinite, though its products with
+    // codes may be numbers; so the codes are taken 2^-12 (2) times as large, exactly, and the scale 2^12 (1/2) times, where it is a number of four bits: below 2^-33
+    // it is not, but then all values are rounded to 0, and from 2^17 on any number makes infinities of codes other than 0.  The operator above takes the scale as fp16 holds it.
+    __device__ __forceinline__ void rounded_once(uint32_t w, uint32_t scale, uint32_t (&out)[4]) const
+    {
+        if constexpr (kHalf) {
+            const float s = __uint_as_float(scale << 16);
+            const bool small = s < 0.00390625f;
+            const float moved = small ? s * 4096.0f : s * 0.5f, held = s < __uint_as_float(0x7f800000u) ? fminf(moved, 65504.0f) : s;
+            const uint32_t k = to_16x2<true>(held, held), upper = w >> 8;
+            const uint32_t even = small ? 0x0c000c00u : 0x40004000u, even_less = small ? 0xb408b408u : 0xe808e808u;   // 2^-12 and 2, -1032 times that
+            const uint32_t odd = small ? 0x01000100u : 0x30003000u, odd_less = small ? 0xa480a480u : 0xd880d880u;     // a sixteenth of that, -72 times it
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const uint32_t u = bits(w, upper, p), code = p & 1 ? fma2<true>(u, odd, odd_less) : fma2<true>(u, even, even_less);
+                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(out[p]) : "r"(code), "r"(k));
+            }
+        } else {
+            (*this)(w, scales(half_twice(scale, false)), out);
         }
     }
 };

@@ -1,13 +1,13 @@
-"""The key/value cache at its edges: scores that grow inside what is taken at once, calls that repeat, captured calls that have given up."""
+"""The key/value cache at its edges: scores that grow inside what is taken at once, calls that repeat, captured calls that have given up, fp16 at both ends."""
 import ctypes
 
 import pytest
 import torch
 
 import paper_2202_07471_b200 as sq
-from cache_cases import Batch, filled, gen, pack
+from cache_cases import Batch, attention, filled, gen, pack, stored
 from paper_2202_07471_b200 import build as lib_build, cache as cache_module
-from test_gpu_cache import BF16, FP16, check_attention, inputs
+from test_gpu_cache import BF16, FP16, check_attention, inputs, same
 
 pytestmark = pytest.mark.gpu
 PROMPT = 3
@@ -113,3 +113,58 @@ def test_a_captured_call_is_right_again_after_it_has_given_up(checked_build, dim
             graph.replay()
             assert torch.equal(out, want) and status() == 0, tries
     assert gave_up > 0
+
+
+def magnitudes(dim):
+    """Rows of every power of two from 2^-40 on, with the mantissas 1, 9/8, 5/4 and 15/8 of a group's largest value and codes of every size; groups of zeros, of values that are too small and without a number."""
+    rows = []
+    for exponent in range(-40, 121):
+        tops = torch.tensor([1.0, 1.125, 1.25, 1.875], dtype=torch.float64).repeat(dim // 128 + 1)[:dim // 32] * 2.0 ** exponent
+        parts = torch.linspace(-1, 1, 32, dtype=torch.float64)
+        rows.append((tops[:, None] * parts).flatten())
+    special = torch.ones(dim, dtype=torch.float64)
+    special[:32], special[32] = 0.0, float("nan")
+    rows.append(special)
+    rows.append(torch.full((dim,), 2.0 ** -101, dtype=torch.float64))
+    return torch.stack(rows)[:, None, :].to(BF16).cuda()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_fp16_values_are_rounded_once_at_every_magnitude(dim):
+    """code * scale, rounded to nearest: also where fp16 holds the values and not the scale, and zeros where the scale is beyond fp16."""
+    k = magnitudes(dim)
+    v = k.flip(0).contiguous()
+    n = k.shape[0]
+    batch = Batch([n], [n], 32)
+    cache = sq.alloc_cache(batch.page_count, 1, dim, page_size=32)
+    sq.squant_cache_write(cache, k, v, *batch.args)
+    rk, rv = sq.squant_cache_read(cache, *batch.args, n, dtype=FP16)
+    for got, x in ((rk, k), (rv, v)):
+        want = stored(x).float().half()   # a value has seven bits: exact in fp32
+        assert want.isinf().any() and (want == 2.0 ** -24).any() and (want == 0).any() and same(got, want)
+    slices = torch.empty((n, 1, dim + 3), dtype=FP16, device="cuda"), torch.empty((n, 1, dim + 3), dtype=FP16, device="cuda")
+    sq.squant_cache_read(cache, *batch.args, n, k=slices[0][..., 3:], v=slices[1][..., 3:])
+    assert same(slices[0][..., 3:], rk) and same(slices[1][..., 3:], rv)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("news", [1, 2, 40])
+def test_fp16_attention_to_small_and_large_values(dim, news):
+    """Of the sizes that fp16 holds: exact values from 2^-18 up to 65,504 (a group's largest); below, the scale is rounded to a multiple of 2^-24, by half of one, and so is
+    its product with the code: up to 7 * 2^-25 + 2^-25 = 2^-22 off, and so is a value's average."""
+    heads, group, n = 1, 8, 48
+    batch = Batch([n], [news], 16)
+    for top, off in ((65504.0, 0.0), (2.0 ** -18, 0.0), (2.0 ** -21, 2.0 ** -22), (5 * 2.0 ** -24, 2.0 ** -22), (2.0 ** -24, 2.0 ** -22)):
+        k = torch.zeros((n, heads, dim), dtype=FP16, device="cuda")
+        v = (torch.rand((n, heads, dim), generator=gen(1), device="cuda") * 2 - 1) * top
+        v[..., ::32] = top
+        cache = sq.alloc_cache(batch.page_count, heads, dim, page_size=16)
+        every = Batch([n], [n], 16)
+        sq.squant_cache_write(cache, k, v.to(FP16), every.lens, batch.pages, every.starts)
+        q = inputs(news, heads * group, dim, FP16, 3)
+        out = sq.squant_cache_attention(q, cache, *batch.args, most=news)
+        want, _ = attention(q, batch, cache)
+        size = stored(v.to(FP16)).abs().amax()
+        # what the kernels round besides (see check_attention), a weight at most 2^-11 and 2^-25
+        assert ((out.double() - want).abs() <= off + 2.0 ** -11 * want.abs() + 2.0 ** -25 + (2.0 ** -11 + 2.0 ** -16 + n * 2.0 ** -25) * size).all(), top
+        assert top < 1e-5 or not out.isnan().any() and (out != 0).any()
