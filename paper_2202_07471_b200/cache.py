@@ -105,6 +105,8 @@ def _index(t: torch.Tensor, shape: Tuple[int, ...], what: str, device: torch.dev
 def _cache_rows(cache: torch.Tensor, lens: torch.Tensor, pages: torch.Tensor, starts: Optional[torch.Tensor], rows: int) -> CacheRows:
     if cache.dtype != torch.uint8 or cache.dim() != 4 or cache.shape[3] not in (18 * 64, 18 * 128, 18 * 256) or not cache.is_contiguous():
         raise ValueError("a cache is a contiguous uint8 tensor [pages, kv heads, page size / 16, 18 * head dim], as of alloc_cache")
+    if cache.shape[1] < 1 or cache.shape[2] < 1:
+        raise ValueError("a cache has at least one kv head and one granule of 16 positions a page")
     device = cache.device
     if lens.dim() != 1 or pages.dim() != 2:
         raise ValueError("lens must be an int32 tensor [batch], pages an int32 tensor [batch, width]")

@@ -423,7 +423,7 @@ bool cache_rows(const at::Tensor *const (&t)[4], int device, int64_t rows, squan
     if (!index_ok(t[1], 1, d) || !index_ok(t[2], 2, d) || (t[3] && !index_ok(t[3], 1, d))) return false;
     const int64_t width = t[0]->size(3), granules = t[0]->size(2), heads = t[0]->size(1), batch = t[1]->size(0);
     if (width != 18 * 64 && width != 18 * 128 && width != 18 * 256) return false;
-    if (granules > (1 << 20) || heads > (1 << 16) || batch >= kMostRows || t[2]->size(0) != batch || t[2]->size(1) > kMostRows || rows > kMostRows) return false;
+    if (granules < 1 || heads < 1 || granules > (1 << 20) || heads > (1 << 16) || batch >= kMostRows || t[2]->size(0) != batch || t[2]->size(1) > kMostRows || rows > kMostRows) return false;
     if (t[3] ? t[3]->size(0) != batch + 1 : rows != batch) return false;
     r.data = t[0]->data_ptr();
     r.page_count = t[0]->size(0);

@@ -168,3 +168,15 @@ def test_fp16_attention_to_small_and_large_values(dim, news):
         # what the kernels round besides (see check_attention), a weight at most 2^-11 and 2^-25
         assert ((out.double() - want).abs() <= off + 2.0 ** -11 * want.abs() + 2.0 ** -25 + (2.0 ** -11 + 2.0 ** -16 + n * 2.0 ** -25) * size).all(), top
         assert top < 1e-5 or not out.isnan().any() and (out != 0).any()
+
+
+def test_a_cache_without_heads_or_positions_is_refused():
+    """By every call, with the binding's error: the native calls divide by the number of heads."""
+    batch = Batch([4, 1], [1, 1], 16)
+    for shape in ((4, 0, 4, 1152), (4, 2, 0, 1152)):
+        cache = torch.zeros(shape, dtype=torch.uint8, device="cuda")
+        x = inputs(2, 2, 64, BF16, 1)
+        for call in (lambda: sq.squant_cache_write(cache, x[:, :shape[1]], x[:, :shape[1]], *batch.args), lambda: sq.squant_cache_read(cache, *batch.args, 2),
+                     lambda: sq.squant_cache_attention(x, cache, *batch.args)):
+            with pytest.raises(ValueError):
+                call()
