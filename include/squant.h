@@ -374,7 +374,7 @@ typedef struct squant_cache_rows {
     void *data;              /* the cache, 16-byte aligned */
     int64_t page_count;
     int32_t kv_heads, head_dim, page_size;
-    int32_t batch;           /* sequences, >= 0 */
+    int32_t batch;           /* sequences, 0 .. 2^30 */
     int32_t width;           /* columns of pages */
     const int32_t *lens;     /* [batch] */
     const int32_t *pages;    /* [batch][width], rows pages_stride elements apart */

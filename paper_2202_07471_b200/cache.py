@@ -115,7 +115,9 @@ def _cache_rows(cache: torch.Tensor, lens: torch.Tensor, pages: torch.Tensor, st
     _index(pages, (batch, pages.shape[1]), "pages", device)
     if starts is not None:
         _index(starts, (batch + 1,), "starts", device)
-    elif rows != batch:
+    if max(cache.shape[1], cache.shape[2] * GRANULE, batch, pages.shape[1]) >= 1 << 31:
+        raise ValueError("kv heads, a page's positions, sequences and columns of pages are counted in 32 bits")
+    if starts is None and rows != batch:
         raise ValueError(f"without starts there is one row a sequence: {rows} rows, {batch} sequences")
     return CacheRows(_ptr(cache), cache.shape[0], cache.shape[1], cache.shape[3] // 18, cache.shape[2] * GRANULE, batch, pages.shape[1], _ptr(lens),
                      _ptr(pages), pages.stride(0), _ptr(starts), rows)

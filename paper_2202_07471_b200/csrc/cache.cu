@@ -57,8 +57,9 @@ int check(const squant_cache_rows &r, uint32_t dtype)
 {
     if (r.head_dim != 64 && r.head_dim != 128 && r.head_dim != 256) return SQUANT_ERR_SHAPE;
     if (r.page_size < sq::kGranule || r.page_size % sq::kGranule || r.page_size > (1 << 24) || r.kv_heads < 1 || r.kv_heads > (1 << 16)) return SQUANT_ERR_SHAPE;
-    if (r.page_count < 0 || r.page_count > (1ll << 31) || r.batch < 0 || r.width < 0 || r.rows < 0 || r.rows > kMaxRows) return SQUANT_ERR_SHAPE;
-    if (r.page_count * r.kv_heads * (r.page_size / sq::kGranule) >= (1ll << 31)) return SQUANT_ERR_SHAPE;   // granules are counted in 32 bits: 2 TB of them
+    if (r.page_count < 0 || r.page_count > (1ll << 31) || r.batch < 0 || r.batch > kMaxRows || r.width < 0 || r.rows < 0 || r.rows > kMaxRows) return SQUANT_ERR_SHAPE;
+    // granules are counted in 32 bits: 2 TB of them (a page's are fewer than 2^37, all of them may be more than 64 bits hold)
+    if (r.page_count > ((1ll << 31) - 1) / (static_cast<int64_t>(r.kv_heads) * (r.page_size / sq::kGranule))) return SQUANT_ERR_SHAPE;
     if (r.batch > 1 && (r.pages_stride < r.width || r.pages_stride > kMaxStride)) return SQUANT_ERR_SHAPE;
     if (!r.starts && r.rows != r.batch) return SQUANT_ERR_SHAPE;
     if (dtype > SQUANT_FP16) return SQUANT_ERR_MODE;
@@ -75,7 +76,7 @@ bool bad_strides(int64_t stride, int64_t head, int64_t heads, int64_t rows, int6
 {
     if (stride < 0 || head < 0 || stride > kMaxStride || head > kMaxStride) return true;
     if (!written) return false;
-    if (heads > 1 && rows > 1) return !(head >= dim && stride >= (heads - 1) * head + dim) && !(stride >= dim && head >= (rows - 1) * stride + dim);
+    if (heads > 1 && rows > 1) return !(head >= dim && stride >= (heads - 1) * head + dim) && !(stride >= dim && head >= dim && rows - 1 <= (head - dim) / stride);   // no product of rows: it may overflow
     return (heads > 1 && head < dim) || (rows > 1 && stride < dim);
 }
 
