@@ -209,10 +209,12 @@ def squant_cache_attention(q: torch.Tensor, cache: torch.Tensor, lens: torch.Ten
     """Softmax attention of queries [rows, heads, head dim] over the cache, which holds their own positions already: a row sees its sequence's positions up to its own.
 
     heads is a multiple of the cache's kv heads; query head h reads kv head h // (heads / kv heads).  scale: of the products, 1 / sqrt(head dim) by default.
-    most: the number of rows that no sequence has more of, where the caller knows it (it helps to choose the kernel and changes nothing else).  With `lse` returns
+    most: the number of rows that no sequence has more of, where the caller knows it: it chooses the kernel, and with it the results' last places; without it, a step of
+    many sequences takes the slower one, for prompts.  With `lse` returns
     (out, logarithms of the sums of exponentials, fp32 [rows, heads]).  out: the tensor to write, like q; in a new one, rows behind the last sequence hold
     anything.  A row that sees nothing is zeros, its lse -infinity.
 
+    Weights are rounded to q's type for their product with the values in sequences of more than 128 rows times query heads of a kv head, and keep twice its bits elsewhere.
     fp16 wants a cache of what fp16 holds: groups of 32 channels up to 65,504.  From 2^-18 on their values are those that squant_cache_read returns, below they are 2^-22 off at
     most."""
     native = None if stream is not None or q.dim() != 3 else _native()

@@ -175,6 +175,7 @@ int64_t most_rows(const squant_cache_attention_args &a)
 // channels 173 and 268, 229 and 220).  Tiles of 16 rows pay where two of 8 take more than one and a half times as long, which with 128 channels they do not: 16 rows' sums
 // and a unit's scores do not fit in 128 registers (32 rows in tiles of 8 and of 16: 64 channels 77 and 60, 128 channels 120 and 120, 256 channels 238 and 175).
 constexpr int most_step_rows(int dim) { return dim == 64 ? 64 : dim == 128 ? 40 : 48; }
+static_assert(std::max({most_step_rows(64), most_step_rows(128), most_step_rows(256)}) <= sq::kWholeRows, "as exact in either kernel");
 constexpr int step_tiles(int dim) { return dim == 128 ? 1 : 2; }   // of 8 rows, beyond 8
 
 int plan(const squant_cache_attention_args &a)

@@ -6,6 +6,11 @@
 //   S = Q K^T   [128 x 128] in tensor memory, a row a lane: softmax warps own a row a thread
 //   P = exp2(scale S - m) over S's place, 16 bits;  O += P V, P from tensor memory
 //
+// Weights are rounded to 16 bits for the product.  In sequences of up to kWholeRows rows what that leaves of them goes through a second one, as in cache_step.cuh: such
+// sequences come to either kernel, by what the caller says of the others, and are as exact in both (drafted tokens 0.00166 off, which is all the output's own rounding, and 80
+// us; with one product 0.0020 and 75 us).  In longer ones 16 bits are all there is: prompts are 0.0021 off instead of 0.0016 in bf16 and 0.0003 instead of 0.0002 in fp16, in
+// 433 us instead of 513 and 351 instead of 432.
+//
 // m is the maximum of the row's first tile.  It is replaced when a later tile has reached 2^8 beyond it, before the next one: then O is scaled, between two products.  Within a
 // tile weights may be as large as their type holds with room to spare, so that a row's scores are read once.  Per 128 positions the tensor cores work 2,048 clocks for both slots, and
 // the exponentials take as long: one slot's products run while the other one's exponentials do.  A tile of up to 128 rows has its positions shared by the slots, every other tile
@@ -28,6 +33,7 @@ namespace sq {
 
 constexpr int kSlotRows = 128;           // the tensor memory's lanes
 constexpr int kPromptConverters = 4;     // warps
+constexpr int kWholeRows = 128;          // more than any sequence has that the host leaves to cache_step_kernel
 constexpr int kTilesAhead = 8;           // score tiles that are being copied, converted or weighed at the same time, at most
 
 template <int D>
@@ -261,6 +267,15 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// Two weights in 16 bits, and what that leaves of them, in 16 bits too.
+template <bool kHalf>
+__device__ __forceinline__ void split(float a, float b, uint32_t &w, uint32_t &rest)
+{
+    w = to_16x2<kHalf>(a, b);
+    float c, d;
+    fma(Two(to_float<kHalf>(static_cast<uint16_t>(w)), to_float<kHalf>(static_cast<uint16_t>(w >> 16))), Two(-1.0f, -1.0f), Two(a, b)).get(c, d);
+    rest = to_16x2<kHalf>(c, d);
+}
 // Scores of 32 positions from `position` on that the row does not see, or whose granules are not there.
 __device__ __forceinline__ void hide(uint32_t (&s)[32], int position, int limit, uint32_t have)
 {
@@ -423,106 +438,138 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                 if (lane == 0) bar_arrive(queries_full);
             }
             const int mine_of = events.of_slot(slot);
-            for (int i = 0; i < mine_of; ++i, ++weighed) {
-                ok = bar_wait_warp(scores_full(slot), weighed & 1, gave_up);
-                if (!ok) break;
-                tc_fence_after();
-                const int step = alone ? i : 2 * i + slot, position = walk.first * S::kRows + step * S::kPositions;
-                const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[(tiles_before + step) % kTilesAhead]);
-                const bool masked = position + S::kPositions - 1 > seen_least || have != (1u << S::kGranules) - 1;
-                const auto scale_sums = [&](float factor) {   // the products with the values of the tiles before have been made
-                    total *= factor;
-                    if (i == 0) return;
+            // Weights of 32 positions take 16 columns, with what rounding leaves of them the place of their scores, which is 32.  Each way has a loop of its own, here and where the products are
+            // made, and this one comes first: a choice in the loop costs part of a prompt 7 % (376 us instead of 351), the other order 1 % (356).
+            const auto weigh_tiles = [&](auto in_two_c) {
+                constexpr bool kTwo = decltype(in_two_c)::value;
+                for (int i = 0; i < mine_of; ++i, ++weighed) {
+                    ok = bar_wait_warp(scores_full(slot), weighed & 1, gave_up);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int step = alone ? i : 2 * i + slot, position = walk.first * S::kRows + step * S::kPositions;
+                    const uint32_t have = *const_cast<volatile uint32_t *>(&granules_there[(tiles_before + step) % kTilesAhead]);
+                    const bool masked = position + S::kPositions - 1 > seen_least || have != (1u << S::kGranules) - 1;
+                    const auto scale_sums = [&](float factor) {   // the products with the values of the tiles before have been made
+                        total *= factor;
+                        if (i == 0) return;
 #pragma unroll 1
-                    for (int j = 0; j < D; j += 32) {
-                        uint32_t o[32];
-                        tmem_ld32(sums + j, o);
+                        for (int j = 0; j < D; j += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(sums + j, o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                        tmem_st32(sums + j, o);
-                    }
-                };
-                const auto weigh = [&](auto some_hidden) {
-                    constexpr bool kMasked = decltype(some_hidden)::value;
-                    if (__any_sync(0xffffffffu, most == kNoScore)) {   // the first scores that a row sees: their maximum
-                        float top = -INFINITY;
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                            tmem_st32(sums + j, o);
+                        }
+                    };
+                    const auto weigh = [&](auto some_hidden) {
+                        constexpr bool kMasked = decltype(some_hidden)::value;
+                        if (__any_sync(0xffffffffu, most == kNoScore)) {   // the first scores that a row sees: their maximum
+                            float top = -INFINITY;
+#pragma unroll 1
+                            for (int j = 0; j < S::kPositions; j += 32) {
+                                uint32_t s[32];
+                                tmem_ld32(scores + j, s);
+                                if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
+#pragma unroll
+                                for (int e = 0; e < 32; e += 2) top = max3(top, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+                            }
+                            const float next = fmaxf(fmaxf(top * scale, most), kNoScore);
+                            scale_sums(exp2_fast(most - next));
+                            most = next;
+                        } else if (__any_sync(0xffffffffu, beyond > kGrowth)) {
+                            scale_sums(exp2_fast(-beyond));
+                            most += beyond;
+                        }
+                        beyond = 0.0f;
+                        const Two by(scale, scale);
+                        Two sum(total, 0.0f);
 #pragma unroll 1
                         for (int j = 0; j < S::kPositions; j += 32) {
                             uint32_t s[32];
                             tmem_ld32(scores + j, s);
                             if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
+                            const Two less(-most, -most);
+                            float x[32], tops[4];
 #pragma unroll
-                            for (int e = 0; e < 32; e += 2) top = max3(top, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-                        }
-                        const float next = fmaxf(fmaxf(top * scale, most), kNoScore);
-                        scale_sums(exp2_fast(most - next));
-                        most = next;
-                    } else if (__any_sync(0xffffffffu, beyond > kGrowth)) {
-                        scale_sums(exp2_fast(-beyond));
-                        most += beyond;
-                    }
-                    beyond = 0.0f;
-                    const Two by(scale, scale);
-                    Two sum(total, 0.0f);
-#pragma unroll 1
-                    for (int j = 0; j < S::kPositions; j += 32) {
-                        uint32_t s[32];
-                        tmem_ld32(scores + j, s);
-                        if constexpr (kMasked) hide(s, position + j, limit, have >> (j / kGranule));
-                        const Two less(-most, -most);
-                        float x[32], tops[4];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            fma(Two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), by, less).get(x[e], x[e + 1]);
-                            tops[e / 2 % 4] = e < 8 ? fmaxf(x[e], x[e + 1]) : max3(tops[e / 2 % 4], x[e], x[e + 1]);
-                        }
-                        float top = max3(max3(tops[0], tops[1], tops[2]), tops[3], beyond);
-                        if (__any_sync(0xffffffffu, top > kRoom)) {
-                            // too far beyond the maximum for 16 bits: what there is of the row is scaled at once, this tile's weights so far among it
-                            tmem_st_wait();   // weights and sums that this tile has stored are about to be loaded
-                            const float factor = exp2_fast(-top);
-                            float a, b;
-                            sum.get(a, b);
-                            total = a + b;
-                            scale_sums(factor);
-                            sum = Two(total, 0.0f);
-                            most += top;
-#pragma unroll 1
-                            for (int k = 0; k < j / 2; k += 8) {
-                                uint32_t w[8];
-                                tmem_ld8(weights + k, w);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    w[e] = to_16x2<kHalf>(to_float<kHalf>(static_cast<uint16_t>(w[e])) * factor, to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) * factor);
-                                tmem_st8(weights + k, w);
+                            for (int e = 0; e < 32; e += 2) {
+                                fma(Two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), by, less).get(x[e], x[e + 1]);
+                                tops[e / 2 % 4] = e < 8 ? fmaxf(x[e], x[e + 1]) : max3(tops[e / 2 % 4], x[e], x[e + 1]);
                             }
+                            float top = max3(max3(tops[0], tops[1], tops[2]), tops[3], beyond);
+                            if (__any_sync(0xffffffffu, top > kRoom)) {
+                                // too far beyond the maximum for 16 bits: what there is of the row is scaled at once, this tile's weights so far among it
+                                tmem_st_wait();   // weights and sums that this tile has stored are about to be loaded
+                                const float factor = exp2_fast(-top);
+                                float a, b;
+                                sum.get(a, b);
+                                total = a + b;
+                                scale_sums(factor);
+                                sum = Two(total, 0.0f);
+                                most += top;
+#pragma unroll 1
+                                for (int k = 0; k < j / 2; k += 8) {
+                                    uint32_t w[8];
+                                    if constexpr (kTwo) {
+                                        const uint32_t at = scores + (k & ~15) + k;   // 32 columns for 16
+                                        uint32_t rest[8];
+                                        tmem_ld8(at, w);
+                                        tmem_ld8(at + 16, rest);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] -= top;
-                            top = 0.0f;
-                        }
-                        beyond = top;
-                        uint32_t w[16];
+                                        for (int e = 0; e < 8; ++e)
+                                            split<kHalf>((to_float<kHalf>(static_cast<uint16_t>(w[e])) + to_float<kHalf>(static_cast<uint16_t>(rest[e]))) * factor,
+                                                         (to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) + to_float<kHalf>(static_cast<uint16_t>(rest[e] >> 16))) * factor, w[e], rest[e]);
+                                        tmem_st8(at, w);
+                                        tmem_st8(at + 16, rest);
+                                    } else {
+                                        tmem_ld8(weights + k, w);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const float a = exp2_fast(x[e]), b = exp2_fast(x[e + 1]);
-                            sum = add(sum, Two(a, b));
-                            w[e / 2] = to_16x2<kHalf>(a, b);
+                                        for (int e = 0; e < 8; ++e)
+                                            w[e] = to_16x2<kHalf>(to_float<kHalf>(static_cast<uint16_t>(w[e])) * factor, to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) * factor);
+                                        tmem_st8(weights + k, w);
+                                    }
+                                }
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) x[e] -= top;
+                                top = 0.0f;
+                            }
+                            beyond = top;
+                            uint32_t w[16];
+                            if constexpr (kTwo) {
+                                uint32_t rest[16];
+#pragma unroll
+                                for (int e = 0; e < 32; e += 2) {
+                                    const float a = exp2_fast(x[e]), b = exp2_fast(x[e + 1]);
+                                    sum = add(sum, Two(a, b));
+                                    split<kHalf>(a, b, w[e / 2], rest[e / 2]);
+                                }
+                                tmem_st16(scores + j, w);
+                                tmem_st16(scores + j + 16, rest);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 32; e += 2) {
+                                    const float a = exp2_fast(x[e]), b = exp2_fast(x[e + 1]);
+                                    sum = add(sum, Two(a, b));
+                                    w[e / 2] = to_16x2<kHalf>(a, b);
+                                }
+                                tmem_st16(weights + j / 2, w);   // the scores there have been read
+                            }
                         }
-                        tmem_st16(weights + j / 2, w);   // the scores there have been read
+                        float a, b;
+                        sum.get(a, b);
+                        total = a + b;
+                        tmem_st_wait();
+                    };
+                    if (!idle) {
+                        if (masked) weigh(std::true_type{});
+                        else weigh(std::false_type{});
                     }
-                    float a, b;
-                    sum.get(a, b);
-                    total = a + b;
-                    tmem_st_wait();
-                };
-                if (!idle) {
-                    if (masked) weigh(std::true_type{});
-                    else weigh(std::false_type{});
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(weights_full(slot));
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(weights_full(slot));
-            }
+            };
+            if (rows_all > kWholeRows) weigh_tiles(std::false_type{});
+            else weigh_tiles(std::true_type{});
             tiles_before += steps;
             if (!ok) break;
             if (mine_of > 0) {
@@ -829,24 +876,26 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
             const int steps = walk.template steps<S::kPositions>(p.group);
             if (steps == 0) continue;
             const Events<S::kSlots> events(steps, walk.rows_all(p.group) - walk.tile * S::kRows > kSlotRows);
+            const bool in_two = walk.rows_all(p.group) <= kWholeRows;
             ok = bar_wait_warp(queries_full, pieces & 1, gave_up);
             // each slot's next product, as soon as what it takes is there: the scores of event at[], or, if they have been asked for, the sums of it
             int at[2] = {0, 1};
             bool asked[2] = {false, false};
             const int used_by = events.shared ? 2 : 1;
-            const auto turn = [&](auto slot_c) {
+            const auto turn = [&](auto slot_c, auto two_c) {
                 constexpr int kSlot = decltype(slot_c)::value;
+                constexpr bool kTwo = decltype(two_c)::value;
                 const int e = at[kSlot];
                 if (e >= events.count) return;
                 const uint32_t tile = tiles_before + events.tile(e), place = tile & 1;
                 if (!asked[kSlot]) {
                     // keys; the scores' place, if the weights of the slot's product before have it, when that has been made
                     if (!bar_test_warp(keys_full(place), tile >> 1 & 1)) return;
-                    if (!S::kApart && summed[kSlot] > 0 && !bar_test_warp(weights_empty(kSlot), (summed[kSlot] - 1) & 1)) return;
+                    if ((!S::kApart || kTwo) && summed[kSlot] > 0 && !bar_test_warp(weights_empty(kSlot), (summed[kSlot] - 1) & 1)) return;
                     tc_fence_after();
                     const bool last = ++keys_used[place] == used_by;
                     if (last) keys_used[place] = 0;
-                    with_flags(place, events.shared, [&](auto place_c, auto shared_c) {
+                    with_flags(place, !kTwo && events.shared, [&](auto place_c, auto shared_c) {
                         constexpr int kPlace = decltype(place_c)::value, kOwn = decltype(shared_c)::value ? kSlot : 0;
                         if (elect_one()) {
 #pragma unroll
@@ -870,8 +919,10 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                         if (elect_one()) {
 #pragma unroll
                             for (int k = 0; k < S::kPositions / 16; ++k)
-                                mma_f16_tmem(S::kFirstSums + kSlot * S::kSums, S::kFirstWeights + kSlot * S::kWeights + 8 * k, desc_low(smem_v + kPlace * S::kOperand + k * 2048, S::kPanel),
-                                             kSumsDesc, k > 0 || !begins);
+#pragma unroll
+                                for (int rest = 0; rest < (kTwo ? 2 : 1); ++rest)
+                                    mma_f16_tmem(S::kFirstSums + kSlot * S::kSums, kTwo ? kSlot * S::kScores + k / 2 * 32 + k % 2 * 8 + 16 * rest : S::kFirstWeights + kSlot * S::kWeights + 8 * k,
+                                                 desc_low(smem_v + kPlace * S::kOperand + k * 2048, S::kPanel), kSumsDesc, k > 0 || rest > 0 || !begins);
                             mma_commit(weights_empty(kSlot));
                             if (last) mma_commit(values_empty(kPlace));
                             if (ends) mma_commit(sums_full(kSlot));
@@ -884,18 +935,22 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                     tries = 0;
                 }
             };
-            while (ok && (at[0] < events.count || (S::kSlots > 1 && at[1] < events.count))) {
-                turn(std::integral_constant<int, 0>{});
-                if constexpr (S::kSlots > 1) turn(std::integral_constant<int, 1>{});
-                // no try waits: a second's worth of them
-                if (__any_sync(0xffffffffu, ++tries > (wait_limit() << 6 | 63) || *gave_up)) {
-                    if (lane == 0) {
-                        *gave_up = 1;
-                        atomicExch(&g_linear_status, 1);
+            const auto products = [&](auto two_c) {
+                while (ok && (at[0] < events.count || (S::kSlots > 1 && at[1] < events.count))) {
+                    turn(std::integral_constant<int, 0>{}, two_c);
+                    if constexpr (S::kSlots > 1) turn(std::integral_constant<int, 1>{}, two_c);
+                    // no try waits: a second's worth of them
+                    if (__any_sync(0xffffffffu, ++tries > (wait_limit() << 6 | 63) || *gave_up)) {
+                        if (lane == 0) {
+                            *gave_up = 1;
+                            atomicExch(&g_linear_status, 1);
+                        }
+                        ok = false;
                     }
-                    ok = false;
                 }
-            }
+            };
+            if (!in_two) products(std::false_type{});
+            else products(std::true_type{});
             tiles_before += steps;
             ++pieces;
         }
