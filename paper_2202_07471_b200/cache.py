@@ -12,7 +12,7 @@ The calls share three int32 tensors next to the cache, which are read on the dev
 Rows behind the last sequence (a batch padded to a fixed size) are left as they are.  Nothing that the tensors hold leads outside the cache: lengths are cut to what
 pages covers, starts to the rows there are, and a page that the cache does not have counts as not there.
 
-None of the calls is recorded by autograd, and inputs that require a gradient are refused where one would be recorded (grad mode on).
+None of the calls is recorded by autograd: inputs that require a gradient are refused where one would be recorded (grad mode on), and inputs that carry a forward-mode tangent.
 """
 from __future__ import annotations
 
@@ -21,6 +21,7 @@ import math
 from typing import Optional, Tuple, Union
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding, linear
 from .binding import _check, load_library
@@ -135,6 +136,8 @@ def _heads(t: torch.Tensor, rows: Optional[int], heads: int, dim: int, what: str
 def _no_graph(what: str, *inputs: Optional[torch.Tensor]) -> None:
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
         raise ValueError(f"{what} is not recorded by autograd: call it under torch.no_grad()")
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in inputs):
+        raise ValueError(f"{what} has no forward-mode derivative: its inputs must not carry a tangent")
 
 
 def _written(*tensors: Optional[torch.Tensor]) -> None:
@@ -211,7 +214,7 @@ def squant_cache_attention(q: torch.Tensor, cache: torch.Tensor, lens: torch.Ten
     heads is a multiple of the cache's kv heads; query head h reads kv head h // (heads / kv heads).  scale: of the products, 1 / sqrt(head dim) by default.
     most: the number of rows that no sequence has more of, where the caller knows it: it chooses the kernel, and with it the results' last places; without it, a step of
     many sequences takes the slower one, for prompts.  With `lse` returns
-    (out, logarithms of the sums of exponentials, fp32 [rows, heads]).  out: the tensor to write, like q; in a new one, rows behind the last sequence hold
+    (out, logarithms of the sums of exponentials, fp32 [rows, heads]).  out: the tensor to write, like q, which it must not overlap; in a new one, rows behind the last sequence hold
     anything.  A row that sees nothing is zeros, its lse -infinity.
 
     Weights are rounded to q's type for their product with the values in sequences of more than 128 rows times query heads of a kv head, and keep twice its bits elsewhere.

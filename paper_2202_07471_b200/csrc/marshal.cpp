@@ -446,6 +446,13 @@ bool heads_ok(const at::Tensor *t, int64_t heads, int64_t dim, at::ScalarType ty
     return t && t->dim() == 3 && t->size(1) == heads && t->size(2) == dim && t->stride(2) == 1 && t->scalar_type() == type && t->device() == d;
 }
 bool sixteen(at::ScalarType type) { return type == at::kBFloat16 || type == at::kHalf; }
+// Derivatives of the cache's inputs, which its calls have none of, backward or forward.
+bool wants_derivative(std::initializer_list<const at::Tensor *> inputs)
+{
+    for (const at::Tensor *t : inputs)
+        if (t && t->unsafeGetTensorImpl()->autograd_meta() && t->_fw_grad(0).defined()) return true;
+    return wants_graph(inputs);
+}
 void written(const at::Tensor &t)
 {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
@@ -461,7 +468,7 @@ PyObject *cache_write(PyObject *, PyObject *args)
         const at::Tensor *t[4], *k, *v;
         for (int i = 0; i < 4; ++i)
             if (!plain(po[i], t[i])) return none();
-        if (!plain(po[4], k) || !plain(po[5], v) || !k || !v || k->dim() != 3 || wants_graph({k, v})) return none();
+        if (!plain(po[4], k) || !plain(po[5], v) || !k || !v || k->dim() != 3 || wants_derivative({k, v})) return none();
         squant_cache_move_args a{};
         if (!cache_rows(t, device, k->size(0), a.rows) || !sixteen(k->scalar_type())) return none();
         const at::Device d = t[0]->device();
@@ -519,7 +526,7 @@ PyObject *cache_attention(PyObject *, PyObject *args)
         const at::Tensor *t[4], *q, *given;
         for (int i = 0; i < 4; ++i)
             if (!plain(po[i], t[i])) return none();
-        if (!plain(po[4], q) || !plain(po[5], given) || !q || q->dim() != 3 || wants_graph({q, given})) return none();
+        if (!plain(po[4], q) || !plain(po[5], given) || !q || q->dim() != 3 || wants_derivative({q, given})) return none();
         squant_cache_attention_args a{};
         if (!cache_rows(t, device, q->size(0), a.rows) || !sixteen(q->scalar_type()) || most < 0) return none();
         const at::Device d = t[0]->device();

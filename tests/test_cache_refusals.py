@@ -3,7 +3,9 @@ import ctypes
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
+import paper_2202_07471_b200 as sq
 from paper_2202_07471_b200 import cache
 from test_cache_host import attention, move
 
@@ -55,3 +57,16 @@ def test_rows_in_one_another_are_refused_where_their_distance_overflows():
         assert lib.squant_cache_attention_plan(ctypes.byref(attention(group=1, out_stride=stride, out_head_stride=head))) > 0
     for stride, head in ((128, 7 * 128 - 1), (255, 128), (130, 6 * 130 + 127), (256, 127), (0, 128)):
         assert lib.squant_cache_attention_plan(ctypes.byref(attention(group=1, out_stride=stride, out_head_stride=head))) == -2
+
+
+def test_tangents_are_refused():
+    """A forward-mode derivative would be lost without a word, whatever grad mode is."""
+    c, x, (lens, pages, starts) = torch.zeros((4, 2, 4, 18 * 64), dtype=torch.uint8), torch.zeros((5, 2, 64), dtype=torch.bfloat16), parts()
+    with forward_ad.dual_level(), torch.no_grad():
+        dual = forward_ad.make_dual(x, x)
+        for call in (lambda: sq.squant_cache_attention(dual, c, lens, pages, starts), lambda: sq.squant_cache_write(c, dual, x, lens, pages, starts),
+                     lambda: sq.squant_cache_write(c, x, dual, lens, pages, starts), lambda: sq.squant_cache_attention(x, c, lens, pages, starts, out=dual)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        with pytest.raises(ValueError, match="CUDA"):
+            sq.squant_cache_attention(x, c, lens, pages, starts)

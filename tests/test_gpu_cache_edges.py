@@ -3,6 +3,7 @@ import ctypes
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import paper_2202_07471_b200 as sq
 from cache_cases import Batch, attention, filled, gen, pack, stored
@@ -213,3 +214,19 @@ def test_a_step_s_precision_does_not_depend_on_the_other_sequences():
         errors.append(float(torch.linalg.norm(out.double() - want) / torch.linalg.norm(want)))
     rounded = float(torch.linalg.norm(want.to(BF16).double() - want) / torch.linalg.norm(want))
     assert plan(q, cache, batch, 0) == PROMPT and max(errors) <= 1.01 * rounded, (errors, rounded)
+
+
+def test_tangents_are_refused():
+    """By the native calls too; what a tangent has been taken off is an ordinary tensor again."""
+    batch = Batch([40, 17], [3, 1], 16)
+    cache = filled(batch, 2, 64, 3)
+    q, k = inputs(4, 8, 64, BF16, 4), inputs(4, 2, 64, BF16, 5)
+    want = sq.squant_cache_attention(q, cache, *batch.args)
+    with forward_ad.dual_level(), torch.no_grad():
+        dq, dk = forward_ad.make_dual(q, q), forward_ad.make_dual(k, k)
+        for call in (lambda: sq.squant_cache_attention(dq, cache, *batch.args), lambda: sq.squant_cache_write(cache, dk, k, *batch.args), lambda: sq.squant_cache_write(cache, k, dk, *batch.args),
+                     lambda: sq.squant_cache_attention(q, cache, *batch.args, out=dq), lambda: sq.squant_cache_read(cache, *batch.args, 4, k=k, v=dk)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        assert torch.equal(sq.squant_cache_attention(forward_ad.unpack_dual(dq).primal, cache, *batch.args), want)
+    assert torch.equal(sq.squant_cache_attention(dq, cache, *batch.args), want)
