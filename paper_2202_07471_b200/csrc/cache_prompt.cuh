@@ -12,7 +12,7 @@
 // 433 us instead of 513 and 351 instead of 432.
 //
 // m is the maximum of the row's first tile.  It is replaced when a later tile has reached 2^8 beyond it, before the next one: then O is scaled, between two products.  Within a
-// tile weights may be as large as their type holds with room to spare, so that a row's scores are read once.  Per 128 positions the tensor cores work 2,048 clocks for both slots, and
+// tile weights may be as large as 2^kRoom, so that a row's scores are read once.  Per 128 positions the tensor cores work 2,048 clocks for both slots, and
 // the exponentials take as long: one slot's products run while the other one's exponentials do.  A tile of up to 128 rows has its positions shared by the slots, every other tile
 // of scores each, and their sums are joined at the end.
 //
@@ -34,6 +34,9 @@ namespace sq {
 constexpr int kSlotRows = 128;           // the tensor memory's lanes
 constexpr int kPromptConverters = 4;     // warps
 constexpr int kWholeRows = 128;          // more than any sequence has that the host leaves to cache_step_kernel
+// Of a weight's exponent.  fp16 holds weights up to 2^16; in bf16 a sum of 2^30 of them times values of 2^80 is inside fp32 (with 64, which bf16 would hold, values from 2^50 on
+// were not, where scores grow).
+constexpr float kRoom = 14.0f;
 constexpr int kTilesAhead = 8;           // score tiles that are being copied, converted or weighed at the same time, at most
 
 template <int D>
@@ -402,7 +405,6 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
             const int limit = walk.limit(min(at, rows_all - 1), p.group), seen_least = walk.seen_least(p.group);
             const bool idle = at - lane >= rows_all;   // all rows of the warp
             float most = kNoScore, total = 0.0f, beyond = 0.0f;   // beyond: how far the tile before reached beyond the maximum
-            constexpr float kRoom = kHalf ? 14.0f : 64.0f;        // of a weight's exponent
             if (steps > 0) {
                 // a row's pieces by neighbouring lanes; with a negative scale the queries change their signs, so that larger scores are larger exponents
                 const int64_t offset = to.row * p.q_stride + to.head * p.q_head;
@@ -497,40 +499,28 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
                             }
                             float top = max3(max3(tops[0], tops[1], tops[2]), tops[3], beyond);
                             if (__any_sync(0xffffffffu, top > kRoom)) {
-                                // too far beyond the maximum for 16 bits: what there is of the row is scaled at once, this tile's weights so far among it
+                                // too far beyond the maximum: what there is of the row is scaled at once, this tile's weights so far among it, by a power of two, which
+                                // rounds none of them again
                                 tmem_st_wait();   // weights and sums that this tile has stored are about to be loaded
-                                const float factor = exp2_fast(-top);
+                                const float down = floorf(top), factor = exp2_fast(-down);   // the row's largest weight stays 1 at least
                                 float a, b;
                                 sum.get(a, b);
                                 total = a + b;
                                 scale_sums(factor);
                                 sum = Two(total, 0.0f);
-                                most += top;
+                                most += down;
 #pragma unroll 1
-                                for (int k = 0; k < j / 2; k += 8) {
+                                for (int k = 0; k < (kTwo ? j : j / 2); k += 8) {
                                     uint32_t w[8];
-                                    if constexpr (kTwo) {
-                                        const uint32_t at = scores + (k & ~15) + k;   // 32 columns for 16
-                                        uint32_t rest[8];
-                                        tmem_ld8(at, w);
-                                        tmem_ld8(at + 16, rest);
+                                    tmem_ld8((kTwo ? scores : weights) + k, w);
 #pragma unroll
-                                        for (int e = 0; e < 8; ++e)
-                                            split<kHalf>((to_float<kHalf>(static_cast<uint16_t>(w[e])) + to_float<kHalf>(static_cast<uint16_t>(rest[e]))) * factor,
-                                                         (to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) + to_float<kHalf>(static_cast<uint16_t>(rest[e] >> 16))) * factor, w[e], rest[e]);
-                                        tmem_st8(at, w);
-                                        tmem_st8(at + 16, rest);
-                                    } else {
-                                        tmem_ld8(weights + k, w);
-#pragma unroll
-                                        for (int e = 0; e < 8; ++e)
-                                            w[e] = to_16x2<kHalf>(to_float<kHalf>(static_cast<uint16_t>(w[e])) * factor, to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) * factor);
-                                        tmem_st8(weights + k, w);
-                                    }
+                                    for (int e = 0; e < 8; ++e)
+                                        w[e] = to_16x2<kHalf>(to_float<kHalf>(static_cast<uint16_t>(w[e])) * factor, to_float<kHalf>(static_cast<uint16_t>(w[e] >> 16)) * factor);
+                                    tmem_st8((kTwo ? scores : weights) + k, w);
                                 }
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) x[e] -= top;
-                                top = 0.0f;
+                                for (int e = 0; e < 32; ++e) x[e] -= down;
+                                top -= down;
                             }
                             beyond = top;
                             uint32_t w[16];

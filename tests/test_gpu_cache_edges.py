@@ -21,9 +21,9 @@ def plan(q, cache, batch, most):
     return cache_module._lib().squant_cache_attention_plan(ctypes.byref(a))
 
 
-def rising(batch, heads, dim, levels):
+def rising(batch, heads, dim, levels, v_scale=1.0):
     """A cache whose position p has the score levels[p], in powers of two, for a query of ones: keys of one magnitude, which the codes keep to 2^-5."""
-    v = torch.randn((batch.page_count, heads, batch.page_size // 16, 16, dim), generator=gen(2), device="cuda")
+    v = torch.randn((batch.page_count, heads, batch.page_size // 16, 16, dim), generator=gen(2), device="cuda") * v_scale
     k = torch.zeros_like(v)
     for b, n in enumerate(batch.lens_list):
         for p in range(n):
@@ -51,8 +51,8 @@ def test_scores_that_grow_several_times_in_one_tile(dim, dtype, news, jumps):
     assert plan(q, cache, batch, max(news)) == PROMPT
     scale = 0.6931471805599453
     out, lse = sq.squant_cache_attention(q, cache, *batch.args, most=max(news), lse=True, scale=scale)
-    # a weight is rounded once, and again whenever it is scaled: at most three times, once for each later 32 of 128 positions; with up to 128 rows to 2^-18 of itself (bf16)
-    check_attention(out, lse, q, batch, cache, scale, rounded_p=2.0 ** -8 if max(news) * group <= 128 else 4)
+    # a weight is rounded once: it is scaled by powers of two
+    check_attention(out, lse, q, batch, cache, scale, rounded_p=max(news) * group > 128)
     again, lse_again = sq.squant_cache_attention(q, cache, *batch.args, most=max(news), lse=True, scale=scale)
     assert torch.equal(out, again) and torch.equal(lse, lse_again)
     assert sq.squant_device_status() is None
@@ -230,3 +230,20 @@ def test_tangents_are_refused():
                 call()
         assert torch.equal(sq.squant_cache_attention(forward_ad.unpack_dual(dq).primal, cache, *batch.args), want)
     assert torch.equal(sq.squant_cache_attention(dq, cache, *batch.args), want)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("news,most", [(300, 0), (20, 0), (3, 3)])
+@pytest.mark.parametrize("jumps", [(0, 60), (60, 0), (3, 40, 20)])
+def test_large_values_where_scores_grow(dim, news, most, jumps):
+    """Values of 2^80: a weight that reaches far beyond the maximum that it is taken against must not carry its product with them out of fp32."""
+    batch = Batch([300], [news], 16, seed=5)
+    level, levels = 0.0, []
+    for i in range(-(-300 // 32)):
+        level += jumps[i % len(jumps)] if i >= 3 else 0
+        levels += [level] * 32
+    cache = rising(batch, 2, dim, levels, v_scale=2.0 ** 80)
+    q = (1 + 0.02 * torch.randn((news, 8, dim), generator=gen(7), device="cuda")).to(BF16)
+    out, lse = sq.squant_cache_attention(q, cache, *batch.args, most=most, lse=True, scale=0.6931471805599453)
+    assert out.isfinite().all()
+    check_attention(out, lse, q, batch, cache, 0.6931471805599453, rounded_p=news * 4 > 128)
