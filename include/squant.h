@@ -412,7 +412,7 @@ typedef struct squant_cache_attention_args {
     uint32_t dtype;          /* of q and out */
     int32_t group;           /* query heads of a kv head */
     int32_t most;            /* rows that no sequence has more of, for the choice of the kernel only; 0: not known */
-    float scale;             /* finite */
+    float scale;             /* finite, also over log 2 */
     const void *q;           /* [rows][kv_heads * group][head_dim] */
     int64_t q_stride, q_head_stride;
     void *out;               /* likewise; no overlap with q */

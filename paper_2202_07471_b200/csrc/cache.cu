@@ -144,6 +144,9 @@ int move(const squant_cache_move_args *args, bool write, void *cuda_stream)
 
 // ---- attention
 
+// For exponents of 2.
+float scale_log2(const squant_cache_attention_args &a) { return static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634); }
+
 int check(const squant_cache_attention_args *args)
 {
     if (!args) return SQUANT_ERR_NULL;
@@ -157,7 +160,7 @@ int check(const squant_cache_attention_args *args)
     if (std::min<int64_t>(static_cast<int64_t>(r.width) * r.page_size, 1ll << 30) * a.group >= (1ll << 37)) return SQUANT_ERR_SHAPE;
     if (bad_strides(a.q_stride, a.q_head_stride, heads, r.rows, r.head_dim, false) ||
         bad_strides(a.out_stride, a.out_head_stride, heads, r.rows, r.head_dim, true)) return SQUANT_ERR_SHAPE;
-    if (!std::isfinite(a.scale)) return SQUANT_ERR_MODE;
+    if (!std::isfinite(scale_log2(a))) return SQUANT_ERR_MODE;
     if (nothing(r)) return SQUANT_OK;
     if (!a.q || !a.out) return SQUANT_ERR_NULL;
     if (misaligned(a.q, 2) || misaligned(a.out, 2) || misaligned(a.lse, 4)) return SQUANT_ERR_ALIGN;
@@ -260,7 +263,7 @@ sq::AttendArgs attend_args(const squant_cache_attention_args &a, const StepPlan 
     p.group = a.group;
     p.q_vector = on_vectors(a.q, a.q_stride, a.q_head_stride);
     p.out_vector = on_vectors(a.out, a.out_stride, a.out_head_stride);
-    p.scale_log2 = static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634);
+    p.scale_log2 = scale_log2(a);
     p.tickets = static_cast<unsigned long long *>(a.workspace);
     p.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(a.workspace) + s.tickets);
     p.nonce = nonce();

@@ -386,7 +386,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
         const int quarter = warp & 3, slot = warp >> 2;
         const uint32_t mine = tmem + (static_cast<uint32_t>(32 * quarter) << 16);   // the warp's lanes of tensor memory
         const uint32_t scores = mine + slot * S::kScores, weights = mine + S::kFirstWeights + slot * S::kWeights, sums = mine + S::kFirstSums + slot * S::kSums;
-        const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);   // 0: no score is hidden by a product with infinity
+        const float scale = fmaxf(fabsf(p.scale_log2), 1.17549435e-38f);   // 0: no score is hidden by a product with infinity; scores of 2^126 make exponents of 1
         uint32_t tiles_before = 0, weighed = 0, summed = 0, pieces = 0, joins = 0;
         int counted = 0;   // tiles shared with other blocks that the block has counted for
         bool ok = true;

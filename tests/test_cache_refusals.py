@@ -59,6 +59,12 @@ def test_rows_in_one_another_are_refused_where_their_distance_overflows():
         assert lib.squant_cache_attention_plan(ctypes.byref(attention(group=1, out_stride=stride, out_head_stride=head))) == -2
 
 
+def test_scales_beyond_fp32_are_refused():
+    lib = cache._lib()
+    for scale, code in ((3e38, -4), (-3.4e38, -4), (2.3e38, 1), (0.0, 1), (-1e-45, 1)):
+        assert lib.squant_cache_attention_plan(ctypes.byref(attention(scale=scale))) == code
+
+
 def test_tangents_are_refused():
     """A forward-mode derivative would be lost without a word, whatever grad mode is."""
     c, x, (lens, pages, starts) = torch.zeros((4, 2, 4, 18 * 64), dtype=torch.uint8), torch.zeros((5, 2, 64), dtype=torch.bfloat16), parts()

@@ -247,3 +247,25 @@ def test_large_values_where_scores_grow(dim, news, most, jumps):
     out, lse = sq.squant_cache_attention(q, cache, *batch.args, most=most, lse=True, scale=0.6931471805599453)
     assert out.isfinite().all()
     check_attention(out, lse, q, batch, cache, 0.6931471805599453, rounded_p=news * 4 > 128)
+
+
+@pytest.mark.parametrize("news,most", [(100, 0), (20, 0), (1, 1)])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_every_finite_scale(dtype, news, most):
+    """0: every position counts the same; small ones of large scores are not taken for larger ones; one whose exponents' scale is beyond fp32 is refused."""
+    batch = Batch([200, 130], [news, news], 16)
+    cache = filled(batch, 2, 64, 5)
+    q = inputs(batch.rows, 8, 64, dtype, 3)
+    for scale in (0.0, -0.0, 1e-20, 1e-38, 1e-45):
+        out, lse = sq.squant_cache_attention(q, cache, *batch.args, most=most, lse=True, scale=scale)
+        check_attention(out, lse, q, batch, cache, scale, rounded_p=news * 4 > 128)
+    if dtype == BF16:
+        shape = (batch.page_count, 2, 1, 16, 64)
+        large = pack((torch.randn(shape, generator=gen(1), device="cuda") * 1e17).to(BF16), torch.randn(shape, generator=gen(2), device="cuda").to(BF16))
+        far = (q.float() * 1e17).to(BF16)
+        for scale in (1e-34, -1e-34, 1e-33):
+            out, lse = sq.squant_cache_attention(far, large, *batch.args, most=most, lse=True, scale=scale)
+            check_attention(out, lse, far, batch, large, scale, rounded_p=news * 4 > 128)
+    for scale in (3e38, -3.4e38):
+        with pytest.raises(sq.SquantError):
+            sq.squant_cache_attention(q, cache, *batch.args, most=most, scale=scale)
