@@ -174,8 +174,9 @@ int64_t most_rows(const squant_cache_attention_args &a)
     return a.most > 0 ? std::min<int64_t>(a.most, a.rows.rows) : a.rows.rows;
 }
 // cache_step_kernel reads the cache once for each of its tiles, cache_prompt_kernel once for 256 rows but at the cost of 128: the line is drawn at as many rows times heads (16
-// sequences of 3,000 to 8,000 positions, 8 kv heads; us for 32 and 64 rows, step and prompt: 64 channels 60 and 97, 114 and 114; 128 channels 120 and 186, 143 and 131; 256
-// channels 173 and 268, 229 and 220).  Tiles of 16 rows pay where two of 8 take more than one and a half times as long, which with 128 channels they do not: 16 rows' sums
+// sequences of 3,000 to 8,000 positions, 8 kv heads; us of step and prompt: 64 channels 97 and 112 for 64 rows, 112 and 109 for 80; 128 channels 131 and 136 for 40, 152 and 136
+// for 48; 256 channels 255 and 288 for 48, 308 and 277 for 56.  Sequences of 200 to 900: 30 and 34, 31 and 37; 35 and 42, 40 and 49; 69 and 66, 91 and 75).
+// Tiles of 16 rows pay where two of 8 take more than one and a half times as long, which with 128 channels they do not: 16 rows' sums
 // and a unit's scores do not fit in 128 registers (32 rows in tiles of 8 and of 16: 64 channels 77 and 60, 128 channels 120 and 120, 256 channels 238 and 175).
 constexpr int most_step_rows(int dim) { return dim == 64 ? 64 : dim == 128 ? 40 : 48; }
 static_assert(std::max({most_step_rows(64), most_step_rows(128), most_step_rows(256)}) <= sq::kWholeRows, "as exact in either kernel");
