@@ -9,7 +9,7 @@
 // Weights are rounded to 16 bits for the product.  In sequences of up to kWholeRows rows what that leaves of them goes through a second one, as in cache_step.cuh: such
 // sequences come to either kernel, by what the caller says of the others, and are as exact in both (drafted tokens 0.00166 off, which is all the output's own rounding, and 80
 // us; with one product 0.0020 and 75 us).  In longer ones 16 bits are all there is: prompts are 0.0021 off instead of 0.0016 in bf16 and 0.0003 instead of 0.0002 in fp16, in
-// 433 us instead of 513 and 351 instead of 432.
+// 434 us instead of 513 and 349 instead of 432.
 //
 // m is the maximum of the row's first tile.  It is replaced when a later tile has reached 2^8 beyond it, before the next one: then O is scaled, between two products.  Within a
 // tile weights may be as large as 2^kRoom, so that a row's scores are read once.  Per 128 positions the tensor cores work 2,048 clocks for both slots, and
@@ -441,7 +441,7 @@ cache_prompt_kernel(const __grid_constant__ AttendArgs p)
             }
             const int mine_of = events.of_slot(slot);
             // Weights of 32 positions take 16 columns, with what rounding leaves of them the place of their scores, which is 32.  Each way has a loop of its own, here and where the products are
-            // made, and this one comes first: a choice in the loop costs part of a prompt 7 % (376 us instead of 351), the other order 1 % (356).
+            // made, and this one comes first: a choice in the loop costs part of a prompt 7 % (376 us instead of 350), the other order 1 % (356).
             const auto weigh_tiles = [&](auto in_two_c) {
                 constexpr bool kTwo = decltype(in_two_c)::value;
                 for (int i = 0; i < mine_of; ++i, ++weighed) {
