@@ -403,7 +403,7 @@ int squant_cache_read(const squant_cache_move_args *args, void *cuda_stream);
  *   s_j = scale * q k_j,  out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = log sum_j exp(s_j)
  * A row that sees nothing gets zeros and lse -infinity.  Products are exact, sums and softmax fp32.  Weights keep twice the bits of q's type for the product with the values, but in
  * sequences of more than 128 rows times group, where they are rounded to q's type.  Which kernel a call takes changes the results of shorter sequences in their last places alone.
- * Results repeat to the bit.  Sums are those of numbers for values up to 2^80 in magnitude and scores inside fp32.
+ * Results repeat to the bit.  Sums stay inside fp32 for values up to 2^80 in magnitude, where scores do.
  * In fp16 the scales are rounded to fp16 before their products with the codes are.  That changes nothing for groups whose largest magnitude is between 2^-18 and 65,504.  Smaller
  * groups' values are off by 2^-22 at most.  Larger ones, which only bf16 holds, overflow: their values become infinities, and from 444,416 on zeros among them NaN.
  */
